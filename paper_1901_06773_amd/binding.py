@@ -25,6 +25,8 @@ PLAN_NONE, PLAN_NAIVE_ALL, PLAN_DYNAMIC = 0, 1, 2
 LOC_HOST, LOC_DEVICE = 0, 1
 F32, BF16 = 0, 1
 DEBUG_POISON = 1
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
+LABEL_NONE = -2 ** 31
 STATUS_NAMES = {0: "ACC_OK", -1: "ACC_EINVAL", -2: "ACC_EUNTRAINABLE", -3: "ACC_EPOOL",
                 -4: "ACC_EHOSTMEM", -5: "ACC_EHIP", -6: "ACC_ESTATE"}
 
@@ -162,6 +164,16 @@ _PROTOS = {
     "acc_op_gap_fwd": (_I, [_VP, _VP, _I, _I, _I, _I, _VP]),
     "acc_op_gap_bwd": (_I, [_VP, _VP, _I, _I, _I, _I, _I, _VP]),
     "acc_op_softmax_ce": (_I, [_VP] * 5 + [_I, _I, _I, _VP]),
+    "acc_op_gn_workspace": (_SZ, [_I] * 4),
+    "acc_op_gn_fwd": (_I, [_VP] * 7 + [_I] * 5 + [_F, _VP, _SZ, _I, _VP]),
+    "acc_op_gn_bwd": (_I, [_VP] * 12 + [_I] * 5 + [_VP, _SZ, _I, _VP]),
+    "acc_op_linear_ce_workspace": (_SZ, [_I] * 5),
+    "acc_op_linear_ce": (_I, [_VP] * 4 + [_I] + [_VP] * 5 + [_I] * 3 + [_VP, _SZ, _I, _VP]),
+    "acc_op_tensor_list_bytes": (_SZ, [C.POINTER(_SZ), _I]),
+    "acc_op_tensor_list": (_I, [C.POINTER(_VP), C.POINTER(_VP), C.POINTER(_SZ), C.POINTER(C.c_int32), _I, _VP, _SZ, _VP]),
+    "acc_op_grad_norm_workspace": (_SZ, []),
+    "acc_op_grad_norm": (_I, [_VP, _SZ, _VP, _VP, _SZ, _VP]),
+    "acc_op_grad_clip": (_I, [_VP, _SZ, _F, _VP, _VP, _SZ, _VP]),
 }
 for _name, (_res, _args) in _PROTOS.items():
     _fn = getattr(_lib, _name)
@@ -597,3 +609,147 @@ def op_softmax_ce(z, labels, loss_rows, loss, dz):
                                 n, classes, _dtype_of(z), _stream_ptr(torch))
     if rc != ACC_OK:
         raise AccError(rc, "acc_op_softmax_ce")
+
+
+def _fits(name, what, t, shape, dtype, device):
+    """Refuses a tensor that the library would read or write otherwise than the caller means."""
+    if t.shape != shape or t.dtype != dtype or t.get_device() != device or not t.is_contiguous():
+        raise AccError(ACC_EINVAL, f"{name}: {what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on the current device (cuda:{device}), "
+                                   f"got {t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
+
+
+def _space(name, ws, device):
+    if ws.get_device() != device or not ws.is_contiguous():
+        raise AccError(ACC_EINVAL, f"{name}: the workspace must be contiguous and on the current device (cuda:{device}), got {ws.device}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def op_gn_workspace(n, hw, c, groups) -> int:
+    return int(_lib.acc_op_gn_workspace(n, hw, c, groups))
+
+
+def op_gn_fwd(x, gamma, beta, res, y, mean, istd, groups, act, eps, ws):
+    """x, res (or None) and y [n, ..., c], gamma and beta [c], mean and istd [n, groups]; act: ACT_NONE, ACT_RELU, ACT_SILU."""
+    import torch
+    device, f32 = torch.cuda.current_device(), torch.float32
+    shape, dtype = x.shape, _dtype_of(x)
+    n, c = shape[0], shape[-1]
+    _fits("op_gn_fwd", "x", x, shape, x.dtype, device)
+    _fits("op_gn_fwd", "y", y, shape, x.dtype, device)
+    if res is not None:
+        _fits("op_gn_fwd", "res", res, shape, x.dtype, device)
+    for what, t, like in (("gamma", gamma, (c,)), ("beta", beta, (c,)), ("mean", mean, (n, groups)), ("istd", istd, (n, groups))):
+        _fits("op_gn_fwd", what, t, like, f32, device)
+    at, size = _space("op_gn_fwd", ws, device)
+    rc = _lib.acc_op_gn_fwd(x.data_ptr(), gamma.data_ptr(), beta.data_ptr(), _ptr(res), y.data_ptr(), mean.data_ptr(), istd.data_ptr(), n,
+                            x.numel() // max(n * c, 1), c, groups, act, eps, at, size, dtype, _stream_ptr(torch))
+    if rc != ACC_OK:
+        raise AccError(rc, _lib.acc_last_error(None).decode())
+
+
+def op_gn_bwd(x, dy, y, res, gamma, beta, mean, istd, dx, dgamma, dbeta, dres, groups, act, ws):
+    """Gradients of op_gn_fwd: dx, dgamma, dbeta and, if wanted, dres (may be dy).  y: the stored output (ACT_RELU, else None);
+    res: the residual of the forward pass (ACT_SILU, or None)."""
+    import torch
+    device, f32 = torch.cuda.current_device(), torch.float32
+    shape, dtype = x.shape, _dtype_of(x)
+    n, c = shape[0], shape[-1]
+    for what, t in (("x", x), ("dy", dy), ("dx", dx), ("y", y), ("res", res), ("dres", dres)):
+        if t is not None:
+            _fits("op_gn_bwd", what, t, shape, x.dtype, device)
+    for what, t, like in (("gamma", gamma, (c,)), ("beta", beta, (c,)), ("mean", mean, (n, groups)), ("istd", istd, (n, groups)),
+                          ("dgamma", dgamma, (c,)), ("dbeta", dbeta, (c,))):
+        _fits("op_gn_bwd", what, t, like, f32, device)
+    at, size = _space("op_gn_bwd", ws, device)
+    rc = _lib.acc_op_gn_bwd(x.data_ptr(), dy.data_ptr(), _ptr(y), _ptr(res), gamma.data_ptr(), beta.data_ptr(), mean.data_ptr(), istd.data_ptr(),
+                            dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), _ptr(dres), n, x.numel() // max(n * c, 1), c, groups, act, at, size, dtype,
+                            _stream_ptr(torch))
+    if rc != ACC_OK:
+        raise AccError(rc, _lib.acc_last_error(None).decode())
+
+
+def op_linear_ce_workspace(n, d, classes, gradients: bool, dtype: int = F32) -> int:
+    return int(_lib.acc_op_linear_ce_workspace(n, d, classes, 1 if gradients else 0, int(dtype)))
+
+
+def op_linear_ce(x, w, bias, labels, loss_rows, loss, dx, dw, db, ws, ignore=None):
+    """Softmax cross-entropy of the logits x w^T + bias, which are not kept.  x [n, d] and w [classes, d], bias [classes] fp32 or None, labels
+    int32 [n]; loss_rows [n], loss [1], dx like x, dw [classes, d] fp32, db [classes] fp32, each optional.  ignore: the label of rows that
+    do not count (None: every row counts)."""
+    import torch
+    device, f32 = torch.cuda.current_device(), torch.float32
+    dtype = _dtype_of(x)
+    n, d = x.shape
+    classes = w.shape[0]
+    for what, t, like, kind in (("x", x, (n, d), x.dtype), ("w", w, (classes, d), x.dtype), ("labels", labels, (n,), torch.int32),
+                                ("bias", bias, (classes,), f32), ("loss_rows", loss_rows, (n,), f32), ("loss", loss, (1,), f32),
+                                ("dx", dx, (n, d), x.dtype), ("dw", dw, (classes, d), f32), ("db", db, (classes,), f32)):
+        if t is not None:
+            _fits("op_linear_ce", what, t, like, kind, device)
+    at, size = _space("op_linear_ce", ws, device)
+    rc = _lib.acc_op_linear_ce(x.data_ptr(), w.data_ptr(), _ptr(bias), labels.data_ptr(), LABEL_NONE if ignore is None else int(ignore), _ptr(loss_rows),
+                               _ptr(loss), _ptr(dx), _ptr(dw), _ptr(db), n, d, classes, at, size, dtype, _stream_ptr(torch))
+    if rc != ACC_OK:
+        raise AccError(rc, _lib.acc_last_error(None).decode())
+
+
+class TensorList:
+    """A list of fp32 / bf16 tensors laid out on their device for op_grad_norm() and op_grad_clip(); written on the current stream.  outs: where
+    the clipped tensors go (None: in place).  Keeps the tensors alive; their values may change, not their storage."""
+
+    def __init__(self, tensors, outs=None):
+        import torch
+        tensors = list(tensors)
+        outs = None if outs is None else list(outs)
+        n = len(tensors)
+        self.device = torch.cuda.current_device()
+        if n == 0 or (outs is not None and len(outs) != n):
+            raise AccError(ACC_EINVAL, "TensorList: no tensors, or another number of outputs")
+        for i, t in enumerate(tensors):
+            _fits("TensorList", f"tensor {i}", t, t.shape, t.dtype, self.device)
+            if outs is not None:
+                _fits("TensorList", f"output {i}", outs[i], t.shape, t.dtype, self.device)
+        self.tensors, self.outs = tensors, outs
+        counts = (_SZ * n)(*[t.numel() for t in tensors])
+        dtypes = (C.c_int32 * n)(*[_dtype_of(t) for t in tensors])
+        src = (_VP * n)(*[t.data_ptr() for t in tensors])
+        dst = None if outs is None else (_VP * n)(*[t.data_ptr() for t in outs])
+        size = int(_lib.acc_op_tensor_list_bytes(counts, n))
+        self.table = torch.empty(max(size, 16), dtype=torch.uint8, device=f"cuda:{self.device}")
+        rc = _lib.acc_op_tensor_list(src, dst, counts, dtypes, n, self.table.data_ptr(), size, _stream_ptr(torch))
+        if rc != ACC_OK:
+            raise AccError(rc, _lib.acc_last_error(None).decode())
+        self._at, self._size = self.table.data_ptr(), size
+
+
+def op_grad_norm_workspace() -> int:
+    return int(_lib.acc_op_grad_norm_workspace())
+
+
+def _norm_call(name, tensors, norm, ws):
+    import torch
+    device = torch.cuda.current_device()
+    if tensors.device != device:
+        raise AccError(ACC_EINVAL, f"{name}: the list lies on cuda:{tensors.device}, the current device is cuda:{device}")
+    _fits(name, "norm", norm, (1,), torch.float32, device)
+    return _space(name, ws, device), _stream_ptr(torch)
+
+
+def op_grad_norm(tensors: TensorList, norm, ws):
+    """norm [1] fp32: the Euclidean norm over all values of the list."""
+    (at, size), stream = _norm_call("op_grad_norm", tensors, norm, ws)
+    rc = _lib.acc_op_grad_norm(tensors._at, tensors._size, norm.data_ptr(), at, size, stream)
+    if rc != ACC_OK:
+        raise AccError(rc, _lib.acc_last_error(None).decode())
+
+
+def op_grad_clip(tensors: TensorList, max_norm, norm, ws):
+    """The list's tensors (or their outputs) scaled so that the norm over all of them is max_norm at most; norm [1]: what it was."""
+    (at, size), stream = _norm_call("op_grad_clip", tensors, norm, ws)
+    rc = _lib.acc_op_grad_clip(tensors._at, tensors._size, max_norm, norm.data_ptr(), at, size, stream)
+    if rc != ACC_OK:
+        raise AccError(rc, _lib.acc_last_error(None).decode())

@@ -223,6 +223,17 @@ hipError_t bn_backward(const void* x, const void* dy, const void* y, const float
                        void* g_out, long rows, int c, void* workspace, int dtype, hipStream_t st,
                        const BnSums* ready_sums = nullptr, bool in_iteration = false);
 
+// Group norm over images of hw x c, act: 0 none, 1 ReLU, 2 SiLU (gn.hip).  x, res, y, dy, dx, dres: dtype; the rest fp32.
+// y: the stored output (ReLU), res: the residual that was added (SiLU; may be null).
+constexpr int kGnMaxSlabs = 256;         // cuts of an image's rows
+size_t gn_workspace_bytes(int n, int hw, int c, int groups);
+hipError_t gn_forward(const void* x, const float* gamma, const float* beta, const void* res, void* y, float* mean, float* istd,
+                      int n, int hw, int c, int groups, int act, float eps, void* workspace, size_t workspace_bytes, int dtype,
+                      hipStream_t st);
+hipError_t gn_backward(const void* x, const void* dy, const void* y, const void* res, const float* gamma, const float* beta,
+                       const float* mean, const float* istd, void* dx, float* dgamma, float* dbeta, void* dres, int n, int hw,
+                       int c, int groups, int act, void* workspace, size_t workspace_bytes, int dtype, hipStream_t st);
+
 hipError_t maxpool_forward(const void* x, void* y, int n, int h, int wd, int c, int r, int s,
                            int stride, int pad, int dtype, hipStream_t st);
 hipError_t maxpool_backward(const void* x, const void* dy, void* dx, int n, int h, int wd, int c,
@@ -249,6 +260,19 @@ hipError_t softmax_ce_forward(const void* z, const int32_t* labels, float* loss_
                               int n, int classes, int dtype, hipStream_t st);
 hipError_t softmax_ce_backward(const void* z, const int32_t* labels, void* dz, int n, int classes,
                                int dtype, hipStream_t st);
+// Softmax cross-entropy of z = x w^T + bias without keeping z (linear_ce.hip); loss_rows, loss, dx, dw, db may each be null.
+size_t linear_ce_workspace_bytes(int n, int d, int classes, int gradients, int dtype);
+hipError_t linear_ce(const void* x, const void* w, const float* bias, const int32_t* labels, int ignore, float* loss_rows,
+                     float* loss, void* dx, float* dw, float* db, int n, int d, int classes, void* workspace,
+                     size_t workspace_bytes, int dtype, hipStream_t st);
+// A list of tensors in device memory, cut into pieces, and the norm over all of them (grad_clip.hip).  dst may be null (in place).
+constexpr int kPieceValues = 16384;
+size_t tensor_list_bytes(const size_t* counts, int n);
+hipError_t tensor_list(const void* const* src, void* const* dst, const size_t* counts, const int32_t* dtypes, int n, void* list,
+                       hipStream_t st);
+size_t grad_norm_workspace_bytes();
+hipError_t grad_norm(const void* list, size_t list_bytes, float* norm, void* workspace, hipStream_t st);
+hipError_t grad_clip(const void* list, size_t list_bytes, float bound, float* norm, void* workspace, hipStream_t st);
 // w <- w - lr * g (fp32); w_bf16 (may be null): rounded copy of the updated weights
 hipError_t sgd_update(float* w, const float* g, float lr, size_t count, void* w_bf16, hipStream_t st);
 hipError_t fill_zero(float* p, size_t count, hipStream_t st);

@@ -2,8 +2,12 @@
 // launchers, for per-layer parity tests and roofline measurements.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <initializer_list>
+#include <new>
+#include <vector>
 
 #include "../../include/accudnn.h"
 #include "kernels.h"
@@ -199,4 +203,104 @@ extern "C" int acc_op_softmax_ce(const void* z, const int32_t* labels, float* lo
   if (!z || !labels || !dtype_ok(dtype) || n <= 0 || classes <= 0 || (!loss_rows && !dz) || (loss_rows && !loss))
     return ACC_EINVAL;
   return status(softmax_ce(z, labels, loss_rows, loss, dz, n, classes, dtype, (hipStream_t)stream));
+}
+
+// The text of a refusal for acc_last_error(NULL).
+static int refuse(const char* text) {
+  set_thread_error(text);
+  return ACC_EINVAL;
+}
+static int told(hipError_t e, const char* text) {
+  if (e == hipSuccess) return ACC_OK;
+  set_thread_error(e == hipErrorInvalidValue ? text : hipGetErrorString(e));
+  return status(e);
+}
+
+extern "C" size_t acc_op_gn_workspace(int n, int hw, int c, int groups) { return al256(gn_workspace_bytes(n, hw, c, groups)); }
+
+extern "C" int acc_op_gn_fwd(const void* x, const float* gamma, const float* beta, const void* res, void* y, float* mean, float* istd, int n, int hw,
+                             int c, int groups, int act, float eps, void* workspace, size_t workspace_bytes, int dtype, void* stream) {
+  if (!dtype_ok(dtype)) return refuse("acc_op_gn_fwd: dtype must be ACC_F32 or ACC_BF16");
+  if (!al16({x, gamma, beta, res, y, mean, istd, workspace})) return refuse("acc_op_gn_fwd: pointers must be 16-byte aligned");
+  return told(gn_forward(x, gamma, beta, res, y, mean, istd, n, hw, c, groups, act, eps, workspace, workspace_bytes, dtype, (hipStream_t)stream),
+              "acc_op_gn_fwd: null pointer, sizes that are not positive or too large, groups that do not divide c, unknown act, eps < 0 or a workspace "
+              "smaller than acc_op_gn_workspace()");
+}
+
+extern "C" int acc_op_gn_bwd(const void* x, const void* dy, const void* y, const void* res, const float* gamma, const float* beta, const float* mean,
+                             const float* istd, void* dx, float* dgamma, float* dbeta, void* dres, int n, int hw, int c, int groups, int act,
+                             void* workspace, size_t workspace_bytes, int dtype, void* stream) {
+  if (!dtype_ok(dtype)) return refuse("acc_op_gn_bwd: dtype must be ACC_F32 or ACC_BF16");
+  if (!al16({x, dy, y, res, gamma, beta, mean, istd, dx, dgamma, dbeta, dres, workspace})) return refuse("acc_op_gn_bwd: pointers must be 16-byte aligned");
+  return told(gn_backward(x, dy, y, res, gamma, beta, mean, istd, dx, dgamma, dbeta, dres, n, hw, c, groups, act, workspace, workspace_bytes, dtype,
+                          (hipStream_t)stream),
+              "acc_op_gn_bwd: null pointer (y is needed with ACC_ACT_RELU), sizes that are not positive or too large, groups that do not divide c, "
+              "unknown act or a workspace smaller than acc_op_gn_workspace()");
+}
+
+extern "C" size_t acc_op_linear_ce_workspace(int n, int d, int classes, int gradients, int dtype) {
+  return linear_ce_workspace_bytes(n, d, classes, gradients, dtype);
+}
+
+extern "C" int acc_op_linear_ce(const void* x, const void* w, const float* bias, const int32_t* labels, int ignore, float* loss_rows, float* loss,
+                                void* dx, float* dw, float* db, int n, int d, int classes, void* workspace, size_t workspace_bytes, int dtype,
+                                void* stream) {
+  if (!dtype_ok(dtype)) return refuse("acc_op_linear_ce: dtype must be ACC_F32 or ACC_BF16");
+  if (!al16({x, w, bias, labels, loss_rows, loss, dx, dw, db, workspace})) return refuse("acc_op_linear_ce: pointers must be 16-byte aligned");
+  return told(linear_ce(x, w, bias, labels, ignore, loss_rows, loss, dx, dw, db, n, d, classes, workspace, workspace_bytes, dtype, (hipStream_t)stream),
+              "acc_op_linear_ce: null pointer, no result asked for, sizes that are not positive or too large, or a workspace smaller than "
+              "acc_op_linear_ce_workspace()");
+}
+
+extern "C" size_t acc_op_tensor_list_bytes(const size_t* counts, int n) {
+  if (!counts || n <= 0) return 0;
+  const size_t b = tensor_list_bytes(counts, n);
+  return b ? al256(b) : 0;
+}
+
+extern "C" int acc_op_tensor_list(const void* const* src, void* const* dst, const size_t* counts, const int32_t* dtypes, int n, void* list,
+                                  size_t list_bytes, void* stream) {
+  if (!src || !counts || !dtypes || n <= 0 || !list) return refuse("acc_op_tensor_list: null pointer or no tensors");
+  if (!al16({list})) return refuse("acc_op_tensor_list: the list must be 16-byte aligned");
+  const size_t need = acc_op_tensor_list_bytes(counts, n);
+  if (!need || list_bytes < need) return refuse("acc_op_tensor_list: the list is smaller than acc_op_tensor_list_bytes(), or too long");
+  try {
+    // what is written must not overlap what another tensor of the list reads or writes: pieces run at once
+    struct Span { uintptr_t lo, hi; int tensor; bool written; };
+    std::vector<Span> spans;
+    spans.reserve(2 * (size_t)n);
+    for (int i = 0; i < n; ++i) {
+      if (!dtype_ok(dtypes[i])) return refuse("acc_op_tensor_list: dtypes must be ACC_F32 or ACC_BF16");
+      if (!counts[i]) continue;
+      const uintptr_t es = dt_size(dtypes[i]), from = (uintptr_t)src[i], to = dst ? (uintptr_t)dst[i] : from;
+      if (!from || !to || from % es || to % es) return refuse("acc_op_tensor_list: null or misaligned tensor");
+      spans.push_back(Span{to, to + counts[i] * es, i, true});
+      if (from != to) spans.push_back(Span{from, from + counts[i] * es, i, false});
+    }
+    std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.lo < b.lo; });
+    uintptr_t end = 0, end_written = 0;              // the furthest end so far, of all and of what is written
+    for (const Span& s : spans) {
+      if (s.written ? s.lo < end : s.lo < end_written) return refuse("acc_op_tensor_list: tensors overlap (or the same one is listed twice)");
+      end = std::max(end, s.hi);
+      if (s.written) end_written = std::max(end_written, s.hi);
+    }
+  } catch (const std::bad_alloc&) {
+    set_thread_error("acc_op_tensor_list: out of host memory");
+    return ACC_EHOSTMEM;
+  }
+  return told(tensor_list(src, dst, counts, dtypes, n, list, (hipStream_t)stream), "acc_op_tensor_list: too long");
+}
+
+extern "C" size_t acc_op_grad_norm_workspace(void) { return grad_norm_workspace_bytes(); }
+
+extern "C" int acc_op_grad_norm(const void* list, size_t list_bytes, float* norm, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!al16({list, norm, workspace})) return refuse("acc_op_grad_norm: pointers must be 16-byte aligned");
+  if (workspace_bytes < grad_norm_workspace_bytes()) return refuse("acc_op_grad_norm: workspace smaller than acc_op_grad_norm_workspace()");
+  return told(grad_norm(list, list_bytes, norm, workspace, (hipStream_t)stream), "acc_op_grad_norm: null pointer or no list");
+}
+
+extern "C" int acc_op_grad_clip(const void* list, size_t list_bytes, float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!al16({list, norm, workspace})) return refuse("acc_op_grad_clip: pointers must be 16-byte aligned");
+  if (workspace_bytes < grad_norm_workspace_bytes()) return refuse("acc_op_grad_clip: workspace smaller than acc_op_grad_norm_workspace()");
+  return told(grad_clip(list, list_bytes, max_norm, norm, workspace, (hipStream_t)stream), "acc_op_grad_clip: null pointer, no list, or max_norm negative or no number");
 }

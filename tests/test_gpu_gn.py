@@ -1,0 +1,250 @@
+"""Group norm with an activation against its formulas in 64 bits.
+
+Tolerances.  u = 2^-24 is a rounding of fp32, h that of the stored type (bf16 2^-8).  A mean or a sum of fp32 values added up in chains of at most
+a few dozen and then in pairs is off by less than 64 u of the mean of the magnitudes; the values that are multiplied and added to one result
+carry less than 32 roundings each (an exponential counts four).  So a result is within h of itself and 256 u of the magnitudes that go into it."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+DT = {"f32": (torch.float32, 2.0 ** -24), "bf16": (torch.bfloat16, 2.0 ** -8)}
+EPS = 1e-5
+
+
+def B():
+    from paper_1901_06773_amd import binding
+    return binding
+
+
+def randn(seed, *shape):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.randn(*shape, generator=g, device="cuda")
+
+
+def groups_of(t, groups):                       # [n, ..., c] -> [n, hw, groups, per]
+    return t.double().reshape(t.shape[0], -1, groups, t.shape[-1] // groups)
+
+
+def mean_of(t):
+    return t.mean((1, 3), keepdim=True)
+
+
+def forward(x, gamma, beta, res, groups, act, eps=EPS, ws=None):
+    n, c = x.shape[0], x.shape[-1]
+    y, mean, istd = torch.full_like(x, float("nan")), torch.empty(n, groups, device="cuda"), torch.empty(n, groups, device="cuda")
+    hw = x.numel() // (n * c)
+    ws = torch.empty(B().op_gn_workspace(n, hw, c, groups), dtype=torch.uint8, device="cuda") if ws is None else ws
+    B().op_gn_fwd(x, gamma, beta, res, y, mean, istd, groups, act, eps, ws)
+    return y, mean, istd
+
+
+def backward(x, dy, y, res, gamma, beta, mean, istd, groups, act, want_res, dres=None):
+    n, c = x.shape[0], x.shape[-1]
+    dx, dg, db = torch.full_like(x, float("nan")), torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+    dres = dres if dres is not None else torch.full_like(x, float("nan")) if want_res else None
+    ws = torch.empty(B().op_gn_workspace(n, x.numel() // (n * c), c, groups), dtype=torch.uint8, device="cuda")
+    B().op_gn_bwd(x, dy, y, res, gamma, beta, mean, istd, dx, dg, db, dres, groups, act, ws)
+    return dx, dg, db, dres
+
+
+def sizes():
+    return [(1, 1, 1, 1, 1), (1, 1, 1, 8, 2), (2, 1, 1, 512, 32), (3, 7, 7, 64, 32), (2, 5, 3, 30, 3), (2, 3, 3, 7, 7), (1, 13, 11, 120, 8), (2, 56, 56, 64, 32),
+            (1, 9, 40, 2056, 8), (3, 2, 2, 4, 1), (300, 3, 3, 16, 4), (1, 112, 112, 8, 1), (2, 33, 17, 96, 1), (5, 14, 14, 256, 256), (1, 1, 700, 24, 2),
+            (2, 28, 28, 512, 32), (4, 7, 7, 2048, 32), (7, 1, 2, 40, 5), (2, 19, 23, 36, 9), (1, 50, 50, 1028, 2), (2, 6, 6, 4104, 1), (1, 130, 127, 32, 16)]
+
+
+def check_forward(x, gamma, beta, res, groups, act, h, eps=EPS, rounding=U):
+    y, mean, istd = forward(x, gamma, beta, res, groups, act, eps)
+    v = groups_of(x, groups)
+    mu = mean_of(v)
+    var = mean_of((v - mu) ** 2)
+    ref_is = (var + eps) ** -0.5
+    size = mean_of(v.abs())
+    assert ((mean.double() - mu.flatten(1)).abs() <= 64 * U * size.flatten(1) + 1e-37).all()
+    # the deviation of the mean enters the variance squared, every deviation carries a rounding of the value
+    assert ((istd.double() / ref_is.flatten(1) - 1).abs() <= 64 * U * (1 + size.flatten(1) * istd.double())).all()
+    ga, be = gamma.double().view(groups, -1), beta.double().view(groups, -1)
+    xh = (v - mu) * ref_is
+    r = groups_of(res, groups) if res is not None else torch.zeros((), dtype=torch.float64, device="cuda")
+    z = xh * ga + be + r
+    ref = {0: z, 1: z.clamp(min=0), 2: z * torch.sigmoid(z)}[act]
+    scale = (xh.abs() + 1 + size * ref_is) * ga.abs() + be.abs() + r.abs()
+    assert ((groups_of(y, groups) - ref).abs() <= h * ref.abs() + 256 * U * scale).all()
+    return y, mean, istd
+
+
+def check_backward(x, dy, y, res, gamma, beta, mean, istd, groups, act, h, want_res):
+    dx, dg, db, dres = backward(x, dy, y if act == 1 else None, res if act == 2 else None, gamma, beta, mean, istd, groups, act, want_res)
+    per = (x.shape[0], 1, groups, 1)
+    v, mu, is_ = groups_of(x, groups), mean.double().view(per), istd.double().view(per)
+    ga, be = gamma.double().view(groups, -1), beta.double().view(groups, -1)
+    xh, g = (v - mu) * is_, groups_of(dy, groups)
+    if act == 1:
+        g = torch.where(groups_of(y, groups) > 0, g, 0.0)
+        g_scale = g.abs()
+    elif act == 2:
+        z = xh * ga + be + (groups_of(res, groups) if res is not None else 0.0)
+        s = torch.sigmoid(z)
+        # s and its slope by a z that is off by a few roundings of its terms
+        g_scale = g.abs() * (1 + (xh * ga).abs() + be.abs() + z.abs())
+        g = g * (s * (1 + z * (1 - s)))
+    else:
+        g_scale = g.abs()
+    a, a_scale = g * ga, g_scale * ga.abs()
+    ref = is_ * (a - mean_of(a) - xh * mean_of(a * xh))
+    scale = is_ * (a_scale + mean_of(a_scale) + xh.abs() * mean_of(a_scale * xh.abs()))
+    assert ((groups_of(dx, groups) - ref).abs() <= h * ref.abs() + 256 * U * scale).all()
+    c = x.shape[-1]
+    assert ((db.double() - g.sum((0, 1)).view(c)).abs() <= 256 * U * g_scale.sum((0, 1)).view(c) + 1e-37).all()
+    assert ((dg.double() - (g * xh).sum((0, 1)).view(c)).abs() <= 256 * U * (g_scale * xh.abs()).sum((0, 1)).view(c) + 1e-37).all()
+    if want_res:
+        assert ((groups_of(dres, groups) - g).abs() <= h * g.abs() + 64 * U * g_scale).all()
+
+
+@pytest.mark.parametrize("act,residual", [(0, False), (1, False), (1, True), (2, False), (2, True), (0, True)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,h,w,c,groups", sizes())
+def test_against_the_formulas(n, h, w, c, groups, dtype, act, residual):
+    td, hs = DT[dtype]
+    x = (randn(1, n, h, w, c) * (0.5 + 0.1 * randn(2, c).abs()) + randn(3, c)).to(td)
+    gamma, beta = 1 + 0.3 * randn(4, c), 0.3 * randn(5, c)
+    res = randn(6, n, h, w, c).to(td) if residual else None
+    y, mean, istd = check_forward(x, gamma, beta, res, groups, act, hs)
+    check_backward(x, randn(7, n, h, w, c).to(td), y, res, gamma, beta, mean, istd, groups, act, hs, residual)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_values_far_from_zero(dtype):
+    td, hs = DT[dtype]
+    x = (1000 + randn(1, 2, 20, 20, 64)).to(td)
+    check_forward(x, torch.ones(64, device="cuda"), torch.zeros(64, device="cuda"), None, 8, 0, hs)
+
+
+@pytest.mark.parametrize("c,groups,hw", [(64, 8, 50), (30, 3, 11), (64, 8, 9000)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_group_of_equal_values_gives_its_shift(c, groups, hw, dtype):
+    td, _ = DT[dtype]
+    x = torch.full((2, 1, hw, c), 0.4375, device="cuda").to(td)
+    beta = randn(1, c)
+    y, mean, istd = forward(x, 1 + randn(2, c), beta, None, groups, 0)
+    assert torch.equal(y, beta.to(td).expand_as(y)) and (mean == 0.4375).all()
+    assert ((istd.double() - EPS ** -0.5).abs() <= 4 * U * EPS ** -0.5).all()
+
+
+@pytest.mark.parametrize("act", [0, 1, 2])
+@pytest.mark.parametrize("hw", [40, 9000])
+def test_a_value_that_is_no_number_stays_in_its_group(hw, act):
+    x = randn(1, 3, 1, hw, 32)
+    x[1, 0, 7, 9] = float("nan")
+    x[2, 0, 3, 30] = float("inf")
+    y, mean, istd = forward(x, torch.ones(32, device="cuda"), torch.zeros(32, device="cuda"), None, 8, act)
+    bad = torch.zeros(3, 8, dtype=torch.bool, device="cuda")
+    bad[1, 2] = bad[2, 7] = True
+    assert torch.equal(torch.isnan(istd), bad)
+    assert torch.equal(torch.isnan(y).view(3, hw, 8, 4).all((1, 3)), bad) and torch.equal(torch.isnan(y).view(3, hw, 8, 4).any((1, 3)), bad)
+
+
+@pytest.mark.parametrize("n,hw,c,groups", [(2, 49, 512, 32), (1, 9000, 64, 8), (3, 30, 30, 3)])
+def test_the_residuals_gradient_in_place_of_the_upstream_one(n, hw, c, groups):
+    x, dy, res = (randn(k, n, 1, hw, c).bfloat16() for k in (1, 2, 3))
+    gamma, beta = randn(4, c), randn(5, c)
+    for act in (0, 1, 2):
+        y, mean, istd = forward(x, gamma, beta, res, groups, act)
+        apart = backward(x, dy, y, res, gamma, beta, mean, istd, groups, act, True)
+        over = dy.clone()
+        joint = backward(x, over, y, res, gamma, beta, mean, istd, groups, act, True, dres=over)
+        assert all(torch.equal(p, q) for p, q in zip(apart, joint))
+
+
+def test_differences():
+    """The gradients against central differences of the forward pass in 64 bits around the library's own."""
+    n, hw, c, groups = 2, 6, 12, 3
+    x, dy, res = (randn(k, n, 1, hw, c) for k in (1, 2, 3))
+    gamma, beta = 1 + 0.2 * randn(4, c), randn(5, c)
+    y, mean, istd = forward(x, gamma, beta, res, groups, 2)
+    dx, dg, db, dres = backward(x, dy, None, res, gamma, beta, mean, istd, groups, 2, True)
+
+    def loss(xv, gv, bv, rv):
+        v = xv.reshape(n, -1, groups, c // groups)
+        mu = mean_of(v)
+        z = ((v - mu) * (mean_of((v - mu) ** 2) + EPS) ** -0.5).reshape(x.shape) * gv + bv + rv
+        return float((z * torch.sigmoid(z) * dy.double()).sum())
+    at = [t.double() for t in (x, gamma, beta, res)]
+    step = 1e-5
+    for k, got in ((0, dx), (1, dg), (2, db), (3, dres)):
+        for i in range(0, got.numel(), max(1, got.numel() // 12)):
+            hi, lo = [t.clone() for t in at], [t.clone() for t in at]
+            hi[k].view(-1)[i] += step
+            lo[k].view(-1)[i] -= step
+            # third derivatives of order 100: the difference is off by 1e-8; the gradient by 1e-5 of the terms it is summed from
+            assert abs(float(got.view(-1)[i]) - (loss(*hi) - loss(*lo)) / (2 * step)) <= 2e-5 * (1 + abs(float(got.view(-1)[i])))
+
+
+@pytest.mark.parametrize("n,hw,c,groups", [(2, 49, 512, 32), (2, 9000, 64, 8), (3, 30, 30, 3)])
+def test_captured_replayed_and_on_another_stream(n, hw, c, groups):
+    x, dy = randn(1, n, 1, hw, c), randn(2, n, 1, hw, c)
+    gamma, beta = randn(3, c), randn(4, c)
+    ws = torch.empty(B().op_gn_workspace(n, hw, c, groups), dtype=torch.uint8, device="cuda")
+    y, mean, istd, dx, dg, db = (torch.empty_like(x), torch.empty(n, groups, device="cuda"), torch.empty(n, groups, device="cuda"), torch.empty_like(x),
+                                 torch.empty(c, device="cuda"), torch.empty(c, device="cuda"))
+
+    def both():
+        B().op_gn_fwd(x, gamma, beta, None, y, mean, istd, groups, 1, EPS, ws)
+        B().op_gn_bwd(x, dy, y, None, gamma, beta, mean, istd, dx, dg, db, None, groups, 1, ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for k in range(4):
+        x.copy_(randn(10 + k, n, 1, hw, c))
+        dy.copy_(randn(20 + k, n, 1, hw, c))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (y, mean, istd, dx, dg, db)]
+        both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, (y, mean, istd, dx, dg, db)))
+
+
+def test_offsets_beyond_32_bits():
+    """The last image of a tensor of 2.3e9 values has the bits that it has alone."""
+    n, hw, c, groups = 3, 12_000_000, 64, 32
+    x = torch.empty(n, 1, hw, c, dtype=torch.bfloat16, device="cuda")
+    x.normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+    gamma, beta = randn(2, c), randn(3, c)
+    # (as many images alone as together, so that an image's rows are cut alike)
+    y, mean, istd = forward(x, gamma, beta, None, groups, 1)
+    v = x[2].double().view(hw, groups, -1)
+    assert ((mean[2].double() - v.mean((0, 2))).abs() <= 1e-6).all()
+    assert ((istd[2].double() * (v.var((0, 2), unbiased=False) + EPS) ** 0.5 - 1).abs() <= 1e-6).all()
+    del v
+    z = ((x[2, 0, -1000:].double().view(1000, groups, -1) - mean[2].double().view(groups, 1)) * istd[2].double().view(groups, 1)).view(1000, c) * gamma.double() + beta.double()
+    assert ((y[2, 0, -1000:].double() - z.clamp(min=0)).abs() <= 2.0 ** -8 * z.abs() + 256 * U * 10).all()
+    dx, dg, db, _ = backward(x, y, y, None, gamma, beta, mean, istd, groups, 1, False)
+    assert torch.isfinite(dx[2, 0, -1000:].float()).all() and torch.isfinite(dg).all()
+    a = y[2].float().view(hw, c) * gamma
+    rows = ((x[2].float().view(hw, groups, -1) - mean[2].view(groups, 1)) * istd[2].view(groups, 1)).view(hw, c)
+    A = a.double().view(hw, groups, -1).mean((0, 2))
+    Bm = (a * rows).double().view(hw, groups, -1).mean((0, 2))
+    ref = (istd[2].double().view(groups, 1) * (a[-1000:].double().view(1000, groups, -1) - A.view(groups, 1) - rows[-1000:].double().view(1000, groups, -1) * Bm.view(groups, 1))).view(1000, c)
+    assert ((dx[2, 0, -1000:].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 1e-4).all()
+
+
+def test_tensors_that_do_not_fit_are_refused():
+    x = randn(1, 2, 4, 4, 16)
+    good = dict(x=x, gamma=randn(2, 16), beta=randn(3, 16), res=None, y=torch.empty_like(x), mean=torch.empty(2, 4, device="cuda"),
+                istd=torch.empty(2, 4, device="cuda"), groups=4, act=0, eps=EPS, ws=torch.empty(B().op_gn_workspace(2, 16, 16, 4), dtype=torch.uint8, device="cuda"))
+    for bad in (dict(x=x.transpose(1, 2)), dict(y=torch.empty(2, 4, 4, 8, device="cuda")), dict(y=torch.empty_like(x).bfloat16()), dict(gamma=torch.zeros(16)),
+                dict(beta=torch.zeros(8, device="cuda")), dict(mean=torch.empty(4, 2, device="cuda")), dict(res=x.cpu()), dict(ws=torch.empty(1 << 20, dtype=torch.uint8)),
+                dict(ws=torch.empty(16, dtype=torch.uint8, device="cuda")), dict(groups=3, mean=torch.empty(2, 3, device="cuda"), istd=torch.empty(2, 3, device="cuda"))):
+        with pytest.raises(B().AccError):
+            B().op_gn_fwd(*{**good, **bad}.values())
+    with pytest.raises(TypeError):
+        B().op_gn_fwd(*{**good, "x": x.half()}.values())
