@@ -11,6 +11,7 @@
 // fp32: products of the convolution kernels (a 1x1 convolution of n pixels), logits and dz of a piece in fp32.
 #include "kernels.h"
 #include "dtype.h"
+#include "linear_ce.h"
 
 #include <climits>
 
@@ -70,21 +71,6 @@ __global__ __launch_bounds__(THREADS) void row_sums_kernel(const float* __restri
   }
 }
 
-// Rows that count, as a factor: scale[0] = 1 / their number (0 if there is none).
-__global__ __launch_bounds__(1024) void count_kernel(const int32_t* __restrict__ labels, int n, int ignore, float* __restrict__ scale) {
-  __shared__ int sh[16];
-  int k = 0;
-  for (int i = threadIdx.x; i < n; i += 1024) k += ignore == INT_MIN || labels[i] != ignore ? 1 : 0;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) k += __shfl_xor(k, o);
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = k;
-  __syncthreads();
-  if (threadIdx.x) return;
-  int t = 0;
-  for (int w = 0; w < 16; ++w) t += sh[w];
-  scale[0] = t ? 1.f / (float)t : 0.f;
-}
-
 // One wave per row: the splits' m and R joined.
 __global__ __launch_bounds__(THREADS) void join_kernel(const float* __restrict__ part, const float* __restrict__ z_label, const int32_t* __restrict__ labels,
                                                        int ignore, float* __restrict__ row_max, float* __restrict__ row_rest, float* __restrict__ loss_rows,
@@ -113,19 +99,27 @@ __global__ __launch_bounds__(THREADS) void join_kernel(const float* __restrict__
   loss_rows[row] = skip ? 0.f : known ? log1pf(rest) - (z_label[row] - mx) : NAN;
 }
 
-// loss = scale * sum of the rows, in a fixed order
-__global__ __launch_bounds__(1024) void mean_kernel(const float* __restrict__ loss_rows, const float* __restrict__ scale, int n, float* __restrict__ loss) {
+// scale[0] = 1 / rows that count (0 if there is none), loss = scale * sum of the rows, in a fixed order
+__global__ __launch_bounds__(1024) void mean_kernel(const float* __restrict__ loss_rows, const int32_t* __restrict__ labels, int ignore, int n,
+                                                    float* __restrict__ scale, float* __restrict__ loss) {
   __shared__ double sh[16];
+  __shared__ int counts[16];
   double s = 0.0;
-  for (int i = threadIdx.x; i < n; i += 1024) s += (double)loss_rows[i];
+  int k = 0;
+  for (int i = threadIdx.x; i < n; i += 1024) {
+    s += (double)loss_rows[i];
+    k += ignore == INT_MIN || labels[i] != ignore ? 1 : 0;
+  }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
+  for (int o = 32; o > 0; o >>= 1) { s += __shfl_xor(s, o); k += __shfl_xor(k, o); }
+  if ((threadIdx.x & 63) == 0) { sh[threadIdx.x >> 6] = s; counts[threadIdx.x >> 6] = k; }
   __syncthreads();
   if (threadIdx.x) return;
   double t = 0.0;
-  for (int w = 0; w < 16; ++w) t += sh[w];
-  *loss = (float)(t * (double)scale[0]);
+  int rows = 0;
+  for (int w = 0; w < 16; ++w) { t += sh[w]; rows += counts[w]; }
+  scale[0] = rows ? 1.f / (float)rows : 0.f;
+  if (loss) *loss = rows ? (float)(t / (double)rows) : 0.f;
 }
 
 // z -> dz in place, columns beyond the classes zero, and the columns' sums over the rows of a workgroup: db_part[workgroup][pitch].
@@ -236,20 +230,6 @@ Plan32 plan32(int n, int d, int classes, bool grads, int dtype) {
   return p;
 }
 
-struct Args {
-  const void *x, *w;
-  const float* bias;
-  const int32_t* labels;
-  int ignore;
-  float *loss_rows, *loss;
-  void* dx;
-  float *dw, *db;
-  int n, d, classes;
-  char* ws;
-  int dtype;
-  hipStream_t st;
-};
-
 #define ACC_TRY(call) do { if (const hipError_t e_ = (call); e_ != hipSuccess) return e_; } while (0)
 
 // out[n][n_out] (+)= in[n][c] * w[n_out][c]^T
@@ -270,13 +250,11 @@ hipError_t widen(const void* in, int dtype, float* out, int rows_in, int cols_in
   return hipGetLastError();
 }
 
-hipError_t run32(const Args& a) {
+hipError_t run32(const LceArgs& a) {
   const bool grads = a.dx || a.dw || a.db;
   const Plan32 p = plan32(a.n, a.d, a.classes, grads, a.dtype);
-  float* const row_max = (float*)(a.ws + p.stats);
-  float *const row_rest = row_max + a.n, *const z_label = row_rest + a.n, *const rows_ws = z_label + a.n, *const scale = rows_ws + a.n;
+  const LceStats s = lce_stats(a, p.stats);
   float *const part = (float*)(a.ws + p.part), *const z = (float*)(a.ws + p.z);
-  float* const loss_rows = a.loss_rows ? a.loss_rows : rows_ws;
   const int dp = (int)p.dp;
   hipStream_t st = a.st;
   const float* x = (const float*)a.x;
@@ -284,7 +262,6 @@ hipError_t run32(const Args& a) {
     x = (const float*)(a.ws + p.x);
     ACC_TRY(widen(a.x, a.dtype, (float*)(a.ws + p.x), a.n, a.d, a.n, dp, st));
   }
-  hipLaunchKernelGGL(count_kernel, dim3(1), dim3(1024), 0, st, a.labels, a.n, a.ignore, scale);
   const size_t es = dt_size(a.dtype);
   // of the piece at hand
   long v0 = 0;
@@ -305,20 +282,17 @@ hipError_t run32(const Args& a) {
   const int splits_piece = (int)((p.piece + kSplitCols - 1) / kSplitCols);
   for (long k = 0; k < p.pieces; ++k) {
     ACC_TRY(logits(k));
-    hipLaunchKernelGGL(row_sums_kernel, dim3((unsigned)(a.n * splits_piece)), dim3(THREADS), 0, st, z, a.bias, a.labels, part, z_label, pitch, cols,
+    hipLaunchKernelGGL(row_sums_kernel, dim3((unsigned)(a.n * splits_piece)), dim3(THREADS), 0, st, z, a.bias, a.labels, part, s.z_label, pitch, cols,
                        (int)v0, kSplitCols, splits_piece, (int)(k * splits_piece), (int)p.splits);
   }
-  hipLaunchKernelGGL(join_kernel, dim3((a.n + THREADS / 64 - 1) / (THREADS / 64)), dim3(THREADS), 0, st, part, z_label, a.labels, a.ignore, row_max, row_rest,
-                     loss_rows, a.n, (int)p.splits, a.classes);
-  if (a.loss) hipLaunchKernelGGL(mean_kernel, dim3(1), dim3(1024), 0, st, loss_rows, scale, a.n, a.loss);
-  ACC_TRY(hipGetLastError());
+  ACC_TRY(lce_join(a, s, part, (int)p.splits));
   if (!grads) return hipSuccess;
   float* const dx = p.own_x ? (float*)(a.ws + p.dx) : (float*)a.dx;
   float* const db_part = (float*)(a.ws + p.db);
   for (long k = 0; k < p.pieces; ++k) {
     if (p.pieces > 1) ACC_TRY(logits(k));
     hipLaunchKernelGGL(dz_kernel, dim3((unsigned)((pitch / 4 + THREADS - 1) / THREADS), (unsigned)p.row_parts), dim3(THREADS), 0, st, z, a.bias, a.labels,
-                       a.ignore, row_max, row_rest, scale, db_part, a.n, pitch, cols, (int)v0);
+                       a.ignore, s.row_max, s.row_rest, s.scale, db_part, a.n, pitch, cols, (int)v0);
     if (a.db)
       hipLaunchKernelGGL(db_kernel, dim3((unsigned)((cols + THREADS - 1) / THREADS)), dim3(THREADS), 0, st, db_part, a.db + v0, (int)p.row_parts, pitch, cols);
     if (a.dx) {
@@ -354,15 +328,25 @@ bool shape_ok(int n, int d, int classes, int dtype) {
 
 }  // namespace
 
+hipError_t lce_join(const LceArgs& a, const LceStats& s, const float* part, int splits) {
+  hipLaunchKernelGGL(join_kernel, dim3((a.n + THREADS / 64 - 1) / (THREADS / 64)), dim3(THREADS), 0, a.st, part, s.z_label, a.labels, a.ignore, s.row_max,
+                     s.row_rest, s.loss_rows, a.n, splits, a.classes);
+  hipLaunchKernelGGL(mean_kernel, dim3(1), dim3(1024), 0, a.st, s.loss_rows, a.labels, a.ignore, a.n, s.scale, a.loss);
+  return hipGetLastError();
+}
+
 size_t linear_ce_workspace_bytes(int n, int d, int classes, int gradients, int dtype) {
-  return shape_ok(n, d, classes, dtype) ? plan32(n, d, classes, gradients != 0, dtype).total : 0;
+  if (!shape_ok(n, d, classes, dtype)) return 0;
+  if (dtype == DT_BF16 && linear_ce_bf16_takes(n, d, classes)) return linear_ce_bf16_workspace_bytes(n, d, classes, gradients != 0);
+  return plan32(n, d, classes, gradients != 0, dtype).total;
 }
 
 hipError_t linear_ce(const void* x, const void* w, const float* bias, const int32_t* labels, int ignore, float* loss_rows, float* loss, void* dx, float* dw,
                      float* db, int n, int d, int classes, void* workspace, size_t workspace_bytes, int dtype, hipStream_t st) {
   if (!x || !w || !labels || !workspace || !(loss_rows || loss || dx || dw || db) || !shape_ok(n, d, classes, dtype)) return hipErrorInvalidValue;
   if (workspace_bytes < linear_ce_workspace_bytes(n, d, classes, dx || dw || db, dtype)) return hipErrorInvalidValue;
-  return run32(Args{x, w, bias, labels, ignore, loss_rows, loss, dx, dw, db, n, d, classes, (char*)workspace, dtype, st});
+  const LceArgs a{x, w, bias, labels, ignore, loss_rows, loss, dx, dw, db, n, d, classes, (char*)workspace, dtype, st};
+  return dtype == DT_BF16 && linear_ce_bf16_takes(n, d, classes) ? linear_ce_bf16(a) : run32(a);
 }
 
 }  // namespace acc
