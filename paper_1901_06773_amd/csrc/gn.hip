@@ -302,6 +302,364 @@ __global__ __launch_bounds__(THREADS) void gn_bwd_apply_kernel(const T* x, const
   }
 }
 
+// ---------------------------------------------------------------------------------- small images: one read, the values stay in registers
+//
+// A workgroup takes all rows of a few neighbouring groups of one image, 64 bytes of channels or more, and keeps them: thread t has V channels of the rows
+// t / tpr, t / tpr + rpi, ...  Forward: mean, then the squares of the deviations from it, both in fp32 (a thread adds at most R values one behind
+// the other, the rest in a tree).  The XCD-wise order of workgroups lets neighbouring slices of a row meet in one L2.
+struct Slice {
+  int hw, c, groups, per;
+  int k, s, slices;                                    // groups and channels of a slice, slices of an image
+  int tpr, rpi;
+  int all;                                             // slices of all images
+};
+
+// sums over a wave; the first lane's order is fixed
+__device__ __forceinline__ float wave_sum_f(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+// Values of the threads, added up per group: val[NV] of a thread belong to NV parts of its channels.  red: NT * NV floats, out: one per group, finish() of the sum.
+template <int NT, int NV, class F>
+__device__ __forceinline__ void group_sums(const float (&val)[NV], float* red, float* out, const Slice& sl, bool active, F finish) {
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) red[tid * NV + j] = active ? val[j] : 0.f;
+  __syncthreads();
+  // a row of red: tpr * NV parts, of which each group has `parts` neighbouring ones
+  const int width = sl.tpr * NV, parts = width / sl.k, count = parts * sl.rpi;
+  for (int g = wave; g < sl.k; g += NT / 64) {
+    float t = 0.f;
+    for (int i = lane; i < count; i += 64) {
+      const int r = i / parts, j = i - r * parts;
+      t += red[r * width + g * parts + j];
+    }
+    t = wave_sum_f(t);
+    if (lane == 0) out[g] = finish(t);
+  }
+  __syncthreads();
+}
+
+// V values added up in pairs
+template <int V> __device__ __forceinline__ float pairs(float (&v)[V]) {
+#pragma unroll
+  for (int o = V / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int j = 0; j < o; ++j) v[j] += v[j + o];
+  return v[0];
+}
+
+// Keeps the compiler from working on more than a few rows of many at a time, which would not fit the registers.
+__device__ __forceinline__ void fence() {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_sched_barrier(0);
+#endif
+}
+// a value that the compiler takes for a new one: what follows from it is worked out again, not kept in registers
+__device__ __forceinline__ uint32_t anew(uint32_t v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(v));
+#endif
+  return v;
+}
+template <int R> __device__ __forceinline__ void pause(int u) {
+  if (R > 4 && (u & 1)) fence();
+}
+
+constexpr int kMaxSliceGroups = 256;
+
+// PERCH: a thread's channels may belong to several groups
+template <class T, int V, int R, int NT, bool PERCH>
+__global__ __launch_bounds__(NT) void gn_fwd_slice_kernel(const T* x, const float* __restrict__ gamma, const float* __restrict__ beta, const T* res,
+                                                          float* __restrict__ mean, float* __restrict__ istd, T* y, int act_kind, float eps, Slice sl, int blocks) {
+  constexpr int NV = PERCH ? V : 1;
+  __shared__ float red[NT * NV];
+  __shared__ float mu_sh[kMaxSliceGroups], is_sh[kMaxSliceGroups];
+  const int at = (blockIdx.x & 7) * (blocks >> 3) + (blockIdx.x >> 3);
+  if (at >= sl.all) return;
+  const int img = at / sl.slices, slice = at - img * sl.slices, tid = threadIdx.x, row0 = tid / sl.tpr, col = tid - row0 * sl.tpr;
+  const int ch = slice * sl.s + col * V;
+  const bool active = row0 < sl.rpi;
+  const int rows = active && row0 < sl.hw ? (sl.hw - 1 - row0) / sl.rpi + 1 : 0;       // of this thread
+  // (an image is less than 4 GiB: byte offsets of 32 bits beside addresses that the workgroup shares, worked out anew for every pass)
+  const size_t base = (size_t)img * sl.hw * sl.c + (size_t)slice * sl.s;
+  const uint32_t off0 = rows > 0 ? ((uint32_t)row0 * (uint32_t)sl.c + (uint32_t)(col * V)) * (uint32_t)sizeof(T) : 0u;
+  const uint32_t step = (uint32_t)sl.rpi * (uint32_t)sl.c * (uint32_t)sizeof(T);
+  const char *const xb = (const char*)(x + base), *const rb = res ? (const char*)(res + base) : nullptr;
+  char* const yb = (char*)(y + base);
+  Vec<T, V> xv[R];
+  uint32_t to = anew(off0);
+#pragma unroll
+  for (int u = 0; u < R; ++u) {
+    xv[u].load((const T*)(xb + (u < rows ? to : 0u)));
+    to += step;
+  }
+  float ga[V], be[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) { ga[j] = active ? gamma[ch + j] : 0.f; be[j] = active ? beta[ch + j] : 0.f; }
+  const float m = (float)sl.hw * (float)sl.per;
+  float val[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) val[j] = 0.f;
+  auto add = [&](float (&v)[V]) {
+    if constexpr (PERCH) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) val[j] += v[j];
+    } else {
+      val[0] += pairs<V>(v);
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < R; ++u)
+    if (u < rows) {
+      float v[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[j] = xv[u].get(j);
+      add(v);
+      pause<R>(u);
+    }
+  group_sums<NT, NV>(val, red, mu_sh, sl, active, [&](float t) { return t / m; });
+  int g[NV];
+  float mu[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    g[j] = active ? (col * V + j) / sl.per : 0;
+    mu[j] = mu_sh[g[j]];
+    val[j] = 0.f;
+  }
+#pragma unroll
+  for (int u = 0; u < R; ++u)
+    if (u < rows) {
+      float v[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float d = xv[u].get(j) - mu[PERCH ? j : 0];
+        v[j] = d * d;
+      }
+      add(v);
+      pause<R>(u);
+    }
+  group_sums<NT, NV>(val, red, is_sh, sl, active, [&](float t) { return (float)(1.0 / sqrt((double)(t / m) + (double)eps)); });
+  for (int i = tid; i < sl.k; i += NT) {
+    const size_t to = (size_t)img * sl.groups + slice * sl.k + i;
+    mean[to] = mu_sh[i];
+    istd[to] = is_sh[i];
+  }
+  if (!active) return;
+  float is[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) is[j] = is_sh[g[j]];
+  to = anew(off0);
+#pragma unroll
+  for (int u = 0; u < R; ++u)
+    if (u < rows) {
+      Vec<T, V> rv;
+      if (res) rv.load((const T*)(rb + to));
+      float o[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int q = PERCH ? j : 0;
+        o[j] = fmaf((xv[u].get(j) - mu[q]) * is[q], ga[j], be[j]);
+        if (res) o[j] += rv.get(j);
+      }
+      if (act_kind == ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) o[j] = act<ACT_RELU>(o[j]);
+      } else if (act_kind == ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) o[j] = act<ACT_SILU>(o[j]);
+      }
+      rv.set(o);
+      rv.store((T*)(yb + to));
+      to += step;
+      pause<R>(u);
+    }
+}
+
+// Backward: x and g in registers (SiLU: x and dy, g worked out twice); per channel the sums of g and g * xhat, left in chan[image][2][c] for
+// gn_params_kernel and added up to A and B here.
+template <class T, int V, int R, int NT, bool PERCH>
+__global__ __launch_bounds__(NT) void gn_bwd_slice_kernel(const T* x, const T* dy, const T* side, const float* __restrict__ gamma,
+                                                          const float* __restrict__ beta, const float* __restrict__ mean, const float* __restrict__ istd,
+                                                          T* dx, T* dres, float* __restrict__ chan, int act_kind, Slice sl, int blocks) {
+  constexpr int NV = PERCH ? V : 1;
+  extern __shared__ float dyn[];                       // [rpi][2][s] sums of the threads, then [parts][2 s], then tot[2 s]
+  __shared__ float coef[2 * kMaxSliceGroups];
+  const int at = (blockIdx.x & 7) * (blocks >> 3) + (blockIdx.x >> 3);
+  if (at >= sl.all) return;
+  const int img = at / sl.slices, slice = at - img * sl.slices, tid = threadIdx.x, row0 = tid / sl.tpr, col = tid - row0 * sl.tpr;
+  const int ch = slice * sl.s + col * V;
+  const bool active = row0 < sl.rpi;
+  const int rows = active && row0 < sl.hw ? (sl.hw - 1 - row0) / sl.rpi + 1 : 0;
+  const size_t base = (size_t)img * sl.hw * sl.c + (size_t)slice * sl.s;
+  const uint32_t off0 = rows > 0 ? ((uint32_t)row0 * (uint32_t)sl.c + (uint32_t)(col * V)) * (uint32_t)sizeof(T) : 0u;
+  const uint32_t step = (uint32_t)sl.rpi * (uint32_t)sl.c * (uint32_t)sizeof(T);
+  const char *const xb = (const char*)(x + base), *const db = (const char*)(dy + base), *const sb = side ? (const char*)(side + base) : nullptr;
+  char *const dxb = (char*)(dx + base), *const drb = dres ? (char*)(dres + base) : nullptr;
+  Vec<T, V> xv[R], gv[R];
+  uint32_t to = anew(off0);
+#pragma unroll
+  for (int u = 0; u < R; ++u) {
+    const uint32_t from = u < rows ? to : 0u;
+    xv[u].load((const T*)(xb + from));
+    gv[u].load((const T*)(db + from));
+    to += step;
+  }
+  float ga[V], be[V], mu[NV], is[NV];
+  int g[NV];
+#pragma unroll
+  for (int j = 0; j < V; ++j) { ga[j] = active ? gamma[ch + j] : 0.f; be[j] = active && act_kind == ACT_SILU ? beta[ch + j] : 0.f; }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    g[j] = active ? (col * V + j) / sl.per : 0;
+    mu[j] = mean[(size_t)img * sl.groups + slice * sl.k + g[j]];
+    is[j] = istd[(size_t)img * sl.groups + slice * sl.k + g[j]];
+  }
+  if (act_kind == ACT_RELU) {
+    to = anew(off0);
+#pragma unroll
+    for (int u = 0; u < R; ++u) {
+      Vec<T, V> yv;
+      yv.load((const T*)(sb + (u < rows ? to : 0u)));
+      to += step;
+      float v[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[j] = yv.get(j) > 0.f ? gv[u].get(j) : 0.f;
+      gv[u].set(v);                                    // (a value or zero: exact)
+      if (R > 4 && (u & 3) == 3) fence();
+    }
+  }
+  auto slope = [&](int u, float (&v)[V]) {             // g of one row
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = gv[u].get(j);
+    if (act_kind == ACT_SILU) {
+      Vec<T, V> rv;
+      if (side) rv.load((const T*)(sb + to));
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int q = PERCH ? j : 0;
+        float z = fmaf((xv[u].get(j) - mu[q]) * is[q], ga[j], be[j]);
+        if (side) z += rv.get(j);
+        v[j] *= silu_slope(z);
+      }
+    }
+  };
+  float s0[V], s1[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) s0[j] = s1[j] = 0.f;
+  to = anew(off0);
+#pragma unroll
+  for (int u = 0; u < R; ++u)
+    if (u < rows) {
+      float v[V];
+      slope(u, v);
+      to += step;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        s0[j] += v[j];
+        s1[j] = fmaf(v[j], (xv[u].get(j) - mu[PERCH ? j : 0]) * is[PERCH ? j : 0], s1[j]);
+      }
+      pause<R>(u);
+    }
+  const int s2 = 2 * sl.s;
+  if (active) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      dyn[row0 * s2 + col * V + j] = s0[j];
+      dyn[row0 * s2 + sl.s + col * V + j] = s1[j];
+    }
+  }
+  __syncthreads();
+  // columns: `parts` threads each, then one
+  const int parts = NT / s2 > 0 ? NT / s2 : 1;
+  float* const sub = dyn + sl.rpi * s2;
+  for (int i = tid; i < parts * s2; i += NT) {
+    const int part = i / s2, cl = i - part * s2;
+    float t = 0.f;
+    for (int r = part; r < sl.rpi; r += parts) t += dyn[r * s2 + cl];
+    sub[i] = t;
+  }
+  __syncthreads();
+  float* const tot = sub + parts * s2;
+  for (int i = tid; i < s2; i += NT) {
+    float t = 0.f;
+    for (int q = 0; q < parts; ++q) t += sub[q * s2 + i];
+    tot[i] = t;
+    const int which = i >= sl.s, cl = i - which * sl.s;
+    chan[(size_t)img * 2 * sl.c + which * sl.c + slice * sl.s + cl] = t;
+  }
+  __syncthreads();
+  const float inv_m = 1.f / ((float)sl.hw * (float)sl.per);
+  for (int w = tid >> 6; w < 2 * sl.k; w += NT / 64) {
+    const int which = w >= sl.k, gg = w - which * sl.k;
+    float t = 0.f;
+    for (int j = tid & 63; j < sl.per; j += 64) t += gamma[slice * sl.s + gg * sl.per + j] * tot[which * sl.s + gg * sl.per + j];
+    t = wave_sum_f(t);
+    if ((tid & 63) == 0) coef[w] = t * inv_m;
+  }
+  __syncthreads();
+  to = anew(off0);
+#pragma unroll
+  for (int u = 0; u < R; ++u)
+    if (u < rows) {
+      float v[V], o[V];
+      slope(u, v);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int q = PERCH ? j : 0;
+        const float xh = (xv[u].get(j) - mu[q]) * is[q];
+        o[j] = is[q] * (v[j] * ga[j] - coef[g[q]] - xh * coef[sl.k + g[q]]);
+      }
+      xv[u].set(o);
+      xv[u].store((T*)(dxb + to));
+      if (dres) {
+        xv[u].set(v);
+        xv[u].store((T*)(drb + to));
+      }
+      to += step;
+      pause<R>(u);
+    }
+}
+
+// The slices of a tensor, if they fit: 64 bytes of channels (a line of memory is then read by two workgroups at most) or as many groups as it takes for
+// whole threads; 32 where 64 do not fit.  Threads and rows of a workgroup: the fewest threads whose registers hold a slice.
+struct SliceCfg {
+  Slice sl;
+  int nt, r;                                           // 0: does not fit
+};
+// rows of a thread of 1024 that fit 128 registers beside what else it needs
+constexpr int slice_rows(int v, bool perch, bool backward) { return !backward ? 20 : v == 4 ? (perch ? 8 : 10) : (perch ? 6 : 8); }
+SliceCfg slice_cfg(int n, int hw, int c, int groups, int v, int es, bool backward) {
+  SliceCfg f{};
+  const int per = c / groups;
+  if ((long)hw * c * es >= 1L << 32) return f;
+  auto fits = [&](int k) {
+    const int tpr = k * per / v;
+    if (tpr > 256) return false;
+    auto rows = [&](int nt) { return (int)(((long)hw + nt / tpr - 1) / (nt / tpr)); };
+    const int nt = rows(256) <= (backward ? 4 : 8) ? 256 : rows(512) <= (backward ? 8 : 16) ? 512 : rows(1024) <= slice_rows(v, per % v != 0, backward) ? 1024 : 0;
+    if (!nt || (long)n * (groups / k) * nt >= (1L << 32) - 8192) return false;         // (a launch has fewer than 2^32 threads)
+    f.nt = nt;
+    f.r = rows(nt);
+    f.sl = Slice{hw, c, groups, per, k, k * per, groups / k, tpr, nt / tpr, n * (groups / k)};
+    return true;
+  };
+  int narrow = 0;                                      // the widest slice of 32 bytes or more that is narrower than 64
+  for (int k = 1; k <= groups && k <= kMaxSliceGroups; ++k) {
+    if (groups % k != 0 || (long)k * per % v != 0) continue;
+    const long bytes = (long)k * per * es;
+    if (bytes < 64 && k < groups) {
+      if (bytes >= 32) narrow = k;
+      continue;
+    }
+    if (!fits(k) && narrow) fits(narrow);
+    return f;
+  }
+  return f;
+}
+
 // `images` x slabs workgroups, about four per compute unit, at least 4 trips of U rows each
 Cover cover(int n, int hw, int c, int groups, int v, long target) {
   Cover cv{};
@@ -361,6 +719,51 @@ void backward_any(const GnArgs& a) {
   hipLaunchKernelGGL(gn_params_kernel, dim3((2 * a.c + 31) / 32), dim3(THREADS), 0, a.st, chan, a.dgamma, a.dbeta, a.n, a.c);
 }
 
+template <class T, int V, int R, int NT, bool PERCH>
+void launch_fwd_slice(const GnArgs& a, const Slice& sl, int act) {
+  const int blocks = (sl.all + 7) / 8 * 8;
+  hipLaunchKernelGGL((gn_fwd_slice_kernel<T, V, R, NT, PERCH>), dim3(blocks), dim3(NT), 0, a.st, (const T*)a.x, a.gamma, a.beta, (const T*)a.side, a.mean,
+                     a.istd, (T*)a.out, act, a.eps, sl, blocks);
+}
+template <class T, int V, int R, int NT, bool PERCH>
+void launch_bwd_slice(const GnArgs& a, const Slice& sl, int act) {
+  const int blocks = (sl.all + 7) / 8 * 8, s2 = 2 * sl.s, parts = NT / s2 > 0 ? NT / s2 : 1;
+  const size_t lds = ((size_t)sl.rpi * s2 + (size_t)parts * s2 + s2) * sizeof(float);
+  float* chan = static_cast<float*>(a.workspace);
+  hipLaunchKernelGGL((gn_bwd_slice_kernel<T, V, R, NT, PERCH>), dim3(blocks), dim3(NT), lds, a.st, (const T*)a.x, (const T*)a.dy, (const T*)a.side, a.gamma,
+                     a.beta, a.mean_in, a.istd_in, (T*)a.out, (T*)a.dres, chan, act, sl, blocks);
+  hipLaunchKernelGGL(gn_params_kernel, dim3((2 * a.c + 31) / 32), dim3(THREADS), 0, a.st, chan, a.dgamma, a.dbeta, a.n, a.c);
+}
+template <class T, int V, bool PERCH>
+bool forward_slices(const GnArgs& a, int act) {
+  const SliceCfg f = slice_cfg(a.n, a.hw, a.c, a.groups, V, (int)sizeof(T), false);
+  if (!f.nt) return false;
+#define ACC_CASE(NT, ROWS) if (constexpr int R = ROWS; f.nt == NT && f.r <= R) { launch_fwd_slice<T, V, R, NT, PERCH>(a, f.sl, act); return true; }
+  ACC_CASE(256, 1) ACC_CASE(256, 2) ACC_CASE(256, 4) ACC_CASE(256, 8) ACC_CASE(512, 8) ACC_CASE(512, 16) ACC_CASE(1024, 16) ACC_CASE(1024, slice_rows(V, PERCH, false))
+#undef ACC_CASE
+  return false;
+}
+template <class T, int V, bool PERCH>
+bool backward_slices(const GnArgs& a, int act) {
+  const SliceCfg f = slice_cfg(a.n, a.hw, a.c, a.groups, V, (int)sizeof(T), true);
+  if (!f.nt) return false;
+#define ACC_CASE(NT, ROWS) if (constexpr int R = ROWS; f.nt == NT && f.r <= R) { launch_bwd_slice<T, V, R, NT, PERCH>(a, f.sl, act); return true; }
+  ACC_CASE(256, 1) ACC_CASE(256, 2) ACC_CASE(256, 4) ACC_CASE(512, 4) ACC_CASE(512, 8) ACC_CASE(1024, slice_rows(V, PERCH, true))
+#undef ACC_CASE
+  return false;
+}
+template <class T, int V>
+bool slices(const GnArgs& a, int act, bool backward) {
+  const bool perch = (a.c / a.groups) % V != 0;
+  if (backward) return perch ? backward_slices<T, V, true>(a, act) : backward_slices<T, V, false>(a, act);
+  return perch ? forward_slices<T, V, true>(a, act) : forward_slices<T, V, false>(a, act);
+}
+// whether the tensor's slices fit a workgroup, which then has been launched
+bool by_slices(const GnArgs& a, int act, int dtype, bool backward) {
+  if (dtype == DT_F32) return a.c % 4 == 0 && slices<float, 4>(a, act, backward);
+  return a.c % 8 == 0 && slices<bf16_t, 8>(a, act, backward);
+}
+
 #define ACC_GN_ACT(F, T, V)                        \
   switch (act) {                                   \
     case ACT_NONE: F<ACT_NONE, T, V>(a); break;    \
@@ -401,6 +804,7 @@ hipError_t gn_forward(const void* x, const float* gamma, const float* beta, cons
   GnArgs a{};
   a.x = x; a.gamma = gamma; a.beta = beta; a.side = res; a.out = y; a.mean = mean; a.istd = istd;
   a.n = n; a.hw = hw; a.c = c; a.groups = groups; a.eps = eps; a.workspace = workspace; a.st = st;
+  if (by_slices(a, act, dtype, false)) return hipGetLastError();
   ACC_GN(forward_any);
   return hipGetLastError();
 }
@@ -415,6 +819,7 @@ hipError_t gn_backward(const void* x, const void* dy, const void* y, const void*
   a.x = x; a.dy = dy; a.side = act == ACT_RELU ? y : act == ACT_SILU ? res : nullptr; a.gamma = gamma; a.beta = beta; a.mean_in = mean; a.istd_in = istd;
   a.out = dx; a.dgamma = dgamma; a.dbeta = dbeta; a.dres = dres;
   a.n = n; a.hw = hw; a.c = c; a.groups = groups; a.workspace = workspace; a.st = st;
+  if (by_slices(a, act, dtype, true)) return hipGetLastError();
   ACC_GN(backward_any);
   return hipGetLastError();
 }
