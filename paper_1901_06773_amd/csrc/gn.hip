@@ -40,14 +40,20 @@ template <> struct Vec<bf16_t, 8> {
     return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
   }
   __device__ __forceinline__ void set(const float (&v)[8]) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)float_to_bf16(v[2 * i]) | ((uint32_t)float_to_bf16(v[2 * i + 1]) << 16);
-    raw = make_uint4(w[0], w[1], w[2], w[3]);
+    raw = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
   }
 };
 
-__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
+// 1 / (1 + e^-z) by the base-two exponential and the reciprocal of the hardware, a rounding or two each; the rounding of z * log2 e makes e^-z wrong by
+// |z| / 1.4 of them more, which is little beside 1 where z is positive and where z is negative leaves a value of at most 1 / 4 of z's size (an exact expf
+// and a division took the kernels from memory to arithmetic: 8 images of 56x56, 64 channels, bf16 forward 39 us)
+__device__ __forceinline__ float sigmoid(float z) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896341f * z));
+#else
+  return z;
+#endif
+}
 template <int ACT> __device__ __forceinline__ float act(float z) {
   if (ACT == ACT_RELU) return z < 0.f ? 0.f : z;       // (a value that is no number stays none)
   if (ACT == ACT_SILU) return z * sigmoid(z);
@@ -58,17 +64,44 @@ __device__ __forceinline__ float silu_slope(float z) {
   return s * (1.f + z * (1.f - s));
 }
 
-// ---------------------------------------------------------------------------------- any size: sums, finish, apply
+// V neighbouring fp32 parameters
+template <int V> __device__ __forceinline__ void load_params(const float* p, float (&v)[V]) {
+  if constexpr (V % 4 == 0) {
+#pragma unroll
+    for (int j = 0; j < V; j += 4) {
+      const float4 q = *reinterpret_cast<const float4*>(p + j);
+      v[j] = q.x; v[j + 1] = q.y; v[j + 2] = q.z; v[j + 3] = q.w;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = p[j];
+  }
+}
+
+// ---------------------------------------------------------------------------------- any size: sums, then apply
 //
-// The rows of an image are cut into slabs; a workgroup adds up, per channel, the rows of one slab for up to THREADS groups of V
-// channels, in fp64 (the square of a mean is subtracted from the mean of squares), and leaves part[image][slab][2][c].
+// The rows of an image are cut into slabs, its channels into slices of whole groups (or a group into several slices, where it is wider than a workgroup).
+// A workgroup adds up one slab of one slice, per channel and then per group, and leaves one pair of sums per group; every workgroup of the second
+// launch joins the slabs of its own groups, while its first rows are on their way, and works on its rows.  A thread adds a few rows in fp32 and these
+// in fp64.
 constexpr int THREADS = 256;
-constexpr int U = 4;                                   // rows of a thread in flight
+template <int BWD, int V> struct Rows { static constexpr int U = BWD && V == 8 ? 2 : 4; };      // rows of a thread on their way, twice
 
 struct Cover {
   int hw, c, groups, per;
-  int tpr, rpi, slices;                                // threads across a row of one slice, rows per trip, slices of channels
-  int slabs, rows_per_slab;
+  int slices, width;                                   // slices of a row, channels of a slice (the last of a row or group may have fewer)
+  int k, s;                                            // groups of a slice, slices of a group: one of them is 1
+  int tpr, rpi;                                        // threads across a slice, rows per trip
+  int slabs, rows_per_slab;                            // of the sums
+  int cuts, rows_per_cut;                              // of the second launch
+  // first channel of a slice, and the end of its channels
+  __host__ __device__ int first(int slice) const { return s > 1 ? slice / s * per + slice % s * width : slice * width; }
+  __host__ __device__ int end(int slice) const {
+    const int all = s > 1 ? (slice / s + 1) * per : c, e = first(slice) + width;
+    return e < all ? e : all;
+  }
+  // pairs of sums per image and slab: one per group, or one per slice
+  __host__ __device__ int slots() const { return s > 1 ? slices : groups; }
 };
 
 template <int ACT, class T, int V>
@@ -78,22 +111,33 @@ __device__ __forceinline__ float slope_times(float dy, float y, float x, float m
   return dy;
 }
 
-// BWD 0: (x, x*x).  BWD 1: (g, g * xhat).  side: the stored output (ReLU) or the residual (SiLU; may be null).
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+// BWD 0: sums of x and x * x, taken from x - p and its square with p the slab's first row (fp32 sums of these lose nothing to a mean that is far from
+// zero); pairs[image][slab][slot][2].  BWD 1: of g and g * xhat, per channel chan[image][slab][2][c], per group with gamma as a factor in pairs.
+// side: the stored output (ReLU) or the residual (SiLU; may be null).
 template <int BWD, int ACT, class T, int V>
 __global__ __launch_bounds__(THREADS) void gn_sums_kernel(const T* __restrict__ x, const T* __restrict__ dy, const T* __restrict__ side,
                                                           const float* __restrict__ gamma, const float* __restrict__ beta,
                                                           const float* __restrict__ mean, const float* __restrict__ istd,
-                                                          double* __restrict__ part, Cover cv) {
-  __shared__ double red[2][THREADS][V];
+                                                          double* __restrict__ pairs, float* __restrict__ chan, Cover cv) {
+  constexpr int U = Rows<BWD, V>::U;
+  __shared__ double red[2][THREADS * V];
   const int tid = threadIdx.x, lane_r = tid / cv.tpr, lane_c = tid - lane_r * cv.tpr;
   const int slice = blockIdx.x % cv.slices, rest = blockIdx.x / cv.slices, slab = rest % cv.slabs, img = rest / cv.slabs;
-  const int ch = (slice * cv.tpr + lane_c) * V;
-  const bool active = lane_r < cv.rpi && ch < cv.c;
+  const int ch0 = cv.first(slice), ch1 = cv.end(slice), ch = ch0 + lane_c * V;
+  const bool active = lane_r < cv.rpi && ch < ch1;
+  const int lo = slab * cv.rows_per_slab, hi = min(lo + cv.rows_per_slab, cv.hw);
   double s0[V], s1[V];
+  float p[V], mu[V], is[V], ga[V], be[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) s0[j] = s1[j] = 0.0;
   if (active) {
-    float mu[V], is[V], ga[V], be[V];
+    const size_t base = (size_t)img * cv.hw * cv.c + ch;
     if (BWD) {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
@@ -103,123 +147,149 @@ __global__ __launch_bounds__(THREADS) void gn_sums_kernel(const T* __restrict__ 
         ga[j] = ACT == ACT_SILU ? gamma[ch + j] : 0.f;
         be[j] = ACT == ACT_SILU ? beta[ch + j] : 0.f;
       }
+    } else {
+      Vec<T, V> first;
+      first.load(x + base + (size_t)lo * cv.c);
+#pragma unroll
+      for (int j = 0; j < V; ++j) p[j] = first.get(j);
     }
-    const int lo = slab * cv.rows_per_slab, hi = min(lo + cv.rows_per_slab, cv.hw);
-    const size_t base = (size_t)img * cv.hw * cv.c + ch;
+    float t0[V], t1[V];
     auto add = [&](const Vec<T, V>& xv, const Vec<T, V>& dv, const Vec<T, V>& sv) {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         if (!BWD) {
-          const double d = (double)xv.get(j);
-          s0[j] += d;
-          s1[j] += d * d;
+          const float d = xv.get(j) - p[j];
+          t0[j] += d;
+          t1[j] = fmaf(d, d, t1[j]);
         } else {
           const float xs = xv.get(j);
           const float g = slope_times<ACT, T, V>(dv.get(j), ACT == ACT_RELU ? sv.get(j) : 0.f, xs, mu[j], is[j], ga[j], be[j],
                                                  ACT == ACT_SILU && side ? sv.get(j) : 0.f);
-          s0[j] += (double)g;
-          s1[j] += (double)g * (double)((xs - mu[j]) * is[j]);
+          t0[j] += g;
+          t1[j] = fmaf(g, (xs - mu[j]) * is[j], t1[j]);
         }
       }
     };
-    int r = lo + lane_r;
-    for (; r + (U - 1) * cv.rpi < hi; r += U * cv.rpi) {
-      Vec<T, V> xv[U], dv[U], sv[U];
+    // the next rows are asked for before these are added
+    Vec<T, V> xv[2][U], dv[2][U], sv[2][U];
+    auto load = [&](int r, int to) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const size_t at = base + (size_t)(r + u * cv.rpi) * cv.c;
-        xv[u].load(x + at);
-        if (BWD) dv[u].load(dy + at);
-        if (BWD && ACT != ACT_NONE && side) sv[u].load(side + at);
+        const int ru = r + u * cv.rpi;
+        const size_t at = base + (size_t)(ru < hi ? ru : lo) * cv.c;      // (a row that does not exist: read, not added)
+        xv[to][u].load(x + at);
+        if (BWD) dv[to][u].load(dy + at);
+        if (BWD && ACT != ACT_NONE && side) sv[to][u].load(side + at);
       }
+    };
+    auto sum = [&](int r, int from) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) add(xv[u], dv[u], sv[u]);
-    }
-    for (; r < hi; r += cv.rpi) {
-      Vec<T, V> xv, dv, sv;
-      const size_t at = base + (size_t)r * cv.c;
-      xv.load(x + at);
-      if (BWD) dv.load(dy + at);
-      if (BWD && ACT != ACT_NONE && side) sv.load(side + at);
-      add(xv, dv, sv);
+      for (int j = 0; j < V; ++j) t0[j] = t1[j] = 0.f;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (r + u * cv.rpi < hi) add(xv[from][u], dv[from][u], sv[from][u]);
+#pragma unroll
+      for (int j = 0; j < V; ++j) { s0[j] += (double)t0[j]; s1[j] += (double)t1[j]; }
+    };
+    const int trip = U * cv.rpi;
+    int r = lo + lane_r;
+    load(r, 0);
+    for (; r < hi; r += 2 * trip) {
+      load(r + trip, 1);
+      sum(r, 0);
+      load(r + 2 * trip, 0);
+      sum(r + trip, 1);
     }
   }
+  // the rows of threads, in order: values j of neighbouring threads side by side (no bank twice), a thread per channel
+  const int wide = cv.tpr * V;
+  if (lane_r < cv.rpi) {
 #pragma unroll
-  for (int j = 0; j < V; ++j) { red[0][tid][j] = s0[j]; red[1][tid][j] = s1[j]; }
+    for (int j = 0; j < V; ++j) { red[0][lane_r * wide + j * cv.tpr + lane_c] = s0[j]; red[1][lane_r * wide + j * cv.tpr + lane_c] = s1[j]; }
+  }
   __syncthreads();
-  if (lane_r == 0 && active) {
-    for (int rr = 1; rr < cv.rpi; ++rr)
+  const double rows = (double)(hi - lo);
+  double c0[V], c1[V];
 #pragma unroll
-      for (int j = 0; j < V; ++j) { s0[j] += red[0][rr * cv.tpr + lane_c][j]; s1[j] += red[1][rr * cv.tpr + lane_c][j]; }
-    double* p = part + ((size_t)img * cv.slabs + slab) * 2 * cv.c + ch;
+  for (int i = 0; i < V; ++i) {
+    const int at = tid + i * THREADS, j = at / cv.tpr, chn = ch0 + (at - j * cv.tpr) * V + j;
+    c0[i] = c1[i] = 0.0;
+    if (at >= wide || chn >= ch1) continue;
+    for (int rr = 0; rr < cv.rpi; ++rr) { c0[i] += red[0][rr * wide + at]; c1[i] += red[1][rr * wide + at]; }
+    if (BWD) {
+      const size_t to = ((size_t)img * cv.slabs + slab) * 2 * cv.c + chn;
+      chan[to] = (float)c0[i];
+      chan[to + cv.c] = (float)c1[i];
+      const double f = (double)gamma[chn];
+      c0[i] *= f;
+      c1[i] *= f;
+    } else {
+      const double q = (double)Elem<T>::load(x + ((size_t)img * cv.hw + lo) * cv.c + chn);
+      c1[i] += q * (2.0 * c0[i] + rows * q);
+      c0[i] += rows * q;
+    }
+  }
+  __syncthreads();
 #pragma unroll
-    for (int j = 0; j < V; ++j) { p[j] = s0[j]; p[cv.c + j] = s1[j]; }
+  for (int i = 0; i < V; ++i) {
+    const int at = tid + i * THREADS, j = at / cv.tpr;
+    if (at < wide) { red[0][(at - j * cv.tpr) * V + j] = c0[i]; red[1][(at - j * cv.tpr) * V + j] = c1[i]; }
+  }
+  __syncthreads();
+  // the channels of a group: a thread each where they are few, else a wave
+  const int per = cv.s > 1 ? ch1 - ch0 : cv.per, count = cv.s > 1 ? 1 : (ch1 - ch0) / cv.per, slot0 = cv.s > 1 ? slice : slice * cv.k;
+  double* const out = pairs + (((size_t)img * cv.slabs + slab) * cv.slots() + slot0) * 2;
+  if (per <= 8) {
+    for (int i = tid; i < 2 * count; i += THREADS) {
+      double t = 0.0;
+      for (int j = 0; j < per; ++j) t += red[i & 1][(i >> 1) * per + j];
+      out[i] = t;
+    }
+  } else {
+    for (int i = tid >> 6; i < 2 * count; i += THREADS / 64) {
+      double t = 0.0;
+      for (int j = tid & 63; j < per; j += 64) t += red[i & 1][(i >> 1) * per + j];
+      t = wave_sum(t);
+      if ((tid & 63) == 0) out[i] = t;
+    }
   }
 }
 
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  return v;
-}
-
-// One wave per group of an image.  Forward: mean and 1/std.
-__global__ __launch_bounds__(THREADS) void gn_fwd_finish_kernel(const double* __restrict__ part, float* __restrict__ mean, float* __restrict__ istd,
-                                                                Cover cv, int all, float eps) {
-  const int at = blockIdx.x * (THREADS / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (at >= all) return;
-  const int img = at / cv.groups, g = at - img * cv.groups;
-  double s = 0.0, ss = 0.0;
-  for (int i = lane; i < cv.per * cv.slabs; i += 64) {
-    const int slab = i / cv.per, j = i - slab * cv.per;
-    const double* p = part + ((size_t)img * cv.slabs + slab) * 2 * cv.c + g * cv.per + j;
-    s += p[0];
-    ss += p[cv.c];
+// The slabs of a workgroup's groups joined: out[group of the slice][2] in LDS.  Groups side by side along the threads, 2^q threads each.
+constexpr int kMaxCoverGroups = 256;
+__device__ __forceinline__ void join_pairs(const double* __restrict__ pairs, int img, int slice, const Cover& cv, double (*out)[2]) {
+  const int tid = threadIdx.x, count = cv.s > 1 ? 1 : (cv.end(slice) - cv.first(slice)) / cv.per;
+  const int entries = cv.slabs * cv.s;                 // of a group
+  int q = 1;
+  while (q < 64 && q < entries && 2 * q * count <= THREADS) q *= 2;
+  const int slot0 = cv.s > 1 ? slice / cv.s * cv.s : slice * cv.k;
+  const double* const base = pairs + (size_t)img * cv.slabs * cv.slots() * 2;
+  for (int g = tid / q; g < (count + THREADS / q - 1) / (THREADS / q) * (THREADS / q); g += THREADS / q) {
+    double a = 0.0, b = 0.0;
+    if (g < count) {
+#pragma unroll 4
+      for (int i = tid % q; i < entries; i += q) {
+        const int slab = i / cv.s, sub = i - slab * cv.s;
+        const double2 v = *reinterpret_cast<const double2*>(base + ((size_t)slab * cv.slots() + slot0 + (cv.s > 1 ? sub : g)) * 2);
+        a += v.x;
+        b += v.y;
+      }
+    }
+    for (int o = 1; o < q; o <<= 1) { a += __shfl_xor(a, o); b += __shfl_xor(b, o); }
+    if (g < count && tid % q == 0) { out[g][0] = a; out[g][1] = b; }
   }
-  s = wave_sum(s);
-  ss = wave_sum(ss);
-  if (lane) return;
-  const double m = (double)cv.per * cv.hw, mu = s / m;
-  double var = ss / m - mu * mu;
-  if (var < 0.0) var = 0.0;
-  mean[at] = (float)mu;
-  istd[at] = (float)(1.0 / sqrt(var + (double)eps));
+  __syncthreads();
 }
 
-// Backward: per channel of the image the sums of g and g * xhat (chan[image][2][c]), per group A and B (coef[image * groups + g][2]).
-__global__ __launch_bounds__(THREADS) void gn_bwd_finish_kernel(const double* __restrict__ part, const float* __restrict__ gamma,
-                                                                float* __restrict__ chan, float* __restrict__ coef, Cover cv, int all) {
-  const int at = blockIdx.x * (THREADS / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (at >= all) return;
-  const int img = at / cv.groups, g = at - img * cv.groups;
-  double a = 0.0, b = 0.0;
-  for (int j = lane; j < cv.per; j += 64) {
-    const int ch = g * cv.per + j;
-    const double* p = part + (size_t)img * cv.slabs * 2 * cv.c + ch;
-    double s0 = 0.0, s1 = 0.0;
-    for (int k = 0; k < cv.slabs; ++k) { s0 += p[(size_t)k * 2 * cv.c]; s1 += p[(size_t)k * 2 * cv.c + cv.c]; }
-    chan[(size_t)img * 2 * cv.c + ch] = (float)s0;
-    chan[(size_t)img * 2 * cv.c + cv.c + ch] = (float)s1;
-    const double ga = (double)gamma[ch];
-    a += ga * s0;
-    b += ga * s1;
-  }
-  a = wave_sum(a);
-  b = wave_sum(b);
-  if (lane) return;
-  const double m = (double)cv.per * cv.hw;
-  coef[2 * (size_t)at] = (float)(a / m);
-  coef[2 * (size_t)at + 1] = (float)(b / m);
-}
-
-// dbeta and dgamma: the images' sums in order, a wave of lanes per channel column
-__global__ __launch_bounds__(THREADS) void gn_params_kernel(const float* __restrict__ chan, float* __restrict__ dgamma, float* __restrict__ dbeta, int n,
-                                                            int c) {
-  __shared__ double red[THREADS];
-  const int col = blockIdx.x * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;      // 8 parts of the images
+// dbeta and dgamma: `rows` rows of 2 c sums added up in order, 32 columns of a workgroup
+__device__ __forceinline__ void sum_params(const float* __restrict__ chan, float* __restrict__ dgamma, float* __restrict__ dbeta, long rows, int c, int block,
+                                           double* red) {
+  const int col = block * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;      // 8 parts of the rows
   double s = 0.0;
-  if (col < 2 * c)
-    for (int i = part; i < n; i += THREADS / 32) s += (double)chan[(size_t)i * 2 * c + col];
+  if (col < 2 * c) {
+#pragma unroll 4
+    for (long i = part; i < rows; i += THREADS / 32) s += (double)chan[(size_t)i * 2 * c + col];
+  }
   red[threadIdx.x] = s;
   __syncthreads();
   if (part || col >= 2 * c) return;
@@ -227,64 +297,121 @@ __global__ __launch_bounds__(THREADS) void gn_params_kernel(const float* __restr
   for (int k = 1; k < THREADS / 32; ++k) s += red[threadIdx.x + 32 * k];
   if (col < c) dbeta[col] = (float)s; else dgamma[col - c] = (float)s;
 }
-
-template <int ACT, class T, int V>
-__global__ __launch_bounds__(THREADS) void gn_apply_kernel(const T* __restrict__ x, const float* __restrict__ gamma, const float* __restrict__ beta,
-                                                           const T* __restrict__ res, const float* __restrict__ mean, const float* __restrict__ istd,
-                                                           T* __restrict__ y, Cover cv) {
-  const int tid = threadIdx.x, lane_r = tid / cv.tpr, lane_c = tid - lane_r * cv.tpr;
-  const int slice = blockIdx.x % cv.slices, rest = blockIdx.x / cv.slices, slab = rest % cv.slabs, img = rest / cv.slabs;
-  const int ch = (slice * cv.tpr + lane_c) * V;
-  if (lane_r >= cv.rpi || ch >= cv.c) return;
-  float mu[V], is[V], ga[V], be[V];
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const size_t g = (size_t)img * cv.groups + (ch + j) / cv.per;
-    mu[j] = mean[g]; is[j] = istd[g]; ga[j] = gamma[ch + j]; be[j] = beta[ch + j];
-  }
-  const int lo = slab * cv.rows_per_slab, hi = min(lo + cv.rows_per_slab, cv.hw);
-  const size_t base = (size_t)img * cv.hw * cv.c + ch;
-  for (int r = lo + lane_r; r < hi; r += cv.rpi) {
-    const size_t at = base + (size_t)r * cv.c;
-    Vec<T, V> xv, rv;
-    xv.load(x + at);
-    if (res) rv.load(res + at);
-    float o[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      float z = fmaf((xv.get(j) - mu[j]) * is[j], ga[j], be[j]);
-      if (res) z += rv.get(j);
-      o[j] = act<ACT>(z);
-    }
-    xv.set(o);
-    xv.store(y + at);
-  }
+__global__ __launch_bounds__(THREADS) void gn_params_kernel(const float* __restrict__ chan, float* __restrict__ dgamma, float* __restrict__ dbeta, int n, int c) {
+  __shared__ double red[THREADS];
+  sum_params(chan, dgamma, dbeta, n, c, blockIdx.x, red);
 }
 
 template <int ACT, class T, int V>
-__global__ __launch_bounds__(THREADS) void gn_bwd_apply_kernel(const T* x, const T* dy, const T* __restrict__ side,
-                                                               const float* __restrict__ gamma, const float* __restrict__ beta,
-                                                               const float* __restrict__ mean, const float* __restrict__ istd,
-                                                               const float* __restrict__ coef, T* dx, T* dres, Cover cv) {
+__global__ __launch_bounds__(THREADS) void gn_apply_kernel(const T* x, const float* __restrict__ gamma, const float* __restrict__ beta, const T* res,
+                                                           const double* __restrict__ pairs, float* __restrict__ mean, float* __restrict__ istd, T* y, float eps,
+                                                           Cover cv) {
+  __shared__ double sums[kMaxCoverGroups][2];
   const int tid = threadIdx.x, lane_r = tid / cv.tpr, lane_c = tid - lane_r * cv.tpr;
-  const int slice = blockIdx.x % cv.slices, rest = blockIdx.x / cv.slices, slab = rest % cv.slabs, img = rest / cv.slabs;
-  const int ch = (slice * cv.tpr + lane_c) * V;
-  if (lane_r >= cv.rpi || ch >= cv.c) return;
-  float mu[V], is[V], ga[V], be[V], ca[V], cb[V];
+  const int slice = blockIdx.x % cv.slices, rest = blockIdx.x / cv.slices, cut = rest % cv.cuts, img = rest / cv.cuts;
+  const int ch0 = cv.first(slice), ch1 = cv.end(slice), ch = ch0 + lane_c * V;
+  const bool active = lane_r < cv.rpi && ch < ch1;
+  const int lo = cut * cv.rows_per_cut, hi = min(lo + cv.rows_per_cut, cv.hw);
+  const size_t base = (size_t)img * cv.hw * cv.c + ch;
+  int r = lo + lane_r;
+  Vec<T, V> xv[2], rv[2];
+  auto load = [&](int row) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int ru = row + u * cv.rpi;
+      const size_t at = base + (size_t)(ru < hi ? ru : row) * cv.c;
+      xv[u].load(x + at);
+      if (res) rv[u].load(res + at);
+    }
+  };
+  if (active && r < hi) load(r);                       // on their way beside the sums
+  join_pairs(pairs, img, slice, cv, sums);
+  const double m = (double)cv.per * cv.hw;
+  const int count = cv.s > 1 ? 1 : (ch1 - ch0) / cv.per, g0 = ch0 / cv.per;
+  for (int g = tid; g < count; g += THREADS) {
+    const double mu = sums[g][0] / m;
+    double var = sums[g][1] / m - mu * mu;
+    if (var < 0.0) var = 0.0;
+    const double is = 1.0 / sqrt(var + (double)eps);
+    float* const put = reinterpret_cast<float*>(&sums[g][0]);
+    put[0] = (float)mu;
+    put[1] = (float)is;
+    if (cut == 0 && (cv.s == 1 || slice % cv.s == 0)) {
+      mean[(size_t)img * cv.groups + g0 + g] = (float)mu;
+      istd[(size_t)img * cv.groups + g0 + g] = (float)is;
+    }
+  }
+  __syncthreads();
+  if (!active) return;
+  float mu[V], is[V], ga[V], be[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const size_t g = (size_t)img * cv.groups + (ch + j) / cv.per;
-    mu[j] = mean[g]; is[j] = istd[g]; ga[j] = gamma[ch + j]; be[j] = ACT == ACT_SILU ? beta[ch + j] : 0.f;
-    ca[j] = coef[2 * g]; cb[j] = coef[2 * g + 1];
+    const float* const got = reinterpret_cast<const float*>(&sums[(ch + j) / cv.per - g0][0]);
+    mu[j] = got[0]; is[j] = got[1];
   }
-  const int lo = slab * cv.rows_per_slab, hi = min(lo + cv.rows_per_slab, cv.hw);
+  load_params<V>(gamma + ch, ga);
+  load_params<V>(beta + ch, be);
+  for (; r < hi; r += 2 * cv.rpi) {
+    if (r != lo + lane_r) load(r);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if (r + u * cv.rpi >= hi) continue;
+      float o[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        float z = fmaf((xv[u].get(j) - mu[j]) * is[j], ga[j], be[j]);
+        if (res) z += rv[u].get(j);
+        o[j] = act<ACT>(z);
+      }
+      Vec<T, V> out;
+      out.set(o);
+      out.store(y + base + (size_t)(r + u * cv.rpi) * cv.c);
+    }
+  }
+}
+
+// The workgroups from `blocks` on add up dgamma and dbeta.
+template <int ACT, class T, int V>
+__global__ __launch_bounds__(THREADS) void gn_bwd_apply_kernel(const T* x, const T* dy, const T* side, const float* __restrict__ gamma,
+                                                               const float* __restrict__ beta, const float* __restrict__ mean, const float* __restrict__ istd,
+                                                               const double* __restrict__ pairs, const float* __restrict__ chan, T* dx, T* dres,
+                                                               float* __restrict__ dgamma, float* __restrict__ dbeta, long chan_rows, int blocks, Cover cv) {
+  __shared__ double sums[kMaxCoverGroups][2];
+  if ((int)blockIdx.x >= blocks) {
+    sum_params(chan, dgamma, dbeta, chan_rows, cv.c, (int)blockIdx.x - blocks, &sums[0][0]);
+    return;
+  }
+  const int tid = threadIdx.x, lane_r = tid / cv.tpr, lane_c = tid - lane_r * cv.tpr;
+  const int slice = blockIdx.x % cv.slices, rest = blockIdx.x / cv.slices, cut = rest % cv.cuts, img = rest / cv.cuts;
+  const int ch0 = cv.first(slice), ch1 = cv.end(slice), ch = ch0 + lane_c * V;
+  const bool active = lane_r < cv.rpi && ch < ch1;
+  const int lo = cut * cv.rows_per_cut, hi = min(lo + cv.rows_per_cut, cv.hw);
   const size_t base = (size_t)img * cv.hw * cv.c + ch;
-  for (int r = lo + lane_r; r < hi; r += cv.rpi) {
-    const size_t at = base + (size_t)r * cv.c;
-    Vec<T, V> xv, dv, sv;
+  int r = lo + lane_r;
+  Vec<T, V> xv, dv, sv;
+  auto load = [&](int row) {
+    const size_t at = base + (size_t)row * cv.c;
     xv.load(x + at);
     dv.load(dy + at);
     if (ACT != ACT_NONE && side) sv.load(side + at);
+  };
+  if (active && r < hi) load(r);
+  join_pairs(pairs, img, slice, cv, sums);
+  if (!active) return;
+  const int g0 = ch0 / cv.per;
+  const double m = (double)cv.per * cv.hw;
+  float mu[V], is[V], ga[V], be[V], ca[V], cb[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int g = (ch + j) / cv.per;
+    mu[j] = mean[(size_t)img * cv.groups + g]; is[j] = istd[(size_t)img * cv.groups + g];
+    ca[j] = (float)(sums[g - g0][0] / m); cb[j] = (float)(sums[g - g0][1] / m);
+  }
+  load_params<V>(gamma + ch, ga);
+  load_params<V>(beta + ch, be);
+  for (; r < hi; r += cv.rpi) {
+    if (r != lo + lane_r) load(r);
+    const size_t at = base + (size_t)r * cv.c;
     float o[V], gv[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
@@ -293,11 +420,12 @@ __global__ __launch_bounds__(THREADS) void gn_bwd_apply_kernel(const T* x, const
                                      ACT == ACT_SILU && side ? sv.get(j) : 0.f);
       o[j] = is[j] * (gv[j] * ga[j] - ca[j] - xh * cb[j]);
     }
-    xv.set(o);
-    xv.store(dx + at);
+    Vec<T, V> out;
+    out.set(o);
+    out.store(dx + at);
     if (dres) {
-      xv.set(gv);
-      xv.store(dres + at);
+      out.set(gv);
+      out.store(dres + at);
     }
   }
 }
@@ -310,32 +438,41 @@ __global__ __launch_bounds__(THREADS) void gn_bwd_apply_kernel(const T* x, const
 struct Slice {
   int hw, c, groups, per;
   int k, s, slices;                                    // groups and channels of a slice, slices of an image
-  int tpr, rpi;
+  int tpr, rpi, trips, rest;                           // hw = trips * rpi + rest
   int all;                                             // slices of all images
 };
 
-// sums over a wave; the first lane's order is fixed
+// The sum over a wave, in every lane, in a fixed order: neighbouring lanes first, by moves that stay in registers (a butterfly through LDS is six
+// trips one after the other).
 __device__ __forceinline__ float wave_sum_f(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+#if defined(__HIP_DEVICE_COMPILE__)
+#define ACC_DPP(ctrl, rows) __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl, rows, 0xf, true))
+  v += ACC_DPP(0x111, 0xf);                            // lanes 1, 2, 4, 8 to the left within a row of sixteen
+  v += ACC_DPP(0x112, 0xf);
+  v += ACC_DPP(0x114, 0xf);
+  v += ACC_DPP(0x118, 0xf);
+  v += ACC_DPP(0x142, 0xa);                            // the row's last lane to the next row
+  v += ACC_DPP(0x143, 0xc);                            // lane 31 to the upper half
+#undef ACC_DPP
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+#else
   return v;
+#endif
 }
-
-// Values of the threads, added up per group: val[NV] of a thread belong to NV parts of its channels.  red: NT * NV floats, out: one per group, finish() of the sum.
+// Values of the threads, added up per group: val[NV] of a thread belong to NV parts of its channels; `to`: where they go in red, whose
+// entries of a group lie side by side (count of them).  out: one per group, finish() of the sum.
 template <int NT, int NV, class F>
-__device__ __forceinline__ void group_sums(const float (&val)[NV], float* red, float* out, const Slice& sl, bool active, F finish) {
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+__device__ __forceinline__ void group_sums(const float (&val)[NV], const int (&to)[NV], float* red, float* out, int groups, int count, F finish) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) red[tid * NV + j] = active ? val[j] : 0.f;
+  for (int j = 0; j < NV; ++j)
+    if (to[j] >= 0) red[to[j]] = val[j];
   __syncthreads();
-  // a row of red: tpr * NV parts, of which each group has `parts` neighbouring ones
-  const int width = sl.tpr * NV, parts = width / sl.k, count = parts * sl.rpi;
-  for (int g = wave; g < sl.k; g += NT / 64) {
+  for (int g = wave; g < groups; g += NT / 64) {
     float t = 0.f;
-    for (int i = lane; i < count; i += 64) {
-      const int r = i / parts, j = i - r * parts;
-      t += red[r * width + g * parts + j];
-    }
+    int i = lane;
+    for (; i + 192 < count; i += 256) t += (red[g * count + i] + red[g * count + i + 64]) + (red[g * count + i + 128] + red[g * count + i + 192]);
+    for (; i < count; i += 64) t += red[g * count + i];
     t = wave_sum_f(t);
     if (lane == 0) out[g] = finish(t);
   }
@@ -382,7 +519,7 @@ __global__ __launch_bounds__(NT) void gn_fwd_slice_kernel(const T* x, const floa
   const int img = at / sl.slices, slice = at - img * sl.slices, tid = threadIdx.x, row0 = tid / sl.tpr, col = tid - row0 * sl.tpr;
   const int ch = slice * sl.s + col * V;
   const bool active = row0 < sl.rpi;
-  const int rows = active && row0 < sl.hw ? (sl.hw - 1 - row0) / sl.rpi + 1 : 0;       // of this thread
+  const int rows = active ? sl.trips + (row0 < sl.rest ? 1 : 0) : 0;      // of this thread
   // (an image is less than 4 GiB: byte offsets of 32 bits beside addresses that the workgroup shares, worked out anew for every pass)
   const size_t base = (size_t)img * sl.hw * sl.c + (size_t)slice * sl.s;
   const uint32_t off0 = rows > 0 ? ((uint32_t)row0 * (uint32_t)sl.c + (uint32_t)(col * V)) * (uint32_t)sizeof(T) : 0u;
@@ -397,8 +534,8 @@ __global__ __launch_bounds__(NT) void gn_fwd_slice_kernel(const T* x, const floa
     to += step;
   }
   float ga[V], be[V];
-#pragma unroll
-  for (int j = 0; j < V; ++j) { ga[j] = active ? gamma[ch + j] : 0.f; be[j] = active ? beta[ch + j] : 0.f; }
+  load_params<V>(gamma + (active ? ch : 0), ga);
+  load_params<V>(beta + (active ? ch : 0), be);
   const float m = (float)sl.hw * (float)sl.per;
   float val[NV];
 #pragma unroll
@@ -420,12 +557,18 @@ __global__ __launch_bounds__(NT) void gn_fwd_slice_kernel(const T* x, const floa
       add(v);
       pause<R>(u);
     }
-  group_sums<NT, NV>(val, red, mu_sh, sl, active, [&](float t) { return t / m; });
-  int g[NV];
+  // a row of threads has tpr * NV parts, a group `parts` neighbouring ones
+  const int parts = sl.tpr * NV / sl.k, count = parts * sl.rpi;
+  int g[NV], to_red[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    g[j] = active ? (col * NV + j) / parts : 0;
+    to_red[j] = active ? g[j] * count + row0 * parts + (col * NV + j - g[j] * parts) : -1;
+  }
+  group_sums<NT, NV>(val, to_red, red, mu_sh, sl.k, count, [&](float t) { return t / m; });
   float mu[NV];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    g[j] = active ? (col * V + j) / sl.per : 0;
     mu[j] = mu_sh[g[j]];
     val[j] = 0.f;
   }
@@ -441,7 +584,7 @@ __global__ __launch_bounds__(NT) void gn_fwd_slice_kernel(const T* x, const floa
       add(v);
       pause<R>(u);
     }
-  group_sums<NT, NV>(val, red, is_sh, sl, active, [&](float t) { return (float)(1.0 / sqrt((double)(t / m) + (double)eps)); });
+  group_sums<NT, NV>(val, to_red, red, is_sh, sl.k, count, [&](float t) { return (float)(1.0 / sqrt((double)(t / m) + (double)eps)); });
   for (int i = tid; i < sl.k; i += NT) {
     const size_t to = (size_t)img * sl.groups + slice * sl.k + i;
     mean[to] = mu_sh[i];
@@ -492,7 +635,7 @@ __global__ __launch_bounds__(NT) void gn_bwd_slice_kernel(const T* x, const T* d
   const int img = at / sl.slices, slice = at - img * sl.slices, tid = threadIdx.x, row0 = tid / sl.tpr, col = tid - row0 * sl.tpr;
   const int ch = slice * sl.s + col * V;
   const bool active = row0 < sl.rpi;
-  const int rows = active && row0 < sl.hw ? (sl.hw - 1 - row0) / sl.rpi + 1 : 0;
+  const int rows = active ? sl.trips + (row0 < sl.rest ? 1 : 0) : 0;
   const size_t base = (size_t)img * sl.hw * sl.c + (size_t)slice * sl.s;
   const uint32_t off0 = rows > 0 ? ((uint32_t)row0 * (uint32_t)sl.c + (uint32_t)(col * V)) * (uint32_t)sizeof(T) : 0u;
   const uint32_t step = (uint32_t)sl.rpi * (uint32_t)sl.c * (uint32_t)sizeof(T);
@@ -509,8 +652,8 @@ __global__ __launch_bounds__(NT) void gn_bwd_slice_kernel(const T* x, const T* d
   }
   float ga[V], be[V], mu[NV], is[NV];
   int g[NV];
-#pragma unroll
-  for (int j = 0; j < V; ++j) { ga[j] = active ? gamma[ch + j] : 0.f; be[j] = active && act_kind == ACT_SILU ? beta[ch + j] : 0.f; }
+  load_params<V>(gamma + (active ? ch : 0), ga);
+  load_params<V>(beta + (active ? ch : 0), be);
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     g[j] = active ? (col * V + j) / sl.per : 0;
@@ -624,7 +767,9 @@ __global__ __launch_bounds__(NT) void gn_bwd_slice_kernel(const T* x, const T* d
 }
 
 // The slices of a tensor, if they fit: 64 bytes of channels (a line of memory is then read by two workgroups at most) or as many groups as it takes for
-// whole threads; 32 where 64 do not fit.  Threads and rows of a workgroup: the fewest threads whose registers hold a slice.
+// whole threads; 32 bytes where 64 do not fit.  Threads and rows of a workgroup: the fewest threads whose registers hold a slice.  Not where a few workgroups would have long
+// slices to work on and the rest of the chip nothing: there the two launches, which cut an image's rows, are faster.
+constexpr int kSliceGroups = 128, kSliceValues = 20000;
 struct SliceCfg {
   Slice sl;
   int nt, r;                                           // 0: does not fit
@@ -643,7 +788,7 @@ SliceCfg slice_cfg(int n, int hw, int c, int groups, int v, int es, bool backwar
     if (!nt || (long)n * (groups / k) * nt >= (1L << 32) - 8192) return false;         // (a launch has fewer than 2^32 threads)
     f.nt = nt;
     f.r = rows(nt);
-    f.sl = Slice{hw, c, groups, per, k, k * per, groups / k, tpr, nt / tpr, n * (groups / k)};
+    f.sl = Slice{hw, c, groups, per, k, k * per, groups / k, tpr, nt / tpr, hw / (nt / tpr), hw % (nt / tpr), n * (groups / k)};
     return true;
   };
   int narrow = 0;                                      // the widest slice of 32 bytes or more that is narrower than 64
@@ -654,30 +799,69 @@ SliceCfg slice_cfg(int n, int hw, int c, int groups, int v, int es, bool backwar
       if (bytes >= 32) narrow = k;
       continue;
     }
-    if (!fits(k) && narrow) fits(narrow);
+    if (fits(k)) {
+      if (f.sl.all < kSliceGroups && (long)hw * k * per > kSliceValues) f.nt = 0;
+    } else if (narrow && fits(narrow) && f.sl.all < 4 * kSliceGroups) {
+      f.nt = 0;
+    }
     return f;
   }
   return f;
 }
 
-// `images` x slabs workgroups, about four per compute unit, at least 4 trips of U rows each
-Cover cover(int n, int hw, int c, int groups, int v, long target) {
+// How the two launches cover a tensor, V channels per thread; false: a row has no slices of whole threads (then one value at a time does).
+constexpr long kSumGroups = 1024, kApplyGroups = 2048;   // workgroups, about
+bool cover(int n, int hw, int c, int groups, int v, Cover* out) {
   Cover cv{};
   cv.hw = hw; cv.c = c; cv.groups = groups; cv.per = c / groups;
-  const int cols = (c + v - 1) / v;
-  cv.slices = (cols + THREADS - 1) / THREADS;
-  cv.tpr = (cols + cv.slices - 1) / cv.slices;
+  if (c % v) return false;
+  const int most = THREADS * v;
+  if (cv.per > most) {                                 // a group is several slices
+    if (cv.per % v) return false;
+    cv.k = 1;
+    cv.s = (cv.per + most - 1) / most;
+    cv.width = ((cv.per + cv.s - 1) / cv.s + v - 1) / v * v;
+    cv.slices = groups * cv.s;
+  } else {
+    int step = 1;                                      // groups that are whole threads
+    while (step * cv.per % v) ++step;
+    if (step * cv.per > most) return false;
+    int fit = most / (step * cv.per) * step;
+    if (fit > kMaxCoverGroups) fit = kMaxCoverGroups;  // (a multiple of step, which divides v)
+    cv.s = 1;
+    cv.slices = (groups + fit - 1) / fit;
+    cv.k = ((groups + cv.slices - 1) / cv.slices + step - 1) / step * step;
+    cv.slices = (groups + cv.k - 1) / cv.k;
+    cv.width = cv.k * cv.per;
+  }
+  cv.tpr = cv.width / v;
   cv.rpi = THREADS / cv.tpr;
-  long slabs = (target + (long)n * cv.slices - 1) / ((long)n * cv.slices);
-  const long most = ((long)hw + (long)cv.rpi * U - 1) / ((long)cv.rpi * U);
-  if (slabs > most) slabs = most;
-  if (slabs > kGnMaxSlabs) slabs = kGnMaxSlabs;
-  if (slabs < 1) slabs = 1;
-  cv.rows_per_slab = (int)((hw + slabs - 1) / slabs);
-  cv.slabs = (hw + cv.rows_per_slab - 1) / cv.rows_per_slab;
-  return cv;
+  auto parts = [&](long target, int trips, long limit, int* count, int* rows) {
+    long p = (target + (long)n * cv.slices - 1) / ((long)n * cv.slices);
+    const long enough = ((long)hw + (long)cv.rpi * trips - 1) / ((long)cv.rpi * trips);
+    if (p > enough) p = enough;
+    if (p > limit) p = limit;
+    if (p < 1) p = 1;
+    *rows = (int)((hw + p - 1) / p);
+    *count = (hw + *rows - 1) / *rows;
+  };
+  // (every workgroup of the second launch joins an image's slabs: more than 64 only where they are large)
+  const long mib = ((long)hw * c) >> 18;
+  parts(kSumGroups, 4, mib < 64 ? 64 : mib < kGnMaxSlabs ? mib : kGnMaxSlabs, &cv.slabs, &cv.rows_per_slab);
+  parts(kApplyGroups, 4, 1L << 30, &cv.cuts, &cv.rows_per_cut);
+  *out = cv;
+  return true;
 }
-constexpr long kSumGroups = 1024, kApplyGroups = 4096;
+// four or eight values per thread where rows allow it
+int cover_for(int n, int hw, int c, int groups, int dtype, Cover* cv) {
+  const int v = dtype == DT_F32 ? 4 : 8;
+  if (cover(n, hw, c, groups, v, cv)) return v;
+  cover(n, hw, c, groups, 1, cv);
+  return 1;
+}
+// sums of the slabs, per group (fp64) and, backward, per channel (fp32)
+size_t pair_bytes(int n, const Cover& cv) { return (size_t)n * cv.slabs * cv.slots() * 2 * sizeof(double); }
+size_t chan_bytes(int n, const Cover& cv) { return (size_t)n * cv.slabs * 2 * cv.c * sizeof(float); }
 
 struct GnArgs {
   const void *x, *dy, *side;
@@ -693,30 +877,24 @@ struct GnArgs {
 };
 
 template <int ACT, class T, int V>
-void forward_any(const GnArgs& a) {
-  const Cover cv = cover(a.n, a.hw, a.c, a.groups, V, kSumGroups), ca = cover(a.n, a.hw, a.c, a.groups, V, kApplyGroups);
-  double* part = static_cast<double*>(a.workspace);
-  const int all = a.n * a.groups;
-  hipLaunchKernelGGL((gn_sums_kernel<0, ACT_NONE, T, V>), dim3((unsigned)(a.n * cv.slabs * cv.slices)), dim3(THREADS), 0, a.st, (const T*)a.x,
-                     (const T*)nullptr, (const T*)nullptr, nullptr, nullptr, nullptr, nullptr, part, cv);
-  hipLaunchKernelGGL(gn_fwd_finish_kernel, dim3((all + THREADS / 64 - 1) / (THREADS / 64)), dim3(THREADS), 0, a.st, part, a.mean, a.istd, cv, all, a.eps);
-  hipLaunchKernelGGL((gn_apply_kernel<ACT, T, V>), dim3((unsigned)(a.n * ca.slabs * ca.slices)), dim3(THREADS), 0, a.st, (const T*)a.x, a.gamma, a.beta,
-                     (const T*)a.side, a.mean, a.istd, (T*)a.out, ca);
+void forward_any(const GnArgs& a, const Cover& cv) {
+  double* pairs = static_cast<double*>(a.workspace);
+  hipLaunchKernelGGL((gn_sums_kernel<0, ACT_NONE, T, V>), dim3((unsigned)((long)a.n * cv.slabs * cv.slices)), dim3(THREADS), 0, a.st, (const T*)a.x,
+                     (const T*)nullptr, (const T*)nullptr, nullptr, nullptr, nullptr, nullptr, pairs, nullptr, cv);
+  hipLaunchKernelGGL((gn_apply_kernel<ACT, T, V>), dim3((unsigned)((long)a.n * cv.cuts * cv.slices)), dim3(THREADS), 0, a.st, (const T*)a.x, a.gamma, a.beta,
+                     (const T*)a.side, pairs, a.mean, a.istd, (T*)a.out, a.eps, cv);
 }
 
 template <int ACT, class T, int V>
-void backward_any(const GnArgs& a) {
-  const Cover cv = cover(a.n, a.hw, a.c, a.groups, V, kSumGroups), ca = cover(a.n, a.hw, a.c, a.groups, V, kApplyGroups);
-  float* chan = static_cast<float*>(a.workspace);
-  const int all = a.n * a.groups;
-  float* coef = chan + 2 * (size_t)a.n * a.c;
-  double* part = reinterpret_cast<double*>(chan + ((2 * (size_t)a.n * a.c + 2 * (size_t)all + 3) & ~(size_t)3));
-  hipLaunchKernelGGL((gn_sums_kernel<1, ACT, T, V>), dim3((unsigned)(a.n * cv.slabs * cv.slices)), dim3(THREADS), 0, a.st, (const T*)a.x,
-                     (const T*)a.dy, (const T*)a.side, a.gamma, a.beta, a.mean_in, a.istd_in, part, cv);
-  hipLaunchKernelGGL(gn_bwd_finish_kernel, dim3((all + THREADS / 64 - 1) / (THREADS / 64)), dim3(THREADS), 0, a.st, part, a.gamma, chan, coef, cv, all);
-  hipLaunchKernelGGL((gn_bwd_apply_kernel<ACT, T, V>), dim3((unsigned)(a.n * ca.slabs * ca.slices)), dim3(THREADS), 0, a.st, (const T*)a.x,
-                     (const T*)a.dy, (const T*)a.side, a.gamma, a.beta, a.mean_in, a.istd_in, coef, (T*)a.out, (T*)a.dres, ca);
-  hipLaunchKernelGGL(gn_params_kernel, dim3((2 * a.c + 31) / 32), dim3(THREADS), 0, a.st, chan, a.dgamma, a.dbeta, a.n, a.c);
+void backward_any(const GnArgs& a, const Cover& cv) {
+  double* pairs = static_cast<double*>(a.workspace);
+  float* chan = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + pair_bytes(a.n, cv));
+  hipLaunchKernelGGL((gn_sums_kernel<1, ACT, T, V>), dim3((unsigned)((long)a.n * cv.slabs * cv.slices)), dim3(THREADS), 0, a.st, (const T*)a.x,
+                     (const T*)a.dy, (const T*)a.side, a.gamma, a.beta, a.mean_in, a.istd_in, pairs, chan, cv);
+  const int blocks = (int)((long)a.n * cv.cuts * cv.slices), params = (2 * a.c + 31) / 32;
+  hipLaunchKernelGGL((gn_bwd_apply_kernel<ACT, T, V>), dim3((unsigned)(blocks + params)), dim3(THREADS), 0, a.st, (const T*)a.x, (const T*)a.dy,
+                     (const T*)a.side, a.gamma, a.beta, a.mean_in, a.istd_in, pairs, chan, (T*)a.out, (T*)a.dres, a.dgamma, a.dbeta, (long)a.n * cv.slabs, blocks,
+                     cv);
 }
 
 template <class T, int V, int R, int NT, bool PERCH>
@@ -764,37 +942,43 @@ bool by_slices(const GnArgs& a, int act, int dtype, bool backward) {
   return a.c % 8 == 0 && slices<bf16_t, 8>(a, act, backward);
 }
 
-#define ACC_GN_ACT(F, T, V)                        \
-  switch (act) {                                   \
-    case ACT_NONE: F<ACT_NONE, T, V>(a); break;    \
-    case ACT_RELU: F<ACT_RELU, T, V>(a); break;    \
-    default: F<ACT_SILU, T, V>(a); break;          \
+#define ACC_GN_ACT(F, T, V)                            \
+  switch (act) {                                       \
+    case ACT_NONE: F<ACT_NONE, T, V>(a, cv); break;    \
+    case ACT_RELU: F<ACT_RELU, T, V>(a, cv); break;    \
+    default: F<ACT_SILU, T, V>(a, cv); break;          \
   }
-#define ACC_GN(F)                                                                                             \
-  do {                                                                                                        \
-    if (dtype == DT_F32) { if (a.c % 4 == 0) ACC_GN_ACT(F, float, 4) else ACC_GN_ACT(F, float, 1) }            \
-    else { if (a.c % 8 == 0) ACC_GN_ACT(F, bf16_t, 8) else ACC_GN_ACT(F, bf16_t, 1) }                          \
+#define ACC_GN(F)                                                                                  \
+  do {                                                                                             \
+    Cover cv;                                                                                      \
+    const int v = cover_for(a.n, a.hw, a.c, a.groups, dtype, &cv);                                 \
+    if (dtype == DT_F32) { if (v == 4) ACC_GN_ACT(F, float, 4) else ACC_GN_ACT(F, float, 1) }      \
+    else { if (v == 8) ACC_GN_ACT(F, bf16_t, 8) else ACC_GN_ACT(F, bf16_t, 1) }                    \
   } while (0)
 
 bool shape_ok(int n, int hw, int c, int groups, int act, int dtype) {
   if (n <= 0 || hw <= 0 || c <= 0 || groups <= 0 || c % groups != 0 || act < ACT_NONE || act > ACT_SILU) return false;
   if (dtype != DT_F32 && dtype != DT_BF16) return false;
-  // a launch has fewer than 2^32 threads (beyond an image each, the workgroups are at most kApplyGroups), a thread counts its rows in 31 bits
-  const long slices = ((long)c + THREADS - 1) / THREADS;
-  return (long)n * groups < (1L << 26) && n * slices + kApplyGroups < (1L << 24) && hw < (1 << 30) && c < (1 << 24);
+  if (hw >= (1 << 30) || c >= (1 << 24) || (long)n * groups >= 1L << 31) return false;      // (a thread counts its rows in 31 bits)
+  Cover cv;
+  cover_for(n, hw, c, groups, dtype, &cv);
+  const long most = (long)n * cv.slices * (cv.slabs > cv.cuts ? cv.slabs : cv.cuts) + (2L * c + 31) / 32;
+  return most < 1L << 24;                              // (a launch has fewer than 2^32 threads)
 }
 
 }  // namespace
 
 size_t gn_workspace_bytes(int n, int hw, int c, int groups) {
-  if (!shape_ok(n, hw, c, groups, ACT_NONE, DT_F32)) return 0;
-  // the sums of the backward pass, whichever width a thread has: per image and slab 2 c doubles, per image 2 c floats, two per group
-  int slabs = 0;
-  for (int v : {1, 4, 8}) {
-    const int s = cover(n, hw, c, groups, v, kSumGroups).slabs;
-    if (s > slabs) slabs = s;
+  if (!shape_ok(n, hw, c, groups, ACT_NONE, DT_F32) || !shape_ok(n, hw, c, groups, ACT_NONE, DT_BF16)) return 0;
+  // the sums of a backward pass in slabs, or one pair of sums per image and channel; whichever storage type needs more
+  size_t most = (size_t)n * 2 * c * sizeof(float);
+  for (int dtype : {(int)DT_F32, (int)DT_BF16}) {
+    Cover cv;
+    cover_for(n, hw, c, groups, dtype, &cv);
+    const size_t b = pair_bytes(n, cv) + chan_bytes(n, cv);
+    if (b > most) most = b;
   }
-  return (size_t)n * slabs * 2 * c * sizeof(double) + (((size_t)2 * n * c + (size_t)2 * n * groups + 3) & ~(size_t)3) * sizeof(float);
+  return most;
 }
 
 hipError_t gn_forward(const void* x, const float* gamma, const float* beta, const void* res, void* y, float* mean, float* istd, int n, int hw, int c,

@@ -90,7 +90,7 @@ template <> struct Wide<bf16_t> {
   static __device__ __forceinline__ void store(bf16_t* p, const float (&v)[8]) {
     vec q;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) q[i] = (uint32_t)float_to_bf16(v[2 * i]) | ((uint32_t)float_to_bf16(v[2 * i + 1]) << 16);
+    for (int i = 0; i < 4; ++i) q[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
     *reinterpret_cast<vec*>(p) = q;
   }
 };

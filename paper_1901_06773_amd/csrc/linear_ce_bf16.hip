@@ -24,10 +24,6 @@ __device__ __forceinline__ float exp_fast(float t) {
 #endif
 }
 
-typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
-typedef float v2f __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t pack2(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(v2f{a, b}, v2bf)); }
-
 // Tile `at` of a launch: every XCD takes a contiguous range (neighbours share operand rows in its L2), rows innermost.
 __device__ __forceinline__ int xcd_tile(int blocks) { return ((int)blockIdx.x & 7) * (blocks >> 3) + ((int)blockIdx.x >> 3); }
 
@@ -199,14 +195,14 @@ __global__ __launch_bounds__(C::THREADS, 2) void lce_dz_kernel(LogitArgs a, int 
           if (edge && n0 + wn0 + 32 * j + 8 * q + 4 * (lane >> 5) + e >= a.cols) p[e] = 0.f;
           sum[j][4 * q + e] += p[e];
         }
-        hi.x = pack2(p[0], p[1]);
-        hi.y = pack2(p[2], p[3]);
+        hi.x = pack_bf16(p[0], p[1]);
+        hi.y = pack_bf16(p[2], p[3]);
         l[0] = p[0] - __uint_as_float(hi.x << 16);
         l[1] = p[1] - __uint_as_float(hi.x & 0xffff0000u);
         l[2] = p[2] - __uint_as_float(hi.y << 16);
         l[3] = p[3] - __uint_as_float(hi.y & 0xffff0000u);
-        lo.x = pack2(l[0], l[1]);
-        lo.y = pack2(l[2], l[3]);
+        lo.x = pack_bf16(l[0], l[1]);
+        lo.y = pack_bf16(l[2], l[3]);
         char* const to = stg + (lane & 31) * EP + (32 * j + 8 * q + 4 * (lane >> 5)) * 2;
         *reinterpret_cast<uint2*>(to) = hi;
         *reinterpret_cast<uint2*>(to + 32 * EP) = lo;
