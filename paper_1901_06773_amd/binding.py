@@ -611,21 +611,39 @@ def op_softmax_ce(z, labels, loss_rows, loss, dz):
         raise AccError(rc, "acc_op_softmax_ce")
 
 
+_torch = None
+
+
+def _here():
+    """torch, the current device and the handle of its current stream."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    try:
+        device = _torch._C._cuda_getDevice()
+        return _torch, device, _torch._C._cuda_getCurrentRawStream(device)
+    except AttributeError:
+        return _torch, _torch.cuda.current_device(), _torch.cuda.current_stream().cuda_stream
+
+
 def _fits(name, what, t, shape, dtype, device):
-    """Refuses a tensor that the library would read or write otherwise than the caller means."""
-    if t.shape != shape or t.dtype != dtype or t.get_device() != device or not t.is_contiguous():
+    """Refuses a tensor that the library would read or write otherwise than the caller means; its address."""
+    if t.dtype is not dtype or t.get_device() != device or t.shape != shape or not t.is_contiguous():
         raise AccError(ACC_EINVAL, f"{name}: {what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on the current device (cuda:{device}), "
                                    f"got {t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
+    return t.data_ptr()
 
 
 def _space(name, ws, device):
     if ws.get_device() != device or not ws.is_contiguous():
         raise AccError(ACC_EINVAL, f"{name}: the workspace must be contiguous and on the current device (cuda:{device}), got {ws.device}")
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    return ws.data_ptr(), ws.nbytes
 
 
-def _ptr(t):
-    return t.data_ptr() if t is not None else None
+def _done(rc):
+    if rc != ACC_OK:
+        raise AccError(rc, _lib.acc_last_error(None).decode())
 
 
 def op_gn_workspace(n, hw, c, groups) -> int:
@@ -634,42 +652,32 @@ def op_gn_workspace(n, hw, c, groups) -> int:
 
 def op_gn_fwd(x, gamma, beta, res, y, mean, istd, groups, act, eps, ws):
     """x, res (or None) and y [n, ..., c], gamma and beta [c], mean and istd [n, groups]; act: ACT_NONE, ACT_RELU, ACT_SILU."""
-    import torch
-    device, f32 = torch.cuda.current_device(), torch.float32
-    shape, dtype = x.shape, _dtype_of(x)
+    torch, device, stream = _here()
+    name, shape, kind, f32, dtype = "op_gn_fwd", x.shape, x.dtype, torch.float32, _dtype_of(x)
     n, c = shape[0], shape[-1]
-    _fits("op_gn_fwd", "x", x, shape, x.dtype, device)
-    _fits("op_gn_fwd", "y", y, shape, x.dtype, device)
-    if res is not None:
-        _fits("op_gn_fwd", "res", res, shape, x.dtype, device)
-    for what, t, like in (("gamma", gamma, (c,)), ("beta", beta, (c,)), ("mean", mean, (n, groups)), ("istd", istd, (n, groups))):
-        _fits("op_gn_fwd", what, t, like, f32, device)
-    at, size = _space("op_gn_fwd", ws, device)
-    rc = _lib.acc_op_gn_fwd(x.data_ptr(), gamma.data_ptr(), beta.data_ptr(), _ptr(res), y.data_ptr(), mean.data_ptr(), istd.data_ptr(), n,
-                            x.numel() // max(n * c, 1), c, groups, act, eps, at, size, dtype, _stream_ptr(torch))
-    if rc != ACC_OK:
-        raise AccError(rc, _lib.acc_last_error(None).decode())
+    at, size = _space(name, ws, device)
+    _done(_lib.acc_op_gn_fwd(_fits(name, "x", x, shape, kind, device), _fits(name, "gamma", gamma, (c,), f32, device),
+                             _fits(name, "beta", beta, (c,), f32, device), None if res is None else _fits(name, "res", res, shape, kind, device),
+                             _fits(name, "y", y, shape, kind, device), _fits(name, "mean", mean, (n, groups), f32, device),
+                             _fits(name, "istd", istd, (n, groups), f32, device), n, x.numel() // max(n * c, 1), c, groups, act, eps, at, size, dtype,
+                             stream))
 
 
 def op_gn_bwd(x, dy, y, res, gamma, beta, mean, istd, dx, dgamma, dbeta, dres, groups, act, ws):
     """Gradients of op_gn_fwd: dx, dgamma, dbeta and, if wanted, dres (may be dy).  y: the stored output (ACT_RELU, else None);
     res: the residual of the forward pass (ACT_SILU, or None)."""
-    import torch
-    device, f32 = torch.cuda.current_device(), torch.float32
-    shape, dtype = x.shape, _dtype_of(x)
+    torch, device, stream = _here()
+    name, shape, kind, f32, dtype = "op_gn_bwd", x.shape, x.dtype, torch.float32, _dtype_of(x)
     n, c = shape[0], shape[-1]
-    for what, t in (("x", x), ("dy", dy), ("dx", dx), ("y", y), ("res", res), ("dres", dres)):
-        if t is not None:
-            _fits("op_gn_bwd", what, t, shape, x.dtype, device)
-    for what, t, like in (("gamma", gamma, (c,)), ("beta", beta, (c,)), ("mean", mean, (n, groups)), ("istd", istd, (n, groups)),
-                          ("dgamma", dgamma, (c,)), ("dbeta", dbeta, (c,))):
-        _fits("op_gn_bwd", what, t, like, f32, device)
-    at, size = _space("op_gn_bwd", ws, device)
-    rc = _lib.acc_op_gn_bwd(x.data_ptr(), dy.data_ptr(), _ptr(y), _ptr(res), gamma.data_ptr(), beta.data_ptr(), mean.data_ptr(), istd.data_ptr(),
-                            dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), _ptr(dres), n, x.numel() // max(n * c, 1), c, groups, act, at, size, dtype,
-                            _stream_ptr(torch))
-    if rc != ACC_OK:
-        raise AccError(rc, _lib.acc_last_error(None).decode())
+    at, size = _space(name, ws, device)
+    _done(_lib.acc_op_gn_bwd(_fits(name, "x", x, shape, kind, device), _fits(name, "dy", dy, shape, kind, device),
+                             None if y is None else _fits(name, "y", y, shape, kind, device),
+                             None if res is None else _fits(name, "res", res, shape, kind, device), _fits(name, "gamma", gamma, (c,), f32, device),
+                             _fits(name, "beta", beta, (c,), f32, device), _fits(name, "mean", mean, (n, groups), f32, device),
+                             _fits(name, "istd", istd, (n, groups), f32, device), _fits(name, "dx", dx, shape, kind, device),
+                             _fits(name, "dgamma", dgamma, (c,), f32, device), _fits(name, "dbeta", dbeta, (c,), f32, device),
+                             None if dres is None else _fits(name, "dres", dres, shape, kind, device), n, x.numel() // max(n * c, 1), c, groups, act,
+                             at, size, dtype, stream))
 
 
 def op_linear_ce_workspace(n, d, classes, gradients: bool, dtype: int = F32) -> int:
@@ -680,21 +688,18 @@ def op_linear_ce(x, w, bias, labels, loss_rows, loss, dx, dw, db, ws, ignore=Non
     """Softmax cross-entropy of the logits x w^T + bias, which are not kept.  x [n, d] and w [classes, d], bias [classes] fp32 or None, labels
     int32 [n]; loss_rows [n], loss [1], dx like x, dw [classes, d] fp32, db [classes] fp32, each optional.  ignore: the label of rows that
     do not count (None: every row counts)."""
-    import torch
-    device, f32 = torch.cuda.current_device(), torch.float32
-    dtype = _dtype_of(x)
+    torch, device, stream = _here()
+    name, f32, i32, kind, dtype = "op_linear_ce", torch.float32, torch.int32, x.dtype, _dtype_of(x)
     n, d = x.shape
     classes = w.shape[0]
-    for what, t, like, kind in (("x", x, (n, d), x.dtype), ("w", w, (classes, d), x.dtype), ("labels", labels, (n,), torch.int32),
-                                ("bias", bias, (classes,), f32), ("loss_rows", loss_rows, (n,), f32), ("loss", loss, (1,), f32),
-                                ("dx", dx, (n, d), x.dtype), ("dw", dw, (classes, d), f32), ("db", db, (classes,), f32)):
-        if t is not None:
-            _fits("op_linear_ce", what, t, like, kind, device)
-    at, size = _space("op_linear_ce", ws, device)
-    rc = _lib.acc_op_linear_ce(x.data_ptr(), w.data_ptr(), _ptr(bias), labels.data_ptr(), LABEL_NONE if ignore is None else int(ignore), _ptr(loss_rows),
-                               _ptr(loss), _ptr(dx), _ptr(dw), _ptr(db), n, d, classes, at, size, dtype, _stream_ptr(torch))
-    if rc != ACC_OK:
-        raise AccError(rc, _lib.acc_last_error(None).decode())
+
+    def given(what, t, shape, dt):
+        return None if t is None else _fits(name, what, t, shape, dt, device)
+    at, size = _space(name, ws, device)
+    _done(_lib.acc_op_linear_ce(_fits(name, "x", x, (n, d), kind, device), _fits(name, "w", w, (classes, d), kind, device), given("bias", bias, (classes,), f32),
+                                _fits(name, "labels", labels, (n,), i32, device), LABEL_NONE if ignore is None else int(ignore),
+                                given("loss_rows", loss_rows, (n,), f32), given("loss", loss, (1,), f32), given("dx", dx, (n, d), kind),
+                                given("dw", dw, (classes, d), f32), given("db", db, (classes,), f32), n, d, classes, at, size, dtype, stream))
 
 
 class TensorList:
@@ -702,27 +707,21 @@ class TensorList:
     the clipped tensors go (None: in place).  Keeps the tensors alive; their values may change, not their storage."""
 
     def __init__(self, tensors, outs=None):
-        import torch
+        torch, device, stream = _here()
         tensors = list(tensors)
         outs = None if outs is None else list(outs)
         n = len(tensors)
-        self.device = torch.cuda.current_device()
+        self.device = device
         if n == 0 or (outs is not None and len(outs) != n):
             raise AccError(ACC_EINVAL, "TensorList: no tensors, or another number of outputs")
-        for i, t in enumerate(tensors):
-            _fits("TensorList", f"tensor {i}", t, t.shape, t.dtype, self.device)
-            if outs is not None:
-                _fits("TensorList", f"output {i}", outs[i], t.shape, t.dtype, self.device)
         self.tensors, self.outs = tensors, outs
-        counts = (_SZ * n)(*[t.numel() for t in tensors])
         dtypes = (C.c_int32 * n)(*[_dtype_of(t) for t in tensors])
-        src = (_VP * n)(*[t.data_ptr() for t in tensors])
-        dst = None if outs is None else (_VP * n)(*[t.data_ptr() for t in outs])
+        src = (_VP * n)(*[_fits("TensorList", "a tensor", t, t.shape, t.dtype, device) for t in tensors])
+        dst = None if outs is None else (_VP * n)(*[_fits("TensorList", "an output", o, t.shape, t.dtype, device) for t, o in zip(tensors, outs)])
+        counts = (_SZ * n)(*[t.numel() for t in tensors])
         size = int(_lib.acc_op_tensor_list_bytes(counts, n))
-        self.table = torch.empty(max(size, 16), dtype=torch.uint8, device=f"cuda:{self.device}")
-        rc = _lib.acc_op_tensor_list(src, dst, counts, dtypes, n, self.table.data_ptr(), size, _stream_ptr(torch))
-        if rc != ACC_OK:
-            raise AccError(rc, _lib.acc_last_error(None).decode())
+        self.table = torch.empty(max(size, 16), dtype=torch.uint8, device=f"cuda:{device}")
+        _done(_lib.acc_op_tensor_list(src, dst, counts, dtypes, n, self.table.data_ptr(), size, stream))
         self._at, self._size = self.table.data_ptr(), size
 
 
@@ -731,25 +730,17 @@ def op_grad_norm_workspace() -> int:
 
 
 def _norm_call(name, tensors, norm, ws):
-    import torch
-    device = torch.cuda.current_device()
+    torch, device, stream = _here()
     if tensors.device != device:
         raise AccError(ACC_EINVAL, f"{name}: the list lies on cuda:{tensors.device}, the current device is cuda:{device}")
-    _fits(name, "norm", norm, (1,), torch.float32, device)
-    return _space(name, ws, device), _stream_ptr(torch)
+    return (_fits(name, "norm", norm, (1,), torch.float32, device), *_space(name, ws, device), stream)
 
 
 def op_grad_norm(tensors: TensorList, norm, ws):
     """norm [1] fp32: the Euclidean norm over all values of the list."""
-    (at, size), stream = _norm_call("op_grad_norm", tensors, norm, ws)
-    rc = _lib.acc_op_grad_norm(tensors._at, tensors._size, norm.data_ptr(), at, size, stream)
-    if rc != ACC_OK:
-        raise AccError(rc, _lib.acc_last_error(None).decode())
+    _done(_lib.acc_op_grad_norm(tensors._at, tensors._size, *_norm_call("op_grad_norm", tensors, norm, ws)))
 
 
 def op_grad_clip(tensors: TensorList, max_norm, norm, ws):
     """The list's tensors (or their outputs) scaled so that the norm over all of them is max_norm at most; norm [1]: what it was."""
-    (at, size), stream = _norm_call("op_grad_clip", tensors, norm, ws)
-    rc = _lib.acc_op_grad_clip(tensors._at, tensors._size, max_norm, norm.data_ptr(), at, size, stream)
-    if rc != ACC_OK:
-        raise AccError(rc, _lib.acc_last_error(None).decode())
+    _done(_lib.acc_op_grad_clip(tensors._at, tensors._size, max_norm, *_norm_call("op_grad_clip", tensors, norm, ws)))
