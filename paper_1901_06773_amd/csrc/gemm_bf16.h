@@ -1,6 +1,6 @@
 // One tile of a plain matrix product on the bf16 matrix cores, for kernels that do something of their own with it:
 //
-//   acc[m][n] = sum_k A[m][k] * B[k][n]  (+ the same with a second A),   m in [m0, m0 + BM), n in [n0, n0 + BN), k in [k_lo, k_hi)
+//   acc[m][n] = sum_k A[m][k] * B[k][n]  (+ the same with a second and third A),   m in [m0, m0 + BM), n in [n0, n0 + BN), k in [k_lo, k_hi)
 //
 // Each operand lies in memory with its values of k side by side (rows of m resp. n) or with its values of m resp. n side by side (rows of k).
 // Either way 16 bytes at a time go straight into LDS as they lie; of the first kind a lane reads its eight values of k, the second kind is transposed
@@ -31,26 +31,27 @@ template <int WM_, int WN_, int MB_, int NB_, int BK_, int NS_, bool AT_, bool B
   static constexpr int A_PART = A_ROWS * A_PITCH, A_BYTES = A_PART * PARTS, STAGE = A_BYTES + B_ROWS * B_PITCH, LDS = NS * STAGE;
   static_assert(AI * A_STEP == A_ROWS && BI * B_STEP == B_ROWS, "whole load instructions");
   static_assert((AT ? A_STEP % 4 : A_STEP % 16) == 0 && (BT ? B_STEP % 4 : B_STEP % 16) == 0, "a thread's rows are permuted alike");
-  static_assert(BK % 32 == 0 && (AT || BK <= 64) && NS >= 2 && NS <= 3, "an even number of steps of 16; rows of 64 or 128 bytes");
+  static_assert(BK % 32 == 0 && (AT || BK <= 64) && NS >= 2 && NS <= 4 && PARTS <= 3, "an even number of steps of 16; rows of 64 or 128 bytes");
 };
 
 struct GemmOperand {
   const void* p;         // 16-byte aligned
+  const void* more[2];   // the other parts of A
   long rows;             // of m resp. n, or of k
   int cols;              // what lies side by side; a multiple of 8
   int pitch;             // elements between rows; a multiple of 8
 };
 
 // A descriptor of the rows [first, first + count) of an operand (as far as they exist), fewer than 4 GiB of them.
-__device__ __forceinline__ srsrc operand_rows(const GemmOperand& o, long first, long count) {
+__device__ __forceinline__ srsrc operand_rows(const GemmOperand& o, const void* p, long first, long count) {
   const long left = o.rows - first, take = left < count ? left : count;
-  return descriptor(static_cast<const char*>(o.p) + (size_t)first * o.pitch * 2, take > 0 ? (size_t)take * o.pitch * 2 : 0);
+  return descriptor(static_cast<const char*>(p) + (size_t)first * o.pitch * 2, take > 0 ? (size_t)take * o.pitch * 2 : 0);
 }
 
 template <class C> using GemmAcc = v16f[C::MB][C::NB];
 
 template <class C>
-__device__ __forceinline__ void gemm_tile(const GemmOperand& A, const GemmOperand& A2, const GemmOperand& B, int m0, int n0, int k_lo, int k_hi, char* lds,
+__device__ __forceinline__ void gemm_tile(const GemmOperand& A, const GemmOperand& B, int m0, int n0, int k_lo, int k_hi, char* lds,
                                           GemmAcc<C>& acc) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int MB = C::MB, NB = C::NB, AI = C::AI, BI = C::BI, NS = C::NS, PARTS = C::PARTS, BK = C::BK;
@@ -72,14 +73,10 @@ __device__ __forceinline__ void gemm_tile(const GemmOperand& A, const GemmOperan
   const int bcol = C::BT ? (tid % C::B_COLS) ^ (row_xor<C::B_PITCH>(brow) << 2) : (tid % C::B_COLS) ^ swz(brow);
   srsrc rs_a[PARTS], rs_b;
   uint32_t a_voff[AI], b_voff[BI];
-  if constexpr (C::AT) {
-    rs_a[0] = operand_rows(A, 0, A.rows);
-    if constexpr (PARTS == 2) rs_a[1] = operand_rows(A2, 0, A2.rows);
-  } else {
-    rs_a[0] = operand_rows(A, m0, C::BM);
-    if constexpr (PARTS == 2) rs_a[1] = operand_rows(A2, m0, C::BM);
-  }
-  rs_b = C::BT ? operand_rows(B, 0, B.rows) : operand_rows(B, n0, C::BN);
+#pragma unroll
+  for (int part = 0; part < PARTS; ++part)
+    rs_a[part] = operand_rows(A, part == 0 ? A.p : A.more[part - 1], C::AT ? 0 : m0, C::AT ? A.rows : C::BM);
+  rs_b = operand_rows(B, B.p, C::BT ? 0 : n0, C::BT ? B.rows : C::BN);
   const uint32_t a_pitch = (uint32_t)A.pitch * 2u, b_pitch = (uint32_t)B.pitch * 2u;
 #pragma unroll
   for (int i = 0; i < AI; ++i) {
@@ -198,7 +195,9 @@ __device__ __forceinline__ void gemm_tile(const GemmOperand& A, const GemmOperan
   // whose stage the next loads overwrite
   auto open = [&](int j) {
     __builtin_amdgcn_sched_barrier(0);
-    if (NS > 2 && chunks - 1 - j >= 1) wait_loads<(NS > 2 ? L : 0)>();
+    const int later = chunks - 1 - j;                 // chunks behind this one that have been issued, NS - 2 at most
+    if (NS > 3 && later >= 2) wait_loads<(NS > 3 ? 2 * L : 0)>();
+    else if (NS > 2 && later >= 1) wait_loads<(NS > 2 ? L : 0)>();
     else wait_loads<0>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");

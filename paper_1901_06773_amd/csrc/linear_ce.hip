@@ -72,11 +72,9 @@ __global__ __launch_bounds__(THREADS) void row_sums_kernel(const float* __restri
 }
 
 // One wave per row: the splits' m and R joined.
-__global__ __launch_bounds__(THREADS) void join_kernel(const float* __restrict__ part, const float* __restrict__ z_label, const int32_t* __restrict__ labels,
-                                                       int ignore, float* __restrict__ row_max, float* __restrict__ row_rest, float* __restrict__ loss_rows,
-                                                       int n, int splits, int classes) {
-  const int row = blockIdx.x * (THREADS / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (row >= n) return;
+__device__ __forceinline__ float join_row(const float* __restrict__ part, const float* __restrict__ z_label, const int32_t* __restrict__ labels, int ignore,
+                                          float* __restrict__ row_max, float* __restrict__ row_rest, int row, int splits, int classes) {
+  const int lane = threadIdx.x & 63;
   const float* p = part + (size_t)row * 2 * splits;
   float mx = -INFINITY;
   for (int i = lane; i < splits; i += 64) mx = fmaxf(mx, p[i]);
@@ -90,23 +88,33 @@ __global__ __launch_bounds__(THREADS) void join_kernel(const float* __restrict__
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) { s += __shfl_xor(s, o); equal += __shfl_xor(equal, o); }
-  if (lane) return;
   const float rest = mx == -INFINITY ? NAN : s + (equal - 1.f);     // (every class ruled out: no distribution)
-  row_max[row] = mx;
-  row_rest[row] = rest;
   const int lab = labels[row];
   const bool skip = ignore != INT_MIN && lab == ignore, known = (unsigned)lab < (unsigned)classes;
-  loss_rows[row] = skip ? 0.f : known ? log1pf(rest) - (z_label[row] - mx) : NAN;
+  if (lane == 0) {
+    row_max[row] = mx;
+    row_rest[row] = rest;
+  }
+  return skip ? 0.f : known ? log1pf(rest) - (z_label[row] - mx) : NAN;
+}
+__global__ __launch_bounds__(THREADS) void join_kernel(const float* __restrict__ part, const float* __restrict__ z_label, const int32_t* __restrict__ labels,
+                                                       int ignore, float* __restrict__ row_max, float* __restrict__ row_rest, float* __restrict__ loss_rows,
+                                                       int n, int splits, int classes) {
+  const int row = blockIdx.x * (THREADS / 64) + (threadIdx.x >> 6);
+  if (row >= n) return;
+  const float l = join_row(part, z_label, labels, ignore, row_max, row_rest, row, splits, classes);
+  if ((threadIdx.x & 63) == 0) loss_rows[row] = l;
 }
 
-// scale[0] = 1 / rows that count (0 if there is none), loss = scale * sum of the rows, in a fixed order
-__global__ __launch_bounds__(1024) void mean_kernel(const float* __restrict__ loss_rows, const int32_t* __restrict__ labels, int ignore, int n,
-                                                    float* __restrict__ scale, float* __restrict__ loss) {
-  __shared__ double sh[16];
-  __shared__ int counts[16];
+// scale[0] = 1 / rows that count (0 if there is none), loss = their mean, of NT threads and in a fixed order.  Either may be null.
+template <int NT>
+__device__ __forceinline__ void mean_of_rows(const float* loss_rows, const int32_t* __restrict__ labels, int ignore, int n, float* __restrict__ scale,
+                                             float* __restrict__ loss) {
+  __shared__ double sh[NT / 64];
+  __shared__ int counts[NT / 64];
   double s = 0.0;
   int k = 0;
-  for (int i = threadIdx.x; i < n; i += 1024) {
+  for (int i = threadIdx.x; i < n; i += NT) {
     s += (double)loss_rows[i];
     k += ignore == INT_MIN || labels[i] != ignore ? 1 : 0;
   }
@@ -117,9 +125,121 @@ __global__ __launch_bounds__(1024) void mean_kernel(const float* __restrict__ lo
   if (threadIdx.x) return;
   double t = 0.0;
   int rows = 0;
-  for (int w = 0; w < 16; ++w) { t += sh[w]; rows += counts[w]; }
-  scale[0] = rows ? 1.f / (float)rows : 0.f;
+  for (int w = 0; w < NT / 64; ++w) { t += sh[w]; rows += counts[w]; }
+  if (scale) scale[0] = rows ? 1.f / (float)rows : 0.f;
   if (loss) *loss = rows ? (float)(t / (double)rows) : 0.f;
+}
+__global__ __launch_bounds__(1024) void mean_kernel(const float* __restrict__ loss_rows, const int32_t* __restrict__ labels, int ignore, int n,
+                                                    float* __restrict__ scale, float* __restrict__ loss) {
+  mean_of_rows<1024>(loss_rows, labels, ignore, n, scale, loss);
+}
+// both, in one workgroup
+__global__ __launch_bounds__(1024) void join_mean_kernel(const float* __restrict__ part, const float* __restrict__ z_label, const int32_t* __restrict__ labels,
+                                                         int ignore, float* __restrict__ row_max, float* __restrict__ row_rest, float* loss_rows, int n,
+                                                         int splits, int classes, float* __restrict__ scale, float* __restrict__ loss) {
+  for (int row = threadIdx.x >> 6; row < n; row += 16) {
+    const float l = join_row(part, z_label, labels, ignore, row_max, row_rest, row, splits, classes);
+    if ((threadIdx.x & 63) == 0) loss_rows[row] = l;
+  }
+  __threadfence_block();
+  __syncthreads();
+  mean_of_rows<1024>(loss_rows, labels, ignore, n, scale, loss);
+}
+
+// A whole row of logits at once, one workgroup per row, up to V values in a thread's registers: the loss, and with `grads` z -> dz in place, columns beyond
+// the classes zero.  The rows that count are counted by every workgroup, while its logits are on their way.
+template <int V, int NT>
+__global__ __launch_bounds__(NT) void rows_kernel(float* __restrict__ z, const float* __restrict__ bias, const int32_t* __restrict__ labels, int ignore,
+                                                  float* __restrict__ loss_rows, int n, int pitch, int cols, int grads) {
+  __shared__ float sh[3][NT / 64];
+  __shared__ int counted;
+  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  float* const zr = z + (size_t)row * pitch;
+  float v[V];
+#pragma unroll
+  for (int u = 0; u < V; ++u) {
+    const int j = tid + u * NT;
+    v[u] = j < cols ? zr[j] : -INFINITY;
+  }
+  if (bias) {
+#pragma unroll
+    for (int u = 0; u < V; ++u) {
+      const int j = tid + u * NT;
+      if (j < cols) v[u] += bias[j];
+    }
+  }
+  const int lab = labels[row];
+  const bool skip = ignore != INT_MIN && lab == ignore, known = (unsigned)lab < (unsigned)cols;
+  int k = 0;
+  if (grads && ignore != INT_MIN)
+    for (int i = tid; i < n; i += NT) k += labels[i] != ignore ? 1 : 0;
+  if (tid == 0) counted = 0;
+  float mx = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < V; ++u) mx = fmaxf(mx, v[u]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+  if (lane == 0) sh[0][wave] = mx;
+  __syncthreads();
+  if (grads && ignore != INT_MIN) atomicAdd(&counted, k);              // (whole numbers: any order gives the same)
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) mx = fmaxf(mx, sh[0][w]);
+  float s = 0.f, equal = 0.f, t_label = 0.f;
+#pragma unroll
+  for (int u = 0; u < V; ++u) {
+    const int j = tid + u * NT;
+    if (j < cols) {
+      const bool top = v[u] == mx;
+      const float t = v[u] - mx;
+      if (j == lab) t_label = t;
+      v[u] = expf(t);
+      equal += top ? 1.f : 0.f;
+      s += top ? 0.f : v[u];
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) { s += __shfl_xor(s, o); equal += __shfl_xor(equal, o); }
+  if (lane == 0) { sh[1][wave] = s; sh[2][wave] = equal; }
+  __syncthreads();
+  s = equal = 0.f;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) { s += sh[1][w]; equal += sh[2][w]; }
+  const float rest = mx == -INFINITY ? NAN : s + (equal - 1.f);
+  if (known ? tid == lab % NT : tid == 0) loss_rows[row] = skip ? 0.f : known ? log1pf(rest) - t_label : NAN;
+  if (!grads) return;
+  const int rows = ignore == INT_MIN ? n : counted;
+  const float inv = skip || rows == 0 ? 0.f : 1.f / (float)rows / (1.f + rest);
+#pragma unroll
+  for (int u = 0; u < V; ++u) {
+    const int j = tid + u * NT;
+    if (j >= pitch) continue;
+    const float p = j == lab ? expm1f(t_label) - rest : v[u];
+    zr[j] = skip || j >= cols ? 0.f : p * inv;
+  }
+}
+
+// The columns' sums of dz over `per` rows each (straight to db where that is all of them), and in a workgroup of its own the mean loss.
+__global__ __launch_bounds__(THREADS) void columns_kernel(const float* __restrict__ dz, float* __restrict__ out, int n, int pitch, int cols, int per, int blocks,
+                                                          int stride, const float* __restrict__ loss_rows, const int32_t* __restrict__ labels, int ignore,
+                                                          float* __restrict__ loss) {
+  if ((int)blockIdx.x >= blocks) {
+    mean_of_rows<THREADS>(loss_rows, labels, ignore, n, nullptr, loss);
+    return;
+  }
+  const int across = (cols + THREADS - 1) / THREADS, slab = blockIdx.x / across, j = (blockIdx.x - slab * across) * THREADS + threadIdx.x;
+  if (j >= cols) return;
+  double s = 0.0;
+  int r = slab * per;
+  const int end = min(r + per, n);
+  for (; r + 16 <= end; r += 16) {
+    float v[16];
+#pragma unroll
+    for (int u = 0; u < 16; ++u) v[u] = dz[(size_t)(r + u) * pitch + j];
+#pragma unroll
+    for (int u = 0; u < 16; ++u) s += (double)v[u];
+  }
+  for (; r < end; ++r) s += (double)dz[(size_t)r * pitch + j];
+  out[(size_t)slab * stride + j] = (float)s;
 }
 
 // z -> dz in place, columns beyond the classes zero, and the columns' sums over the rows of a workgroup: db_part[workgroup][pitch].
@@ -134,20 +254,25 @@ __global__ __launch_bounds__(THREADS) void dz_kernel(float* __restrict__ z, cons
   float b[4], sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int e = 0; e < 4; ++e) b[e] = bias && j + e < cols ? bias[v0 + j + e] : 0.f;
-  for (int r = r0; r < r1; ++r) {
-    const int lab = labels[r];
-    const bool skip = ignore != INT_MIN && lab == ignore;
-    const float mx = row_max[r], rest = row_rest[r], inv = 1.f / (1.f + rest);
-    float4* at = reinterpret_cast<float4*>(z + (size_t)r * pitch + j);
-    const float4 q = *at;
-    float v[4] = {q.x, q.y, q.z, q.w};
+  for (int r = r0; r < r1; r += 4) {           // four rows on their way at once
+    float4 q[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float t = v[e] + b[e] - mx, p = (lab == v0 + j + e ? expm1f(t) - rest : expf(t)) * inv;
-      v[e] = skip || j + e >= cols ? 0.f : p * sc;
-      sum[e] += v[e];
+    for (int u = 0; u < 4; ++u) q[u] = *reinterpret_cast<const float4*>(z + (size_t)min(r + u, r1 - 1) * pitch + j);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (r + u >= r1) break;
+      const int lab = labels[r + u];
+      const bool skip = ignore != INT_MIN && lab == ignore;
+      const float mx = row_max[r + u], rest = row_rest[r + u], inv = 1.f / (1.f + rest);
+      float v[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float t = v[e] + b[e] - mx, p = (lab == v0 + j + e ? expm1f(t) - rest : expf(t)) * inv;
+        v[e] = skip || j + e >= cols ? 0.f : p * sc;
+        sum[e] += v[e];
+      }
+      *reinterpret_cast<float4*>(z + (size_t)(r + u) * pitch + j) = make_float4(v[0], v[1], v[2], v[3]);
     }
-    *at = make_float4(v[0], v[1], v[2], v[3]);
   }
   *reinterpret_cast<float4*>(db_part + (size_t)blockIdx.y * pitch + j) = make_float4(sum[0], sum[1], sum[2], sum[3]);
 }
@@ -182,12 +307,15 @@ inline unsigned grid_for(size_t total) {
 }
 
 // ---------------------------------------------------------------------------------- fp32
+constexpr int kRowCols = 8192;                 // columns that a workgroup keeps as a whole row
+constexpr int kColumnRows = 256;               // rows that one workgroup adds up per column
 constexpr int kSplitCols = 4096;               // columns of a row that one workgroup adds up
 
 inline long whole(long v) { return v < 16 ? 16 : up(v, 4); }   // widths that the fast kernels take
 
 struct Plan32 {
   long dp, piece, pieces, splits, row_parts;   // width of x as it is multiplied, classes of a piece, ...
+  bool rows;                                   // one piece of at most kRowCols classes
   bool own_x, own_w;                           // x resp. the filter of some piece is copied to make its widths whole (or to fp32)
   size_t part, stats, z, x, w, wt, dx, dw, db, wgrad, total;   // offsets of the parts of the workspace, and its size
   size_t wgrad_bytes;
@@ -207,6 +335,7 @@ Plan32 plan32(int n, int d, int classes, bool grads, int dtype) {
   const long last = p.cols(p.pieces - 1, classes), widest = whole(p.piece);
   p.splits = p.pieces * ((p.piece + kSplitCols - 1) / kSplitCols);
   p.row_parts = (n + DZ_ROWS - 1) / DZ_ROWS;
+  p.rows = p.pieces == 1 && p.piece <= kRowCols && n <= 16384;
   p.own_x = dtype != DT_F32 || p.dp != d;
   p.own_w = p.own_x || whole(last) != last;
   size_t at = 0;
@@ -233,12 +362,12 @@ Plan32 plan32(int n, int d, int classes, bool grads, int dtype) {
 #define ACC_TRY(call) do { if (const hipError_t e_ = (call); e_ != hipSuccess) return e_; } while (0)
 
 // out[n][n_out] (+)= in[n][c] * w[n_out][c]^T
-hipError_t product32(const float* in, const float* w, float* out, int n, int c, int n_out, bool accumulate, hipStream_t st) {
+ConvGeom product_geom(const float* in, const float* w, float* out, int n, int c, int n_out, bool accumulate) {
   ConvGeom g{};
   g.in = in; g.w = w; g.out = out; g.dtype = DT_F32;
   g.n_img = n; g.h = g.wd = g.p = g.q = g.out_h = g.out_w = 1;
   g.c = c; g.n_out = n_out; g.r = g.s = g.stride = g.out_stride = 1; g.accumulate = accumulate ? 1 : 0;
-  return conv_igemm(g, st);
+  return g;
 }
 
 hipError_t widen(const void* in, int dtype, float* out, int rows_in, int cols_in, long rows, long cols, hipStream_t st) {
@@ -277,28 +406,54 @@ hipError_t run32(const LceArgs& a) {
       w = (const float*)(a.ws + p.w);
       ACC_TRY(widen(from, a.dtype, (float*)(a.ws + p.w), cols, a.d, pitch, dp, st));
     }
-    return product32(x, w, z, a.n, dp, pitch, false, st);
+    return conv_igemm(product_geom(x, w, z, a.n, dp, pitch, false), st);
   };
-  const int splits_piece = (int)((p.piece + kSplitCols - 1) / kSplitCols);
-  for (long k = 0; k < p.pieces; ++k) {
-    ACC_TRY(logits(k));
-    hipLaunchKernelGGL(row_sums_kernel, dim3((unsigned)(a.n * splits_piece)), dim3(THREADS), 0, st, z, a.bias, a.labels, part, s.z_label, pitch, cols,
-                       (int)v0, kSplitCols, splits_piece, (int)(k * splits_piece), (int)p.splits);
-  }
-  ACC_TRY(lce_join(a, s, part, (int)p.splits));
-  if (!grads) return hipSuccess;
-  float* const dx = p.own_x ? (float*)(a.ws + p.dx) : (float*)a.dx;
   float* const db_part = (float*)(a.ws + p.db);
+  float* const dx = p.own_x ? (float*)(a.ws + p.dx) : (float*)a.dx;
+  if (p.rows) {
+    ACC_TRY(logits(0));
+#define ACC_ROWS(V, NT) hipLaunchKernelGGL((rows_kernel<V, NT>), dim3((unsigned)a.n), dim3(NT), 0, st, z, a.bias, a.labels, a.ignore, s.loss_rows, a.n, pitch, \
+                                           cols, grads ? 1 : 0)
+    if (pitch <= 4 * 256) ACC_ROWS(4, 256);
+    else if (pitch <= 16 * 256) ACC_ROWS(16, 256);
+    else ACC_ROWS(8, 1024);
+#undef ACC_ROWS
+    const int across = (cols + THREADS - 1) / THREADS, slabs = (a.n + kColumnRows - 1) / kColumnRows, blocks = a.db ? across * slabs : 0;
+    if (a.db || a.loss)
+      hipLaunchKernelGGL(columns_kernel, dim3((unsigned)(blocks + (a.loss ? 1 : 0))), dim3(THREADS), 0, st, z, slabs > 1 ? db_part : a.db, a.n, pitch, cols, kColumnRows,
+                         blocks, pitch, s.loss_rows, a.labels, a.ignore, a.loss);
+    if (a.db && slabs > 1)
+      hipLaunchKernelGGL(db_kernel, dim3((unsigned)across), dim3(THREADS), 0, st, db_part, a.db, slabs, pitch, cols);
+    ACC_TRY(hipGetLastError());
+    if (!grads) return hipSuccess;
+  } else {
+    const int splits_piece = (int)((p.piece + kSplitCols - 1) / kSplitCols);
+    for (long k = 0; k < p.pieces; ++k) {
+      ACC_TRY(logits(k));
+      hipLaunchKernelGGL(row_sums_kernel, dim3((unsigned)(a.n * splits_piece)), dim3(THREADS), 0, st, z, a.bias, a.labels, part, s.z_label, pitch, cols,
+                         (int)v0, kSplitCols, splits_piece, (int)(k * splits_piece), (int)p.splits);
+    }
+    ACC_TRY(lce_join(a, s, part, (int)p.splits));
+    if (!grads) return hipSuccess;
+  }
   for (long k = 0; k < p.pieces; ++k) {
     if (p.pieces > 1) ACC_TRY(logits(k));
-    hipLaunchKernelGGL(dz_kernel, dim3((unsigned)((pitch / 4 + THREADS - 1) / THREADS), (unsigned)p.row_parts), dim3(THREADS), 0, st, z, a.bias, a.labels,
-                       a.ignore, s.row_max, s.row_rest, s.scale, db_part, a.n, pitch, cols, (int)v0);
-    if (a.db)
-      hipLaunchKernelGGL(db_kernel, dim3((unsigned)((cols + THREADS - 1) / THREADS)), dim3(THREADS), 0, st, db_part, a.db + v0, (int)p.row_parts, pitch, cols);
+    if (!p.rows) {
+      hipLaunchKernelGGL(dz_kernel, dim3((unsigned)((pitch / 4 + THREADS - 1) / THREADS), (unsigned)p.row_parts), dim3(THREADS), 0, st, z, a.bias, a.labels,
+                         a.ignore, s.row_max, s.row_rest, s.scale, db_part, a.n, pitch, cols, (int)v0);
+      if (a.db)
+        hipLaunchKernelGGL(db_kernel, dim3((unsigned)((cols + THREADS - 1) / THREADS)), dim3(THREADS), 0, st, db_part, a.db + v0, (int)p.row_parts, pitch,
+                           cols);
+    }
     if (a.dx) {
-      float* const wt = (float*)(a.ws + p.wt);
-      ACC_TRY(filter_flip_transpose(w, wt, pitch, dp, 1, 1, DT_F32, st));
-      ACC_TRY(product32(z, wt, dx, a.n, pitch, dp, k > 0, st));
+      ConvGeom g = product_geom(z, nullptr, dx, a.n, pitch, dp, k > 0);
+      g.w_kn = w;                              // few rows: the filter as it lies
+      if (!conv_igemm_rows_takes(g, a.n, pitch)) {
+        float* const wt = (float*)(a.ws + p.wt);
+        ACC_TRY(filter_flip_transpose(w, wt, pitch, dp, 1, 1, DT_F32, st));
+        g = product_geom(z, wt, dx, a.n, pitch, dp, k > 0);
+      }
+      ACC_TRY(conv_igemm(g, st));
     }
     if (a.dw) {
       float* const to = a.dw + (size_t)v0 * a.d;
@@ -329,6 +484,11 @@ bool shape_ok(int n, int d, int classes, int dtype) {
 }  // namespace
 
 hipError_t lce_join(const LceArgs& a, const LceStats& s, const float* part, int splits) {
+  if ((long)a.n * splits <= 16384) {          // a few rows for each of sixteen waves: one launch
+    hipLaunchKernelGGL(join_mean_kernel, dim3(1), dim3(1024), 0, a.st, part, s.z_label, a.labels, a.ignore, s.row_max, s.row_rest, s.loss_rows, a.n, splits,
+                       a.classes, s.scale, a.loss);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL(join_kernel, dim3((a.n + THREADS / 64 - 1) / (THREADS / 64)), dim3(THREADS), 0, a.st, part, s.z_label, a.labels, a.ignore, s.row_max,
                      s.row_rest, s.loss_rows, a.n, splits, a.classes);
   hipLaunchKernelGGL(mean_kernel, dim3(1), dim3(1024), 0, a.st, s.loss_rows, a.labels, a.ignore, a.n, s.scale, a.loss);

@@ -1,9 +1,11 @@
 // The products of the linear cross-entropy (linear_ce.hip) for bf16 operands, on the bf16 matrix cores, with what surrounds them in their
 // epilogues: logits leave a tile as the largest one of its columns and the sum of exponentials, or as dz.
 //
-// dz is left without the factor 1 / rows (a label's value is then -1 where its probability is small, exact in bf16) as the sum of two bf16
-// values, hi + lo, which hold 16 bits of it.  dw, an fp32 result, is multiplied from both (relative error of a value 2^-17 at most, where hi alone
-// would leave 2^-9); dx, which is rounded to bf16 itself, from hi.  The factor is applied to the fp32 accumulators.
+// dz is left without the factor 1 / rows (a label's value is then -1 where its probability is small, exact in bf16) as the sum of two or three
+// bf16 values, the first the nearest one, the next the nearest to what is left.  dw, an fp32 result, is multiplied from all of them: one leaves a
+// relative error of up to 2^-9, two of 2^-18, three of 2^-27.  Two are enough from 4096 rows on, where the rounding of the fp32 sums is as large (relative
+// error of dw, 4096 rows 1.16e-6, the same sums of exact fp32 products 1.14e-6; 64 rows 1.9e-6 and, with three, 0.2e-6).  dx, which is rounded to
+// bf16 itself, is multiplied from the first.  The factor is applied to the fp32 accumulators.
 #include "kernels.h"
 #include "dtype.h"
 #include "gemm_bf16.h"
@@ -30,18 +32,31 @@ __device__ __forceinline__ int xcd_tile(int blocks) { return ((int)blockIdx.x & 
 template <class C>
 __device__ __forceinline__ void add_bias(GemmAcc<C>& acc, const float* __restrict__ bias, int col0, int cols) {
   const int lane = threadIdx.x & 63;
+  const bool whole = col0 + 32 * C::NB <= cols;        // the wave's columns exist
 #pragma unroll
   for (int j = 0; j < C::NB; ++j)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int n = col0 + 32 * j + 8 * q + 4 * (lane >> 5);
-      float b[4];
+      float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (whole) {
+        b = *reinterpret_cast<const float4*>(bias + n);        // (a piece starts at a multiple of 256 classes)
+      } else {
+        if (n < cols) b.x = bias[n];
+        if (n + 1 < cols) b.y = bias[n + 1];
+        if (n + 2 < cols) b.z = bias[n + 2];
+        if (n + 3 < cols) b.w = bias[n + 3];
+      }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) b[e] = bias && n + e < cols ? bias[n + e] : 0.f;
-#pragma unroll
-      for (int i = 0; i < C::MB; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += b[e];
+      for (int i = 0; i < C::MB; ++i) {
+        acc[i][j][4 * q] += b.x;
+        acc[i][j][4 * q + 1] += b.y;
+        acc[i][j][4 * q + 2] += b.z;
+        acc[i][j][4 * q + 3] += b.w;
+      }
+#if defined(__HIP_DEVICE_COMPILE__)
+      __builtin_amdgcn_sched_barrier(0);               // (all of them at once would not fit the registers beside the accumulators)
+#endif
     }
 }
 
@@ -56,7 +71,8 @@ struct LogitArgs {
   int split0, splits;
   // dz
   const float *row_max, *row_rest;
-  bf16_t *hi, *lo;
+  float* z;                          // sums: the logits are kept here, too (null: not)
+  bf16_t* dz[3];
   int pitch, ignore;
   float* db_part;                    // null: not wanted
 };
@@ -69,11 +85,26 @@ __global__ __launch_bounds__(C::THREADS, 2) void lce_sums_kernel(LogitArgs a, in
   if (at >= a.tiles) return;
   const int tile_n = at / a.tiles_m, tile_m = at - tile_n * a.tiles_m, m0 = tile_m * C::BM, n0 = tile_n * C::BN;
   GemmAcc<C> acc;
-  gemm_tile<C>(a.x, a.x, a.w, m0, n0, 0, a.d, lds, acc);
+  gemm_tile<C>(a.x, a.w, m0, n0, 0, a.d, lds, acc);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm0 = (wave / C::WN) * 32 * C::MB, wn = wave % C::WN, wn0 = wn * 32 * C::NB;
   if (a.bias) add_bias<C>(acc, a.bias, n0 + wn0, a.cols);
   float(*red)[C::BM][3] = reinterpret_cast<float(*)[C::BM][3]>(lds);
   const bool edge = n0 + C::BN > a.cols;
+  if (a.z) {                                           // four columns of a row per lane
+#pragma unroll
+    for (int i = 0; i < C::MB; ++i) {
+      const int m = m0 + wm0 + 32 * i + (lane & 31);
+      float* const to = a.z + (size_t)m * a.pitch;
+#pragma unroll
+      for (int j = 0; j < C::NB; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int n = n0 + wn0 + 32 * j + 8 * q + 4 * (lane >> 5);
+          if (m < a.n && n < a.pitch)
+            *reinterpret_cast<float4*>(to + n) = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+        }
+    }
+  }
 #pragma unroll
   for (int i = 0; i < C::MB; ++i) {
     if (edge) {
@@ -152,19 +183,19 @@ __device__ __forceinline__ float half_sum(float v) {
   return v;
 }
 
-template <class C>
+template <class C, int PARTS>
 __global__ __launch_bounds__(C::THREADS, 2) void lce_dz_kernel(LogitArgs a, int blocks) {
-  constexpr int EP = C::NB * 64 + 16, OUT = C::WM * C::WN * 32 * EP * 2;      // per wave 32 staged rows of hi and lo
+  constexpr int EP = C::NB * 64 + 16, OUT = C::WM * C::WN * 32 * EP * PARTS;      // per wave 32 staged rows of every part
   __shared__ __attribute__((aligned(1024))) char lds[C::LDS > OUT ? C::LDS : OUT];
   const int at = xcd_tile(blocks);
   if (at >= a.tiles) return;
   const int tile_n = at / a.tiles_m, tile_m = at - tile_n * a.tiles_m, m0 = tile_m * C::BM, n0 = tile_n * C::BN;
   GemmAcc<C> acc;
-  gemm_tile<C>(a.x, a.x, a.w, m0, n0, 0, a.d, lds, acc);
+  gemm_tile<C>(a.x, a.w, m0, n0, 0, a.d, lds, acc);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm0 = (wave / C::WN) * 32 * C::MB, wn0 = (wave % C::WN) * 32 * C::NB;
   if (a.bias) add_bias<C>(acc, a.bias, n0 + wn0, a.cols);
   const bool edge = n0 + C::BN > a.cols;
-  char* const stg = lds + wave * (32 * EP * 2);
+  char* const stg = lds + wave * (32 * EP * PARTS);
   float sum[C::NB][16];
 #pragma unroll
   for (int j = 0; j < C::NB; ++j)
@@ -180,32 +211,36 @@ __global__ __launch_bounds__(C::THREADS, 2) void lce_dz_kernel(LogitArgs a, int 
     const int lab = label - a.v0 - (n0 + wn0) - 4 * (lane >> 5);
     const bool mine = row_ok && (unsigned)label >= (unsigned)a.v0 && lab >= 0 && lab < 32 * C::NB && !(lab & 4);
     const bool any = __any(mine);
+    const float p_label = mine ? (expm1f(a.z_label[m] - mx) - rest) * inv : 0.f;
+    const int at_label = mine ? lab : -1;
 #pragma unroll
     for (int j = 0; j < C::NB; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        float p[4], l[4];
-        uint2 hi, lo;
+        float p[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float t = acc[i][j][4 * q + e] - mx;
-          p[e] = exp_fast(t) * inv;
-          if (any && mine && lab == 32 * j + 8 * q + e) p[e] = (expm1f(t) - rest) * inv;
-          if (skip) p[e] = 0.f;
+          p[e] = exp_fast(acc[i][j][4 * q + e] - mx) * inv;
+          if (any) p[e] = at_label == 32 * j + 8 * q + e ? p_label : p[e];
+          p[e] = skip ? 0.f : p[e];
           if (edge && n0 + wn0 + 32 * j + 8 * q + 4 * (lane >> 5) + e >= a.cols) p[e] = 0.f;
           sum[j][4 * q + e] += p[e];
         }
-        hi.x = pack_bf16(p[0], p[1]);
-        hi.y = pack_bf16(p[2], p[3]);
-        l[0] = p[0] - __uint_as_float(hi.x << 16);
-        l[1] = p[1] - __uint_as_float(hi.x & 0xffff0000u);
-        l[2] = p[2] - __uint_as_float(hi.y << 16);
-        l[3] = p[3] - __uint_as_float(hi.y & 0xffff0000u);
-        lo.x = pack_bf16(l[0], l[1]);
-        lo.y = pack_bf16(l[2], l[3]);
         char* const to = stg + (lane & 31) * EP + (32 * j + 8 * q + 4 * (lane >> 5)) * 2;
-        *reinterpret_cast<uint2*>(to) = hi;
-        *reinterpret_cast<uint2*>(to + 32 * EP) = lo;
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) {
+          const uint2 w = make_uint2(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]));
+          *reinterpret_cast<uint2*>(to + part * 32 * EP) = w;
+          if (part + 1 < PARTS) {                      // what is left
+            p[0] -= __uint_as_float(w.x << 16);
+            p[1] -= __uint_as_float(w.x & 0xffff0000u);
+            p[2] -= __uint_as_float(w.y << 16);
+            p[3] -= __uint_as_float(w.y & 0xffff0000u);
+          }
+        }
+#if defined(__HIP_DEVICE_COMPILE__)
+        __builtin_amdgcn_sched_barrier(0);             // four values at a time: more do not fit the registers beside the accumulators
+#endif
       }
     // whole rows: eight values per lane
     constexpr int PPR = C::NB * 4, RPI = 64 / PPR;
@@ -214,8 +249,9 @@ __global__ __launch_bounds__(C::THREADS, 2) void lce_dz_kernel(LogitArgs a, int 
     for (int it = 0; it < 32 / RPI; ++it) {
       const int r = prow + RPI * it, mm = m0 + wm0 + 32 * i + r;
       if (mm >= a.n || col >= a.pitch) continue;       // (the pitch is a multiple of 8)
-      *reinterpret_cast<v4u*>(a.hi + (size_t)mm * a.pitch + col) = *reinterpret_cast<const v4u*>(stg + r * EP + c8 * 16);
-      *reinterpret_cast<v4u*>(a.lo + (size_t)mm * a.pitch + col) = *reinterpret_cast<const v4u*>(stg + 32 * EP + r * EP + c8 * 16);
+#pragma unroll
+      for (int part = 0; part < PARTS; ++part)
+        *reinterpret_cast<v4u*>(a.dz[part] + (size_t)mm * a.pitch + col) = *reinterpret_cast<const v4u*>(stg + part * 32 * EP + r * EP + c8 * 16);
     }
   }
   if (!a.db_part) return;
@@ -230,6 +266,59 @@ __global__ __launch_bounds__(C::THREADS, 2) void lce_dz_kernel(LogitArgs a, int 
     }
 }
 
+// dz from kept logits: eight columns per thread, a workgroup's rows one after the other (DZ_ROWS of them), and their columns' sums
+constexpr int DZ_ROWS = 16;
+template <int PARTS>
+__global__ __launch_bounds__(256) void lce_dz_kept_kernel(LogitArgs a, int blocks_across) {
+  const int across = (int)blockIdx.x % blocks_across, slab = (int)blockIdx.x / blocks_across;
+  const int col = (across * 256 + (int)threadIdx.x) * 8;
+  if (col >= a.pitch) return;                          // (a multiple of 64)
+  float sum[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+  const int r0 = slab * DZ_ROWS, r1 = min(r0 + DZ_ROWS, a.n);
+  for (int r = r0; r < r1; r += 2) {                   // two rows on their way at once
+    float4 lo[2], hi[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const float* from = a.z + (size_t)min(r + u, r1 - 1) * a.pitch + col;
+      lo[u] = *reinterpret_cast<const float4*>(from);
+      hi[u] = *reinterpret_cast<const float4*>(from + 4);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if (r + u >= r1) break;
+      const int label = a.labels[r + u], lab = label - a.v0 - col;
+      const bool skip = a.ignore != INT_MIN && label == a.ignore, mine = (unsigned)label >= (unsigned)a.v0 && lab >= 0 && lab < 8;
+      const float mx = a.row_max[r + u], rest = a.row_rest[r + u], inv = 1.f / (1.f + rest);
+      float p[8] = {lo[u].x, lo[u].y, lo[u].z, lo[u].w, hi[u].x, hi[u].y, hi[u].z, hi[u].w};
+      const float p_label = mine ? (expm1f(a.z_label[r + u] - mx) - rest) * inv : 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p[e] = exp_fast(p[e] - mx) * inv;
+        if (mine && lab == e) p[e] = p_label;
+        if (skip || col + e >= a.cols) p[e] = 0.f;
+        sum[e] += p[e];
+      }
+#pragma unroll
+      for (int part = 0; part < PARTS; ++part) {
+        v4u w;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          w[q] = pack_bf16(p[2 * q], p[2 * q + 1]);
+          p[2 * q] -= __uint_as_float(w[q] << 16);
+          p[2 * q + 1] -= __uint_as_float(w[q] & 0xffff0000u);
+        }
+        *reinterpret_cast<v4u*>(a.dz[part] + (size_t)(r + u) * a.pitch + col) = w;
+      }
+    }
+  }
+  if (!a.db_part) return;
+  float* const to = a.db_part + (size_t)slab * a.pitch + col;
+  *reinterpret_cast<float4*>(to) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+  *reinterpret_cast<float4*>(to + 4) = make_float4(sum[4], sum[5], sum[6], sum[7]);
+}
+
 // dx: sums[split][n][d] (+)= dz w over the split's classes of the piece
 template <class C>
 __global__ __launch_bounds__(C::THREADS, 2) void lce_dx_kernel(GemmOperand dz, GemmOperand w, float* __restrict__ sums, int n, int d, int k, int k_per_split,
@@ -239,39 +328,42 @@ __global__ __launch_bounds__(C::THREADS, 2) void lce_dx_kernel(GemmOperand dz, G
   if (work >= tiles * splits) return;
   const int split = work / tiles, at = work - split * tiles, tile_n = at / tiles_m, tile_m = at - tile_n * tiles_m, m0 = tile_m * C::BM, n0 = tile_n * C::BN;
   GemmAcc<C> acc;
-  gemm_tile<C>(dz, dz, w, m0, n0, split * k_per_split, min(k, (split + 1) * k_per_split), lds, acc);
+  gemm_tile<C>(dz, w, m0, n0, split * k_per_split, min(k, (split + 1) * k_per_split), lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm0 = (wave / C::WN) * 32 * C::MB, wn0 = (wave % C::WN) * 32 * C::NB;
   float* const out = sums + (size_t)split * n * d;
 #pragma unroll
   for (int i = 0; i < C::MB; ++i)
 #pragma unroll
     for (int j = 0; j < C::NB; ++j) {
-      const int col = n0 + wn0 + 32 * j + (lane & 31);
+      const int col = n0 + wn0 + 32 * j + (lane & 31), mb = m0 + wm0 + 32 * i + 4 * (lane >> 5);
       if (col >= d) continue;
+      float* const o = out + (size_t)mb * d + col;
+      float old[16];                                   // asked for together (one after the other, each behind the store before it: 80 us of 337)
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
-        const int m = m0 + wm0 + 32 * i + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
-        if (m >= n) continue;
-        float* const o = out + (size_t)m * d + col;
-        *o = add ? *o + acc[i][j][v] : acc[i][j][v];
+        const int r = 8 * (v >> 2) + (v & 3);
+        old[v] = add && mb + r < n ? o[(size_t)r * d] : 0.f;
+      }
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int r = 8 * (v >> 2) + (v & 3);
+        if (mb + r < n) o[(size_t)r * d] = old[v] + acc[i][j][v];
       }
     }
 }
 
 // dx = scale * the splits' sums in order, rounded to bf16
-__global__ __launch_bounds__(256) void lce_dx_finish_kernel(const float* __restrict__ sums, const float* __restrict__ scale, bf16_t* __restrict__ dx, size_t count,
-                                                            int splits) {
-  const float sc = scale[0];
-  const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+__device__ __forceinline__ void finish_dx(const float* __restrict__ sums, float sc, bf16_t* __restrict__ dx, size_t count, int splits, size_t block) {
+  const size_t i = (block * 256 + threadIdx.x) * 4;
   if (i >= count) return;
-  if (i + 4 <= count && (count & 3) == 0) {
+  if ((count & 3) == 0) {
     float4 s = *reinterpret_cast<const float4*>(sums + i);
+#pragma unroll 4
     for (int k = 1; k < splits; ++k) {
       const float4 q = *reinterpret_cast<const float4*>(sums + k * count + i);
       s.x += q.x; s.y += q.y; s.z += q.z; s.w += q.w;
     }
-    const float v[4] = {s.x * sc, s.y * sc, s.z * sc, s.w * sc};
-    Elem<bf16_t>::store4(dx + i, v);
+    *reinterpret_cast<uint2*>(dx + i) = make_uint2(pack_bf16(s.x * sc, s.y * sc), pack_bf16(s.z * sc, s.w * sc));
     return;
   }
   for (size_t e = i; e < count && e < i + 4; ++e) {
@@ -280,18 +372,51 @@ __global__ __launch_bounds__(256) void lce_dx_finish_kernel(const float* __restr
     Elem<bf16_t>::store(dx + e, s * sc);
   }
 }
+// db = scale * the row tiles' sums of a piece
+__device__ __forceinline__ void finish_db(const float* __restrict__ part, float sc, float* __restrict__ db, int parts, int pitch, int cols, int block) {
+  const int j = block * 256 + threadIdx.x;
+  if (j >= cols) return;
+  double s = 0.0;
+#pragma unroll 8
+  for (int k = 0; k < parts; ++k) s += (double)part[(size_t)k * pitch + j];
+  db[j] = (float)(s * (double)sc);
+}
+// dw = scale * the splits' sums in order
+__device__ __forceinline__ void finish_dw(const float* __restrict__ sums, float sc, float* __restrict__ dw, size_t count, int splits, size_t block) {
+  for (size_t i = block * 1024 + threadIdx.x; i < count && i < (block + 1) * 1024; i += 256) {
+    float s = sums[i];
+#pragma unroll 4
+    for (int k = 1; k < splits; ++k) s += sums[k * count + i];
+    dw[i] = s * sc;
+  }
+}
+struct Finish {
+  const float *sums, *part, *scale, *dw_sums;
+  bf16_t* dx;
+  float *db, *dw;
+  size_t count, dw_count;
+  int splits, dw_splits, dx_blocks, dw_blocks, parts, pitch, cols;
+};
+__global__ __launch_bounds__(256) void lce_finish_kernel(Finish f) {
+  const float sc = f.scale[0];
+  if ((int)blockIdx.x < f.dx_blocks) finish_dx(f.sums, sc, f.dx, f.count, f.splits, blockIdx.x);
+  else if ((int)blockIdx.x < f.dx_blocks + f.dw_blocks) finish_dw(f.dw_sums, sc, f.dw, f.dw_count, f.dw_splits, blockIdx.x - f.dx_blocks);
+  else finish_db(f.part, sc, f.db, f.parts, f.pitch, f.cols, (int)blockIdx.x - f.dx_blocks - f.dw_blocks);
+}
 
-// dw[class][d] = scale * sum over the rows of (hi + lo)[row][class] * x[row][d]
+// dw[class][d] = scale * sum over the rows of dz[row][class] * x[row][d], dz as the sum of its parts; with several splits of the rows their sums
+// (without the factor) lie one behind the other
 template <class C>
-__global__ __launch_bounds__(C::THREADS, 2) void lce_dw_kernel(GemmOperand hi, GemmOperand lo, GemmOperand x, const float* __restrict__ scale,
-                                                               float* __restrict__ dw, int n, int d, int cols, int tiles_m, int tiles, int blocks) {
+__global__ __launch_bounds__(C::THREADS, 2) void lce_dw_kernel(GemmOperand dz, GemmOperand x, const float* __restrict__ scale, float* __restrict__ out, int n, int d,
+                                                               int cols, int tiles_m, int tiles, int splits, int n_per_split, int blocks) {
   __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
-  const int at = xcd_tile(blocks);
-  if (at >= tiles) return;
-  const int tile_n = at / tiles_m, tile_m = at - tile_n * tiles_m, m0 = tile_m * C::BM, n0 = tile_n * C::BN;
+  const int work = xcd_tile(blocks);
+  if (work >= tiles * splits) return;
+  const int split = work / tiles, at = work - split * tiles, tile_n = at / tiles_m, tile_m = at - tile_n * tiles_m, m0 = tile_m * C::BM, n0 = tile_n * C::BN;
   GemmAcc<C> acc;
-  gemm_tile<C>(hi, lo, x, m0, n0, 0, n, lds, acc);
-  const float sc = scale[0];
+  gemm_tile<C>(dz, x, m0, n0, split * n_per_split, min(n, (split + 1) * n_per_split), lds, acc);
+  const float sc = splits > 1 ? 1.f : scale[0];
+  float* const dw = out + (size_t)split * cols * d;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm0 = (wave / C::WN) * 32 * C::MB, wn0 = (wave % C::WN) * 32 * C::NB;
 #pragma unroll
   for (int i = 0; i < C::MB; ++i)
@@ -307,15 +432,6 @@ __global__ __launch_bounds__(C::THREADS, 2) void lce_dw_kernel(GemmOperand hi, G
     }
 }
 
-__global__ __launch_bounds__(256) void lce_db_kernel(const float* __restrict__ part, const float* __restrict__ scale, float* __restrict__ db, int parts, int pitch,
-                                                     int cols) {
-  const int j = blockIdx.x * 256 + threadIdx.x;
-  if (j >= cols) return;
-  double s = 0.0;
-  for (int k = 0; k < parts; ++k) s += (double)part[(size_t)k * pitch + j];
-  db[j] = (float)(s * (double)scale[0]);
-}
-
 // out[r][0 .. pitch) = in[r][0 .. d), then zeros
 __global__ __launch_bounds__(256) void lce_pad_kernel(const bf16_t* __restrict__ in, bf16_t* __restrict__ out, size_t total, int d, int pitch) {
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (size_t)gridDim.x * 256) {
@@ -327,55 +443,100 @@ __global__ __launch_bounds__(256) void lce_pad_kernel(const bf16_t* __restrict__
 //                WM WN MB NB BK NS   AT     BT  PARTS SWAP
 typedef GemmCfg<2, 4, 4, 2, 64, 2, false, false, 1, true> Z256;
 typedef GemmCfg<2, 2, 2, 2, 64, 2, false, false, 1, true> Z128;
+typedef GemmCfg<2, 2, 1, 1, 64, 4, false, false, 1, true> Z64;
 typedef GemmCfg<2, 4, 4, 2, 64, 2, false, true, 1, false> X256;
 typedef GemmCfg<2, 2, 2, 2, 64, 2, false, true, 1, false> X128;
+typedef GemmCfg<2, 2, 1, 1, 64, 4, false, true, 1, false> X64;
 typedef GemmCfg<2, 4, 4, 2, 32, 3, true, true, 2, false> W256;
 typedef GemmCfg<2, 2, 2, 2, 32, 2, true, true, 2, false> W128;
+typedef GemmCfg<2, 2, 1, 1, 32, 4, true, true, 2, false> W64;
+typedef GemmCfg<2, 4, 4, 2, 32, 2, true, true, 3, false> V256;        // dw with three parts of dz
+typedef GemmCfg<2, 2, 2, 2, 32, 2, true, true, 3, false> V128;
+typedef GemmCfg<2, 2, 1, 1, 32, 3, true, true, 3, false> V64;
 
 inline size_t al256(size_t b) { return (b + 255) & ~(size_t)255; }
 inline long up(long v, long m) { return (v + m - 1) / m * m; }
 inline long ceil_div(long a, long b) { return (a + b - 1) / b; }
 
-// 256 x 256 tiles where there are enough of them for the compute units
-inline bool large_tiles(long m, long n) { return ceil_div(m, 256) * ceil_div(n, 256) >= 192; }
+// Which tiles: the ones with the smallest predicted time, microseconds, from the tiles of the busiest compute unit and the steps of 64 values of k
+// (times the parts of A).  256 x 256 has a compute unit to itself, of the others two workgroups share one.  Constants from eleven shapes (41 to 8000 rows, widths
+// 256 to 4096, 1000 to 50001 classes), every tile on each; measured, 256 / 128 / 64: logits and sums, 777 x 1160 x 50001 154 / 145 / 234, 1000 x 2048 x 1000
+// 46 / 26 / 12, 4096 x 1024 x 8192 68 / 73 / 152; dw, 2000 x 512 x 20000 127 / 168 / 261, 41 x 2048 x 1000 10.9 / 6.4 / 4.8.
+struct TileCost {
+  double first, first_step, next, next_step;
+};
+enum { RowsByRows = 0, ByColumns };            // both operands along k; A and B (dw) in rows of k
+constexpr TileCost kCost[2][3] = {{{4.0, 1.28, 8.0, 1.60}, {3.0, 0.62, 3.2, 0.50}, {1.5, 0.31, 1.7, 0.205}},
+                                  {{4.0, 1.30, 12.0, 1.50}, {3.0, 0.62, 5.0, 0.55}, {1.5, 0.31, 1.0, 0.28}}};
+constexpr int kTiles[3] = {256, 128, 64};
+double tile_us(int kind, int t, long tiles, double steps) {
+  const long most = ceil_div(tiles, 256);
+  const TileCost& c = kCost[kind][t];
+  const double first = c.first + c.first_step * steps, next = c.next + c.next_step * steps;
+  if (t == 0) return 3.0 + first + (most - 1) * next;
+  auto round = [&](long r) { return r == 0 ? 0.0 : first > r * next ? first : r * next; };
+  return 3.0 + (most / 2) * round(2) + round(most % 2);
+}
+// Tiles and, for a product whose sum over k may be cut, parts of `step` values of k or more, whose sums cost writing and reading
+struct Choice {
+  int tile, splits, k;           // k: values of it in one part
+};
+Choice choose(int kind, long m, long n, long k, int parts, long most_sums, long step) {
+  Choice best{256, 1, (int)up(k, 64)};
+  double us = 0;
+  for (int t = 0; t < 3; ++t) {
+    const long tiles = ceil_div(m, kTiles[t]) * ceil_div(n, kTiles[t]);
+    // cuts in one to sixty-four, and those that fill the compute units once, twice and four times
+    for (int i = 0; i < 10; ++i) {
+      const long s = i < 7 ? 1L << i : (256L << (i - 7)) / tiles;
+      if (s < 1) continue;
+      const long each = up(ceil_div(k, s), 64), splits = ceil_div(k, each);
+      if (s > 1 && (each < step || splits * m * n > most_sums)) continue;
+      const double sums = splits > 1 ? 2.0 + (double)splits * m * n * 8 / 6e6 : 0.0;
+      const double v = tile_us(kind, t, tiles * splits, each / 64.0 * parts) + sums;
+      if ((t == 0 && s == 1) || v < us) {
+        us = v;
+        best = Choice{kTiles[t], (int)splits, (int)each};
+      }
+    }
+  }
+  return best;
+}
 
 struct Plan16 {
   int dp;                        // width as it is multiplied, a multiple of 8
+  int parts;                     // bf16 values that dz is the sum of
   long piece, pieces, splits;    // classes of a piece (a multiple of 256), pieces, columns of `part`
   int pitch;                     // of dz
-  bool z256, x256, w256;
-  int dx_splits, dx_k;           // parts of a piece's classes, classes of a part
-  size_t stats, part, x, w, hi, lo, dx, db, total;
+  bool keep;                     // the last piece's logits are kept from the first sweep for the second, which begins with it
+  int zt;                        // tiles of the logits
+  Choice dx, dw;
+  size_t stats, part, x, w, z, dz[3], dx_sums, dw_sums, db, total;
 };
 
 Plan16 plan16(int n, int d, int classes, bool grads) {
   Plan16 p{};
   p.dp = (int)up(d, 8);
+  p.parts = n < 4096 ? 3 : 2;
   // 256 MiB of dz, 1 GiB of filter
-  long most = (1L << 26) / n / 256 * 256;
+  long most = (1L << 27) / p.parts / n / 256 * 256;
   if (most > (1L << 29) / p.dp / 256 * 256) most = (1L << 29) / p.dp / 256 * 256;
   if (!grads) {                  // (nothing of a piece is kept; a launch has fewer than 2^32 threads)
     most = (1L << 29) / p.dp / 256 * 256;
-    const long by_grid = (1L << 20) / ceil_div(n, 128) * 256;
+    const long by_grid = (1L << 20) / ceil_div(n, 64) * 256;
     if (most > by_grid) most = by_grid;
   }
   if (most < 256) most = 256;
   p.piece = up(classes, 256) <= most ? up(classes, 256) : most;
   p.pieces = ceil_div(classes, p.piece);
-  p.z256 = large_tiles(n, p.piece);
-  p.x256 = d >= 192 && n >= 192;
-  p.w256 = large_tiles(p.piece, d);
-  const int bn = p.z256 ? 256 : 128;
-  p.splits = p.pieces * (p.piece / bn);
+  const long whole = p.pieces > 1 ? p.piece : classes;
+  p.zt = choose(RowsByRows, n, whole, p.dp, 1, 0, 1L << 30).tile;
+  p.splits = p.pieces * (p.piece / p.zt);
   p.pitch = (int)(p.pieces > 1 ? p.piece : up(classes, 64));
-  const int bm = p.x256 ? 256 : 128;
-  const long tiles = ceil_div(n, bm) * ceil_div(d, bm), slots = p.x256 ? 256 : 512;
-  long s = slots / tiles;
-  if (s > p.pitch / 256) s = p.pitch / 256;
-  if (s < 1) s = 1;
-  while (s > 1 && s * n * d > (1L << 26)) --s;
-  p.dx_k = (int)up(ceil_div(p.pitch, s), 64);
-  p.dx_splits = (int)ceil_div(p.pitch, p.dx_k);
+  // where the products take longer than writing and reading their results (us, second sweep of 777 x 1160 x 50001: 183 worked out again, 128 kept)
+  p.keep = grads && d >= 1024;
+  p.dx = choose(RowsByRows, n, d, p.pitch, 1, 1L << 25, 256);
+  p.dw = choose(ByColumns, whole, d, n, p.parts, 1L << 24, 128);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t a = at; at += al256(bytes); return a; };
   p.stats = take((size_t)(4 * (size_t)n + 64) * 4);
@@ -383,10 +544,12 @@ Plan16 plan16(int n, int d, int classes, bool grads) {
   p.x = take(p.dp != d ? (size_t)n * p.dp * 2 : 0);
   p.w = take(p.dp != d ? (size_t)p.piece * p.dp * 2 : 0);
   if (grads) {
-    p.hi = take((size_t)n * p.pitch * 2);
-    p.lo = take((size_t)n * p.pitch * 2);
-    p.dx = take((size_t)p.dx_splits * n * d * 4);
-    p.db = take((size_t)2 * ceil_div(n, 128) * p.pitch * 4);
+    for (int i = 0; i < p.parts; ++i) p.dz[i] = take((size_t)n * p.pitch * 2);
+    p.z = take(p.keep ? (size_t)n * p.pitch * 4 : 0);
+    p.dx_sums = take((size_t)p.dx.splits * n * d * 4);
+    p.dw_sums = take(p.dw.splits > 1 ? (size_t)p.dw.splits * whole * d * 4 : 0);
+    const long slabs = ceil_div(n, DZ_ROWS), tiles = 2 * ceil_div(n, p.zt);
+    p.db = take((size_t)(p.keep && slabs > tiles ? slabs : tiles) * p.pitch * 4);
   }
   p.total = at;
   return p;
@@ -395,6 +558,29 @@ Plan16 plan16(int n, int d, int classes, bool grads) {
 template <class C> inline dim3 grid_of(long work, int* blocks) {
   *blocks = (int)((work + 7) / 8 * 8);
   return dim3((unsigned)*blocks);
+}
+template <class C> void launch_sums(const LogitArgs& g, hipStream_t st) {
+  int blocks;
+  const dim3 grid = grid_of<C>(g.tiles, &blocks);
+  hipLaunchKernelGGL(lce_sums_kernel<C>, grid, dim3(C::THREADS), 0, st, g, blocks);
+}
+template <class C> void launch_dz(const LogitArgs& g, int parts, hipStream_t st) {
+  int blocks;
+  const dim3 grid = grid_of<C>(g.tiles, &blocks);
+  if (parts == 3) hipLaunchKernelGGL((lce_dz_kernel<C, 3>), grid, dim3(C::THREADS), 0, st, g, blocks);
+  else hipLaunchKernelGGL((lce_dz_kernel<C, 2>), grid, dim3(C::THREADS), 0, st, g, blocks);
+}
+template <class C> void launch_dx(const GemmOperand& dz, const GemmOperand& w, float* sums, int n, int d, int k, const Plan16& p, bool add, hipStream_t st) {
+  const int tm = (int)ceil_div(n, C::BM), tiles = tm * (int)ceil_div(d, C::BN);
+  int blocks;
+  const dim3 grid = grid_of<C>((long)tiles * p.dx.splits, &blocks);
+  hipLaunchKernelGGL(lce_dx_kernel<C>, grid, dim3(C::THREADS), 0, st, dz, w, sums, n, d, k, p.dx.k, tm, tiles, p.dx.splits, add ? 1 : 0, blocks);
+}
+template <class C> void launch_dw(const GemmOperand& dz, const GemmOperand& x, const float* scale, float* dw, int n, int d, int cols, const Plan16& p, hipStream_t st) {
+  const int tm = (int)ceil_div(cols, C::BM), tiles = tm * (int)ceil_div(d, C::BN);
+  int blocks;
+  const dim3 grid = grid_of<C>((long)tiles * p.dw.splits, &blocks);
+  hipLaunchKernelGGL(lce_dw_kernel<C>, grid, dim3(C::THREADS), 0, st, dz, x, scale, dw, n, d, cols, tm, tiles, p.dw.splits, p.dw.k, blocks);
 }
 
 }  // namespace
@@ -418,66 +604,77 @@ hipError_t linear_ce_bf16(const LceArgs& a) {
   };
   if (p.dp != a.d) x = pad(a.x, p.x, a.n);
   LogitArgs g{};
-  g.x = GemmOperand{x, a.n, p.dp, p.dp};
+  g.x = GemmOperand{x, {}, a.n, p.dp, p.dp};
   g.labels = a.labels;
   g.n = a.n; g.d = p.dp;
   g.part = (float*)(a.ws + p.part); g.z_label = s.z_label; g.splits = (int)p.splits;
   g.row_max = s.row_max; g.row_rest = s.row_rest;
-  g.hi = (bf16_t*)(a.ws + p.hi); g.lo = (bf16_t*)(a.ws + p.lo); g.pitch = p.pitch; g.ignore = a.ignore;
+  for (int i = 0; i < p.parts; ++i) g.dz[i] = (bf16_t*)(a.ws + p.dz[i]);
+  g.pitch = p.pitch; g.ignore = a.ignore;
   g.db_part = a.db ? (float*)(a.ws + p.db) : nullptr;
-  const int bm = p.z256 ? 256 : 128;
-  g.tiles_m = (int)ceil_div(a.n, bm);
+  g.tiles_m = (int)ceil_div(a.n, p.zt);
   auto piece = [&](long k) {
     g.v0 = (int)(k * p.piece);
     g.cols = (int)(a.classes - g.v0 < p.piece ? a.classes - g.v0 : p.piece);
     const bf16_t* w = (const bf16_t*)a.w + (size_t)g.v0 * a.d;
     if (p.dp != a.d) w = pad(w, p.w, g.cols);
-    g.w = GemmOperand{w, g.cols, p.dp, p.dp};
+    g.w = GemmOperand{w, {}, g.cols, p.dp, p.dp};
     g.bias = a.bias ? a.bias + g.v0 : nullptr;
-    g.split0 = (int)(k * (p.piece / bm));
+    g.split0 = (int)(k * (p.piece / p.zt));
   };
-  int blocks;
   for (long k = 0; k < p.pieces; ++k) {
     piece(k);
-    // every column of `part`: those of a last piece that has fewer classes, too
-    g.tiles = (int)(g.tiles_m * (p.piece / bm));
-    if (p.z256) hipLaunchKernelGGL(lce_sums_kernel<Z256>, grid_of<Z256>(g.tiles, &blocks), dim3(Z256::THREADS), 0, st, g, blocks);
-    else hipLaunchKernelGGL(lce_sums_kernel<Z128>, grid_of<Z128>(g.tiles, &blocks), dim3(Z128::THREADS), 0, st, g, blocks);
+    g.tiles = (int)(g.tiles_m * (p.piece / p.zt));     // every column of `part`: those of a last piece that has fewer classes, too
+    g.z = p.keep && k + 1 == p.pieces ? (float*)(a.ws + p.z) : nullptr;
+    if (p.zt == 256) launch_sums<Z256>(g, st);
+    else if (p.zt == 128) launch_sums<Z128>(g, st);
+    else launch_sums<Z64>(g, st);
   }
   if (const hipError_t e = lce_join(a, s, g.part, (int)p.splits); e != hipSuccess || !grads) return e;
-  for (long k = 0; k < p.pieces; ++k) {
-    if (k > 0 || p.pieces > 1) piece(k);
-    const int pitch_here = p.pieces > 1 ? (int)up(g.cols, 64) : p.pitch;        // classes of the piece that are multiplied
-    g.tiles = (int)(g.tiles_m * ceil_div(pitch_here, bm));
-    if (p.z256) hipLaunchKernelGGL(lce_dz_kernel<Z256>, grid_of<Z256>(g.tiles, &blocks), dim3(Z256::THREADS), 0, st, g, blocks);
-    else hipLaunchKernelGGL(lce_dz_kernel<Z128>, grid_of<Z128>(g.tiles, &blocks), dim3(Z128::THREADS), 0, st, g, blocks);
-    if (a.db)
-      hipLaunchKernelGGL(lce_db_kernel, dim3((unsigned)((g.cols + 255) / 256)), dim3(256), 0, st, g.db_part, s.scale, a.db + g.v0, 2 * g.tiles_m, p.pitch, g.cols);
-    const GemmOperand hi{g.hi, a.n, p.pitch, p.pitch}, lo{g.lo, a.n, p.pitch, p.pitch};
+  float* const sums = (float*)(a.ws + p.dx_sums);
+  for (long k = p.pieces - 1; k >= 0; --k) {           // (the last piece is still there)
+    const bool first = k + 1 == p.pieces, last = k == 0;
+    if (!first) piece(k);
+    const int wide = p.pieces > 1 ? (int)up(g.cols, 64) : p.pitch;        // classes of the piece that are multiplied
+    int db_parts = 2 * g.tiles_m;
+    if (first && p.keep) {
+      const int across = (p.pitch / 8 + 255) / 256;
+      db_parts = (int)ceil_div(a.n, DZ_ROWS);
+      if (p.parts == 3) hipLaunchKernelGGL(lce_dz_kept_kernel<3>, dim3((unsigned)(across * db_parts)), dim3(256), 0, st, g, across);
+      else hipLaunchKernelGGL(lce_dz_kept_kernel<2>, dim3((unsigned)(across * db_parts)), dim3(256), 0, st, g, across);
+    } else {
+      g.tiles = (int)(g.tiles_m * ceil_div(wide, p.zt));
+      if (p.zt == 256) launch_dz<Z256>(g, p.parts, st);
+      else if (p.zt == 128) launch_dz<Z128>(g, p.parts, st);
+      else launch_dz<Z64>(g, p.parts, st);
+    }
+    const GemmOperand dz{g.dz[0], {g.dz[1], g.dz[2]}, a.n, p.pitch, p.pitch};
     if (a.dx) {
-      float* const sums = (float*)(a.ws + p.dx);
-      const int tm = (int)ceil_div(a.n, p.x256 ? 256 : 128), tiles = tm * (int)ceil_div(a.d, p.x256 ? 256 : 128);
-      const long work = (long)tiles * p.dx_splits;
-      if (p.x256)
-        hipLaunchKernelGGL(lce_dx_kernel<X256>, grid_of<X256>(work, &blocks), dim3(X256::THREADS), 0, st, hi, g.w, sums, a.n, a.d, pitch_here, p.dx_k, tm, tiles,
-                           p.dx_splits, k > 0, blocks);
-      else
-        hipLaunchKernelGGL(lce_dx_kernel<X128>, grid_of<X128>(work, &blocks), dim3(X128::THREADS), 0, st, hi, g.w, sums, a.n, a.d, pitch_here, p.dx_k, tm, tiles,
-                           p.dx_splits, k > 0, blocks);
+      if (p.dx.tile == 256) launch_dx<X256>(dz, g.w, sums, a.n, a.d, wide, p, !first, st);
+      else if (p.dx.tile == 128) launch_dx<X128>(dz, g.w, sums, a.n, a.d, wide, p, !first, st);
+      else launch_dx<X64>(dz, g.w, sums, a.n, a.d, wide, p, !first, st);
     }
+    float* const dw = a.dw ? a.dw + (size_t)g.v0 * a.d : nullptr;
+    float* const dw_sums = (float*)(a.ws + p.dw_sums);
     if (a.dw) {
-      const int tm = (int)ceil_div(g.cols, p.w256 ? 256 : 128), tiles = tm * (int)ceil_div(a.d, p.w256 ? 256 : 128);
-      float* const dw = a.dw + (size_t)g.v0 * a.d;
-      if (p.w256)
-        hipLaunchKernelGGL(lce_dw_kernel<W256>, grid_of<W256>(tiles, &blocks), dim3(W256::THREADS), 0, st, hi, lo, g.x, s.scale, dw, a.n, a.d, g.cols, tm, tiles, blocks);
-      else
-        hipLaunchKernelGGL(lce_dw_kernel<W128>, grid_of<W128>(tiles, &blocks), dim3(W128::THREADS), 0, st, hi, lo, g.x, s.scale, dw, a.n, a.d, g.cols, tm, tiles, blocks);
+#define ACC_DW(C) launch_dw<C>(dz, g.x, s.scale, p.dw.splits > 1 ? dw_sums : dw, a.n, a.d, g.cols, p, st)
+      if (p.parts == 3) { if (p.dw.tile == 256) ACC_DW(V256); else if (p.dw.tile == 128) ACC_DW(V128); else ACC_DW(V64); }
+      else { if (p.dw.tile == 256) ACC_DW(W256); else if (p.dw.tile == 128) ACC_DW(W128); else ACC_DW(W64); }
+#undef ACC_DW
     }
-  }
-  if (a.dx) {
-    const size_t count = (size_t)a.n * a.d;
-    hipLaunchKernelGGL(lce_dx_finish_kernel, dim3((unsigned)((count + 1023) / 1024)), dim3(256), 0, st, (const float*)(a.ws + p.dx), s.scale, (bf16_t*)a.dx, count,
-                       p.dx_splits);
+    Finish f{};
+    f.scale = s.scale;
+    if (a.dx && last) {
+      f.sums = sums; f.dx = (bf16_t*)a.dx; f.count = (size_t)a.n * a.d; f.splits = p.dx.splits;
+      f.dx_blocks = (int)((f.count + 1023) / 1024);
+    }
+    if (a.dw && p.dw.splits > 1) {
+      f.dw_sums = dw_sums; f.dw = dw; f.dw_count = (size_t)g.cols * a.d; f.dw_splits = p.dw.splits;
+      f.dw_blocks = (int)((f.dw_count + 1023) / 1024);
+    }
+    if (a.db) { f.part = g.db_part; f.db = a.db + g.v0; f.parts = db_parts; f.pitch = p.pitch; f.cols = g.cols; }
+    const int blocks = f.dx_blocks + f.dw_blocks + (a.db ? (g.cols + 255) / 256 : 0);
+    if (blocks) hipLaunchKernelGGL(lce_finish_kernel, dim3((unsigned)blocks), dim3(256), 0, st, f);
   }
   return hipGetLastError();
 }
