@@ -29,6 +29,14 @@ __device__ __forceinline__ float exp_fast(float t) {
 // Tile `at` of a launch: every XCD takes a contiguous range (neighbours share operand rows in its L2), rows innermost.
 __device__ __forceinline__ int xcd_tile(int blocks) { return ((int)blockIdx.x & 7) * (blocks >> 3) + ((int)blockIdx.x >> 3); }
 
+// Which tile: columns in blocks of four, within a block row by row, so that the workgroups of an XCD that run at the same time (thirty-two) stand eight by
+// four and share operand rows both ways.
+struct TileAt { int m, n; };
+__device__ __forceinline__ TileAt tile_at(int at, int tiles_m, int tiles) {
+  const int block = at / (4 * tiles_m), in = at - block * 4 * tiles_m, left = tiles / tiles_m - 4 * block, width = left < 4 ? left : 4, m = in / width;
+  return TileAt{m, 4 * block + in - m * width};
+}
+
 template <class C>
 __device__ __forceinline__ void add_bias(GemmAcc<C>& acc, const float* __restrict__ bias, int col0, int cols) {
   const int lane = threadIdx.x & 63;
@@ -83,7 +91,8 @@ __global__ __launch_bounds__(C::THREADS, 2) void lce_sums_kernel(LogitArgs a, in
   __shared__ __attribute__((aligned(1024))) char lds[C::LDS > RED ? C::LDS : RED];
   const int at = xcd_tile(blocks);
   if (at >= a.tiles) return;
-  const int tile_n = at / a.tiles_m, tile_m = at - tile_n * a.tiles_m, m0 = tile_m * C::BM, n0 = tile_n * C::BN;
+  const TileAt where = tile_at(at, a.tiles_m, a.tiles);
+  const int tile_m = where.m, tile_n = where.n, m0 = tile_m * C::BM, n0 = tile_n * C::BN;
   GemmAcc<C> acc;
   gemm_tile<C>(a.x, a.w, m0, n0, 0, a.d, lds, acc);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm0 = (wave / C::WN) * 32 * C::MB, wn = wave % C::WN, wn0 = wn * 32 * C::NB;
@@ -189,7 +198,8 @@ __global__ __launch_bounds__(C::THREADS, 2) void lce_dz_kernel(LogitArgs a, int 
   __shared__ __attribute__((aligned(1024))) char lds[C::LDS > OUT ? C::LDS : OUT];
   const int at = xcd_tile(blocks);
   if (at >= a.tiles) return;
-  const int tile_n = at / a.tiles_m, tile_m = at - tile_n * a.tiles_m, m0 = tile_m * C::BM, n0 = tile_n * C::BN;
+  const TileAt where = tile_at(at, a.tiles_m, a.tiles);
+  const int tile_m = where.m, tile_n = where.n, m0 = tile_m * C::BM, n0 = tile_n * C::BN;
   GemmAcc<C> acc;
   gemm_tile<C>(a.x, a.w, m0, n0, 0, a.d, lds, acc);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm0 = (wave / C::WN) * 32 * C::MB, wn0 = (wave % C::WN) * 32 * C::NB;
@@ -326,7 +336,9 @@ __global__ __launch_bounds__(C::THREADS, 2) void lce_dx_kernel(GemmOperand dz, G
   __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
   const int work = xcd_tile(blocks);
   if (work >= tiles * splits) return;
-  const int split = work / tiles, at = work - split * tiles, tile_n = at / tiles_m, tile_m = at - tile_n * tiles_m, m0 = tile_m * C::BM, n0 = tile_n * C::BN;
+  const int split = work / tiles, at = work - split * tiles;
+  const TileAt where = tile_at(at, tiles_m, tiles);
+  const int m0 = where.m * C::BM, n0 = where.n * C::BN;
   GemmAcc<C> acc;
   gemm_tile<C>(dz, w, m0, n0, split * k_per_split, min(k, (split + 1) * k_per_split), lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm0 = (wave / C::WN) * 32 * C::MB, wn0 = (wave % C::WN) * 32 * C::NB;
@@ -412,7 +424,9 @@ __global__ __launch_bounds__(C::THREADS, 2) void lce_dw_kernel(GemmOperand dz, G
   __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
   const int work = xcd_tile(blocks);
   if (work >= tiles * splits) return;
-  const int split = work / tiles, at = work - split * tiles, tile_n = at / tiles_m, tile_m = at - tile_n * tiles_m, m0 = tile_m * C::BM, n0 = tile_n * C::BN;
+  const int split = work / tiles, at = work - split * tiles;
+  const TileAt where = tile_at(at, tiles_m, tiles);
+  const int m0 = where.m * C::BM, n0 = where.n * C::BN;
   GemmAcc<C> acc;
   gemm_tile<C>(dz, x, m0, n0, split * n_per_split, min(n, (split + 1) * n_per_split), lds, acc);
   const float sc = splits > 1 ? 1.f : scale[0];
