@@ -7,6 +7,17 @@
 
 namespace acc {
 
+// Tile `at` of a launch: every XCD takes a contiguous range (neighbours share operand rows in its L2), rows innermost.
+__device__ __forceinline__ int xcd_tile(int blocks) { return ((int)blockIdx.x & 7) * (blocks >> 3) + ((int)blockIdx.x >> 3); }
+
+// Which tile: columns in blocks of four, within a block row by row, so that the workgroups of an XCD that run at the same time (thirty-two) stand eight by
+// four and share operand rows both ways.
+struct TileAt { int m, n; };
+__device__ __forceinline__ TileAt tile_at(int at, int tiles_m, int tiles) {
+  const int block = at / (4 * tiles_m), in = at - block * 4 * tiles_m, left = tiles / tiles_m - 4 * block, width = left < 4 ? left : 4, m = in / width;
+  return TileAt{m, 4 * block + in - m * width};
+}
+
 struct LceArgs {
   const void *x, *w;
   const float* bias;

@@ -26,17 +26,6 @@ __device__ __forceinline__ float exp_fast(float t) {
 #endif
 }
 
-// Tile `at` of a launch: every XCD takes a contiguous range (neighbours share operand rows in its L2), rows innermost.
-__device__ __forceinline__ int xcd_tile(int blocks) { return ((int)blockIdx.x & 7) * (blocks >> 3) + ((int)blockIdx.x >> 3); }
-
-// Which tile: columns in blocks of four, within a block row by row, so that the workgroups of an XCD that run at the same time (thirty-two) stand eight by
-// four and share operand rows both ways.
-struct TileAt { int m, n; };
-__device__ __forceinline__ TileAt tile_at(int at, int tiles_m, int tiles) {
-  const int block = at / (4 * tiles_m), in = at - block * 4 * tiles_m, left = tiles / tiles_m - 4 * block, width = left < 4 ? left : 4, m = in / width;
-  return TileAt{m, 4 * block + in - m * width};
-}
-
 template <class C>
 __device__ __forceinline__ void add_bias(GemmAcc<C>& acc, const float* __restrict__ bias, int col0, int cols) {
   const int lane = threadIdx.x & 63;
@@ -545,7 +534,7 @@ Plan16 plan16(int n, int d, int classes, bool grads) {
   p.pieces = ceil_div(classes, p.piece);
   const long whole = p.pieces > 1 ? p.piece : classes;
   p.zt = choose(RowsByRows, n, whole, p.dp, 1, 0, 1L << 30).tile;
-  p.splits = p.pieces * (p.piece / p.zt);
+  p.splits = (p.pieces - 1) * (p.piece / p.zt) + ceil_div(classes - (p.pieces - 1) * p.piece, p.zt);
   p.pitch = (int)(p.pieces > 1 ? p.piece : up(classes, 64));
   // where the products take longer than writing and reading their results (us, second sweep of 777 x 1160 x 50001: 183 worked out again, 128 kept)
   p.keep = grads && d >= 1024;
@@ -638,7 +627,7 @@ hipError_t linear_ce_bf16(const LceArgs& a) {
   };
   for (long k = 0; k < p.pieces; ++k) {
     piece(k);
-    g.tiles = (int)(g.tiles_m * (p.piece / p.zt));     // every column of `part`: those of a last piece that has fewer classes, too
+    g.tiles = (int)(g.tiles_m * ceil_div(g.cols, p.zt));
     g.z = p.keep && k + 1 == p.pieces ? (float*)(a.ws + p.z) : nullptr;
     if (p.zt == 256) launch_sums<Z256>(g, st);
     else if (p.zt == 128) launch_sums<Z128>(g, st);
