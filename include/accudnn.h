@@ -414,10 +414,11 @@ int acc_op_softmax_ce(const void* z, const int32_t* labels, float* loss_rows, fl
  * decides; batch norm is acc_op_bn_*).  x [n][hw][c] NHWC; y = act(gamma * (x - mean) * istd + beta (+ res)); mean and istd:
  * n * groups floats each.  groups divides c; any c (sixteen bytes of channels at a time where a row is whole ones, one value at a time
  * otherwise).  act: ACC_ACT_RELU max(z, 0), ACC_ACT_SILU z / (1 + exp(-z)).  Values that are no numbers stay none.
- * bwd: g = dy * act'(z); dbeta = sum of g, dgamma = sum of g * (x - mean) * istd over n and hw; dx; dres (may be NULL, may be dy) = g.
+ * bwd: g = dy * act'(z); dbeta = sum of g, dgamma = sum of g * (x - mean) * istd over n and hw; dx; dres (may be NULL) = g.
  * y: the stored output, needed for ACC_ACT_RELU (g = dy where y > 0, else 0); res: the residual that went into the forward pass,
  * for ACC_ACT_SILU (NULL if there was none).  mean and istd are those of the forward pass.  workspace: acc_op_gn_workspace() bytes
- * (enough for both directions and storage types); nothing in it needs to be kept or cleared.  No atomics: the same bits every time. */
+ * (enough for both directions and storage types); nothing in it needs to be kept or cleared.  No atomics: the same bits every time.
+ * y may be x or res, dx may be x or dy, dres may be dy; nothing else that is written may overlap another argument (ACC_EINVAL). */
 enum { ACC_ACT_NONE = 0, ACC_ACT_RELU = 1, ACC_ACT_SILU = 2 };
 size_t acc_op_gn_workspace(int n, int hw, int c, int groups);
 int acc_op_gn_fwd(const void* x, const float* gamma, const float* beta, const void* res, void* y, float* mean, float* istd,
@@ -430,12 +431,13 @@ int acc_op_gn_bwd(const void* x, const void* dy, const void* y, const void* res,
 /* A fully connected layer with its softmax cross-entropy, without the logits: z = x w^T + bias is worked out in pieces of the
  * classes and never kept whole (n * classes values are the largest map of a head with many classes), loss and gradients as
  * acc_op_softmax_ce defines them.  x [n][d], w [classes][d] and dx [n][d] are stored as dtype; bias [classes] (may be NULL), loss_rows [n], loss [1],
- * dw [classes][d] and db [classes] are fp32; labels [n] int32, device.  Sums, logits and dz are fp32 (dz of bf16 operands as the sum of two
- * bf16 values in dw, as one in dx, which is rounded to bf16 itself).
+ * dw [classes][d] and db [classes] are fp32; labels [n] int32, device.  Sums, logits and dz are fp32 (dz of bf16 operands: the sum of two
+ * bf16 values in dw, of three for fewer than 4096 rows; one in dx, which is rounded to bf16 itself).
  * ignore: rows with this label do not count (padding): loss_rows is 0 there, their gradient is 0, and the mean is over the others (0 if
  * there are none); their x still has to be finite.  ACC_LABEL_NONE: every row counts.  Any other label outside [0, classes): the row's loss is
  * NaN and its gradient has no one-hot term.  Logits of minus infinity (a bias that rules a class out) have probability 0.
- * loss_rows, loss, dx, dw, db: each may be NULL, at least one is not; without dx, dw and db no gradient is computed.
+ * loss_rows, loss, dx, dw, db: each may be NULL, at least one is not; without dx, dw and db no gradient is computed.  What is written may not
+ * overlap another argument (ACC_EINVAL).
  * n <= 2^20, d <= 65536, classes <= 2^24.  workspace: acc_op_linear_ce_workspace() bytes, gradients = whether any of dx, dw, db is asked for. */
 #define ACC_LABEL_NONE INT32_MIN
 size_t acc_op_linear_ce_workspace(int n, int d, int classes, int gradients, int dtype);
@@ -451,7 +453,7 @@ int acc_op_linear_ce(const void* x, const void* w, const float* bias, const int3
  * place.  What is written may not overlap any other tensor of the list (ACC_EINVAL; so the same tensor may not be listed twice).
  * list_bytes: the size of the list's memory, the same in every call, at least acc_op_tensor_list_bytes() (0: no list, or more than 2^30 pieces of 16384 values).
  * norm: one float, device.  workspace: acc_op_grad_norm_workspace() bytes, not shared by calls that overlap.
- * acc_op_grad_clip: dst = src * (norm <= max_norm ? 1 : max_norm / norm), rounded once; max_norm >= 0.  A norm that is NaN makes every value
+ * acc_op_grad_clip: dst = src * (norm <= max_norm ? 1 : max_norm / norm), the quotient in fp32, the product rounded to the tensor's type; max_norm >= 0.  A norm that is NaN makes every value
  * NaN, an infinite one every finite value 0.  Squares and sums are fp64, in a fixed order. */
 size_t acc_op_tensor_list_bytes(const size_t* counts, int n);
 int acc_op_tensor_list(const void* const* src, void* const* dst, const size_t* counts, const int32_t* dtypes, int n, void* list,

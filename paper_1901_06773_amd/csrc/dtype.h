@@ -26,8 +26,8 @@ __host__ __device__ inline bf16_t float_to_bf16(float f) {
   return (bf16_t)(c.u >> 16);
 }
 
-// Two values in one word, rounded to nearest even by the conversion instruction (four instructions and more a value otherwise: group norm,
-// bf16 2048 channels, 64 images of 7x7 forward 15.4 -> 11 us).
+// Two values in one word, rounded to nearest even by the conversion instruction (four instructions and more a value otherwise: group norm
+// forward, bf16, 256 channels, 64 images of 56x56 62 -> 58 us, 2048 channels, 64 images of 7x7 14.4 -> 13.8).
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 #if defined(__HIP_DEVICE_COMPILE__)
   typedef __bf16 v2bf __attribute__((ext_vector_type(2)));

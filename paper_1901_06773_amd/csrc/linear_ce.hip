@@ -547,7 +547,8 @@ Plan32 plan32(int n, int d, int classes, bool grads, int dtype) {
   // 256 x 64 x 50000 50 / 132, and of few rows and classes 41 x 2048 x 1000 11.5 / 5.9, 16 x 2048 x 4096 20 / 16; dw 4096 x 1024 x 8192 546 / 346,
   // 1024 x 256 x 8192 47 / 40, 256 x 2048 x 32768 288 / 303, 4096 x 128 x 1000 14 / 17.
   const double units = (double)n * d * p.piece;
-  const bool whole = !p.widen && d % 4 == 0 && d >= 16 && classes >= 16 && classes % 4 == 0 && classes % p.piece % 16 == 0;
+  // (and the convolution's fast loads reach 4 GiB)
+  const bool whole = !p.widen && (long)n * d * 4 <= 0xFFFFFF00L && (long)p.piece * d * 4 <= 0xFFFFFF00L && d % 4 == 0 && d >= 16 && classes >= 16 && classes % 4 == 0 && classes % p.piece % 16 == 0;
   p.conv_z = whole && d >= 128 && n >= 64 && units >= 1e9;
   p.conv_dx = whole && ((units >= 2e9 && (long)n * d >= 1L << 21) || (n <= 64 && classes <= 4096 && d >= 256));
   p.conv_dw = whole && d >= 256 && (n >= 512 || n <= 64);

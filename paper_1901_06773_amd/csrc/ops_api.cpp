@@ -216,12 +216,41 @@ static int told(hipError_t e, const char* text) {
   return status(e);
 }
 
+// What a call writes must not overlap anything else that it is given, but for tensors of the same kind that begin at the same address where a value is read
+// by the thread that writes it (`over`).  Null: not given.
+struct Given {
+  const void* p;
+  size_t bytes;
+  const void* over[2];
+};
+static bool clash(std::initializer_list<Given> written, std::initializer_list<Given> read) {
+  auto meet = [](const Given& a, const Given& b) {
+    const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+    return x && y && x < y + b.bytes && y < x + a.bytes;
+  };
+  for (const Given* w = written.begin(); w != written.end(); ++w) {
+    for (const Given* v = w + 1; v != written.end(); ++v)
+      if (meet(*w, *v)) return true;
+    for (const Given& r : read)
+      if (meet(*w, r) && !(w->p == r.p && w->bytes == r.bytes && (w->over[0] == r.p || w->over[1] == r.p))) return true;
+  }
+  return false;
+}
+// sizes that the launchers look at (and may refuse) anyway: here only that the products below don't overflow
+static bool sizes_ok(int a, int b, int c) { return a > 0 && b > 0 && c > 0 && (double)a * b * c < 1e15; }
+
 extern "C" size_t acc_op_gn_workspace(int n, int hw, int c, int groups) { return al256(gn_workspace_bytes(n, hw, c, groups)); }
 
 extern "C" int acc_op_gn_fwd(const void* x, const float* gamma, const float* beta, const void* res, void* y, float* mean, float* istd, int n, int hw,
                              int c, int groups, int act, float eps, void* workspace, size_t workspace_bytes, int dtype, void* stream) {
   if (!dtype_ok(dtype)) return refuse("acc_op_gn_fwd: dtype must be ACC_F32 or ACC_BF16");
   if (!al16({x, gamma, beta, res, y, mean, istd, workspace})) return refuse("acc_op_gn_fwd: pointers must be 16-byte aligned");
+  if (sizes_ok(n, hw, c) && groups > 0) {
+    const size_t map = (size_t)n * hw * c * dt_size(dtype), row = (size_t)c * 4, stats = (size_t)n * groups * 4;
+    if (clash({{y, map, {x, res}}, {mean, stats, {}}, {istd, stats, {}}, {workspace, workspace_bytes, {}}},
+              {{x, map, {}}, {res, map, {}}, {gamma, row, {}}, {beta, row, {}}}))
+      return refuse("acc_op_gn_fwd: what is written overlaps another argument (y may be x or res)");
+  }
   return told(gn_forward(x, gamma, beta, res, y, mean, istd, n, hw, c, groups, act, eps, workspace, workspace_bytes, dtype, (hipStream_t)stream),
               "acc_op_gn_fwd: null pointer, sizes that are not positive or too large, groups that do not divide c, unknown act, eps < 0 or a workspace "
               "smaller than acc_op_gn_workspace()");
@@ -232,6 +261,13 @@ extern "C" int acc_op_gn_bwd(const void* x, const void* dy, const void* y, const
                              void* workspace, size_t workspace_bytes, int dtype, void* stream) {
   if (!dtype_ok(dtype)) return refuse("acc_op_gn_bwd: dtype must be ACC_F32 or ACC_BF16");
   if (!al16({x, dy, y, res, gamma, beta, mean, istd, dx, dgamma, dbeta, dres, workspace})) return refuse("acc_op_gn_bwd: pointers must be 16-byte aligned");
+  if (sizes_ok(n, hw, c) && groups > 0) {
+    const size_t map = (size_t)n * hw * c * dt_size(dtype), row = (size_t)c * 4, stats = (size_t)n * groups * 4;
+    if (clash({{dx, map, {x, dy}}, {dres, map, {dy}}, {dgamma, row, {}}, {dbeta, row, {}}, {workspace, workspace_bytes, {}}},
+              {{x, map, {}}, {dy, map, {}}, {act == ACC_ACT_RELU ? y : nullptr, map, {}}, {act == ACC_ACT_SILU ? res : nullptr, map, {}}, {gamma, row, {}},
+               {beta, row, {}}, {mean, stats, {}}, {istd, stats, {}}}))
+      return refuse("acc_op_gn_bwd: what is written overlaps another argument (dx may be x or dy, dres may be dy)");
+  }
   return told(gn_backward(x, dy, y, res, gamma, beta, mean, istd, dx, dgamma, dbeta, dres, n, hw, c, groups, act, workspace, workspace_bytes, dtype,
                           (hipStream_t)stream),
               "acc_op_gn_bwd: null pointer (y is needed with ACC_ACT_RELU), sizes that are not positive or too large, groups that do not divide c, "
@@ -247,6 +283,12 @@ extern "C" int acc_op_linear_ce(const void* x, const void* w, const float* bias,
                                 void* stream) {
   if (!dtype_ok(dtype)) return refuse("acc_op_linear_ce: dtype must be ACC_F32 or ACC_BF16");
   if (!al16({x, w, bias, labels, loss_rows, loss, dx, dw, db, workspace})) return refuse("acc_op_linear_ce: pointers must be 16-byte aligned");
+  if (sizes_ok(n, d, classes)) {
+    const size_t es = dt_size(dtype), nx = (size_t)n * d, nw = (size_t)classes * d;
+    if (clash({{loss_rows, (size_t)n * 4, {}}, {loss, 4, {}}, {dx, nx * es, {}}, {dw, nw * 4, {}}, {db, (size_t)classes * 4, {}}, {workspace, workspace_bytes, {}}},
+              {{x, nx * es, {}}, {w, nw * es, {}}, {bias, (size_t)classes * 4, {}}, {labels, (size_t)n * 4, {}}}))
+      return refuse("acc_op_linear_ce: what is written overlaps another argument");
+  }
   return told(linear_ce(x, w, bias, labels, ignore, loss_rows, loss, dx, dw, db, n, d, classes, workspace, workspace_bytes, dtype, (hipStream_t)stream),
               "acc_op_linear_ce: null pointer, no result asked for, sizes that are not positive or too large, or a workspace smaller than "
               "acc_op_linear_ce_workspace()");

@@ -159,6 +159,28 @@ def test_the_residuals_gradient_in_place_of_the_upstream_one(n, hw, c, groups):
         assert all(torch.equal(p, q) for p, q in zip(apart, joint))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,hw,c,groups", [(2, 49, 512, 32), (200, 49, 256, 32), (1, 9000, 64, 8), (3, 30, 30, 3)])
+def test_in_place(n, hw, c, groups, dtype):
+    dt = DT[dtype][0]
+    x, res, dy = (randn(k, n, hw, c).to(dt) for k in (1, 2, 3))
+    gamma, beta = randn(4, c), randn(5, c)
+    ws = torch.empty(B().op_gn_workspace(n, hw, c, groups), dtype=torch.uint8, device="cuda")
+    for act in (0, 1, 2):
+        y, mean, istd = forward(x, gamma, beta, res, groups, act)
+        for over in ("x", "res"):
+            t = dict(x=x.clone(), res=res.clone())
+            B().op_gn_fwd(t["x"], gamma, beta, t["res"], t[over], mean, istd, groups, act, EPS, ws)
+            assert torch.equal(t[over], y)
+        stored, side = (y if act == 1 else None), (res if act == 2 else None)
+        dx, dg, db, dres = backward(x, dy, stored, side, gamma, beta, mean, istd, groups, act, True)
+        for over in ("x", "dy"):
+            t = dict(x=x.clone(), dy=dy.clone())
+            g2, b2, r2 = torch.empty_like(dg), torch.empty_like(db), torch.empty_like(x)
+            B().op_gn_bwd(t["x"], t["dy"], stored, side, gamma, beta, mean, istd, t[over], g2, b2, r2, groups, act, ws)
+            assert all(torch.equal(a, b) for a, b in ((t[over], dx), (g2, dg), (b2, db), (r2, dres)))
+
+
 def test_differences():
     """The gradients against central differences of the forward pass in 64 bits around the library's own."""
     n, hw, c, groups = 2, 6, 12, 3

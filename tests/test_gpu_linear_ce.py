@@ -93,6 +93,39 @@ def test_several_pieces(n, d, classes, dtype):
     agree(call(x, w, b, labels), reference(x, w, b, labels), dtype)
 
 
+# widths of one to three values, odd ones, few rows with a long sum that is cut, more rows than a launch of whole rows takes, an odd last piece
+ODD = [(1, 1, 8193), (17, 2, 20000), (700, 3, 8195), (66, 57, 9001), (42, 2050, 8301), (129, 1027, 131), (20000, 9, 40), (16385, 3, 4), (8000, 61, 20001),
+       (64, 4096, 8300), (2000, 17, 3), (33, 700, 16999)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,d,classes", ODD)
+def test_odd_widths(n, d, classes, dtype):
+    x, w, b, labels = inputs(n, d, classes, dtype)
+    labels[::5] = -7
+    got, ref = call(x, w, b, labels, ignore=-7), reference(x, w, b, labels, ignore=-7)
+    agree(got, ref, dtype)
+    for k in ("rows", "dw"):
+        assert torch.equal(call(x, w, b, labels, ignore=-7, want=(k,))[k], got[k]), k
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,d,classes", [(65, 57, 9001), (42, 2050, 8301), (129, 1027, 131), (7, 3, 5), (8000, 61, 20001)])
+def test_nothing_is_written_behind_the_results(n, d, classes, dtype):
+    x, w, b, labels = inputs(n, d, classes, dtype)
+    behind = 4096
+
+    def buffer(count, dt=torch.float32):
+        return torch.full((count + behind,), 77.0, device="cuda", dtype=dt)
+    size = B().op_linear_ce_workspace(n, d, classes, True, B()._dtype_of(x))
+    bufs = dict(rows=buffer(n), loss=buffer(1), dx=buffer(n * d, x.dtype), dw=buffer(classes * d), db=buffer(classes),
+                ws=torch.full((size + behind,), 77, device="cuda", dtype=torch.uint8))
+    B().op_linear_ce(x, w, b, labels, bufs["rows"][:n], bufs["loss"][:1], bufs["dx"][:n * d].view(n, d), bufs["dw"][:classes * d].view(classes, d),
+                     bufs["db"][:classes], bufs["ws"][:size])
+    assert all((v[-behind:] == 77).all() for v in bufs.values())
+    assert all(torch.isfinite(v).all() for k, v in bufs.items() if k != "ws")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,d,classes", [(1, 64, 100), (90, 72, 300), (300, 256, 2000)])
 def test_rows_that_do_not_count(n, d, classes, dtype):

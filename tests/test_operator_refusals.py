@@ -15,10 +15,14 @@ def text():
     return L.acc_last_error(None).decode()
 
 
-GN = dict(x=P, gamma=P, beta=P, res=None, y=P, mean=P, istd=P, n=2, hw=9, c=12, groups=3, act=1, eps=1e-5, ws=P, size=BIG, dtype=B.F32)
-GNB = dict(x=P, dy=P, y=P, res=None, gamma=P, beta=P, mean=P, istd=P, dx=P, dgamma=P, dbeta=P, dres=None, n=2, hw=9, c=12, groups=3, act=1, ws=P,
-           size=BIG, dtype=B.F32)
-CE = dict(x=P, w=P, bias=None, labels=P, ignore=-1, rows=P, loss=P, dx=P, dw=P, db=P, n=4, d=8, classes=5, ws=P, size=BIG, dtype=B.BF16)
+def at(k):
+    return k << 44            # far from one another
+
+
+GN = dict(x=at(1), gamma=at(2), beta=at(3), res=None, y=at(4), mean=at(5), istd=at(6), n=2, hw=9, c=12, groups=3, act=1, eps=1e-5, ws=at(7), size=BIG, dtype=B.F32)
+GNB = dict(x=at(1), dy=at(2), y=at(3), res=None, gamma=at(4), beta=at(5), mean=at(6), istd=at(7), dx=at(8), dgamma=at(9), dbeta=at(10), dres=None, n=2,
+           hw=9, c=12, groups=3, act=1, ws=at(11), size=BIG, dtype=B.F32)
+CE = dict(x=at(1), w=at(2), bias=None, labels=at(3), ignore=-1, rows=at(4), loss=at(5), dx=at(6), dw=at(7), db=at(8), n=4, d=8, classes=5, ws=at(9), size=BIG, dtype=B.BF16)
 
 
 def refused(fn, good, **bad):
@@ -47,6 +51,19 @@ def test_group_norm_backward(bad):
                                  dict(x=ODD), dict(w=ODD), dict(labels=ODD), dict(dw=ODD), dict(bias=ODD), dict(dtype=7)])
 def test_linear_cross_entropy(bad):
     refused(L.acc_op_linear_ce, CE, **bad)
+
+
+@pytest.mark.parametrize("fn,good,bad", [
+    (L.acc_op_gn_fwd, GN, dict(y=at(1) + 16)), (L.acc_op_gn_fwd, GN, dict(mean=at(6))), (L.acc_op_gn_fwd, GN, dict(istd=at(3) + 32)),
+    (L.acc_op_gn_fwd, GN, dict(ws=at(1) - 4096)), (L.acc_op_gn_fwd, GN, dict(res=at(4) + 64)),
+    (L.acc_op_gn_bwd, GNB, dict(dx=at(3))), (L.acc_op_gn_bwd, GNB, dict(dx=at(2), dres=at(2))), (L.acc_op_gn_bwd, GNB, dict(dres=at(1))),
+    (L.acc_op_gn_bwd, GNB, dict(dgamma=at(10))), (L.acc_op_gn_bwd, GNB, dict(dbeta=at(5))), (L.acc_op_gn_bwd, GNB, dict(dx=at(2) + 16)),
+    (L.acc_op_gn_bwd, GNB, dict(act=2, y=None, res=at(8))),
+    (L.acc_op_linear_ce, CE, dict(dx=at(1))), (L.acc_op_linear_ce, CE, dict(dw=at(2))), (L.acc_op_linear_ce, CE, dict(bias=at(8))),
+    (L.acc_op_linear_ce, CE, dict(rows=at(3))), (L.acc_op_linear_ce, CE, dict(db=at(7) + 16)), (L.acc_op_linear_ce, CE, dict(ws=at(2) - 256))])
+def test_results_over_other_arguments(fn, good, bad):
+    refused(fn, good, **bad)
+    assert "overlaps" in text()
 
 
 def test_workspaces_of_sizes_that_are_refused():
