@@ -370,10 +370,7 @@ struct Product32 {
   int k, k_per_split, add, tiles_m, tiles, work;
 };
 template <class C>
-__global__ __launch_bounds__(C::THREADS) void product32_kernel(Product32 a, int blocks) {
-  __shared__ __attribute__((aligned(16))) float lds[C::LDS];
-  const int work = xcd_tile(blocks);
-  if (work >= a.work) return;
+__device__ __forceinline__ void product32(const Product32& a, int work, float* lds) {
   const int split = work / a.tiles;
   const TileAt where = tile_at(work - split * a.tiles, a.tiles_m, a.tiles);
   const int rows = a.a.extent, cols = a.b.extent, m0 = where.m * C::BM, n0 = where.n * C::BN;
@@ -399,6 +396,12 @@ __global__ __launch_bounds__(C::THREADS) void product32_kernel(Product32 a, int 
           if (c + e < cols) to[e] = a.add ? to[e] + acc[i][j][e] : acc[i][j][e];
       }
     }
+}
+template <class C>
+__global__ __launch_bounds__(C::THREADS) void product32_kernel(Product32 a, int blocks) {
+  __shared__ __attribute__((aligned(16))) float lds[C::LDS];
+  const int work = xcd_tile(blocks);
+  if (work < a.work) product32<C>(a, work, lds);
 }
 
 // ---------------------------------------------------------------------------------- the last launch of a piece
@@ -435,8 +438,7 @@ __device__ __forceinline__ void join_sums(const float* __restrict__ sums, T* __r
   }
 }
 template <class T>
-__global__ __launch_bounds__(THREADS) void finish32_kernel(Finish32 f) {
-  unsigned block = blockIdx.x;
+__device__ __forceinline__ void finish32(const Finish32& f, unsigned block) {
   if (block < f.dx_blocks) return join_sums<T>(f.dx_sums, (T*)f.dx, f.dx_count, f.dx_splits, block);
   block -= f.dx_blocks;
   if (block < f.dw_blocks) return join_sums<float>(f.dw_sums, f.dw, f.dw_count, f.dw_splits, block);
@@ -462,6 +464,25 @@ __global__ __launch_bounds__(THREADS) void finish32_kernel(Finish32 f) {
   sh[threadIdx.x] = s;
   __syncthreads();
   if (threadIdx.x < 64 && j < f.cols) f.db[(size_t)slab * f.pitch + j] = (float)(sh[threadIdx.x] + sh[threadIdx.x + 64] + sh[threadIdx.x + 128] + sh[threadIdx.x + 192]);
+}
+template <class T>
+__global__ __launch_bounds__(THREADS) void finish32_kernel(Finish32 f) { finish32<T>(f, blockIdx.x); }
+
+// dx, dw, db and the mean loss in one launch, 64 x 64 tiles.  They all wait for dz only: where there are few tiles, three launches less.
+typedef Gemm32Cfg<2, 2, 2, 2, false, true> Dx64;
+typedef Gemm32Cfg<2, 2, 2, 2, true, true> Dw64;
+__global__ __launch_bounds__(THREADS) void grads32_kernel(Product32 dx, Product32 dw, Finish32 rest, int dx_blocks, int dw_blocks) {
+  __shared__ __attribute__((aligned(16))) float lds[Dx64::LDS > Dw64::LDS ? Dx64::LDS : Dw64::LDS];
+  const int block = blockIdx.x;                        // (each part begins at a multiple of eight)
+  if (block < dx_blocks) {
+    const int work = (block & 7) * (dx_blocks >> 3) + (block >> 3);
+    if (work < dx.work) product32<Dx64>(dx, work, lds);
+  } else if (block < dx_blocks + dw_blocks) {
+    const int work = (block & 7) * (dw_blocks >> 3) + ((block - dx_blocks) >> 3);
+    if (work < dw.work) product32<Dw64>(dw, work, lds);
+  } else {
+    finish32<float>(rest, (unsigned)(block - dx_blocks - dw_blocks));
+  }
 }
 // the slabs' sums
 __global__ __launch_bounds__(THREADS) void db_kernel(const float* __restrict__ part, float* __restrict__ db, int parts, int pitch, int cols) {
@@ -493,10 +514,10 @@ struct Cut {
 };
 constexpr int kTile32[3][2] = {{32, 128}, {64, 64}, {128, 128}};
 constexpr double kChunk32[3][2] = {{0.93, 0.68}, {0.88, 0.66}, {3.0, 2.1}};
-Cut cut32(long m, long n, long k, long most_sums) {
+Cut cut32(long m, long n, long k, long most_sums, int only = -1) {
   Cut best{1, 1, (int)up(k, 32)};
   double us = 0;
-  for (int t = 0; t < 3; ++t) {
+  for (int t = only < 0 ? 0 : only; t < (only < 0 ? 3 : only + 1); ++t) {
     const long tiles = ceil_div(m, kTile32[t][0]) * ceil_div(n, kTile32[t][1]);
     for (int i = 0; i < 10; ++i) {
       const long s = i < 7 ? 1L << i : (256L << (i - 7)) / tiles;
@@ -504,8 +525,8 @@ Cut cut32(long m, long n, long k, long most_sums) {
       const long each = up(ceil_div(k, s), 32), splits = ceil_div(k, each);
       if (s > 1 && (each < 128 || splits * m * n > most_sums)) continue;
       const double one = each / 32.0 * kChunk32[t][0], all = ceil_div(tiles * splits, 256) * (each / 32.0) * kChunk32[t][1];
-      const double v = (one > all ? one : all) + (splits > 1 ? 2.0 + 0.15 * splits + (double)splits * m * n * 8 / 5e6 : 0.0);
-      if ((t == 0 && i == 0) || v < us) {
+      const double v = (one > all ? one : all) + (splits > 1 ? (only < 0 ? 2.0 : 5.0) + 0.15 * splits + (double)splits * m * n * 8 / 5e6 : 0.0);
+      if (us == 0 || v < us) {
         us = v;
         best = Cut{t, (int)splits, (int)each};
       }
@@ -521,6 +542,7 @@ struct Plan32 {
   bool conv_z, conv_dx, conv_dw; // products of the convolution kernels
   bool late;                     // the logits' sums and bias in a launch of their own: row_sums_kernel
   bool widen;                    // bf16 operands are copied
+  bool together;                 // dx, dw, db and the mean in one launch
   int dz_rows, slabs;            // rows of a workgroup of dz_kernel, and workgroups
   Cut z, dx, dw;
   bool sum_dx;                   // dx from `dx_sums`
@@ -544,17 +566,21 @@ Plan32 plan32(int n, int d, int classes, bool grads, int dtype) {
   // here at up to 140, any width, with the sum over k cut where there are few tiles.  Measured, us, here / convolution: logits 1024 x 2048 x 32768
   // 1134 / 804, 256 x 2048 x 32768 292 / 218, 1024 x 1024 x 1000 33 / 28, 256 x 512 x 10000 42 / 40, but 300 x 2048 x 1000 26 / 35, 1024 x 64 x 50000
   // 114 / 173, 32 x 1024 x 32768 39 / 54; dx 4096 x 1024 x 8192 519 / 350, 1024 x 1024 x 8192 137 / 136, 256 x 2048 x 32768 268 / 412,
-  // 256 x 64 x 50000 50 / 132, and of few rows and classes 41 x 2048 x 1000 11.5 / 5.9, 16 x 2048 x 4096 20 / 16; dw 4096 x 1024 x 8192 546 / 346,
+  // 256 x 64 x 50000 50 / 132, and of few rows and classes (all results) 41 x 2048 x 1000 33 / 30, 16 x 2048 x 4096 58 / 52, 64 x 256 x 256 19 / 26; dw 4096 x 1024 x 8192 546 / 346,
   // 1024 x 256 x 8192 47 / 40, 256 x 2048 x 32768 288 / 303, 4096 x 128 x 1000 14 / 17.
   const double units = (double)n * d * p.piece;
   // (and the convolution's fast loads reach 4 GiB)
   const bool whole = !p.widen && (long)n * d * 4 <= 0xFFFFFF00L && (long)p.piece * d * 4 <= 0xFFFFFF00L && d % 4 == 0 && d >= 16 && classes >= 16 && classes % 4 == 0 && classes % p.piece % 16 == 0;
   p.conv_z = whole && d >= 128 && n >= 64 && units >= 1e9;
-  p.conv_dx = whole && ((units >= 2e9 && (long)n * d >= 1L << 21) || (n <= 64 && classes <= 4096 && d >= 256));
-  p.conv_dw = whole && d >= 256 && (n >= 512 || n <= 64);
+  p.conv_dx = whole && ((units >= 2e9 && (long)n * d >= 1L << 21) || (n <= 64 && classes >= 640 && classes <= 4096 && d >= 256));
+  p.conv_dw = whole && d >= 256 && (n >= 512 || (n <= 64 && classes >= 640));
   p.z = cut32(n, p.piece, d, p.rows || (p.pieces == 1 && n * p.piece <= 1L << 22) ? 1L << 24 : 0);
   p.dx = cut32(n, d, p.piece, 1L << 25);
   p.dw = cut32(p.piece, d, n, 1L << 24);
+  const Cut dx = cut32(n, d, p.piece, 1L << 25, 1), dw = cut32(p.piece, d, n, 1L << 24, 1);
+  auto works = [](long m, long k, const Cut& c) { return ceil_div(m, 64) * ceil_div(k, 64) * c.splits; };
+  p.together = !p.conv_dx && !p.conv_dw && works(n, d, dx) + works(p.piece, d, dw) <= 1024;
+  if (p.together) { p.dx = dx; p.dw = dw; }
   p.late = !p.rows && (p.conv_z || p.z.splits > 1);
   const long split_cols = p.late ? kSplitCols : kTile32[p.z.tile][1];
   p.splits = (p.pieces - 1) * ceil_div(p.piece, split_cols) + ceil_div(classes - (p.pieces - 1) * p.piece, split_cols);
@@ -607,11 +633,13 @@ hipError_t widen(const void* in, float* out, size_t total, hipStream_t st) {
 
 inline unsigned whole_eights(long work) { return (unsigned)((work + 7) / 8 * 8); }
 
-template <bool AT, bool BT> hipError_t product32(Product32 g, const Cut& c, hipStream_t st) {
+void cut_into(Product32& g, const Cut& c) {
   g.tiles_m = (int)ceil_div(g.a.extent, kTile32[c.tile][0]);
   g.tiles = g.tiles_m * (int)ceil_div(g.b.extent, kTile32[c.tile][1]);
   g.k_per_split = c.k;
   g.work = g.tiles * c.splits;
+}
+template <bool AT, bool BT> hipError_t launch_product32(const Product32& g, const Cut& c, hipStream_t st) {
   const unsigned blocks = whole_eights(g.work);
   if (c.tile == 0) hipLaunchKernelGGL((product32_kernel<Gemm32Cfg<1, 4, 2, 2, AT, BT>>), dim3(blocks), dim3(256), 0, st, g, (int)blocks);
   else if (c.tile == 1) hipLaunchKernelGGL((product32_kernel<Gemm32Cfg<2, 2, 2, 2, AT, BT>>), dim3(blocks), dim3(256), 0, st, g, (int)blocks);
@@ -697,25 +725,23 @@ hipError_t run32(const LceArgs& a) {
       hipLaunchKernelGGL(dz_kernel, dim3((unsigned)ceil_div(pitch / 4, THREADS), (unsigned)p.slabs), dim3(THREADS), 0, st, z, p.late ? a.bias : nullptr, a.labels,
                          a.ignore, s.row_max, s.row_rest, s.scale, a.db ? db_part : nullptr, a.n, pitch, cols, (int)v0, p.dz_rows);
     Finish32 f{};
-    if (a.dx) {
-      if (p.conv_dx) {
-        ConvGeom g = product_geom(z, nullptr, (float*)a.dx, a.n, cols, a.d, !first);
-        g.w_kn = w;                              // few rows: the filter as it lies
-        if (!conv_igemm_rows_takes(g, a.n, cols)) {
-          float* const wt = (float*)(a.ws + p.wt);
-          ACC_TRY(filter_flip_transpose(w, wt, cols, a.d, 1, 1, DT_F32, st));
-          g = product_geom(z, wt, (float*)a.dx, a.n, cols, a.d, !first);
-        }
-        ACC_TRY(conv_igemm(g, st));
-      } else {
-        Product32 g{};
-        g.a = {z, a.n, pitch}; g.b = {w, a.d, a.d}; g.out = dx_out; g.k = cols; g.add = !first;
-        Cut c = p.dx;
-        ACC_TRY((product32<false, true>(g, c, st)));
-        if (p.sum_dx && last) {
-          f.dx_sums = dx_out; f.dx = a.dx; f.dx_count = (size_t)a.n * a.d; f.dx_splits = p.dx.splits;
-          f.dx_blocks = (unsigned)((f.dx_count + 1023) / 1024);
-        }
+    Product32 gx{}, gw{};
+    if (a.dx && p.conv_dx) {
+      ConvGeom g = product_geom(z, nullptr, (float*)a.dx, a.n, cols, a.d, !first);
+      g.w_kn = w;                              // few rows: the filter as it lies
+      if (!conv_igemm_rows_takes(g, a.n, cols)) {
+        float* const wt = (float*)(a.ws + p.wt);
+        ACC_TRY(filter_flip_transpose(w, wt, cols, a.d, 1, 1, DT_F32, st));
+        g = product_geom(z, wt, (float*)a.dx, a.n, cols, a.d, !first);
+      }
+      ACC_TRY(conv_igemm(g, st));
+    } else if (a.dx) {
+      gx.a = {z, a.n, pitch}; gx.b = {w, a.d, a.d}; gx.out = dx_out; gx.k = cols; gx.add = !first;
+      cut_into(gx, p.dx);
+      if (!p.together) ACC_TRY((launch_product32<false, true>(gx, p.dx, st)));
+      if (p.sum_dx && last) {
+        f.dx_sums = dx_out; f.dx = a.dx; f.dx_count = (size_t)a.n * a.d; f.dx_splits = p.dx.splits;
+        f.dx_blocks = (unsigned)((f.dx_count + 1023) / 1024);
       }
     }
     if (a.dw) {
@@ -727,28 +753,38 @@ hipError_t run32(const LceArgs& a) {
         g.workspace = (float*)(a.ws + p.wgrad); g.workspace_bytes = p.wgrad_bytes;
         ACC_TRY(conv_wgrad(g, st));
       } else {
-        Product32 g{};
-        g.a = {z, cols, pitch}; g.b = {x, a.d, a.d}; g.k = a.n;
-        g.out = p.dw.splits > 1 ? (float*)(a.ws + p.dw_sums) : to;
-        ACC_TRY((product32<true, true>(g, p.dw, st)));
+        gw.a = {z, cols, pitch}; gw.b = {x, a.d, a.d}; gw.k = a.n;
+        gw.out = p.dw.splits > 1 ? (float*)(a.ws + p.dw_sums) : to;
+        cut_into(gw, p.dw);
+        if (!p.together) ACC_TRY((launch_product32<true, true>(gw, p.dw, st)));
         if (p.dw.splits > 1) {
-          f.dw_sums = g.out; f.dw = to; f.dw_count = (size_t)cols * a.d; f.dw_splits = p.dw.splits;
+          f.dw_sums = gw.out; f.dw = to; f.dw_count = (size_t)cols * a.d; f.dw_splits = p.dw.splits;
           f.dw_blocks = (unsigned)((f.dw_count + 1023) / 1024);
         }
       }
     }
     int slabs = 1;
+    Finish32 r{};
     if (a.db) {
-      f.columns = p.rows ? z : db_part; f.rows = p.rows ? a.n : p.slabs; f.pitch = pitch; f.cols = cols; f.across = (int)ceil_div(cols, 64);
-      slabs = (int)ceil_div(f.rows, kColumnRows);
-      f.db = slabs > 1 ? db_part : a.db + v0;
-      f.db_blocks = (unsigned)(f.across * slabs);
+      r.columns = p.rows ? z : db_part; r.rows = p.rows ? a.n : p.slabs; r.pitch = pitch; r.cols = cols; r.across = (int)ceil_div(cols, 64);
+      slabs = (int)ceil_div(r.rows, kColumnRows);
+      r.db = slabs > 1 ? db_part : a.db + v0;
+      r.db_blocks = (unsigned)(r.across * slabs);
     }
-    if (p.rows) { f.loss_rows = s.loss_rows; f.labels = a.labels; f.loss = a.loss; f.n = a.n; f.ignore = a.ignore; }
-    const unsigned blocks = f.dx_blocks + f.dw_blocks + f.db_blocks + (p.rows && a.loss ? 1 : 0);
-    if (blocks) {
-      if (a.dtype == DT_F32) hipLaunchKernelGGL(finish32_kernel<float>, dim3(blocks), dim3(THREADS), 0, st, f);
-      else hipLaunchKernelGGL(finish32_kernel<bf16_t>, dim3(blocks), dim3(THREADS), 0, st, f);
+    if (p.rows) { r.loss_rows = s.loss_rows; r.labels = a.labels; r.loss = a.loss; r.n = a.n; r.ignore = a.ignore; }
+    const unsigned rest = r.db_blocks + (p.rows && a.loss ? 1 : 0), sums = f.dx_blocks + f.dw_blocks;
+    if (p.together) {
+      const unsigned bx = whole_eights(gx.work), bw = whole_eights(gw.work);
+      if (bx + bw + rest) hipLaunchKernelGGL(grads32_kernel, dim3(bx + bw + rest), dim3(THREADS), 0, st, gx, gw, r, (int)bx, (int)bw);
+    } else if (rest) {                           // with the sums
+      r.dx_sums = f.dx_sums; r.dx = f.dx; r.dx_count = f.dx_count; r.dx_splits = f.dx_splits; r.dx_blocks = f.dx_blocks;
+      r.dw_sums = f.dw_sums; r.dw = f.dw; r.dw_count = f.dw_count; r.dw_splits = f.dw_splits; r.dw_blocks = f.dw_blocks;
+      f = r;
+    }
+    if (sums + (p.together ? 0 : rest)) {
+      const dim3 grid(sums + (p.together ? 0 : rest));
+      if (a.dtype == DT_F32) hipLaunchKernelGGL(finish32_kernel<float>, grid, dim3(THREADS), 0, st, f);
+      else hipLaunchKernelGGL(finish32_kernel<bf16_t>, grid, dim3(THREADS), 0, st, f);
     }
     if (slabs > 1) hipLaunchKernelGGL(db_kernel, dim3((unsigned)ceil_div(cols, THREADS)), dim3(THREADS), 0, st, db_part, a.db, slabs, pitch, cols);
   }

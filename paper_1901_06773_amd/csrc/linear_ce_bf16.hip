@@ -318,32 +318,44 @@ __global__ __launch_bounds__(256) void lce_dz_kept_kernel(LogitArgs a, int block
   *reinterpret_cast<float4*>(to + 4) = make_float4(sum[4], sum[5], sum[6], sum[7]);
 }
 
-// dx: sums[split][n][d] (+)= dz w over the split's classes of the piece
+// dx: sums[split][n][d] (+)= dz w over the split's classes of the piece, or dx itself where there is one split of one piece
+struct DxArgs {
+  GemmOperand dz, w;
+  float* sums;
+  bf16_t* dx;                    // not null: scaled and rounded here
+  const float* scale;
+  int n, d, k, k_per_split, tiles_m, tiles, work, add;
+};
 template <class C>
-__global__ __launch_bounds__(C::THREADS, 2) void lce_dx_kernel(GemmOperand dz, GemmOperand w, float* __restrict__ sums, int n, int d, int k, int k_per_split,
-                                                               int tiles_m, int tiles, int splits, int add, int blocks) {
-  __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
-  const int work = xcd_tile(blocks);
-  if (work >= tiles * splits) return;
-  const int split = work / tiles, at = work - split * tiles;
-  const TileAt where = tile_at(at, tiles_m, tiles);
+__device__ __forceinline__ void dx_tile(const DxArgs& a, int work, char* lds) {
+  const int split = work / a.tiles, at = work - split * a.tiles, n = a.n, d = a.d;
+  const TileAt where = tile_at(at, a.tiles_m, a.tiles);
   const int m0 = where.m * C::BM, n0 = where.n * C::BN;
   GemmAcc<C> acc;
-  gemm_tile<C>(dz, w, m0, n0, split * k_per_split, min(k, (split + 1) * k_per_split), lds, acc);
+  gemm_tile<C>(a.dz, a.w, m0, n0, split * a.k_per_split, min(a.k, (split + 1) * a.k_per_split), lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm0 = (wave / C::WN) * 32 * C::MB, wn0 = (wave % C::WN) * 32 * C::NB;
-  float* const out = sums + (size_t)split * n * d;
+  float* const out = a.sums + (size_t)split * n * d;
+  const float sc = a.dx ? a.scale[0] : 1.f;
 #pragma unroll
   for (int i = 0; i < C::MB; ++i)
 #pragma unroll
     for (int j = 0; j < C::NB; ++j) {
       const int col = n0 + wn0 + 32 * j + (lane & 31), mb = m0 + wm0 + 32 * i + 4 * (lane >> 5);
       if (col >= d) continue;
+      if (a.dx) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int r = 8 * (v >> 2) + (v & 3);
+          if (mb + r < n) Elem<bf16_t>::store(a.dx + (size_t)(mb + r) * d + col, acc[i][j][v] * sc);
+        }
+        continue;
+      }
       float* const o = out + (size_t)mb * d + col;
       float old[16];                                   // asked for together (one after the other, each behind the store before it: 80 us of 337)
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         const int r = 8 * (v >> 2) + (v & 3);
-        old[v] = add && mb + r < n ? o[(size_t)r * d] : 0.f;
+        old[v] = a.add && mb + r < n ? o[(size_t)r * d] : 0.f;
       }
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
@@ -351,6 +363,12 @@ __global__ __launch_bounds__(C::THREADS, 2) void lce_dx_kernel(GemmOperand dz, G
         if (mb + r < n) o[(size_t)r * d] = old[v] + acc[i][j][v];
       }
     }
+}
+template <class C>
+__global__ __launch_bounds__(C::THREADS, 2) void lce_dx_kernel(DxArgs a, int blocks) {
+  __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
+  const int work = xcd_tile(blocks);
+  if (work < a.work) dx_tile<C>(a, work, lds);
 }
 
 // dx = scale * the splits' sums in order, rounded to bf16
@@ -407,19 +425,21 @@ __global__ __launch_bounds__(256) void lce_finish_kernel(Finish f) {
 
 // dw[class][d] = scale * sum over the rows of dz[row][class] * x[row][d], dz as the sum of its parts; with several splits of the rows their sums
 // (without the factor) lie one behind the other
+struct DwArgs {
+  GemmOperand dz, x;
+  const float* scale;
+  float* out;
+  int n, d, cols, n_per_split, tiles_m, tiles, work;
+};
 template <class C>
-__global__ __launch_bounds__(C::THREADS, 2) void lce_dw_kernel(GemmOperand dz, GemmOperand x, const float* __restrict__ scale, float* __restrict__ out, int n, int d,
-                                                               int cols, int tiles_m, int tiles, int splits, int n_per_split, int blocks) {
-  __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
-  const int work = xcd_tile(blocks);
-  if (work >= tiles * splits) return;
-  const int split = work / tiles, at = work - split * tiles;
-  const TileAt where = tile_at(at, tiles_m, tiles);
+__device__ __forceinline__ void dw_tile(const DwArgs& a, int work, char* lds) {
+  const int split = work / a.tiles, at = work - split * a.tiles, d = a.d;
+  const TileAt where = tile_at(at, a.tiles_m, a.tiles);
   const int m0 = where.m * C::BM, n0 = where.n * C::BN;
   GemmAcc<C> acc;
-  gemm_tile<C>(dz, x, m0, n0, split * n_per_split, min(n, (split + 1) * n_per_split), lds, acc);
-  const float sc = splits > 1 ? 1.f : scale[0];
-  float* const dw = out + (size_t)split * cols * d;
+  gemm_tile<C>(a.dz, a.x, m0, n0, split * a.n_per_split, min(a.n, (split + 1) * a.n_per_split), lds, acc);
+  const float sc = a.work > a.tiles ? 1.f : a.scale[0];
+  float* const dw = a.out + (size_t)split * a.cols * d;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm0 = (wave / C::WN) * 32 * C::MB, wn0 = (wave % C::WN) * 32 * C::NB;
 #pragma unroll
   for (int i = 0; i < C::MB; ++i)
@@ -430,9 +450,32 @@ __global__ __launch_bounds__(C::THREADS, 2) void lce_dw_kernel(GemmOperand dz, G
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         const int m = m0 + wm0 + 32 * i + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
-        if (m < cols) dw[(size_t)m * d + col] = acc[i][j][v] * sc;
+        if (m < a.cols) dw[(size_t)m * d + col] = acc[i][j][v] * sc;
       }
     }
+}
+template <class C>
+__global__ __launch_bounds__(C::THREADS, 2) void lce_dw_kernel(DwArgs a, int blocks) {
+  __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
+  const int work = xcd_tile(blocks);
+  if (work < a.work) dw_tile<C>(a, work, lds);
+}
+
+// dx, dw and db in one launch: they all wait for dz only, so where there are few tiles two launches less
+template <class CX, class CW>
+__global__ __launch_bounds__(256, 2) void lce_grads_kernel(DxArgs x, DwArgs w, Finish rest, int x_blocks, int w_blocks) {
+  static_assert(CX::THREADS == 256 && CW::THREADS == 256, "one shape of workgroups");
+  __shared__ __attribute__((aligned(1024))) char lds[CX::LDS > CW::LDS ? CX::LDS : CW::LDS];
+  const int block = blockIdx.x;                        // (each part begins at a multiple of eight)
+  if (block < x_blocks) {
+    const int work = (block & 7) * (x_blocks >> 3) + (block >> 3);
+    if (work < x.work) dx_tile<CX>(x, work, lds);
+  } else if (block < x_blocks + w_blocks) {
+    const int work = (block & 7) * (w_blocks >> 3) + ((block - x_blocks) >> 3);
+    if (work < w.work) dw_tile<CW>(w, work, lds);
+  } else {
+    finish_db(rest.part, rest.scale[0], rest.db, rest.parts, rest.pitch, rest.cols, block - x_blocks - w_blocks);
+  }
 }
 
 // out[r][0 .. pitch) = in[r][0 .. d), then zeros
@@ -484,10 +527,10 @@ double tile_us(int kind, int t, long tiles, double steps) {
 struct Choice {
   int tile, splits, k;           // k: values of it in one part
 };
-Choice choose(int kind, long m, long n, long k, int parts, long most_sums, long step) {
+Choice choose(int kind, long m, long n, long k, int parts, long most_sums, long step, int first = 0) {
   Choice best{256, 1, (int)up(k, 64)};
   double us = 0;
-  for (int t = 0; t < 3; ++t) {
+  for (int t = first; t < 3; ++t) {
     const long tiles = ceil_div(m, kTiles[t]) * ceil_div(n, kTiles[t]);
     // cuts in one to sixty-four, and those that fill the compute units once, twice and four times
     for (int i = 0; i < 10; ++i) {
@@ -495,9 +538,9 @@ Choice choose(int kind, long m, long n, long k, int parts, long most_sums, long 
       if (s < 1) continue;
       const long each = up(ceil_div(k, s), 64), splits = ceil_div(k, each);
       if (s > 1 && (each < step || splits * m * n > most_sums)) continue;
-      const double sums = splits > 1 ? 2.0 + (double)splits * m * n * 8 / 6e6 : 0.0;
+      const double sums = splits > 1 ? (first ? 5.0 : 2.0) + (double)splits * m * n * 8 / 6e6 : 0.0;      // (5: a launch for them alone)
       const double v = tile_us(kind, t, tiles * splits, each / 64.0 * parts) + sums;
-      if ((t == 0 && s == 1) || v < us) {
+      if (us == 0 || v < us) {
         us = v;
         best = Choice{kTiles[t], (int)splits, (int)each};
       }
@@ -513,6 +556,7 @@ struct Plan16 {
   int pitch;                     // of dz
   bool keep;                     // the last piece's logits are kept from the first sweep for the second, which begins with it
   int zt;                        // tiles of the logits
+  bool together;                 // dx, dw and db in one launch of 64 x 64 tiles
   Choice dx, dw;
   size_t stats, part, x, w, z, dz[3], dx_sums, dw_sums, db, total;
 };
@@ -540,6 +584,9 @@ Plan16 plan16(int n, int d, int classes, bool grads) {
   p.keep = grads && d >= 1024;
   p.dx = choose(RowsByRows, n, d, p.pitch, 1, 1L << 25, 256);
   p.dw = choose(ByColumns, whole, d, n, p.parts, 1L << 24, 128);
+  const Choice dx = choose(RowsByRows, n, d, p.pitch, 1, 1L << 25, 256, 2), dw = choose(ByColumns, whole, d, n, p.parts, 1L << 24, 128, 2);
+  p.together = p.pieces == 1 && ceil_div(d, 64) * (ceil_div(n, 64) * dx.splits + ceil_div(whole, 64) * dw.splits) <= 1024;
+  if (p.together) { p.dx = dx; p.dw = dw; }
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t a = at; at += al256(bytes); return a; };
   p.stats = take((size_t)(4 * (size_t)n + 64) * 4);
@@ -573,17 +620,15 @@ template <class C> void launch_dz(const LogitArgs& g, int parts, hipStream_t st)
   if (parts == 3) hipLaunchKernelGGL((lce_dz_kernel<C, 3>), grid, dim3(C::THREADS), 0, st, g, blocks);
   else hipLaunchKernelGGL((lce_dz_kernel<C, 2>), grid, dim3(C::THREADS), 0, st, g, blocks);
 }
-template <class C> void launch_dx(const GemmOperand& dz, const GemmOperand& w, float* sums, int n, int d, int k, const Plan16& p, bool add, hipStream_t st) {
-  const int tm = (int)ceil_div(n, C::BM), tiles = tm * (int)ceil_div(d, C::BN);
+template <class C> void launch_dx(const DxArgs& g, hipStream_t st) {
   int blocks;
-  const dim3 grid = grid_of<C>((long)tiles * p.dx.splits, &blocks);
-  hipLaunchKernelGGL(lce_dx_kernel<C>, grid, dim3(C::THREADS), 0, st, dz, w, sums, n, d, k, p.dx.k, tm, tiles, p.dx.splits, add ? 1 : 0, blocks);
+  const dim3 grid = grid_of<C>(g.work, &blocks);
+  hipLaunchKernelGGL(lce_dx_kernel<C>, grid, dim3(C::THREADS), 0, st, g, blocks);
 }
-template <class C> void launch_dw(const GemmOperand& dz, const GemmOperand& x, const float* scale, float* dw, int n, int d, int cols, const Plan16& p, hipStream_t st) {
-  const int tm = (int)ceil_div(cols, C::BM), tiles = tm * (int)ceil_div(d, C::BN);
+template <class C> void launch_dw(const DwArgs& g, hipStream_t st) {
   int blocks;
-  const dim3 grid = grid_of<C>((long)tiles * p.dw.splits, &blocks);
-  hipLaunchKernelGGL(lce_dw_kernel<C>, grid, dim3(C::THREADS), 0, st, dz, x, scale, dw, n, d, cols, tm, tiles, p.dw.splits, p.dw.k, blocks);
+  const dim3 grid = grid_of<C>(g.work, &blocks);
+  hipLaunchKernelGGL(lce_dw_kernel<C>, grid, dim3(C::THREADS), 0, st, g, blocks);
 }
 
 }  // namespace
@@ -652,22 +697,35 @@ hipError_t linear_ce_bf16(const LceArgs& a) {
       else launch_dz<Z64>(g, p.parts, st);
     }
     const GemmOperand dz{g.dz[0], {g.dz[1], g.dz[2]}, a.n, p.pitch, p.pitch};
+    DxArgs gx{};
+    DwArgs gw{};
+    const bool direct = p.together && p.dx.splits == 1;
     if (a.dx) {
-      if (p.dx.tile == 256) launch_dx<X256>(dz, g.w, sums, a.n, a.d, wide, p, !first, st);
-      else if (p.dx.tile == 128) launch_dx<X128>(dz, g.w, sums, a.n, a.d, wide, p, !first, st);
-      else launch_dx<X64>(dz, g.w, sums, a.n, a.d, wide, p, !first, st);
+      gx.dz = dz; gx.w = g.w; gx.sums = sums; gx.dx = direct ? (bf16_t*)a.dx : nullptr; gx.scale = s.scale;
+      gx.n = a.n; gx.d = a.d; gx.k = wide; gx.k_per_split = p.dx.k; gx.add = first ? 0 : 1;
+      gx.tiles_m = (int)ceil_div(a.n, p.dx.tile); gx.tiles = gx.tiles_m * (int)ceil_div(a.d, p.dx.tile); gx.work = gx.tiles * p.dx.splits;
     }
     float* const dw = a.dw ? a.dw + (size_t)g.v0 * a.d : nullptr;
     float* const dw_sums = (float*)(a.ws + p.dw_sums);
     if (a.dw) {
-#define ACC_DW(C) launch_dw<C>(dz, g.x, s.scale, p.dw.splits > 1 ? dw_sums : dw, a.n, a.d, g.cols, p, st)
+      gw.dz = dz; gw.x = g.x; gw.scale = s.scale; gw.out = p.dw.splits > 1 ? dw_sums : dw;
+      gw.n = a.n; gw.d = a.d; gw.cols = g.cols; gw.n_per_split = p.dw.k;
+      gw.tiles_m = (int)ceil_div(g.cols, p.dw.tile); gw.tiles = gw.tiles_m * (int)ceil_div(a.d, p.dw.tile); gw.work = gw.tiles * p.dw.splits;
+    }
+    if (!p.together && a.dx) {
+      if (p.dx.tile == 256) launch_dx<X256>(gx, st);
+      else if (p.dx.tile == 128) launch_dx<X128>(gx, st);
+      else launch_dx<X64>(gx, st);
+    }
+    if (!p.together && a.dw) {
+#define ACC_DW(C) launch_dw<C>(gw, st)
       if (p.parts == 3) { if (p.dw.tile == 256) ACC_DW(V256); else if (p.dw.tile == 128) ACC_DW(V128); else ACC_DW(V64); }
       else { if (p.dw.tile == 256) ACC_DW(W256); else if (p.dw.tile == 128) ACC_DW(W128); else ACC_DW(W64); }
 #undef ACC_DW
     }
     Finish f{};
     f.scale = s.scale;
-    if (a.dx && last) {
+    if (a.dx && last && !direct) {
       f.sums = sums; f.dx = (bf16_t*)a.dx; f.count = (size_t)a.n * a.d; f.splits = p.dx.splits;
       f.dx_blocks = (int)((f.count + 1023) / 1024);
     }
@@ -676,7 +734,13 @@ hipError_t linear_ce_bf16(const LceArgs& a) {
       f.dw_blocks = (int)((f.dw_count + 1023) / 1024);
     }
     if (a.db) { f.part = g.db_part; f.db = a.db + g.v0; f.parts = db_parts; f.pitch = p.pitch; f.cols = g.cols; }
-    const int blocks = f.dx_blocks + f.dw_blocks + (a.db ? (g.cols + 255) / 256 : 0);
+    const int db_blocks = a.db ? (g.cols + 255) / 256 : 0;
+    if (p.together) {
+      const int bx = (gx.work + 7) / 8 * 8, bw = (gw.work + 7) / 8 * 8;
+      if (p.parts == 3) hipLaunchKernelGGL((lce_grads_kernel<X64, V64>), dim3((unsigned)(bx + bw + db_blocks)), dim3(256), 0, st, gx, gw, f, bx, bw);
+      else hipLaunchKernelGGL((lce_grads_kernel<X64, W64>), dim3((unsigned)(bx + bw + db_blocks)), dim3(256), 0, st, gx, gw, f, bx, bw);
+    }
+    const int blocks = f.dx_blocks + f.dw_blocks + (p.together ? 0 : db_blocks);
     if (blocks) hipLaunchKernelGGL(lce_finish_kernel, dim3((unsigned)blocks), dim3(256), 0, st, f);
   }
   return hipGetLastError();
