@@ -80,63 +80,15 @@ __global__ __launch_bounds__(THREADS) void row_sums_kernel(float* __restrict__ z
   }
 }
 
-// The splits' m and R of a row joined, by `lanes` (a power of two) neighbouring lanes.
-__device__ __forceinline__ float join_row(const float* __restrict__ part, const float* __restrict__ z_label, const int32_t* __restrict__ labels, int ignore,
-                                          float* __restrict__ row_max, float* __restrict__ row_rest, int row, int splits, int classes, int lanes) {
-  const int lane = threadIdx.x & (lanes - 1);
-  const float* p = part + (size_t)row * 2 * splits;
-  const int lab = labels[row];
-  const float at_label = z_label[row];
-  float mx = -INFINITY;
-  for (int i = lane; i < splits; i += lanes) mx = fmaxf(mx, p[i]);
-  for (int o = lanes >> 1; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-  float s = 0.f, equal = 0.f;
-  for (int i = lane; i < splits; i += lanes) {
-    const bool top = p[i] == mx;
-    equal += top ? 1.f : 0.f;
-    s += top ? p[splits + i] : (1.f + p[splits + i]) * expf(p[i] - mx);
-  }
-  for (int o = lanes >> 1; o > 0; o >>= 1) { s += __shfl_xor(s, o); equal += __shfl_xor(equal, o); }
-  const float rest = mx == -INFINITY ? NAN : s + (equal - 1.f);     // (every class ruled out: no distribution)
-  const bool skip = ignore != INT_MIN && lab == ignore, known = (unsigned)lab < (unsigned)classes;
-  if (lane == 0) {
-    row_max[row] = mx;
-    row_rest[row] = rest;
-  }
-  return skip ? 0.f : known ? log1pf(rest) - (at_label - mx) : NAN;
-}
 __global__ __launch_bounds__(THREADS) void join_kernel(const float* __restrict__ part, const float* __restrict__ z_label, const int32_t* __restrict__ labels,
                                                        int ignore, float* __restrict__ row_max, float* __restrict__ row_rest, float* __restrict__ loss_rows,
                                                        int n, int splits, int classes, int lanes) {
   const int row = (blockIdx.x * THREADS + threadIdx.x) / lanes;
   if (row >= n) return;
-  const float l = join_row(part, z_label, labels, ignore, row_max, row_rest, row, splits, classes, lanes);
-  if ((threadIdx.x & (lanes - 1)) == 0) loss_rows[row] = l;
+  const RowStats r = join_row(part, z_label, labels, ignore, row, splits, classes, lanes);
+  if ((threadIdx.x & (lanes - 1)) == 0) { row_max[row] = r.max; row_rest[row] = r.rest; loss_rows[row] = r.loss; }
 }
 
-// scale[0] = 1 / rows that count (0 if there is none), loss = their mean, of NT threads and in a fixed order.  Either may be null.
-template <int NT>
-__device__ __forceinline__ void mean_of_rows(const float* loss_rows, const int32_t* __restrict__ labels, int ignore, int n, float* __restrict__ scale,
-                                             float* __restrict__ loss) {
-  __shared__ double sh[NT / 64];
-  __shared__ int counts[NT / 64];
-  double s = 0.0;
-  int k = 0;
-  for (int i = threadIdx.x; i < n; i += NT) {
-    s += (double)loss_rows[i];
-    k += ignore == INT_MIN || labels[i] != ignore ? 1 : 0;
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) { s += __shfl_xor(s, o); k += __shfl_xor(k, o); }
-  if ((threadIdx.x & 63) == 0) { sh[threadIdx.x >> 6] = s; counts[threadIdx.x >> 6] = k; }
-  __syncthreads();
-  if (threadIdx.x) return;
-  double t = 0.0;
-  int rows = 0;
-  for (int w = 0; w < NT / 64; ++w) { t += sh[w]; rows += counts[w]; }
-  if (scale) scale[0] = rows ? 1.f / (float)rows : 0.f;
-  if (loss) *loss = rows ? (float)(t / (double)rows) : 0.f;
-}
 __global__ __launch_bounds__(1024) void mean_kernel(const float* __restrict__ loss_rows, const int32_t* __restrict__ labels, int ignore, int n,
                                                     float* __restrict__ scale, float* __restrict__ loss) {
   mean_of_rows<1024>(loss_rows, labels, ignore, n, scale, loss);
@@ -146,8 +98,8 @@ __global__ __launch_bounds__(1024) void join_mean_kernel(const float* __restrict
                                                          int ignore, float* __restrict__ row_max, float* __restrict__ row_rest, float* loss_rows, int n,
                                                          int splits, int classes, float* __restrict__ scale, float* __restrict__ loss, int lanes) {
   for (int row = threadIdx.x / lanes; row < n; row += 1024 / lanes) {
-    const float l = join_row(part, z_label, labels, ignore, row_max, row_rest, row, splits, classes, lanes);
-    if ((threadIdx.x & (lanes - 1)) == 0) loss_rows[row] = l;
+    const RowStats r = join_row(part, z_label, labels, ignore, row, splits, classes, lanes);
+    if ((threadIdx.x & (lanes - 1)) == 0) { row_max[row] = r.max; row_rest[row] = r.rest; loss_rows[row] = r.loss; }
   }
   __threadfence_block();
   __syncthreads();

@@ -72,6 +72,9 @@ struct LogitArgs {
   bf16_t* dz[3];
   int pitch, ignore;
   float* db_part;                    // null: not wanted
+  // dz that joins the rows' sums itself
+  int join, classes;
+  float *loss_rows, *scale;
 };
 
 template <class C>
@@ -185,12 +188,29 @@ template <class C, int PARTS>
 __global__ __launch_bounds__(C::THREADS, 2) void lce_dz_kernel(LogitArgs a, int blocks) {
   constexpr int EP = C::NB * 64 + 16, OUT = C::WM * C::WN * 32 * EP * PARTS;      // per wave 32 staged rows of every part
   __shared__ __attribute__((aligned(1024))) char lds[C::LDS > OUT ? C::LDS : OUT];
+  constexpr bool JOINS = C::BM == 64;                  // (the larger tiles' registers are full)
+  __shared__ float row_max[JOINS ? C::BM : 1], row_rest[JOINS ? C::BM : 1];
+  if (JOINS && (int)blockIdx.x >= blocks) {                     // (with `join`)
+    mean_of_rows<C::THREADS>(nullptr, a.labels, a.ignore, a.n, a.scale, nullptr);
+    return;
+  }
   const int at = xcd_tile(blocks);
   if (at >= a.tiles) return;
   const TileAt where = tile_at(at, a.tiles_m, a.tiles);
   const int tile_m = where.m, tile_n = where.n, m0 = tile_m * C::BM, n0 = tile_n * C::BN;
+  constexpr int LANES = C::THREADS / C::BM;            // of a row
+  if (const int r = threadIdx.x / LANES, m = m0 + r; JOINS && m < a.n) {
+    RowStats st{0.f, 0.f, 0.f};
+    if (a.join) st = join_row(a.part, a.z_label, a.labels, a.ignore, m, a.splits, a.classes, LANES);
+    else { st.max = a.row_max[m]; st.rest = a.row_rest[m]; }
+    if (threadIdx.x % LANES == 0) {
+      row_max[r] = st.max; row_rest[r] = st.rest;
+      if (a.join && tile_n == 0) a.loss_rows[m] = st.loss;
+    }
+  }
   GemmAcc<C> acc;
   gemm_tile<C>(a.x, a.w, m0, n0, 0, a.d, lds, acc);
+  if (JOINS) __syncthreads();                          // the rows' sums are there
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm0 = (wave / C::WN) * 32 * C::MB, wn0 = (wave % C::WN) * 32 * C::NB;
   if (a.bias) add_bias<C>(acc, a.bias, n0 + wn0, a.cols);
   const bool edge = n0 + C::BN > a.cols;
@@ -205,7 +225,7 @@ __global__ __launch_bounds__(C::THREADS, 2) void lce_dz_kernel(LogitArgs a, int 
     const int m = m0 + wm0 + 32 * i + (lane & 31);
     const bool row_ok = m < a.n;
     const int label = row_ok ? a.labels[m] : -1;
-    const float mx = row_ok ? a.row_max[m] : 0.f, rest = row_ok ? a.row_rest[m] : 0.f, inv = 1.f / (1.f + rest);
+    const float mx = !row_ok ? 0.f : JOINS ? row_max[m - m0] : a.row_max[m], rest = !row_ok ? 0.f : JOINS ? row_rest[m - m0] : a.row_rest[m], inv = 1.f / (1.f + rest);
     const bool skip = !row_ok || (a.ignore != INT_MIN && label == a.ignore);
     const int lab = label - a.v0 - (n0 + wn0) - 4 * (lane >> 5);
     const bool mine = row_ok && (unsigned)label >= (unsigned)a.v0 && lab >= 0 && lab < 32 * C::NB && !(lab & 4);
@@ -335,14 +355,15 @@ __device__ __forceinline__ void dx_tile(const DxArgs& a, int work, char* lds) {
   gemm_tile<C>(a.dz, a.w, m0, n0, split * a.k_per_split, min(a.k, (split + 1) * a.k_per_split), lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm0 = (wave / C::WN) * 32 * C::MB, wn0 = (wave % C::WN) * 32 * C::NB;
   float* const out = a.sums + (size_t)split * n * d;
-  const float sc = a.dx ? a.scale[0] : 1.f;
+  const bool direct = C::BM == 64 && a.dx;             // (of launches with few tiles only)
+  const float sc = direct ? a.scale[0] : 1.f;
 #pragma unroll
   for (int i = 0; i < C::MB; ++i)
 #pragma unroll
     for (int j = 0; j < C::NB; ++j) {
       const int col = n0 + wn0 + 32 * j + (lane & 31), mb = m0 + wm0 + 32 * i + 4 * (lane >> 5);
       if (col >= d) continue;
-      if (a.dx) {
+      if (direct) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
           const int r = 8 * (v >> 2) + (v & 3);
@@ -429,17 +450,18 @@ struct DwArgs {
   GemmOperand dz, x;
   const float* scale;
   float* out;
-  int n, d, cols, n_per_split, tiles_m, tiles, work;
+  int n, d, cols, n_per_split, tiles_m, tiles, splits;
 };
 template <class C>
-__device__ __forceinline__ void dw_tile(const DwArgs& a, int work, char* lds) {
-  const int split = work / a.tiles, at = work - split * a.tiles, d = a.d;
-  const TileAt where = tile_at(at, a.tiles_m, a.tiles);
+__device__ __forceinline__ void dw_tile(const GemmOperand& dz, const GemmOperand& x, const float* __restrict__ scale, float* __restrict__ out, int n, int d, int cols,
+                                        int n_per_split, int tiles_m, int tiles, int splits, int work, char* lds) {
+  const int split = work / tiles, at = work - split * tiles;
+  const TileAt where = tile_at(at, tiles_m, tiles);
   const int m0 = where.m * C::BM, n0 = where.n * C::BN;
   GemmAcc<C> acc;
-  gemm_tile<C>(a.dz, a.x, m0, n0, split * a.n_per_split, min(a.n, (split + 1) * a.n_per_split), lds, acc);
-  const float sc = a.work > a.tiles ? 1.f : a.scale[0];
-  float* const dw = a.out + (size_t)split * a.cols * d;
+  gemm_tile<C>(dz, x, m0, n0, split * n_per_split, min(n, (split + 1) * n_per_split), lds, acc);
+  const float sc = splits > 1 ? 1.f : scale[0];
+  float* const dw = out + (size_t)split * cols * d;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm0 = (wave / C::WN) * 32 * C::MB, wn0 = (wave % C::WN) * 32 * C::NB;
 #pragma unroll
   for (int i = 0; i < C::MB; ++i)
@@ -450,20 +472,28 @@ __device__ __forceinline__ void dw_tile(const DwArgs& a, int work, char* lds) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         const int m = m0 + wm0 + 32 * i + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
-        if (m < a.cols) dw[(size_t)m * d + col] = acc[i][j][v] * sc;
+        if (m < cols) dw[(size_t)m * d + col] = acc[i][j][v] * sc;
       }
     }
 }
 template <class C>
-__global__ __launch_bounds__(C::THREADS, 2) void lce_dw_kernel(DwArgs a, int blocks) {
+__global__ __launch_bounds__(C::THREADS, 2) void lce_dw_kernel(GemmOperand dz, GemmOperand x, const float* __restrict__ scale, float* __restrict__ out, int n, int d,
+                                                               int cols, int n_per_split, int tiles_m, int tiles, int splits, int blocks) {
   __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
   const int work = xcd_tile(blocks);
-  if (work < a.work) dw_tile<C>(a, work, lds);
+  if (work >= tiles * splits) return;
+  dw_tile<C>(dz, x, scale, out, n, d, cols, n_per_split, tiles_m, tiles, splits, work, lds);
 }
 
-// dx, dw and db in one launch: they all wait for dz only, so where there are few tiles two launches less
+struct MeanArgs {
+  const float* loss_rows;
+  const int32_t* labels;
+  float* loss;
+  int n, ignore;
+};
+// dx, dw, db (and the mean loss) in one launch: they all wait for dz only, so where there are few tiles two launches less
 template <class CX, class CW>
-__global__ __launch_bounds__(256, 2) void lce_grads_kernel(DxArgs x, DwArgs w, Finish rest, int x_blocks, int w_blocks) {
+__global__ __launch_bounds__(256, 2) void lce_grads_kernel(DxArgs x, DwArgs w, Finish rest, MeanArgs mean, int x_blocks, int w_blocks, int db_blocks) {
   static_assert(CX::THREADS == 256 && CW::THREADS == 256, "one shape of workgroups");
   __shared__ __attribute__((aligned(1024))) char lds[CX::LDS > CW::LDS ? CX::LDS : CW::LDS];
   const int block = blockIdx.x;                        // (each part begins at a multiple of eight)
@@ -472,9 +502,11 @@ __global__ __launch_bounds__(256, 2) void lce_grads_kernel(DxArgs x, DwArgs w, F
     if (work < x.work) dx_tile<CX>(x, work, lds);
   } else if (block < x_blocks + w_blocks) {
     const int work = (block & 7) * (w_blocks >> 3) + ((block - x_blocks) >> 3);
-    if (work < w.work) dw_tile<CW>(w, work, lds);
-  } else {
+    if (work < w.tiles * w.splits) dw_tile<CW>(w.dz, w.x, w.scale, w.out, w.n, w.d, w.cols, w.n_per_split, w.tiles_m, w.tiles, w.splits, work, lds);
+  } else if (block < x_blocks + w_blocks + db_blocks) {
     finish_db(rest.part, rest.scale[0], rest.db, rest.parts, rest.pitch, rest.cols, block - x_blocks - w_blocks);
+  } else {
+    mean_of_rows<256>(mean.loss_rows, mean.labels, mean.ignore, mean.n, nullptr, mean.loss);
   }
 }
 
@@ -557,6 +589,7 @@ struct Plan16 {
   bool keep;                     // the last piece's logits are kept from the first sweep for the second, which begins with it
   int zt;                        // tiles of the logits
   bool together;                 // dx, dw and db in one launch of 64 x 64 tiles
+  bool join;                     // the rows' sums are joined by the workgroups of dz, not by a launch of their own
   Choice dx, dw;
   size_t stats, part, x, w, z, dz[3], dx_sums, dw_sums, db, total;
 };
@@ -587,6 +620,8 @@ Plan16 plan16(int n, int d, int classes, bool grads) {
   const Choice dx = choose(RowsByRows, n, d, p.pitch, 1, 1L << 25, 256, 2), dw = choose(ByColumns, whole, d, n, p.parts, 1L << 24, 128, 2);
   p.together = p.pieces == 1 && ceil_div(d, 64) * (ceil_div(n, 64) * dx.splits + ceil_div(whole, 64) * dw.splits) <= 1024;
   if (p.together) { p.dx = dx; p.dw = dw; }
+  // (a row's sums are then read by every tile across)
+  p.join = grads && p.together && !p.keep && p.zt == 64 && p.splits <= 16;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t a = at; at += al256(bytes); return a; };
   p.stats = take((size_t)(4 * (size_t)n + 64) * 4);
@@ -616,7 +651,8 @@ template <class C> void launch_sums(const LogitArgs& g, hipStream_t st) {
 }
 template <class C> void launch_dz(const LogitArgs& g, int parts, hipStream_t st) {
   int blocks;
-  const dim3 grid = grid_of<C>(g.tiles, &blocks);
+  dim3 grid = grid_of<C>(g.tiles, &blocks);
+  if (g.join) ++grid.x;
   if (parts == 3) hipLaunchKernelGGL((lce_dz_kernel<C, 3>), grid, dim3(C::THREADS), 0, st, g, blocks);
   else hipLaunchKernelGGL((lce_dz_kernel<C, 2>), grid, dim3(C::THREADS), 0, st, g, blocks);
 }
@@ -627,8 +663,8 @@ template <class C> void launch_dx(const DxArgs& g, hipStream_t st) {
 }
 template <class C> void launch_dw(const DwArgs& g, hipStream_t st) {
   int blocks;
-  const dim3 grid = grid_of<C>(g.work, &blocks);
-  hipLaunchKernelGGL(lce_dw_kernel<C>, grid, dim3(C::THREADS), 0, st, g, blocks);
+  const dim3 grid = grid_of<C>((long)g.tiles * g.splits, &blocks);
+  hipLaunchKernelGGL(lce_dw_kernel<C>, grid, dim3(C::THREADS), 0, st, g.dz, g.x, g.scale, g.out, g.n, g.d, g.cols, g.n_per_split, g.tiles_m, g.tiles, g.splits, blocks);
 }
 
 }  // namespace
@@ -661,6 +697,7 @@ hipError_t linear_ce_bf16(const LceArgs& a) {
   g.pitch = p.pitch; g.ignore = a.ignore;
   g.db_part = a.db ? (float*)(a.ws + p.db) : nullptr;
   g.tiles_m = (int)ceil_div(a.n, p.zt);
+  g.join = p.join; g.classes = a.classes; g.loss_rows = s.loss_rows; g.scale = s.scale;
   auto piece = [&](long k) {
     g.v0 = (int)(k * p.piece);
     g.cols = (int)(a.classes - g.v0 < p.piece ? a.classes - g.v0 : p.piece);
@@ -678,7 +715,9 @@ hipError_t linear_ce_bf16(const LceArgs& a) {
     else if (p.zt == 128) launch_sums<Z128>(g, st);
     else launch_sums<Z64>(g, st);
   }
-  if (const hipError_t e = lce_join(a, s, g.part, (int)p.splits); e != hipSuccess || !grads) return e;
+  if (!p.join) {
+    if (const hipError_t e = lce_join(a, s, g.part, (int)p.splits); e != hipSuccess || !grads) return e;
+  }
   float* const sums = (float*)(a.ws + p.dx_sums);
   for (long k = p.pieces - 1; k >= 0; --k) {           // (the last piece is still there)
     const bool first = k + 1 == p.pieces, last = k == 0;
@@ -710,7 +749,7 @@ hipError_t linear_ce_bf16(const LceArgs& a) {
     if (a.dw) {
       gw.dz = dz; gw.x = g.x; gw.scale = s.scale; gw.out = p.dw.splits > 1 ? dw_sums : dw;
       gw.n = a.n; gw.d = a.d; gw.cols = g.cols; gw.n_per_split = p.dw.k;
-      gw.tiles_m = (int)ceil_div(g.cols, p.dw.tile); gw.tiles = gw.tiles_m * (int)ceil_div(a.d, p.dw.tile); gw.work = gw.tiles * p.dw.splits;
+      gw.tiles_m = (int)ceil_div(g.cols, p.dw.tile); gw.tiles = gw.tiles_m * (int)ceil_div(a.d, p.dw.tile); gw.splits = p.dw.splits;
     }
     if (!p.together && a.dx) {
       if (p.dx.tile == 256) launch_dx<X256>(gx, st);
@@ -736,9 +775,11 @@ hipError_t linear_ce_bf16(const LceArgs& a) {
     if (a.db) { f.part = g.db_part; f.db = a.db + g.v0; f.parts = db_parts; f.pitch = p.pitch; f.cols = g.cols; }
     const int db_blocks = a.db ? (g.cols + 255) / 256 : 0;
     if (p.together) {
-      const int bx = (gx.work + 7) / 8 * 8, bw = (gw.work + 7) / 8 * 8;
-      if (p.parts == 3) hipLaunchKernelGGL((lce_grads_kernel<X64, V64>), dim3((unsigned)(bx + bw + db_blocks)), dim3(256), 0, st, gx, gw, f, bx, bw);
-      else hipLaunchKernelGGL((lce_grads_kernel<X64, W64>), dim3((unsigned)(bx + bw + db_blocks)), dim3(256), 0, st, gx, gw, f, bx, bw);
+      const int bx = (gx.work + 7) / 8 * 8, bw = (gw.tiles * gw.splits + 7) / 8 * 8;
+      const MeanArgs mean{s.loss_rows, a.labels, a.loss, a.n, a.ignore};
+      const dim3 grid((unsigned)(bx + bw + db_blocks + (p.join && a.loss ? 1 : 0)));
+      if (p.parts == 3) hipLaunchKernelGGL((lce_grads_kernel<X64, V64>), grid, dim3(256), 0, st, gx, gw, f, mean, bx, bw, db_blocks);
+      else hipLaunchKernelGGL((lce_grads_kernel<X64, W64>), grid, dim3(256), 0, st, gx, gw, f, mean, bx, bw, db_blocks);
     }
     const int blocks = f.dx_blocks + f.dw_blocks + (p.together ? 0 : db_blocks);
     if (blocks) hipLaunchKernelGGL(lce_finish_kernel, dim3((unsigned)blocks), dim3(256), 0, st, f);
