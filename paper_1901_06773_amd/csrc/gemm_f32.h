@@ -1,28 +1,35 @@
-// One tile of a plain matrix product on the fp32 matrix cores, for kernels that do something of their own with it:
+// One tile of a plain matrix product of fp32 operands, for kernels that do something of their own with it:
 //
 //   acc[m][n] = sum_k A[m][k] * B[k][n],   m in [m0, m0 + BM), n in [n0, n0 + BN), k in [k_lo, k_hi)
 //
 // Each operand lies in memory with its values of k side by side (rows of m resp. n) or with its values of m resp. n side by side (rows of k), at any
 // width: 16 bytes at a time from addresses that need be aligned to 4 only, so odd widths cost no copy.  Loads that would pass the end of a row begin
 // earlier and are shifted; rows that don't exist repeat the last one, whose results nobody stores, and values of k beyond k_hi are zero in both operands.
-// A chunk of 32 values of k waits in registers while the one before it is multiplied out of LDS.  The matrix instructions bound it (256 operations per
-// cycle and compute unit: a 128 x 128 x 32 chunk takes 4096 cycles, its LDS traffic a tenth of that), so one stage of LDS is enough and leaves room for
-// several workgroups on a compute unit.  1024 x 2048 x 32768: 1134 us, 121 TFLOP/s of 157.
+// A chunk of 32 values of k waits in registers while the one before it is multiplied out of LDS; one stage of LDS leaves room for two workgroups and more
+// on a compute unit, which cover each other's barriers.
+//
+// Small tiles multiply on the fp32 matrix cores (256 operations per cycle and compute unit; LDS traffic a tenth of that).  Large ones (SPLIT) write each
+// value to LDS as the sum of three bf16 values, which hold its 24 bits, and add the six products that matter on the bf16 matrix cores: a chunk of 128 x 128
+// takes them 1536 cycles in place of 4096, beside some 800 of splitting.  1024 x 2048 x 32768, us, all in fp32 / split: 1134 / 686 (200 TFLOP/s).
 #pragma once
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
 
+#include "dtype.h"
+
 namespace acc {
 
-// WM x WN waves, each MB x NB blocks of 16 x 16.  AT / BT: the operand lies in rows of k.
-template <int WM_, int WN_, int MB_, int NB_, bool AT_, bool BT_> struct Gemm32Cfg {
+// WM x WN waves, each MB x NB blocks of 16 x 16.  AT / BT: the operand lies in rows of k.  SPLIT: products on the bf16 matrix cores.
+template <int WM_, int WN_, int MB_, int NB_, bool AT_, bool BT_, bool SPLIT_> struct Gemm32Cfg {
   static constexpr int WM = WM_, WN = WN_, MB = MB_, NB = NB_, BK = 32;
-  static constexpr bool AT = AT_, BT = BT_;
+  static constexpr bool AT = AT_, BT = BT_, SPLIT = SPLIT_;
   static constexpr int THREADS = 64 * WM * WN, BM = 16 * MB * WM, BN = 16 * NB * WN;
+  static constexpr int SPLIT_PITCH = 20;               // a row's 32 bf16 values, and 16 bytes that set the next row off
   // floats between staged rows: the sixteen rows (resp. four groups of sixteen columns) that a read takes at once fall on different banks
   static constexpr int A_PITCH = AT ? BM + 4 : BK + 4, B_PITCH = BT ? BN + 4 : BK + 4;
-  static constexpr int A_FLOATS = (AT ? BK : BM) * A_PITCH, B_FLOATS = (BT ? BK : BN) * B_PITCH, LDS = A_FLOATS + B_FLOATS;
+  static constexpr int A_FLOATS = SPLIT ? 3 * BM * SPLIT_PITCH : (AT ? BK : BM) * A_PITCH, B_FLOATS = SPLIT ? 3 * BN * SPLIT_PITCH : (BT ? BK : BN) * B_PITCH;
+  static constexpr int LDS = A_FLOATS + B_FLOATS;      // floats
   static constexpr int AI = BM * BK / 4 / THREADS, BI = BN * BK / 4 / THREADS;     // loads of a thread per chunk
   static_assert(AI * THREADS * 4 == BM * BK && BI * THREADS * 4 == BN * BK, "whole loads");
 };
@@ -104,6 +111,70 @@ template <int EXTENT, bool T, int LOADS, int PITCH, int THREADS> struct Gemm32Lo
   }
 };
 
+// v = h + m + l, each a bf16 value (8 significant bits), of four values that lie side by side
+struct Split4 {
+  uint2 h, m, l;
+};
+__device__ __forceinline__ Split4 split4(f32x4 v) {
+  auto rest = [](f32x4 a, uint2 p) {
+    return f32x4{a.x - __uint_as_float(p.x << 16), a.y - __uint_as_float(p.x & 0xffff0000u), a.z - __uint_as_float(p.y << 16),
+                 a.w - __uint_as_float(p.y & 0xffff0000u)};
+  };
+  auto pack = [](f32x4 a) { return make_uint2(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w)); };
+  // (the upper half as it is: rounded, the largest values would become infinite)
+  auto upper = [](float a, float b) { return (__float_as_uint(a) >> 16) | (__float_as_uint(b) & 0xffff0000u); };
+  Split4 s;
+  s.h = make_uint2(upper(v.x, v.y), upper(v.z, v.w));
+  v = rest(v, s.h);
+  s.m = pack(v);
+  s.l = pack(rest(v, s.m));
+  return s;
+}
+
+// The same for products on the bf16 matrix cores: three planes of EXTENT rows of 32 values of k.  Rows of k: a thread takes four of them in four columns
+// 32 apart, so that its values of k lie side by side in LDS and those of neighbouring threads in neighbouring rows.
+template <int EXTENT, bool T, int LOADS, int PITCH, int THREADS> struct Gemm32SplitLoader : Gemm32Loader<EXTENT, T, LOADS, PITCH, THREADS> {
+  typedef Gemm32Loader<EXTENT, T, LOADS, PITCH, THREADS> Base;
+  static_assert(!T || (EXTENT == 128 && THREADS == 256 && LOADS == 4), "eight groups of four values of k");
+  using Base::q;
+  __device__ __forceinline__ void load(const Gemm32Operand& o, int left) {
+    if constexpr (T) {
+      const int k = (threadIdx.x >> 5) * 4, c = threadIdx.x & 31;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool there = k + e < left;
+        const float* row = this->base + (size_t)min(k + e, left - 1) * o.pitch;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float v = row[min(c + 32 * i, this->end - 1)];
+          q[i][e] = there ? v : 0.f;
+        }
+      }
+      this->base += (size_t)32 * o.pitch;
+    } else {
+      Base::load(o, left);
+    }
+  }
+  __device__ __forceinline__ void stage(float* lds) const {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int u = threadIdx.x + i * THREADS;
+      const int at = T ? ((threadIdx.x & 31) + 32 * i) * PITCH + (threadIdx.x >> 5) * 2 : (u / 8) * PITCH + (u % 8) * 2;
+      const Split4 s = split4(q[i]);
+      *reinterpret_cast<uint2*>(lds + at) = s.h;
+      *reinterpret_cast<uint2*>(lds + EXTENT * PITCH + at) = s.m;
+      *reinterpret_cast<uint2*>(lds + 2 * EXTENT * PITCH + at) = s.l;
+    }
+  }
+};
+
+template <bool SPLIT, int EXTENT, bool T, int LOADS, int PITCH, int SPLIT_PITCH, int THREADS> struct Gemm32LoaderOf {
+  typedef Gemm32Loader<EXTENT, T, LOADS, PITCH, THREADS> type;
+};
+template <int EXTENT, bool T, int LOADS, int PITCH, int SPLIT_PITCH, int THREADS> struct Gemm32LoaderOf<true, EXTENT, T, LOADS, PITCH, SPLIT_PITCH, THREADS> {
+  typedef Gemm32SplitLoader<EXTENT, T, LOADS, SPLIT_PITCH, THREADS> type;
+};
+
 // The accumulators are those of the transposed block: a lane holds columns 4 * (lane / 16) .. + 3 of row lane % 16.
 template <class C>
 __device__ __forceinline__ void gemm32_tile(const Gemm32Operand& A, const Gemm32Operand& B, int m0, int n0, int k_lo, int k_hi, float* lds,
@@ -117,8 +188,8 @@ __device__ __forceinline__ void gemm32_tile(const Gemm32Operand& A, const Gemm32
   for (int i = 0; i < C::MB; ++i)
 #pragma unroll
     for (int j = 0; j < C::NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  Gemm32Loader<C::BM, C::AT, C::AI, C::A_PITCH, C::THREADS> a;
-  Gemm32Loader<C::BN, C::BT, C::BI, C::B_PITCH, C::THREADS> b;
+  typename Gemm32LoaderOf<C::SPLIT, C::BM, C::AT, C::AI, C::A_PITCH, C::SPLIT_PITCH, C::THREADS>::type a;
+  typename Gemm32LoaderOf<C::SPLIT, C::BN, C::BT, C::BI, C::B_PITCH, C::SPLIT_PITCH, C::THREADS>::type b;
   a.start(A, m0, k_lo);
   b.start(B, n0, k_lo);
   if (k_lo < k_hi) {
@@ -133,6 +204,28 @@ __device__ __forceinline__ void gemm32_tile(const Gemm32Operand& A, const Gemm32
     if (k + C::BK < k_hi) {
       a.load(A, k_hi - k - C::BK);
       b.load(B, k_hi - k - C::BK);
+    }
+    if constexpr (C::SPLIT) {
+      // lane group g holds values of k 8 g .. 8 g + 7; the six largest products, the smallest of them first
+      typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+      bf16x8 fb[3][C::NB];
+#pragma unroll
+      for (int p = 0; p < 3; ++p)
+#pragma unroll
+        for (int j = 0; j < C::NB; ++j)
+          fb[p][j] = *reinterpret_cast<const bf16x8*>(lb + (p * C::BN + wn0 + 16 * j + row) * C::SPLIT_PITCH + 4 * group);
+#pragma unroll
+      for (int i = 0; i < C::MB; ++i) {
+        bf16x8 fa[3];
+#pragma unroll
+        for (int p = 0; p < 3; ++p) fa[p] = *reinterpret_cast<const bf16x8*>(la + (p * C::BM + wm0 + 16 * i + row) * C::SPLIT_PITCH + 4 * group);
+        constexpr int PA[6] = {2, 0, 1, 1, 0, 0}, PB[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+        for (int u = 0; u < 6; ++u)
+#pragma unroll
+          for (int j = 0; j < C::NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[PB[u]][j], fa[PA[u]], acc[i][j], 0, 0, 0);
+      }
+      continue;
     }
     // lane group g multiplies values of k 4 g + e of each sixteen in step e
 #pragma unroll

@@ -8,8 +8,8 @@
 // both operands.  With one piece the logits of the first sweep are still there.  2 n d classes operations for the loss, 6 more (4 with
 // one piece) for the gradients, which is what bounds it.
 //
-// fp32: logits and dz of a piece in fp32, products of the convolution kernels (a 1x1 convolution of n pixels) where those are faster, else of the kernels
-// here (gemm_f32.h), whose epilogue takes the rows' sums along.  Few classes (8192 in one piece): a launch turns whole rows of logits into dz.
+// fp32: logits and dz of a piece in fp32, products by gemm_f32.h, whose epilogue takes the rows' sums along.  Few classes (8192 in one piece): a launch turns
+// whole rows of logits into dz.  Few tiles: dx, dw, db and the mean loss in one launch.
 #include "kernels.h"
 #include "dtype.h"
 #include "gemm_f32.h"
@@ -225,8 +225,7 @@ __global__ __launch_bounds__(THREADS) void dz_kernel(float* __restrict__ z, cons
   if (db_part) *reinterpret_cast<float4*>(db_part + (size_t)blockIdx.y * pitch + j) = make_float4(sum[0], sum[1], sum[2], sum[3]);
 }
 
-// ---------------------------------------------------------------------------------- products of this file
-// The shapes that the convolution kernels do not take or are slow for (widths that are not whole, few tiles with a long sum).
+// ---------------------------------------------------------------------------------- products
 struct Logits32 {
   Gemm32Operand x, w;
   const float* bias;             // null: none, or added later
@@ -421,8 +420,8 @@ template <class T>
 __global__ __launch_bounds__(THREADS) void finish32_kernel(Finish32 f) { finish32<T>(f, blockIdx.x); }
 
 // dx, dw, db and the mean loss in one launch, 64 x 64 tiles.  They all wait for dz only: where there are few tiles, three launches less.
-typedef Gemm32Cfg<2, 2, 2, 2, false, true> Dx64;
-typedef Gemm32Cfg<2, 2, 2, 2, true, true> Dw64;
+typedef Gemm32Cfg<2, 2, 2, 2, false, true, false> Dx64;
+typedef Gemm32Cfg<2, 2, 2, 2, true, true, false> Dw64;
 __global__ __launch_bounds__(THREADS) void grads32_kernel(Product32 dx, Product32 dw, Finish32 rest, int dx_blocks, int dw_blocks) {
   __shared__ __attribute__((aligned(16))) float lds[Dx64::LDS > Dw64::LDS ? Dx64::LDS : Dw64::LDS];
   const int block = blockIdx.x;                        // (each part begins at a multiple of eight)
@@ -459,13 +458,13 @@ inline long ceil_div(long a, long b) { return (a + b - 1) / b; }
 
 // Tiles and, for a product whose sum over k may be cut, parts of 128 values of k or more.  Predicted time, us: the chunks of a tile one after the other,
 // or all chunks of the busiest compute unit at the rate that its workgroups reach together; the sums of the parts cost writing and reading.  Constants from
-// every tile on ten shapes (16 to 3835 rows); measured, 32 x 128 / 64 x 64 / 128 x 128: logits 16 x 816 x 16719 27 / 39 / 68, 393 x 72 x 1523
-// 8.1 / 8.0 / 14, 1024 x 1024 x 8192 180 / 171 / 149; dx 666 x 57 x 55313 177 / 85 / 123, 3835 x 328 x 859 60 / 50 / 38; dw 42 x 4064 x 10407 80 / 68 / 76.
+// every tile on ten shapes (16 to 3835 rows); measured, 32 x 128 / 64 x 64 / 128 x 128 (split): logits 16 x 816 x 16719 27 / 39 / 60, 1024 x 1024 x 8192
+// 180 / 171 / 104; dx 666 x 57 x 55313 177 / 85 / 82, 2520 x 304 x 14775 588 / 287 / 166; dw 344 x 816 x 63060 434 / 389 / 251.
 struct Cut {
   int tile, splits, k;           // tile: 0 32 x 128, 1 64 x 64, 2 128 x 128; k: values of it in one part
 };
 constexpr int kTile32[3][2] = {{32, 128}, {64, 64}, {128, 128}};
-constexpr double kChunk32[3][2] = {{0.93, 0.68}, {0.88, 0.66}, {3.0, 2.1}};
+constexpr double kChunk32[3][2] = {{0.93, 0.68}, {0.88, 0.66}, {2.1, 1.4}};
 Cut cut32(long m, long n, long k, long most_sums, int only = -1) {
   Cut best{1, 1, (int)up(k, 32)};
   double us = 0;
@@ -487,53 +486,59 @@ Cut cut32(long m, long n, long k, long most_sums, int only = -1) {
   return best;
 }
 
+// out[n][n_out] = in[n][c] * w[n_out][c]^T, as a convolution
+ConvGeom product_geom(const float* in, const float* w, float* out, int n, int c, int n_out) {
+  ConvGeom g{};
+  g.in = in; g.w = w; g.out = out; g.dtype = DT_F32;
+  g.n_img = n; g.h = g.wd = g.p = g.q = g.out_h = g.out_w = 1;
+  g.c = c; g.n_out = n_out; g.r = g.s = g.stride = g.out_stride = 1;
+  return g;
+}
+
 struct Plan32 {
   long piece, pieces, splits;    // classes of a piece, pieces, columns of `part`
   int pitch;                     // of z
   bool rows;                     // one piece of at most kRowCols classes: a workgroup per row
-  bool conv_z, conv_dx, conv_dw; // products of the convolution kernels
+  bool conv;                     // dx and dw by the convolution kernels
   bool late;                     // the logits' sums and bias in a launch of their own: row_sums_kernel
   bool widen;                    // bf16 operands are copied
   bool together;                 // dx, dw, db and the mean in one launch
   int dz_rows, slabs;            // rows of a workgroup of dz_kernel, and workgroups
   Cut z, dx, dw;
   bool sum_dx;                   // dx from `dx_sums`
-  size_t stats, part, logits, x, w, wt, dx_sums, dw_sums, db, wgrad, total;   // offsets of the parts of the workspace, and its size
+  size_t stats, part, logits, x, w, dx_sums, dw_sums, db, wgrad, total;   // offsets of the parts of the workspace, and its size
   size_t wgrad_bytes;
 };
 
 Plan32 plan32(int n, int d, int classes, bool grads, int dtype) {
   Plan32 p{};
-  // 256 MiB of logits, 1 GiB of filter, and what the transposing launch takes
+  // 256 MiB of logits, and of the filter 1 GiB in fp32 where it is copied
   long most = (1L << 26) / n / 128 * 128;
-  if (most > (1L << 28) / d / 128 * 128) most = (1L << 28) / d / 128 * 128;
-  if (most > 1L << 20) most = 1L << 20;
+  if (dtype != DT_F32 && most > (1L << 28) / d / 128 * 128) most = (1L << 28) / d / 128 * 128;
   if (most < 128) most = 128;
   p.piece = classes <= most ? classes : most;
   p.pieces = ceil_div(classes, p.piece);
   p.pitch = (int)up(p.piece, 4);
   p.rows = p.pieces == 1 && p.piece <= kRowCols && n <= 16384;
   p.widen = dtype != DT_F32;
-  // The convolution kernels take whole widths, and multiply at 200 to 260 TFLOP/s (three bf16 values per fp32 one) where there are enough tiles; the kernels
-  // here at up to 140, any width, with the sum over k cut where there are few tiles.  Measured, us, here / convolution: logits 1024 x 2048 x 32768
-  // 1134 / 804, 256 x 2048 x 32768 292 / 218, 1024 x 1024 x 1000 33 / 28, 256 x 512 x 10000 42 / 40, but 300 x 2048 x 1000 26 / 35, 1024 x 64 x 50000
-  // 114 / 173, 32 x 1024 x 32768 39 / 54; dx 4096 x 1024 x 8192 519 / 350, 1024 x 1024 x 8192 137 / 136, 256 x 2048 x 32768 268 / 412,
-  // 256 x 64 x 50000 50 / 132, and of few rows and classes (all results) 41 x 2048 x 1000 33 / 30, 16 x 2048 x 4096 58 / 52, 64 x 256 x 256 19 / 26; dw 4096 x 1024 x 8192 546 / 346,
-  // 1024 x 256 x 8192 47 / 40, 256 x 2048 x 32768 288 / 303, 4096 x 128 x 1000 14 / 17.
-  const double units = (double)n * d * p.piece;
-  // (and the convolution's fast loads reach 4 GiB)
-  const bool whole = !p.widen && (long)n * d * 4 <= 0xFFFFFF00L && (long)p.piece * d * 4 <= 0xFFFFFF00L && d % 4 == 0 && d >= 16 && classes >= 16 && classes % 4 == 0 && classes % p.piece % 16 == 0;
-  p.conv_z = whole && d >= 128 && n >= 64 && units >= 1e9;
-  p.conv_dx = whole && ((units >= 2e9 && (long)n * d >= 1L << 21) || (n <= 64 && classes >= 640 && classes <= 4096 && d >= 256));
-  p.conv_dw = whole && d >= 256 && (n >= 512 || (n <= 64 && classes >= 640));
+  // Few rows and classes of whole widths: the convolution kernels' launches, which deal the sum out among the waves of a workgroup, are faster than cutting it
+  // and a launch for the parts' sums (us, all results, here / convolution: 41 x 2048 x 1000 33 / 30, 16 x 2048 x 4096 58 / 52, 64 x 256 x 256 19 / 26).
+  // Elsewhere the kernels here are (1024 x 2048 x 32768: logits 726 / 825, dx 740 / 1023, dw 775 / 841).
+  p.conv = !p.widen && p.pieces == 1 && n <= 64 && classes >= 640 && classes <= 4096 && classes % 4 == 0 && d >= 256 && d % 8 == 0;
+  if (p.conv) {
+    static const float any[4] = {};
+    ConvGeom g = product_geom(any, nullptr, nullptr, n, classes, d);
+    g.w_kn = any;
+    p.conv = conv_igemm_rows_takes(g, n, classes);
+  }
   p.z = cut32(n, p.piece, d, p.rows || (p.pieces == 1 && n * p.piece <= 1L << 22) ? 1L << 24 : 0);
   p.dx = cut32(n, d, p.piece, 1L << 25);
   p.dw = cut32(p.piece, d, n, 1L << 24);
   const Cut dx = cut32(n, d, p.piece, 1L << 25, 1), dw = cut32(p.piece, d, n, 1L << 24, 1);
   auto works = [](long m, long k, const Cut& c) { return ceil_div(m, 64) * ceil_div(k, 64) * c.splits; };
-  p.together = !p.conv_dx && !p.conv_dw && works(n, d, dx) + works(p.piece, d, dw) <= 1024;
+  p.together = !p.conv && works(n, d, dx) + works(p.piece, d, dw) <= 1024;
   if (p.together) { p.dx = dx; p.dw = dw; }
-  p.late = !p.rows && (p.conv_z || p.z.splits > 1);
+  p.late = !p.rows && p.z.splits > 1;
   const long split_cols = p.late ? kSplitCols : kTile32[p.z.tile][1];
   p.splits = (p.pieces - 1) * ceil_div(p.piece, split_cols) + ceil_div(classes - (p.pieces - 1) * p.piece, split_cols);
   // rows of a workgroup of dz_kernel: some two thousand workgroups, at most 512 of them down a column
@@ -541,25 +546,19 @@ Plan32 plan32(int n, int d, int classes, bool grads, int dtype) {
   p.dz_rows = (int)up(ceil_div((long)n * across, 2048), 4);
   if (p.dz_rows < ceil_div(n, 512)) p.dz_rows = (int)up(ceil_div(n, 512), 4);
   p.slabs = (int)ceil_div(n, p.dz_rows);
-  p.sum_dx = p.widen || (!p.conv_dx && p.dx.splits > 1);
+  p.sum_dx = p.widen || (!p.conv && p.dx.splits > 1);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t a = at; at += al256(bytes); return a; };
   p.stats = take((size_t)(4 * (size_t)n + 64) * 4);
   p.part = take(p.rows ? 0 : (size_t)n * 2 * p.splits * 4);
-  p.logits = take(p.rows || p.late || grads ? (size_t)n * p.pitch * 4 * (p.conv_z ? 1 : p.z.splits) : 0);
+  p.logits = take(p.rows || p.late || grads ? (size_t)n * p.pitch * 4 * p.z.splits : 0);
   p.x = take(p.widen ? (size_t)n * d * 4 : 0);
   p.w = take(p.widen ? (size_t)p.piece * d * 4 : 0);
   if (grads) {
-    p.wt = take(p.conv_dx ? (size_t)p.pitch * d * 4 : 0);
     p.dx_sums = take(p.sum_dx ? (size_t)p.dx.splits * n * d * 4 : 0);
-    p.dw_sums = take(!p.conv_dw && p.dw.splits > 1 ? (size_t)p.dw.splits * p.piece * d * 4 : 0);
+    p.dw_sums = take(!p.conv && p.dw.splits > 1 ? (size_t)p.dw.splits * p.piece * d * 4 : 0);
     p.db = take((size_t)(p.rows ? ceil_div(n, kColumnRows) : p.slabs) * p.pitch * 4);
-    if (p.conv_dw) {
-      const int last = (int)(classes - (p.pieces - 1) * p.piece);
-      p.wgrad_bytes = wgrad_workspace_bytes(n, 1, 1, d, (int)p.piece, 1, 1, DT_F32);
-      const size_t tail = wgrad_workspace_bytes(n, 1, 1, d, last, 1, 1, DT_F32);
-      if (tail > p.wgrad_bytes) p.wgrad_bytes = tail;
-    }
+    if (p.conv) p.wgrad_bytes = wgrad_workspace_bytes(n, 1, 1, d, classes, 1, 1, DT_F32);
     p.wgrad = take(p.wgrad_bytes);
   }
   p.total = at;
@@ -567,15 +566,6 @@ Plan32 plan32(int n, int d, int classes, bool grads, int dtype) {
 }
 
 #define ACC_TRY(call) do { if (const hipError_t e_ = (call); e_ != hipSuccess) return e_; } while (0)
-
-// out[n][n_out] (+)= in[n][c] * w[n_out][c]^T
-ConvGeom product_geom(const float* in, const float* w, float* out, int n, int c, int n_out, bool accumulate) {
-  ConvGeom g{};
-  g.in = in; g.w = w; g.out = out; g.dtype = DT_F32;
-  g.n_img = n; g.h = g.wd = g.p = g.q = g.out_h = g.out_w = 1;
-  g.c = c; g.n_out = n_out; g.r = g.s = g.stride = g.out_stride = 1; g.accumulate = accumulate ? 1 : 0;
-  return g;
-}
 
 hipError_t widen(const void* in, float* out, size_t total, hipStream_t st) {
   const size_t b = (total + THREADS - 1) / THREADS;
@@ -593,9 +583,9 @@ void cut_into(Product32& g, const Cut& c) {
 }
 template <bool AT, bool BT> hipError_t launch_product32(const Product32& g, const Cut& c, hipStream_t st) {
   const unsigned blocks = whole_eights(g.work);
-  if (c.tile == 0) hipLaunchKernelGGL((product32_kernel<Gemm32Cfg<1, 4, 2, 2, AT, BT>>), dim3(blocks), dim3(256), 0, st, g, (int)blocks);
-  else if (c.tile == 1) hipLaunchKernelGGL((product32_kernel<Gemm32Cfg<2, 2, 2, 2, AT, BT>>), dim3(blocks), dim3(256), 0, st, g, (int)blocks);
-  else hipLaunchKernelGGL((product32_kernel<Gemm32Cfg<2, 2, 4, 4, AT, BT>>), dim3(blocks), dim3(256), 0, st, g, (int)blocks);
+  if (c.tile == 0) hipLaunchKernelGGL((product32_kernel<Gemm32Cfg<1, 4, 2, 2, AT, BT, false>>), dim3(blocks), dim3(256), 0, st, g, (int)blocks);
+  else if (c.tile == 1) hipLaunchKernelGGL((product32_kernel<Gemm32Cfg<2, 2, 2, 2, AT, BT, false>>), dim3(blocks), dim3(256), 0, st, g, (int)blocks);
+  else hipLaunchKernelGGL((product32_kernel<Gemm32Cfg<2, 2, 4, 4, AT, BT, true>>), dim3(blocks), dim3(256), 0, st, g, (int)blocks);
   return hipGetLastError();
 }
 
@@ -605,9 +595,9 @@ hipError_t logits32(Logits32 g, const Cut& c, int n, int tiles_n, hipStream_t st
   g.k_per_split = c.k;
   g.work = g.tiles * c.splits;
   const unsigned blocks = whole_eights(g.work);
-  if (c.tile == 0) hipLaunchKernelGGL((logits32_kernel<Gemm32Cfg<1, 4, 2, 2, false, false>>), dim3(blocks), dim3(256), 0, st, g, (int)blocks);
-  else if (c.tile == 1) hipLaunchKernelGGL((logits32_kernel<Gemm32Cfg<2, 2, 2, 2, false, false>>), dim3(blocks), dim3(256), 0, st, g, (int)blocks);
-  else hipLaunchKernelGGL((logits32_kernel<Gemm32Cfg<2, 2, 4, 4, false, false>>), dim3(blocks), dim3(256), 0, st, g, (int)blocks);
+  if (c.tile == 0) hipLaunchKernelGGL((logits32_kernel<Gemm32Cfg<1, 4, 2, 2, false, false, false>>), dim3(blocks), dim3(256), 0, st, g, (int)blocks);
+  else if (c.tile == 1) hipLaunchKernelGGL((logits32_kernel<Gemm32Cfg<2, 2, 2, 2, false, false, false>>), dim3(blocks), dim3(256), 0, st, g, (int)blocks);
+  else hipLaunchKernelGGL((logits32_kernel<Gemm32Cfg<2, 2, 4, 4, false, false, true>>), dim3(blocks), dim3(256), 0, st, g, (int)blocks);
   return hipGetLastError();
 }
 
@@ -636,28 +626,23 @@ hipError_t run32(const LceArgs& a) {
       w = (const float*)(a.ws + p.w);
       ACC_TRY(widen(from, (float*)(a.ws + p.w), (size_t)cols * a.d, st));
     }
-    const int pitch = p.conv_z ? cols : p.pitch, tile_n = kTile32[p.z.tile][1];      // (the convolution's pixels lie close together)
-    if (p.conv_z) {
-      ACC_TRY(conv_igemm(product_geom(x, w, z, a.n, a.d, cols, false), st));
-    } else {
-      Logits32 g{};
-      g.x = {x, a.n, a.d}; g.w = {w, cols, a.d};
-      g.bias = a.bias && !p.rows && !p.late ? a.bias + v0 : nullptr;
-      g.labels = a.labels; g.z = keep || p.late ? z : nullptr; g.part = sums && !p.late ? part : nullptr; g.z_label = s.z_label;
-      g.d = a.d; g.pitch = pitch; g.v0 = (int)v0; g.split0 = (int)(k * ceil_div(p.piece, tile_n)); g.splits = (int)p.splits;
-      ACC_TRY(logits32(g, p.z, a.n, (int)ceil_div(cols, tile_n), st));
-    }
+    const int pitch = p.pitch, tile_n = kTile32[p.z.tile][1];
+    Logits32 g{};
+    g.x = {x, a.n, a.d}; g.w = {w, cols, a.d};
+    g.bias = a.bias && !p.rows && !p.late ? a.bias + v0 : nullptr;
+    g.labels = a.labels; g.z = keep || p.late ? z : nullptr; g.part = sums && !p.late ? part : nullptr; g.z_label = s.z_label;
+    g.d = a.d; g.pitch = pitch; g.v0 = (int)v0; g.split0 = (int)(k * ceil_div(p.piece, tile_n)); g.splits = (int)p.splits;
+    ACC_TRY(logits32(g, p.z, a.n, (int)ceil_div(cols, tile_n), st));
     if (!sums || !p.late) return hipSuccess;
     const int here = (int)ceil_div(cols, kSplitCols);
     hipLaunchKernelGGL(row_sums_kernel, dim3((unsigned)(a.n * here)), dim3(THREADS), 0, st, z, a.bias, a.labels, part, s.z_label, pitch, cols, (int)v0, kSplitCols,
-                       here, (int)(k * ceil_div(p.piece, kSplitCols)), (int)p.splits, p.conv_z ? 1 : p.z.splits, (size_t)a.n * pitch);
+                       here, (int)(k * ceil_div(p.piece, kSplitCols)), (int)p.splits, p.z.splits, (size_t)a.n * pitch);
     return hipGetLastError();
   };
   if (p.rows) {
     ACC_TRY(logits(0, false, true));
-    const int splits = p.conv_z ? 1 : p.z.splits;
 #define ACC_ROWS(V, NT) hipLaunchKernelGGL((rows_kernel<V, NT>), dim3((unsigned)a.n), dim3(NT), 0, st, z, a.bias, a.labels, a.ignore, s.loss_rows, a.n, p.pitch, \
-                                           cols, grads ? 1 : 0, splits)
+                                           cols, grads ? 1 : 0, p.z.splits)
     if (p.pitch <= 4 * 256) ACC_ROWS(4, 256);
     else if (p.pitch <= 16 * 256) ACC_ROWS(16, 256);
     else ACC_ROWS(8, 1024);
@@ -672,20 +657,15 @@ hipError_t run32(const LceArgs& a) {
   for (long k = p.pieces - 1; k >= 0; --k) {           // (the last piece is still there)
     const bool first = k + 1 == p.pieces, last = k == 0;
     if (!first) ACC_TRY(logits(k, false, true));
-    const int pitch = p.conv_z ? cols : p.pitch;       // (the convolution's pixels lie close together)
+    const int pitch = p.pitch;
     if (!p.rows)
       hipLaunchKernelGGL(dz_kernel, dim3((unsigned)ceil_div(pitch / 4, THREADS), (unsigned)p.slabs), dim3(THREADS), 0, st, z, p.late ? a.bias : nullptr, a.labels,
                          a.ignore, s.row_max, s.row_rest, s.scale, a.db ? db_part : nullptr, a.n, pitch, cols, (int)v0, p.dz_rows);
     Finish32 f{};
     Product32 gx{}, gw{};
-    if (a.dx && p.conv_dx) {
-      ConvGeom g = product_geom(z, nullptr, (float*)a.dx, a.n, cols, a.d, !first);
-      g.w_kn = w;                              // few rows: the filter as it lies
-      if (!conv_igemm_rows_takes(g, a.n, cols)) {
-        float* const wt = (float*)(a.ws + p.wt);
-        ACC_TRY(filter_flip_transpose(w, wt, cols, a.d, 1, 1, DT_F32, st));
-        g = product_geom(z, wt, (float*)a.dx, a.n, cols, a.d, !first);
-      }
+    if (a.dx && p.conv) {
+      ConvGeom g = product_geom(z, nullptr, (float*)a.dx, a.n, cols, a.d);
+      g.w_kn = w;                              // the filter as it lies
       ACC_TRY(conv_igemm(g, st));
     } else if (a.dx) {
       gx.a = {z, a.n, pitch}; gx.b = {w, a.d, a.d}; gx.out = dx_out; gx.k = cols; gx.add = !first;
@@ -698,7 +678,7 @@ hipError_t run32(const LceArgs& a) {
     }
     if (a.dw) {
       float* const to = a.dw + (size_t)v0 * a.d;
-      if (p.conv_dw) {
+      if (p.conv) {
         WgradGeom g{};
         g.x = x; g.dy = z; g.dw = to; g.dtype = DT_F32;
         g.n_img = a.n; g.h = g.wd = g.p = g.q = 1; g.cin = a.d; g.cout = cols; g.r = g.s = g.stride = 1;
