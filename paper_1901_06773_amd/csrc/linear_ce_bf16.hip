@@ -510,11 +510,24 @@ __global__ __launch_bounds__(256, 2) void lce_grads_kernel(DxArgs x, DwArgs w, F
   }
 }
 
-// out[r][0 .. pitch) = in[r][0 .. d), then zeros
-__global__ __launch_bounds__(256) void lce_pad_kernel(const bf16_t* __restrict__ in, bf16_t* __restrict__ out, size_t total, int d, int pitch) {
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (size_t)gridDim.x * 256) {
-    const size_t r = i / pitch, c = i - r * pitch;
-    out[i] = c < (size_t)d ? in[r * d + c] : (bf16_t)0;
+// out[r][0 .. pitch) = in[r][0 .. d), then zeros; eight values per thread, read at any address (11261 rows of 3015: 62 us one by one, 28 so)
+__global__ __launch_bounds__(256) void lce_pad_kernel(const bf16_t* __restrict__ in, bf16_t* __restrict__ out, size_t eights, int d, int pitch) {
+  typedef uint32_t any __attribute__((ext_vector_type(4), aligned(2)));
+  const size_t across = pitch / 8;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < eights; i += (size_t)gridDim.x * 256) {
+    const size_t r = i / across;
+    const int c = (int)(i - r * across) * 8;
+    const bf16_t* from = in + r * d + c;
+    v4u v;
+    if (c + 8 <= d) {
+      const any q = *reinterpret_cast<const any*>(from);
+      v = v4u{q.x, q.y, q.z, q.w};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        v[e] = (c + 2 * e < d ? (uint32_t)from[2 * e] : 0u) | (c + 2 * e + 1 < d ? (uint32_t)from[2 * e + 1] << 16 : 0u);
+    }
+    *reinterpret_cast<v4u*>(out + i * 8) = v;
   }
 }
 
@@ -681,9 +694,9 @@ hipError_t linear_ce_bf16(const LceArgs& a) {
   hipStream_t st = a.st;
   const bf16_t* x = (const bf16_t*)a.x;
   auto pad = [&](const void* in, size_t at, long rows) {
-    const size_t total = (size_t)rows * p.dp;
-    const unsigned blocks = (unsigned)(total / 256 + 1 < 4096 ? total / 256 + 1 : 4096);
-    hipLaunchKernelGGL(lce_pad_kernel, dim3(blocks), dim3(256), 0, st, (const bf16_t*)in, (bf16_t*)(a.ws + at), total, a.d, p.dp);
+    const size_t eights = (size_t)rows * p.dp / 8;
+    const unsigned blocks = (unsigned)(eights / 256 + 1 < 4096 ? eights / 256 + 1 : 4096);
+    hipLaunchKernelGGL(lce_pad_kernel, dim3(blocks), dim3(256), 0, st, (const bf16_t*)in, (bf16_t*)(a.ws + at), eights, a.d, p.dp);
     return (const bf16_t*)(a.ws + at);
   };
   if (p.dp != a.d) x = pad(a.x, p.x, a.n);
