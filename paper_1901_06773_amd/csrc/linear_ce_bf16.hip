@@ -77,6 +77,8 @@ struct LogitArgs {
   float *loss_rows, *scale;
 };
 
+// Logits of a tile, of which the largest one of a row and the sum of exponentials leave it.  4096 x 2048 x 16384: 250 us, 1097 TFLOP/s (a large library product
+// reaches 1378); matrix cores busy 60 % of the time.
 template <class C>
 __global__ __launch_bounds__(C::THREADS, 2) void lce_sums_kernel(LogitArgs a, int blocks) {
   constexpr int RED = C::WN * C::BM * 3 * 4;
@@ -184,6 +186,7 @@ __device__ __forceinline__ float half_sum(float v) {
   return v;
 }
 
+// The logits again, which leave as dz, and the columns' sums of a tile.  4096 x 2048 x 16384, two parts: 291 us, 945 TFLOP/s beside writing 268 MB.
 template <class C, int PARTS>
 __global__ __launch_bounds__(C::THREADS, 2) void lce_dz_kernel(LogitArgs a, int blocks) {
   constexpr int EP = C::NB * 64 + 16, OUT = C::WM * C::WN * 32 * EP * PARTS;      // per wave 32 staged rows of every part
@@ -285,7 +288,8 @@ __global__ __launch_bounds__(C::THREADS, 2) void lce_dz_kernel(LogitArgs a, int 
     }
 }
 
-// dz from kept logits: eight columns per thread, a workgroup's rows one after the other (DZ_ROWS of them), and their columns' sums
+// dz from kept logits: eight columns per thread, a workgroup's rows one after the other (DZ_ROWS of them), and their columns' sums.  4096 x 16384, two parts:
+// 109 us for 537 MB, 4.9 TB/s.
 constexpr int DZ_ROWS = 16;
 template <int PARTS>
 __global__ __launch_bounds__(256) void lce_dz_kept_kernel(LogitArgs a, int blocks_across) {
@@ -338,7 +342,8 @@ __global__ __launch_bounds__(256) void lce_dz_kept_kernel(LogitArgs a, int block
   *reinterpret_cast<float4*>(to + 4) = make_float4(sum[4], sum[5], sum[6], sum[7]);
 }
 
-// dx: sums[split][n][d] (+)= dz w over the split's classes of the piece, or dx itself where there is one split of one piece
+// dx: sums[split][n][d] (+)= dz w over the split's classes of the piece, or dx itself where there is one split of one piece.  4096 x 2048 x 16384: 243 us,
+// 1131 TFLOP/s.
 struct DxArgs {
   GemmOperand dz, w;
   float* sums;
@@ -445,7 +450,7 @@ __global__ __launch_bounds__(256) void lce_finish_kernel(Finish f) {
 }
 
 // dw[class][d] = scale * sum over the rows of dz[row][class] * x[row][d], dz as the sum of its parts; with several splits of the rows their sums
-// (without the factor) lie one behind the other
+// (without the factor) lie one behind the other.  4096 x 2048 x 16384, two parts: 418 us, 1315 TFLOP/s of the matrix cores (75 % busy).
 struct DwArgs {
   GemmOperand dz, x;
   const float* scale;
@@ -491,7 +496,8 @@ struct MeanArgs {
   float* loss;
   int n, ignore;
 };
-// dx, dw, db (and the mean loss) in one launch: they all wait for dz only, so where there are few tiles two launches less
+// dx, dw, db (and the mean loss) in one launch: they all wait for dz only, so where there are few tiles two launches less (us, all results, before / with it:
+// 64 x 64 x 64 22.3 / 18.9, 1000 x 1024 x 1000 59.6 / 49.6; and with the rows' sums joined by dz, 64 x 64 x 64 14.9)
 template <class CX, class CW>
 __global__ __launch_bounds__(256, 2) void lce_grads_kernel(DxArgs x, DwArgs w, Finish rest, MeanArgs mean, int x_blocks, int w_blocks, int db_blocks) {
   static_assert(CX::THREADS == 256 && CW::THREADS == 256, "one shape of workgroups");
