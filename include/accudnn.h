@@ -283,6 +283,13 @@ int acc_get_timeline(acc_ctx* ctx, int which, acc_timeline_entry* out, int max_e
  * until the step is done; *loss_out is the mean cross-entropy at the pre-update weights. */
 int acc_train_step(acc_ctx* ctx, const float* images, int images_loc, const int32_t* labels,
                    float lr, float* loss_out);
+/* Gradient clipping inside the iteration: the update takes g * (N <= max_norm ? 1 : max_norm / N) with N the Euclidean norm over all
+ * gradients of the network, as acc_op_grad_clip() scales them (the quotient and the product rounded to fp32); the stored gradients
+ * (acc_get_grads) stay as they are.  max_norm = 0, the default: no clipping and no norm; INFINITY: the norm only.  No memory beyond the
+ * plan's: the partial sums use the part of the pool that an iteration's maps have left.  A norm that is NaN makes all weights NaN.
+ * acc_get_grad_norm: N of the last iteration (ACC_ESTATE if it had no max_norm). */
+int acc_set_grad_clip(acc_ctx* ctx, float max_norm);
+int acc_get_grad_norm(acc_ctx* ctx, float* norm);
 /* What the last iteration did (Sec. 6.2.2 and 6.2.3 verify the memory and the transfer model
  * on such figures: bytes in the pool, bytes over the link, copy durations). */
 int acc_get_stats(acc_ctx* ctx, acc_stats* out);

@@ -143,6 +143,8 @@ _PROTOS = {
     "acc_get_stats": (_I, [_VP, C.POINTER(acc_stats)]),
     "acc_set_profiling": (_I, [_VP, _I]),
     "acc_set_debug": (_I, [_VP, _I]),
+    "acc_set_grad_clip": (_I, [_VP, _F]),
+    "acc_get_grad_norm": (_I, [_VP, C.POINTER(_F)]),
     "acc_set_graph": (_I, [_VP, _I]),
     "acc_capture_output": (_I, [_VP, _I, _VP, _SZ]),
     "acc_inject_output": (_I, [_VP, _I, _VP, _SZ]),
@@ -386,6 +388,19 @@ class Context:
     def set_wgrad_overlap(self, on: bool):
         """Weight gradients on their own stream beside the data gradients (default), or on the compute stream."""
         self._check(_lib.acc_set_wgrad_overlap(self._h, 1 if on else 0))
+
+    def set_grad_clip(self, max_norm: float):
+        """Updates with gradients scaled so that their norm is max_norm at most (0: as they are; inf: the norm is measured only)."""
+        rc = _lib.acc_set_grad_clip(self._h, float(max_norm))
+        if rc == ACC_EINVAL:
+            raise AccError(rc, _lib.acc_last_error(None).decode())
+        self._check(rc)
+
+    def grad_norm(self) -> float:
+        """Norm of the last train_step's gradient, before scaling."""
+        n = _F(0.0)
+        self._check(_lib.acc_get_grad_norm(self._h, C.byref(n)))
+        return float(n.value)
 
     def set_debug(self, poison: bool):
         """Verification mode: NaN-poison everything the plan has released or not yet brought back,

@@ -67,6 +67,9 @@ struct acc_ctx {
   bool profiling = false;
   bool kernel_profiling = false;
   bool calibrating = false;     // input batch is synthesised on the device
+  ClippedUpdate clipped = nullptr;   // acc_set_grad_clip(): the update that scales the gradient; null: plain SGD
+  float max_norm = 0.f, last_norm = 0.f;
+  bool have_norm = false;
   struct KProbe { int variant; double flops; hipEvent_t a, b; int step, role; double ms; };
   std::vector<KProbe> kprobes;  // one per convolution kernel launch of the last profiled step
   size_t kprobes_used = 0;
@@ -77,7 +80,7 @@ struct acc_ctx {
   std::vector<double> step_ms;
   std::vector<size_t> cur_off;  // per tensor, while executing
   acc_stats stats{};
-  float* h_loss = nullptr;      // pinned: [0] loss, then (as 64-bit words 1..2) what the poison scan found
+  float* h_loss = nullptr;      // pinned: [0] loss, (as 64-bit words 2..3) what the poison scan found, [kNormWord] the norm
   // The compute part of an iteration that swaps nothing, captured once per plan into a HIP graph
   // and replayed (acc_set_graph): everything between the input copies and the update kernel.
   bool use_graph = false;
@@ -701,6 +704,16 @@ hipError_t fill_words(void* p, size_t bytes, uint32_t v, hipStream_t st) {
   return hipGetLastError();
 }
 
+constexpr int kNormWord = 16;        // of the block that begins with the loss: the gradient's norm
+
+// Nothing in the dynamic part of the pool is needed any more at this point: the norm's partial sums go there.
+hipError_t update_weights(acc_ctx* c, float lr, hipStream_t st) {
+  if (!c->clipped || c->calibrating) return sgd_update(c->d_params, c->d_grads, lr, c->g.param_elems, c->d_params16, st);
+  const size_t room = c->plan.dyn_top < c->dyn_cap ? c->plan.dyn_top : c->dyn_cap;
+  return c->clipped(c->d_params, c->d_grads, lr, c->max_norm, c->g.param_elems, c->d_params16, c->d_loss + kNormWord, c->dyn, room, st);
+}
+
+
 // launches the kernels of one step on the compute stream
 // Adds up the parts of the last conv weight gradient on the stream it ran on; the compute
 // stream then waits for that stream (the update reads the result).
@@ -949,7 +962,7 @@ hipError_t run_step(acc_ctx* c, int j, float lr) {
     case K_SGD:
       if (hipError_t e = flush_pending_reduce(c); e != hipSuccess) return e;
       if (c->capturing) return hipSuccess;   // the learning rate is an argument: the update is launched after the graph
-      return sgd_update(c->d_params, c->d_grads, lr, g.param_elems, c->d_params16, st);
+      return update_weights(c, lr, st);
   }
   return hipErrorInvalidValue;
 }
@@ -1199,10 +1212,11 @@ extern "C" int acc_train_step(acc_ctx* c, const float* images, int images_loc, c
       }
       HIPCHK(c, hipGraphLaunch(c->graph_exec, c->s_c));
     }
-    const hipError_t eu = sgd_update(c->d_params, c->d_grads, lr, g.param_elems, c->d_params16, c->s_c);
+    const hipError_t eu = update_weights(c, lr, c->s_c);
     if (eu != hipSuccess) return c->hipfail(eu, "sgd_update");
   }
-  HIPCHK(c, hipMemcpyAsync(c->h_loss, c->d_loss, sizeof(float), hipMemcpyDeviceToHost, c->s_c));
+  const bool clipped = c->clipped && !c->calibrating;
+  HIPCHK(c, hipMemcpyAsync(c->h_loss, c->d_loss, clipped ? (kNormWord + 1) * sizeof(float) : sizeof(float), hipMemcpyDeviceToHost, c->s_c));
   HIPCHK(c, hipEventRecord(c->ev_end, c->s_c));
   const double t_issued = now_ms();
   HIPCHK(c, hipStreamSynchronize(c->s_c));
@@ -1213,6 +1227,8 @@ extern "C" int acc_train_step(acc_ctx* c, const float* images, int images_loc, c
   if (c->s_w) HIPCHK(c, hipStreamSynchronize(c->s_w));
   const double t_done = now_ms();
   if (loss_out) *loss_out = *c->h_loss;
+  if (clipped) c->last_norm = c->h_loss[kNormWord];
+  c->have_norm = clipped;
   c->stats.step_ms = t_done - t_host0;
   c->stats.host_issue_ms = t_issued - t_host0;
   c->stats.host_wait_ms = t_waited;
@@ -1313,6 +1329,20 @@ extern "C" int acc_get_timeline(acc_ctx* c, int which, acc_timeline_entry* out, 
 extern "C" int acc_get_stats(acc_ctx* c, acc_stats* out) {
   if (!c || !out) return ACC_EINVAL;
   *out = c->stats;
+  return ACC_OK;
+}
+
+int acc::set_clipped_update(acc_ctx* c, ClippedUpdate update, float max_norm) {
+  if (!c->have_res) return c->fail(ACC_ESTATE, "context has no device resources");
+  c->clipped = update;
+  c->max_norm = max_norm;
+  return ACC_OK;
+}
+
+extern "C" int acc_get_grad_norm(acc_ctx* c, float* norm) {
+  if (!c || !norm) return ACC_EINVAL;
+  if (!c->have_norm) return c->fail(ACC_ESTATE, "the last iteration did not measure the gradient's norm (acc_set_grad_clip)");
+  *norm = c->last_norm;
   return ACC_OK;
 }
 

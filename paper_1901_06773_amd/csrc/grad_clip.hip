@@ -229,6 +229,29 @@ __global__ __launch_bounds__(THREADS) void clip_kernel(const char* list, uint32_
   }
 }
 
+// The same over one contiguous region, and an SGD step with the scaled gradient, which is not stored.  60.2 M parameters: 42 us (5.7 TB/s) more than the plain step of 118, one more
+// reading of the gradient.
+__global__ __launch_bounds__(THREADS) void region_sums_kernel(const float* __restrict__ g, size_t count, double* __restrict__ sums) {
+  double s = 0.0;
+  for (size_t at = (size_t)blockIdx.x * kPieceValues; at < count; at += (size_t)gridDim.x * kPieceValues) {
+    const Piece pc{g + at, nullptr, (uint32_t)(count - at < (size_t)kPieceValues ? count - at : (size_t)kPieceValues), DT_F32};
+    s += piece_squares<float>(pc);
+  }
+  s = block_sum(s);
+  if (threadIdx.x == 0) sums[blockIdx.x] = s;
+}
+__global__ __launch_bounds__(THREADS) void clipped_sgd_kernel(float* __restrict__ w, const float* __restrict__ g, float lr, size_t count, bf16_t* __restrict__ w16,
+                                                              const double* __restrict__ sums, int sum_count, float bound, float* __restrict__ norm) {
+  const double n = total_norm(sums, sum_count);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
+  const float f = clip_factor(n, bound);
+  for (size_t i = (size_t)blockIdx.x * THREADS + threadIdx.x; i < count; i += (size_t)gridDim.x * THREADS) {
+    const float v = fmaf(-lr, g[i] * f, w[i]);
+    w[i] = v;
+    if (w16) w16[i] = float_to_bf16(v);
+  }
+}
+
 // From 1024 pieces on (64 MB of fp32) the results are written past the caches, which then still hold more of what the norm has read (us, gradients of
 // ResNet-152, 241 MB, 145 -> 117; 140 MB of bf16 90 -> 73; 40 MB of fp32 22.1 -> 22.5, and there the update that follows finds the results in the
 // caches).  Pieces taken from the last to the first gain nothing more (118), nor do eight loads in flight (117).
@@ -280,6 +303,19 @@ hipError_t tensor_list(const void* const* src, void* const* dst, const size_t* c
 }
 
 size_t grad_norm_workspace_bytes() { return kMaxSums * sizeof(double); }
+
+hipError_t sgd_update_clipped(float* w, const float* g, float lr, float max_norm, size_t count, void* w_bf16, float* norm, void* scratch,
+                              size_t scratch_bytes, hipStream_t st) {
+  if (!w || !g || !norm || !scratch || scratch_bytes < 256 || !(max_norm >= 0.f)) return hipErrorInvalidValue;
+  const size_t room = scratch_bytes / sizeof(double), pieces = (count + kPieceValues - 1) / kPieceValues;
+  size_t sums = room < (size_t)kMaxSums ? room : (size_t)kMaxSums;
+  if (sums > pieces) sums = pieces ? pieces : 1;
+  hipLaunchKernelGGL(region_sums_kernel, dim3((unsigned)sums), dim3(THREADS), 0, st, g, count, static_cast<double*>(scratch));
+  const size_t blocks = (count + THREADS - 1) / THREADS;
+  hipLaunchKernelGGL(clipped_sgd_kernel, dim3((unsigned)(blocks < 1 ? 1 : blocks < 4096 ? blocks : 4096)), dim3(THREADS), 0, st, w, g, lr, count, (bf16_t*)w_bf16,
+                     static_cast<const double*>(scratch), (int)sums, max_norm, norm);
+  return hipGetLastError();
+}
 
 hipError_t grad_norm(const void* list, size_t list_bytes, float* norm, void* workspace, hipStream_t st) {
   if (!list || !norm || !workspace || list_bytes < sizeof(ListHeader)) return hipErrorInvalidValue;

@@ -275,6 +275,15 @@ hipError_t grad_norm(const void* list, size_t list_bytes, float* norm, void* wor
 hipError_t grad_clip(const void* list, size_t list_bytes, float bound, float* norm, void* workspace, hipStream_t st);
 // w <- w - lr * g (fp32); w_bf16 (may be null): rounded copy of the updated weights
 hipError_t sgd_update(float* w, const float* g, float lr, size_t count, void* w_bf16, hipStream_t st);
+// The same with g scaled so that its Euclidean norm is max_norm at most; norm (device): what it was.  scratch: 256 bytes at least, up to 16 KiB are used.
+hipError_t sgd_update_clipped(float* w, const float* g, float lr, float max_norm, size_t count, void* w_bf16, float* norm, void* scratch,
+                              size_t scratch_bytes, hipStream_t st);
+typedef hipError_t (*ClippedUpdate)(float*, const float*, float, float, size_t, void*, float*, void*, size_t, hipStream_t);
+// The update of a context's iterations (engine.hip); null: plain SGD.  The executor is handed the function and does not name it.
+}  // namespace acc
+struct acc_ctx;
+namespace acc {
+int set_clipped_update(acc_ctx* c, ClippedUpdate update, float max_norm);
 hipError_t fill_zero(float* p, size_t count, hipStream_t st);
 // y[n][hw][c] (dtype) = x[n][c][hw] (fp32)
 hipError_t nchw_to_nhwc(const float* x, void* y, int n, int c, int hw, int dtype, hipStream_t st);

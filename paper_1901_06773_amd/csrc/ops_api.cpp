@@ -333,6 +333,12 @@ extern "C" int acc_op_tensor_list(const void* const* src, void* const* dst, cons
   return told(tensor_list(src, dst, counts, dtypes, n, list, (hipStream_t)stream), "acc_op_tensor_list: too long");
 }
 
+extern "C" int acc_set_grad_clip(acc_ctx* ctx, float max_norm) {
+  if (!ctx) return refuse("acc_set_grad_clip: no context");
+  if (!(max_norm >= 0.f)) return refuse("acc_set_grad_clip: max_norm negative or no number");
+  return set_clipped_update(ctx, max_norm > 0.f ? sgd_update_clipped : nullptr, max_norm);
+}
+
 extern "C" size_t acc_op_grad_norm_workspace(void) { return grad_norm_workspace_bytes(); }
 
 extern "C" int acc_op_grad_norm(const void* list, size_t list_bytes, float* norm, void* workspace, size_t workspace_bytes, void* stream) {
