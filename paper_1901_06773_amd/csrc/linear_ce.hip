@@ -528,7 +528,7 @@ Plan32 plan32(int n, int d, int classes, bool grads, int dtype) {
   // Elsewhere the kernels here are (1024 x 2048 x 32768: logits 726 / 825, dx 740 / 1023, dw 775 / 841).
   p.conv = !p.widen && p.pieces == 1 && n <= 64 && classes >= 640 && classes <= 4096 && classes % 4 == 0 && d >= 256 && d % 8 == 0;
   if (p.conv) {
-    static const float any[4] = {};
+    alignas(16) static const float any[4] = {};      // (an aligned address: all that the question looks at)
     ConvGeom g = product_geom(any, nullptr, nullptr, n, classes, d);
     g.w_kn = any;
     p.conv = conv_igemm_rows_takes(g, n, classes);

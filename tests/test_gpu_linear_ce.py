@@ -126,6 +126,30 @@ def test_nothing_is_written_behind_the_results(n, d, classes, dtype):
     assert all(torch.isfinite(v).all() for k, v in bufs.items() if k != "ws")
 
 
+@pytest.mark.parametrize("dtype,d", [("f32", 1031), ("bf16", 2072)])
+def test_offsets_beyond_32_bits(dtype, d):
+    n, classes = 24, 1100003                    # 4.5 GB of weights, and of their gradient in fp32
+    x, w, b, labels = inputs(n, d, classes, dtype)
+    labels[0], labels[1] = classes - 1, 0
+    got = call(x, w, b, labels)
+    x64, z = x.double(), torch.empty(n, classes, dtype=torch.float64, device="cuda")
+    step = 100000
+    for v in range(0, classes, step):
+        z[:, v:v + step] = x64 @ w[v:v + step].double().T + b[v:v + step].double()
+    at = (torch.arange(n, device="cuda"), labels.long())
+    rows = torch.logsumexp(z, 1) - z[at]
+    dz = torch.softmax(z, 1)
+    dz[at] -= 1.0
+    dz /= n
+    dx = torch.zeros(n, d, dtype=torch.float64, device="cuda")
+    for v in range(0, classes, step):
+        dx += dz[:, v:v + step] @ w[v:v + step].double()
+    agree({k: got[k] for k in ("rows", "loss", "dx", "db")}, dict(rows=rows, loss=rows.mean().view(1), dx=dx, db=dz.sum(0)), dtype)
+    for v in (0, 400000, 1000000, classes - 1000):
+        part = slice(v, v + 1000)
+        agree(dict(dw=got["dw"][part]), dict(dw=dz[:, part].T @ x64), dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,d,classes", [(1, 64, 100), (90, 72, 300), (300, 256, 2000)])
 def test_rows_that_do_not_count(n, d, classes, dtype):
