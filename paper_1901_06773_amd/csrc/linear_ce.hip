@@ -500,7 +500,7 @@ ConvGeom product_geom(const float* in, const float* w, float* out, int n, int c,
 struct Plan32 {
   long piece, pieces, splits;    // classes of a piece, pieces, columns of `part`
   int pitch;                     // of z
-  bool rows;                     // one piece of at most kRowCols classes: a workgroup per row
+  bool rows;                     // few rows and classes: a workgroup per row
   bool conv;                     // dx and dw by the convolution kernels
   bool late;                     // the logits' sums and bias in a launch of their own: row_sums_kernel
   bool widen;                    // bf16 operands are copied
@@ -521,7 +521,9 @@ Plan32 plan32(int n, int d, int classes, bool grads, int dtype) {
   p.piece = classes <= most ? classes : most;
   p.pieces = ceil_div(classes, p.piece);
   p.pitch = (int)up(p.piece, 4);
-  p.rows = p.pieces == 1 && p.piece <= kRowCols && n <= 16384;
+  // (us, all results, a workgroup per row / sums with the logits: 300 x 64 x 40 24 / 32, 1024 x 512 x 1000 58 / 63, 4096 x 512 x 1000 146 / 150,
+  // 16384 x 256 x 1000 235 / 226, 512 x 128 x 8000 71 / 69, 2048 x 64 x 8000 131 / 118, 4096 x 128 x 4000 193 / 172)
+  p.rows = p.pieces == 1 && n <= 4096 && p.piece <= (n <= 512 ? kRowCols : kRowCols / 4);
   p.widen = dtype != DT_F32;
   // Few rows and classes of whole widths: the convolution kernels' launches, which deal the sum out among the waves of a workgroup, are faster than cutting it
   // and a launch for the parts' sums (us, all results, here / convolution: 41 x 2048 x 1000 33 / 30, 16 x 2048 x 4096 58 / 52, 64 x 256 x 256 19 / 26).
