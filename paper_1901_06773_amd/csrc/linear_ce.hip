@@ -8,7 +8,7 @@
 // both operands.  With one piece the logits of the first sweep are still there.  2 n d classes operations for the loss, 6 more (4 with
 // one piece) for the gradients, which is what bounds it.
 //
-// fp32: logits and dz of a piece in fp32, products by gemm_f32.h, whose epilogue takes the rows' sums along.  Few classes (8192 in one piece): a launch turns
+// fp32: logits and dz of a piece in fp32, products by gemm_f32.h, whose epilogue takes the rows' sums along.  Few rows and classes: a launch turns
 // whole rows of logits into dz.  Few tiles: dx, dw, db and the mean loss in one launch.
 #include "kernels.h"
 #include "dtype.h"
