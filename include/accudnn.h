@@ -424,7 +424,7 @@ int acc_op_softmax_ce(const void* z, const int32_t* labels, float* loss_rows, fl
  * bwd: g = dy * act'(z); dbeta = sum of g, dgamma = sum of g * (x - mean) * istd over n and hw; dx; dres (may be NULL) = g.
  * y: the stored output, needed for ACC_ACT_RELU (g = dy where y > 0, else 0); res: the residual that went into the forward pass,
  * for ACC_ACT_SILU (NULL if there was none).  mean and istd are those of the forward pass.  workspace: acc_op_gn_workspace() bytes
- * (enough for both directions and storage types); nothing in it needs to be kept or cleared.  No atomics: the same bits every time.
+ * (enough for both directions and storage types; 0: the sizes are refused); nothing in it needs to be kept or cleared.  No atomics: the same bits every time.
  * y may be x or res, dx may be x or dy, dres may be dy; nothing else that is written may overlap another argument (ACC_EINVAL). */
 enum { ACC_ACT_NONE = 0, ACC_ACT_RELU = 1, ACC_ACT_SILU = 2 };
 size_t acc_op_gn_workspace(int n, int hw, int c, int groups);

@@ -999,6 +999,7 @@ bool shape_ok(int n, int hw, int c, int groups, int act, int dtype) {
 
 }  // namespace
 
+// (0: refused, for either storage type, as the calls are: one size serves both)
 size_t gn_workspace_bytes(int n, int hw, int c, int groups) {
   if (!shape_ok(n, hw, c, groups, ACT_NONE, DT_F32) || !shape_ok(n, hw, c, groups, ACT_NONE, DT_BF16)) return 0;
   // the sums of a backward pass in slabs, or one pair of sums per image and channel; whichever storage type needs more
@@ -1011,11 +1012,16 @@ size_t gn_workspace_bytes(int n, int hw, int c, int groups) {
   }
   return most;
 }
+// whether the sizes are taken and the workspace holds what a call writes into it
+static bool room_ok(int n, int hw, int c, int groups, int act, int dtype, size_t workspace_bytes) {
+  const size_t need = gn_workspace_bytes(n, hw, c, groups);
+  return need && workspace_bytes >= need && shape_ok(n, hw, c, groups, act, dtype);
+}
 
 hipError_t gn_forward(const void* x, const float* gamma, const float* beta, const void* res, void* y, float* mean, float* istd, int n, int hw, int c,
                       int groups, int act, float eps, void* workspace, size_t workspace_bytes, int dtype, hipStream_t st) {
   if (!x || !gamma || !beta || !y || !mean || !istd || !workspace || !(eps >= 0.f)) return hipErrorInvalidValue;
-  if (!shape_ok(n, hw, c, groups, act, dtype) || workspace_bytes < gn_workspace_bytes(n, hw, c, groups)) return hipErrorInvalidValue;
+  if (!room_ok(n, hw, c, groups, act, dtype, workspace_bytes)) return hipErrorInvalidValue;
   GnArgs a{};
   a.x = x; a.gamma = gamma; a.beta = beta; a.side = res; a.out = y; a.mean = mean; a.istd = istd;
   a.n = n; a.hw = hw; a.c = c; a.groups = groups; a.eps = eps; a.workspace = workspace; a.st = st;
@@ -1028,7 +1034,7 @@ hipError_t gn_backward(const void* x, const void* dy, const void* y, const void*
                        const float* istd, void* dx, float* dgamma, float* dbeta, void* dres, int n, int hw, int c, int groups, int act, void* workspace,
                        size_t workspace_bytes, int dtype, hipStream_t st) {
   if (!x || !dy || !gamma || !beta || !mean || !istd || !dx || !dgamma || !dbeta || !workspace) return hipErrorInvalidValue;
-  if (!shape_ok(n, hw, c, groups, act, dtype) || workspace_bytes < gn_workspace_bytes(n, hw, c, groups)) return hipErrorInvalidValue;
+  if (!room_ok(n, hw, c, groups, act, dtype, workspace_bytes)) return hipErrorInvalidValue;
   if (act == ACT_RELU && !y) return hipErrorInvalidValue;
   GnArgs a{};
   a.x = x; a.dy = dy; a.side = act == ACT_RELU ? y : act == ACT_SILU ? res : nullptr; a.gamma = gamma; a.beta = beta; a.mean_in = mean; a.istd_in = istd;

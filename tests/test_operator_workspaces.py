@@ -1,0 +1,37 @@
+"""Workspace sizes and refusals agree, on the C entry points and without a GPU: nothing here reaches a device."""
+import pytest
+
+from paper_1901_06773_amd import binding as B
+
+L = B.lib()
+
+
+def at(k):
+    return k << 44            # far from one another; nothing reads them
+
+
+def gn_forward(n, hw, c, groups, size, dtype):
+    return L.acc_op_gn_fwd(at(1), at(2), at(3), None, at(4), at(5), at(6), n, hw, c, groups, 0, 1e-5, at(7), size, dtype, None)
+
+
+def gn_backward(n, hw, c, groups, size, dtype):
+    return L.acc_op_gn_bwd(at(1), at(2), None, None, at(3), at(4), at(5), at(6), at(7), at(8), at(9), None, n, hw, c, groups, 0, at(10), size, dtype, None)
+
+
+# sizes that one storage type alone would take: a bf16 row of 516 channels is read value by value, in four times the workgroups
+@pytest.mark.parametrize("n,hw,c,groups", [(4194304, 1, 516, 4), (4194304, 1, 516, 2), (4194304, 1, 900, 4)])
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+def test_group_norm_of_sizes_without_a_workspace_is_refused(n, hw, c, groups, dtype):
+    assert L.acc_op_gn_workspace(n, hw, c, groups) == 0
+    for size in (16, 1 << 40):
+        for call in (gn_forward, gn_backward):
+            assert call(n, hw, c, groups, size, dtype) == B.ACC_EINVAL, (call.__name__, size)
+
+
+@pytest.mark.parametrize("n,hw,c,groups", [(4000000, 1, 516, 4), (1, 1, 1, 1), (3, 49, 30, 3), (64, 3136, 256, 32)])
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+def test_group_norm_with_a_smaller_workspace_is_refused(n, hw, c, groups, dtype):
+    size = L.acc_op_gn_workspace(n, hw, c, groups)
+    assert size > 0
+    for call in (gn_forward, gn_backward):
+        assert call(n, hw, c, groups, size - 256, dtype) == B.ACC_EINVAL
