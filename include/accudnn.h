@@ -439,7 +439,7 @@ int acc_op_gn_bwd(const void* x, const void* dy, const void* y, const void* res,
  * classes and never kept whole (n * classes values are the largest map of a head with many classes), loss and gradients as
  * acc_op_softmax_ce defines them.  x [n][d], w [classes][d] and dx [n][d] are stored as dtype; bias [classes] (may be NULL), loss_rows [n], loss [1],
  * dw [classes][d] and db [classes] are fp32; labels [n] int32, device.  Sums, logits and dz are fp32 (dz of bf16 operands: the sum of two
- * bf16 values in dw, of three for fewer than 4096 rows; one in dx, which is rounded to bf16 itself).
+ * bf16 values in dx and dw, of three in dw for fewer than 4096 rows).
  * ignore: rows with this label do not count (padding): loss_rows is 0 there, their gradient is 0, and the mean is over the others (0 if
  * there are none); their x still has to be finite.  ACC_LABEL_NONE: every row counts.  Any other label outside [0, classes): the row's loss is
  * NaN and its gradient has no one-hot term.  Logits of minus infinity (a bias that rules a class out) have probability 0.

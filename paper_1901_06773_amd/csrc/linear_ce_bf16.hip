@@ -2,10 +2,12 @@
 // epilogues: logits leave a tile as the largest one of its columns and the sum of exponentials, or as dz.
 //
 // dz is left without the factor 1 / rows (a label's value is then -1 where its probability is small, exact in bf16) as the sum of two or three
-// bf16 values, the first the nearest one, the next the nearest to what is left.  dw, an fp32 result, is multiplied from all of them: one leaves a
-// relative error of up to 2^-9, two of 2^-18, three of 2^-27.  Two are enough from 4096 rows on, where the rounding of the fp32 sums is as large (relative
-// error of dw, 4096 rows 1.16e-6, the same sums of exact fp32 products 1.14e-6; 64 rows 1.9e-6 and, with three, 0.2e-6).  dx, which is rounded to
-// bf16 itself, is multiplied from the first.  The factor is applied to the fp32 accumulators.
+// bf16 values, the first the nearest one, the next the nearest to what is left: one leaves a relative error of up to 2^-8, two of 2^-16, three of 2^-24.
+// dw, an fp32 result, is multiplied from all of them.  Two are enough from 4096 rows on, where the rounding of the fp32 sums is as large (relative
+// error of dw, 4096 rows 1.16e-6, the same sums of exact fp32 products 1.14e-6; 64 rows 1.9e-6 and, with three, 0.2e-6).  dx is multiplied from the first
+// two: one would do if its errors stayed beside the result's own rounding, but a row of dz sums to zero, so that what the classes' weights have in common cancels
+// in dx and its errors do not (relative error of dx, 300 x 128 x 10, weights with a common part of 10 and 30 times their spread: one value 0.012 and 0.038, two
+// 0.0017, which is the rounding of the result; 4096 x 2048 x 65536, all results, 4720 and 5525 us).  The factor is applied to the fp32 accumulators.
 #include "kernels.h"
 #include "dtype.h"
 #include "gemm_bf16.h"
@@ -342,8 +344,7 @@ __global__ __launch_bounds__(256) void lce_dz_kept_kernel(LogitArgs a, int block
   *reinterpret_cast<float4*>(to + 4) = make_float4(sum[4], sum[5], sum[6], sum[7]);
 }
 
-// dx: sums[split][n][d] (+)= dz w over the split's classes of the piece, or dx itself where there is one split of one piece.  4096 x 2048 x 16384: 243 us,
-// 1131 TFLOP/s.
+// dx: sums[split][n][d] (+)= dz w over the split's classes of the piece, dz as the sum of its first two parts, or dx itself where there is one split of one piece.
 struct DxArgs {
   GemmOperand dz, w;
   float* sums;
@@ -541,9 +542,9 @@ __global__ __launch_bounds__(256) void lce_pad_kernel(const bf16_t* __restrict__
 typedef GemmCfg<2, 4, 4, 2, 64, 2, false, false, 1, true> Z256;
 typedef GemmCfg<2, 2, 2, 2, 64, 2, false, false, 1, true> Z128;
 typedef GemmCfg<2, 2, 1, 1, 64, 4, false, false, 1, true> Z64;
-typedef GemmCfg<2, 4, 4, 2, 64, 2, false, true, 1, false> X256;
-typedef GemmCfg<2, 2, 2, 2, 64, 2, false, true, 1, false> X128;
-typedef GemmCfg<2, 2, 1, 1, 64, 4, false, true, 1, false> X64;
+typedef GemmCfg<2, 4, 4, 2, 32, 3, false, true, 2, false> X256;        // dx
+typedef GemmCfg<2, 2, 2, 2, 32, 3, false, true, 2, false> X128;
+typedef GemmCfg<2, 2, 1, 1, 32, 4, false, true, 2, false> X64;
 typedef GemmCfg<2, 4, 4, 2, 32, 3, true, true, 2, false> W256;
 typedef GemmCfg<2, 2, 2, 2, 32, 2, true, true, 2, false> W128;
 typedef GemmCfg<2, 2, 1, 1, 32, 4, true, true, 2, false> W64;
@@ -562,7 +563,7 @@ inline long ceil_div(long a, long b) { return (a + b - 1) / b; }
 struct TileCost {
   double first, first_step, next, next_step;
 };
-enum { RowsByRows = 0, ByColumns };            // both operands along k; A and B (dw) in rows of k
+enum { RowsByRows = 0, ByColumns };            // both operands along k, in steps of 64; B in rows of k, steps of 32 (dx, dw)
 constexpr TileCost kCost[2][3] = {{{4.0, 1.28, 8.0, 1.60}, {3.0, 0.62, 3.2, 0.50}, {1.5, 0.31, 1.7, 0.205}},
                                   {{4.0, 1.30, 12.0, 1.50}, {3.0, 0.62, 5.0, 0.55}, {1.5, 0.31, 1.0, 0.28}}};
 constexpr int kTiles[3] = {256, 128, 64};
@@ -634,9 +635,9 @@ Plan16 plan16(int n, int d, int classes, bool grads) {
   p.pitch = (int)(p.pieces > 1 ? p.piece : up(classes, 64));
   // where the products take longer than writing and reading their results (us, second sweep of 777 x 1160 x 50001: 183 worked out again, 128 kept)
   p.keep = grads && d >= 1024;
-  p.dx = choose(RowsByRows, n, d, p.pitch, 1, 1L << 25, 256);
+  p.dx = choose(ByColumns, n, d, p.pitch, 2, 1L << 25, 256);
   p.dw = choose(ByColumns, whole, d, n, p.parts, 1L << 24, 128);
-  const Choice dx = choose(RowsByRows, n, d, p.pitch, 1, 1L << 25, 256, 2), dw = choose(ByColumns, whole, d, n, p.parts, 1L << 24, 128, 2);
+  const Choice dx = choose(ByColumns, n, d, p.pitch, 2, 1L << 25, 256, 2), dw = choose(ByColumns, whole, d, n, p.parts, 1L << 24, 128, 2);
   p.together = p.pieces == 1 && ceil_div(d, 64) * (ceil_div(n, 64) * dx.splits + ceil_div(whole, 64) * dw.splits) <= 1024;
   if (p.together) { p.dx = dx; p.dw = dw; }
   // (a row's sums are then read by every tile across)

@@ -1,0 +1,51 @@
+"""How many bits the gradients of the linear cross-entropy keep, against 64 bits, where fewer would show.
+
+Tolerances.  A value held as the sum of two bf16 values is off by 2^-16 of itself at most, of three by 2^-24; a result rounded to bf16 by 2^-8 of itself.  Sums and
+logits add 2e-5 of the magnitudes that are summed (test_gpu_linear_ce.py)."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def B():
+    from paper_1901_06773_amd import binding
+    return binding
+
+
+def inputs(n, d, classes, common, seed=3):
+    """bf16 operands; the classes' weights have a part in common, `common` times as large as what sets them apart."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def randn(*s):
+        return torch.randn(*s, generator=g, device="cuda")
+    w = 2 / d ** 0.5 * (randn(classes, d) + common * randn(d))
+    labels = torch.randint(classes, (n,), generator=g, device="cuda", dtype=torch.int32)
+    x = randn(n, d) + w[labels.long()] * torch.rand(n, 1, generator=g, device="cuda") / (1 + common)
+    return x.bfloat16(), w.bfloat16(), labels
+
+
+def gradients(x, w, labels):
+    n, d = x.shape
+    classes = w.shape[0]
+    dx, dw = torch.empty_like(x), torch.empty(classes, d, device="cuda")
+    ws = torch.empty(B().op_linear_ce_workspace(n, d, classes, True, B()._dtype_of(x)), dtype=torch.uint8, device="cuda")
+    B().op_linear_ce(x, w, None, labels, None, None, dx, dw, None, ws)
+    return dx, dw
+
+
+def dz_of(x, w, labels):
+    n = x.shape[0]
+    dz = torch.softmax(x.double() @ w.double().T, 1)
+    dz[torch.arange(n, device="cuda"), labels.long()] -= 1.0
+    return dz / n
+
+
+@pytest.mark.parametrize("common", [0, 10, 30])
+@pytest.mark.parametrize("n,d,classes", [(64, 256, 1000), (300, 128, 10), (256, 1160, 5000), (777, 520, 3001), (4100, 64, 33333), (4100, 1032, 2000)])
+def test_what_the_weights_have_in_common_cancels_in_dx(n, d, classes, common):
+    x, w, labels = inputs(n, d, classes, common)
+    dx, _ = gradients(x, w, labels)
+    dz = dz_of(x, w, labels)
+    ref, summed = dz @ w.double(), dz.abs() @ w.double().abs()
+    assert (dx.double() - ref).norm() <= 2.0 ** -8 * ref.norm() + (2.0 ** -16 + 2e-5) * summed.norm()
