@@ -9,6 +9,7 @@
 // Bound by memory.  A sum over rows is a sum per channel first, in a fixed order, then over the channels of a group: no atomics.
 #include "kernels.h"
 #include "dtype.h"
+#include "gn_shape.h"
 
 namespace acc {
 namespace {
@@ -458,13 +459,6 @@ __global__ __launch_bounds__(THREADS) void gn_bwd_apply_kernel(const T* x, const
 // A workgroup takes all rows of a few neighbouring groups of one image, 64 bytes of channels or more, and keeps them: thread t has V channels of the rows
 // t / tpr, t / tpr + rpi, ...  Forward: mean, then the squares of the deviations from it, both in fp32 (a thread adds at most R values one behind
 // the other, the rest in a tree).  The XCD-wise order of workgroups lets neighbouring slices of a row meet in one L2.
-struct Slice {
-  int hw, c, groups, per;
-  int k, s, slices;                                    // groups and channels of a slice, slices of an image
-  int tpr, rpi, trips, rest;                           // hw = trips * rpi + rest
-  int all;                                             // slices of all images
-};
-
 // The sum over a wave, in every lane, in a fixed order: neighbouring lanes first, by moves that stay in registers (a butterfly through LDS is six
 // trips one after the other).
 __device__ __forceinline__ float wave_sum_f(float v) {
@@ -527,8 +521,6 @@ __device__ __forceinline__ uint32_t anew(uint32_t v) {
 template <int R> __device__ __forceinline__ void pause(int u) {
   if (R > 4 && (u & 1)) fence();
 }
-
-constexpr int kMaxSliceGroups = 256;
 
 // One pass over the data: a slice's rows stay in registers between the sums and the results.  Bound by memory: 64 images of 56x56, 256 channels, bf16 42 us for
 // 206 MB (4.9 TB/s; every value is fetched once and written once), where the two launches take 56.
@@ -790,51 +782,6 @@ __global__ __launch_bounds__(NT) void gn_bwd_slice_kernel(const T* x, const T* d
       to += step;
       pause<R>(u);
     }
-}
-
-// The slices of a tensor, if they fit: 64 bytes of channels (a line of memory is then read by two workgroups at most) or as many groups as it takes for
-// whole threads; 32 bytes where 64 do not fit.  Threads and rows of a workgroup: the fewest threads whose registers hold a slice.  Not where a few workgroups would have long
-// slices to work on and the rest of the chip nothing: there the two launches, which cut an image's rows, are faster.  Measured, us, slices / two launches:
-// forward, 51200 values in a slice, bf16, 1 image 40x40 of 512 channels (16 workgroups) 10.0 / 16.2; 100352, bf16 56x56 of 256, 2 images (16) 13.6 / 11.8, 8 (64)
-// 15.4 / 18.0; 32-byte slices backward, 56x56 of 256, fp32 4 images (128) 25.5 / 22.7, 8 (256) 28.7 / 36.1, bf16 16 (256) 27.1 / 45.8.
-constexpr int kSliceGroups = 64, kSliceValues = 60000, kNarrowSlices = 256;
-struct SliceCfg {
-  Slice sl;
-  int nt, r;                                           // 0: does not fit
-};
-// rows of a thread of 1024 that fit 128 registers beside what else it needs
-constexpr int slice_rows(int v, bool perch, bool backward) { return !backward ? 20 : v == 4 ? (perch ? 8 : 10) : (perch ? 6 : 8); }
-SliceCfg slice_cfg(int n, int hw, int c, int groups, int v, int es, bool backward) {
-  SliceCfg f{};
-  const int per = c / groups;
-  if ((long)hw * c * es >= 1L << 32) return f;
-  auto fits = [&](int k) {
-    const int tpr = k * per / v;
-    if (tpr > 256) return false;
-    auto rows = [&](int nt) { return (int)(((long)hw + nt / tpr - 1) / (nt / tpr)); };
-    const int nt = rows(256) <= (backward ? 4 : 8) ? 256 : rows(512) <= (backward ? 8 : 16) ? 512 : rows(1024) <= slice_rows(v, per % v != 0, backward) ? 1024 : 0;
-    if (!nt || (long)n * (groups / k) * nt >= (1L << 32) - 8192) return false;         // (a launch has fewer than 2^32 threads)
-    f.nt = nt;
-    f.r = rows(nt);
-    f.sl = Slice{hw, c, groups, per, k, k * per, groups / k, tpr, nt / tpr, hw / (nt / tpr), hw % (nt / tpr), n * (groups / k)};
-    return true;
-  };
-  int narrow = 0;                                      // the widest slice of 32 bytes or more that is narrower than 64
-  for (int k = 1; k <= groups && k <= kMaxSliceGroups; ++k) {
-    if (groups % k != 0 || (long)k * per % v != 0) continue;
-    const long bytes = (long)k * per * es;
-    if (bytes < 64 && k < groups) {
-      if (bytes >= 32) narrow = k;
-      continue;
-    }
-    if (fits(k)) {
-      if (f.sl.all < kSliceGroups && (long)hw * k * per > kSliceValues) f.nt = 0;
-    } else if (narrow && fits(narrow) && f.sl.all < kNarrowSlices) {
-      f.nt = 0;
-    }
-    return f;
-  }
-  return f;
 }
 
 // How the two launches cover a tensor, V channels per thread; false: a row has no slices of whole threads (then one value at a time does).
