@@ -287,7 +287,7 @@ int acc_train_step(acc_ctx* ctx, const float* images, int images_loc, const int3
  * gradients of the network, as acc_op_grad_clip() scales them (the quotient and the product rounded to fp32); the stored gradients
  * (acc_get_grads) stay as they are.  max_norm = 0, the default: no clipping and no norm; INFINITY: the norm only.  No memory beyond the
  * plan's: the partial sums use the part of the pool that an iteration's maps have left.  A norm that is NaN makes all weights NaN.
- * acc_get_grad_norm: N of the last iteration (ACC_ESTATE if it had no max_norm). */
+ * acc_get_grad_norm: N of the last iteration (ACC_ESTATE if it had no max_norm, or failed). */
 int acc_set_grad_clip(acc_ctx* ctx, float max_norm);
 int acc_get_grad_norm(acc_ctx* ctx, float* norm);
 /* What the last iteration did (Sec. 6.2.2 and 6.2.3 verify the memory and the transfer model

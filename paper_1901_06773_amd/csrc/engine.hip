@@ -1006,6 +1006,7 @@ extern "C" int acc_train_step(acc_ctx* c, const float* images, int images_loc, c
       for (const acc_ctx::Capture& cp : list)
         if (cp.cap < (size_t)P.k * g.tensors[cp.tensor].bytes_per_image)
           return c->fail(ACC_EINVAL, "a capture / injection buffer is smaller than the layer's output at this minibatch");
+  c->have_norm = false;                // (an iteration that fails leaves none)
   const bool poison = (c->debug_flags & ACC_DEBUG_POISON) != 0;
   unsigned long long* d_scan = (unsigned long long*)((char*)c->d_loss + 16);
   if (poison) {
