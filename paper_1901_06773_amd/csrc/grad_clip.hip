@@ -277,7 +277,7 @@ hipError_t tensor_list(const void* const* src, void* const* dst, const size_t* c
   if (!bytes) return hipErrorInvalidValue;
   ListBatch b{};
   b.total = (uint32_t)((bytes - sizeof(ListHeader)) / sizeof(Piece));
-  for (int i = 0; i < n || i == 0;) {
+  for (int i = 0; i < n;) {
     const int from = i;
     uint32_t pieces = 0;
     for (uint32_t& w : b.bf16) w = 0;
@@ -297,7 +297,6 @@ hipError_t tensor_list(const void* const* src, void* const* dst, const size_t* c
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     b.at += pieces;
-    if (n == 0) break;
   }
   return hipSuccess;
 }
