@@ -373,27 +373,30 @@ struct Finish32 {
   unsigned dx_blocks, dw_blocks, db_blocks;
 };
 constexpr int kColumnRows = 1024;
+// 1024 values of a workgroup at a time; 2^20 workgroups at most, as a launch has fewer than 2^32 threads
+inline unsigned join_blocks(size_t count) { const size_t b = (count + 1023) / 1024; return (unsigned)(b < 1u << 20 ? b : 1u << 20); }
 template <class T>
-__device__ __forceinline__ void join_sums(const float* __restrict__ sums, T* __restrict__ out, size_t count, int splits, size_t block) {
-  for (size_t i = block * 1024 + threadIdx.x; i < count && i < (block + 1) * 1024; i += THREADS) {
-    float s = sums[i];
-    int k = 1;
-    for (; k + 8 <= splits; k += 8) {
-      float q[8];
+__device__ __forceinline__ void join_sums(const float* __restrict__ sums, T* __restrict__ out, size_t count, int splits, size_t block, size_t blocks) {
+  for (; block * 1024 < count; block += blocks)
+    for (size_t i = block * 1024 + threadIdx.x; i < count && i < (block + 1) * 1024; i += THREADS) {
+      float s = sums[i];
+      int k = 1;
+      for (; k + 8 <= splits; k += 8) {
+        float q[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) q[u] = sums[(k + u) * count + i];
+        for (int u = 0; u < 8; ++u) q[u] = sums[(k + u) * count + i];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) s += q[u];
+        for (int u = 0; u < 8; ++u) s += q[u];
+      }
+      for (; k < splits; ++k) s += sums[k * count + i];
+      Elem<T>::store(out + i, s);
     }
-    for (; k < splits; ++k) s += sums[k * count + i];
-    Elem<T>::store(out + i, s);
-  }
 }
 template <class T>
 __device__ __forceinline__ void finish32(const Finish32& f, unsigned block) {
-  if (block < f.dx_blocks) return join_sums<T>(f.dx_sums, (T*)f.dx, f.dx_count, f.dx_splits, block);
+  if (block < f.dx_blocks) return join_sums<T>(f.dx_sums, (T*)f.dx, f.dx_count, f.dx_splits, block, f.dx_blocks);
   block -= f.dx_blocks;
-  if (block < f.dw_blocks) return join_sums<float>(f.dw_sums, f.dw, f.dw_count, f.dw_splits, block);
+  if (block < f.dw_blocks) return join_sums<float>(f.dw_sums, f.dw, f.dw_count, f.dw_splits, block, f.dw_blocks);
   block -= f.dw_blocks;
   if (block >= f.db_blocks) return mean_of_rows<THREADS>(f.loss_rows, f.labels, f.ignore, f.n, nullptr, f.loss);
   // sixty-four columns, a quarter of the slab's rows to each wave
@@ -677,7 +680,7 @@ hipError_t run32(const LceArgs& a) {
       if (!p.together) ACC_TRY((launch_product32<false, true>(gx, p.dx, st)));
       if (p.sum_dx && last) {
         f.dx_sums = dx_out; f.dx = a.dx; f.dx_count = (size_t)a.n * a.d; f.dx_splits = p.dx.splits;
-        f.dx_blocks = (unsigned)((f.dx_count + 1023) / 1024);
+        f.dx_blocks = join_blocks(f.dx_count);
       }
     }
     if (a.dw) {
@@ -695,7 +698,7 @@ hipError_t run32(const LceArgs& a) {
         if (!p.together) ACC_TRY((launch_product32<true, true>(gw, p.dw, st)));
         if (p.dw.splits > 1) {
           f.dw_sums = gw.out; f.dw = to; f.dw_count = (size_t)cols * a.d; f.dw_splits = p.dw.splits;
-          f.dw_blocks = (unsigned)((f.dw_count + 1023) / 1024);
+          f.dw_blocks = join_blocks(f.dw_count);
         }
       }
     }
