@@ -457,11 +457,12 @@ int acc_op_linear_ce(const void* x, const void* w, const float* bias, const int3
  * addresses and sizes not): acc_op_tensor_list() writes it in stream order, from kernel arguments, so it may be captured; the host arrays
  * (src, dst, counts, dtypes; n entries each) may go once it returns.  A tensor is counts[i] contiguous values (0: it is passed over) of
  * ACC_F32 or ACC_BF16 at any address that its type allows.  dst: where acc_op_grad_clip() writes (dst[i] may be src[i]); NULL: in
- * place.  What is written may not overlap any other tensor of the list (ACC_EINVAL; so the same tensor may not be listed twice).
+ * place.  What is written may not overlap any other tensor of the list or the list's own memory (ACC_EINVAL; so the same tensor may not be listed twice).
  * list_bytes: the size of the list's memory, the same in every call, at least acc_op_tensor_list_bytes() (0: no list, or more than 2^30 pieces of 16384 values).
- * norm: one float, device.  workspace: acc_op_grad_norm_workspace() bytes, not shared by calls that overlap.
+ * norm: one float, device.  workspace: acc_op_grad_norm_workspace() bytes, not shared by calls that overlap.  List, norm and workspace may not overlap
+ * (ACC_EINVAL), nor may they lie in a tensor of the list (which the host cannot see).
  * acc_op_grad_clip: dst = src * (norm <= max_norm ? 1 : max_norm / norm), the quotient in fp32, the product rounded to the tensor's type; max_norm >= 0.  A norm that is NaN makes every value
- * NaN, an infinite one every finite value 0.  Squares and sums are fp64, in a fixed order. */
+ * NaN, an infinite one beyond a finite max_norm every finite value 0.  Squares and sums are fp64, in a fixed order. */
 size_t acc_op_tensor_list_bytes(const size_t* counts, int n);
 int acc_op_tensor_list(const void* const* src, void* const* dst, const size_t* counts, const int32_t* dtypes, int n, void* list,
                        size_t list_bytes, void* stream);

@@ -310,7 +310,8 @@ extern "C" int acc_op_tensor_list(const void* const* src, void* const* dst, cons
     // what is written must not overlap what another tensor of the list reads or writes: pieces run at once
     struct Span { uintptr_t lo, hi; int tensor; bool written; };
     std::vector<Span> spans;
-    spans.reserve(2 * (size_t)n);
+    spans.reserve(2 * (size_t)n + 1);
+    spans.push_back(Span{(uintptr_t)list, (uintptr_t)list + need, -1, true});      // the list itself
     for (int i = 0; i < n; ++i) {
       if (!dtype_ok(dtypes[i])) return refuse("acc_op_tensor_list: dtypes must be ACC_F32 or ACC_BF16");
       if (!counts[i]) continue;
@@ -322,7 +323,7 @@ extern "C" int acc_op_tensor_list(const void* const* src, void* const* dst, cons
     std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.lo < b.lo; });
     uintptr_t end = 0, end_written = 0;              // the furthest end so far, of all and of what is written
     for (const Span& s : spans) {
-      if (s.written ? s.lo < end : s.lo < end_written) return refuse("acc_op_tensor_list: tensors overlap (or the same one is listed twice)");
+      if (s.written ? s.lo < end : s.lo < end_written) return refuse("acc_op_tensor_list: tensors overlap one another (or the same one is listed twice) or the list's memory");
       end = std::max(end, s.hi);
       if (s.written) end_written = std::max(end_written, s.hi);
     }
@@ -344,11 +345,13 @@ extern "C" size_t acc_op_grad_norm_workspace(void) { return grad_norm_workspace_
 extern "C" int acc_op_grad_norm(const void* list, size_t list_bytes, float* norm, void* workspace, size_t workspace_bytes, void* stream) {
   if (!al16({list, norm, workspace})) return refuse("acc_op_grad_norm: pointers must be 16-byte aligned");
   if (workspace_bytes < grad_norm_workspace_bytes()) return refuse("acc_op_grad_norm: workspace smaller than acc_op_grad_norm_workspace()");
+  if (clash({{norm, 4, {}}, {workspace, workspace_bytes, {}}}, {{list, list_bytes, {}}})) return refuse("acc_op_grad_norm: list, norm and workspace overlap");
   return told(grad_norm(list, list_bytes, norm, workspace, (hipStream_t)stream), "acc_op_grad_norm: null pointer or no list");
 }
 
 extern "C" int acc_op_grad_clip(const void* list, size_t list_bytes, float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream) {
   if (!al16({list, norm, workspace})) return refuse("acc_op_grad_clip: pointers must be 16-byte aligned");
   if (workspace_bytes < grad_norm_workspace_bytes()) return refuse("acc_op_grad_clip: workspace smaller than acc_op_grad_norm_workspace()");
+  if (clash({{norm, 4, {}}, {workspace, workspace_bytes, {}}}, {{list, list_bytes, {}}})) return refuse("acc_op_grad_clip: list, norm and workspace overlap");
   return told(grad_clip(list, list_bytes, max_norm, norm, workspace, (hipStream_t)stream), "acc_op_grad_clip: null pointer, no list, or max_norm negative or no number");
 }
