@@ -442,7 +442,8 @@ int acc_op_gn_bwd(const void* x, const void* dy, const void* y, const void* res,
  * bf16 values in dx and dw, of three in dw for fewer than 4096 rows).
  * ignore: rows with this label do not count (padding): loss_rows is 0 there, their gradient is 0, and the mean is over the others (0 if
  * there are none); their x still has to be finite.  ACC_LABEL_NONE: every row counts.  Any other label outside [0, classes): the row's loss is
- * NaN and its gradient has no one-hot term.  Logits of minus infinity (a bias that rules a class out) have probability 0.
+ * NaN and its gradient has no one-hot term.  Logits of minus infinity (a bias that rules a class out) have probability 0.  x and w have to be finite: a row
+ * of x that is not has a loss that is infinite or NaN (large fp32 products make NaN of an infinity), and so have the gradients that it enters.
  * loss_rows, loss, dx, dw, db: each may be NULL, at least one is not; without dx, dw and db no gradient is computed.  What is written may not
  * overlap another argument (ACC_EINVAL).
  * n <= 2^20, d <= 65536, classes <= 2^24.  workspace: acc_op_linear_ce_workspace() bytes, gradients = whether any of dx, dw, db is asked for. */

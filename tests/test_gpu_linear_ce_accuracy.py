@@ -49,3 +49,22 @@ def test_what_the_weights_have_in_common_cancels_in_dx(n, d, classes, common):
     dz = dz_of(x, w, labels)
     ref, summed = dz @ w.double(), dz.abs() @ w.double().abs()
     assert (dx.double() - ref).norm() <= 2.0 ** -8 * ref.norm() + (2.0 ** -16 + 2e-5) * summed.norm()
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,d,classes", [(9, 64, 100), (300, 256, 1500), (1024, 512, 8192), (600, 512, 30000)])
+def test_a_row_that_is_not_finite_has_no_finite_loss_and_leaves_the_others(n, d, classes, dtype, value):
+    x, w, labels = (t if t.dtype == torch.int32 else t.to(dtype) for t in inputs(n, d, classes, 0))
+
+    def losses():
+        rows = torch.empty(n, device="cuda")
+        ws = torch.empty(B().op_linear_ce_workspace(n, d, classes, False, B()._dtype_of(x)), dtype=torch.uint8, device="cuda")
+        B().op_linear_ce(x, w, None, labels, rows, None, None, None, None, ws)
+        return rows
+    whole = losses()
+    x[5, d // 2] = value
+    rows = losses()
+    assert torch.isfinite(whole).all() and not torch.isfinite(rows[5])
+    others = torch.arange(n, device="cuda") != 5
+    assert torch.equal(rows[others], whole[others])
