@@ -51,6 +51,41 @@ def test_what_the_weights_have_in_common_cancels_in_dx(n, d, classes, common):
     assert (dx.double() - ref).norm() <= 2.0 ** -8 * ref.norm() + (2.0 ** -16 + 2e-5) * summed.norm()
 
 
+# A gradient's sum of up to 2048 products is rounded some 400 times, by 2^-24 of a partial sum that grows as the square root: 2^-24 * (400 / 2 / 3)^(1/2) = 2^-21 of the
+# result.  A logit of 8 that is off by a rounding or two moves dz by 2^-21 to 2^-20 of itself.
+
+
+@pytest.mark.parametrize("n,d,classes", [(64, 256, 1000), (512, 256, 1000), (1000, 512, 4000), (1024, 64, 20000), (777, 1160, 3001)])
+def test_dw_of_bf16_operands_keeps_three_values_of_dz(n, d, classes):
+    """Three values are within 2^-24 and leave the sums' own error; two are off by 2^-19.5 and more."""
+    x, w, labels = inputs(n, d, classes, 0)
+    _, dw = gradients(x, w, labels)
+    ref = dz_of(x, w, labels).T @ x.double()
+    assert (dw.double() - ref).norm() <= 2.0 ** -20 * ref.norm()
+
+
+@pytest.mark.parametrize("n,d,classes", [(4096, 256, 1000), (5001, 520, 4000)])
+def test_dw_of_many_rows_keeps_two_values_of_dz(n, d, classes):
+    """Two values are within 2^-16, and 2^-19 as errors at random; one is off by 2^-10."""
+    x, w, labels = inputs(n, d, classes, 0)
+    _, dw = gradients(x, w, labels)
+    ref = dz_of(x, w, labels).T @ x.double()
+    assert (dw.double() - ref).norm() <= 2.0 ** -18 * ref.norm()
+
+
+@pytest.mark.parametrize("n,d,classes", [(1024, 1024, 8192), (2048, 512, 20000), (1000, 515, 9001), (600, 512, 30000), (777, 1160, 5000)])
+def test_fp32_products_on_the_bf16_matrix_cores_keep_three_values(n, d, classes):
+    """Sizes of 128 x 128 tiles in all three products.  An fp32 value held as two bf16 values instead of three leaves 2^-17 of a sum (6.9e-6)."""
+    x, w, labels = inputs(n, d, classes, 0)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x = x.float() + 2.0 ** -9 * torch.rand(n, d, generator=g, device="cuda")       # (all 24 bits)
+    w = w.float() * (1 + 2.0 ** -9 * torch.rand(classes, d, generator=g, device="cuda"))
+    dx, dw = gradients(x, w, labels)
+    dz = dz_of(x, w, labels)
+    for got, ref in ((dx, dz @ w.double()), (dw, dz.T @ x.double())):
+        assert (got.double() - ref).norm() <= 2.0 ** -18 * ref.norm()
+
+
 @pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("n,d,classes", [(9, 64, 100), (300, 256, 1500), (1024, 512, 8192), (600, 512, 30000)])
