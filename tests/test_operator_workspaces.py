@@ -35,3 +35,22 @@ def test_group_norm_with_a_smaller_workspace_is_refused(n, hw, c, groups, dtype)
     assert size > 0
     for call in (gn_forward, gn_backward):
         assert call(n, hw, c, groups, size - 256, dtype) == B.ACC_EINVAL
+
+
+def ce_bytes(n, d, classes):
+    return L.acc_op_linear_ce_workspace(n, d, classes, 1, B.BF16)
+
+
+@pytest.mark.parametrize("n,d,classes,kept", [(1000, 1024, 1000, False), (64, 1024, 300, False), (41, 2048, 1000, False), (200, 1024, 3000, False),
+                                              (4096, 512, 16384, False), (777, 512, 50001, True), (6, 216, 49305, True), (16, 640, 100000, True),
+                                              (4096, 2048, 16384, True), (777, 1160, 50001, True)])
+def test_which_logits_the_linear_cross_entropy_keeps(n, d, classes, kept):
+    """Kept logits are the part of the workspace that a loss alone has no use for, beside dz as two or three bf16 values and sums."""
+    pitch = -(-classes // 64) * 64
+    parts = 3 if n < 4096 else 2
+    logits, dz = n * pitch * 4, parts * n * pitch * 2
+    # sums of dx and dw in up to 2^25 and 2^24 values, and of db
+    least = dz + n * d * 4
+    assert ce_bytes(n, d, classes) >= least + (logits if kept else 0)
+    if not kept:
+        assert ce_bytes(n, d, classes) - ce_bytes(n, d - 16, classes) < logits
