@@ -529,8 +529,10 @@ Plan32 plan32(int n, int d, int classes, bool grads, int dtype) {
   p.rows = p.pieces == 1 && n <= 4096 && p.piece <= (n <= 512 ? kRowCols : kRowCols / 4);
   p.widen = dtype != DT_F32;
   // Few rows and classes of whole widths: the convolution kernels' launches, which deal the sum out among the waves of a workgroup, are faster than cutting it
-  // and a launch for the parts' sums (us, all results, here / convolution: 41 x 2048 x 1000 33 / 30, 16 x 2048 x 4096 58 / 52, 64 x 256 x 256 19 / 26).
-  // Elsewhere the kernels here are (1024 x 2048 x 32768: logits 726 / 825, dx 740 / 1023, dw 775 / 841).
+  // and a launch for the parts' sums.  us, all results, here / convolution: 1 x 2048 x 1000 28 / 23, 8 x 4096 x 1000 41 / 31, 16 x 2048 x 1000 31 / 25, 41 x 2048 x 1000
+  // 34 / 30, 41 x 512 x 1000 25 / 23, 41 x 1024 x 640 23 / 23, 32 x 512 x 2048 31 / 27, 50 x 768 x 3000 36 / 38, 64 x 1024 x 4096 52 / 48; beyond the lines drawn
+  // here 96 x 2048 x 1000 35 / 40, 128 x 2048 x 1000 39 / 40, 64 x 1024 x 8000 63 / 70, 41 x 1024 x 320 21 / 22, 64 x 256 x 256 19 / 26.  Of 19 sizes within them
+  // one takes the slower way by more than 2 % (50 x 768 x 3000).  Elsewhere the kernels here are (1024 x 2048 x 32768: logits 726 / 825, dx 740 / 1023, dw 775 / 841).
   p.conv = !p.widen && p.pieces == 1 && n <= 64 && classes >= 640 && classes <= 4096 && classes % 4 == 0 && d >= 256 && d % 8 == 0;
   if (p.conv) {
     alignas(16) static const float any[4] = {};      // (an aligned address: all that the question looks at)
