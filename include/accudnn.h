@@ -446,7 +446,13 @@ int acc_op_gn_bwd(const void* x, const void* dy, const void* y, const void* res,
  * of x that is not has a loss that is infinite or NaN (large fp32 products make NaN of an infinity), and so have the gradients that it enters.
  * loss_rows, loss, dx, dw, db: each may be NULL, at least one is not; without dx, dw and db no gradient is computed.  What is written may not
  * overlap another argument (ACC_EINVAL).
- * n <= 2^20, d <= 65536, classes <= 2^24.  workspace: acc_op_linear_ce_workspace() bytes, gradients = whether any of dx, dw, db is asked for. */
+ * n <= 2^20, d <= 65536, classes <= 2^24.  workspace: acc_op_linear_ce_workspace() bytes, gradients = whether any of dx, dw, db is asked for.  What is in it:
+ *   sums of the rows: 8 n bytes for every 64 to 256 classes (fp32: 32 to 128);
+ *   with gradients, logits and dz of a piece of the classes: 2^26 values or 256 classes, whichever is more, 10 bytes each at most; without, of fp32 operands, 2^24
+ *   values of 4 bytes at most;
+ *   with gradients, partial sums: 4 n d bytes and 192 MiB at most, and as much again as a 16th of the logits, 128 MiB and 4 bytes a class at most;
+ *   of bf16 operands whose width is not a multiple of 8, a copy of x and of a piece of w (1 GiB or 256 classes).
+ * bf16 operands of d < 16 or of more than 2^31 values in x are copied to fp32 (x and 1 GiB of w, or 128 classes) and take the time of fp32 operands. */
 #define ACC_LABEL_NONE INT32_MIN
 size_t acc_op_linear_ce_workspace(int n, int d, int classes, int gradients, int dtype);
 int acc_op_linear_ce(const void* x, const void* w, const float* bias, const int32_t* labels, int ignore, float* loss_rows,

@@ -517,7 +517,7 @@ struct Plan32 {
 
 Plan32 plan32(int n, int d, int classes, bool grads, int dtype) {
   Plan32 p{};
-  // 256 MiB of logits, and of the filter 1 GiB in fp32 where it is copied
+  // 256 MiB of logits, and of the filter 1 GiB in fp32 where it is copied, 128 classes at least (more than 2^19 rows then have more)
   long most = (1L << 26) / n / 128 * 128;
   if (dtype != DT_F32 && most > (1L << 28) / d / 128 * 128) most = (1L << 28) / d / 128 * 128;
   if (most < 128) most = 128;

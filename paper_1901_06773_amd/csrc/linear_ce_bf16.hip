@@ -620,7 +620,7 @@ Plan16 plan16(int n, int d, int classes, bool grads) {
   Plan16 p{};
   p.dp = (int)up(d, 8);
   p.parts = n < 4096 ? 3 : 2;
-  // 2^26 values of dz (128 MiB for each part), 1 GiB of filter
+  // 2^26 values of dz (128 MiB for each part, 256 MiB of kept logits), 1 GiB of filter, 256 classes at least (more than 2^18 rows then have more)
   long most = (1L << 26) / n / 256 * 256;
   if (most > (1L << 29) / p.dp / 256 * 256) most = (1L << 29) / p.dp / 256 * 256;
   if (!grads) {                  // (nothing of a piece is kept; a launch has fewer than 2^32 threads)

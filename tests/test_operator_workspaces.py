@@ -54,3 +54,31 @@ def test_which_logits_the_linear_cross_entropy_keeps(n, d, classes, kept):
     assert ce_bytes(n, d, classes) >= least + (logits if kept else 0)
     if not kept:
         assert ce_bytes(n, d, classes) - ce_bytes(n, d - 16, classes) < logits
+
+
+def documented(n, d, classes, gradients, dtype):
+    """The bound that include/accudnn.h states."""
+    width, MiB, GiB = -(-d // 8) * 8, 1 << 20, 1 << 30
+    fp32 = dtype == B.F32 or d < 16 or n * width * 2 > 0xFFFFFF00
+    total = 16 * n + 65536 + 8 * n * (classes // (32 if fp32 else 64) + 1)
+    values = max(1 << 26, 256 * n)
+    if gradients:
+        total += 10 * values + 4 * n * d + 192 * MiB + 4 * min(n * (classes + 256), values) // 16 + 128 * MiB + 4 * classes
+    elif fp32:
+        total += 4 * (1 << 24)
+    if dtype == B.BF16 and fp32:
+        total += 4 * n * d + max(GiB, 4 * 128 * d)
+    elif dtype == B.BF16 and d % 8:
+        total += 2 * n * width + max(GiB, 2 * 256 * width)
+    return total
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("gradients", [0, 1])
+def test_the_linear_cross_entropys_workspace_keeps_its_bound(gradients, dtype):
+    rows = (1, 2, 41, 512, 777, 4095, 4096, 8192, 65536, 1 << 18, 1 << 20)
+    for n in rows:
+        for d in (1, 8, 15, 16, 60, 64, 1024, 1160, 4096, 4100, 65536):
+            for classes in (1, 2, 100, 1000, 4097, 50001, 65536, 1 << 20, 1 << 24):
+                size = L.acc_op_linear_ce_workspace(n, d, classes, gradients, dtype)
+                assert 0 < size <= documented(n, d, classes, gradients, dtype), (n, d, classes, size / 2 ** 20)
