@@ -42,7 +42,7 @@ def ce_bytes(n, d, classes):
 
 
 @pytest.mark.parametrize("n,d,classes,kept", [(1000, 1024, 1000, False), (64, 1024, 300, False), (41, 2048, 1000, False), (200, 1024, 3000, False),
-                                              (4096, 512, 16384, False), (777, 512, 50001, True), (6, 216, 49305, True), (16, 640, 100000, True),
+                                              (4096, 512, 16384, False), (65536, 1024, 1000, False), (131072, 512, 100, False), (777, 512, 50001, True), (6, 216, 49305, True), (16, 640, 100000, True),
                                               (4096, 2048, 16384, True), (777, 1160, 50001, True)])
 def test_which_logits_the_linear_cross_entropy_keeps(n, d, classes, kept):
     """Kept logits are the part of the workspace that a loss alone has no use for, beside dz as two or three bf16 values and sums."""
