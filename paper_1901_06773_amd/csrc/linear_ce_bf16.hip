@@ -644,12 +644,13 @@ Plan16 plan16(int n, int d, int classes, bool grads) {
   // (a row's sums are then read by every tile across)
   p.join = grads && p.together && p.zt == 64 && p.splits <= 16;
   // The last piece's logits are kept where working them out again takes longer than writing and reading them, by predicted times: a launch, of up to sixteen rows
-  // one behind the other, the columns' sums of sixteen rows each, which a thread adds up (66 ns each), and another launch for the rows' sums where dz would join them.  us, all results, worked out again / kept: 43 x 1064 x 10 21 / 28, 1000 x 1024 x 1000
-  // 42 / 51, 200 x 1024 x 3000 46 / 50, 4096 x 512 x 16384 565 / 619, 1 x 1024 x 1000 26 / 23, 6 x 216 x 49305 73 / 57, 777 x 512 x 50001 489 / 448, 4096 x 2048 x 16384
-  // 1394 / 1314, 65536 x 1024 x 1000 971 / 1186, 131072 x 512 x 100 506 / 889.  Of 140 sizes (up to 2^20 rows, widths 16 to 4096, 2 to 100000
-  // classes) four take the slower way by more than 5 %, 10 at most.
+  // one behind the other, the columns' sums of sixteen rows each, which a thread adds up (66 ns each), and another launch for the rows' sums where dz would
+  // join them.  us, all results, worked out again / kept: 43 x 1064 x 10 21 / 28, 1000 x 1024 x 1000 42 / 51, 200 x 1024 x 3000 46 / 50, 4096 x 512 x 16384
+  // 565 / 619, 65536 x 1024 x 1000 971 / 1186, 131072 x 512 x 100 506 / 889; 1 x 1024 x 1000 26 / 23, 6 x 216 x 49305 73 / 57, 777 x 512 x 50001 489 / 448,
+  // 4096 x 2048 x 16384 1394 / 1314.  Of 140 sizes (up to 2^20 rows, widths 16 to 4096, 2 to 100000 classes) four take the slower way by more than 5 %, 10 at most.
   const double again = tile_us(RowsByRows, p.zt == 256 ? 0 : p.zt == 128 ? 1 : 2, ceil_div(n, p.zt) * ceil_div(whole, p.zt), p.dp / 64.0);
-  p.keep = grads && again > 3.5 + 0.5 * (n < DZ_ROWS ? n : DZ_ROWS) + (double)n * p.pitch * 8 / 5e6 + 0.066 * (ceil_div(n, DZ_ROWS) - ceil_div(n, p.zt)) + (p.join ? 5.0 : 0.0);
+  const double kept = 3.5 + 0.5 * (n < DZ_ROWS ? n : DZ_ROWS) + (double)n * p.pitch * 8 / 5e6 + 0.066 * (ceil_div(n, DZ_ROWS) - ceil_div(n, p.zt)) + (p.join ? 5.0 : 0.0);
+  p.keep = grads && again > kept;
   if (p.keep) p.join = false;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t a = at; at += al256(bytes); return a; };

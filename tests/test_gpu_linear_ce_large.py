@@ -1,4 +1,5 @@
-"""Linear cross-entropy of more values than a launch has threads (2^32): 2^34 values of x and of its gradient.  Tolerances of test_gpu_linear_ce.py."""
+"""Linear cross-entropy of the most rows there may be, and of more values than a launch has threads (2^32): 2^34 values of x and of its gradient.  Tolerances of
+test_gpu_linear_ce.py; a sum over n rows is off by 2^-24 n^(1/2) more (roundings at random of partial sums that grow as the root)."""
 import pytest
 import torch
 
@@ -32,4 +33,18 @@ def test_a_gradient_of_more_values_than_a_launch_has_threads():
         assert (dx[part].double() - ref).norm() <= (2.0 ** -7 + T.TOL) * ref.norm()
     assert abs(float(loss) - float(rows.double().mean())) <= 1e-6
     del x, dx, ws
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype,d,classes", [("f32", 4, 300), ("bf16", 24, 700), ("bf16", 1032, 70)])
+def test_the_most_rows_that_are_taken(dtype, d, classes):
+    n = 1 << 20
+    torch.cuda.empty_cache()
+    x, w, b, labels = T.inputs(n, d, classes, dtype)
+    labels[::7] = -1
+    got, ref = T.call(x, w, b, labels, ignore=-1), T.reference(x, w, b, labels, ignore=-1)
+    for k, v in got.items():
+        tol = T.TOL + (2.0 ** -14 if k in ("dw", "db") else 0.0) + (2.0 ** -8 if k == "dx" and dtype == "bf16" else 0.0)
+        assert torch.isfinite(v).all() and (v.double() - ref[k]).norm() <= tol * ref[k].norm(), k
+    del got, ref, x
     torch.cuda.empty_cache()
