@@ -11,8 +11,9 @@
 // Small tiles multiply on the fp32 matrix cores (256 operations per cycle and compute unit; LDS traffic a tenth of that).  Large ones (SPLIT) write each
 // value to LDS as the sum of three bf16 values, which hold its 24 bits, and add the six products that matter on the bf16 matrix cores: a chunk of 128 x 128
 // takes them 1536 cycles in place of 4096, beside some 800 of splitting.  1024 x 2048 x 32768, us, all in fp32 / split: 1134 / 686 (200 TFLOP/s).
-// The three products left out are at most 2^-21 of the whole one together, 2.3e-8 of a sum of 2048 (whose fp32 roundings are 3.5e-7).  An infinity has no such sum (what is left of it is NaN, and so are its products), and of values
-// below 2^-110 the last parts fall under the smallest bf16 value: they are held to 2^-134, not to 24 bits.
+// The three products left out are at most 2^-21 of the whole one together, 2.3e-8 of a sum of 2048 (whose fp32 roundings are 3.5e-7).  An infinity has no such
+// sum (what is left of it is NaN, and so are its products), and of values below 2^-110 the last parts fall under the smallest bf16 value: they are held to
+// 2^-134, not to 24 bits.
 #pragma once
 #include <hip/hip_runtime.h>
 

@@ -23,7 +23,8 @@ struct Slice {
 //   backward, bf16, 56x56, 256 in 32                       30 / 27   32 / 33   32 / 35   34 / 48   57 / 53   61 / 62   116 / 104
 //   forward, fp32, 80x80, 128 in 16                        28 / 24   30 / 31   31 / 32   34 / 39   55 / 46   63 / 60   123 / 116
 //   forward, bf16, 80x80, 256 in 32                        30 / 30   32 / 33   33 / 34   36 / 40   59 / 44   69 / 62   129 / 123
-// Of 884 sizes timed both ways (40 to 2048 workgroups, maps of 48x48 to 96x96, both types) the way taken is more than 5 % behind the other in 88, 1.3 % on average.
+// Of 884 sizes timed both ways (40 to 2048 workgroups, maps of 48x48 to 96x96, both types) the way taken is more than 5 % behind the other in 88 (35 % at
+// most, bf16, 48x48 and 50x50 of 512 channels at 448 to 512 workgroups), 1.3 % on average.
 constexpr int kSliceGroups = 64, kSliceValues = 60000, kNarrowLeast = 176, kNarrowMost = 256;
 struct SliceCfg {
   Slice sl;

@@ -3,13 +3,14 @@
 //
 // dz is left without the factor 1 / rows (a label's value is then -1 where its probability is small, exact in bf16) as the sum of two or three
 // bf16 values, the first the nearest one, the next the nearest to what is left: one leaves a relative error of up to 2^-8, two of 2^-16, three of 2^-24.
-// dw, an fp32 result, is multiplied from all of them.  Two leave 1.2e-6 to 1.7e-6 of it, however many rows there are, where the roundings of a sum in fp32 grow with the
-// root of the rows (relative errors of dw, 1e-6, 64 / 512 / 1024 / 2048 / 4096 / 8192 / 16384 rows: fp32 throughout 0.2 / 0.4 / 0.6 / 0.8 / 1.15 / 1.6 / 2.3; three values
-// 0.1 / 0.25 / 0.3 / 0.4 / 0.6 / 0.3 / 0.4; 256 to 512 wide, 1000 to 4000 classes).  So from 4096 rows on, where two values are off by at most half as much again as fp32 sums, there
-// are two, and three below, where they would be off by two to eight times as much (4096 x 2048 x 65536, all results, two / three: 5.5 / 6.7 ms).  dx is multiplied from the first
-// two: one would do if its errors stayed beside the result's own rounding, but a row of dz sums to zero, so that what the classes' weights have in common cancels
-// in dx and its errors do not (relative error of dx, 300 x 128 x 10, weights with a common part of 10 and 30 times their spread: one value 0.012 and 0.038, two
-// 0.0017, which is the rounding of the result; 4096 x 2048 x 65536, all results, 4720 and 5525 us).  The factor is applied to the fp32 accumulators.
+// dw, an fp32 result, is multiplied from all of them.  Two leave 1.2e-6 to 1.7e-6 of it, however many rows there are, where the roundings of a sum in
+// fp32 grow with the root of the rows (relative errors of dw, 1e-6, 64 / 512 / 1024 / 2048 / 4096 / 8192 / 16384 rows: fp32 throughout 0.2 / 0.4 / 0.6 /
+// 0.8 / 1.15 / 1.6 / 2.3; three values 0.1 / 0.25 / 0.3 / 0.4 / 0.6 / 0.3 / 0.4; 256 to 512 wide, 1000 to 4000 classes).  So from 4096 rows on, where two
+// values are off by at most half as much again as fp32 sums, there are two, and three below, where they would be off by two to eight times as much
+// (4096 x 2048 x 65536, all results, two / three: 5.5 / 6.7 ms).  dx is multiplied from the first two: one would do if its errors stayed beside the result's
+// own rounding, but a row of dz sums to zero, so that what the classes' weights have in common cancels in dx and its errors do not (relative error of dx,
+// 300 x 128 x 10, weights with a common part of 10 and 30 times their spread: one value 0.012 and 0.038, two 0.0017, which is the rounding of the result;
+// 4096 x 2048 x 65536, all results, 4720 and 5525 us).  The factor is applied to the fp32 accumulators.
 #include "kernels.h"
 #include "dtype.h"
 #include "gemm_bf16.h"
