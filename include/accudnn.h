@@ -459,6 +459,28 @@ int acc_op_linear_ce(const void* x, const void* w, const float* bias, const int3
                      float* loss, void* dx, float* dw, float* db, int n, int d, int classes, void* workspace,
                      size_t workspace_bytes, int dtype, void* stream);
 
+/* Learning from a teacher: its top logits, which stand for all of them, and the loss of a student's logits against them.
+ * acc_op_top_logits: the k largest of each row of z [n][classes] (dtype) with their classes, largest first, of equal ones the lower class first; index
+ * [n][k] int32, top [n][k] fp32.  Both zeros are equal (and come out as 0); what is no number counts as larger than any number.  The same results every time.
+ * n <= 2^20, classes <= 2^20, k <= 1024, k <= classes, fewer than 2^22 workgroups (a row, or 2^16 fp32 or 2^17 bf16 logits of a longer one, each).
+ * workspace: acc_op_top_logits_workspace() bytes (0 for rows that need none, and for sizes that are refused).
+ * acc_op_distill: z [n][classes] the student's logits, index and top [n][k] the teacher's: classes and logits of a row in any order, ended by the first
+ * negative class (what stands behind it is not read for anything).  With p = softmax(top / T) over the row's list and q = softmax(z / T) over all classes
+ *   loss_rows = alpha T^2 sum_j p_j (log p_j - log q_j) + (1 - alpha) (logsumexp(z) - z[label]),  loss = mean over the rows that count,
+ *   dz = (alpha T (q - p) + (1 - alpha) (softmax(z) - onehot)) / rows that count.
+ * labels [n] int32 may be NULL, with alpha = 1 (the teacher alone); 0 < alpha <= 1, 0 < T < infinity.  With labels the rows whose label is not `ignore` count
+ * (ACC_LABEL_NONE: all), without them the rows whose list is not empty; others have loss 0 and gradient 0 whatever their z holds.  A row that counts and has no
+ * list has the label's term alone.  A class that is listed twice has the sum of its entries' probabilities in dz, and both entries in the loss.  A
+ * listed class beyond the last one makes the row's loss NaN and has no term in dz, and so does a label outside [0, classes) where alpha < 1.  Listed logits of minus infinity have probability 0; a
+ * row whose listed logits or whose z are all minus infinity, or contain infinity, has NaN in its loss and in dz (at the listed classes resp. at all).  loss_rows [n], loss [1], dz [n][classes] (dtype): each
+ * may be NULL, at least one is not; dz may be z, nothing else that is written may overlap another argument (ACC_EINVAL).  n, classes <= 2^20, k <= 1024.
+ * workspace: acc_op_distill_workspace() bytes (0: the sizes are refused); nothing in it needs to be kept or cleared.  No atomics: the same bits every time. */
+size_t acc_op_top_logits_workspace(int n, int classes, int k, int dtype);
+int acc_op_top_logits(const void* z, int32_t* index, float* top, int n, int classes, int k, void* workspace, size_t workspace_bytes, int dtype, void* stream);
+size_t acc_op_distill_workspace(int n, int classes, int k, int dtype);
+int acc_op_distill(const void* z, const int32_t* index, const float* top, const int32_t* labels, int ignore, float temperature, float alpha, float* loss_rows,
+                   float* loss, void* dz, int n, int classes, int k, void* workspace, size_t workspace_bytes, int dtype, void* stream);
+
 /* The Euclidean norm over all values of many tensors, and the tensors scaled so that it does not exceed a bound.  The list of
  * tensors is laid out once in the caller's device memory and used as often as wanted (the tensors' values may change, their
  * addresses and sizes not): acc_op_tensor_list() writes it in stream order, from kernel arguments, so it may be captured; the host arrays

@@ -171,6 +171,10 @@ _PROTOS = {
     "acc_op_gn_bwd": (_I, [_VP] * 12 + [_I] * 5 + [_VP, _SZ, _I, _VP]),
     "acc_op_linear_ce_workspace": (_SZ, [_I] * 5),
     "acc_op_linear_ce": (_I, [_VP] * 4 + [_I] + [_VP] * 5 + [_I] * 3 + [_VP, _SZ, _I, _VP]),
+    "acc_op_top_logits_workspace": (_SZ, [_I] * 4),
+    "acc_op_top_logits": (_I, [_VP] * 3 + [_I] * 3 + [_VP, _SZ, _I, _VP]),
+    "acc_op_distill_workspace": (_SZ, [_I] * 4),
+    "acc_op_distill": (_I, [_VP] * 4 + [_I, _F, _F] + [_VP] * 3 + [_I] * 3 + [_VP, _SZ, _I, _VP]),
     "acc_op_tensor_list_bytes": (_SZ, [C.POINTER(_SZ), _I]),
     "acc_op_tensor_list": (_I, [C.POINTER(_VP), C.POINTER(_VP), C.POINTER(_SZ), C.POINTER(C.c_int32), _I, _VP, _SZ, _VP]),
     "acc_op_grad_norm_workspace": (_SZ, []),
@@ -715,6 +719,44 @@ def op_linear_ce(x, w, bias, labels, loss_rows, loss, dx, dw, db, ws, ignore=Non
                                 _fits(name, "labels", labels, (n,), i32, device), LABEL_NONE if ignore is None else int(ignore),
                                 given("loss_rows", loss_rows, (n,), f32), given("loss", loss, (1,), f32), given("dx", dx, (n, d), kind),
                                 given("dw", dw, (classes, d), f32), given("db", db, (classes,), f32), n, d, classes, at, size, dtype, stream))
+
+
+def op_top_logits_workspace(n, classes, k, dtype: int = F32) -> int:
+    return int(_lib.acc_op_top_logits_workspace(n, classes, k, int(dtype)))
+
+
+def op_top_logits(z, index, top, ws):
+    """The k largest of each row of z [n, classes], largest first, equal ones by their class: index int32 [n, k], top fp32 [n, k].  ws may be None where
+    op_top_logits_workspace() is 0."""
+    torch, device, stream = _here()
+    name, kind, dtype = "op_top_logits", z.dtype, _dtype_of(z)
+    n, classes = z.shape
+    k = index.shape[-1]
+    at, size = (None, 0) if ws is None else _space(name, ws, device)
+    _done(_lib.acc_op_top_logits(_fits(name, "z", z, (n, classes), kind, device), _fits(name, "index", index, (n, k), torch.int32, device),
+                                 _fits(name, "top", top, (n, k), torch.float32, device), n, classes, k, at, size, dtype, stream))
+
+
+def op_distill_workspace(n, classes, k, dtype: int = F32) -> int:
+    return int(_lib.acc_op_distill_workspace(n, classes, k, int(dtype)))
+
+
+def op_distill(z, index, top, labels, loss_rows, loss, dz, temperature, alpha, ws, ignore=None):
+    """Distillation loss of the logits z [n, classes] against a teacher's top logits (index int32, top fp32, [n, k]; a list ends at its first negative class)
+    and, with the share 1 - alpha, labels int32 [n] (None: alpha is 1); loss_rows [n], loss [1] fp32 and dz like z (may be z), each optional.  ignore: the
+    label of rows that do not count (None: every row counts)."""
+    torch, device, stream = _here()
+    name, f32, i32, kind, dtype = "op_distill", torch.float32, torch.int32, z.dtype, _dtype_of(z)
+    n, classes = z.shape
+    k = index.shape[-1]
+
+    def given(what, t, shape, dt):
+        return None if t is None else _fits(name, what, t, shape, dt, device)
+    at, size = _space(name, ws, device)
+    _done(_lib.acc_op_distill(_fits(name, "z", z, (n, classes), kind, device), _fits(name, "index", index, (n, k), i32, device),
+                              _fits(name, "top", top, (n, k), f32, device), given("labels", labels, (n,), i32), LABEL_NONE if ignore is None else int(ignore),
+                              temperature, alpha, given("loss_rows", loss_rows, (n,), f32), given("loss", loss, (1,), f32),
+                              given("dz", dz, (n, classes), kind), n, classes, k, at, size, dtype, stream))
 
 
 class TensorList:

@@ -1,0 +1,519 @@
+// Distillation: the loss of a student's logits against a list of a teacher's largest ones, and its gradient.  Of row i, with the teacher's logits t_j of the
+// classes c_j of its list, temperature T and, where there are labels, their share:
+//
+//   p = softmax(t / T) over the list,  q = softmax(z / T) over all classes,  s = softmax(z)
+//   loss_i = alpha T^2 sum_j p_j (log p_j - log q_cj) + (1 - alpha) (lse(z) - z_label),   loss = mean over the rows that count
+//   dz = (alpha T (q - p) + (1 - alpha) (s - onehot)) / rows that count
+//
+// A row is read once, into the registers of a wave or a workgroup, and its gradient written from there: memory bounds it.  Rows that no registers hold, and
+// long ones where there are few, are cut: a launch leaves the sums of each part, the next joins them and writes the gradient.  One wave works out the list's
+// probabilities while the row is on its way; the few classes of the list (and the label) are written again, behind a barrier, with their own terms.
+//
+// Sums of exponentials go without the largest one, which is 1: with R the sum of the others', log(1 + R) and, of a class that both give more than a half,
+// q - p = (1 - p) - (1 - q) keep R where a class is all but certain.
+#include "kernels.h"
+#include "row_chunks.h"
+
+#include <climits>
+
+namespace acc {
+namespace {
+
+constexpr float LOG2E = 1.44269504088896341f;
+__device__ __forceinline__ float exp2_fast(float t) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_exp2f(t);
+#else
+  return t;
+#endif
+}
+
+struct DistillArgs {
+  const void* z;
+  const int32_t* index;
+  const float* top;
+  const int32_t* labels;       // null: the teacher alone
+  int ignore;
+  float inv_t, soft, hard, soft_slope;      // 1 / T, alpha T^2, 1 - alpha, alpha T
+  float *loss_rows, *loss;
+  void* dz;                    // null: the loss alone
+  int n, classes, k;
+  const int* counts;           // rows that count, in parts; null: counted here
+  int count_parts;
+  // cut rows
+  float *part, *at_list;       // part[row][4][splits]: the largest logit and R at both temperatures; at_list[row][k + 1]: logits of the list and of the label
+  int splits, chunks_per_split;
+};
+
+__device__ __forceinline__ bool row_counts(const DistillArgs& a, int row) {
+  return a.labels ? a.ignore == INT_MIN || a.labels[row] != a.ignore : a.index[(size_t)row * a.k] >= 0;
+}
+// Rows that count among all, by NT threads; sh: NT / 64 numbers
+template <int NT> __device__ __forceinline__ int counted(const DistillArgs& a, int* sh) {
+  int c = 0;
+  if (a.counts) {
+    for (int i = threadIdx.x % NT; i < a.count_parts; i += NT) c += a.counts[i];
+  } else {
+    for (int i = threadIdx.x % NT; i < a.n; i += NT) c += row_counts(a, i) ? 1 : 0;
+  }
+  return row_reduce<NT>(c, sh, [](int x, int y) { return x + y; });
+}
+
+// The list of a row, by one wave: probabilities and classes into LDS, and what the loss needs of them.
+struct List {
+  int length;                  // entries before the first negative class
+  float entropy;               // sum p log p
+  bool bad;                    // a class beyond the last one
+};
+__device__ __forceinline__ List read_list(const DistillArgs& a, int row, int32_t* cls, float* p, float* rest_of) {
+  const int lane = threadIdx.x & 63;
+  const int32_t* const index = a.index + (size_t)row * a.k;
+  const float* const top = a.top + (size_t)row * a.k;
+  List l{a.k, 0.f, false};
+  float mx = -INFINITY;
+  for (int j0 = 0; j0 < a.k; j0 += 64) {
+    const int j = j0 + lane, c = j < a.k ? index[j] : 0;
+    const float t = j < a.k ? top[j] : 0.f;
+    const unsigned long long ends = __ballot(j < a.k && c < 0);
+    if (ends) l.length = j0 + __ffsll(ends) - 1;
+    if (j < l.length) {
+      cls[j] = c;
+      p[j] = t;
+      mx = fmaxf(mx, t);
+      l.bad |= c >= a.classes;
+    }
+    if (ends) break;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+  l.bad = __any(l.bad);
+  float s = 0.f, equal = 0.f;
+  for (int j = lane; j < l.length; j += 64) {
+    const float t = p[j];
+    const bool is_top = t == mx;
+    equal += is_top ? 1.f : 0.f;
+    s += is_top ? 0.f : expf((t - mx) * a.inv_t);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) { s += __shfl_xor(s, o); equal += __shfl_xor(equal, o); }
+  const float rest = fabsf(mx) == INFINITY ? NAN : s + (equal - 1.f), inv = 1.f / (1.f + rest), log_sum = log1pf(rest);
+  float h = 0.f;
+  for (int j = lane; j < l.length; j += 64) {
+    const float v = (p[j] - mx) * a.inv_t, e = expf(v);
+    p[j] = e * inv;
+    rest_of[j] = (rest - expm1f(v)) * inv;             // 1 - p
+    h += e == 0.f ? 0.f : e * inv * (v - log_sum);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) h += __shfl_xor(h, o);
+  l.entropy = h;
+  return l;
+}
+
+// What a row's sums come to
+struct RowSums {
+  float max, rest, rest1;      // the largest logit; R at the temperature and at 1
+};
+// The loss of a row, by one wave; z_of: the logits of the list's classes
+__device__ __forceinline__ float loss_of(const DistillArgs& a, const List& l, const RowSums& r, const float* p, const float* z_of, int label, float z_label) {
+  const int lane = threadIdx.x & 63;
+  float loss = 0.f;
+  if (l.length) {
+    float d = 0.f;
+    for (int j = lane; j < l.length; j += 64) d += p[j] == 0.f ? 0.f : p[j] * ((z_of[j] - r.max) * a.inv_t);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) d += __shfl_xor(d, o);
+    loss = a.soft * (l.entropy - d + log1pf(r.rest));
+    if (l.bad) loss = NAN;
+  }
+  if (a.hard > 0.f) loss += (unsigned)label < (unsigned)a.classes ? a.hard * (log1pf(r.rest1) - (z_label - r.max)) : NAN;
+  return loss;
+}
+
+// What the gradient of any class is made of
+struct Slope {
+  float inv_t2, soft, hard, max;      // log2 e / T; alpha T / rows / (1 + R), 0 without a list; (1 - alpha) / rows / (1 + R1)
+  template <bool HARD> __device__ __forceinline__ float of(float z) const {
+    const float d = z - max;
+    float v = exp2_fast(d * inv_t2) * soft;
+    if (HARD) v += exp2_fast(d * LOG2E) * hard;
+    return v;
+  }
+};
+__device__ __forceinline__ Slope slope_of(const DistillArgs& a, const RowSums& r, int length, float inv_rows) {
+  return Slope{a.inv_t * LOG2E, length ? a.soft_slope * inv_rows / (1.f + r.rest) : 0.f, a.hard * inv_rows / (1.f + r.rest1), r.max};
+}
+
+// The gradient of the classes [lo, hi) that are in the list, and of the label, by NT threads: their own terms.
+template <class T, int NT, bool HARD>
+__device__ __forceinline__ void write_listed(const DistillArgs& a, T* dz, int lo, int hi, int length, const int32_t* cls, const float* p, const float* rest_of,
+                                             const float* z_of, const RowSums& r, int label, float z_label, float inv_rows) {
+  const float inv = 1.f / (1.f + r.rest), inv1 = 1.f / (1.f + r.rest1);
+  for (int j = threadIdx.x % NT; j <= length; j += NT) {
+    const int c = j < length ? cls[j] : label;
+    if (j == length && (!HARD || (unsigned)label >= (unsigned)a.classes)) continue;
+    if (c < lo || c >= hi) continue;
+    // a class that is listed more than once has all of its entries' probabilities, by the first one
+    float sum = j < length ? p[j] : 0.f;
+    int times = 1;
+    bool first = true;
+    for (int i = 0; i < length; ++i) {
+      const bool same = cls[i] == c;
+      first = first && !(same && i < j);
+      if (same && i > j) { sum += p[i]; ++times; }
+    }
+    if (!first) continue;
+    const float z = j < length ? z_of[j] : z_label, d = z - r.max;
+    float v = 0.f;
+    if (length) {
+      const float u = d * a.inv_t, q = expf(u) * inv;
+      const float diff = j < length && times == 1 && q > 0.5f && sum > 0.5f ? rest_of[j] - (r.rest - expm1f(u)) * inv : q - sum;
+      v = a.soft_slope * diff;
+    }
+    if (HARD) v += a.hard * (c == label ? (expm1f(d) - r.rest1) * inv1 : expf(d) * inv1);
+    Elem<T>::store(dz + c, v * inv_rows);
+  }
+}
+
+// sums of a thread's chunks about the row's largest logit
+template <bool HARD, class Row>
+__device__ __forceinline__ void add_chunk(const chunk16& q, float max, float inv_t2, bool careful, float& s, float& s1, float& equal) {
+#pragma unroll
+  for (int e = 0; e < Row::PER; ++e) {
+    const float v = Row::value(q, e), d = v - max;
+    const float x = exp2_fast(d * inv_t2), x1 = HARD ? exp2_fast(d * LOG2E) : 0.f;
+    if (careful && v == max) equal += 1.f;
+    else { s += x; s1 += x1; }
+  }
+}
+
+// A row by NT threads, CH chunks each.  lists: 4 k words of LDS.
+template <class T, int NT, int CH, bool HARD>
+__device__ __forceinline__ void distill_row(const DistillArgs& a, int row, float inv_rows, float* lists, float (*sh)[NT / 64]) {
+  typedef RowChunks<T> Row;
+  const int tid = threadIdx.x % NT;
+  const T* const z = static_cast<const T*>(a.z) + (size_t)row * a.classes;
+  T* const dz = a.dz ? static_cast<T*>(a.dz) + (size_t)row * a.classes : nullptr;
+  const Row r(z, a.classes);
+  if (!row_counts(a, row)) {
+    if (tid == 0) a.loss_rows[row] = 0.f;
+    if (dz)
+#pragma unroll
+      for (int u = 0; u < CH; ++u)
+        if (tid + u * NT < r.chunks) r.store(dz, tid + u * NT, chunk16{0, 0, 0, 0});
+    return;
+  }
+  chunk16 q[CH];
+#pragma unroll
+  for (int u = 0; u < CH; ++u)
+    if (tid + u * NT < r.chunks) q[u] = r.load(z, tid + u * NT);
+  int32_t* const cls = reinterpret_cast<int32_t*>(lists);
+  float *const p = lists + a.k, *const rest_of = lists + 2 * a.k, *const z_of = lists + 3 * a.k;
+  const int label = HARD ? a.labels[row] : -1;
+  float z_label = 0.f;
+  if (HARD && (unsigned)label < (unsigned)a.classes) z_label = Elem<T>::load(z + label);
+  List l{};
+  if (tid < 64) {
+    l = read_list(a, row, cls, p, rest_of);
+    for (int j = tid; j < l.length; j += 64) z_of[j] = cls[j] < a.classes ? Elem<T>::load(z + cls[j]) : NAN;
+  }
+  float own = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < CH; ++u)
+    if (tid + u * NT < r.chunks) {
+#pragma unroll
+      for (int e = 0; e < Row::PER; ++e) own = fmaxf(own, Row::value(q[u], e));
+    }
+  RowSums t;
+  t.max = row_reduce<NT>(own, sh[0], [](float x, float y) { return fmaxf(x, y); });
+  const float inv_t2 = a.inv_t * LOG2E;
+  float s = 0.f, s1 = 0.f, equal = 0.f;
+  if (own == t.max) {
+#pragma unroll
+    for (int u = 0; u < CH; ++u)
+      if (tid + u * NT < r.chunks) add_chunk<HARD, Row>(q[u], t.max, inv_t2, true, s, s1, equal);
+  } else {
+#pragma unroll
+    for (int u = 0; u < CH; ++u)
+      if (tid + u * NT < r.chunks) add_chunk<HARD, Row>(q[u], t.max, inv_t2, false, s, s1, equal);
+  }
+  auto add = [](float x, float y) { return x + y; };
+  if (NT > 64 && tid == 0) sh[4][0] = __int_as_float(l.length);
+  s = row_reduce<NT>(s, sh[1], add);
+  equal = row_reduce<NT>(equal, sh[2], add);
+  if (HARD) s1 = row_reduce<NT>(s1, sh[3], add);
+  const bool none = fabsf(t.max) == INFINITY;          // no distribution
+  t.rest = none ? NAN : s + (equal - 1.f);
+  t.rest1 = none ? NAN : s1 + (equal - 1.f);
+  const int length = NT > 64 ? __float_as_int(sh[4][0]) : l.length;
+  if (tid < 64) {
+    const float loss = loss_of(a, l, t, p, z_of, label, z_label);
+    if (tid == 0) a.loss_rows[row] = loss;
+  }
+  if (!dz) return;
+  const Slope g = slope_of(a, t, length, inv_rows);
+#pragma unroll
+  for (int u = 0; u < CH; ++u)
+    if (tid + u * NT < r.chunks) {
+      float v[Row::PER];
+#pragma unroll
+      for (int e = 0; e < Row::PER; ++e) v[e] = g.template of<HARD>(Row::value(q[u], e));
+      r.store(dz, tid + u * NT, Row::pack(v));
+    }
+  row_sync<NT>();
+  write_listed<T, NT, HARD>(a, dz, 0, a.classes, length, cls, p, rest_of, z_of, t, label, z_label, inv_rows);
+}
+
+// loss = sum of loss_rows / rows that count, NT threads, fixed order
+template <int NT> __device__ __forceinline__ void mean_loss(const DistillArgs& a, int rows) {
+  __shared__ double sh[NT / 64];
+  double s = 0.0;
+  for (int i = threadIdx.x; i < a.n; i += NT) s += (double)a.loss_rows[i];
+  s = row_reduce<NT>(s, sh, [](double x, double y) { return x + y; });
+  if (threadIdx.x == 0) *a.loss = rows ? (float)(s / (double)rows) : 0.f;
+}
+
+template <class T, int NT, int CH, bool HARD>
+__global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a) {
+  extern __shared__ float lists[];
+  __shared__ float sh[5][NT / 64];
+  __shared__ int shc[NT / 64];
+  const int rows = a.dz ? counted<NT>(a, shc) : 1;
+  distill_row<T, NT, CH, HARD>(a, blockIdx.x, rows ? 1.f / (float)rows : 0.f, lists, sh);
+}
+
+// A wave per row; with one workgroup the mean, too
+template <class T, int CH, bool HARD>
+__global__ __launch_bounds__(1024) void distill_waves_kernel(DistillArgs a, int threads) {
+  extern __shared__ float lists[];
+  __shared__ float sh[16][5][1];
+  __shared__ int total;
+  const int wave = threadIdx.x >> 6, waves = threads >> 6;
+  if (wave == 0) {
+    const int c = counted<64>(a, nullptr);
+    if (threadIdx.x == 0) total = c;
+  }
+  __syncthreads();
+  const int rows = total;
+  for (int row = (int)blockIdx.x * waves + wave; row < a.n; row += (int)gridDim.x * waves) {
+    distill_row<T, 64, CH, HARD>(a, row, rows ? 1.f / (float)rows : 0.f, lists + (size_t)wave * 4 * a.k, sh[wave]);
+    row_sync<64>();
+  }
+  if (gridDim.x > 1 || !a.loss) return;
+  __threadfence_block();
+  __syncthreads();
+  if (threads == 1024) mean_loss<1024>(a, rows);
+}
+
+// Cut rows: the sums of a part
+template <class T, bool HARD>
+__global__ __launch_bounds__(256) void distill_part_kernel(DistillArgs a) {
+  typedef RowChunks<T> Row;
+  __shared__ float sh[5][4];
+  const int row = (int)blockIdx.x / a.splits, sp = (int)blockIdx.x - row * a.splits, tid = threadIdx.x;
+  const T* const z = static_cast<const T*>(a.z) + (size_t)row * a.classes;
+  if (!row_counts(a, row)) return;
+  const Row r(z, a.classes);
+  const int c0 = sp * a.chunks_per_split, c1 = min(c0 + a.chunks_per_split, r.chunks);
+  if (sp == 0) {
+    float* const at = a.at_list + (size_t)row * (a.k + 1);
+    for (int j = tid; j < a.k; j += 256) {
+      const int c = a.index[(size_t)row * a.k + j];
+      at[j] = (unsigned)c < (unsigned)a.classes ? Elem<T>::load(z + c) : NAN;
+    }
+    if (HARD && tid == 0) at[a.k] = (unsigned)a.labels[row] < (unsigned)a.classes ? Elem<T>::load(z + a.labels[row]) : NAN;
+  }
+  float own = -INFINITY, s = 0.f, s1 = 0.f, equal = 0.f;
+  const float inv_t2 = a.inv_t * LOG2E;
+  for (int c = c0 + tid; c < c1; c += 256) {
+    const chunk16 q = r.load(z, c);
+#pragma unroll
+    for (int e = 0; e < Row::PER; ++e) own = fmaxf(own, Row::value(q, e));
+  }
+  const float mx = row_reduce<256>(own, sh[0], [](float x, float y) { return fmaxf(x, y); });
+  for (int c = c0 + tid; c < c1; c += 256) add_chunk<HARD, Row>(r.load(z, c), mx, inv_t2, own == mx, s, s1, equal);
+  auto add = [](float x, float y) { return x + y; };
+  s = row_reduce<256>(s, sh[1], add);
+  equal = row_reduce<256>(equal, sh[2], add);
+  if (HARD) s1 = row_reduce<256>(s1, sh[3], add);
+  if (tid == 0) {
+    float* const p = a.part + (size_t)row * 4 * a.splits + sp;
+    const bool none = mx == -INFINITY && !(s != s);    // (nothing but minus infinity: the other parts decide)
+    p[0] = mx;
+    p[a.splits] = none ? -1.f : s + (equal - 1.f);
+    p[2 * a.splits] = none ? -1.f : s1 + (equal - 1.f);
+  }
+}
+
+// Cut rows: the parts joined (64 at most), the loss by the first workgroup, a part of the gradient by each
+template <class T, bool HARD>
+__global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a) {
+  typedef RowChunks<T> Row;
+  extern __shared__ float lists[];
+  __shared__ int shc[4];
+  __shared__ int length_of;
+  const int row = (int)blockIdx.x / a.splits, sp = (int)blockIdx.x - row * a.splits, tid = threadIdx.x, lane = tid & 63;
+  const int rows = counted<256>(a, shc);
+  const float inv_rows = rows ? 1.f / (float)rows : 0.f;
+  const T* const z = static_cast<const T*>(a.z) + (size_t)row * a.classes;
+  T* const dz = a.dz ? static_cast<T*>(a.dz) + (size_t)row * a.classes : nullptr;
+  const Row r(z, a.classes);
+  const int c0 = sp * a.chunks_per_split, c1 = min(c0 + a.chunks_per_split, r.chunks);
+  if (!row_counts(a, row)) {
+    if (tid == 0 && sp == 0) a.loss_rows[row] = 0.f;
+    if (dz)
+      for (int c = c0 + tid; c < c1; c += 256) r.store(dz, c, chunk16{0, 0, 0, 0});
+    return;
+  }
+  const float* const at = a.part + (size_t)row * 4 * a.splits;
+  const bool mine = lane < a.splits;
+  const float m = mine ? at[lane] : -INFINITY, rest = mine ? at[a.splits + lane] : -1.f, rest1 = mine ? at[2 * a.splits + lane] : -1.f;
+  RowSums t;
+  t.max = row_reduce<64>(m, (float*)nullptr, [](float x, float y) { return fmaxf(x, y); });
+  const bool top = mine && m == t.max;
+  float s = top ? rest : (1.f + rest) * exp2_fast((m - t.max) * (a.inv_t * LOG2E)), s1 = top ? rest1 : (1.f + rest1) * exp2_fast((m - t.max) * LOG2E);
+  if (!mine) s = s1 = 0.f;
+  auto add = [](float x, float y) { return x + y; };
+  const float equal = row_reduce<64>(top ? 1.f : 0.f, (float*)nullptr, add);
+  s = row_reduce<64>(s, (float*)nullptr, add);
+  s1 = row_reduce<64>(s1, (float*)nullptr, add);
+  const bool none = fabsf(t.max) == INFINITY;
+  t.rest = none ? NAN : s + (equal - 1.f);
+  t.rest1 = none ? NAN : s1 + (equal - 1.f);
+  int32_t* const cls = reinterpret_cast<int32_t*>(lists);
+  float *const p = lists + a.k, *const rest_of = lists + 2 * a.k, *const z_of = lists + 3 * a.k;
+  const float* const kept = a.at_list + (size_t)row * (a.k + 1);
+  const int label = HARD ? a.labels[row] : -1;
+  const float z_label = HARD ? kept[a.k] : 0.f;
+  if (tid < 64) {
+    const List l = read_list(a, row, cls, p, rest_of);
+    for (int j = tid; j < l.length; j += 64) z_of[j] = kept[j];
+    if (tid == 0) length_of = l.length;
+    if (sp == 0) {
+      row_sync<64>();
+      const float loss = loss_of(a, l, t, p, z_of, label, z_label);
+      if (tid == 0) a.loss_rows[row] = loss;
+    }
+  }
+  if (!dz) return;
+  __syncthreads();
+  const Slope g = slope_of(a, t, length_of, inv_rows);
+  for (int c = c0 + tid; c < c1; c += 256) {
+    const chunk16 q = r.load(z, c);
+    float v[Row::PER];
+#pragma unroll
+    for (int e = 0; e < Row::PER; ++e) v[e] = g.template of<HARD>(Row::value(q, e));
+    r.store(dz, c, Row::pack(v));
+  }
+  __syncthreads();
+  write_listed<T, 256, HARD>(a, dz, r.at(c0), c1 < r.chunks ? r.at(c1) : a.classes, length_of, cls, p, rest_of, z_of, t, label, z_label, inv_rows);
+}
+
+__global__ __launch_bounds__(1024) void distill_mean_kernel(DistillArgs a) {
+  __shared__ int sh[16];
+  mean_loss<1024>(a, counted<1024>(a, sh));
+}
+// rows that count, 4096 rows to a workgroup
+__global__ __launch_bounds__(256) void distill_count_kernel(DistillArgs a, int* counts) {
+  __shared__ int sh[4];
+  int c = 0;
+  const int first = (int)blockIdx.x * 4096, end = min(first + 4096, a.n);
+  for (int i = first + (int)threadIdx.x; i < end; i += 256) c += row_counts(a, i) ? 1 : 0;
+  c = row_reduce<256>(c, sh, [](int x, int y) { return x + y; });
+  if (threadIdx.x == 0) counts[blockIdx.x] = c;
+}
+
+inline size_t al256(size_t b) { return (b + 255) & ~(size_t)255; }
+inline long ceil_div(long a, long b) { return (a + b - 1) / b; }
+
+constexpr int kMostTop = 1024, kMostClasses = 1 << 20, kMostRows = 1 << 20;
+
+struct DistillPlan {
+  bool waves;                  // a wave per row
+  bool one;                    // in one workgroup, with the mean
+  int splits, chunks_per_split;      // 1: a workgroup per row
+  int chunks, count_parts;     // count_parts 0: every workgroup counts the rows
+  size_t rows, counts, part, at_list, total;
+};
+DistillPlan distill_plan(int n, int classes, int k, int dtype) {
+  DistillPlan p{};
+  const int per = dtype == DT_BF16 ? 8 : 4;
+  p.chunks = (classes + per - 1) / per + 1;            // (a row may begin inside one)
+  p.waves = p.chunks <= 64 * 4;
+  p.one = p.waves && n <= 64 && k <= 128;
+  p.splits = 1;
+  if (p.chunks > 1024 * 16) {
+    p.splits = (int)ceil_div(p.chunks, 4112);          // 64 KiB to a part: 64 parts at most
+    p.chunks_per_split = (int)ceil_div(p.chunks, p.splits);
+  }
+  p.count_parts = n > 1024 ? (int)ceil_div(n, 4096) : 0;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t a = at; at += al256(bytes); return a; };
+  p.rows = take((size_t)n * 4);
+  p.counts = take((size_t)p.count_parts * 4);
+  p.part = take(p.splits > 1 ? (size_t)n * 4 * p.splits * 4 : 0);
+  p.at_list = take(p.splits > 1 ? (size_t)n * (k + 1) * 4 : 0);
+  p.total = at;
+  return p;
+}
+bool distill_ok(int n, int classes, int k, int dtype) {
+  return n > 0 && classes > 0 && k > 0 && n <= kMostRows && classes <= kMostClasses && k <= kMostTop && (dtype == DT_F32 || dtype == DT_BF16) &&
+         (long)n * distill_plan(n, classes, k, dtype).splits < 1L << 22;       // (a launch has fewer than 2^32 threads)
+}
+
+template <class T, bool HARD> hipError_t launch_distill(const DistillArgs& a, const DistillPlan& p, hipStream_t st) {
+  const size_t lists = (size_t)4 * a.k * 4;
+  if (p.splits > 1) {
+    const dim3 grid((unsigned)(a.n * p.splits));
+    hipLaunchKernelGGL((distill_part_kernel<T, HARD>), grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL((distill_join_kernel<T, HARD>), grid, dim3(256), lists, st, a);
+  } else if (p.waves) {
+    const int threads = p.one ? 1024 : 128;
+    const dim3 grid(p.one ? 1u : (unsigned)ceil_div(a.n, threads / 64));
+#define ACC_WAVES(CH) hipLaunchKernelGGL((distill_waves_kernel<T, CH, HARD>), grid, dim3(threads), lists * (threads / 64), st, a, threads)
+    if (p.chunks <= 64) ACC_WAVES(1);
+    else if (p.chunks <= 128) ACC_WAVES(2);
+    else ACC_WAVES(4);
+#undef ACC_WAVES
+  } else {
+#define ACC_ROWS(NT, CH) if (p.chunks <= NT * CH) { hipLaunchKernelGGL((distill_rows_kernel<T, NT, CH, HARD>), dim3((unsigned)a.n), dim3(NT), lists, st, a); break; }
+    do {
+      ACC_ROWS(256, 2) ACC_ROWS(256, 4) ACC_ROWS(256, 8) ACC_ROWS(256, 16) ACC_ROWS(512, 16) ACC_ROWS(1024, 16)
+    } while (false);
+#undef ACC_ROWS
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t distill_workspace_bytes(int n, int classes, int k, int dtype) { return distill_ok(n, classes, k, dtype) ? distill_plan(n, classes, k, dtype).total : 0; }
+
+hipError_t distill(const void* z, const int32_t* index, const float* top, const int32_t* labels, int ignore, float temperature, float alpha, float* loss_rows,
+                   float* loss, void* dz, int n, int classes, int k, void* workspace, size_t workspace_bytes, int dtype, hipStream_t st) {
+  if (!z || !index || !top || !workspace || !(loss_rows || loss || dz) || !distill_ok(n, classes, k, dtype)) return hipErrorInvalidValue;
+  if (!(temperature > 0.f) || temperature == INFINITY || !(alpha > 0.f && alpha <= 1.f) || (!labels && alpha != 1.f)) return hipErrorInvalidValue;
+  const DistillPlan p = distill_plan(n, classes, k, dtype);
+  if (workspace_bytes < p.total) return hipErrorInvalidValue;
+  char* const ws = (char*)workspace;
+  DistillArgs a{};
+  a.z = z; a.index = index; a.top = top; a.labels = labels; a.ignore = ignore;
+  a.inv_t = 1.f / temperature; a.soft = alpha * temperature * temperature; a.hard = 1.f - alpha; a.soft_slope = alpha * temperature;
+  a.loss_rows = loss_rows ? loss_rows : (float*)(ws + p.rows);
+  a.loss = loss; a.dz = dz; a.n = n; a.classes = classes; a.k = k;
+  a.part = (float*)(ws + p.part); a.at_list = (float*)(ws + p.at_list); a.splits = p.splits; a.chunks_per_split = p.chunks_per_split;
+  if (p.count_parts && (dz || loss)) {
+    int* const counts = (int*)(ws + p.counts);
+    hipLaunchKernelGGL(distill_count_kernel, dim3((unsigned)p.count_parts), dim3(256), 0, st, a, counts);
+    a.counts = counts; a.count_parts = p.count_parts;
+  }
+  const bool hard = alpha < 1.f;
+  hipError_t e;
+  if (dtype == DT_BF16) e = hard ? launch_distill<bf16_t, true>(a, p, st) : launch_distill<bf16_t, false>(a, p, st);
+  else e = hard ? launch_distill<float, true>(a, p, st) : launch_distill<float, false>(a, p, st);
+  if (e != hipSuccess || !loss || p.one) return e;
+  hipLaunchKernelGGL(distill_mean_kernel, dim3(1), dim3(1024), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace acc

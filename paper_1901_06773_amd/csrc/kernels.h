@@ -265,6 +265,15 @@ size_t linear_ce_workspace_bytes(int n, int d, int classes, int gradients, int d
 hipError_t linear_ce(const void* x, const void* w, const float* bias, const int32_t* labels, int ignore, float* loss_rows,
                      float* loss, void* dx, float* dw, float* db, int n, int d, int classes, void* workspace,
                      size_t workspace_bytes, int dtype, hipStream_t st);
+// The k largest logits of each row with their classes (top_logits.hip).
+size_t top_logits_workspace_bytes(int n, int classes, int k, int dtype);
+hipError_t top_logits(const void* z, int32_t* index, float* top, int n, int classes, int k, void* workspace, size_t workspace_bytes, int dtype,
+                      hipStream_t st);
+// Loss against a teacher's top logits and its gradient (distill.hip); labels, loss_rows, loss and dz may each be null.
+size_t distill_workspace_bytes(int n, int classes, int k, int dtype);
+hipError_t distill(const void* z, const int32_t* index, const float* top, const int32_t* labels, int ignore, float temperature, float alpha,
+                   float* loss_rows, float* loss, void* dz, int n, int classes, int k, void* workspace, size_t workspace_bytes, int dtype,
+                   hipStream_t st);
 // A list of tensors in device memory, cut into pieces, and the norm over all of them (grad_clip.hip).  dst may be null (in place).
 constexpr int kPieceValues = 16384;
 size_t tensor_list_bytes(const size_t* counts, int n);

@@ -294,6 +294,43 @@ extern "C" int acc_op_linear_ce(const void* x, const void* w, const float* bias,
               "acc_op_linear_ce_workspace()");
 }
 
+extern "C" size_t acc_op_top_logits_workspace(int n, int classes, int k, int dtype) { return top_logits_workspace_bytes(n, classes, k, dtype); }
+
+extern "C" int acc_op_top_logits(const void* z, int32_t* index, float* top, int n, int classes, int k, void* workspace, size_t workspace_bytes, int dtype,
+                                 void* stream) {
+  if (!dtype_ok(dtype)) return refuse("acc_op_top_logits: dtype must be ACC_F32 or ACC_BF16");
+  if (!al16({z, index, top, workspace})) return refuse("acc_op_top_logits: pointers must be 16-byte aligned");
+  if (sizes_ok(n, classes, 1) && k > 0) {
+    const size_t list = (size_t)n * k * 4;
+    if (clash({{index, list, {}}, {top, list, {}}, {workspace, workspace_bytes, {}}}, {{z, (size_t)n * classes * dt_size(dtype), {}}}))
+      return refuse("acc_op_top_logits: what is written overlaps another argument");
+  }
+  return told(top_logits(z, index, top, n, classes, k, workspace, workspace_bytes, dtype, (hipStream_t)stream),
+              "acc_op_top_logits: null pointer, sizes that are not positive or too large, more entries than classes or a workspace smaller than "
+              "acc_op_top_logits_workspace()");
+}
+
+extern "C" size_t acc_op_distill_workspace(int n, int classes, int k, int dtype) { return distill_workspace_bytes(n, classes, k, dtype); }
+
+extern "C" int acc_op_distill(const void* z, const int32_t* index, const float* top, const int32_t* labels, int ignore, float temperature, float alpha,
+                              float* loss_rows, float* loss, void* dz, int n, int classes, int k, void* workspace, size_t workspace_bytes, int dtype,
+                              void* stream) {
+  if (!dtype_ok(dtype)) return refuse("acc_op_distill: dtype must be ACC_F32 or ACC_BF16");
+  if (!al16({z, index, top, labels, loss_rows, loss, dz, workspace})) return refuse("acc_op_distill: pointers must be 16-byte aligned");
+  if (!(temperature > 0.f) || std::isinf(temperature)) return refuse("acc_op_distill: the temperature must be positive and finite");
+  if (!(alpha > 0.f && alpha <= 1.f) || (!labels && alpha != 1.f)) return refuse("acc_op_distill: alpha must lie in (0, 1], and be 1 without labels");
+  if (sizes_ok(n, classes, 1) && k > 0) {
+    const size_t list = (size_t)n * k * 4, rows = (size_t)n * 4, map = (size_t)n * classes * dt_size(dtype);
+    if (clash({{loss_rows, rows, {}}, {loss, 4, {}}, {dz, map, {z}}, {workspace, workspace_bytes, {}}},
+              {{z, map, {}}, {index, list, {}}, {top, list, {}}, {labels, rows, {}}}))
+      return refuse("acc_op_distill: what is written overlaps another argument (dz may be z)");
+  }
+  return told(distill(z, index, top, labels, ignore, temperature, alpha, loss_rows, loss, dz, n, classes, k, workspace, workspace_bytes, dtype,
+                      (hipStream_t)stream),
+              "acc_op_distill: null pointer, no result asked for, sizes that are not positive or too large, or a workspace smaller than "
+              "acc_op_distill_workspace()");
+}
+
 extern "C" size_t acc_op_tensor_list_bytes(const size_t* counts, int n) {
   if (!counts || n <= 0) return 0;
   const size_t b = tensor_list_bytes(counts, n);

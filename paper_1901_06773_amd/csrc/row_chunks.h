@@ -1,0 +1,92 @@
+// A row of values that a workgroup (or a wave) keeps in its registers, sixteen bytes of it at a time.
+//
+// Rows of an odd number of values begin at any address that their type allows.  A row is cut at multiples of sixteen bytes of memory, not of the row, so
+// that every whole chunk is one aligned load or store; the first and the last chunk may hold values of the neighbouring rows, which are neither read
+// nor written: those two go value by value.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "dtype.h"
+
+namespace acc {
+
+typedef unsigned chunk16 __attribute__((ext_vector_type(4)));
+
+template <class T> struct RowChunks {
+  static constexpr int PER = 16 / (int)sizeof(T);      // values of a chunk
+  long first;          // the value of the row that chunk 0 begins with: 0, or up to PER - 1 before it
+  int count, chunks;
+  __host__ __device__ __forceinline__ RowChunks(const T* row, int count_) : count(count_) {
+    const int before = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+    first = -before;
+    chunks = (before + count + PER - 1) / PER;
+  }
+  __device__ __forceinline__ int at(int c) const { return c * PER + (int)first; }      // value that chunk c begins with
+  // chunk c; what lies beyond the row is minus infinity
+  __device__ __forceinline__ chunk16 load(const T* row, int c) const {
+    const int e0 = at(c);
+    if (e0 >= 0 && e0 + PER <= count) return *reinterpret_cast<const chunk16*>(row + e0);
+    union { chunk16 v; T e[PER]; } u;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      if constexpr (sizeof(T) == 2) u.e[e] = 0xff80;
+      else u.e[e] = -INFINITY;
+      if (e0 + e >= 0 && e0 + e < count) u.e[e] = row[e0 + e];
+    }
+    return u.v;
+  }
+  __device__ __forceinline__ void store(T* row, int c, const chunk16& v) const {
+    const int e0 = at(c);
+    if (e0 >= 0 && e0 + PER <= count) { *reinterpret_cast<chunk16*>(row + e0) = v; return; }
+    union { chunk16 v; T e[PER]; } u;
+    u.v = v;
+#pragma unroll
+    for (int e = 0; e < PER; ++e)
+      if (e0 + e >= 0 && e0 + e < count) row[e0 + e] = u.e[e];
+  }
+  static __device__ __forceinline__ float value(const chunk16& v, int e) {
+    if constexpr (sizeof(T) == 2) return __uint_as_float(e & 1 ? v[e >> 1] & 0xffff0000u : v[e >> 1] << 16);
+    else return __uint_as_float(v[e]);
+  }
+  static __device__ __forceinline__ chunk16 pack(const float (&f)[PER]) {
+    chunk16 v;
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = pack_bf16(f[2 * q], f[2 * q + 1]);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = __float_as_uint(f[q]);
+    }
+    return v;
+  }
+};
+
+// Reductions over the NT threads that share a row: one wave without a barrier, or a workgroup by way of sh (NT / 64 values of its own for every call
+// between two barriers).  Everybody gets the result.
+template <int NT> __device__ __forceinline__ void row_sync() {
+  if constexpr (NT == 64) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __threadfence_block();                             // (a wave's LDS and memory accesses are done)
+    __builtin_amdgcn_wave_barrier();
+#endif
+  } else {
+    __syncthreads();
+  }
+}
+template <int NT, class V, class F> __device__ __forceinline__ V row_reduce(V v, V* sh, F op) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = op(v, __shfl_xor(v, o));
+  if constexpr (NT > 64) {
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = sh[0];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) v = op(v, sh[w]);
+  }
+  return v;
+}
+
+}  // namespace acc
