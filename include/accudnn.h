@@ -459,6 +459,23 @@ int acc_op_linear_ce(const void* x, const void* w, const float* bias, const int3
                      float* loss, void* dx, float* dw, float* db, int n, int d, int classes, void* workspace,
                      size_t workspace_bytes, int dtype, void* stream);
 
+/* A gated linear layer: two projections of the same rows (pixels of a map, or features), of which the gate a scales the value b through an activation.
+ *   ab = x w^T + bias,  h = act(a) * b;   da = dh b act'(a),  db = dh act(a),  dx = [da | db] w,  dw = [da | db]^T x,  dbias = their sums over the rows.
+ * x [rows][d], w [2 f][d] (f rows of the gate, then f of the value), h and dh [rows][f], ab [rows][2 f] (the projections, gate first), dx [rows][d]: stored as
+ * dtype; bias [2 f], dw [2 f][d] and db [2 f]: fp32.  bias may be NULL (none).  act: ACC_ACT_* (the slope of ACC_ACT_RELU at 0 is 0).
+ * ab in fwd may be NULL; otherwise the projections are kept there.  ab in bwd: the kept ones (bias is then not looked at; bf16: gradients are those at the rounded values), or NULL:
+ * they are worked out again, half as much work more in place of 2 rows f values of memory.  dx, dw, db in bwd: each may be NULL, at least one is not.
+ * Sums and statistics are fp32; [da | db] of bf16 operands is rounded to bf16 for dx, and the sum of two bf16 values (of three for fewer than 4096 rows) for dw.
+ * Values that are not finite stay in the results that they enter (an infinity among fp32 operands may make NaN of them).
+ * rows <= 2^24, d, f <= 65536, f d (each rounded up to a multiple of 8) below 2^30 - 2^20, rows (d + f) <= 2^36.  workspace: acc_op_glu_workspace() bytes (0
+ * forward for up to four rows, and for sizes that are refused); nothing in it needs to be kept or cleared.  What is written may not overlap another argument
+ * (ACC_EINVAL).  No atomics: the same bits every time. */
+size_t acc_op_glu_workspace(int rows, int d, int f, int backward, int dtype);
+int acc_op_glu_fwd(const void* x, const void* w, const float* bias, void* h, void* ab, int rows, int d, int f, int act, void* workspace,
+                   size_t workspace_bytes, int dtype, void* stream);
+int acc_op_glu_bwd(const void* x, const void* w, const float* bias, const void* ab, const void* dh, void* dx, float* dw, float* db, int rows, int d, int f,
+                   int act, void* workspace, size_t workspace_bytes, int dtype, void* stream);
+
 /* Learning from a teacher: its top logits, which stand for all of them, and the loss of a student's logits against them.
  * acc_op_top_logits: the k largest of each row of z [n][classes] (dtype) with their classes, largest first, of equal ones the lower class first; index
  * [n][k] int32, top [n][k] fp32.  Both zeros are equal (and come out as 0); what is no number counts as larger than any number.  The same results every time.

@@ -171,6 +171,9 @@ _PROTOS = {
     "acc_op_gn_bwd": (_I, [_VP] * 12 + [_I] * 5 + [_VP, _SZ, _I, _VP]),
     "acc_op_linear_ce_workspace": (_SZ, [_I] * 5),
     "acc_op_linear_ce": (_I, [_VP] * 4 + [_I] + [_VP] * 5 + [_I] * 3 + [_VP, _SZ, _I, _VP]),
+    "acc_op_glu_workspace": (_SZ, [_I] * 5),
+    "acc_op_glu_fwd": (_I, [_VP] * 5 + [_I] * 4 + [_VP, _SZ, _I, _VP]),
+    "acc_op_glu_bwd": (_I, [_VP] * 8 + [_I] * 4 + [_VP, _SZ, _I, _VP]),
     "acc_op_top_logits_workspace": (_SZ, [_I] * 4),
     "acc_op_top_logits": (_I, [_VP] * 3 + [_I] * 3 + [_VP, _SZ, _I, _VP]),
     "acc_op_distill_workspace": (_SZ, [_I] * 4),
@@ -719,6 +722,38 @@ def op_linear_ce(x, w, bias, labels, loss_rows, loss, dx, dw, db, ws, ignore=Non
                                 _fits(name, "labels", labels, (n,), i32, device), LABEL_NONE if ignore is None else int(ignore),
                                 given("loss_rows", loss_rows, (n,), f32), given("loss", loss, (1,), f32), given("dx", dx, (n, d), kind),
                                 given("dw", dw, (classes, d), f32), given("db", db, (classes,), f32), n, d, classes, at, size, dtype, stream))
+
+
+def op_glu_workspace(rows, d, f, backward: bool, dtype: int = F32) -> int:
+    return int(_lib.acc_op_glu_workspace(rows, d, f, 1 if backward else 0, int(dtype)))
+
+
+def op_glu_fwd(x, w, bias, h, ab, act, ws):
+    """h = act(gate) * value of the projections x w^T + bias.  x [..., d], w [2 f, d] (rows of the gate, then of the value), bias [2 f] fp32 or None, h [..., f];
+    ab [..., 2 f]: where the projections are kept, or None.  act: ACT_NONE, ACT_RELU, ACT_SILU.  ws may be None where op_glu_workspace() is 0."""
+    torch, device, stream = _here()
+    name, kind, dtype, shape = "op_glu_fwd", x.dtype, _dtype_of(x), x.shape
+    d, f, lead = shape[-1], w.shape[0] // 2, shape[:-1]
+    at, size = (None, 0) if ws is None else _space(name, ws, device)
+    _done(_lib.acc_op_glu_fwd(_fits(name, "x", x, shape, kind, device), _fits(name, "w", w, (2 * f, d), kind, device),
+                              None if bias is None else _fits(name, "bias", bias, (2 * f,), torch.float32, device), _fits(name, "h", h, (*lead, f), kind, device),
+                              None if ab is None else _fits(name, "ab", ab, (*lead, 2 * f), kind, device), x.numel() // max(d, 1), d, f, act, at, size, dtype,
+                              stream))
+
+
+def op_glu_bwd(x, w, bias, ab, dh, dx, dw, db, act, ws):
+    """Gradients of op_glu_fwd from dh [..., f]: dx like x, dw [2 f, d] fp32, db [2 f] fp32, each optional.  ab: the kept projections, or None: they are worked
+    out again from x, w and bias."""
+    torch, device, stream = _here()
+    name, kind, dtype, shape, f32 = "op_glu_bwd", x.dtype, _dtype_of(x), x.shape, torch.float32
+    d, f, lead = shape[-1], w.shape[0] // 2, shape[:-1]
+
+    def given(what, t, shape, dt):
+        return None if t is None else _fits(name, what, t, shape, dt, device)
+    at, size = _space(name, ws, device)
+    _done(_lib.acc_op_glu_bwd(_fits(name, "x", x, shape, kind, device), _fits(name, "w", w, (2 * f, d), kind, device), given("bias", bias, (2 * f,), f32),
+                              given("ab", ab, (*lead, 2 * f), kind), _fits(name, "dh", dh, (*lead, f), kind, device), given("dx", dx, shape, kind),
+                              given("dw", dw, (2 * f, d), f32), given("db", db, (2 * f,), f32), x.numel() // max(d, 1), d, f, act, at, size, dtype, stream))
 
 
 def op_top_logits_workspace(n, classes, k, dtype: int = F32) -> int:

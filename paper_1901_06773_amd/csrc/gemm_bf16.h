@@ -19,9 +19,12 @@ namespace acc {
 // WM x WN waves, each MB x NB blocks of 32 x 32; BK values of k per chunk, NS stages in LDS.  AT / BT: the operand lies in rows of k.  PARTS: A is
 // the sum of so many matrices of the same layout (their products go to the same accumulators).  SWAP: the accumulators are those of the transposed
 // block: register v of a lane holds column 8 * (v / 4) + 4 * (lane / 32) + v % 4 of row lane % 32; otherwise row and column change places.
-template <int WM_, int WN_, int MB_, int NB_, int BK_, int NS_, bool AT_, bool BT_, int PARTS_, bool SWAP_> struct GemmCfg {
+// PAIR: B is two matrices of the same sizes (B.p and B.more[0]); blocks of 32 of their rows take turns, so that a wave's block 2 j + 1 holds, in the same lanes
+// and registers, the second matrix's products of the columns that its block 2 j holds the first one's of: n0 and BN / 2 columns of each.
+template <int WM_, int WN_, int MB_, int NB_, int BK_, int NS_, bool AT_, bool BT_, int PARTS_, bool SWAP_, bool PAIR_ = false> struct GemmCfg {
   static constexpr int WM = WM_, WN = WN_, MB = MB_, NB = NB_, BK = BK_, NS = NS_, PARTS = PARTS_;
-  static constexpr bool AT = AT_, BT = BT_, SWAP = SWAP_;
+  static constexpr bool AT = AT_, BT = BT_, SWAP = SWAP_, PAIR = PAIR_;
+  static_assert(!PAIR_ || (!BT_ && NB_ % 2 == 0), "rows of k side by side, whole pairs");
   static constexpr int THREADS = 64 * WM * WN, BM = 32 * MB * WM, BN = 32 * NB * WN;
   static constexpr int A_PITCH = AT ? BM * 2 : BK * 2, B_PITCH = BT ? BN * 2 : BK * 2;      // bytes of a staged row
   static constexpr int A_COLS = A_PITCH / 16, B_COLS = B_PITCH / 16;
@@ -36,7 +39,7 @@ template <int WM_, int WN_, int MB_, int NB_, int BK_, int NS_, bool AT_, bool B
 
 struct GemmOperand {
   const void* p;         // 16-byte aligned
-  const void* more[2];   // the other parts of A
+  const void* more[2];   // the other parts of A; the second matrix of a pair B
   long rows;             // of m resp. n, or of k
   int cols;              // what lies side by side; a multiple of 8
   int pitch;             // elements between rows; a multiple of 8
@@ -76,7 +79,9 @@ __device__ __forceinline__ void gemm_tile(const GemmOperand& A, const GemmOperan
 #pragma unroll
   for (int part = 0; part < PARTS; ++part)
     rs_a[part] = operand_rows(A, part == 0 ? A.p : A.more[part - 1], C::AT ? 0 : m0, C::AT ? A.rows : C::BM);
-  rs_b = operand_rows(B, B.p, C::BT ? 0 : n0, C::BT ? B.rows : C::BN);
+  rs_b = operand_rows(B, B.p, C::BT ? 0 : n0, C::BT ? B.rows : C::BN / (C::PAIR ? 2 : 1));
+  srsrc rs_b2 = rs_b;
+  if constexpr (C::PAIR) rs_b2 = operand_rows(B, B.more[0], n0, C::BN / 2);
   const uint32_t a_pitch = (uint32_t)A.pitch * 2u, b_pitch = (uint32_t)B.pitch * 2u;
 #pragma unroll
   for (int i = 0; i < AI; ++i) {
@@ -86,7 +91,8 @@ __device__ __forceinline__ void gemm_tile(const GemmOperand& A, const GemmOperan
   }
 #pragma unroll
   for (int i = 0; i < BI; ++i) {
-    const int row = brow + C::B_STEP * i;
+    int row = brow + C::B_STEP * i;
+    if constexpr (C::PAIR) row = ((row >> 6) << 5) + (row & 31);
     const bool ok = C::BT ? n0 + bcol * 8 < B.cols : n0 + row < B.rows;
     b_voff[i] = ok ? (uint32_t)row * b_pitch + (uint32_t)(C::BT ? n0 * 2 : 0) + (uint32_t)bcol * 16u : OUTSIDE;
   }
@@ -104,7 +110,9 @@ __device__ __forceinline__ void gemm_tile(const GemmOperand& A, const GemmOperan
     } else {
       const int i = u - LA;
       const bool ok = C::BT ? k_next + brow + C::B_STEP * i < kb_hi : k_next + bcol * 8 < kb_hi;
-      load_lds16(rs_b, ok ? b_voff[i] : OUTSIDE, C::BT ? (uint32_t)k_next * b_pitch : (uint32_t)k_next * 2u, at + C::A_BYTES + i * (C::THREADS * 16));
+      // (a wave's load fills 8 or 16 rows: all of them are of one matrix)
+      const bool second = C::PAIR && ((wave * (64 / C::B_COLS) + C::B_STEP * i) >> 5) & 1;
+      load_lds16(second ? rs_b2 : rs_b, ok ? b_voff[i] : OUTSIDE, C::BT ? (uint32_t)k_next * b_pitch : (uint32_t)k_next * 2u, at + C::A_BYTES + i * (C::THREADS * 16));
     }
     if (u == L - 1) k_next += BK;
   };

@@ -23,10 +23,13 @@
 
 namespace acc {
 
-// WM x WN waves, each MB x NB blocks of 16 x 16.  AT / BT: the operand lies in rows of k.  SPLIT: products on the bf16 matrix cores.
-template <int WM_, int WN_, int MB_, int NB_, bool AT_, bool BT_, bool SPLIT_> struct Gemm32Cfg {
+// WM x WN waves, each MB x NB blocks of 16 x 16.  AT / BT: the operand lies in rows of k.  SPLIT: products on the bf16 matrix cores.  PAIR: B is two matrices
+// of the same sizes (`second` floats apart); blocks of 16 of their rows take turns, so that block 2 j + 1 of a wave holds the second matrix's products of the
+// columns that its block 2 j holds the first one's of: n0 and BN / 2 columns of each.
+template <int WM_, int WN_, int MB_, int NB_, bool AT_, bool BT_, bool SPLIT_, bool PAIR_ = false> struct Gemm32Cfg {
   static constexpr int WM = WM_, WN = WN_, MB = MB_, NB = NB_, BK = 32;
-  static constexpr bool AT = AT_, BT = BT_, SPLIT = SPLIT_;
+  static constexpr bool AT = AT_, BT = BT_, SPLIT = SPLIT_, PAIR = PAIR_;
+  static_assert(!PAIR_ || (!BT_ && NB_ % 2 == 0), "rows of k side by side, whole pairs");
   static constexpr int THREADS = 64 * WM * WN, BM = 16 * MB * WM, BN = 16 * NB * WN;
   static constexpr int SPLIT_PITCH = 20;               // a row's 32 bf16 values, and 16 bytes that set the next row off
   // floats between staged rows: the sixteen rows (resp. four groups of sixteen columns) that a read takes at once fall on different banks
@@ -44,6 +47,7 @@ struct Gemm32Operand {
   const float* p;
   int extent;            // of m resp. n
   int pitch;             // floats between rows
+  uint32_t second = 0;   // floats to the second matrix of a pair
 };
 
 template <class C> using Gemm32Acc = f32x4[C::MB][C::NB];
@@ -71,7 +75,7 @@ template <int EXTENT, bool T, int LOADS, int PITCH, int THREADS> struct Gemm32Lo
   uint32_t off[LOADS];   // floats
   int end;               // rows of k: where the columns end, seen from x0; else unused
   bool edge;
-  __device__ __forceinline__ void start(const Gemm32Operand& o, int x0, int k_lo) {
+  __device__ __forceinline__ void start(const Gemm32Operand& o, int x0, int k_lo, bool pair = false) {
     const int left = o.extent - x0;
     base = T ? o.p + (size_t)k_lo * o.pitch + x0 : o.p + (size_t)x0 * o.pitch + k_lo;
     end = left;
@@ -80,6 +84,7 @@ template <int EXTENT, bool T, int LOADS, int PITCH, int THREADS> struct Gemm32Lo
     for (int i = 0; i < LOADS; ++i) {
       const int u = threadIdx.x + i * THREADS;
       if (T) off[i] = (uint32_t)(u / (EXTENT / 4)) * (uint32_t)o.pitch + (uint32_t)(u % (EXTENT / 4)) * 4u;
+      else if (pair) off[i] = (uint32_t)min(((u / 8) >> 5) * 16 + ((u / 8) & 15), left - 1) * (uint32_t)o.pitch + (uint32_t)(u % 8) * 4u + (((u / 8) & 16) ? o.second : 0u);
       else off[i] = (uint32_t)min(u / 8, left - 1) * (uint32_t)o.pitch + (uint32_t)(u % 8) * 4u;
     }
   }
@@ -194,7 +199,7 @@ __device__ __forceinline__ void gemm32_tile(const Gemm32Operand& A, const Gemm32
   typename Gemm32LoaderOf<C::SPLIT, C::BM, C::AT, C::AI, C::A_PITCH, C::SPLIT_PITCH, C::THREADS>::type a;
   typename Gemm32LoaderOf<C::SPLIT, C::BN, C::BT, C::BI, C::B_PITCH, C::SPLIT_PITCH, C::THREADS>::type b;
   a.start(A, m0, k_lo);
-  b.start(B, n0, k_lo);
+  b.start(B, n0, k_lo, C::PAIR);
   if (k_lo < k_hi) {
     a.load(A, k_hi - k_lo);
     b.load(B, k_hi - k_lo);

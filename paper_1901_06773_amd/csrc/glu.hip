@@ -1,0 +1,465 @@
+// A gated linear layer: two projections of the same rows, of which one, through an activation, scales the other.
+//
+//   ab = x w^T + bias, w [2 f][d]: rows of the gate a, then of the value b;  h = act(a) b
+//   da = dh b act'(a),  db = dh act(a);  with dz = [da | db]:  dx = dz w,  dw = dz^T x,  dbias = sum over the rows of dz
+//
+// 4 rows d f operations forward, 8 backward and 4 more where the projections were not kept: bound by the matrix cores but for few rows, where reading w is.
+// Gate and value are worked out by the same workgroup, so that neither is in memory unless it is to be kept.  The backward pass writes dz (a workspace), as
+// two products read it.  Few tiles: the projections' sums are cut, and launches that work value by value add the parts and do the rest.
+// Up to four rows: every wave takes a few columns and all rows, the layer's weights once through the vector units.
+#include "kernels.h"
+#include "glu.h"
+#include "product32.h"
+
+namespace acc {
+namespace {
+
+typedef uint32_t any16 __attribute__((ext_vector_type(4), aligned(2)));
+
+// V neighbouring values as floats, at any address that the type allows; `left` of them exist
+template <class T, int V> __device__ __forceinline__ void get(const T* p, int left, float (&v)[V]) {
+  if (V > 1 && left >= V) {
+    if constexpr (sizeof(T) == 2) {
+      const any16 q = *reinterpret_cast<const any16*>(p);
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[e] = __uint_as_float(e & 1 ? q[e >> 1] & 0xffff0000u : q[e >> 1] << 16);
+    } else {
+      const f32x4_any q = *reinterpret_cast<const f32x4_any*>(p);
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[e] = q[e];
+    }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = e < left ? Elem<T>::load(p + e) : 0.f;
+}
+template <class T, int V> __device__ __forceinline__ void put(T* p, int left, const float (&v)[V]) {
+  if (V > 1 && left >= V) {
+    if constexpr (sizeof(T) == 2) {
+      any16 q;
+#pragma unroll
+      for (int e = 0; e < V / 2; ++e) q[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+      *reinterpret_cast<any16*>(p) = q;
+    } else {
+      f32x4_any q;
+#pragma unroll
+      for (int e = 0; e < V; ++e) q[e] = v[e];
+      *reinterpret_cast<f32x4_any*>(p) = q;
+    }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e)
+    if (e < left) Elem<T>::store(p + e, v[e]);
+}
+
+// ---------------------------------------------------------------------------------- value by value
+template <class T> struct PointWidth { static constexpr int value = 16 / (int)sizeof(T); };
+
+template <class T, bool BWD, int PARTS>
+__global__ __launch_bounds__(256) void glu_point_kernel(PointArgs a) {
+  constexpr int V = PointWidth<T>::value;
+  __shared__ float sh[BWD ? 2 * V : 1][256];
+  const int tx = threadIdx.x % a.tx, ty = threadIdx.x / a.tx, step = 256 / a.tx;
+  const int across = (int)blockIdx.x % a.across, slab = (int)blockIdx.x / a.across;
+  const int c = (across * a.tx + tx) * V, left = a.f - c;
+  const size_t whole = (size_t)a.rows * 2 * a.half;
+  float ba[V], bb[V], sa[V], sb[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    ba[e] = a.bias && e < left ? a.bias[c + e] : 0.f;
+    bb[e] = a.bias && e < left ? a.bias[a.f + c + e] : 0.f;
+    sa[e] = sb[e] = 0.f;
+  }
+  const int r1 = min((slab + 1) * a.slab, a.rows);
+  for (int r = slab * a.slab + ty; r < r1 && left > 0; r += step) {
+    float g[V], v[V];
+    if (a.sums) {
+      const float* const from = a.sums + (size_t)r * 2 * a.half + c;
+#pragma unroll
+      for (int e = 0; e < V; ++e) { g[e] = ba[e]; v[e] = bb[e]; }
+      for (int s = 0; s < a.splits; ++s) {
+#pragma unroll
+        for (int e = 0; e < V; e += 4) {
+          float p[4], q[4];
+          get<float, 4>(from + s * whole + e, left - e, p);
+          get<float, 4>(from + s * whole + a.half + e, left - e, q);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) { g[e + u] += p[u]; v[e + u] += q[u]; }
+        }
+      }
+    } else {
+      const T* const from = static_cast<const T*>(a.ab_in) + (size_t)r * 2 * a.f + c;
+      get<T, V>(from, left, g);
+      get<T, V>(from + a.f, left, v);
+    }
+    if constexpr (!BWD) {
+      float h[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) h[e] = glu_act(a.act, g[e]) * v[e];
+      put<T, V>(static_cast<T*>(a.h) + (size_t)r * a.f + c, left, h);
+      if (a.ab) {
+        T* const to = static_cast<T*>(a.ab) + (size_t)r * 2 * a.f + c;
+        put<T, V>(to, left, g);
+        put<T, V>(to + a.f, left, v);
+      }
+    } else {
+      float dh[V];
+      get<T, V>(static_cast<const T*>(a.dh) + (size_t)r * a.f + c, left, dh);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        float da, db;
+        glu_slopes(a.act, g[e], v[e], dh[e], da, db);
+        g[e] = e < left ? da : 0.f;
+        v[e] = e < left ? db : 0.f;
+        sa[e] += g[e];
+        sb[e] += v[e];
+      }
+      // (columns up to a.half exist and are zero from a.f on)
+#pragma unroll
+      for (int part = 0; part < PARTS; ++part) {
+        T* const to = static_cast<T*>(a.dz[part]) + (size_t)r * a.pitch + c;
+        put<T, V>(to, a.half - c, g);
+        put<T, V>(to + a.half, a.half - c, v);
+        if (part + 1 < PARTS) {
+#pragma unroll
+          for (int e = 0; e < V; e += 2) {
+            const uint32_t p = pack_bf16(g[e], g[e + 1]), q = pack_bf16(v[e], v[e + 1]);
+            g[e] -= __uint_as_float(p << 16); g[e + 1] -= __uint_as_float(p & 0xffff0000u);
+            v[e] -= __uint_as_float(q << 16); v[e + 1] -= __uint_as_float(q & 0xffff0000u);
+          }
+        }
+      }
+    }
+  }
+  if constexpr (BWD) {
+    if (!a.db_part) return;
+#pragma unroll
+    for (int e = 0; e < V; ++e) { sh[e][threadIdx.x] = sa[e]; sh[V + e][threadIdx.x] = sb[e]; }
+    __syncthreads();
+    // column e of the tx threads that hold it, row by row of threads
+    for (int i = threadIdx.x; i < a.tx * 2 * V; i += 256) {
+      const int t = i % a.tx, e = i / a.tx, col = (across * a.tx + t) * V + (e % V);
+      if (col >= a.f) continue;
+      float s = 0.f;
+      for (int y = 0; y < step; ++y) s += sh[e][y * a.tx + t];
+      a.db_part[(size_t)slab * a.pitch + col + (e < V ? 0 : a.half)] = s;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------- sums of parts
+template <class T>
+__global__ __launch_bounds__(256) void glu_finish_kernel(GluFinish f, unsigned dx_blocks, unsigned dw_blocks) {
+  unsigned block = blockIdx.x;
+  if (block < dx_blocks) return join_sums<T>(f.dx_sums, (T*)f.dx, f.dx_count, f.dx_splits, block, dx_blocks);
+  block -= dx_blocks;
+  if (block < dw_blocks) return join_sums<float>(f.dw_sums, f.dw, f.dw_count, f.dw_splits, block, dw_blocks);
+  block -= dw_blocks;
+  // sixteen columns, sixteen threads down each
+  __shared__ double sh[256];
+  const int j = (int)block * 16 + (threadIdx.x & 15);
+  double s = 0.0;
+  if (j < 2 * f.f) {
+    const float* const p = f.db_part + (j < f.f ? j : f.half + j - f.f);
+    for (int k = threadIdx.x >> 4; k < f.db_parts; k += 16) s += (double)p[(size_t)k * f.pitch];
+  }
+  sh[threadIdx.x] = s;
+  __syncthreads();
+  if (threadIdx.x >= 16 || j >= 2 * f.f) return;
+  for (int k = 1; k < 16; ++k) s += sh[threadIdx.x + 16 * k];
+  f.db[j] = (float)s;
+}
+
+// ---------------------------------------------------------------------------------- few rows
+// R rows: a wave's columns one after the other, sixteen bytes of w's rows to a lane, all rows of x against them.
+template <class T, int R>
+__global__ __launch_bounds__(256) void glu_few_kernel(const T* __restrict__ x, const T* __restrict__ w, const float* __restrict__ bias, T* __restrict__ h,
+                                                      T* __restrict__ ab, int d, int f, int act) {
+  constexpr int V = 16 / (int)sizeof(T);
+  const int lane = threadIdx.x & 63, waves = (int)gridDim.x * 4;
+  for (int c = (int)blockIdx.x * 4 + (threadIdx.x >> 6); c < f; c += waves) {
+    const T *const wa = w + (size_t)c * d, *const wb = w + (size_t)(f + c) * d;
+    float a[R], b[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) a[r] = b[r] = 0.f;
+#pragma unroll 2
+    for (int k = lane * V; k < d; k += 64 * V) {
+      float va[V], vb[V], vx[V];
+      get<T, V>(wa + k, d - k, va);
+      get<T, V>(wb + k, d - k, vb);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        get<T, V>(x + (size_t)r * d + k, d - k, vx);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          a[r] = fmaf(va[e], vx[e], a[r]);
+          b[r] = fmaf(vb[e], vx[e], b[r]);
+        }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) { a[r] += __shfl_xor(a[r], o); b[r] += __shfl_xor(b[r], o); }
+    const float ba = bias ? bias[c] : 0.f, bb = bias ? bias[f + c] : 0.f;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (lane == r) {
+        const float g = a[r] + ba, v = b[r] + bb;
+        Elem<T>::store(h + (size_t)r * f + c, glu_act(act, g) * v);
+        if (ab) {
+          Elem<T>::store(ab + (size_t)r * 2 * f + c, g);
+          Elem<T>::store(ab + (size_t)r * 2 * f + f + c, v);
+        }
+      }
+  }
+}
+constexpr int kFewRows = 4;
+template <class T> hipError_t glu_few(const GluArgs& a) {
+  const dim3 grid((unsigned)(ceil_div(a.f, 4) < 4096 ? ceil_div(a.f, 4) : 4096));
+#define ACC_FEW(R) hipLaunchKernelGGL((glu_few_kernel<T, R>), grid, dim3(256), 0, a.st, (const T*)a.x, (const T*)a.w, a.bias, (T*)a.h, (T*)a.ab, a.d, a.f, a.act)
+  switch (a.rows) {
+    case 1: ACC_FEW(1); break;
+    case 2: ACC_FEW(2); break;
+    case 3: ACC_FEW(3); break;
+    default: ACC_FEW(4);
+  }
+#undef ACC_FEW
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------------- fp32 products
+struct Pair32 {
+  Gemm32Operand x, w;          // w.second: from the gate's rows to the value's
+  const float* bias;
+  int rows, d, f, act, tiles_m, tiles;
+  float *h, *ab;               // forward
+  const float* dh;             // backward
+  float *dz, *db_part;
+};
+template <class C, bool BWD>
+__global__ __launch_bounds__(C::THREADS) void glu32_kernel(Pair32 a, int blocks) {
+  __shared__ __attribute__((aligned(16))) float lds[C::LDS];
+  const int at = xcd_tile(blocks);
+  if (at >= a.tiles) return;
+  const TileAt where = tile_at(at, a.tiles_m, a.tiles);
+  const int m0 = where.m * C::BM, n0 = where.n * (C::BN / 2);
+  Gemm32Acc<C> acc;
+  gemm32_tile<C>(a.x, a.w, m0, n0, 0, a.d, lds, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm0 = (wave / C::WN) * 16 * C::MB, col0 = n0 + (wave % C::WN) * 8 * C::NB + 4 * (lane >> 4);
+  const size_t f = a.f;
+#pragma unroll
+  for (int j = 0; j < C::NB / 2; ++j) {
+    const int c = col0 + 16 * j, left = a.f - c;
+    float ba[4], bb[4], sa[4], sb[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      ba[e] = a.bias && e < left ? a.bias[c + e] : 0.f;
+      bb[e] = a.bias && e < left ? a.bias[f + c + e] : 0.f;
+      sa[e] = sb[e] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < C::MB; ++i) {
+      const int m = m0 + wm0 + 16 * i + (lane & 15);
+      if (m >= a.rows || left <= 0) continue;
+      float g[4], v[4], o[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { g[e] = acc[i][2 * j][e] + ba[e]; v[e] = acc[i][2 * j + 1][e] + bb[e]; }
+      if constexpr (!BWD) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = glu_act(a.act, g[e]) * v[e];
+        put<float, 4>(a.h + m * f + c, left, o);
+        if (a.ab) {
+          put<float, 4>(a.ab + m * 2 * f + c, left, g);
+          put<float, 4>(a.ab + m * 2 * f + f + c, left, v);
+        }
+      } else {
+        get<float, 4>(a.dh + m * f + c, left, o);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float da, db;
+          glu_slopes(a.act, g[e], v[e], o[e], da, db);
+          g[e] = da;
+          v[e] = db;
+          sa[e] += da;
+          sb[e] += db;
+        }
+        put<float, 4>(a.dz + m * 2 * f + c, left, g);
+        put<float, 4>(a.dz + m * 2 * f + f + c, left, v);
+      }
+    }
+    if (BWD && a.db_part) {
+      float* const to = a.db_part + (size_t)(where.m * C::WM + wave / C::WN) * 2 * f + c;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) { sa[e] += __shfl_xor(sa[e], o); sb[e] += __shfl_xor(sb[e], o); }
+        if ((lane & 15) == 0 && e < left) { to[e] = sa[e]; to[f + e] = sb[e]; }
+      }
+    }
+  }
+}
+
+struct GluPlan32 {
+  int tile;
+  bool cut;
+  Cut proj, dx, dw;
+  int db_parts;
+  size_t sums, dz, dx_sums, dw_sums, db, total;
+};
+GluPlan32 glu_plan32(int rows, int d, int f, bool backward, bool kept) {
+  GluPlan32 p{};
+  const long wide = 2L * f;
+  const Cut whole = cut32(rows, wide, d, 0);
+  p.tile = whole.tile;
+  p.proj = cut32(rows, wide, d, 1L << 24);
+  p.cut = !kept && p.proj.splits > 1 && p.proj.us + 3.0 < whole.us;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t a = at; at += al256(bytes); return a; };
+  p.sums = take(p.cut ? (size_t)p.proj.splits * rows * wide * 4 : 0);
+  if (backward) {
+    p.dx = cut32(rows, d, wide, 1L << 25);
+    p.dw = cut32(wide, d, rows, 1L << 25);
+    p.dz = take((size_t)rows * wide * 4);
+    p.dx_sums = take(p.dx.splits > 1 ? (size_t)p.dx.splits * rows * d * 4 : 0);
+    p.dw_sums = take(p.dw.splits > 1 ? (size_t)p.dw.splits * wide * d * 4 : 0);
+    PointArgs q{};
+    q.rows = rows; q.f = f;
+    p.db_parts = kept || p.cut ? glu_point_shape(q, DT_F32) : (int)ceil_div(rows, kTile32[p.tile][0]) * (p.tile == 0 ? 1 : 2);
+    p.db = take((size_t)p.db_parts * wide * 4);
+  }
+  p.total = at;
+  return p;
+}
+template <class C> void launch_pair32(const Pair32& g, bool backward, hipStream_t st) {
+  const unsigned blocks = whole_eights(g.tiles);
+  if (backward) hipLaunchKernelGGL((glu32_kernel<C, true>), dim3(blocks), dim3(C::THREADS), 0, st, g, (int)blocks);
+  else hipLaunchKernelGGL((glu32_kernel<C, false>), dim3(blocks), dim3(C::THREADS), 0, st, g, (int)blocks);
+}
+
+hipError_t glu32(const GluArgs& a, bool backward) {
+  const bool kept = backward && a.ab_in;
+  const GluPlan32 p = glu_plan32(a.rows, a.d, a.f, backward, kept);
+  const float *x = (const float*)a.x, *w = (const float*)a.w;
+  float *const dz = (float*)(a.ws + p.dz), *const db_part = backward && a.db ? (float*)(a.ws + p.db) : nullptr;
+  hipStream_t st = a.st;
+  const int wide = 2 * a.f;
+  if (kept || p.cut) {
+    PointArgs q{};
+    q.ab_in = a.ab_in; q.dh = a.dh; q.h = a.h; q.ab = a.ab; q.dz[0] = dz; q.db_part = db_part;
+    q.rows = a.rows; q.f = a.f; q.act = a.act; q.half = a.f; q.pitch = wide;
+    if (!kept) {
+      Product32 g{};
+      g.a = {x, a.rows, a.d}; g.b = {w, wide, a.d}; g.out = (float*)(a.ws + p.sums); g.k = a.d;
+      cut_into(g, p.proj);
+      if (const hipError_t e = launch_product32<false, false>(g, p.proj, st); e != hipSuccess) return e;
+      q.sums = g.out; q.splits = p.proj.splits; q.bias = a.bias;
+    }
+    glu_point_shape(q, DT_F32);
+    if (const hipError_t e = glu_point(q, backward, 1, DT_F32, st); e != hipSuccess || !backward) return e;
+  } else {
+    Pair32 g{};
+    g.x = {x, a.rows, a.d}; g.w = {w, a.f, a.d, (uint32_t)a.f * (uint32_t)a.d};
+    g.bias = a.bias; g.rows = a.rows; g.d = a.d; g.f = a.f; g.act = a.act;
+    g.tiles_m = (int)ceil_div(a.rows, kTile32[p.tile][0]); g.tiles = g.tiles_m * (int)ceil_div(a.f, kTile32[p.tile][1] / 2);
+    g.h = (float*)a.h; g.ab = (float*)a.ab; g.dh = (const float*)a.dh; g.dz = dz; g.db_part = db_part;
+    if (p.tile == 0) launch_pair32<Gemm32Cfg<1, 4, 2, 2, false, false, false, true>>(g, backward, st);
+    else if (p.tile == 1) launch_pair32<Gemm32Cfg<2, 2, 2, 2, false, false, false, true>>(g, backward, st);
+    else launch_pair32<Gemm32Cfg<2, 2, 4, 4, false, false, true, true>>(g, backward, st);
+    if (!backward) return hipGetLastError();
+  }
+  GluFinish f{};
+  if (a.dx) {
+    Product32 g{};
+    g.a = {dz, a.rows, wide}; g.b = {w, a.d, a.d}; g.k = wide;
+    g.out = p.dx.splits > 1 ? (float*)(a.ws + p.dx_sums) : (float*)a.dx;
+    cut_into(g, p.dx);
+    if (const hipError_t e = launch_product32<false, true>(g, p.dx, st); e != hipSuccess) return e;
+    if (p.dx.splits > 1) { f.dx_sums = g.out; f.dx = a.dx; f.dx_count = (size_t)a.rows * a.d; f.dx_splits = p.dx.splits; }
+  }
+  if (a.dw) {
+    Product32 g{};
+    g.a = {dz, wide, wide}; g.b = {x, a.d, a.d}; g.k = a.rows;
+    g.out = p.dw.splits > 1 ? (float*)(a.ws + p.dw_sums) : a.dw;
+    cut_into(g, p.dw);
+    if (const hipError_t e = launch_product32<true, true>(g, p.dw, st); e != hipSuccess) return e;
+    if (p.dw.splits > 1) { f.dw_sums = g.out; f.dw = a.dw; f.dw_count = (size_t)wide * a.d; f.dw_splits = p.dw.splits; }
+  }
+  if (a.db) { f.db_part = db_part; f.db = a.db; f.db_parts = p.db_parts; f.pitch = wide; f.half = a.f; f.f = a.f; }
+  return glu_finish(f, DT_F32, st);
+}
+
+// w takes fewer than 4 GiB as bf16 values, a launch fewer than 2^32 threads
+bool glu_ok(int rows, int d, int f, int dtype) {
+  return rows > 0 && d > 0 && f > 0 && rows <= (1 << 24) && d <= (1 << 16) && f <= (1 << 16) && (long)up(d, 8) * up(f, 8) < (1L << 30) - (1L << 20) &&
+         (long)rows * (d + f) <= 1L << 36 && (dtype == DT_F32 || dtype == DT_BF16);
+}
+
+}  // namespace
+
+int glu_point_shape(PointArgs& a, int dtype) {
+  const int v = dtype == DT_BF16 ? 8 : 4, chunks = (a.f + v - 1) / v;
+  a.tx = 1;
+  while (a.tx < chunks && a.tx < 256) a.tx *= 2;
+  a.across = (int)ceil_div(chunks, a.tx);
+  // some two thousand workgroups, at most 512 of them down a column
+  const int step = 256 / a.tx;
+  long each = ceil_div((long)a.rows * a.across, 2048);
+  if (each < ceil_div(a.rows, 512)) each = ceil_div(a.rows, 512);
+  a.slab = (int)up(each, step);
+  return (int)ceil_div(a.rows, a.slab);
+}
+
+hipError_t glu_point(const PointArgs& a, bool backward, int parts, int dtype, hipStream_t st) {
+  const dim3 grid((unsigned)(ceil_div(a.rows, a.slab) * a.across));
+#define ACC_POINT(T, BWD, PARTS) hipLaunchKernelGGL((glu_point_kernel<T, BWD, PARTS>), grid, dim3(256), 0, st, a)
+  if (dtype == DT_F32) { if (backward) ACC_POINT(float, true, 1); else ACC_POINT(float, false, 1); }
+  else if (!backward) ACC_POINT(bf16_t, false, 1);
+  else if (parts == 3) ACC_POINT(bf16_t, true, 3);
+  else if (parts == 2) ACC_POINT(bf16_t, true, 2);
+  else ACC_POINT(bf16_t, true, 1);
+#undef ACC_POINT
+  return hipGetLastError();
+}
+
+hipError_t glu_finish(const GluFinish& f, int dtype, hipStream_t st) {
+  const unsigned bx = f.dx_splits > 1 ? join_blocks(f.dx_count) : 0, bw = f.dw_splits > 1 ? join_blocks(f.dw_count) : 0;
+  const unsigned blocks = bx + bw + (f.db ? (unsigned)ceil_div(2L * f.f, 16) : 0);
+  if (blocks) {
+    if (dtype == DT_F32) hipLaunchKernelGGL(glu_finish_kernel<float>, dim3(blocks), dim3(256), 0, st, f, bx, bw);
+    else hipLaunchKernelGGL(glu_finish_kernel<bf16_t>, dim3(blocks), dim3(256), 0, st, f, bx, bw);
+  }
+  return hipGetLastError();
+}
+
+size_t glu_workspace_bytes(int rows, int d, int f, int backward, int dtype) {
+  if (!glu_ok(rows, d, f, dtype)) return 0;
+  if (!backward && rows <= kFewRows) return 0;
+  if (dtype == DT_BF16) return glu_bf16_workspace_bytes(rows, d, f, backward != 0);
+  const size_t again = glu_plan32(rows, d, f, backward != 0, false).total, kept = backward ? glu_plan32(rows, d, f, true, true).total : 0;
+  return again > kept ? again : kept;
+}
+
+hipError_t glu_forward(const void* x, const void* w, const float* bias, void* h, void* ab, int rows, int d, int f, int act, void* workspace,
+                       size_t workspace_bytes, int dtype, hipStream_t st) {
+  if (!x || !w || !h || act < GLU_NONE || act > GLU_SILU || !glu_ok(rows, d, f, dtype)) return hipErrorInvalidValue;
+  const size_t need = glu_workspace_bytes(rows, d, f, 0, dtype);
+  if (workspace_bytes < need || (need && !workspace)) return hipErrorInvalidValue;
+  GluArgs a{};
+  a.x = x; a.w = w; a.bias = bias; a.h = h; a.ab = ab; a.rows = rows; a.d = d; a.f = f; a.act = act; a.ws = (char*)workspace; a.dtype = dtype; a.st = st;
+  if (rows <= kFewRows) return dtype == DT_BF16 ? glu_few<bf16_t>(a) : glu_few<float>(a);
+  return dtype == DT_BF16 ? glu_bf16(a, false) : glu32(a, false);
+}
+
+hipError_t glu_backward(const void* x, const void* w, const float* bias, const void* ab, const void* dh, void* dx, float* dw, float* db, int rows, int d, int f,
+                        int act, void* workspace, size_t workspace_bytes, int dtype, hipStream_t st) {
+  if (!x || !w || !dh || !workspace || !(dx || dw || db) || act < GLU_NONE || act > GLU_SILU || !glu_ok(rows, d, f, dtype)) return hipErrorInvalidValue;
+  if (workspace_bytes < glu_workspace_bytes(rows, d, f, 1, dtype)) return hipErrorInvalidValue;
+  GluArgs a{};
+  a.x = x; a.w = w; a.bias = bias; a.ab_in = ab; a.dh = dh; a.dx = dx; a.dw = dw; a.db = db;
+  a.rows = rows; a.d = d; a.f = f; a.act = act; a.ws = (char*)workspace; a.dtype = dtype; a.st = st;
+  return dtype == DT_BF16 ? glu_bf16(a, true) : glu32(a, true);
+}
+
+}  // namespace acc

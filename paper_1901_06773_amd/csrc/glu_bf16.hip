@@ -1,0 +1,543 @@
+// The products of the gated layer (glu.hip) for bf16 operands, on the bf16 matrix cores.
+//
+// Gate and value of the same columns are products of one tile (GemmCfg's PAIR): they meet in the same registers, where h = act(a) b, or in the backward pass,
+// which works them out again, their gradients da and db, leaves them.  Those are [rows][2 f] = dz, and the rest is that of a linear layer: dx = dz w, dw = dz^T x.
+//
+// dz is kept as the sum of bf16 values, the first the nearest one, the next the nearest to what is left (relative errors of 2^-8, 2^-16, 2^-24).  dx, rounded to
+// bf16 itself, is multiplied from the first: the errors of its 2 f terms are independent and add up to one more rounding of the result's size (relative error of dx,
+// one value / two: measured below at the kernel).  dw, an fp32 result, is multiplied from two, of fewer than 4096 rows from three, where two would show beside
+// the roundings of a sum of so few terms in fp32.
+#include "glu.h"
+
+#include "gemm_bf16.h"
+#include "gemm_tiles.h"
+
+namespace acc {
+namespace {
+
+struct PairArgs {
+  GemmOperand x, w;            // w.p the gate's rows, w.more[0] the value's
+  const float* bias;           // [2 f], or null
+  int rows, d, f, act, tiles_m, tiles;
+  bf16_t *h, *ab;              // forward
+  const bf16_t* dh;            // backward
+  bf16_t* dz[3];
+  int pitch, half;             // of dz: columns, and where the value's begin
+  float* db_part;
+};
+
+// 32 rows of a wave's columns by way of LDS, so that memory sees whole pieces of rows: EP bytes a staged row.
+template <class C> struct Stage {
+  static constexpr int COLS = 16 * C::NB, EP = COLS * 2 + 16, PER = COLS / 8, ROWS = 64 / PER, BYTES = 32 * EP;      // PER lanes to a row
+};
+// rows of `pitch` values from `to` on; columns [0, left) and rows [0, rows) exist.  whole: sixteen bytes at a time
+template <class C> __device__ __forceinline__ void rows_out(const char* stg, bf16_t* to, size_t pitch, int rows, int left, bool whole) {
+  typedef Stage<C> S;
+  const int lane = threadIdx.x & 63, c = 8 * (lane % S::PER);
+#pragma unroll
+  for (int it = 0; it < 32 / S::ROWS; ++it) {
+    const int r = lane / S::PER + S::ROWS * it;
+    if (r >= rows || c >= left) continue;
+    const v4u v = *reinterpret_cast<const v4u*>(stg + r * S::EP + c * 2);
+    bf16_t* const o = to + r * pitch + c;
+    if (whole) { *reinterpret_cast<v4u*>(o) = v; continue; }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (c + e < left) o[e] = (bf16_t)(v[e >> 1] >> (16 * (e & 1)));
+  }
+}
+template <class C> __device__ __forceinline__ void rows_in(char* stg, const bf16_t* from, size_t pitch, int rows, int left, bool whole) {
+  typedef Stage<C> S;
+  const int lane = threadIdx.x & 63, c = 8 * (lane % S::PER);
+#pragma unroll
+  for (int it = 0; it < 32 / S::ROWS; ++it) {
+    const int r = lane / S::PER + S::ROWS * it;
+    v4u v = {0, 0, 0, 0};
+    if (r < rows && c < left) {
+      const bf16_t* const o = from + r * pitch + c;
+      if (whole) v = *reinterpret_cast<const v4u*>(o);
+      else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (c + e < left) v[e >> 1] |= (uint32_t)o[e] << (16 * (e & 1));
+      }
+    }
+    *reinterpret_cast<v4u*>(stg + r * S::EP + c * 2) = v;
+  }
+}
+__device__ __forceinline__ void wave_lds_done() {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#endif
+}
+
+template <class C>
+__device__ __forceinline__ void add_pair_bias(GemmAcc<C>& acc, const float* __restrict__ bias, int col0, int f) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int j = 0; j < C::NB; ++j)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int n = col0 + 32 * (j >> 1) + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
+      const float b = n < f ? bias[n + (j & 1 ? f : 0)] : 0.f;
+#pragma unroll
+      for (int i = 0; i < C::MB; ++i) acc[i][j][v] += b;
+    }
+}
+
+// h, and the projections where they are kept
+template <class C>
+__global__ __launch_bounds__(C::THREADS, 2) void glu_fwd_kernel(PairArgs a, int blocks) {
+  typedef Stage<C> S;
+  constexpr int OUT = C::WM * C::WN * S::BYTES;
+  __shared__ __attribute__((aligned(1024))) char lds[C::LDS > OUT ? C::LDS : OUT];
+  const int at = xcd_tile(blocks);
+  if (at >= a.tiles) return;
+  const TileAt where = tile_at(at, a.tiles_m, a.tiles);
+  const int m0 = where.m * C::BM, n0 = where.n * (C::BN / 2);
+  GemmAcc<C> acc;
+  gemm_tile<C>(a.x, a.w, m0, n0, 0, a.d, lds, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm0 = (wave / C::WN) * 32 * C::MB, col0 = n0 + (wave % C::WN) * S::COLS;
+  if (a.bias) add_pair_bias<C>(acc, a.bias, col0, a.f);
+  char *const stg = lds + wave * S::BYTES, *const mine = stg + (lane & 31) * S::EP + 8 * (lane >> 5);
+  const bool whole = (a.f & 7) == 0;
+#pragma unroll
+  for (int i = 0; i < C::MB; ++i) {
+    const int m = m0 + wm0 + 32 * i;
+    auto out = [&](bf16_t* to, size_t pitch, auto value) {
+#pragma unroll
+      for (int j = 0; j < C::NB / 2; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = value(acc[i][2 * j][4 * q + e], acc[i][2 * j + 1][4 * q + e]);
+          *reinterpret_cast<uint2*>(mine + 64 * j + 16 * q) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+        }
+      wave_lds_done();
+      rows_out<C>(stg, to + (size_t)m * pitch + col0, pitch, a.rows - m, a.f - col0, whole);
+      wave_lds_done();
+    };
+    out(a.h, a.f, [&](float g, float v) { return glu_act(a.act, g) * v; });
+    if (!a.ab) continue;
+    out(a.ab, 2 * (size_t)a.f, [](float g, float) { return g; });
+    out(a.ab + a.f, 2 * (size_t)a.f, [](float, float v) { return v; });
+  }
+}
+
+// sum over the 32 lanes of each half of the wave, in lanes 31 and 63
+__device__ __forceinline__ float half_sum(float v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+#define ACC_DPP(ctrl, rows) __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl, rows, 0xf, true))
+  v += ACC_DPP(0x111, 0xf);
+  v += ACC_DPP(0x112, 0xf);
+  v += ACC_DPP(0x114, 0xf);
+  v += ACC_DPP(0x118, 0xf);
+  v += ACC_DPP(0x142, 0xa);
+#undef ACC_DPP
+#endif
+  return v;
+}
+
+// The projections again, which leave as dz, and the columns' sums of a tile
+template <class C, int PARTS>
+__global__ __launch_bounds__(C::THREADS, 2) void glu_dz_kernel(PairArgs a, int blocks) {
+  typedef Stage<C> S;
+  constexpr int OUT = C::WM * C::WN * S::BYTES;
+  __shared__ __attribute__((aligned(1024))) char lds[C::LDS > OUT ? C::LDS : OUT];
+  const int at = xcd_tile(blocks);
+  if (at >= a.tiles) return;
+  const TileAt where = tile_at(at, a.tiles_m, a.tiles);
+  const int m0 = where.m * C::BM, n0 = where.n * (C::BN / 2);
+  GemmAcc<C> acc;
+  gemm_tile<C>(a.x, a.w, m0, n0, 0, a.d, lds, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm0 = (wave / C::WN) * 32 * C::MB, col0 = n0 + (wave % C::WN) * S::COLS;
+  if (a.bias) add_pair_bias<C>(acc, a.bias, col0, a.f);
+  char *const stg = lds + wave * S::BYTES, *const mine = stg + (lane & 31) * S::EP + 8 * (lane >> 5);
+  const bool whole = (a.f & 7) == 0;
+#pragma unroll
+  for (int i = 0; i < C::MB; ++i) {
+    const int m = m0 + wm0 + 32 * i;
+    rows_in<C>(stg, a.dh + (size_t)m * a.f + col0, a.f, a.rows - m, a.f - col0, whole);
+    wave_lds_done();
+#pragma unroll
+    for (int j = 0; j < C::NB / 2; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint2 w = *reinterpret_cast<const uint2*>(mine + 64 * j + 16 * q);
+        const float dh[4] = {__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u)};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float da, db;
+          glu_slopes(a.act, acc[i][2 * j][4 * q + e], acc[i][2 * j + 1][4 * q + e], dh[e], da, db);
+          const bool there = m + (lane & 31) < a.rows;         // (a row that isn't has the bias for its projections, and a dh of zero)
+          acc[i][2 * j][4 * q + e] = there ? da : 0.f;
+          acc[i][2 * j + 1][4 * q + e] = there ? db : 0.f;
+        }
+      }
+    wave_lds_done();
+  }
+  if (a.db_part) {
+    float* const to = a.db_part + (size_t)(where.m * C::WM + wave / C::WN) * a.pitch;
+#pragma unroll
+    for (int j = 0; j < C::NB; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        float t = 0.f;
+#pragma unroll
+        for (int i = 0; i < C::MB; ++i) t += acc[i][j][v];
+        t = half_sum(t);
+        const int n = col0 + 32 * (j >> 1) + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
+        if ((lane & 31) == 31 && n < a.half) to[n + (j & 1 ? a.half : 0)] = t;
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < C::MB; ++i) {
+    const int m = m0 + wm0 + 32 * i;
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+      for (int side = 0; side < 2; ++side) {
+#pragma unroll
+        for (int j = 0; j < C::NB / 2; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            v16f& p = acc[i][2 * j + side];
+            const uint2 w = make_uint2(pack_bf16(p[4 * q], p[4 * q + 1]), pack_bf16(p[4 * q + 2], p[4 * q + 3]));
+            *reinterpret_cast<uint2*>(mine + 64 * j + 16 * q) = w;
+            if (part + 1 < PARTS) {                    // what is left
+              p[4 * q] -= __uint_as_float(w.x << 16);
+              p[4 * q + 1] -= __uint_as_float(w.x & 0xffff0000u);
+              p[4 * q + 2] -= __uint_as_float(w.y << 16);
+              p[4 * q + 3] -= __uint_as_float(w.y & 0xffff0000u);
+            }
+          }
+        wave_lds_done();
+        rows_out<C>(stg, a.dz[part] + (size_t)m * a.pitch + col0 + (side ? a.half : 0), a.pitch, a.rows - m, a.half - col0, true);
+        wave_lds_done();
+      }
+  }
+}
+
+// out[split][rows][cols] = A B over the split's k, fp32, or rounded to bf16 where there is one split
+struct ProductArgs {
+  GemmOperand a, b;
+  float* sums;
+  bf16_t* out;                 // not null: here
+  int rows, cols, k, k_per_split, tiles_m, tiles, work;
+};
+template <class C>
+__device__ __forceinline__ void glu_product(const ProductArgs& a, int work, char* lds) {
+  static_assert(C::SWAP, "four columns of a row to a lane");
+  const int split = work / a.tiles;
+  const TileAt where = tile_at(work - split * a.tiles, a.tiles_m, a.tiles);
+  const int m0 = where.m * C::BM, n0 = where.n * C::BN;
+  GemmAcc<C> acc;
+  gemm_tile<C>(a.a, a.b, m0, n0, split * a.k_per_split, min(a.k, (split + 1) * a.k_per_split), lds, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm0 = (wave / C::WN) * 32 * C::MB, wn0 = (wave % C::WN) * 32 * C::NB;
+  const bool whole = (a.cols & 7) == 0;
+#pragma unroll
+  for (int i = 0; i < C::MB; ++i) {
+    const int m = m0 + wm0 + 32 * i + (lane & 31);
+#pragma unroll
+    for (int j = 0; j < C::NB; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int n = n0 + wn0 + 32 * j + 8 * q + 4 * (lane >> 5);
+        if (m >= a.rows || n >= a.cols) continue;
+        const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        if (a.out) {
+          bf16_t* const o = a.out + (size_t)m * a.cols + n;
+          if (whole) { *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])); continue; }
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (n + e < a.cols) Elem<bf16_t>::store(o + e, v[e]);
+        } else {
+          float* const o = a.sums + (size_t)split * a.rows * a.cols + (size_t)m * a.cols + n;
+          if (whole) { *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]); continue; }
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (n + e < a.cols) o[e] = v[e];
+        }
+      }
+  }
+}
+template <class C>
+__global__ __launch_bounds__(C::THREADS, 2) void glu_product_kernel(ProductArgs a, int blocks) {
+  __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
+  const int work = xcd_tile(blocks);
+  if (work < a.work) glu_product<C>(a, work, lds);
+}
+
+// dw[column of dz][d] = sum over the split's rows of dz x, dz as the sum of its parts
+struct GluDwArgs {
+  GemmOperand dz, x;
+  float* out;                  // [split][2 f][d]
+  int rows, d, f, half, per_split, tiles_m, tiles, work;
+};
+template <class C>
+__device__ __forceinline__ void glu_dw(const GluDwArgs& a, int work, char* lds) {
+  const int split = work / a.tiles;
+  const TileAt where = tile_at(work - split * a.tiles, a.tiles_m, a.tiles);
+  const int m0 = where.m * C::BM, n0 = where.n * C::BN, first = split * a.per_split, count = min(a.per_split, a.rows - first);
+  // (from the split's first row on: its rows take fewer than 4 GiB)
+  GemmOperand dz = a.dz, x = a.x;
+  dz.p = static_cast<const bf16_t*>(dz.p) + (size_t)first * dz.pitch;
+#pragma unroll
+  for (int p = 0; p + 1 < C::PARTS; ++p) dz.more[p] = static_cast<const bf16_t*>(dz.more[p]) + (size_t)first * dz.pitch;
+  x.p = static_cast<const bf16_t*>(x.p) + (size_t)first * x.pitch;
+  dz.rows = x.rows = count;
+  GemmAcc<C> acc;
+  gemm_tile<C>(dz, x, m0, n0, 0, count, lds, acc);
+  float* const out = a.out + (size_t)split * 2 * a.f * a.d;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm0 = (wave / C::WN) * 32 * C::MB, wn0 = (wave % C::WN) * 32 * C::NB;
+#pragma unroll
+  for (int i = 0; i < C::MB; ++i)
+#pragma unroll
+    for (int j = 0; j < C::NB; ++j) {
+      const int col = n0 + wn0 + 32 * j + (lane & 31);
+      if (col >= a.d) continue;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int m = m0 + wm0 + 32 * i + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3), side = m >= a.half ? 1 : 0, r = m - side * a.half;
+        if (r < a.f) out[(size_t)(r + side * a.f) * a.d + col] = acc[i][j][v];
+      }
+    }
+}
+template <class C>
+__global__ __launch_bounds__(C::THREADS, 2) void glu_dw_kernel(GluDwArgs a, int blocks) {
+  __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
+  const int work = xcd_tile(blocks);
+  if (work < a.work) glu_dw<C>(a, work, lds);
+}
+// dx and dw in one launch where there are few tiles: both wait for dz only
+template <class CX, class CW>
+__global__ __launch_bounds__(256, 2) void glu_grads_kernel(ProductArgs x, GluDwArgs w, int x_blocks, int w_blocks) {
+  static_assert(CX::THREADS == 256 && CW::THREADS == 256, "one shape of workgroups");
+  __shared__ __attribute__((aligned(1024))) char lds[CX::LDS > CW::LDS ? CX::LDS : CW::LDS];
+  const int block = blockIdx.x;                        // (each part begins at a multiple of eight)
+  if (block < x_blocks) {
+    const int work = (block & 7) * (x_blocks >> 3) + (block >> 3);
+    if (work < x.work) glu_product<CX>(x, work, lds);
+  } else {
+    const int work = (block & 7) * (w_blocks >> 3) + ((block - x_blocks) >> 3);
+    if (work < w.work) glu_dw<CW>(w, work, lds);
+  }
+}
+
+// out[r][0 .. pitch) = in[r][0 .. cols), then zeros; of 2 * split_row rows the second half goes to row r + gap, the `gap` rows before it and behind it are zero.  Eight
+// values per thread, read at any address.
+__global__ __launch_bounds__(256) void glu_pad_kernel(const bf16_t* __restrict__ in, bf16_t* __restrict__ out, size_t eights, int cols, int pitch, int split_row, int gap) {
+  typedef uint32_t any __attribute__((ext_vector_type(4), aligned(2)));
+  const size_t across = pitch / 8;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < eights; i += (size_t)gridDim.x * 256) {
+    const size_t to = i / across;
+    const int c = (int)(i - to * across) * 8;
+    const bool between = to >= (size_t)split_row && to < (size_t)split_row + gap;
+    const size_t r = to < (size_t)split_row ? to : to - gap;
+    const bf16_t* from = in + r * cols + c;
+    v4u v = {0, 0, 0, 0};
+    if (between || r >= 2 * (size_t)split_row) {       // (between the two and behind them)
+    } else if (c + 8 <= cols) {
+      const any q = *reinterpret_cast<const any*>(from);
+      v = v4u{q.x, q.y, q.z, q.w};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        v[e] = (c + 2 * e < cols ? (uint32_t)from[2 * e] : 0u) | (c + 2 * e + 1 < cols ? (uint32_t)from[2 * e + 1] << 16 : 0u);
+    }
+    *reinterpret_cast<v4u*>(out + i * 8) = v;
+  }
+}
+
+//                WM WN MB NB BK NS   AT     BT  PARTS SWAP  PAIR
+typedef GemmCfg<4, 2, 2, 4, 64, 2, false, false, 1, true, true> G256;      // gate and value
+typedef GemmCfg<2, 2, 2, 2, 64, 2, false, false, 1, true, true> G128;
+typedef GemmCfg<2, 1, 1, 2, 64, 4, false, false, 1, true, true> G64;
+typedef GemmCfg<2, 2, 2, 2, 64, 2, false, false, 1, true> S128;            // projections in parts
+typedef GemmCfg<2, 2, 1, 1, 64, 4, false, false, 1, true> S64;
+typedef GemmCfg<2, 4, 4, 2, 64, 2, false, true, 1, true> X256;             // dx
+typedef GemmCfg<2, 2, 2, 2, 64, 2, false, true, 1, true> X128;
+typedef GemmCfg<2, 2, 1, 1, 64, 4, false, true, 1, true> X64;
+typedef GemmCfg<2, 4, 4, 2, 32, 3, true, true, 2, false> W256;             // dw
+typedef GemmCfg<2, 2, 2, 2, 32, 2, true, true, 2, false> W128;
+typedef GemmCfg<2, 2, 1, 1, 32, 4, true, true, 2, false> W64;
+typedef GemmCfg<2, 4, 4, 2, 32, 2, true, true, 3, false> V256;             // dw with three parts of dz
+typedef GemmCfg<2, 2, 2, 2, 32, 2, true, true, 3, false> V128;
+typedef GemmCfg<2, 2, 1, 1, 32, 3, true, true, 3, false> V64;
+
+struct GluPlan16 {
+  int dp, fp;                  // widths as they are multiplied, multiples of 8
+  bool pad_x, pad_w;
+  int parts;                   // bf16 values that dz is the sum of
+  int tile;                    // of gate and value together
+  bool cut;                    // the projections' sums in parts, and what follows value by value
+  Choice proj, dx, dw;
+  bool together;               // dx and dw in one launch of 64 x 64 tiles
+  int db_parts;
+  size_t x, w, sums, dz[3], dx_sums, dw_sums, db, total;
+};
+
+GluPlan16 glu_plan16(int rows, int d, int f, bool backward, bool kept) {
+  GluPlan16 p{};
+  p.dp = (int)up(d, 8);
+  p.fp = (int)up(f, 8);
+  p.pad_x = p.dp != d;
+  p.pad_w = p.pad_x || p.fp != f;
+  p.parts = rows < 4096 ? 3 : 2;
+  const long wide = 2L * p.fp;
+  double us = 0;
+  for (int t = 0; t < 3; ++t) {
+    const double v = tile_us(RowsByRows, t, ceil_div(rows, kTiles[t]) * ceil_div(wide, kTiles[t]), p.dp / 64.0);
+    if (t == 0 || v < us) { us = v; p.tile = kTiles[t]; }
+  }
+  // few tiles of a long sum: parts of it, whose sums a second launch adds up
+  p.proj = choose(RowsByRows, rows, wide, p.dp, 1, 1L << 24, 128, 1);
+  p.cut = !kept && p.proj.splits > 1 && p.proj.us + 1.0 < us;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t a = at; at += al256(bytes); return a; };
+  p.x = take(p.pad_x ? (size_t)rows * p.dp * 2 : 0);
+  p.w = take(p.pad_w && !(kept && !backward) ? (size_t)wide * p.dp * 2 : 0);
+  p.sums = take(p.cut ? (size_t)p.proj.splits * rows * wide * 4 : 0);
+  if (backward) {
+    p.dx = choose(ByColumns, rows, d, wide, 1, 1L << 25, 256);
+    p.dw = choose(ByColumns, wide, d, rows, p.parts, 1L << 25, 128);
+    const Choice dx = choose(ByColumns, rows, d, wide, 1, 1L << 25, 256, 2), dw = choose(ByColumns, wide, d, rows, p.parts, 1L << 25, 128, 2);
+    p.together = ceil_div(d, 64) * (ceil_div(rows, 64) * dx.splits + ceil_div(wide, 64) * dw.splits) <= 1024;
+    if (p.together) { p.dx = dx; p.dw = dw; }
+    // rows of a part of dw: fewer than 4 GiB of dz and of x
+    const long most = (0xF0000000L / (2 * (wide > p.dp ? wide : p.dp))) / 64 * 64;
+    if (p.dw.k > most) {
+      p.dw.k = (int)most;
+      p.dw.splits = (int)ceil_div(rows, most);
+    }
+    for (int i = 0; i < p.parts; ++i) p.dz[i] = take((size_t)rows * wide * 2);
+    p.dx_sums = take(p.dx.splits > 1 ? (size_t)p.dx.splits * rows * d * 4 : 0);
+    p.dw_sums = take(p.dw.splits > 1 ? (size_t)p.dw.splits * 2 * f * d * 4 : 0);
+    PointArgs q{};
+    q.rows = rows; q.f = f;
+    p.db_parts = kept || p.cut ? glu_point_shape(q, DT_BF16) : (int)ceil_div(rows, p.tile) * (p.tile == 256 ? 4 : 2);
+    p.db = take((size_t)p.db_parts * wide * 4);
+  }
+  p.total = at;
+  return p;
+}
+
+unsigned whole_eights16(long work) { return (unsigned)((work + 7) / 8 * 8); }
+
+template <class C> void launch_pair(const PairArgs& g, bool backward, int parts, hipStream_t st) {
+  const unsigned blocks = whole_eights16(g.tiles);
+  if (!backward) hipLaunchKernelGGL(glu_fwd_kernel<C>, dim3(blocks), dim3(C::THREADS), 0, st, g, (int)blocks);
+  else if (parts == 3) hipLaunchKernelGGL((glu_dz_kernel<C, 3>), dim3(blocks), dim3(C::THREADS), 0, st, g, (int)blocks);
+  else hipLaunchKernelGGL((glu_dz_kernel<C, 2>), dim3(blocks), dim3(C::THREADS), 0, st, g, (int)blocks);
+}
+template <class C> void launch_product(const ProductArgs& g, hipStream_t st) {
+  const unsigned blocks = whole_eights16(g.work);
+  hipLaunchKernelGGL(glu_product_kernel<C>, dim3(blocks), dim3(C::THREADS), 0, st, g, (int)blocks);
+}
+template <class C> void launch_dw(const GluDwArgs& g, hipStream_t st) {
+  const unsigned blocks = whole_eights16(g.work);
+  hipLaunchKernelGGL(glu_dw_kernel<C>, dim3(blocks), dim3(C::THREADS), 0, st, g, (int)blocks);
+}
+
+}  // namespace
+
+size_t glu_bf16_workspace_bytes(int rows, int d, int f, bool backward) {
+  const size_t again = glu_plan16(rows, d, f, backward, false).total, kept = backward ? glu_plan16(rows, d, f, true, true).total : 0;
+  return again > kept ? again : kept;
+}
+
+hipError_t glu_bf16(const GluArgs& a, bool backward) {
+  const bool kept = backward && a.ab_in;
+  const GluPlan16 p = glu_plan16(a.rows, a.d, a.f, backward, kept);
+  hipStream_t st = a.st;
+  const bf16_t *x = (const bf16_t*)a.x, *w = (const bf16_t*)a.w;
+  auto pad = [&](const bf16_t* in, size_t at, long rows_out, int split_row, int gap) {
+    const size_t eights = (size_t)rows_out * p.dp / 8;
+    const unsigned blocks = (unsigned)(eights / 256 + 1 < 4096 ? eights / 256 + 1 : 4096);
+    hipLaunchKernelGGL(glu_pad_kernel, dim3(blocks), dim3(256), 0, st, in, (bf16_t*)(a.ws + at), eights, a.d, p.dp, split_row, gap);
+    return (const bf16_t*)(a.ws + at);
+  };
+  if (p.pad_x && (!kept || a.dw)) x = pad(x, p.x, a.rows, a.rows, 0);
+  if (p.pad_w && (!kept || a.dx)) w = pad(w, p.w, 2L * p.fp, a.f, p.fp - a.f);
+  const int wide = 2 * p.fp;
+  bf16_t* dz[3] = {(bf16_t*)(a.ws + p.dz[0]), (bf16_t*)(a.ws + p.dz[1]), (bf16_t*)(a.ws + p.dz[2])};
+  float* const db_part = backward && a.db ? (float*)(a.ws + p.db) : nullptr;
+  const int parts = !a.dw ? 1 : p.parts;
+  if (kept || p.cut) {
+    PointArgs q{};
+    q.ab_in = a.ab_in; q.dh = a.dh; q.h = a.h; q.ab = a.ab;
+    q.rows = a.rows; q.f = a.f; q.act = a.act; q.half = p.fp; q.pitch = wide;
+    for (int i = 0; i < 3; ++i) q.dz[i] = dz[i];
+    q.db_part = db_part;
+    if (!kept) {
+      ProductArgs g{};
+      g.a = GemmOperand{x, {}, a.rows, p.dp, p.dp};
+      g.b = GemmOperand{w, {}, wide, p.dp, p.dp};
+      g.sums = (float*)(a.ws + p.sums);
+      g.rows = a.rows; g.cols = wide; g.k = p.dp; g.k_per_split = p.proj.k;
+      g.tiles_m = (int)ceil_div(a.rows, p.proj.tile); g.tiles = g.tiles_m * (int)ceil_div(wide, p.proj.tile); g.work = g.tiles * p.proj.splits;
+      if (p.proj.tile == 128) launch_product<S128>(g, st);
+      else launch_product<S64>(g, st);
+      q.sums = g.sums; q.splits = p.proj.splits; q.bias = a.bias;
+    }
+    glu_point_shape(q, DT_BF16);
+    if (const hipError_t e = glu_point(q, backward, parts, DT_BF16, st); e != hipSuccess || !backward) return e;
+  } else {
+    PairArgs g{};
+    g.x = GemmOperand{x, {}, a.rows, p.dp, p.dp};
+    g.w = GemmOperand{w, {w + (size_t)p.fp * p.dp}, a.f, p.dp, p.dp};
+    g.bias = a.bias;
+    g.rows = a.rows; g.d = p.dp; g.f = a.f; g.act = a.act;
+    g.tiles_m = (int)ceil_div(a.rows, p.tile); g.tiles = g.tiles_m * (int)ceil_div(p.fp, p.tile / 2);
+    g.h = (bf16_t*)a.h; g.ab = (bf16_t*)a.ab; g.dh = (const bf16_t*)a.dh;
+    for (int i = 0; i < 3; ++i) g.dz[i] = dz[i];
+    g.pitch = wide; g.half = p.fp; g.db_part = db_part;
+    if (p.tile == 256) launch_pair<G256>(g, backward, p.parts, st);
+    else if (p.tile == 128) launch_pair<G128>(g, backward, p.parts, st);
+    else launch_pair<G64>(g, backward, p.parts, st);
+    if (!backward) return hipGetLastError();
+  }
+  const GemmOperand z{dz[0], {dz[1], dz[2]}, a.rows, wide, wide};
+  ProductArgs gx{};
+  GluDwArgs gw{};
+  GluFinish f{};
+  if (a.dx) {
+    gx.a = z;
+    gx.b = GemmOperand{w, {}, wide, p.dp, p.dp};
+    gx.sums = (float*)(a.ws + p.dx_sums); gx.out = p.dx.splits > 1 ? nullptr : (bf16_t*)a.dx;
+    gx.rows = a.rows; gx.cols = a.d; gx.k = wide; gx.k_per_split = p.dx.k;
+    gx.tiles_m = (int)ceil_div(a.rows, p.dx.tile); gx.tiles = gx.tiles_m * (int)ceil_div(a.d, p.dx.tile); gx.work = gx.tiles * p.dx.splits;
+    if (p.dx.splits > 1) { f.dx_sums = gx.sums; f.dx = a.dx; f.dx_count = (size_t)a.rows * a.d; f.dx_splits = p.dx.splits; }
+  }
+  if (a.dw) {
+    gw.dz = z;
+    gw.x = GemmOperand{x, {}, a.rows, p.dp, p.dp};
+    gw.out = p.dw.splits > 1 ? (float*)(a.ws + p.dw_sums) : a.dw;
+    gw.rows = a.rows; gw.d = a.d; gw.f = a.f; gw.half = p.fp; gw.per_split = p.dw.k;
+    gw.tiles_m = (int)ceil_div(wide, p.dw.tile); gw.tiles = gw.tiles_m * (int)ceil_div(a.d, p.dw.tile); gw.work = gw.tiles * p.dw.splits;
+    if (p.dw.splits > 1) { f.dw_sums = gw.out; f.dw = a.dw; f.dw_count = 2 * (size_t)a.f * a.d; f.dw_splits = p.dw.splits; }
+  }
+  if (p.together) {
+    const unsigned bx = whole_eights16(gx.work), bw = whole_eights16(gw.work);
+    if (bx + bw == 0) {
+    } else if (p.parts == 3) hipLaunchKernelGGL((glu_grads_kernel<X64, V64>), dim3(bx + bw), dim3(256), 0, st, gx, gw, (int)bx, (int)bw);
+    else hipLaunchKernelGGL((glu_grads_kernel<X64, W64>), dim3(bx + bw), dim3(256), 0, st, gx, gw, (int)bx, (int)bw);
+  } else {
+    if (a.dx) {
+      if (p.dx.tile == 256) launch_product<X256>(gx, st);
+      else if (p.dx.tile == 128) launch_product<X128>(gx, st);
+      else launch_product<X64>(gx, st);
+    }
+    if (a.dw) {
+      if (p.parts == 3) { if (p.dw.tile == 256) launch_dw<V256>(gw, st); else if (p.dw.tile == 128) launch_dw<V128>(gw, st); else launch_dw<V64>(gw, st); }
+      else { if (p.dw.tile == 256) launch_dw<W256>(gw, st); else if (p.dw.tile == 128) launch_dw<W128>(gw, st); else launch_dw<W64>(gw, st); }
+    }
+  }
+  if (a.db) { f.db_part = db_part; f.db = a.db; f.db_parts = p.db_parts; f.pitch = wide; f.half = p.fp; f.f = a.f; }
+  return glu_finish(f, DT_BF16, st);
+}
+
+}  // namespace acc

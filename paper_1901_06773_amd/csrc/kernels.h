@@ -265,6 +265,12 @@ size_t linear_ce_workspace_bytes(int n, int d, int classes, int gradients, int d
 hipError_t linear_ce(const void* x, const void* w, const float* bias, const int32_t* labels, int ignore, float* loss_rows,
                      float* loss, void* dx, float* dw, float* db, int n, int d, int classes, void* workspace,
                      size_t workspace_bytes, int dtype, hipStream_t st);
+// A gated linear layer and its gradients (glu.hip); bias, ab, dx, dw and db may each be null.
+size_t glu_workspace_bytes(int rows, int d, int f, int backward, int dtype);
+hipError_t glu_forward(const void* x, const void* w, const float* bias, void* h, void* ab, int rows, int d, int f, int act, void* workspace,
+                       size_t workspace_bytes, int dtype, hipStream_t st);
+hipError_t glu_backward(const void* x, const void* w, const float* bias, const void* ab, const void* dh, void* dx, float* dw, float* db, int rows, int d,
+                        int f, int act, void* workspace, size_t workspace_bytes, int dtype, hipStream_t st);
 // The k largest logits of each row with their classes (top_logits.hip).
 size_t top_logits_workspace_bytes(int n, int classes, int k, int dtype);
 hipError_t top_logits(const void* z, int32_t* index, float* top, int n, int classes, int k, void* workspace, size_t workspace_bytes, int dtype,

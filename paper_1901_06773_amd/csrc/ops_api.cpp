@@ -294,6 +294,37 @@ extern "C" int acc_op_linear_ce(const void* x, const void* w, const float* bias,
               "acc_op_linear_ce_workspace()");
 }
 
+extern "C" size_t acc_op_glu_workspace(int rows, int d, int f, int backward, int dtype) { return glu_workspace_bytes(rows, d, f, backward, dtype); }
+
+extern "C" int acc_op_glu_fwd(const void* x, const void* w, const float* bias, void* h, void* ab, int rows, int d, int f, int act, void* workspace,
+                              size_t workspace_bytes, int dtype, void* stream) {
+  if (!dtype_ok(dtype)) return refuse("acc_op_glu_fwd: dtype must be ACC_F32 or ACC_BF16");
+  if (!al16({x, w, bias, h, ab, workspace})) return refuse("acc_op_glu_fwd: pointers must be 16-byte aligned");
+  if (sizes_ok(rows, d, 1) && sizes_ok(rows, f, 1)) {
+    const size_t es = dt_size(dtype), nh = (size_t)rows * f * es;
+    if (clash({{h, nh, {}}, {ab, 2 * nh, {}}, {workspace, workspace_bytes, {}}},
+              {{x, (size_t)rows * d * es, {}}, {w, 2 * (size_t)f * d * es, {}}, {bias, 2 * (size_t)f * 4, {}}}))
+      return refuse("acc_op_glu_fwd: what is written overlaps another argument");
+  }
+  return told(glu_forward(x, w, bias, h, ab, rows, d, f, act, workspace, workspace_bytes, dtype, (hipStream_t)stream),
+              "acc_op_glu_fwd: null pointer, sizes that are not positive or too large, unknown act or a workspace smaller than acc_op_glu_workspace()");
+}
+
+extern "C" int acc_op_glu_bwd(const void* x, const void* w, const float* bias, const void* ab, const void* dh, void* dx, float* dw, float* db, int rows, int d,
+                              int f, int act, void* workspace, size_t workspace_bytes, int dtype, void* stream) {
+  if (!dtype_ok(dtype)) return refuse("acc_op_glu_bwd: dtype must be ACC_F32 or ACC_BF16");
+  if (!al16({x, w, bias, ab, dh, dx, dw, db, workspace})) return refuse("acc_op_glu_bwd: pointers must be 16-byte aligned");
+  if (sizes_ok(rows, d, 1) && sizes_ok(rows, f, 1)) {
+    const size_t es = dt_size(dtype), nx = (size_t)rows * d * es, nh = (size_t)rows * f * es, nw = 2 * (size_t)f * d, nb = 2 * (size_t)f * 4;
+    if (clash({{dx, nx, {}}, {dw, nw * 4, {}}, {db, nb, {}}, {workspace, workspace_bytes, {}}},
+              {{x, nx, {}}, {w, nw * es, {}}, {ab ? nullptr : bias, nb, {}}, {ab, 2 * nh, {}}, {dh, nh, {}}}))
+      return refuse("acc_op_glu_bwd: what is written overlaps another argument");
+  }
+  return told(glu_backward(x, w, bias, ab, dh, dx, dw, db, rows, d, f, act, workspace, workspace_bytes, dtype, (hipStream_t)stream),
+              "acc_op_glu_bwd: null pointer, no result asked for, sizes that are not positive or too large, unknown act or a workspace smaller than "
+              "acc_op_glu_workspace()");
+}
+
 extern "C" size_t acc_op_top_logits_workspace(int n, int classes, int k, int dtype) { return top_logits_workspace_bytes(n, classes, k, dtype); }
 
 extern "C" int acc_op_top_logits(const void* z, int32_t* index, float* top, int n, int classes, int k, void* workspace, size_t workspace_bytes, int dtype,

@@ -1,0 +1,257 @@
+"""The gated linear layer against its formulas in 64 bits.
+
+Tolerances.  A projection of d <= 4096 products is off by fewer than 2^-24 (2 d^(1/2) + 8) < 8e-6 of the sum of their sizes (roundings at random; the split
+fp32 products leave out 2^-21 at most): 1e-5.  The activation and its slope are known to 2^-20 of themselves and move by at most 1.1 times what the gate moves (the slope by
+half of that).  From there errors are added up as sizes: of h, and of dz = [da | db], which is held to 2^-8 of itself for the dx of bf16 operands, to
+2^-16 for their dw and to 2^-24 otherwise, through both products, whose own sums are known to 1e-5 of their sizes; results in bf16 are rounded to
+2^-8.  Where a gate lies within its error of 0 the slope of a ReLU is either.  Sums of sizes are far from what errors at random add up to, so whole
+tensors are held, as norms, to 2e-5 as well (dx in bf16: to 2^-7, a rounding of dz and one of its own)."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+ACT = {"none": 0, "relu": 1, "silu": 2}
+E = 1e-5
+
+
+def B():
+    from paper_1901_06773_amd import binding
+    return binding
+
+
+def inputs(rows, d, f, dtype, seed=1, bias=True):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    def r(*shape):
+        return torch.randn(*shape, generator=g, device="cuda")
+    return r(rows, d).to(DT[dtype]), (r(2 * f, d) / d ** 0.5).to(DT[dtype]), 0.3 * r(2 * f) if bias else None, r(rows, f).to(DT[dtype])
+
+
+def workspace(rows, d, f, backward, dtype):
+    size = B().op_glu_workspace(rows, d, f, backward, B().F32 if dtype == "f32" else B().BF16)
+    return torch.full((size,), 255, dtype=torch.uint8, device="cuda") if size else None      # NaN wherever something is read that was not written
+
+
+def forward(x, w, bias, act, dtype, keep=True):
+    rows, d, f = x.shape[0], x.shape[1], w.shape[0] // 2
+    h = torch.full((rows, f), float("nan"), device="cuda", dtype=x.dtype)
+    ab = torch.full((rows, 2 * f), float("nan"), device="cuda", dtype=x.dtype) if keep else None
+    B().op_glu_fwd(x, w, bias, h, ab, ACT[act], workspace(rows, d, f, False, dtype))
+    return h, ab
+
+
+def backward(x, w, bias, ab, dh, act, dtype, want=("dx", "dw", "db")):
+    rows, d, f = x.shape[0], x.shape[1], w.shape[0] // 2
+    nan = float("nan")
+    out = dict(dx=torch.full_like(x, nan), dw=torch.full((2 * f, d), nan, device="cuda"), db=torch.full((2 * f,), nan, device="cuda"))
+    out = {k: v if k in want else None for k, v in out.items()}
+    B().op_glu_bwd(x, w, bias, ab, dh, out["dx"], out["dw"], out["db"], ACT[act], workspace(rows, d, f, True, dtype))
+    return out
+
+
+def curve(a, act):
+    if act == "relu":
+        return a.clamp(min=0), (a > 0).double()
+    if act == "silu":
+        s = torch.sigmoid(a)
+        return a * s, s * (1 + a * (1 - s))
+    return a, torch.ones_like(a)
+
+
+def projections(x, w, bias):
+    p, size = x.double() @ w.double().T, x.double().abs() @ w.double().abs().T
+    return (p, size) if bias is None else (p + bias.double(), size + bias.double().abs())
+
+
+def near(got, ref, bound, what, norm=None):
+    assert torch.isfinite(got).all(), what
+    off = (got.double() - ref).abs()
+    assert (off <= bound + 1e-37).all(), (what, float((off - bound).max()), int((off - bound).argmax()))
+    if norm is not None and ref.numel() > 64:
+        assert off.norm() <= norm * ref.norm() + 1e-30, (what, float(off.norm() / ref.norm()))
+
+
+def check_forward(x, w, bias, act, dtype, keep=True):
+    h, ab = forward(x, w, bias, act, dtype, keep)
+    half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    p, size = projections(x, w, bias)
+    a, b = p.chunk(2, 1)
+    va, sb = curve(a, act)[0], E * size[:, w.shape[0] // 2:]
+    sa = 1.1 * E * size[:, :w.shape[0] // 2] + 2.0 ** -20 * va.abs()
+    bound = sa * (b.abs() + sb) + va.abs() * sb
+    near(h, va * b, bound + half * ((va * b).abs() + bound), "h", 2.0 ** -8 + 2e-5 if dtype == "bf16" else 2e-5)
+    if keep:
+        near(ab, p, E * size + half * (p.abs() + E * size), "ab", 2.0 ** -8 + 2e-5 if dtype == "bf16" else 2e-5)
+    return ab
+
+
+def check_backward(x, w, bias, ab, dh, act, dtype):
+    f = w.shape[0] // 2
+    got = backward(x, w, bias, ab, dh, act, dtype)
+    if ab is None:
+        p, size = projections(x, w, bias)
+        size = E * size
+    else:
+        p, size = ab.double(), torch.zeros(ab.shape, dtype=torch.float64, device="cuda")
+    a, b, ea, eb, g = *p.chunk(2, 1), *size.chunk(2, 1), dh.double()
+    v, s = curve(a, act)
+    dz = torch.cat([g * b * s, g * v], 1)
+    es = torch.where(a.abs() <= ea, 1.0, 0.0) if act == "relu" else 0.5 * ea + 2.0 ** -20 * (s.abs() + 1e-3) + 2.0 ** -20 * (a * s).abs()
+    err = torch.cat([g.abs() * (eb * (s.abs() + es) + b.abs() * es), g.abs() * (1.1 * ea + 2.0 ** -20 * v.abs())], 1) + 2.0 ** -22 * dz.abs()
+    x64, w64 = x.double(), w.double()
+    one, more, half = (2.0 ** -8, 2.0 ** -16, 2.0 ** -8) if dtype == "bf16" else (2.0 ** -24, 2.0 ** -24, 2.0 ** -24)
+    dx, dw, db = dz @ w64, dz.T @ x64, dz.sum(0)
+    ex = (err + (one + E) * dz.abs()) @ w64.abs()
+    near(got["dx"], dx, ex + half * (dx.abs() + ex), "dx", 2.0 ** -7 + 2e-5 if dtype == "bf16" else 2e-5)
+    near(got["dw"], dw, (err + (more + E) * dz.abs()).T @ x64.abs() + 2.0 ** -24 * dw.abs(), "dw", 2.0 ** -16 + 2e-5)
+    near(got["db"], db, err.sum(0) + E * dz.abs().sum(0) + 2.0 ** -24 * db.abs(), "db", 2e-5 * 4 if act == "relu" else 2e-5)
+
+
+# one row, one value; up to four rows and more; widths of no whole eights and odd ones; each tile, sums that are cut, several launches or one; two and three
+# parts of dz on both sides of 4096 rows
+SIZES = [(1, 1, 1), (1, 8, 8), (2, 3, 5), (3, 512, 100), (4, 24, 1), (4, 2050, 37), (5, 16, 16), (5, 2, 9), (1, 4096, 33), (9, 4096, 40), (7, 1160, 1003),
+         (64, 64, 64), (65, 72, 57), (130, 96, 200), (257, 264, 130), (300, 40, 1000), (1000, 17, 3), (33, 1027, 129), (31, 2048, 16), (512, 512, 512),
+         (2009, 100, 65), (4095, 32, 24), (4096, 32, 24), (4100, 64, 40), (5001, 9, 11), (8192, 256, 1024), (3000, 1024, 512), (16400, 64, 520), (20000, 1, 1)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,d,f", SIZES)
+def test_against_the_formulas(rows, d, f, dtype):
+    for act, bias in (("silu", True), ("relu", False), ("none", True)):
+        x, w, b, dh = inputs(rows, d, f, dtype, bias=bias)
+        ab = check_forward(x, w, b, act, dtype)
+        check_backward(x, w, b, None, dh, act, dtype)
+        check_backward(x, w, b, ab, dh, act, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,d,f", [(3, 40, 30), (70, 520, 65), (4200, 33, 20), (900, 256, 512)])
+def test_results_one_by_one_and_again(rows, d, f, dtype):
+    x, w, b, dh = inputs(rows, d, f, dtype)
+    h, ab = forward(x, w, b, "silu", dtype)
+    assert torch.equal(forward(x, w, b, "silu", dtype, keep=False)[0], h)
+    for kept in (None, ab):
+        got = backward(x, w, b, kept, dh, "silu", dtype)
+        for _ in range(2):
+            again = backward(x, w, b, kept, dh, "silu", dtype)
+            assert all(torch.equal(again[k], got[k]) for k in got)
+        for k in got:
+            assert torch.equal(backward(x, w, b, kept, dh, "silu", dtype, want=(k,))[k], got[k]), k
+    # the bias of kept projections is not looked at
+    assert all(torch.equal(v, got[k]) for k, v in backward(x, w, torch.full_like(b, float("nan")), ab, dh, "silu", dtype).items())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,d,f", [(3, 37, 29), (65, 57, 91), (4200, 33, 20), (700, 256, 520)])
+def test_nothing_is_written_behind_the_results(rows, d, f, dtype):
+    x, w, b, dh = inputs(rows, d, f, dtype)
+    behind = 4096
+
+    def buffer(count, dt):
+        return torch.full((count + behind,), 77, device="cuda", dtype=dt)
+    sizes = [B().op_glu_workspace(rows, d, f, back, B()._dtype_of(x)) for back in (False, True)]
+    ws = [buffer(s, torch.uint8) for s in sizes]
+    h, ab, dx, dw, db = buffer(rows * f, x.dtype), buffer(rows * 2 * f, x.dtype), buffer(rows * d, x.dtype), buffer(2 * f * d, torch.float32), buffer(2 * f, torch.float32)
+    B().op_glu_fwd(x, w, b, h[:rows * f].view(rows, f), ab[:rows * 2 * f].view(rows, 2 * f), 2, ws[0][:sizes[0]] if sizes[0] else None)
+    for kept in (None, ab[:rows * 2 * f].view(rows, 2 * f)):
+        B().op_glu_bwd(x, w, b, kept, dh, dx[:rows * d].view(rows, d), dw[:2 * f * d].view(2 * f, d), db[:2 * f], 2, ws[1][:sizes[1]])
+    assert all((t[-behind:] == 77).all() for t in (h, ab, dx, dw, db, *ws))
+
+
+@pytest.mark.parametrize("rows,d,f,act", [(6, 20, 10, "silu"), (70, 33, 17, "silu"), (40, 16, 24, "none")])
+def test_gradient_against_differences(rows, d, f, act):
+    # the sum of dh h along a direction: its central difference is off by h^2 / 6 times the third derivative and by 2^-24 of the sizes of h over h, both of
+    # which the bound below counts (|act'''| <= 1, directions of unit values: three factors of a projection's slope)
+    x, w, b, dh = inputs(rows, d, f, "f32")
+    got = backward(x, w, b, None, dh, act, "f32")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    step = 2.0 ** -6
+    for k, t in (("dx", x), ("dw", w), ("db", b)):
+        v = torch.zeros_like(t).view(-1)
+        v[torch.randint(t.numel(), (3,), generator=g, device="cuda")] = 1.0
+        v = v.view(t.shape)
+
+        def total(sign):
+            moved = [u + sign * step * v if u is t else u for u in (x, w, b)]
+            return float((forward(*moved, act, "f32", keep=False)[0].double() * dh.double()).sum())
+        size = float((dh.double().abs() * forward(x, w, b, act, "f32", keep=False)[0].double().abs()).sum())
+        reach = float(dh.abs().max() * (x.abs().max() + 1) ** 3 * 27 * (max(rows, f) + 1))
+        assert abs((total(1) - total(-1)) / (2 * step) - float((got[k].double() * v).sum())) <= step ** 2 / 6 * reach + 2.0 ** -20 * size / step, k
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,d,f", [(4, 64, 32), (70, 64, 40), (300, 512, 256)])
+def test_values_that_are_not_finite(rows, d, f, dtype):
+    x, w, b, dh = inputs(rows, d, f, dtype)
+    x[1, 3] = float("nan")
+    x[2, 5] = float("inf")
+    h, ab = forward(x, w, b, "silu", dtype)
+    assert torch.isnan(h[1]).all() and torch.isnan(ab[1]).all()
+    assert not torch.isfinite(ab[2]).any() and not torch.isfinite(h[2]).all()
+    others = [r for r in range(rows) if r not in (1, 2)]
+    assert torch.isfinite(h[others]).all() and torch.isfinite(ab[others]).all()
+    got = backward(x, w, b, None, dh, "none", dtype)
+    assert torch.isfinite(got["dx"][others]).all() and not torch.isfinite(got["dx"][1]).any()
+    # large gates: no overflow on the way
+    x, w, b, dh = inputs(rows, d, f, dtype)
+    b[:f] = torch.where(torch.arange(f, device="cuda") % 2 == 0, 3e4, -3e4)
+    h, _ = forward(x, w, b, "silu", dtype)
+    assert torch.isfinite(h).all() and (h[:, 1::2] == 0).all()
+    got = backward(x, w, b, None, dh, "silu", dtype)
+    assert all(torch.isfinite(v).all() for v in got.values())
+
+
+def test_offsets_beyond_32_bits():
+    rows, d, f = 300000, 16, 4096                       # 4.9 GB of kept projections and as much of each part of dz
+    x, w, b, _ = inputs(rows, d, f, "bf16")
+    dh = torch.zeros(rows, f, device="cuda", dtype=torch.bfloat16)
+    at = torch.tensor([0, 1, 70000, 140000, 262143, 262144, 299999], device="cuda")
+    dh[at] = torch.randn(len(at), f, device="cuda").to(torch.bfloat16)
+    h, ab = forward(x, w, b, "silu", "bf16")
+    p, _ = projections(x[at], w, b)
+    a, v = p.chunk(2, 1)
+    assert (h[at].double() - a * torch.sigmoid(a) * v).norm() <= (2.0 ** -8 + 2e-5) * (a * torch.sigmoid(a) * v).norm()
+    assert (ab[at].double() - p).norm() <= (2.0 ** -8 + 2e-5) * p.norm()
+    for kept in (ab, None):
+        got = backward(x, w, b, kept, dh, "silu", "bf16")
+        q = ab[at].double() if kept is not None else p
+        a, v = q.chunk(2, 1)
+        value, slope = curve(a, "silu")
+        dz = torch.cat([dh[at].double() * v * slope, dh[at].double() * value], 1)
+        assert (got["dx"][at].double() - dz @ w.double()).norm() <= (2.0 ** -7 + 2e-5) * (dz @ w.double()).norm()
+        assert (got["dw"].double() - dz.T @ x[at].double()).norm() <= (2.0 ** -16 + 2e-5) * (dz.T @ x[at].double()).norm()
+        assert (got["db"].double() - dz.sum(0)).norm() <= 2e-5 * dz.abs().sum(0).norm()
+        assert (got["dx"].float().abs().sum(1) != 0).sum() == len(at)
+        del got
+
+
+def test_replayed_and_on_another_stream():
+    rows, d, f = 300, 520, 260
+    x, w, b, dh = inputs(rows, d, f, "bf16")
+    h, ab, dx = torch.empty_like(dh), torch.empty(rows, 2 * f, dtype=x.dtype, device="cuda"), torch.empty_like(x)
+    dw, db = torch.empty(2 * f, d, device="cuda"), torch.empty(2 * f, device="cuda")
+    ws = [workspace(rows, d, f, back, "bf16") for back in (False, True)]
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=other):
+        B().op_glu_fwd(x, w, b, h, ab, 2, ws[0])
+        B().op_glu_bwd(x, w, b, ab, dh, dx, dw, db, 2, ws[1])
+    for seed in (2, 3, 4):
+        for to, v in zip((x, w, b, dh), inputs(rows, d, f, "bf16", seed=seed)):
+            to.copy_(v)
+        graph.replay()
+        torch.cuda.synchronize()
+        h2, ab2 = forward(x, w, b, "silu", "bf16")
+        got = backward(x, w, b, ab2, dh, "silu", "bf16")
+        assert torch.equal(h, h2) and torch.equal(ab, ab2) and all(torch.equal(v, got[k]) for k, v in (("dx", dx), ("dw", dw), ("db", db)))
+
+
+def test_maps_as_they_lie():
+    n, hw, d, f = 3, 7, 64, 48
+    x, w, b, dh = inputs(n * hw * hw, d, f, "bf16")
+    h = torch.empty(n, hw, hw, f, device="cuda", dtype=x.dtype)
+    B().op_glu_fwd(x.view(n, hw, hw, d), w, b, h, None, 2, workspace(n * hw * hw, d, f, False, "bf16"))
+    assert torch.equal(h.view(-1, f), forward(x, w, b, "silu", "bf16")[0])
