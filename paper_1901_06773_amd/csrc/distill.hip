@@ -48,16 +48,29 @@ struct DistillArgs {
 __device__ __forceinline__ bool row_counts(const DistillArgs& a, int row) {
   return a.labels ? a.ignore == INT_MIN || a.labels[row] != a.ignore : a.index[(size_t)row * a.k] >= 0;
 }
-// Rows that count among all, by NT threads; sh: NT / 64 numbers
-template <int NT> __device__ __forceinline__ int counted(const DistillArgs& a, int* sh) {
+// Rows that count among all: a thread's part of NT threads'
+template <int NT> __device__ __forceinline__ int count_part(const DistillArgs& a) {
   int c = 0;
   if (a.counts) {
     for (int i = threadIdx.x % NT; i < a.count_parts; i += NT) c += a.counts[i];
   } else {
+#pragma unroll 4
     for (int i = threadIdx.x % NT; i < a.n; i += NT) c += row_counts(a, i) ? 1 : 0;
   }
-  return row_reduce<NT>(c, sh, [](int x, int y) { return x + y; });
+  return c;
 }
+struct Add {
+  template <class V> __device__ __forceinline__ V operator()(V x, V y) const { return x + y; }
+};
+struct Larger {
+  __device__ __forceinline__ float operator()(float x, float y) const { return fmaxf(x, y); }
+};
+template <int NT> struct RowShared {
+  float v[4][NT / 64];
+  int count[NT / 64], length;
+};
+// words of LDS for a list: four arrays
+__host__ __device__ __forceinline__ int list_pitch(int k) { return (k + 3) & ~3; }
 
 // The list of a row, by one wave: probabilities and classes into LDS, and what the loss needs of them.
 struct List {
@@ -84,9 +97,9 @@ __device__ __forceinline__ List read_list(const DistillArgs& a, int row, int32_t
     }
     if (ends) break;
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+  mx = wave_reduce(mx, Larger());
   l.bad = __any(l.bad);
+  if (lane < (4 - (l.length & 3)) % 4) cls[l.length + lane] = -1;        // (write_listed() looks at four at a time)
   float s = 0.f, equal = 0.f;
   for (int j = lane; j < l.length; j += 64) {
     const float t = p[j];
@@ -94,8 +107,8 @@ __device__ __forceinline__ List read_list(const DistillArgs& a, int row, int32_t
     equal += is_top ? 1.f : 0.f;
     s += is_top ? 0.f : expf((t - mx) * a.inv_t);
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) { s += __shfl_xor(s, o); equal += __shfl_xor(equal, o); }
+  s = wave_reduce(s, Add());
+  equal = wave_reduce(equal, Add());
   const float rest = fabsf(mx) == INFINITY ? NAN : s + (equal - 1.f), inv = 1.f / (1.f + rest), log_sum = log1pf(rest);
   float h = 0.f;
   for (int j = lane; j < l.length; j += 64) {
@@ -104,9 +117,7 @@ __device__ __forceinline__ List read_list(const DistillArgs& a, int row, int32_t
     rest_of[j] = (rest - expm1f(v)) * inv;             // 1 - p
     h += e == 0.f ? 0.f : e * inv * (v - log_sum);
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) h += __shfl_xor(h, o);
-  l.entropy = h;
+  l.entropy = wave_reduce(h, Add());
   return l;
 }
 
@@ -121,8 +132,7 @@ __device__ __forceinline__ float loss_of(const DistillArgs& a, const List& l, co
   if (l.length) {
     float d = 0.f;
     for (int j = lane; j < l.length; j += 64) d += p[j] == 0.f ? 0.f : p[j] * ((z_of[j] - r.max) * a.inv_t);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) d += __shfl_xor(d, o);
+    d = wave_reduce(d, Add());
     loss = a.soft * (l.entropy - d + log1pf(r.rest));
     if (l.bad) loss = NAN;
   }
@@ -155,14 +165,20 @@ __device__ __forceinline__ void write_listed(const DistillArgs& a, T* dz, int lo
     if (c < lo || c >= hi) continue;
     // a class that is listed more than once has all of its entries' probabilities, by the first one
     float sum = j < length ? p[j] : 0.f;
-    int times = 1;
-    bool first = true;
-    for (int i = 0; i < length; ++i) {
-      const bool same = cls[i] == c;
-      first = first && !(same && i < j);
-      if (same && i > j) { sum += p[i]; ++times; }
+    int times = 0;
+    for (int i = 0; i < length; i += 4) {
+      const int4 q = *reinterpret_cast<const int4*>(cls + i);
+      times += (q.x == c ? 1 : 0) + (q.y == c ? 1 : 0) + (q.z == c ? 1 : 0) + (q.w == c ? 1 : 0);
     }
-    if (!first) continue;
+    if (times > (j < length ? 1 : 0)) {
+      bool first = true;
+      for (int i = 0; i < length; ++i) {
+        const bool same = cls[i] == c;
+        first = first && !(same && i < j);
+        if (same && i > j) sum += p[i];
+      }
+      if (!first) continue;
+    }
     const float z = j < length ? z_of[j] : z_label, d = z - r.max;
     float v = 0.f;
     if (length) {
@@ -187,9 +203,9 @@ __device__ __forceinline__ void add_chunk(const chunk16& q, float max, float inv
   }
 }
 
-// A row by NT threads, CH chunks each.  lists: 4 k words of LDS.
+// A row by NT threads, CH chunks each.  lists: 4 list_pitch(k) words of LDS.
 template <class T, int NT, int CH, bool HARD>
-__device__ __forceinline__ void distill_row(const DistillArgs& a, int row, float inv_rows, float* lists, float (*sh)[NT / 64]) {
+__device__ __forceinline__ void distill_row(const DistillArgs& a, int row, float* lists, RowShared<NT>& sh) {
   typedef RowChunks<T> Row;
   const int tid = threadIdx.x % NT;
   const T* const z = static_cast<const T*>(a.z) + (size_t)row * a.classes;
@@ -208,7 +224,8 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, int row, float
   for (int u = 0; u < CH; ++u)
     if (tid + u * NT < r.chunks) q[u] = r.load(z, tid + u * NT);
   int32_t* const cls = reinterpret_cast<int32_t*>(lists);
-  float *const p = lists + a.k, *const rest_of = lists + 2 * a.k, *const z_of = lists + 3 * a.k;
+  const int pitch = list_pitch(a.k);
+  float *const p = lists + pitch, *const rest_of = lists + 2 * pitch, *const z_of = lists + 3 * pitch;
   const int label = HARD ? a.labels[row] : -1;
   float z_label = 0.f;
   if (HARD && (unsigned)label < (unsigned)a.classes) z_label = Elem<T>::load(z + label);
@@ -224,8 +241,9 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, int row, float
 #pragma unroll
       for (int e = 0; e < Row::PER; ++e) own = fmaxf(own, Row::value(q[u], e));
     }
+  int rows = dz ? count_part<NT>(a) : 0;
   RowSums t;
-  t.max = row_reduce<NT>(own, sh[0], [](float x, float y) { return fmaxf(x, y); });
+  t.max = row_reduce<NT>(own, sh.v[0], Larger());
   const float inv_t2 = a.inv_t * LOG2E;
   float s = 0.f, s1 = 0.f, equal = 0.f;
   if (own == t.max) {
@@ -237,15 +255,25 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, int row, float
     for (int u = 0; u < CH; ++u)
       if (tid + u * NT < r.chunks) add_chunk<HARD, Row>(q[u], t.max, inv_t2, false, s, s1, equal);
   }
-  auto add = [](float x, float y) { return x + y; };
-  if (NT > 64 && tid == 0) sh[4][0] = __int_as_float(l.length);
-  s = row_reduce<NT>(s, sh[1], add);
-  equal = row_reduce<NT>(equal, sh[2], add);
-  if (HARD) s1 = row_reduce<NT>(s1, sh[3], add);
+  if (NT > 64 && tid == 0) sh.length = l.length;
+  // (one barrier for all of them)
+  s = wave_reduce(s, Add());
+  equal = wave_reduce(equal, Add());
+  rows = wave_reduce(rows, Add());
+  if (HARD) s1 = wave_reduce(s1, Add());
+  if constexpr (NT > 64) {
+    if ((tid & 63) == 0) { sh.v[1][tid >> 6] = s; sh.v[2][tid >> 6] = equal; sh.v[3][tid >> 6] = s1; sh.count[tid >> 6] = rows; }
+    __syncthreads();
+    s = join_waves<NT>(sh.v[1], Add());
+    equal = join_waves<NT>(sh.v[2], Add());
+    s1 = HARD ? join_waves<NT>(sh.v[3], Add()) : 0.f;
+    rows = join_waves<NT>(sh.count, Add());
+  }
+  const float inv_rows = rows ? 1.f / (float)rows : 0.f;
   const bool none = fabsf(t.max) == INFINITY;          // no distribution
   t.rest = none ? NAN : s + (equal - 1.f);
   t.rest1 = none ? NAN : s1 + (equal - 1.f);
-  const int length = NT > 64 ? __float_as_int(sh[4][0]) : l.length;
+  const int length = NT > 64 ? sh.length : l.length;
   if (tid < 64) {
     const float loss = loss_of(a, l, t, p, z_of, label, z_label);
     if (tid == 0) a.loss_rows[row] = loss;
@@ -264,52 +292,40 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, int row, float
   write_listed<T, NT, HARD>(a, dz, 0, a.classes, length, cls, p, rest_of, z_of, t, label, z_label, inv_rows);
 }
 
-// loss = sum of loss_rows / rows that count, NT threads, fixed order
-template <int NT> __device__ __forceinline__ void mean_loss(const DistillArgs& a, int rows) {
-  __shared__ double sh[NT / 64];
-  double s = 0.0;
-  for (int i = threadIdx.x; i < a.n; i += NT) s += (double)a.loss_rows[i];
-  s = row_reduce<NT>(s, sh, [](double x, double y) { return x + y; });
-  if (threadIdx.x == 0) *a.loss = rows ? (float)(s / (double)rows) : 0.f;
-}
-
 template <class T, int NT, int CH, bool HARD>
-__global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a) {
-  extern __shared__ float lists[];
-  __shared__ float sh[5][NT / 64];
-  __shared__ int shc[NT / 64];
-  const int rows = a.dz ? counted<NT>(a, shc) : 1;
-  distill_row<T, NT, CH, HARD>(a, blockIdx.x, rows ? 1.f / (float)rows : 0.f, lists, sh);
+__global__ __launch_bounds__(NT, CH == 8 ? 8 : 4) void distill_rows_kernel(DistillArgs a) {
+  extern __shared__ __attribute__((aligned(16))) float lists[];
+  __shared__ RowShared<NT> sh;
+  distill_row<T, NT, CH, HARD>(a, blockIdx.x, lists, sh);
 }
 
-// A wave per row; with one workgroup the mean, too
+// A wave per row; in one workgroup (with all rows, sixteen at most) the mean, too
 template <class T, int CH, bool HARD>
-__global__ __launch_bounds__(1024) void distill_waves_kernel(DistillArgs a, int threads) {
-  extern __shared__ float lists[];
-  __shared__ float sh[16][5][1];
-  __shared__ int total;
-  const int wave = threadIdx.x >> 6, waves = threads >> 6;
-  if (wave == 0) {
-    const int c = counted<64>(a, nullptr);
-    if (threadIdx.x == 0) total = c;
-  }
-  __syncthreads();
-  const int rows = total;
-  for (int row = (int)blockIdx.x * waves + wave; row < a.n; row += (int)gridDim.x * waves) {
-    distill_row<T, 64, CH, HARD>(a, row, rows ? 1.f / (float)rows : 0.f, lists + (size_t)wave * 4 * a.k, sh[wave]);
-    row_sync<64>();
+__global__ __launch_bounds__(1024) void distill_waves_kernel(DistillArgs a) {
+  extern __shared__ __attribute__((aligned(16))) float lists[];
+  const int wave = threadIdx.x >> 6, row = (int)blockIdx.x * (int)(blockDim.x >> 6) + wave;
+  if (row < a.n) {
+    RowShared<64> sh;                                  // (one wave needs none of it)
+    distill_row<T, 64, CH, HARD>(a, row, lists + (size_t)wave * 4 * list_pitch(a.k), sh);
   }
   if (gridDim.x > 1 || !a.loss) return;
   __threadfence_block();
   __syncthreads();
-  if (threads == 1024) mean_loss<1024>(a, rows);
+  if (threadIdx.x) return;
+  double s = 0.0;
+  int rows = 0;
+  for (int i = 0; i < a.n; ++i) {
+    s += (double)a.loss_rows[i];
+    rows += row_counts(a, i) ? 1 : 0;
+  }
+  *a.loss = rows ? (float)(s / (double)rows) : 0.f;
 }
 
 // Cut rows: the sums of a part
 template <class T, bool HARD>
 __global__ __launch_bounds__(256) void distill_part_kernel(DistillArgs a) {
   typedef RowChunks<T> Row;
-  __shared__ float sh[5][4];
+  __shared__ float sh[4][4];
   const int row = (int)blockIdx.x / a.splits, sp = (int)blockIdx.x - row * a.splits, tid = threadIdx.x;
   const T* const z = static_cast<const T*>(a.z) + (size_t)row * a.classes;
   if (!row_counts(a, row)) return;
@@ -330,12 +346,11 @@ __global__ __launch_bounds__(256) void distill_part_kernel(DistillArgs a) {
 #pragma unroll
     for (int e = 0; e < Row::PER; ++e) own = fmaxf(own, Row::value(q, e));
   }
-  const float mx = row_reduce<256>(own, sh[0], [](float x, float y) { return fmaxf(x, y); });
+  const float mx = row_reduce<256>(own, sh[0], Larger());
   for (int c = c0 + tid; c < c1; c += 256) add_chunk<HARD, Row>(r.load(z, c), mx, inv_t2, own == mx, s, s1, equal);
-  auto add = [](float x, float y) { return x + y; };
-  s = row_reduce<256>(s, sh[1], add);
-  equal = row_reduce<256>(equal, sh[2], add);
-  if (HARD) s1 = row_reduce<256>(s1, sh[3], add);
+  s = row_reduce<256>(s, sh[1], Add());
+  equal = row_reduce<256>(equal, sh[2], Add());
+  if (HARD) s1 = row_reduce<256>(s1, sh[3], Add());
   if (tid == 0) {
     float* const p = a.part + (size_t)row * 4 * a.splits + sp;
     const bool none = mx == -INFINITY && !(s != s);    // (nothing but minus infinity: the other parts decide)
@@ -349,11 +364,11 @@ __global__ __launch_bounds__(256) void distill_part_kernel(DistillArgs a) {
 template <class T, bool HARD>
 __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a) {
   typedef RowChunks<T> Row;
-  extern __shared__ float lists[];
+  extern __shared__ __attribute__((aligned(16))) float lists[];
   __shared__ int shc[4];
   __shared__ int length_of;
   const int row = (int)blockIdx.x / a.splits, sp = (int)blockIdx.x - row * a.splits, tid = threadIdx.x, lane = tid & 63;
-  const int rows = counted<256>(a, shc);
+  const int rows = row_reduce<256>(count_part<256>(a), shc, Add());
   const float inv_rows = rows ? 1.f / (float)rows : 0.f;
   const T* const z = static_cast<const T*>(a.z) + (size_t)row * a.classes;
   T* const dz = a.dz ? static_cast<T*>(a.dz) + (size_t)row * a.classes : nullptr;
@@ -369,19 +384,19 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a) {
   const bool mine = lane < a.splits;
   const float m = mine ? at[lane] : -INFINITY, rest = mine ? at[a.splits + lane] : -1.f, rest1 = mine ? at[2 * a.splits + lane] : -1.f;
   RowSums t;
-  t.max = row_reduce<64>(m, (float*)nullptr, [](float x, float y) { return fmaxf(x, y); });
+  t.max = wave_reduce(m, Larger());
   const bool top = mine && m == t.max;
   float s = top ? rest : (1.f + rest) * exp2_fast((m - t.max) * (a.inv_t * LOG2E)), s1 = top ? rest1 : (1.f + rest1) * exp2_fast((m - t.max) * LOG2E);
   if (!mine) s = s1 = 0.f;
-  auto add = [](float x, float y) { return x + y; };
-  const float equal = row_reduce<64>(top ? 1.f : 0.f, (float*)nullptr, add);
-  s = row_reduce<64>(s, (float*)nullptr, add);
-  s1 = row_reduce<64>(s1, (float*)nullptr, add);
+  const float equal = wave_reduce(top ? 1.f : 0.f, Add());
+  s = wave_reduce(s, Add());
+  s1 = wave_reduce(s1, Add());
   const bool none = fabsf(t.max) == INFINITY;
   t.rest = none ? NAN : s + (equal - 1.f);
   t.rest1 = none ? NAN : s1 + (equal - 1.f);
   int32_t* const cls = reinterpret_cast<int32_t*>(lists);
-  float *const p = lists + a.k, *const rest_of = lists + 2 * a.k, *const z_of = lists + 3 * a.k;
+  const int pitch = list_pitch(a.k);
+  float *const p = lists + pitch, *const rest_of = lists + 2 * pitch, *const z_of = lists + 3 * pitch;
   const float* const kept = a.at_list + (size_t)row * (a.k + 1);
   const int label = HARD ? a.labels[row] : -1;
   const float z_label = HARD ? kept[a.k] : 0.f;
@@ -409,17 +424,25 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a) {
   write_listed<T, 256, HARD>(a, dz, r.at(c0), c1 < r.chunks ? r.at(c1) : a.classes, length_of, cls, p, rest_of, z_of, t, label, z_label, inv_rows);
 }
 
+// loss = sum of loss_rows / rows that count, in a fixed order
 __global__ __launch_bounds__(1024) void distill_mean_kernel(DistillArgs a) {
   __shared__ int sh[16];
-  mean_loss<1024>(a, counted<1024>(a, sh));
+  __shared__ double shd[16];
+  double s = 0.0;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < a.n; i += 1024) s += (double)a.loss_rows[i];
+  const int rows = row_reduce<1024>(count_part<1024>(a), sh, Add());
+  s = row_reduce<1024>(s, shd, Add());
+  if (threadIdx.x == 0) *a.loss = rows ? (float)(s / (double)rows) : 0.f;
 }
-// rows that count, 4096 rows to a workgroup
-__global__ __launch_bounds__(256) void distill_count_kernel(DistillArgs a, int* counts) {
+// rows that count, `each` rows to a workgroup
+__global__ __launch_bounds__(256) void distill_count_kernel(DistillArgs a, int* counts, int each) {
   __shared__ int sh[4];
   int c = 0;
-  const int first = (int)blockIdx.x * 4096, end = min(first + 4096, a.n);
+  const int first = (int)blockIdx.x * each, end = min(first + each, a.n);
+#pragma unroll 4
   for (int i = first + (int)threadIdx.x; i < end; i += 256) c += row_counts(a, i) ? 1 : 0;
-  c = row_reduce<256>(c, sh, [](int x, int y) { return x + y; });
+  c = row_reduce<256>(c, sh, Add());
   if (threadIdx.x == 0) counts[blockIdx.x] = c;
 }
 
@@ -430,23 +453,25 @@ constexpr int kMostTop = 1024, kMostClasses = 1 << 20, kMostRows = 1 << 20;
 
 struct DistillPlan {
   bool waves;                  // a wave per row
-  bool one;                    // in one workgroup, with the mean
+  bool one;                    // sixteen rows at most, in one workgroup, with the mean
   int splits, chunks_per_split;      // 1: a workgroup per row
-  int chunks, count_parts;     // count_parts 0: every workgroup counts the rows
+  int chunks;
+  int count_parts, count_each; // rows that count: parts of so many rows (256 at most); 0: every workgroup counts them all
   size_t rows, counts, part, at_list, total;
 };
 DistillPlan distill_plan(int n, int classes, int k, int dtype) {
   DistillPlan p{};
   const int per = dtype == DT_BF16 ? 8 : 4;
-  p.chunks = (classes + per - 1) / per + 1;            // (a row may begin inside one)
+  p.chunks = (classes + per - 1) / per + (classes % per ? 1 : 0);      // (a row begins inside one where the rows are not whole ones)
   p.waves = p.chunks <= 64 * 4;
-  p.one = p.waves && n <= 64 && k <= 128;
+  p.one = p.waves && n <= 16 && k <= 128;
   p.splits = 1;
   if (p.chunks > 1024 * 16) {
     p.splits = (int)ceil_div(p.chunks, 4112);          // 64 KiB to a part: 64 parts at most
     p.chunks_per_split = (int)ceil_div(p.chunks, p.splits);
   }
-  p.count_parts = n > 1024 ? (int)ceil_div(n, 4096) : 0;
+  p.count_each = n > 65536 ? (int)ceil_div(n, 256) : 256;
+  p.count_parts = n > 1024 ? (int)ceil_div(n, p.count_each) : 0;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t a = at; at += al256(bytes); return a; };
   p.rows = take((size_t)n * 4);
@@ -462,15 +487,15 @@ bool distill_ok(int n, int classes, int k, int dtype) {
 }
 
 template <class T, bool HARD> hipError_t launch_distill(const DistillArgs& a, const DistillPlan& p, hipStream_t st) {
-  const size_t lists = (size_t)4 * a.k * 4;
+  const size_t lists = (size_t)4 * list_pitch(a.k) * 4;
   if (p.splits > 1) {
     const dim3 grid((unsigned)(a.n * p.splits));
     hipLaunchKernelGGL((distill_part_kernel<T, HARD>), grid, dim3(256), 0, st, a);
     hipLaunchKernelGGL((distill_join_kernel<T, HARD>), grid, dim3(256), lists, st, a);
   } else if (p.waves) {
-    const int threads = p.one ? 1024 : 128;
+    const int threads = p.one ? 64 * a.n : a.n <= 2048 ? 64 : 256;
     const dim3 grid(p.one ? 1u : (unsigned)ceil_div(a.n, threads / 64));
-#define ACC_WAVES(CH) hipLaunchKernelGGL((distill_waves_kernel<T, CH, HARD>), grid, dim3(threads), lists * (threads / 64), st, a, threads)
+#define ACC_WAVES(CH) hipLaunchKernelGGL((distill_waves_kernel<T, CH, HARD>), grid, dim3(threads), lists * (threads / 64), st, a)
     if (p.chunks <= 64) ACC_WAVES(1);
     else if (p.chunks <= 128) ACC_WAVES(2);
     else ACC_WAVES(4);
@@ -478,7 +503,7 @@ template <class T, bool HARD> hipError_t launch_distill(const DistillArgs& a, co
   } else {
 #define ACC_ROWS(NT, CH) if (p.chunks <= NT * CH) { hipLaunchKernelGGL((distill_rows_kernel<T, NT, CH, HARD>), dim3((unsigned)a.n), dim3(NT), lists, st, a); break; }
     do {
-      ACC_ROWS(256, 2) ACC_ROWS(256, 4) ACC_ROWS(256, 8) ACC_ROWS(256, 16) ACC_ROWS(512, 16) ACC_ROWS(1024, 16)
+      ACC_ROWS(256, 2) ACC_ROWS(256, 4) ACC_ROWS(256, 8) ACC_ROWS(512, 8) ACC_ROWS(1024, 8) ACC_ROWS(1024, 16)
     } while (false);
 #undef ACC_ROWS
   }
@@ -504,14 +529,14 @@ hipError_t distill(const void* z, const int32_t* index, const float* top, const 
   a.part = (float*)(ws + p.part); a.at_list = (float*)(ws + p.at_list); a.splits = p.splits; a.chunks_per_split = p.chunks_per_split;
   if (p.count_parts && (dz || loss)) {
     int* const counts = (int*)(ws + p.counts);
-    hipLaunchKernelGGL(distill_count_kernel, dim3((unsigned)p.count_parts), dim3(256), 0, st, a, counts);
+    hipLaunchKernelGGL(distill_count_kernel, dim3((unsigned)p.count_parts), dim3(256), 0, st, a, counts, p.count_each);
     a.counts = counts; a.count_parts = p.count_parts;
   }
   const bool hard = alpha < 1.f;
   hipError_t e;
   if (dtype == DT_BF16) e = hard ? launch_distill<bf16_t, true>(a, p, st) : launch_distill<bf16_t, false>(a, p, st);
   else e = hard ? launch_distill<float, true>(a, p, st) : launch_distill<float, false>(a, p, st);
-  if (e != hipSuccess || !loss || p.one) return e;
+  if (e != hipSuccess || !loss || (p.one || (p.waves && n == 1))) return e;
   hipLaunchKernelGGL(distill_mean_kernel, dim3(1), dim3(1024), 0, st, a);
   return hipGetLastError();
 }

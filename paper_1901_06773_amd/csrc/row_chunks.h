@@ -8,6 +8,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "dtype.h"
 
@@ -76,15 +77,38 @@ template <int NT> __device__ __forceinline__ void row_sync() {
     __syncthreads();
   }
 }
-template <int NT, class V, class F> __device__ __forceinline__ V row_reduce(V v, V* sh, F op) {
+// over 2^k = N <= 16 neighbouring lanes, by rotations in a row of sixteen: after each the values repeat with half the period, so that all lanes have the same bits
+template <int N, class V, class F> __device__ __forceinline__ V row16_reduce(V v, F op) {
+  static_assert(sizeof(V) == 4 || sizeof(V) == 8, "one or two words");
+#if defined(__HIP_DEVICE_COMPILE__)
+  auto turned = [](V x, auto by) {
+    constexpr int ctrl = 0x120 + decltype(by)::value;
+    union { V v; int w[sizeof(V) / 4]; } u;
+    u.v = x;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = op(v, __shfl_xor(v, o));
+    for (int i = 0; i < (int)(sizeof(V) / 4); ++i) u.w[i] = __builtin_amdgcn_update_dpp(0, u.w[i], ctrl, 0xf, 0xf, false);
+    return u.v;
+  };
+  if constexpr (N >= 16) v = op(v, turned(v, std::integral_constant<int, 8>()));
+  if constexpr (N >= 8) v = op(v, turned(v, std::integral_constant<int, 4>()));
+  if constexpr (N >= 4) v = op(v, turned(v, std::integral_constant<int, 2>()));
+  if constexpr (N >= 2) v = op(v, turned(v, std::integral_constant<int, 1>()));
+#endif
+  return v;
+}
+template <class V, class F> __device__ __forceinline__ V wave_reduce(V v, F op) {
+  v = row16_reduce<16>(v, op);
+  v = op(v, __shfl_xor(v, 16));
+  return op(v, __shfl_xor(v, 32));
+}
+// the waves' values, which lie in LDS
+template <int NT, class V, class F> __device__ __forceinline__ V join_waves(const V* sh, F op) { return row16_reduce<NT / 64>(sh[threadIdx.x & (NT / 64 - 1)], op); }
+template <int NT, class V, class F> __device__ __forceinline__ V row_reduce(V v, V* sh, F op) {
+  v = wave_reduce(v, op);
   if constexpr (NT > 64) {
     if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = sh[0];
-#pragma unroll
-    for (int w = 1; w < NT / 64; ++w) v = op(v, sh[w]);
+    v = join_waves<NT>(sh, op);
   }
   return v;
 }

@@ -36,31 +36,40 @@ struct TopArgs {
 
 template <int NT> struct TopRoom { static constexpr int value = NT == 64 ? 512 : NT == 256 ? 1024 : 2048; };      // candidates in LDS, at least k
 
-// The largest t (of the bits `step` and up) that `want` of the threads' whole numbers reach, by one wave, from LDS.
-template <int NT> __device__ __forceinline__ uint32_t reached_by(const uint32_t* keys, int want) {
-  const int lane = threadIdx.x & 63;
-  uint32_t mine[NT / 64];
-#pragma unroll
-  for (int u = 0; u < NT / 64; ++u) mine[u] = keys[lane + 64 * u];
+// The largest t, of its upper sixteen bits (a bound: the lower half may as well be zero), that `want` of the threads' keys reach.  Every wave looks at all
+// keys and tries another value of the next bits: log2 of the waves at a time, one barrier each (one wave, bit by bit: 1024 keys 1.6 us, so 0.5).
+template <int NT> __device__ __forceinline__ uint32_t reached_by(const uint32_t* keys, int want, int (*sh)[NT / 64]) {
+  constexpr int W = NT / 64, BITS = W >= 16 ? 4 : W >= 8 ? 3 : W >= 4 ? 2 : 1;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint32_t t = 0;
-  for (int bit = 31; bit >= 16; --bit) {               // (a bound: the lower half may as well be zero)
-    const uint32_t mid = t | (1u << bit);
+  int turn = 0;
+  for (int shift = 32 - BITS; shift > 16 - BITS; shift -= BITS) {
+    const uint32_t mid = t | ((W == 1 ? 1u : (uint32_t)wave) << shift);
     int c = 0;
 #pragma unroll
-    for (int u = 0; u < NT / 64; ++u) c += __popcll(__ballot(mine[u] >= mid));
-    if (c >= want) t = mid;
+    for (int u = 0; u < W; ++u) c += __popcll(__ballot(keys[lane + 64 * u] >= mid));
+    if constexpr (W == 1) {
+      if (c >= want) t = mid;
+    } else {
+      if (lane == 0) sh[turn][wave] = c;
+      __syncthreads();
+      int best = 0;
+#pragma unroll
+      for (int w = 1; w < W; ++w) best = sh[turn][w] >= want ? w : best;       // (the counts fall with w)
+      t |= (uint32_t)best << shift;
+      turn ^= 1;
+    }
   }
   return t;
 }
 
 template <class T, int NT, int CH>
-__global__ __launch_bounds__(NT) void top_kernel(TopArgs a) {
+__global__ __launch_bounds__(NT, CH == 8 ? 8 : 4) void top_kernel(TopArgs a) {
   typedef RowChunks<T> Row;
   constexpr int PER = Row::PER, ROOM = TopRoom<NT>::value, W = NT / 64;
   __shared__ unsigned long long cand[ROOM];
   __shared__ uint32_t keys[NT];
   __shared__ int counter, waves[2][W];
-  __shared__ float bound;
   const int tid = threadIdx.x, row_at = (int)blockIdx.x / a.segments, seg = (int)blockIdx.x - row_at * a.segments;
   const int from = seg * a.segment, count = min(a.segment, a.classes - from), want = min(a.k, count);
   const T* const row = static_cast<const T*>(a.z) + (size_t)row_at * a.classes + from;
@@ -80,12 +89,7 @@ __global__ __launch_bounds__(NT) void top_kernel(TopArgs a) {
   keys[tid] = tid < r.chunks ? order_of(mx) : 0;
   if (tid == 0) counter = 0;
   row_sync<NT>();
-  if (tid < 64) {
-    const float b = want <= min(NT, r.chunks) ? value_of(max(reached_by<NT>(keys, want), order_of(-INFINITY))) : -INFINITY;
-    if (tid == 0) bound = b;
-  }
-  row_sync<NT>();
-  const float low = bound;
+  const float low = want <= min(NT, r.chunks) ? value_of(max(reached_by<NT>(keys, want, waves), order_of(-INFINITY))) : -INFINITY;
   // f(key, column) for every value of the row, from the caches: the registers of the first two sweeps would not fit with this unrolled
   auto each = [&](auto f) {
 #pragma unroll 1
@@ -130,16 +134,14 @@ __global__ __launch_bounds__(NT) void top_kernel(TopArgs a) {
   if (found > ROOM) {
     int turn = 0;
     auto total = [&](int mine) {                       // the threads' sum
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o);
+      auto add = [](int x, int y) { return x + y; };
+      mine = wave_reduce(mine, add);
       if constexpr (NT > 64) {
         int* const w = waves[turn];
         turn ^= 1;
         if ((tid & 63) == 0) w[tid >> 6] = mine;
         __syncthreads();
-        mine = 0;
-#pragma unroll
-        for (int i = 0; i < W; ++i) mine += w[i];
+        mine = join_waves<NT>(w, add);
       }
       return mine;
     };
@@ -171,9 +173,35 @@ __global__ __launch_bounds__(NT) void top_kernel(TopArgs a) {
     row_sync<NT>();
     found = counter;
   }
-  // sorted, largest first, up to the next power of two
+  const size_t out = ((size_t)row_at * a.segments + seg) * a.k;
+  auto give = [&](int i, unsigned long long c) {
+    const int at = from + (int)(0xFFFFFFFFu - (uint32_t)c);
+    a.index[out + i] = a.map ? a.map[(size_t)row_at * a.classes + at] : at;
+    a.top[out + i] = value_of((uint32_t)(c >> 32));
+  };
+  for (int i = want + tid; i < a.k; i += NT) {         // (of a short last segment: behind all of its row's values)
+    a.index[out + i] = -1;
+    a.top[out + i] = -INFINITY;
+  }
   int size = 1;
   while (size < found) size *= 2;
+  // Few: each is compared with all others, by as many threads as there are for it; its rank is its place.  More: sorted, largest first.  (Per row of 65536, 70
+  // found: sorting 128 in 28 steps with a barrier each took 1.3 us, this 0.2.)
+  if (size <= NT && (size / 64) * size <= NT) {
+    const int per = NT / size, i = tid / per, part = tid % per;
+    const unsigned long long c = i < found ? cand[i] : 0;
+    int rank = 0;
+    for (int j = part; j < found; j += per) rank += cand[j] > c ? 1 : 0;
+    for (int o = 1; o < min(per, 64); o <<= 1) rank += __shfl_xor(rank, o);
+    if (per > 64) {                                    // (so few that a wave has only one of them)
+      if ((tid & 63) == 0) keys[tid >> 6] = (uint32_t)rank;
+      row_sync<NT>();
+      rank = 0;
+      for (int w = 0; w < per / 64; ++w) rank += (int)keys[(i * per >> 6) + w];
+    }
+    if (part == 0 && i < found && rank < want) give(rank, c);
+    return;
+  }
   for (int i = found + tid; i < size; i += NT) cand[i] = 0;
   row_sync<NT>();
   for (int span = 2; span <= size; span *= 2)
@@ -185,18 +213,7 @@ __global__ __launch_bounds__(NT) void top_kernel(TopArgs a) {
       }
       row_sync<NT>();
     }
-  const size_t out = ((size_t)row_at * a.segments + seg) * a.k;
-  for (int i = tid; i < a.k; i += NT) {
-    if (i >= want) {                                   // (of a short last segment: behind all of its row's values)
-      a.index[out + i] = -1;
-      a.top[out + i] = -INFINITY;
-      continue;
-    }
-    const unsigned long long c = cand[i];
-    const int at = from + (int)(0xFFFFFFFFu - (uint32_t)c);
-    a.index[out + i] = a.map ? a.map[(size_t)row_at * a.classes + at] : at;
-    a.top[out + i] = value_of((uint32_t)(c >> 32));
-  }
+  for (int i = tid; i < want; i += NT) give(i, cand[i]);
 }
 
 inline size_t al256(size_t b) { return (b + 255) & ~(size_t)255; }
@@ -222,13 +239,14 @@ TopPlan top_plan(int n, int classes, int k, int dtype) {
 
 template <class T> hipError_t launch_top(const TopArgs& a, hipStream_t st) {
   constexpr int PER = RowChunks<T>::PER;
-  const int chunks = (a.segment + PER - 1) / PER + 1;
+  // (a row begins inside a chunk where the rows are not whole ones)
+  const int chunks = (a.segment + PER - 1) / PER + (a.classes % PER ? 1 : 0);
   const dim3 grid((unsigned)(a.n * a.segments));
 #define ACC_TOP(NT, CH) if (chunks <= NT * CH && a.k <= TopRoom<NT>::value) { hipLaunchKernelGGL((top_kernel<T, NT, CH>), grid, dim3(NT), 0, st, a); return hipGetLastError(); }
   ACC_TOP(64, 1) ACC_TOP(64, 4)
-  ACC_TOP(256, 4) ACC_TOP(256, 16)
-  ACC_TOP(512, 16)
-  ACC_TOP(1024, 16)
+  ACC_TOP(256, 4) ACC_TOP(256, 8)
+  ACC_TOP(512, 8)
+  ACC_TOP(1024, 8) ACC_TOP(1024, 16)
 #undef ACC_TOP
   return hipErrorInvalidValue;
 }
