@@ -6,8 +6,8 @@
 //   dz = (alpha T (q - p) + (1 - alpha) (s - onehot)) / rows that count
 //
 // A row is read once, into the registers of a wave or a workgroup, and its gradient written from there: memory bounds it.  Rows that no registers hold, and
-// long ones where there are few, are cut: a launch leaves the sums of each part, the next joins them and writes the gradient.  One wave works out the list's
-// probabilities while the row is on its way; the few classes of the list (and the label) are written again, behind a barrier, with their own terms.
+// long ones where there are few, are cut: a launch leaves the sums of each part, the next joins them and writes the gradient.  The list's probabilities are worked out
+// by the same threads, an entry each, while the row is on its way; the few classes of the list (and the label) are written again, behind a barrier, with their own terms.
 //
 // Sums of exponentials go without the largest one, which is 1: with R the sum of the others', log(1 + R) and, of a class that both give more than a half,
 // q - p = (1 - p) - (1 - q) keep R where a class is all but certain.
@@ -65,77 +65,83 @@ struct Add {
 struct Larger {
   __device__ __forceinline__ float operator()(float x, float y) const { return fmaxf(x, y); }
 };
+struct Lower {
+  __device__ __forceinline__ int operator()(int x, int y) const { return min(x, y); }
+};
 template <int NT> struct RowShared {
-  float v[4][NT / 64];
-  int count[NT / 64], length;
+  float v[8][NT / 64];
+  int n[2][NT / 64];
 };
-// words of LDS for a list: four arrays
-__host__ __device__ __forceinline__ int list_pitch(int k) { return (k + 3) & ~3; }
 
-// The list of a row, by one wave: probabilities and classes into LDS, and what the loss needs of them.
+// The list of a row in LDS, four arrays of list_pitch(k) words; entry j is its thread's, j modulo NT.
 struct List {
+  int32_t* cls;                // -1 from `length` on
+  float *t, *p, *z;            // the teacher's logits, probabilities; the student's logits of these classes
   int length;                  // entries before the first negative class
-  float entropy;               // sum p log p
-  bool bad;                    // a class beyond the last one
+  float max, rest, inv, log_sum;
 };
-__device__ __forceinline__ List read_list(const DistillArgs& a, int row, int32_t* cls, float* p, float* rest_of) {
-  const int lane = threadIdx.x & 63;
+__host__ __device__ __forceinline__ int list_pitch(int k) { return (k + 3) & ~3; }
+__device__ __forceinline__ List list_in(float* lds, int k) {
+  const int pitch = list_pitch(k);
+  return List{reinterpret_cast<int32_t*>(lds), lds + pitch, lds + 2 * pitch, lds + 3 * pitch, 0, 0.f, 0.f, 0.f, 0.f};
+}
+// entries, and the student's logits by z_at(entry, class); returns the thread's idea of the length
+template <int NT, class F> __device__ __forceinline__ int list_read(const DistillArgs& a, int row, const List& l, F z_at) {
   const int32_t* const index = a.index + (size_t)row * a.k;
   const float* const top = a.top + (size_t)row * a.k;
-  List l{a.k, 0.f, false};
-  float mx = -INFINITY;
-  for (int j0 = 0; j0 < a.k; j0 += 64) {
-    const int j = j0 + lane, c = j < a.k ? index[j] : 0;
+  int length = a.k;
+  for (int j = threadIdx.x % NT; j < list_pitch(a.k); j += NT) {
+    const int c = j < a.k ? index[j] : -1;
     const float t = j < a.k ? top[j] : 0.f;
-    const unsigned long long ends = __ballot(j < a.k && c < 0);
-    if (ends) l.length = j0 + __ffsll(ends) - 1;
-    if (j < l.length) {
-      cls[j] = c;
-      p[j] = t;
-      mx = fmaxf(mx, t);
-      l.bad |= c >= a.classes;
-    }
-    if (ends) break;
+    const float z = (unsigned)c < (unsigned)a.classes ? z_at(j, c) : NAN;
+    if (c < 0) length = min(length, j);
+    l.cls[j] = c;
+    l.t[j] = t;
+    l.z[j] = z;
   }
-  mx = wave_reduce(mx, Larger());
-  l.bad = __any(l.bad);
-  if (lane < (4 - (l.length & 3)) % 4) cls[l.length + lane] = -1;        // (write_listed() looks at four at a time)
-  float s = 0.f, equal = 0.f;
-  for (int j = lane; j < l.length; j += 64) {
-    const float t = p[j];
-    const bool is_top = t == mx;
-    equal += is_top ? 1.f : 0.f;
-    s += is_top ? 0.f : expf((t - mx) * a.inv_t);
+  return length;
+}
+// behind its end, and the largest logit before it
+template <int NT> __device__ __forceinline__ float list_end(const DistillArgs& a, const List& l) {
+  float mx = -INFINITY;
+  for (int j = threadIdx.x % NT; j < list_pitch(a.k); j += NT) {
+    if (j >= l.length) l.cls[j] = -1;
+    else mx = fmaxf(mx, l.t[j]);
   }
-  s = wave_reduce(s, Add());
-  equal = wave_reduce(equal, Add());
-  const float rest = fabsf(mx) == INFINITY ? NAN : s + (equal - 1.f), inv = 1.f / (1.f + rest), log_sum = log1pf(rest);
-  float h = 0.f;
-  for (int j = lane; j < l.length; j += 64) {
-    const float v = (p[j] - mx) * a.inv_t, e = expf(v);
-    p[j] = e * inv;
-    rest_of[j] = (rest - expm1f(v)) * inv;             // 1 - p
-    h += e == 0.f ? 0.f : e * inv * (v - log_sum);
+  return mx;
+}
+template <int NT> __device__ __forceinline__ void list_sum(const DistillArgs& a, const List& l, float& s, float& equal) {
+  s = equal = 0.f;
+  for (int j = threadIdx.x % NT; j < l.length; j += NT) {
+    const bool top = l.t[j] == l.max;
+    equal += top ? 1.f : 0.f;
+    s += top ? 0.f : exp2_fast((l.t[j] - l.max) * (a.inv_t * LOG2E));
   }
-  l.entropy = wave_reduce(h, Add());
-  return l;
+}
+__device__ __forceinline__ void list_known(List& l, float s, float equal) {
+  l.rest = fabsf(l.max) == INFINITY ? NAN : s + (equal - 1.f);
+  l.inv = 1.f / (1.f + l.rest);
+  l.log_sum = log1pf(l.rest);
+}
+// probabilities; the thread's part of sum p (log p - z / T)
+template <int NT> __device__ __forceinline__ float list_loss(const DistillArgs& a, const List& l, float max) {
+  float d = 0.f;
+  for (int j = threadIdx.x % NT; j < l.length; j += NT) {
+    const float v = (l.t[j] - l.max) * a.inv_t, p = exp2_fast(v * LOG2E) * l.inv;
+    l.p[j] = p;
+    if (l.cls[j] >= a.classes) d = NAN;
+    else if (p != 0.f) d += p * (v - l.log_sum) - p * ((l.z[j] - max) * a.inv_t);
+  }
+  return d;
 }
 
 // What a row's sums come to
 struct RowSums {
   float max, rest, rest1;      // the largest logit; R at the temperature and at 1
 };
-// The loss of a row, by one wave; z_of: the logits of the list's classes
-__device__ __forceinline__ float loss_of(const DistillArgs& a, const List& l, const RowSums& r, const float* p, const float* z_of, int label, float z_label) {
-  const int lane = threadIdx.x & 63;
-  float loss = 0.f;
-  if (l.length) {
-    float d = 0.f;
-    for (int j = lane; j < l.length; j += 64) d += p[j] == 0.f ? 0.f : p[j] * ((z_of[j] - r.max) * a.inv_t);
-    d = wave_reduce(d, Add());
-    loss = a.soft * (l.entropy - d + log1pf(r.rest));
-    if (l.bad) loss = NAN;
-  }
+// d: the list's parts together
+__device__ __forceinline__ float loss_of(const DistillArgs& a, int length, float d, const RowSums& r, int label, float z_label) {
+  float loss = length ? a.soft * (d + log1pf(r.rest)) : 0.f;
   if (a.hard > 0.f) loss += (unsigned)label < (unsigned)a.classes ? a.hard * (log1pf(r.rest1) - (z_label - r.max)) : NAN;
   return loss;
 }
@@ -156,37 +162,45 @@ __device__ __forceinline__ Slope slope_of(const DistillArgs& a, const RowSums& r
 
 // The gradient of the classes [lo, hi) that are in the list, and of the label, by NT threads: their own terms.
 template <class T, int NT, bool HARD>
-__device__ __forceinline__ void write_listed(const DistillArgs& a, T* dz, int lo, int hi, int length, const int32_t* cls, const float* p, const float* rest_of,
-                                             const float* z_of, const RowSums& r, int label, float z_label, float inv_rows) {
+__device__ __forceinline__ void write_listed(const DistillArgs& a, T* dz, int lo, int hi, const List& l, const RowSums& r, int label, float z_label, float inv_rows) {
   const float inv = 1.f / (1.f + r.rest), inv1 = 1.f / (1.f + r.rest1);
-  for (int j = threadIdx.x % NT; j <= length; j += NT) {
-    const int c = j < length ? cls[j] : label;
-    if (j == length && (!HARD || (unsigned)label >= (unsigned)a.classes)) continue;
+  for (int j = threadIdx.x % NT; j <= l.length; j += NT) {
+    const bool entry = j < l.length;
+    const int c = entry ? l.cls[j] : label;
+    if (!entry && (!HARD || (unsigned)label >= (unsigned)a.classes)) continue;
     if (c < lo || c >= hi) continue;
     // a class that is listed more than once has all of its entries' probabilities, by the first one
-    float sum = j < length ? p[j] : 0.f;
+    float sum = entry ? l.p[j] : 0.f;
     int times = 0;
-    for (int i = 0; i < length; i += 4) {
-      const int4 q = *reinterpret_cast<const int4*>(cls + i);
+#pragma unroll 4
+    for (int i = 0; i < l.length; i += 4) {
+      const int4 q = *reinterpret_cast<const int4*>(l.cls + i);
       times += (q.x == c ? 1 : 0) + (q.y == c ? 1 : 0) + (q.z == c ? 1 : 0) + (q.w == c ? 1 : 0);
     }
-    if (times > (j < length ? 1 : 0)) {
+    if (!entry && times) continue;                     // (a listed label is its entry's)
+    if (times > 1) {
       bool first = true;
-      for (int i = 0; i < length; ++i) {
-        const bool same = cls[i] == c;
+      for (int i = 0; i < l.length; ++i) {
+        const bool same = l.cls[i] == c;
         first = first && !(same && i < j);
-        if (same && i > j) sum += p[i];
+        if (same && i > j) sum += l.p[i];
       }
       if (!first) continue;
     }
-    const float z = j < length ? z_of[j] : z_label, d = z - r.max;
+    const float d = (entry ? l.z[j] : z_label) - r.max;
     float v = 0.f;
-    if (length) {
-      const float u = d * a.inv_t, q = expf(u) * inv;
-      const float diff = j < length && times == 1 && q > 0.5f && sum > 0.5f ? rest_of[j] - (r.rest - expm1f(u)) * inv : q - sum;
+    if (l.length) {
+      const float u = d * a.inv_t, q = exp2_fast(u * LOG2E) * inv;
+      float diff = q - sum;
+      if (entry && times == 1 && q > 0.5f && sum > 0.5f)
+        diff = (l.rest - expm1f((l.t[j] - l.max) * a.inv_t)) * l.inv - (r.rest - expm1f(u)) * inv;
       v = a.soft_slope * diff;
     }
-    if (HARD) v += a.hard * (c == label ? (expm1f(d) - r.rest1) * inv1 : expf(d) * inv1);
+    if (HARD) {
+      float own = exp2_fast(d * LOG2E) * inv1;
+      if (c == label) own = own > 0.5f ? (expm1f(d) - r.rest1) * inv1 : own - 1.f;
+      v += a.hard * own;
+    }
     Elem<T>::store(dz + c, v * inv_rows);
   }
 }
@@ -210,7 +224,17 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, int row, float
   const int tid = threadIdx.x % NT;
   const T* const z = static_cast<const T*>(a.z) + (size_t)row * a.classes;
   T* const dz = a.dz ? static_cast<T*>(a.dz) + (size_t)row * a.classes : nullptr;
-  const Row r(z, a.classes);
+  const Row r(z, a.classes, (long)(a.n - row) * a.classes);
+  // Short rows are asked for before it is known whether they count: everything is then on its way at once.
+  constexpr bool EAGER = NT <= 256;
+  chunk16 q[CH];
+  auto ask = [&]() {
+#pragma unroll
+    for (int u = 0; u < CH; ++u)
+      if (tid + u * NT < r.chunks) q[u] = r.load(z, tid + u * NT);
+  };
+  int rows = dz ? count_part<NT>(a) : 0;
+  if (EAGER) ask();
   if (!row_counts(a, row)) {
     if (tid == 0) a.loss_rows[row] = 0.f;
     if (dz)
@@ -219,31 +243,30 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, int row, float
         if (tid + u * NT < r.chunks) r.store(dz, tid + u * NT, chunk16{0, 0, 0, 0});
     return;
   }
-  chunk16 q[CH];
-#pragma unroll
-  for (int u = 0; u < CH; ++u)
-    if (tid + u * NT < r.chunks) q[u] = r.load(z, tid + u * NT);
-  int32_t* const cls = reinterpret_cast<int32_t*>(lists);
-  const int pitch = list_pitch(a.k);
-  float *const p = lists + pitch, *const rest_of = lists + 2 * pitch, *const z_of = lists + 3 * pitch;
+  if (!EAGER) ask();
+  List l = list_in(lists, a.k);
   const int label = HARD ? a.labels[row] : -1;
   float z_label = 0.f;
   if (HARD && (unsigned)label < (unsigned)a.classes) z_label = Elem<T>::load(z + label);
-  List l{};
-  if (tid < 64) {
-    l = read_list(a, row, cls, p, rest_of);
-    for (int j = tid; j < l.length; j += 64) z_of[j] = cls[j] < a.classes ? Elem<T>::load(z + cls[j]) : NAN;
-  }
+  l.length = row_reduce<NT>(list_read<NT>(a, row, l, [&](int, int c) { return Elem<T>::load(z + c); }), sh.n[0], Lower());
+  const float own_top = list_end<NT>(a, l);
   float own = -INFINITY;
 #pragma unroll
   for (int u = 0; u < CH; ++u)
     if (tid + u * NT < r.chunks) {
+      r.cut(q[u], tid + u * NT);
 #pragma unroll
       for (int e = 0; e < Row::PER; ++e) own = fmaxf(own, Row::value(q[u], e));
     }
-  int rows = dz ? count_part<NT>(a) : 0;
   RowSums t;
-  t.max = row_reduce<NT>(own, sh.v[0], Larger());
+  t.max = wave_reduce(own, Larger());
+  l.max = wave_reduce(own_top, Larger());
+  if constexpr (NT > 64) {
+    if ((tid & 63) == 0) { sh.v[0][tid >> 6] = t.max; sh.v[1][tid >> 6] = l.max; }
+    __syncthreads();
+    t.max = join_waves<NT>(sh.v[0], Larger());
+    l.max = join_waves<NT>(sh.v[1], Larger());
+  }
   const float inv_t2 = a.inv_t * LOG2E;
   float s = 0.f, s1 = 0.f, equal = 0.f;
   if (own == t.max) {
@@ -255,41 +278,49 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, int row, float
     for (int u = 0; u < CH; ++u)
       if (tid + u * NT < r.chunks) add_chunk<HARD, Row>(q[u], t.max, inv_t2, false, s, s1, equal);
   }
-  if (NT > 64 && tid == 0) sh.length = l.length;
-  // (one barrier for all of them)
+  float ls, lequal;
+  list_sum<NT>(a, l, ls, lequal);
   s = wave_reduce(s, Add());
   equal = wave_reduce(equal, Add());
   rows = wave_reduce(rows, Add());
   if (HARD) s1 = wave_reduce(s1, Add());
-  if constexpr (NT > 64) {
-    if ((tid & 63) == 0) { sh.v[1][tid >> 6] = s; sh.v[2][tid >> 6] = equal; sh.v[3][tid >> 6] = s1; sh.count[tid >> 6] = rows; }
+  ls = wave_reduce(ls, Add());
+  lequal = wave_reduce(lequal, Add());
+  if constexpr (NT > 64) {                             // (one barrier for all of them)
+    if ((tid & 63) == 0) {
+      const int w = tid >> 6;
+      sh.v[2][w] = s; sh.v[3][w] = equal; sh.v[4][w] = s1; sh.v[5][w] = ls; sh.v[6][w] = lequal; sh.n[1][w] = rows;
+    }
     __syncthreads();
-    s = join_waves<NT>(sh.v[1], Add());
-    equal = join_waves<NT>(sh.v[2], Add());
-    s1 = HARD ? join_waves<NT>(sh.v[3], Add()) : 0.f;
-    rows = join_waves<NT>(sh.count, Add());
+    s = join_waves<NT>(sh.v[2], Add());
+    equal = join_waves<NT>(sh.v[3], Add());
+    if (HARD) s1 = join_waves<NT>(sh.v[4], Add());
+    ls = join_waves<NT>(sh.v[5], Add());
+    lequal = join_waves<NT>(sh.v[6], Add());
+    rows = join_waves<NT>(sh.n[1], Add());
   }
   const float inv_rows = rows ? 1.f / (float)rows : 0.f;
   const bool none = fabsf(t.max) == INFINITY;          // no distribution
   t.rest = none ? NAN : s + (equal - 1.f);
   t.rest1 = none ? NAN : s1 + (equal - 1.f);
-  const int length = NT > 64 ? sh.length : l.length;
-  if (tid < 64) {
-    const float loss = loss_of(a, l, t, p, z_of, label, z_label);
-    if (tid == 0) a.loss_rows[row] = loss;
+  list_known(l, ls, lequal);
+  float d = wave_reduce(list_loss<NT>(a, l, t.max), Add());
+  if (NT > 64 && (tid & 63) == 0) sh.v[7][tid >> 6] = d;
+  if (dz) {
+    const Slope g = slope_of(a, t, l.length, inv_rows);
+#pragma unroll
+    for (int u = 0; u < CH; ++u)
+      if (tid + u * NT < r.chunks) {
+        float v[Row::PER];
+#pragma unroll
+        for (int e = 0; e < Row::PER; ++e) v[e] = g.template of<HARD>(Row::value(q[u], e));
+        r.store(dz, tid + u * NT, Row::pack(v));
+      }
   }
-  if (!dz) return;
-  const Slope g = slope_of(a, t, length, inv_rows);
-#pragma unroll
-  for (int u = 0; u < CH; ++u)
-    if (tid + u * NT < r.chunks) {
-      float v[Row::PER];
-#pragma unroll
-      for (int e = 0; e < Row::PER; ++e) v[e] = g.template of<HARD>(Row::value(q[u], e));
-      r.store(dz, tid + u * NT, Row::pack(v));
-    }
   row_sync<NT>();
-  write_listed<T, NT, HARD>(a, dz, 0, a.classes, length, cls, p, rest_of, z_of, t, label, z_label, inv_rows);
+  if (NT > 64 && tid < 64) d = join_waves<NT>(sh.v[7], Add());
+  if (tid == 0) a.loss_rows[row] = loss_of(a, l.length, d, t, label, z_label);
+  if (dz) write_listed<T, NT, HARD>(a, dz, 0, a.classes, l, t, label, z_label, inv_rows);
 }
 
 template <class T, int NT, int CH, bool HARD>
@@ -329,7 +360,7 @@ __global__ __launch_bounds__(256) void distill_part_kernel(DistillArgs a) {
   const int row = (int)blockIdx.x / a.splits, sp = (int)blockIdx.x - row * a.splits, tid = threadIdx.x;
   const T* const z = static_cast<const T*>(a.z) + (size_t)row * a.classes;
   if (!row_counts(a, row)) return;
-  const Row r(z, a.classes);
+  const Row r(z, a.classes, (long)(a.n - row) * a.classes);
   const int c0 = sp * a.chunks_per_split, c1 = min(c0 + a.chunks_per_split, r.chunks);
   if (sp == 0) {
     float* const at = a.at_list + (size_t)row * (a.k + 1);
@@ -342,12 +373,17 @@ __global__ __launch_bounds__(256) void distill_part_kernel(DistillArgs a) {
   float own = -INFINITY, s = 0.f, s1 = 0.f, equal = 0.f;
   const float inv_t2 = a.inv_t * LOG2E;
   for (int c = c0 + tid; c < c1; c += 256) {
-    const chunk16 q = r.load(z, c);
+    chunk16 q = r.load(z, c);
+    r.cut(q, c);
 #pragma unroll
     for (int e = 0; e < Row::PER; ++e) own = fmaxf(own, Row::value(q, e));
   }
   const float mx = row_reduce<256>(own, sh[0], Larger());
-  for (int c = c0 + tid; c < c1; c += 256) add_chunk<HARD, Row>(r.load(z, c), mx, inv_t2, own == mx, s, s1, equal);
+  for (int c = c0 + tid; c < c1; c += 256) {
+    chunk16 q = r.load(z, c);
+    r.cut(q, c);
+    add_chunk<HARD, Row>(q, mx, inv_t2, own == mx, s, s1, equal);
+  }
   s = row_reduce<256>(s, sh[1], Add());
   equal = row_reduce<256>(equal, sh[2], Add());
   if (HARD) s1 = row_reduce<256>(s1, sh[3], Add());
@@ -365,14 +401,14 @@ template <class T, bool HARD>
 __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a) {
   typedef RowChunks<T> Row;
   extern __shared__ __attribute__((aligned(16))) float lists[];
-  __shared__ int shc[4];
-  __shared__ int length_of;
+  __shared__ int shc[4], shn[4];
+  __shared__ float sh[4][4];
   const int row = (int)blockIdx.x / a.splits, sp = (int)blockIdx.x - row * a.splits, tid = threadIdx.x, lane = tid & 63;
   const int rows = row_reduce<256>(count_part<256>(a), shc, Add());
   const float inv_rows = rows ? 1.f / (float)rows : 0.f;
   const T* const z = static_cast<const T*>(a.z) + (size_t)row * a.classes;
   T* const dz = a.dz ? static_cast<T*>(a.dz) + (size_t)row * a.classes : nullptr;
-  const Row r(z, a.classes);
+  const Row r(z, a.classes, (long)(a.n - row) * a.classes);
   const int c0 = sp * a.chunks_per_split, c1 = min(c0 + a.chunks_per_split, r.chunks);
   if (!row_counts(a, row)) {
     if (tid == 0 && sp == 0) a.loss_rows[row] = 0.f;
@@ -394,25 +430,21 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a) {
   const bool none = fabsf(t.max) == INFINITY;
   t.rest = none ? NAN : s + (equal - 1.f);
   t.rest1 = none ? NAN : s1 + (equal - 1.f);
-  int32_t* const cls = reinterpret_cast<int32_t*>(lists);
-  const int pitch = list_pitch(a.k);
-  float *const p = lists + pitch, *const rest_of = lists + 2 * pitch, *const z_of = lists + 3 * pitch;
   const float* const kept = a.at_list + (size_t)row * (a.k + 1);
   const int label = HARD ? a.labels[row] : -1;
   const float z_label = HARD ? kept[a.k] : 0.f;
-  if (tid < 64) {
-    const List l = read_list(a, row, cls, p, rest_of);
-    for (int j = tid; j < l.length; j += 64) z_of[j] = kept[j];
-    if (tid == 0) length_of = l.length;
-    if (sp == 0) {
-      row_sync<64>();
-      const float loss = loss_of(a, l, t, p, z_of, label, z_label);
-      if (tid == 0) a.loss_rows[row] = loss;
-    }
-  }
+  List l = list_in(lists, a.k);
+  l.length = row_reduce<256>(list_read<256>(a, row, l, [&](int j, int) { return kept[j]; }), shn, Lower());
+  l.max = row_reduce<256>(list_end<256>(a, l), sh[0], Larger());
+  float ls, lequal;
+  list_sum<256>(a, l, ls, lequal);
+  ls = row_reduce<256>(ls, sh[1], Add());
+  lequal = row_reduce<256>(lequal, sh[2], Add());
+  list_known(l, ls, lequal);
+  const float d = row_reduce<256>(list_loss<256>(a, l, t.max), sh[3], Add());
+  if (tid == 0 && sp == 0) a.loss_rows[row] = loss_of(a, l.length, d, t, label, z_label);
   if (!dz) return;
-  __syncthreads();
-  const Slope g = slope_of(a, t, length_of, inv_rows);
+  const Slope g = slope_of(a, t, l.length, inv_rows);
   for (int c = c0 + tid; c < c1; c += 256) {
     const chunk16 q = r.load(z, c);
     float v[Row::PER];
@@ -421,7 +453,7 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a) {
     r.store(dz, c, Row::pack(v));
   }
   __syncthreads();
-  write_listed<T, 256, HARD>(a, dz, r.at(c0), c1 < r.chunks ? r.at(c1) : a.classes, length_of, cls, p, rest_of, z_of, t, label, z_label, inv_rows);
+  write_listed<T, 256, HARD>(a, dz, r.at(c0), c1 < r.chunks ? r.at(c1) : a.classes, l, t, label, z_label, inv_rows);
 }
 
 // loss = sum of loss_rows / rows that count, in a fixed order
@@ -452,7 +484,7 @@ inline long ceil_div(long a, long b) { return (a + b - 1) / b; }
 constexpr int kMostTop = 1024, kMostClasses = 1 << 20, kMostRows = 1 << 20;
 
 struct DistillPlan {
-  bool waves;                  // a wave per row
+  bool waves;                  // a wave per row, an entry of its list to a lane
   bool one;                    // sixteen rows at most, in one workgroup, with the mean
   int splits, chunks_per_split;      // 1: a workgroup per row
   int chunks;
@@ -463,8 +495,8 @@ DistillPlan distill_plan(int n, int classes, int k, int dtype) {
   DistillPlan p{};
   const int per = dtype == DT_BF16 ? 8 : 4;
   p.chunks = (classes + per - 1) / per + (classes % per ? 1 : 0);      // (a row begins inside one where the rows are not whole ones)
-  p.waves = p.chunks <= 64 * 4;
-  p.one = p.waves && n <= 16 && k <= 128;
+  p.waves = p.chunks <= 64 * 4 && k <= 64;
+  p.one = p.waves && n <= 16;
   p.splits = 1;
   if (p.chunks > 1024 * 16) {
     p.splits = (int)ceil_div(p.chunks, 4112);          // 64 KiB to a part: 64 parts at most

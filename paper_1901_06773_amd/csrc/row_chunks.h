@@ -1,8 +1,8 @@
 // A row of values that a workgroup (or a wave) keeps in its registers, sixteen bytes of it at a time.
 //
 // Rows of an odd number of values begin at any address that their type allows.  A row is cut at multiples of sixteen bytes of memory, not of the row, so
-// that every whole chunk is one aligned load or store; the first and the last chunk may hold values of the neighbouring rows, which are neither read
-// nor written: those two go value by value.
+// that every chunk is one aligned load; the first and the last may hold values of the neighbouring rows, which are cut off once all loads are on their way.
+// They are written value by value.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -19,25 +19,36 @@ typedef unsigned chunk16 __attribute__((ext_vector_type(4)));
 template <class T> struct RowChunks {
   static constexpr int PER = 16 / (int)sizeof(T);      // values of a chunk
   long first;          // the value of the row that chunk 0 begins with: 0, or up to PER - 1 before it
+  long ahead;          // values of the tensor from the row's first on
   int count, chunks;
-  __host__ __device__ __forceinline__ RowChunks(const T* row, int count_) : count(count_) {
+  __device__ __forceinline__ RowChunks(const T* row, int count_, long ahead_) : ahead(ahead_), count(count_) {
     const int before = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
     first = -before;
     chunks = (before + count + PER - 1) / PER;
   }
   __device__ __forceinline__ int at(int c) const { return c * PER + (int)first; }      // value that chunk c begins with
-  // chunk c; what lies beyond the row is minus infinity
+  // chunk c with what lies beside the row in it: what cut() is for
   __device__ __forceinline__ chunk16 load(const T* row, int c) const {
     const int e0 = at(c);
-    if (e0 >= 0 && e0 + PER <= count) return *reinterpret_cast<const chunk16*>(row + e0);
-    union { chunk16 v; T e[PER]; } u;
+    if (e0 + PER <= ahead) return *reinterpret_cast<const chunk16*>(row + e0);         // (a tensor begins on such an address)
+    union { chunk16 v; T e[PER]; } u;                  // the tensor's last values
 #pragma unroll
-    for (int e = 0; e < PER; ++e) {
-      if constexpr (sizeof(T) == 2) u.e[e] = 0xff80;
-      else u.e[e] = -INFINITY;
-      if (e0 + e >= 0 && e0 + e < count) u.e[e] = row[e0 + e];
-    }
+    for (int e = 0; e < PER; ++e) u.e[e] = row[e0 + e < ahead ? e0 + e : ahead - 1];
     return u.v;
+  }
+  // what lies beyond the row is minus infinity
+  __device__ __forceinline__ void cut(chunk16& v, int c) const {
+    const int e0 = at(c);
+    if (e0 >= 0 && e0 + PER <= count) return;
+    union { chunk16 v; T e[PER]; } u;
+    u.v = v;
+#pragma unroll
+    for (int e = 0; e < PER; ++e)
+      if (e0 + e < 0 || e0 + e >= count) {
+        if constexpr (sizeof(T) == 2) u.e[e] = 0xff80;
+        else u.e[e] = -INFINITY;
+      }
+    v = u.v;
   }
   __device__ __forceinline__ void store(T* row, int c, const chunk16& v) const {
     const int e0 = at(c);

@@ -34,11 +34,14 @@ struct TopArgs {
   int n, classes, k, segment, segments;
 };
 
-template <int NT> struct TopRoom { static constexpr int value = NT == 64 ? 512 : NT == 256 ? 1024 : 2048; };      // candidates in LDS, at least k
+// Candidates that LDS has room for, at least k; groups that a thread's values are dealt out to, each of which gives its largest one to the bound.
+template <int NT, int CH, int PER> struct TopShape {
+  static constexpr int room = NT == 64 ? 512 : NT < 1024 ? 1024 : CH == 1 ? 4096 : 2048, groups = NT == 1024 && CH == 1 && PER == 8 ? 4 : 1;
+};
 
 // The largest t, of its upper sixteen bits (a bound: the lower half may as well be zero), that `want` of the threads' keys reach.  Every wave looks at all
 // keys and tries another value of the next bits: log2 of the waves at a time, one barrier each (one wave, bit by bit: 1024 keys 1.6 us, so 0.5).
-template <int NT> __device__ __forceinline__ uint32_t reached_by(const uint32_t* keys, int want, int (*sh)[NT / 64]) {
+template <int NT, int GROUPS> __device__ __forceinline__ uint32_t reached_by(const uint32_t* keys, int want, int (*sh)[NT / 64]) {
   constexpr int W = NT / 64, BITS = W >= 16 ? 4 : W >= 8 ? 3 : W >= 4 ? 2 : 1;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint32_t t = 0;
@@ -47,7 +50,7 @@ template <int NT> __device__ __forceinline__ uint32_t reached_by(const uint32_t*
     const uint32_t mid = t | ((W == 1 ? 1u : (uint32_t)wave) << shift);
     int c = 0;
 #pragma unroll
-    for (int u = 0; u < W; ++u) c += __popcll(__ballot(keys[lane + 64 * u] >= mid));
+    for (int u = 0; u < W * GROUPS; ++u) c += __popcll(__ballot(keys[lane + 64 * u] >= mid));
     if constexpr (W == 1) {
       if (c >= want) t = mid;
     } else {
@@ -66,30 +69,35 @@ template <int NT> __device__ __forceinline__ uint32_t reached_by(const uint32_t*
 template <class T, int NT, int CH>
 __global__ __launch_bounds__(NT, CH == 8 ? 8 : 4) void top_kernel(TopArgs a) {
   typedef RowChunks<T> Row;
-  constexpr int PER = Row::PER, ROOM = TopRoom<NT>::value, W = NT / 64;
+  constexpr int PER = Row::PER, ROOM = TopShape<NT, CH, PER>::room, GROUPS = TopShape<NT, CH, PER>::groups, W = NT / 64;
   __shared__ unsigned long long cand[ROOM];
-  __shared__ uint32_t keys[NT];
+  __shared__ uint32_t keys[NT * GROUPS];
   __shared__ int counter, waves[2][W];
   const int tid = threadIdx.x, row_at = (int)blockIdx.x / a.segments, seg = (int)blockIdx.x - row_at * a.segments;
   const int from = seg * a.segment, count = min(a.segment, a.classes - from), want = min(a.k, count);
   const T* const row = static_cast<const T*>(a.z) + (size_t)row_at * a.classes + from;
-  const Row r(row, count);
+  const Row r(row, count, (long)(a.n - row_at) * a.classes - from);
   chunk16 q[CH];
-  float mx = -INFINITY;
 #pragma unroll
   for (int u = 0; u < CH; ++u)
     if (tid + u * NT < r.chunks) q[u] = r.load(row, tid + u * NT);
+  float mx[GROUPS];
+#pragma unroll
+  for (int g = 0; g < GROUPS; ++g) mx[g] = -INFINITY;
 #pragma unroll
   for (int u = 0; u < CH; ++u)
     if (tid + u * NT < r.chunks) {
+      r.cut(q[u], tid + u * NT);
 #pragma unroll
-      for (int e = 0; e < PER; ++e) mx = fmaxf(mx, Row::value(q[u], e));        // (what is no number reaches any bound)
+      for (int e = 0; e < PER; ++e) mx[e * GROUPS / PER] = fmaxf(mx[e * GROUPS / PER], Row::value(q[u], e));        // (what is no number reaches any bound)
     }
-  // keys of the threads without a value are the lowest
-  keys[tid] = tid < r.chunks ? order_of(mx) : 0;
+  // keys of the threads without a value are the lowest, those of a group without one (at an end of the row) minus infinity's
+#pragma unroll
+  for (int g = 0; g < GROUPS; ++g) keys[tid + g * NT] = tid < r.chunks ? order_of(mx[g]) : 0;
   if (tid == 0) counter = 0;
   row_sync<NT>();
-  const float low = want <= min(NT, r.chunks) ? value_of(max(reached_by<NT>(keys, want, waves), order_of(-INFINITY))) : -INFINITY;
+  // (a group without a value counts as minus infinity: a bound that needs it leaves out nothing)
+  const float low = want <= GROUPS * min(NT, r.chunks) ? value_of(max(reached_by<NT, GROUPS>(keys, want, waves), order_of(-INFINITY))) : -INFINITY;
   // f(key, column) for every value of the row, from the caches: the registers of the first two sweeps would not fit with this unrolled
   auto each = [&](auto f) {
 #pragma unroll 1
@@ -242,11 +250,21 @@ template <class T> hipError_t launch_top(const TopArgs& a, hipStream_t st) {
   // (a row begins inside a chunk where the rows are not whole ones)
   const int chunks = (a.segment + PER - 1) / PER + (a.classes % PER ? 1 : 0);
   const dim3 grid((unsigned)(a.n * a.segments));
-#define ACC_TOP(NT, CH) if (chunks <= NT * CH && a.k <= TopRoom<NT>::value) { hipLaunchKernelGGL((top_kernel<T, NT, CH>), grid, dim3(NT), 0, st, a); return hipGetLastError(); }
+  // The smallest workgroup that holds a row, of which all values fit LDS or the bound leaves out most: with k as many as three quarters of the groups it still
+  // leaves out half (10^3 rows of 1306 bf16 logits, k = 118: by a wave, whose 64 threads bound nothing, 108 us).  Sorting more than 128 values is slow in one wave.
+#define ACC_TOP(NT, CH)                                                                                                    \
+  {                                                                                                                        \
+    typedef TopShape<NT, CH, PER> S;                                                                                       \
+    const bool bounded = 4 * a.k <= 3 * S::groups * (chunks < NT ? chunks : NT);                                           \
+    if (chunks <= NT * CH && a.k <= S::room && (bounded || a.segment <= (NT < 1024 ? 2 * NT : S::room) || (NT == 1024 && CH > 1))) { \
+      hipLaunchKernelGGL((top_kernel<T, NT, CH>), grid, dim3(NT), 0, st, a);                                               \
+      return hipGetLastError();                                                                                            \
+    }                                                                                                                      \
+  }
   ACC_TOP(64, 1) ACC_TOP(64, 4)
-  ACC_TOP(256, 4) ACC_TOP(256, 8)
+  ACC_TOP(256, 1) ACC_TOP(256, 4) ACC_TOP(256, 8)
   ACC_TOP(512, 8)
-  ACC_TOP(1024, 8) ACC_TOP(1024, 16)
+  ACC_TOP(1024, 1) ACC_TOP(1024, 8) ACC_TOP(1024, 16)
 #undef ACC_TOP
   return hipErrorInvalidValue;
 }

@@ -42,7 +42,8 @@ def check(z, k):
 # one class, every entry, lists longer than a wave or than the threads of a row, widths that begin rows anywhere, each size of workgroup, rows in segments
 SIZES = [(1, 1, 1), (3, 2, 1), (5, 2, 2), (64, 1000, 16), (9, 63, 63), (4, 257, 65), (300, 10, 3), (7, 1021, 5), (33, 2039, 200), (3, 2048, 1024), (2, 1024, 1024),
          (5, 4099, 7), (40, 8191, 300), (6, 16385, 64), (11, 30011, 511), (3, 50001, 100), (2, 65409, 1), (2, 65536, 600), (3, 131008, 64), (2, 131009, 64),
-         (2, 131072, 256), (3, 300007, 33), (1, 1 << 20, 1024), (2, (1 << 20) - 3, 5)]
+         (2, 131072, 256), (5, 1306, 118), (9, 183, 33), (9, 183, 150), (4, 2500, 900), (3, 4500, 1024), (3, 8200, 800), (3, 8192, 1024), (2, 4097, 1024),
+         (3, 300007, 33), (1, 1 << 20, 1024), (2, (1 << 20) - 3, 5)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
