@@ -68,7 +68,25 @@ struct GluFinish {
   size_t dx_count, dw_count;
   int dx_splits, dw_splits, db_parts, pitch, half, f;
 };
-hipError_t glu_finish(const GluFinish& f, int dtype, hipStream_t st);
+// the sums of parts, and db unless another launch has it
+hipError_t glu_finish(const GluFinish& f, bool db, int dtype, hipStream_t st);
+constexpr int kDbColumns = 16;       // columns of db to a workgroup, sixteen threads down each
+inline unsigned glu_db_blocks(const GluFinish& f) { return f.db ? (unsigned)((2L * f.f + kDbColumns - 1) / kDbColumns) : 0; }
+__device__ __forceinline__ void glu_db(const GluFinish& f, int block) {
+  __shared__ double sh[256];
+  const int j = block * kDbColumns + (threadIdx.x & 15);
+  double s = 0.0;
+  if (j < 2 * f.f) {
+    const float* const p = f.db_part + (j < f.f ? j : f.half + j - f.f);
+#pragma unroll 8
+    for (int k = threadIdx.x >> 4; k < f.db_parts; k += 16) s += (double)p[(size_t)k * f.pitch];
+  }
+  sh[threadIdx.x] = s;
+  __syncthreads();
+  if (threadIdx.x >= 16 || j >= 2 * f.f) return;
+  for (int k = 1; k < 16; ++k) s += sh[threadIdx.x + 16 * k];
+  f.db[j] = (float)s;
+}
 
 size_t glu_bf16_workspace_bytes(int rows, int d, int f, bool backward);
 hipError_t glu_bf16(const GluArgs& a, bool backward);

@@ -156,19 +156,7 @@ __global__ __launch_bounds__(256) void glu_finish_kernel(GluFinish f, unsigned d
   block -= dx_blocks;
   if (block < dw_blocks) return join_sums<float>(f.dw_sums, f.dw, f.dw_count, f.dw_splits, block, dw_blocks);
   block -= dw_blocks;
-  // sixteen columns, sixteen threads down each
-  __shared__ double sh[256];
-  const int j = (int)block * 16 + (threadIdx.x & 15);
-  double s = 0.0;
-  if (j < 2 * f.f) {
-    const float* const p = f.db_part + (j < f.f ? j : f.half + j - f.f);
-    for (int k = threadIdx.x >> 4; k < f.db_parts; k += 16) s += (double)p[(size_t)k * f.pitch];
-  }
-  sh[threadIdx.x] = s;
-  __syncthreads();
-  if (threadIdx.x >= 16 || j >= 2 * f.f) return;
-  for (int k = 1; k < 16; ++k) s += sh[threadIdx.x + 16 * k];
-  f.db[j] = (float)s;
+  glu_db(f, (int)block);
 }
 
 // ---------------------------------------------------------------------------------- few rows
@@ -301,9 +289,27 @@ __global__ __launch_bounds__(C::THREADS) void glu32_kernel(Pair32 a, int blocks)
   }
 }
 
+// dx, dw and db in one launch of 64 x 64 tiles: they all wait for dz only, so where there are few tiles two launches less
+typedef Gemm32Cfg<2, 2, 2, 2, false, true, false> GluDx64;
+typedef Gemm32Cfg<2, 2, 2, 2, true, true, false> GluDw64;
+__global__ __launch_bounds__(256) void glu_grads32_kernel(Product32 dx, Product32 dw, GluFinish f, int dx_blocks, int dw_blocks) {
+  __shared__ __attribute__((aligned(16))) float lds[GluDx64::LDS > GluDw64::LDS ? GluDx64::LDS : GluDw64::LDS];
+  const int block = blockIdx.x;                        // (each part begins at a multiple of eight)
+  if (block < dx_blocks) {
+    const int work = (block & 7) * (dx_blocks >> 3) + (block >> 3);
+    if (work < dx.work) product32<GluDx64>(dx, work, lds);
+  } else if (block < dx_blocks + dw_blocks) {
+    const int work = (block & 7) * (dw_blocks >> 3) + ((block - dx_blocks) >> 3);
+    if (work < dw.work) product32<GluDw64>(dw, work, lds);
+  } else {
+    glu_db(f, block - dx_blocks - dw_blocks);
+  }
+}
+
 struct GluPlan32 {
   int tile;
   bool cut;
+  bool together;
   Cut proj, dx, dw;
   int db_parts;
   size_t sums, dz, dx_sums, dw_sums, db, total;
@@ -321,6 +327,9 @@ GluPlan32 glu_plan32(int rows, int d, int f, bool backward, bool kept) {
   if (backward) {
     p.dx = cut32(rows, d, wide, 1L << 25);
     p.dw = cut32(wide, d, rows, 1L << 25);
+    const Cut dx = cut32(rows, d, wide, 1L << 25, 1), dw = cut32(wide, d, rows, 1L << 25, 1);
+    p.together = ceil_div(d, 64) * (ceil_div(rows, 64) * dx.splits + ceil_div(wide, 64) * dw.splits) <= 1024;
+    if (p.together) { p.dx = dx; p.dw = dw; }
     p.dz = take((size_t)rows * wide * 4);
     p.dx_sums = take(p.dx.splits > 1 ? (size_t)p.dx.splits * rows * d * 4 : 0);
     p.dw_sums = take(p.dw.splits > 1 ? (size_t)p.dw.splits * wide * d * 4 : 0);
@@ -370,24 +379,28 @@ hipError_t glu32(const GluArgs& a, bool backward) {
     if (!backward) return hipGetLastError();
   }
   GluFinish f{};
+  Product32 gx{}, gw{};
   if (a.dx) {
-    Product32 g{};
-    g.a = {dz, a.rows, wide}; g.b = {w, a.d, a.d}; g.k = wide;
-    g.out = p.dx.splits > 1 ? (float*)(a.ws + p.dx_sums) : (float*)a.dx;
-    cut_into(g, p.dx);
-    if (const hipError_t e = launch_product32<false, true>(g, p.dx, st); e != hipSuccess) return e;
-    if (p.dx.splits > 1) { f.dx_sums = g.out; f.dx = a.dx; f.dx_count = (size_t)a.rows * a.d; f.dx_splits = p.dx.splits; }
+    gx.a = {dz, a.rows, wide}; gx.b = {w, a.d, a.d}; gx.k = wide;
+    gx.out = p.dx.splits > 1 ? (float*)(a.ws + p.dx_sums) : (float*)a.dx;
+    cut_into(gx, p.dx);
+    if (p.dx.splits > 1) { f.dx_sums = gx.out; f.dx = a.dx; f.dx_count = (size_t)a.rows * a.d; f.dx_splits = p.dx.splits; }
   }
   if (a.dw) {
-    Product32 g{};
-    g.a = {dz, wide, wide}; g.b = {x, a.d, a.d}; g.k = a.rows;
-    g.out = p.dw.splits > 1 ? (float*)(a.ws + p.dw_sums) : a.dw;
-    cut_into(g, p.dw);
-    if (const hipError_t e = launch_product32<true, true>(g, p.dw, st); e != hipSuccess) return e;
-    if (p.dw.splits > 1) { f.dw_sums = g.out; f.dw = a.dw; f.dw_count = (size_t)wide * a.d; f.dw_splits = p.dw.splits; }
+    gw.a = {dz, wide, wide}; gw.b = {x, a.d, a.d}; gw.k = a.rows;
+    gw.out = p.dw.splits > 1 ? (float*)(a.ws + p.dw_sums) : a.dw;
+    cut_into(gw, p.dw);
+    if (p.dw.splits > 1) { f.dw_sums = gw.out; f.dw = a.dw; f.dw_count = (size_t)wide * a.d; f.dw_splits = p.dw.splits; }
   }
   if (a.db) { f.db_part = db_part; f.db = a.db; f.db_parts = p.db_parts; f.pitch = wide; f.half = a.f; f.f = a.f; }
-  return glu_finish(f, DT_F32, st);
+  if (p.together) {
+    const unsigned bx = whole_eights(gx.work), bw = whole_eights(gw.work);
+    hipLaunchKernelGGL(glu_grads32_kernel, dim3(bx + bw + glu_db_blocks(f)), dim3(256), 0, st, gx, gw, f, (int)bx, (int)bw);
+  } else {
+    if (a.dx) if (const hipError_t e = launch_product32<false, true>(gx, p.dx, st); e != hipSuccess) return e;
+    if (a.dw) if (const hipError_t e = launch_product32<true, true>(gw, p.dw, st); e != hipSuccess) return e;
+  }
+  return glu_finish(f, !p.together, DT_F32, st);
 }
 
 // w takes fewer than 4 GiB as bf16 values, a launch fewer than 2^32 threads
@@ -423,9 +436,9 @@ hipError_t glu_point(const PointArgs& a, bool backward, int parts, int dtype, hi
   return hipGetLastError();
 }
 
-hipError_t glu_finish(const GluFinish& f, int dtype, hipStream_t st) {
+hipError_t glu_finish(const GluFinish& f, bool db, int dtype, hipStream_t st) {
   const unsigned bx = f.dx_splits > 1 ? join_blocks(f.dx_count) : 0, bw = f.dw_splits > 1 ? join_blocks(f.dw_count) : 0;
-  const unsigned blocks = bx + bw + (f.db ? (unsigned)ceil_div(2L * f.f, 16) : 0);
+  const unsigned blocks = bx + bw + (db ? glu_db_blocks(f) : 0);
   if (blocks) {
     if (dtype == DT_F32) hipLaunchKernelGGL(glu_finish_kernel<float>, dim3(blocks), dim3(256), 0, st, f, bx, bw);
     else hipLaunchKernelGGL(glu_finish_kernel<bf16_t>, dim3(blocks), dim3(256), 0, st, f, bx, bw);

@@ -23,7 +23,8 @@ struct PairArgs {
   const bf16_t* dh;            // backward
   bf16_t* dz[3];
   int pitch, half;             // of dz: columns, and where the value's begin
-  float* db_part;
+  float* db_part;              // sums of a wave's rows
+  int whole;                   // forward: tiles in one piece; those behind them (a last, short round of the compute units) in four
 };
 
 // 32 rows of a wave's columns by way of LDS, so that memory sees whole pieces of rows: EP bytes a staged row.
@@ -87,16 +88,14 @@ __device__ __forceinline__ void add_pair_bias(GemmAcc<C>& acc, const float* __re
     }
 }
 
-// h, and the projections where they are kept
+// LDS of a tile: its operands, then its staged results
+template <class C> struct TileLds {
+  static constexpr int OUT = C::WM * C::WN * Stage<C>::BYTES, value = C::LDS > OUT ? C::LDS : OUT;
+};
+// h, and the projections where they are kept, of the tile that begins at row m0 and column n0
 template <class C>
-__global__ __launch_bounds__(C::THREADS, 2) void glu_fwd_kernel(PairArgs a, int blocks) {
+__device__ __forceinline__ void glu_fwd_tile(const PairArgs& a, int m0, int n0, char* lds) {
   typedef Stage<C> S;
-  constexpr int OUT = C::WM * C::WN * S::BYTES;
-  __shared__ __attribute__((aligned(1024))) char lds[C::LDS > OUT ? C::LDS : OUT];
-  const int at = xcd_tile(blocks);
-  if (at >= a.tiles) return;
-  const TileAt where = tile_at(at, a.tiles_m, a.tiles);
-  const int m0 = where.m * C::BM, n0 = where.n * (C::BN / 2);
   GemmAcc<C> acc;
   gemm_tile<C>(a.x, a.w, m0, n0, 0, a.d, lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm0 = (wave / C::WN) * 32 * C::MB, col0 = n0 + (wave % C::WN) * S::COLS;
@@ -141,16 +140,10 @@ __device__ __forceinline__ float half_sum(float v) {
   return v;
 }
 
-// The projections again, which leave as dz, and the columns' sums of a tile
+// The projections again, which leave as dz, and the columns' sums of each 32 C::MB rows of a tile
 template <class C, int PARTS>
-__global__ __launch_bounds__(C::THREADS, 2) void glu_dz_kernel(PairArgs a, int blocks) {
+__device__ __forceinline__ void glu_dz_tile(const PairArgs& a, int m0, int n0, char* lds) {
   typedef Stage<C> S;
-  constexpr int OUT = C::WM * C::WN * S::BYTES;
-  __shared__ __attribute__((aligned(1024))) char lds[C::LDS > OUT ? C::LDS : OUT];
-  const int at = xcd_tile(blocks);
-  if (at >= a.tiles) return;
-  const TileAt where = tile_at(at, a.tiles_m, a.tiles);
-  const int m0 = where.m * C::BM, n0 = where.n * (C::BN / 2);
   GemmAcc<C> acc;
   gemm_tile<C>(a.x, a.w, m0, n0, 0, a.d, lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm0 = (wave / C::WN) * 32 * C::MB, col0 = n0 + (wave % C::WN) * S::COLS;
@@ -180,7 +173,7 @@ __global__ __launch_bounds__(C::THREADS, 2) void glu_dz_kernel(PairArgs a, int b
     wave_lds_done();
   }
   if (a.db_part) {
-    float* const to = a.db_part + (size_t)(where.m * C::WM + wave / C::WN) * a.pitch;
+    float* const to = a.db_part + (size_t)((m0 + wm0) / (32 * C::MB)) * a.pitch;
 #pragma unroll
     for (int j = 0; j < C::NB; ++j)
 #pragma unroll
@@ -219,6 +212,37 @@ __global__ __launch_bounds__(C::THREADS, 2) void glu_dz_kernel(PairArgs a, int b
         wave_lds_done();
       }
   }
+}
+
+// C: the tiles; Q: a quarter of one, in as many threads
+template <class C, class Q, class F> __device__ __forceinline__ void each_pair_tile(const PairArgs& a, int blocks, F f) {
+  const int block = blockIdx.x;
+  if (block < blocks) {
+    const int at = (block & 7) * (blocks >> 3) + (block >> 3);
+    if (at >= a.whole) return;
+    const TileAt where = tile_at(at, a.tiles_m, a.tiles);
+    f(C(), where.m * C::BM, where.n * (C::BN / 2));
+  } else {
+    const int rest = (int)gridDim.x - blocks, in = block - blocks, sub = (in & 7) * (rest >> 3) + (in >> 3), at = a.whole + (sub >> 2);
+    if (at >= a.tiles) return;
+    const TileAt where = tile_at(at, a.tiles_m, a.tiles);
+    const int m0 = where.m * C::BM + (sub & 1) * Q::BM, n0 = where.n * (C::BN / 2) + ((sub >> 1) & 1) * (Q::BN / 2);
+    if (m0 < a.rows && n0 < a.half) f(Q(), m0, n0);
+  }
+}
+template <class C, class Q>
+__global__ __launch_bounds__(C::THREADS, 2) void glu_fwd_kernel(PairArgs a, int blocks) {
+  static_assert(C::THREADS == Q::THREADS, "one shape of workgroups");
+  __shared__ __attribute__((aligned(1024))) char lds[TileLds<C>::value > TileLds<Q>::value ? TileLds<C>::value : TileLds<Q>::value];
+  each_pair_tile<C, Q>(a, blocks, [&](auto c, int m0, int n0) { glu_fwd_tile<decltype(c)>(a, m0, n0, lds); });
+}
+template <class C, int PARTS>
+__global__ __launch_bounds__(C::THREADS, 2) void glu_dz_kernel(PairArgs a, int blocks) {
+  __shared__ __attribute__((aligned(1024))) char lds[TileLds<C>::value];
+  const int at = xcd_tile(blocks);
+  if (at >= a.tiles) return;
+  const TileAt where = tile_at(at, a.tiles_m, a.tiles);
+  glu_dz_tile<C, PARTS>(a, where.m * C::BM, where.n * (C::BN / 2), lds);
 }
 
 // out[split][rows][cols] = A B over the split's k, fp32, or rounded to bf16 where there is one split
@@ -312,18 +336,20 @@ __global__ __launch_bounds__(C::THREADS, 2) void glu_dw_kernel(GluDwArgs a, int 
   const int work = xcd_tile(blocks);
   if (work < a.work) glu_dw<C>(a, work, lds);
 }
-// dx and dw in one launch where there are few tiles: both wait for dz only
+// dx, dw and db in one launch where there are few tiles: they all wait for dz only
 template <class CX, class CW>
-__global__ __launch_bounds__(256, 2) void glu_grads_kernel(ProductArgs x, GluDwArgs w, int x_blocks, int w_blocks) {
+__global__ __launch_bounds__(256, 2) void glu_grads_kernel(ProductArgs x, GluDwArgs w, GluFinish f, int x_blocks, int w_blocks) {
   static_assert(CX::THREADS == 256 && CW::THREADS == 256, "one shape of workgroups");
   __shared__ __attribute__((aligned(1024))) char lds[CX::LDS > CW::LDS ? CX::LDS : CW::LDS];
   const int block = blockIdx.x;                        // (each part begins at a multiple of eight)
   if (block < x_blocks) {
     const int work = (block & 7) * (x_blocks >> 3) + (block >> 3);
     if (work < x.work) glu_product<CX>(x, work, lds);
-  } else {
+  } else if (block < x_blocks + w_blocks) {
     const int work = (block & 7) * (w_blocks >> 3) + ((block - x_blocks) >> 3);
     if (work < w.work) glu_dw<CW>(w, work, lds);
+  } else {
+    glu_db(f, block - x_blocks - w_blocks);
   }
 }
 
@@ -354,8 +380,10 @@ __global__ __launch_bounds__(256) void glu_pad_kernel(const bf16_t* __restrict__
 
 //                WM WN MB NB BK NS   AT     BT  PARTS SWAP  PAIR
 typedef GemmCfg<4, 2, 2, 4, 64, 2, false, false, 1, true, true> G256;      // gate and value
+typedef GemmCfg<4, 2, 1, 2, 64, 3, false, false, 1, true, true> G256Q;     // a quarter of that
+typedef GemmCfg<2, 2, 4, 2, 32, 3, false, false, 1, true, true> G256N;     // 256 x 128: two workgroups a compute unit
 typedef GemmCfg<2, 2, 2, 2, 64, 2, false, false, 1, true, true> G128;
-typedef GemmCfg<2, 1, 1, 2, 64, 4, false, false, 1, true, true> G64;
+typedef GemmCfg<2, 1, 1, 2, 64, 3, false, false, 1, true, true> G64;
 typedef GemmCfg<2, 2, 2, 2, 64, 2, false, false, 1, true> S128;            // projections in parts
 typedef GemmCfg<2, 2, 1, 1, 64, 4, false, false, 1, true> S64;
 typedef GemmCfg<2, 4, 4, 2, 64, 2, false, true, 1, true> X256;             // dx
@@ -368,11 +396,39 @@ typedef GemmCfg<2, 4, 4, 2, 32, 2, true, true, 3, false> V256;             // dw
 typedef GemmCfg<2, 2, 2, 2, 32, 2, true, true, 3, false> V128;
 typedef GemmCfg<2, 2, 1, 1, 32, 3, true, true, 3, false> V64;
 
+// Which tile of gate and value, by predicted time as in gemm_tiles.h.  Constants from sixty sizes (rows 32 to 30000, widths 32 to 4096 and 6000), every tile on each.
+struct PairTile {
+  int m, n, db_rows;           // n: columns of both together; rows of a wave
+  bool alone;                  // one workgroup a compute unit
+  TileCost cost[2];            // forward, backward
+};
+constexpr PairTile kPair[4] = {{256, 256, 64, true, {{6.0, 1.2, 7.7, 1.86}, {22.7, 1.27, 30.3, 1.7}}},
+                               {256, 128, 128, false, {{4.0, 1.2, 4.0, 1.0}, {14.5, 1.2, 10.9, 0.92}}},
+                               {128, 128, 64, false, {{0.1, 0.79, 2.2, 0.5}, {9.9, 0.84, 7.4, 0.5}}},
+                               {64, 64, 32, false, {{1.3, 0.24, 0.85, 0.225}, {5.6, 0.42, 1.8, 0.12}}}};
+// Tiles in one piece, forward: those of whole rounds of the compute units, where what is left is half a round at most.  us, without quarters / with: 12544 rows,
+// 1024 to 2 x 4096 (6.1 rounds) 219 / 206, 8449, 1024 to 2 x 1040 (1.2) 52 / 43, 4161, 1536 to 2 x 2200 (1.2) 73 / 60.
+long pair_whole(const PairTile& t, long tiles) {
+  const long rest = tiles % 256;
+  return t.alone && tiles > 256 && rest <= 128 ? tiles - rest : tiles;
+}
+double pair_us(const PairTile& t, bool backward, long tiles, double steps) {
+  const TileCost& c = t.cost[backward];
+  const double first = c.first + c.first_step * steps, next = c.next + c.next_step * steps;
+  if (t.alone) {
+    const long whole = backward ? tiles : pair_whole(t, tiles);
+    return 3.0 + first + (ceil_div(whole, 256) - 1) * next + ceil_div(4 * (tiles - whole), 256) * 0.35 * next;
+  }
+  const long most = ceil_div(tiles, 256);
+  auto round = [&](long r) { return r == 0 ? 0.0 : first > r * next ? first : r * next; };
+  return 3.0 + (most / 2) * round(2) + round(most % 2);
+}
+
 struct GluPlan16 {
   int dp, fp;                  // widths as they are multiplied, multiples of 8
   bool pad_x, pad_w;
   int parts;                   // bf16 values that dz is the sum of
-  int tile;                    // of gate and value together
+  PairTile tile;               // of gate and value together
   bool cut;                    // the projections' sums in parts, and what follows value by value
   Choice proj, dx, dw;
   bool together;               // dx and dw in one launch of 64 x 64 tiles
@@ -389,13 +445,13 @@ GluPlan16 glu_plan16(int rows, int d, int f, bool backward, bool kept) {
   p.parts = rows < 4096 ? 3 : 2;
   const long wide = 2L * p.fp;
   double us = 0;
-  for (int t = 0; t < 3; ++t) {
-    const double v = tile_us(RowsByRows, t, ceil_div(rows, kTiles[t]) * ceil_div(wide, kTiles[t]), p.dp / 64.0);
-    if (t == 0 || v < us) { us = v; p.tile = kTiles[t]; }
+  for (const PairTile& t : kPair) {
+    const double v = pair_us(t, backward, ceil_div(rows, t.m) * ceil_div(p.fp, t.n / 2), p.dp / 64.0);
+    if (us == 0 || v < us) { us = v; p.tile = t; }
   }
   // few tiles of a long sum: parts of it, whose sums a second launch adds up
   p.proj = choose(RowsByRows, rows, wide, p.dp, 1, 1L << 24, 128, 1);
-  p.cut = !kept && p.proj.splits > 1 && p.proj.us + 1.0 < us;
+  p.cut = !kept && p.proj.splits > 1 && p.proj.us + (backward ? 7.0 : 2.0) < us;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t a = at; at += al256(bytes); return a; };
   p.x = take(p.pad_x ? (size_t)rows * p.dp * 2 : 0);
@@ -418,8 +474,8 @@ GluPlan16 glu_plan16(int rows, int d, int f, bool backward, bool kept) {
     p.dw_sums = take(p.dw.splits > 1 ? (size_t)p.dw.splits * 2 * f * d * 4 : 0);
     PointArgs q{};
     q.rows = rows; q.f = f;
-    p.db_parts = kept || p.cut ? glu_point_shape(q, DT_BF16) : (int)ceil_div(rows, p.tile) * (p.tile == 256 ? 4 : 2);
-    p.db = take((size_t)p.db_parts * wide * 4);
+    p.db_parts = kept || p.cut ? glu_point_shape(q, DT_BF16) : (int)ceil_div(rows, p.tile.db_rows);
+    p.db = take((size_t)(kept || p.cut ? p.db_parts : up(rows, p.tile.m) / p.tile.db_rows) * wide * 4);
   }
   p.total = at;
   return p;
@@ -427,9 +483,9 @@ GluPlan16 glu_plan16(int rows, int d, int f, bool backward, bool kept) {
 
 unsigned whole_eights16(long work) { return (unsigned)((work + 7) / 8 * 8); }
 
-template <class C> void launch_pair(const PairArgs& g, bool backward, int parts, hipStream_t st) {
-  const unsigned blocks = whole_eights16(g.tiles);
-  if (!backward) hipLaunchKernelGGL(glu_fwd_kernel<C>, dim3(blocks), dim3(C::THREADS), 0, st, g, (int)blocks);
+template <class C, class Q> void launch_pair(const PairArgs& g, bool backward, int parts, hipStream_t st) {
+  const unsigned blocks = whole_eights16(backward ? g.tiles : g.whole), grid = blocks + whole_eights16(4L * (g.tiles - g.whole));
+  if (!backward) hipLaunchKernelGGL((glu_fwd_kernel<C, Q>), dim3(grid), dim3(C::THREADS), 0, st, g, (int)blocks);
   else if (parts == 3) hipLaunchKernelGGL((glu_dz_kernel<C, 3>), dim3(blocks), dim3(C::THREADS), 0, st, g, (int)blocks);
   else hipLaunchKernelGGL((glu_dz_kernel<C, 2>), dim3(blocks), dim3(C::THREADS), 0, st, g, (int)blocks);
 }
@@ -491,13 +547,15 @@ hipError_t glu_bf16(const GluArgs& a, bool backward) {
     g.w = GemmOperand{w, {w + (size_t)p.fp * p.dp}, a.f, p.dp, p.dp};
     g.bias = a.bias;
     g.rows = a.rows; g.d = p.dp; g.f = a.f; g.act = a.act;
-    g.tiles_m = (int)ceil_div(a.rows, p.tile); g.tiles = g.tiles_m * (int)ceil_div(p.fp, p.tile / 2);
+    g.tiles_m = (int)ceil_div(a.rows, p.tile.m); g.tiles = g.tiles_m * (int)ceil_div(p.fp, p.tile.n / 2);
+    g.whole = (int)pair_whole(p.tile, g.tiles);
     g.h = (bf16_t*)a.h; g.ab = (bf16_t*)a.ab; g.dh = (const bf16_t*)a.dh;
     for (int i = 0; i < 3; ++i) g.dz[i] = dz[i];
     g.pitch = wide; g.half = p.fp; g.db_part = db_part;
-    if (p.tile == 256) launch_pair<G256>(g, backward, p.parts, st);
-    else if (p.tile == 128) launch_pair<G128>(g, backward, p.parts, st);
-    else launch_pair<G64>(g, backward, p.parts, st);
+    if (p.tile.m == 256 && p.tile.n == 256) launch_pair<G256, G256Q>(g, backward, p.parts, st);
+    else if (p.tile.m == 256) launch_pair<G256N, G256N>(g, backward, p.parts, st);
+    else if (p.tile.m == 128) launch_pair<G128, G128>(g, backward, p.parts, st);
+    else launch_pair<G64, G64>(g, backward, p.parts, st);
     if (!backward) return hipGetLastError();
   }
   const GemmOperand z{dz[0], {dz[1], dz[2]}, a.rows, wide, wide};
@@ -520,11 +578,12 @@ hipError_t glu_bf16(const GluArgs& a, bool backward) {
     gw.tiles_m = (int)ceil_div(wide, p.dw.tile); gw.tiles = gw.tiles_m * (int)ceil_div(a.d, p.dw.tile); gw.work = gw.tiles * p.dw.splits;
     if (p.dw.splits > 1) { f.dw_sums = gw.out; f.dw = a.dw; f.dw_count = 2 * (size_t)a.f * a.d; f.dw_splits = p.dw.splits; }
   }
+  if (a.db) { f.db_part = db_part; f.db = a.db; f.db_parts = p.db_parts; f.pitch = wide; f.half = p.fp; f.f = a.f; }
   if (p.together) {
     const unsigned bx = whole_eights16(gx.work), bw = whole_eights16(gw.work);
-    if (bx + bw == 0) {
-    } else if (p.parts == 3) hipLaunchKernelGGL((glu_grads_kernel<X64, V64>), dim3(bx + bw), dim3(256), 0, st, gx, gw, (int)bx, (int)bw);
-    else hipLaunchKernelGGL((glu_grads_kernel<X64, W64>), dim3(bx + bw), dim3(256), 0, st, gx, gw, (int)bx, (int)bw);
+    const dim3 grid(bx + bw + glu_db_blocks(f));
+    if (p.parts == 3) hipLaunchKernelGGL((glu_grads_kernel<X64, V64>), grid, dim3(256), 0, st, gx, gw, f, (int)bx, (int)bw);
+    else hipLaunchKernelGGL((glu_grads_kernel<X64, W64>), grid, dim3(256), 0, st, gx, gw, f, (int)bx, (int)bw);
   } else {
     if (a.dx) {
       if (p.dx.tile == 256) launch_product<X256>(gx, st);
@@ -536,8 +595,7 @@ hipError_t glu_bf16(const GluArgs& a, bool backward) {
       else { if (p.dw.tile == 256) launch_dw<W256>(gw, st); else if (p.dw.tile == 128) launch_dw<W128>(gw, st); else launch_dw<W64>(gw, st); }
     }
   }
-  if (a.db) { f.db_part = db_part; f.db = a.db; f.db_parts = p.db_parts; f.pitch = wide; f.half = p.fp; f.f = a.f; }
-  return glu_finish(f, DT_BF16, st);
+  return glu_finish(f, !p.together, DT_BF16, st);
 }
 
 }  // namespace acc
