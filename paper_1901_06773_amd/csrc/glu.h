@@ -12,24 +12,22 @@ namespace acc {
 
 enum { GLU_NONE = 0, GLU_RELU = 1, GLU_SILU = 2 };     // as ACC_ACT_*
 
+// act(a) = a s, act'(a) = s (1 + a (1 - s)) with s = 1, s = 1 where a is above 0 and 0 elsewhere (ReLU), or the sigmoid (SiLU): one way for all three.  (A branch for
+// each makes the code of a tile, whose registers are named in it value by value, three times as long: a launch with one tile to a compute unit waits
+// for its instructions.)  Where s is 0 or 1 a product with it is left out, so that an infinity times 0 makes no NaN.  A value that is no number stays none.
+__device__ __forceinline__ float glu_share(int act, float a) {
+  const float s = sigmoid(a), step = a <= 0.f ? 0.f : 1.f;
+  return act == GLU_SILU ? s : act == GLU_RELU ? step : 1.f;
+}
 __device__ __forceinline__ float glu_act(int act, float a) {
-  if (act == GLU_RELU) return a < 0.f ? 0.f : a;       // (a value that is no number stays none)
-  if (act == GLU_SILU) return a * sigmoid(a);
-  return a;
+  const float s = glu_share(act, a);
+  return s == 0.f ? 0.f : a * s;
 }
 // gradients of h = act(a) b at a and b
 __device__ __forceinline__ void glu_slopes(int act, float a, float b, float dh, float& da, float& db) {
-  if (act == GLU_RELU) {
-    da = a > 0.f ? dh * b : 0.f;
-    db = dh * (a < 0.f ? 0.f : a);
-  } else if (act == GLU_SILU) {
-    const float s = sigmoid(a);
-    da = dh * b * (s * (1.f + a * (1.f - s)));
-    db = dh * (a * s);
-  } else {
-    da = dh * b;
-    db = dh * a;
-  }
+  const float s = glu_share(act, a);
+  da = s == 0.f ? 0.f : dh * b * (s == 1.f ? 1.f : s * (1.f + a * (1.f - s)));
+  db = s == 0.f ? 0.f : dh * (a * s);
 }
 
 struct GluArgs {

@@ -11,6 +11,8 @@
 #include "glu.h"
 #include "product32.h"
 
+#include <type_traits>
+
 namespace acc {
 namespace {
 
@@ -56,7 +58,7 @@ template <class T, int V> __device__ __forceinline__ void put(T* p, int left, co
 // ---------------------------------------------------------------------------------- value by value
 template <class T> struct PointWidth { static constexpr int value = 16 / (int)sizeof(T); };
 
-template <class T, bool BWD, int PARTS>
+template <class T, bool BWD, int PARTS, bool SUMS>
 __global__ __launch_bounds__(256) void glu_point_kernel(PointArgs a) {
   constexpr int V = PointWidth<T>::value;
   __shared__ float sh[BWD ? 2 * V : 1][256];
@@ -74,20 +76,28 @@ __global__ __launch_bounds__(256) void glu_point_kernel(PointArgs a) {
   const int r1 = min((slab + 1) * a.slab, a.rows);
   for (int r = slab * a.slab + ty; r < r1 && left > 0; r += step) {
     float g[V], v[V];
-    if (a.sums) {
+    if constexpr (SUMS) {
       const float* const from = a.sums + (size_t)r * 2 * a.half + c;
 #pragma unroll
       for (int e = 0; e < V; ++e) { g[e] = ba[e]; v[e] = bb[e]; }
-      for (int s = 0; s < a.splits; ++s) {
+      auto add = [&](int s0, auto several) {           // so many parts on their way at once
+        constexpr int U = decltype(several)::value;
+        float p[U][V], q[U][V];
 #pragma unroll
-        for (int e = 0; e < V; e += 4) {
-          float p[4], q[4];
-          get<float, 4>(from + s * whole + e, left - e, p);
-          get<float, 4>(from + s * whole + a.half + e, left - e, q);
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-          for (int u = 0; u < 4; ++u) { g[e + u] += p[u]; v[e + u] += q[u]; }
-        }
-      }
+          for (int e = 0; e < V; e += 4) {
+            get<float, 4>(from + (s0 + u) * whole + e, left - e, *reinterpret_cast<float(*)[4]>(&p[u][e]));
+            get<float, 4>(from + (s0 + u) * whole + a.half + e, left - e, *reinterpret_cast<float(*)[4]>(&q[u][e]));
+          }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int e = 0; e < V; ++e) { g[e] += p[u][e]; v[e] += q[u][e]; }
+      };
+      int s = 0;
+      for (; s + 4 <= a.splits; s += 4) add(s, std::integral_constant<int, 4>());
+      for (; s < a.splits; ++s) add(s, std::integral_constant<int, 1>());
     } else {
       const T* const from = static_cast<const T*>(a.ab_in) + (size_t)r * 2 * a.f + c;
       get<T, V>(from, left, g);
@@ -149,12 +159,30 @@ __global__ __launch_bounds__(256) void glu_point_kernel(PointArgs a) {
 }
 
 // ---------------------------------------------------------------------------------- sums of parts
+// Many parts of few values: sixty-four values to a workgroup, a quarter of the parts to each wave
+constexpr int kManyParts = 16;
+template <class T> __device__ __forceinline__ void join_many(const float* __restrict__ sums, T* __restrict__ out, size_t count, int splits, size_t block) {
+  __shared__ float sh[256];
+  const size_t i = block * 64 + (threadIdx.x & 63);
+  const int each = (splits + 3) / 4, k0 = (int)(threadIdx.x >> 6) * each, k1 = min(k0 + each, splits);
+  float s = 0.f;
+  if (i < count) {
+#pragma unroll 8
+    for (int k = k0; k < k1; ++k) s += sums[(size_t)k * count + i];
+  }
+  sh[threadIdx.x] = s;
+  __syncthreads();
+  if (threadIdx.x < 64 && i < count) Elem<T>::store(out + i, ((s + sh[threadIdx.x + 64]) + sh[threadIdx.x + 128]) + sh[threadIdx.x + 192]);
+}
+inline bool many_parts(size_t count, int splits) { return splits >= kManyParts && count <= 1u << 20; }
 template <class T>
-__global__ __launch_bounds__(256) void glu_finish_kernel(GluFinish f, unsigned dx_blocks, unsigned dw_blocks) {
+__global__ __launch_bounds__(256) void glu_finish_kernel(GluFinish f, unsigned dx_blocks, unsigned dw_blocks, int many) {
   unsigned block = blockIdx.x;
-  if (block < dx_blocks) return join_sums<T>(f.dx_sums, (T*)f.dx, f.dx_count, f.dx_splits, block, dx_blocks);
+  if (block < dx_blocks)
+    return many & 1 ? join_many<T>(f.dx_sums, (T*)f.dx, f.dx_count, f.dx_splits, block) : join_sums<T>(f.dx_sums, (T*)f.dx, f.dx_count, f.dx_splits, block, dx_blocks);
   block -= dx_blocks;
-  if (block < dw_blocks) return join_sums<float>(f.dw_sums, f.dw, f.dw_count, f.dw_splits, block, dw_blocks);
+  if (block < dw_blocks)
+    return many & 2 ? join_many<float>(f.dw_sums, f.dw, f.dw_count, f.dw_splits, block) : join_sums<float>(f.dw_sums, f.dw, f.dw_count, f.dw_splits, block, dw_blocks);
   block -= dw_blocks;
   glu_db(f, (int)block);
 }
@@ -306,6 +334,8 @@ __global__ __launch_bounds__(256) void glu_grads32_kernel(Product32 dx, Product3
   }
 }
 
+constexpr double kSaved = 3.0;         // us
+
 struct GluPlan32 {
   int tile;
   bool cut;
@@ -329,7 +359,12 @@ GluPlan32 glu_plan32(int rows, int d, int f, bool backward, bool kept) {
     p.dw = cut32(wide, d, rows, 1L << 25);
     const Cut dx = cut32(rows, d, wide, 1L << 25, 1), dw = cut32(wide, d, rows, 1L << 25, 1);
     p.together = ceil_div(d, 64) * (ceil_div(rows, 64) * dx.splits + ceil_div(wide, 64) * dw.splits) <= 1024;
-    if (p.together) { p.dx = dx; p.dw = dw; }
+    if (p.together) {
+      p.dx = dx; p.dw = dw;
+      // (whole sums save the launch that adds parts)
+      const Cut x1 = cut32(rows, d, wide, 0, 1), w1 = cut32(wide, d, rows, 0, 1);
+      if (x1.us < dx.us + kSaved && w1.us < dw.us + kSaved) { p.dx = x1; p.dw = w1; }
+    }
     p.dz = take((size_t)rows * wide * 4);
     p.dx_sums = take(p.dx.splits > 1 ? (size_t)p.dx.splits * rows * d * 4 : 0);
     p.dw_sums = take(p.dw.splits > 1 ? (size_t)p.dw.splits * wide * d * 4 : 0);
@@ -426,22 +461,24 @@ int glu_point_shape(PointArgs& a, int dtype) {
 
 hipError_t glu_point(const PointArgs& a, bool backward, int parts, int dtype, hipStream_t st) {
   const dim3 grid((unsigned)(ceil_div(a.rows, a.slab) * a.across));
-#define ACC_POINT(T, BWD, PARTS) hipLaunchKernelGGL((glu_point_kernel<T, BWD, PARTS>), grid, dim3(256), 0, st, a)
-  if (dtype == DT_F32) { if (backward) ACC_POINT(float, true, 1); else ACC_POINT(float, false, 1); }
-  else if (!backward) ACC_POINT(bf16_t, false, 1);
-  else if (parts == 3) ACC_POINT(bf16_t, true, 3);
-  else if (parts == 2) ACC_POINT(bf16_t, true, 2);
-  else ACC_POINT(bf16_t, true, 1);
+#define ACC_POINT(T, BWD, PARTS, SUMS) hipLaunchKernelGGL((glu_point_kernel<T, BWD, PARTS, SUMS>), grid, dim3(256), 0, st, a)
+  if (!backward) { if (dtype == DT_F32) ACC_POINT(float, false, 1, true); else ACC_POINT(bf16_t, false, 1, true); }
+  else if (dtype == DT_F32) { if (a.sums) ACC_POINT(float, true, 1, true); else ACC_POINT(float, true, 1, false); }
+  else if (parts == 3) { if (a.sums) ACC_POINT(bf16_t, true, 3, true); else ACC_POINT(bf16_t, true, 3, false); }
+  else if (parts == 2) { if (a.sums) ACC_POINT(bf16_t, true, 2, true); else ACC_POINT(bf16_t, true, 2, false); }
+  else { if (a.sums) ACC_POINT(bf16_t, true, 1, true); else ACC_POINT(bf16_t, true, 1, false); }
 #undef ACC_POINT
   return hipGetLastError();
 }
 
 hipError_t glu_finish(const GluFinish& f, bool db, int dtype, hipStream_t st) {
-  const unsigned bx = f.dx_splits > 1 ? join_blocks(f.dx_count) : 0, bw = f.dw_splits > 1 ? join_blocks(f.dw_count) : 0;
+  const int many = (many_parts(f.dx_count, f.dx_splits) ? 1 : 0) | (many_parts(f.dw_count, f.dw_splits) ? 2 : 0);
+  const unsigned bx = f.dx_splits <= 1 ? 0 : many & 1 ? (unsigned)((f.dx_count + 63) / 64) : join_blocks(f.dx_count);
+  const unsigned bw = f.dw_splits <= 1 ? 0 : many & 2 ? (unsigned)((f.dw_count + 63) / 64) : join_blocks(f.dw_count);
   const unsigned blocks = bx + bw + (db ? glu_db_blocks(f) : 0);
   if (blocks) {
-    if (dtype == DT_F32) hipLaunchKernelGGL(glu_finish_kernel<float>, dim3(blocks), dim3(256), 0, st, f, bx, bw);
-    else hipLaunchKernelGGL(glu_finish_kernel<bf16_t>, dim3(blocks), dim3(256), 0, st, f, bx, bw);
+    if (dtype == DT_F32) hipLaunchKernelGGL(glu_finish_kernel<float>, dim3(blocks), dim3(256), 0, st, f, bx, bw, many);
+    else hipLaunchKernelGGL(glu_finish_kernel<bf16_t>, dim3(blocks), dim3(256), 0, st, f, bx, bw, many);
   }
   return hipGetLastError();
 }

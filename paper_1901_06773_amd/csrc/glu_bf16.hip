@@ -29,41 +29,60 @@ struct PairArgs {
 
 // 32 rows of a wave's columns by way of LDS, so that memory sees whole pieces of rows: EP bytes a staged row.
 template <class C> struct Stage {
-  static constexpr int COLS = 16 * C::NB, EP = COLS * 2 + 16, PER = COLS / 8, ROWS = 64 / PER, BYTES = 32 * EP;      // PER lanes to a row
+  static constexpr int COLS = 16 * C::NB, EP = COLS * 2 + 16, PER = COLS / 8, ROWS = 64 / PER, ONE = 32 * EP, BYTES = 3 * ONE;      // PER lanes to a row; three results at once
 };
-// rows of `pitch` values from `to` on; columns [0, left) and rows [0, rows) exist.  whole: sixteen bytes at a time
-template <class C> __device__ __forceinline__ void rows_out(const char* stg, bf16_t* to, size_t pitch, int rows, int left, bool whole) {
+// What a lane moves of 32 staged rows
+template <class C> struct StagePart { v4u v[32 / Stage<C>::ROWS]; };
+template <class C> __device__ __forceinline__ StagePart<C> staged(const char* stg) {
+  typedef Stage<C> S;
+  const int lane = threadIdx.x & 63;
+  StagePart<C> p;
+#pragma unroll
+  for (int it = 0; it < 32 / S::ROWS; ++it) p.v[it] = *reinterpret_cast<const v4u*>(stg + (lane / S::PER + S::ROWS * it) * S::EP + 16 * (lane % S::PER));
+  return p;
+}
+template <class C> __device__ __forceinline__ void stage(char* stg, const StagePart<C>& p) {
+  typedef Stage<C> S;
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int it = 0; it < 32 / S::ROWS; ++it) *reinterpret_cast<v4u*>(stg + (lane / S::PER + S::ROWS * it) * S::EP + 16 * (lane % S::PER)) = p.v[it];
+}
+// To and from rows of `pitch` values, a multiple of eight; columns [0, left) and rows [0, rows) exist.
+template <class C> __device__ __forceinline__ void rows_out(const StagePart<C>& p, bf16_t* to, size_t pitch, int rows, int left) {
   typedef Stage<C> S;
   const int lane = threadIdx.x & 63, c = 8 * (lane % S::PER);
 #pragma unroll
   for (int it = 0; it < 32 / S::ROWS; ++it) {
     const int r = lane / S::PER + S::ROWS * it;
-    if (r >= rows || c >= left) continue;
-    const v4u v = *reinterpret_cast<const v4u*>(stg + r * S::EP + c * 2);
-    bf16_t* const o = to + r * pitch + c;
-    if (whole) { *reinterpret_cast<v4u*>(o) = v; continue; }
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (c + e < left) o[e] = (bf16_t)(v[e >> 1] >> (16 * (e & 1)));
+    if (r < rows && c < left) *reinterpret_cast<v4u*>(to + r * pitch + c) = p.v[it];
   }
 }
-template <class C> __device__ __forceinline__ void rows_in(char* stg, const bf16_t* from, size_t pitch, int rows, int left, bool whole) {
+template <class C> __device__ __forceinline__ StagePart<C> rows_in(const bf16_t* from, size_t pitch, int rows, int left) {
   typedef Stage<C> S;
   const int lane = threadIdx.x & 63, c = 8 * (lane % S::PER);
+  StagePart<C> p;
 #pragma unroll
   for (int it = 0; it < 32 / S::ROWS; ++it) {
     const int r = lane / S::PER + S::ROWS * it;
-    v4u v = {0, 0, 0, 0};
-    if (r < rows && c < left) {
-      const bf16_t* const o = from + r * pitch + c;
-      if (whole) v = *reinterpret_cast<const v4u*>(o);
-      else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (c + e < left) v[e >> 1] |= (uint32_t)o[e] << (16 * (e & 1));
-      }
-    }
-    *reinterpret_cast<v4u*>(stg + r * S::EP + c * 2) = v;
+    p.v[it] = r < rows && c < left ? *reinterpret_cast<const v4u*>(from + r * pitch + c) : v4u{0, 0, 0, 0};
+  }
+  return p;
+}
+// The same for any pitch, value by value: a wave along the rows.
+template <class C> __device__ __forceinline__ void values_out(const char* stg, bf16_t* to, size_t pitch, int rows, int left) {
+  typedef Stage<C> S;
+#pragma unroll 1
+  for (int i = threadIdx.x & 63; i < 32 * S::COLS; i += 64) {
+    const int r = i / S::COLS, c = i % S::COLS;
+    if (r < rows && c < left) to[r * pitch + c] = *reinterpret_cast<const bf16_t*>(stg + r * S::EP + 2 * c);
+  }
+}
+template <class C> __device__ __forceinline__ void values_in(char* stg, const bf16_t* from, size_t pitch, int rows, int left) {
+  typedef Stage<C> S;
+#pragma unroll 4
+  for (int i = threadIdx.x & 63; i < 32 * S::COLS; i += 64) {
+    const int r = i / S::COLS, c = i % S::COLS;
+    *reinterpret_cast<bf16_t*>(stg + r * S::EP + 2 * c) = r < rows && c < left ? from[r * pitch + c] : (bf16_t)0;
   }
 }
 __device__ __forceinline__ void wave_lds_done() {
@@ -77,14 +96,29 @@ __device__ __forceinline__ void wave_lds_done() {
 template <class C>
 __device__ __forceinline__ void add_pair_bias(GemmAcc<C>& acc, const float* __restrict__ bias, int col0, int f) {
   const int lane = threadIdx.x & 63;
+  const bool fours = (f & 3) == 0;
 #pragma unroll
   for (int j = 0; j < C::NB; ++j)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const int n = col0 + 32 * (j >> 1) + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
-      const float b = n < f ? bias[n + (j & 1 ? f : 0)] : 0.f;
+    for (int q = 0; q < 4; ++q) {
+      const int n = col0 + 32 * (j >> 1) + 8 * q + 4 * (lane >> 5);
+      const float* const from = bias + n + (j & 1 ? f : 0);
+      float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (fours) {
+        if (n < f) b = *reinterpret_cast<const float4*>(from);
+      } else {
+        if (n < f) b.x = from[0];
+        if (n + 1 < f) b.y = from[1];
+        if (n + 2 < f) b.z = from[2];
+        if (n + 3 < f) b.w = from[3];
+      }
 #pragma unroll
-      for (int i = 0; i < C::MB; ++i) acc[i][j][v] += b;
+      for (int i = 0; i < C::MB; ++i) {
+        acc[i][j][4 * q] += b.x;
+        acc[i][j][4 * q + 1] += b.y;
+        acc[i][j][4 * q + 2] += b.z;
+        acc[i][j][4 * q + 3] += b.w;
+      }
     }
 }
 
@@ -104,8 +138,8 @@ __device__ __forceinline__ void glu_fwd_tile(const PairArgs& a, int m0, int n0, 
   const bool whole = (a.f & 7) == 0;
 #pragma unroll
   for (int i = 0; i < C::MB; ++i) {
-    const int m = m0 + wm0 + 32 * i;
-    auto out = [&](bf16_t* to, size_t pitch, auto value) {
+    const int m = m0 + wm0 + 32 * i, rows = a.rows - m, left = a.f - col0;
+    auto put = [&](int which, auto value) {
 #pragma unroll
       for (int j = 0; j < C::NB / 2; ++j)
 #pragma unroll
@@ -113,16 +147,32 @@ __device__ __forceinline__ void glu_fwd_tile(const PairArgs& a, int m0, int n0, 
           float v[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = value(acc[i][2 * j][4 * q + e], acc[i][2 * j + 1][4 * q + e]);
-          *reinterpret_cast<uint2*>(mine + 64 * j + 16 * q) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+          *reinterpret_cast<uint2*>(mine + which * S::ONE + 64 * j + 16 * q) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
         }
-      wave_lds_done();
-      rows_out<C>(stg, to + (size_t)m * pitch + col0, pitch, a.rows - m, a.f - col0, whole);
-      wave_lds_done();
     };
-    out(a.h, a.f, [&](float g, float v) { return glu_act(a.act, g) * v; });
-    if (!a.ab) continue;
-    out(a.ab, 2 * (size_t)a.f, [](float g, float) { return g; });
-    out(a.ab + a.f, 2 * (size_t)a.f, [](float, float v) { return v; });
+    put(0, [&](float g, float v) { return glu_act(a.act, g) * v; });
+    if (a.ab) {
+      put(1, [](float g, float) { return g; });
+      put(2, [](float, float v) { return v; });
+    }
+    wave_lds_done();
+    bf16_t *const h = a.h + (size_t)m * a.f + col0, *const ab = a.ab + (size_t)m * 2 * a.f + col0;
+    if (whole) {
+      const StagePart<C> p = staged<C>(stg);
+      if (a.ab) {
+        const StagePart<C> g = staged<C>(stg + S::ONE), v = staged<C>(stg + 2 * S::ONE);
+        rows_out<C>(g, ab, 2 * (size_t)a.f, rows, left);
+        rows_out<C>(v, ab + a.f, 2 * (size_t)a.f, rows, left);
+      }
+      rows_out<C>(p, h, a.f, rows, left);
+    } else {
+      values_out<C>(stg, h, a.f, rows, left);
+      if (a.ab) {
+        values_out<C>(stg + S::ONE, ab, 2 * (size_t)a.f, rows, left);
+        values_out<C>(stg + 2 * S::ONE, ab + a.f, 2 * (size_t)a.f, rows, left);
+      }
+    }
+    wave_lds_done();
   }
 }
 
@@ -150,11 +200,20 @@ __device__ __forceinline__ void glu_dz_tile(const PairArgs& a, int m0, int n0, c
   if (a.bias) add_pair_bias<C>(acc, a.bias, col0, a.f);
   char *const stg = lds + wave * S::BYTES, *const mine = stg + (lane & 31) * S::EP + 8 * (lane >> 5);
   const bool whole = (a.f & 7) == 0;
+  StagePart<C> dh_rows[C::MB];                         // (all of them on their way at once)
+  if (whole)
+#pragma unroll
+    for (int i = 0; i < C::MB; ++i) {
+      const int m = m0 + wm0 + 32 * i;
+      dh_rows[i] = rows_in<C>(a.dh + (size_t)m * a.f + col0, a.f, a.rows - m, a.f - col0);
+    }
 #pragma unroll
   for (int i = 0; i < C::MB; ++i) {
     const int m = m0 + wm0 + 32 * i;
-    rows_in<C>(stg, a.dh + (size_t)m * a.f + col0, a.f, a.rows - m, a.f - col0, whole);
+    if (whole) stage<C>(stg, dh_rows[i]);
+    else values_in<C>(stg, a.dh + (size_t)m * a.f + col0, a.f, a.rows - m, a.f - col0);
     wave_lds_done();
+    const bool there = m + (lane & 31) < a.rows;     // (a row that isn't has the bias for its projections, and a dh of zero)
 #pragma unroll
     for (int j = 0; j < C::NB / 2; ++j)
 #pragma unroll
@@ -165,7 +224,6 @@ __device__ __forceinline__ void glu_dz_tile(const PairArgs& a, int m0, int n0, c
         for (int e = 0; e < 4; ++e) {
           float da, db;
           glu_slopes(a.act, acc[i][2 * j][4 * q + e], acc[i][2 * j + 1][4 * q + e], dh[e], da, db);
-          const bool there = m + (lane & 31) < a.rows;         // (a row that isn't has the bias for its projections, and a dh of zero)
           acc[i][2 * j][4 * q + e] = there ? da : 0.f;
           acc[i][2 * j + 1][4 * q + e] = there ? db : 0.f;
         }
@@ -190,16 +248,16 @@ __device__ __forceinline__ void glu_dz_tile(const PairArgs& a, int m0, int n0, c
   for (int i = 0; i < C::MB; ++i) {
     const int m = m0 + wm0 + 32 * i;
 #pragma unroll
-    for (int part = 0; part < PARTS; ++part)
+    for (int part = 0; part < PARTS; ++part) {
 #pragma unroll
-      for (int side = 0; side < 2; ++side) {
+      for (int side = 0; side < 2; ++side)
 #pragma unroll
         for (int j = 0; j < C::NB / 2; ++j)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             v16f& p = acc[i][2 * j + side];
             const uint2 w = make_uint2(pack_bf16(p[4 * q], p[4 * q + 1]), pack_bf16(p[4 * q + 2], p[4 * q + 3]));
-            *reinterpret_cast<uint2*>(mine + 64 * j + 16 * q) = w;
+            *reinterpret_cast<uint2*>(mine + side * S::ONE + 64 * j + 16 * q) = w;
             if (part + 1 < PARTS) {                    // what is left
               p[4 * q] -= __uint_as_float(w.x << 16);
               p[4 * q + 1] -= __uint_as_float(w.x & 0xffff0000u);
@@ -207,10 +265,13 @@ __device__ __forceinline__ void glu_dz_tile(const PairArgs& a, int m0, int n0, c
               p[4 * q + 3] -= __uint_as_float(w.y & 0xffff0000u);
             }
           }
-        wave_lds_done();
-        rows_out<C>(stg, a.dz[part] + (size_t)m * a.pitch + col0 + (side ? a.half : 0), a.pitch, a.rows - m, a.half - col0, true);
-        wave_lds_done();
-      }
+      wave_lds_done();
+      const StagePart<C> g = staged<C>(stg), v = staged<C>(stg + S::ONE);
+      bf16_t* const to = a.dz[part] + (size_t)m * a.pitch + col0;
+      rows_out<C>(g, to, a.pitch, a.rows - m, a.half - col0);
+      rows_out<C>(v, to + a.half, a.pitch, a.rows - m, a.half - col0);
+      wave_lds_done();
+    }
   }
 }
 
@@ -424,6 +485,8 @@ double pair_us(const PairTile& t, bool backward, long tiles, double steps) {
   return 3.0 + (most / 2) * round(2) + round(most % 2);
 }
 
+constexpr double kSaved = 3.0;
+
 struct GluPlan16 {
   int dp, fp;                  // widths as they are multiplied, multiples of 8
   bool pad_x, pad_w;
@@ -441,7 +504,6 @@ GluPlan16 glu_plan16(int rows, int d, int f, bool backward, bool kept) {
   p.dp = (int)up(d, 8);
   p.fp = (int)up(f, 8);
   p.pad_x = p.dp != d;
-  p.pad_w = p.pad_x || p.fp != f;
   p.parts = rows < 4096 ? 3 : 2;
   const long wide = 2L * p.fp;
   double us = 0;
@@ -450,19 +512,26 @@ GluPlan16 glu_plan16(int rows, int d, int f, bool backward, bool kept) {
     if (us == 0 || v < us) { us = v; p.tile = t; }
   }
   // few tiles of a long sum: parts of it, whose sums a second launch adds up
-  p.proj = choose(RowsByRows, rows, wide, p.dp, 1, 1L << 24, 128, 1);
+  p.proj = choose(RowsByRows, rows, wide, p.dp, 1, 1L << 24, p.dp > 2048 ? up(ceil_div(p.dp, 16), 64) : 128, 1);       // (sixteen parts at most)
   p.cut = !kept && p.proj.splits > 1 && p.proj.us + (backward ? 7.0 : 2.0) < us;
+  // (the pair's tiles take gate and value from where they lie; a product over both, or over their rows, wants each half a multiple of eight)
+  p.pad_w = p.pad_x || (p.fp != f && (backward || p.cut));
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t a = at; at += al256(bytes); return a; };
   p.x = take(p.pad_x ? (size_t)rows * p.dp * 2 : 0);
-  p.w = take(p.pad_w && !(kept && !backward) ? (size_t)wide * p.dp * 2 : 0);
+  p.w = take(p.pad_w ? (size_t)wide * p.dp * 2 : 0);
   p.sums = take(p.cut ? (size_t)p.proj.splits * rows * wide * 4 : 0);
   if (backward) {
     p.dx = choose(ByColumns, rows, d, wide, 1, 1L << 25, 256);
     p.dw = choose(ByColumns, wide, d, rows, p.parts, 1L << 25, 128);
     const Choice dx = choose(ByColumns, rows, d, wide, 1, 1L << 25, 256, 2), dw = choose(ByColumns, wide, d, rows, p.parts, 1L << 25, 128, 2);
     p.together = ceil_div(d, 64) * (ceil_div(rows, 64) * dx.splits + ceil_div(wide, 64) * dw.splits) <= 1024;
-    if (p.together) { p.dx = dx; p.dw = dw; }
+    if (p.together) {
+      p.dx = dx; p.dw = dw;
+      // (whole sums save the launch that adds parts)
+      const Choice x1 = choose(ByColumns, rows, d, wide, 1, 0, 256, 2), w1 = choose(ByColumns, wide, d, rows, p.parts, 0, 128, 2);
+      if (x1.us < dx.us + kSaved && w1.us < dw.us + kSaved) { p.dx = x1; p.dw = w1; }
+    }
     // rows of a part of dw: fewer than 4 GiB of dz and of x
     const long most = (0xF0000000L / (2 * (wide > p.dp ? wide : p.dp))) / 64 * 64;
     if (p.dw.k > most) {
@@ -544,7 +613,7 @@ hipError_t glu_bf16(const GluArgs& a, bool backward) {
   } else {
     PairArgs g{};
     g.x = GemmOperand{x, {}, a.rows, p.dp, p.dp};
-    g.w = GemmOperand{w, {w + (size_t)p.fp * p.dp}, a.f, p.dp, p.dp};
+    g.w = GemmOperand{w, {w + (size_t)(p.pad_w ? p.fp : a.f) * p.dp}, a.f, p.dp, p.dp};
     g.bias = a.bias;
     g.rows = a.rows; g.d = p.dp; g.f = a.f; g.act = a.act;
     g.tiles_m = (int)ceil_div(a.rows, p.tile.m); g.tiles = g.tiles_m * (int)ceil_div(p.fp, p.tile.n / 2);
