@@ -160,7 +160,6 @@ __global__ __launch_bounds__(256) void glu_point_kernel(PointArgs a) {
 
 // ---------------------------------------------------------------------------------- sums of parts
 // Many parts of few values: sixty-four values to a workgroup, a quarter of the parts to each wave
-constexpr int kManyParts = 16;
 template <class T> __device__ __forceinline__ void join_many(const float* __restrict__ sums, T* __restrict__ out, size_t count, int splits, size_t block) {
   __shared__ float sh[256];
   const size_t i = block * 64 + (threadIdx.x & 63);
@@ -174,7 +173,8 @@ template <class T> __device__ __forceinline__ void join_many(const float* __rest
   __syncthreads();
   if (threadIdx.x < 64 && i < count) Elem<T>::store(out + i, ((s + sh[threadIdx.x + 64]) + sh[threadIdx.x + 128]) + sh[threadIdx.x + 192]);
 }
-inline bool many_parts(size_t count, int splits) { return splits >= kManyParts && count <= 1u << 20; }
+// (us, all gradients, so / in slabs of 1024 values: 196 x 512, 8 parts or so 36 / 41, 48 x 456 23 / 28, 777 x 1160 118 / 114, 1000 x 512 51 / 48)
+inline bool many_parts(size_t count, int splits) { return splits >= 16 ? count <= 1u << 20 : splits >= 4 && count <= 1u << 18; }
 template <class T>
 __global__ __launch_bounds__(256) void glu_finish_kernel(GluFinish f, unsigned dx_blocks, unsigned dw_blocks, int many) {
   unsigned block = blockIdx.x;

@@ -25,7 +25,7 @@ COMMON = [dict(x=None), dict(w=None), dict(rows=0), dict(d=0), dict(f=0), dict(r
           dict(d=1 << 15, f=1 << 15), dict(d=1 << 16, f=1 << 16), dict(rows=1 << 24, d=1 << 13), dict(act=3), dict(act=-1), dict(dtype=2), dict(x=at(1) + 8), dict(w=at(2) + 2)]
 
 
-@pytest.mark.parametrize("bad", COMMON + [dict(h=None), dict(h=at(3) + 4), dict(ab=at(5) + 8), dict(rows=3000, d=512, f=33, size=16), dict(d=17, ws=None),
+@pytest.mark.parametrize("bad", COMMON + [dict(h=None), dict(h=at(3) + 4), dict(ab=at(5) + 8), dict(rows=3000, d=513, f=33, size=16), dict(d=17, ws=None),
                                           dict(h=at(1)), dict(h=at(2) + 64), dict(ab=at(3) + 512), dict(ab=at(4), size=4096), dict(bias=at(3) + 16)])
 def test_forward(bad):
     refused(L.acc_op_glu_fwd, FWD, **bad)
