@@ -468,8 +468,8 @@ int acc_op_linear_ce(const void* x, const void* w, const float* bias, const int3
  * Sums and statistics are fp32; [da | db] of bf16 operands is rounded to bf16 for dx, and the sum of two bf16 values (of three for fewer than 4096 rows) for dw.
  * Values that are not finite stay in the results that they enter (an infinity among fp32 operands may make NaN of them).
  * rows <= 2^24, d, f <= 65536, f d (each rounded up to a multiple of 8) below 2^30 - 2^20, rows (d + f) <= 2^36.  workspace: acc_op_glu_workspace() bytes (0
- * forward for up to four rows, and for sizes that are refused); nothing in it needs to be kept or cleared.  What is written may not overlap another argument
- * (ACC_EINVAL).  No atomics: the same bits every time. */
+ * forward for up to four rows, and for sizes that are refused); nothing in it needs to be kept or cleared, and it is not shared by calls that overlap.  What is written may not overlap another
+ * argument (ACC_EINVAL).  No atomics: the same bits every time. */
 size_t acc_op_glu_workspace(int rows, int d, int f, int backward, int dtype);
 int acc_op_glu_fwd(const void* x, const void* w, const float* bias, void* h, void* ab, int rows, int d, int f, int act, void* workspace,
                    size_t workspace_bytes, int dtype, void* stream);
@@ -491,7 +491,8 @@ int acc_op_glu_bwd(const void* x, const void* w, const float* bias, const void* 
  * listed class beyond the last one makes the row's loss NaN and has no term in dz, and so does a label outside [0, classes) where alpha < 1.  Listed logits of minus infinity have probability 0; a
  * row whose listed logits or whose z are all minus infinity, or contain infinity, has NaN in its loss and in dz (at the listed classes resp. at all).  loss_rows [n], loss [1], dz [n][classes] (dtype): each
  * may be NULL, at least one is not; dz may be z, nothing else that is written may overlap another argument (ACC_EINVAL).  n, classes <= 2^20, k <= 1024.
- * workspace: acc_op_distill_workspace() bytes (0: the sizes are refused); nothing in it needs to be kept or cleared.  No atomics: the same bits every time. */
+ * workspace: acc_op_distill_workspace() bytes (0: the sizes are refused); nothing in either workspace needs to be kept or cleared, and none is shared by
+ * calls that overlap.  The same bits every time. */
 size_t acc_op_top_logits_workspace(int n, int classes, int k, int dtype);
 int acc_op_top_logits(const void* z, int32_t* index, float* top, int n, int classes, int k, void* workspace, size_t workspace_bytes, int dtype, void* stream);
 size_t acc_op_distill_workspace(int n, int classes, int k, int dtype);

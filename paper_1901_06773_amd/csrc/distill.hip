@@ -456,16 +456,30 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a) {
   write_listed<T, 256, HARD>(a, dz, r.at(c0), c1 < r.chunks ? r.at(c1) : a.classes, l, t, label, z_label, inv_rows);
 }
 
-// loss = sum of loss_rows / rows that count, in a fixed order
-__global__ __launch_bounds__(1024) void distill_mean_kernel(DistillArgs a) {
+// loss = sum of loss_rows / rows that count, in a fixed order; `parts` sums of parts, or the rows themselves (0)
+__global__ __launch_bounds__(1024) void distill_mean_kernel(DistillArgs a, const double* sums, int parts) {
   __shared__ int sh[16];
   __shared__ double shd[16];
   double s = 0.0;
+  if (parts) {
+    for (int i = threadIdx.x; i < parts; i += 1024) s += sums[i];
+  } else {
 #pragma unroll 4
-  for (int i = threadIdx.x; i < a.n; i += 1024) s += (double)a.loss_rows[i];
+    for (int i = threadIdx.x; i < a.n; i += 1024) s += (double)a.loss_rows[i];
+  }
   const int rows = row_reduce<1024>(count_part<1024>(a), sh, Add());
   s = row_reduce<1024>(s, shd, Add());
   if (threadIdx.x == 0) *a.loss = rows ? (float)(s / (double)rows) : 0.f;
+}
+// sums of the loss of `each` rows
+__global__ __launch_bounds__(256) void distill_sum_kernel(DistillArgs a, double* sums, int each) {
+  __shared__ double sh[4];
+  double s = 0.0;
+  const int first = (int)blockIdx.x * each, end = min(first + each, a.n);
+#pragma unroll 4
+  for (int i = first + (int)threadIdx.x; i < end; i += 256) s += (double)a.loss_rows[i];
+  s = row_reduce<256>(s, sh, Add());
+  if (threadIdx.x == 0) sums[blockIdx.x] = s;
 }
 // rows that count, `each` rows to a workgroup
 __global__ __launch_bounds__(256) void distill_count_kernel(DistillArgs a, int* counts, int each) {
@@ -489,7 +503,8 @@ struct DistillPlan {
   int splits, chunks_per_split;      // 1: a workgroup per row
   int chunks;
   int count_parts, count_each; // rows that count: parts of so many rows (256 at most); 0: every workgroup counts them all
-  size_t rows, counts, part, at_list, total;
+  bool sum_parts;              // the loss by parts of as many rows
+  size_t rows, counts, sums, part, at_list, total;
 };
 DistillPlan distill_plan(int n, int classes, int k, int dtype) {
   DistillPlan p{};
@@ -504,9 +519,11 @@ DistillPlan distill_plan(int n, int classes, int k, int dtype) {
   }
   p.count_each = n > 65536 ? (int)ceil_div(n, 256) : 256;
   p.count_parts = n > 1024 ? (int)ceil_div(n, p.count_each) : 0;
+  p.sum_parts = n > 16384;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t a = at; at += al256(bytes); return a; };
   p.rows = take((size_t)n * 4);
+  p.sums = take(p.sum_parts ? (size_t)p.count_parts * 8 : 0);
   p.counts = take((size_t)p.count_parts * 4);
   p.part = take(p.splits > 1 ? (size_t)n * 4 * p.splits * 4 : 0);
   p.at_list = take(p.splits > 1 ? (size_t)n * (k + 1) * 4 : 0);
@@ -569,7 +586,9 @@ hipError_t distill(const void* z, const int32_t* index, const float* top, const 
   if (dtype == DT_BF16) e = hard ? launch_distill<bf16_t, true>(a, p, st) : launch_distill<bf16_t, false>(a, p, st);
   else e = hard ? launch_distill<float, true>(a, p, st) : launch_distill<float, false>(a, p, st);
   if (e != hipSuccess || !loss || (p.one || (p.waves && n == 1))) return e;
-  hipLaunchKernelGGL(distill_mean_kernel, dim3(1), dim3(1024), 0, st, a);
+  double* const sums = (double*)(ws + p.sums);
+  if (p.sum_parts) hipLaunchKernelGGL(distill_sum_kernel, dim3((unsigned)p.count_parts), dim3(256), 0, st, a, sums, p.count_each);
+  hipLaunchKernelGGL(distill_mean_kernel, dim3(1), dim3(1024), 0, st, a, sums, p.sum_parts ? p.count_parts : 0);
   return hipGetLastError();
 }
 

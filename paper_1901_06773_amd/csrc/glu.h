@@ -66,6 +66,9 @@ struct GluFinish {
   size_t dx_count, dw_count;
   int dx_splits, dw_splits, db_parts, pitch, half, f;
 };
+// Many parts of db are added up in slabs first, into `slabs` (kDbSlabs rows of `pitch`), which then are its parts
+constexpr int kDbSlabs = 64, kDbMany = 512;
+hipError_t glu_db_slabs(GluFinish& f, float* slabs, hipStream_t st);
 // the sums of parts, and db unless another launch has it
 hipError_t glu_finish(const GluFinish& f, bool db, int dtype, hipStream_t st);
 constexpr int kDbColumns = 16;       // columns of db to a workgroup, sixteen threads down each

@@ -187,6 +187,21 @@ __global__ __launch_bounds__(256) void glu_finish_kernel(GluFinish f, unsigned d
   glu_db(f, (int)block);
 }
 
+// sixty-four columns of a slab, every fourth of its rows to a wave
+__global__ __launch_bounds__(256) void glu_db_slabs_kernel(const float* __restrict__ part, float* __restrict__ slabs, int parts, int each, int pitch, int across) {
+  __shared__ double sh[256];
+  const int slab = (int)blockIdx.x / across, j = ((int)blockIdx.x - slab * across) * 64 + (threadIdx.x & 63);
+  const int first = slab * each, end = min(first + each, parts);
+  double s = 0.0;
+  if (j < pitch) {
+#pragma unroll 8
+    for (int r = first + (int)(threadIdx.x >> 6); r < end; r += 4) s += (double)part[(size_t)r * pitch + j];
+  }
+  sh[threadIdx.x] = s;
+  __syncthreads();
+  if (threadIdx.x < 64 && j < pitch) slabs[(size_t)slab * pitch + j] = (float)(((s + sh[threadIdx.x + 64]) + sh[threadIdx.x + 128]) + sh[threadIdx.x + 192]);
+}
+
 // ---------------------------------------------------------------------------------- few rows
 // R rows: a wave's columns one after the other, sixteen bytes of w's rows to a lane, all rows of x against them.
 template <class T, int R>
@@ -342,7 +357,7 @@ struct GluPlan32 {
   bool together;
   Cut proj, dx, dw;
   int db_parts;
-  size_t sums, dz, dx_sums, dw_sums, db, total;
+  size_t sums, dz, dx_sums, dw_sums, db, slabs, total;
 };
 GluPlan32 glu_plan32(int rows, int d, int f, bool backward, bool kept) {
   GluPlan32 p{};
@@ -372,6 +387,7 @@ GluPlan32 glu_plan32(int rows, int d, int f, bool backward, bool kept) {
     q.rows = rows; q.f = f;
     p.db_parts = kept || p.cut ? glu_point_shape(q, DT_F32) : (int)ceil_div(rows, kTile32[p.tile][0]) * (p.tile == 0 ? 1 : 2);
     p.db = take((size_t)p.db_parts * wide * 4);
+    p.slabs = take(p.db_parts > kDbMany ? (size_t)kDbSlabs * wide * 4 : 0);
   }
   p.total = at;
   return p;
@@ -428,6 +444,7 @@ hipError_t glu32(const GluArgs& a, bool backward) {
     if (p.dw.splits > 1) { f.dw_sums = gw.out; f.dw = a.dw; f.dw_count = (size_t)wide * a.d; f.dw_splits = p.dw.splits; }
   }
   if (a.db) { f.db_part = db_part; f.db = a.db; f.db_parts = p.db_parts; f.pitch = wide; f.half = a.f; f.f = a.f; }
+  if (const hipError_t e = glu_db_slabs(f, (float*)(a.ws + p.slabs), st); e != hipSuccess) return e;
   if (p.together) {
     const unsigned bx = whole_eights(gx.work), bw = whole_eights(gw.work);
     hipLaunchKernelGGL(glu_grads32_kernel, dim3(bx + bw + glu_db_blocks(f)), dim3(256), 0, st, gx, gw, f, (int)bx, (int)bw);
@@ -468,6 +485,15 @@ hipError_t glu_point(const PointArgs& a, bool backward, int parts, int dtype, hi
   else if (parts == 2) { if (a.sums) ACC_POINT(bf16_t, true, 2, true); else ACC_POINT(bf16_t, true, 2, false); }
   else { if (a.sums) ACC_POINT(bf16_t, true, 1, true); else ACC_POINT(bf16_t, true, 1, false); }
 #undef ACC_POINT
+  return hipGetLastError();
+}
+
+hipError_t glu_db_slabs(GluFinish& f, float* slabs, hipStream_t st) {
+  if (!f.db || f.db_parts <= kDbMany) return hipSuccess;
+  const int each = (int)ceil_div(f.db_parts, kDbSlabs), across = (int)ceil_div(f.pitch, 64), count = (int)ceil_div(f.db_parts, each);
+  hipLaunchKernelGGL(glu_db_slabs_kernel, dim3((unsigned)(count * across)), dim3(256), 0, st, f.db_part, slabs, f.db_parts, each, f.pitch, across);
+  f.db_part = slabs;
+  f.db_parts = count;
   return hipGetLastError();
 }
 

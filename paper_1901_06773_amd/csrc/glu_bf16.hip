@@ -27,64 +27,63 @@ struct PairArgs {
   int whole;                   // forward: tiles in one piece; those behind them (a last, short round of the compute units) in four
 };
 
-// 32 rows of a wave's columns by way of LDS, so that memory sees whole pieces of rows: EP bytes a staged row.
-template <class C> struct Stage {
-  static constexpr int COLS = 16 * C::NB, EP = COLS * 2 + 16, PER = COLS / 8, ROWS = 64 / PER, ONE = 32 * EP, BYTES = 3 * ONE;      // PER lanes to a row; three results at once
-};
-// What a lane moves of 32 staged rows
-template <class C> struct StagePart { v4u v[32 / Stage<C>::ROWS]; };
-template <class C> __device__ __forceinline__ StagePart<C> staged(const char* stg) {
-  typedef Stage<C> S;
-  const int lane = threadIdx.x & 63;
-  StagePart<C> p;
+// 32 rows of COLS values of a wave by way of LDS, so that memory sees whole pieces of rows: EP bytes a staged row, PER lanes to a row.
+template <int COLS_> struct Stage {
+  static constexpr int COLS = COLS_, EP = COLS * 2 + 16, PER = COLS / 8, ROWS = 64 / PER, ONE = 32 * EP, PARTS = 32 / ROWS;
+  v4u v[PARTS];                                        // what a lane moves of them
+
+  __device__ __forceinline__ void from_lds(const char* stg) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-  for (int it = 0; it < 32 / S::ROWS; ++it) p.v[it] = *reinterpret_cast<const v4u*>(stg + (lane / S::PER + S::ROWS * it) * S::EP + 16 * (lane % S::PER));
-  return p;
-}
-template <class C> __device__ __forceinline__ void stage(char* stg, const StagePart<C>& p) {
-  typedef Stage<C> S;
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int it = 0; it < 32 / S::ROWS; ++it) *reinterpret_cast<v4u*>(stg + (lane / S::PER + S::ROWS * it) * S::EP + 16 * (lane % S::PER)) = p.v[it];
-}
-// To and from rows of `pitch` values, a multiple of eight; columns [0, left) and rows [0, rows) exist.
-template <class C> __device__ __forceinline__ void rows_out(const StagePart<C>& p, bf16_t* to, size_t pitch, int rows, int left) {
-  typedef Stage<C> S;
-  const int lane = threadIdx.x & 63, c = 8 * (lane % S::PER);
-#pragma unroll
-  for (int it = 0; it < 32 / S::ROWS; ++it) {
-    const int r = lane / S::PER + S::ROWS * it;
-    if (r < rows && c < left) *reinterpret_cast<v4u*>(to + r * pitch + c) = p.v[it];
+    for (int it = 0; it < PARTS; ++it) v[it] = *reinterpret_cast<const v4u*>(stg + (lane / PER + ROWS * it) * EP + 16 * (lane % PER));
   }
-}
-template <class C> __device__ __forceinline__ StagePart<C> rows_in(const bf16_t* from, size_t pitch, int rows, int left) {
-  typedef Stage<C> S;
-  const int lane = threadIdx.x & 63, c = 8 * (lane % S::PER);
-  StagePart<C> p;
+  __device__ __forceinline__ void to_lds(char* stg) const {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-  for (int it = 0; it < 32 / S::ROWS; ++it) {
-    const int r = lane / S::PER + S::ROWS * it;
-    p.v[it] = r < rows && c < left ? *reinterpret_cast<const v4u*>(from + r * pitch + c) : v4u{0, 0, 0, 0};
+    for (int it = 0; it < PARTS; ++it) *reinterpret_cast<v4u*>(stg + (lane / PER + ROWS * it) * EP + 16 * (lane % PER)) = v[it];
   }
-  return p;
-}
-// The same for any pitch, value by value: a wave along the rows.
-template <class C> __device__ __forceinline__ void values_out(const char* stg, bf16_t* to, size_t pitch, int rows, int left) {
-  typedef Stage<C> S;
+  // To and from rows of `pitch` values (2^17 at most) at any address that bf16 values may have; columns [0, left) and rows [0, rows) exist.  Eights that are
+  // whole go out here, what is left of a row's last one by ends_out() from LDS.
+  typedef uint32_t any __attribute__((ext_vector_type(4), aligned(2)));
+  __device__ __forceinline__ void out(bf16_t* to, size_t pitch, int rows, int left) const {
+    const int lane = threadIdx.x & 63, c = 8 * (lane % PER);
+#pragma unroll
+    for (int it = 0; it < PARTS; ++it) {
+      const int r = lane / PER + ROWS * it;
+      if (r < rows && c + 8 <= left) *reinterpret_cast<any*>(to + ((uint32_t)r * (uint32_t)pitch + (uint32_t)c)) = any{v[it].x, v[it].y, v[it].z, v[it].w};
+    }
+  }
+  // Rows of eight values or more: the last eight end with the row and are shifted, zeros behind them.  What lies outside is read from the last row and column that exist and
+  // dropped: a branch around a load, with all accumulators alive, made the compiler spill some of them.
+  __device__ __forceinline__ void in(const bf16_t* from, int pitch, int rows, int left) {
+    const int lane = threadIdx.x & 63, c = 8 * (lane % PER), over = c + 8 > left ? c + 8 - left : 0;
+#pragma unroll
+    for (int it = 0; it < PARTS; ++it) {
+      const int r = lane / PER + ROWS * it;
+      const any q = *reinterpret_cast<const any*>(from + (min(r, rows - 1) * pitch + c - over));
+      const bool there = r < rows && over < 8;
+      v[it] = v4u{there ? q.x : 0u, there ? q.y : 0u, there ? q.z : 0u, there ? q.w : 0u};
+    }
+    const bool shifted = ends(left);
+#pragma unroll
+    for (int it = 0; it < PARTS; ++it) {
+      v4u q = v[it];
+      if (shifted && (over & 4)) q = v4u{q.z, q.w, 0, 0};
+      if (shifted && (over & 2)) q = v4u{q.y, q.z, q.w, 0};
+      if (shifted && (over & 1)) q = v4u{q.x >> 16 | q.y << 16, q.y >> 16 | q.z << 16, q.z >> 16 | q.w << 16, q.w >> 16};
+      v[it] = q;
+    }
+  }
+  static __device__ __forceinline__ bool ends(int left) { return left > 0 && left < COLS && (left & 7) != 0; }
+  static __device__ __forceinline__ void ends_out(const char* stg, bf16_t* to, size_t pitch, int rows, int left) {
+    const int first = left & ~7, count = left & 7;
 #pragma unroll 1
-  for (int i = threadIdx.x & 63; i < 32 * S::COLS; i += 64) {
-    const int r = i / S::COLS, c = i % S::COLS;
-    if (r < rows && c < left) to[r * pitch + c] = *reinterpret_cast<const bf16_t*>(stg + r * S::EP + 2 * c);
+    for (int i = threadIdx.x & 63; i < 32 * count; i += 64) {
+      const int r = i / count, c = first + i % count;
+      if (r < rows) to[r * pitch + c] = *reinterpret_cast<const bf16_t*>(stg + r * EP + 2 * c);
+    }
   }
-}
-template <class C> __device__ __forceinline__ void values_in(char* stg, const bf16_t* from, size_t pitch, int rows, int left) {
-  typedef Stage<C> S;
-#pragma unroll 4
-  for (int i = threadIdx.x & 63; i < 32 * S::COLS; i += 64) {
-    const int r = i / S::COLS, c = i % S::COLS;
-    *reinterpret_cast<bf16_t*>(stg + r * S::EP + 2 * c) = r < rows && c < left ? from[r * pitch + c] : (bf16_t)0;
-  }
-}
+};
 __device__ __forceinline__ void wave_lds_done() {
 #if defined(__HIP_DEVICE_COMPILE__)
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -93,49 +92,65 @@ __device__ __forceinline__ void wave_lds_done() {
 #endif
 }
 
-template <class C>
-__device__ __forceinline__ void add_pair_bias(GemmAcc<C>& acc, const float* __restrict__ bias, int col0, int f) {
-  const int lane = threadIdx.x & 63;
-  const bool fours = (f & 3) == 0;
+// The accumulators one by one: as sixteen registers that must lie side by side, some of them were spilled between their uses.
+template <class C> using Values = float[C::MB][C::NB][16];
+template <class C> __device__ __forceinline__ void values_of(const GemmAcc<C>& acc, Values<C>& v) {
 #pragma unroll
-  for (int j = 0; j < C::NB; ++j)
+  for (int i = 0; i < C::MB; ++i)
+#pragma unroll
+    for (int j = 0; j < C::NB; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[i][j][e] = acc[i][j][e];
+}
+// f >= 4.  Read without a branch of their own: the last four end with the row and are shifted, zeros behind them.
+template <class C>
+__device__ __forceinline__ void add_pair_bias(Values<C>& acc, const float* __restrict__ bias, int col0, int f) {
+  typedef float any __attribute__((ext_vector_type(4), aligned(4)));
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int j = 0; j < C::NB; ++j) {
+    any b[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int n = col0 + 32 * (j >> 1) + 8 * q + 4 * (lane >> 5);
-      const float* const from = bias + n + (j & 1 ? f : 0);
-      float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (fours) {
-        if (n < f) b = *reinterpret_cast<const float4*>(from);
-      } else {
-        if (n < f) b.x = from[0];
-        if (n + 1 < f) b.y = from[1];
-        if (n + 2 < f) b.z = from[2];
-        if (n + 3 < f) b.w = from[3];
-      }
-#pragma unroll
-      for (int i = 0; i < C::MB; ++i) {
-        acc[i][j][4 * q] += b.x;
-        acc[i][j][4 * q + 1] += b.y;
-        acc[i][j][4 * q + 2] += b.z;
-        acc[i][j][4 * q + 3] += b.w;
-      }
+      b[q] = *reinterpret_cast<const any*>(bias + min(n, f - 4) + (j & 1 ? f : 0));
     }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int n = col0 + 32 * (j >> 1) + 8 * q + 4 * (lane >> 5), over = n - min(n, f - 4);
+      any v = b[q];
+      if (over & 2) v = any{v.z, v.w, 0.f, 0.f};
+      if (over & 1) v = any{v.y, v.z, v.w, 0.f};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < C::MB; ++i) acc[i][j][4 * q + e] += over < 4 ? v[e] : 0.f;
+    }
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_sched_barrier(0);
+#endif
+  }
 }
 
-// LDS of a tile: its operands, then its staged results
+// LDS of a tile: its operands, then its results, three at once of every wave
 template <class C> struct TileLds {
-  static constexpr int OUT = C::WM * C::WN * Stage<C>::BYTES, value = C::LDS > OUT ? C::LDS : OUT;
+  static constexpr int WAVE = 3 * Stage<16 * C::NB>::ONE, OUT = C::WM * C::WN * WAVE, value = C::LDS > OUT ? C::LDS : OUT;
 };
 // h, and the projections where they are kept, of the tile that begins at row m0 and column n0
 template <class C>
 __device__ __forceinline__ void glu_fwd_tile(const PairArgs& a, int m0, int n0, char* lds) {
-  typedef Stage<C> S;
-  GemmAcc<C> acc;
-  gemm_tile<C>(a.x, a.w, m0, n0, 0, a.d, lds, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm0 = (wave / C::WN) * 32 * C::MB, col0 = n0 + (wave % C::WN) * S::COLS;
+  typedef Stage<16 * C::NB> S;
+  Values<C> acc;
+  m0 = __builtin_amdgcn_readfirstlane(m0);
+  n0 = __builtin_amdgcn_readfirstlane(n0);
+  {
+    GemmAcc<C> sums;
+    gemm_tile<C>(a.x, a.w, m0, n0, 0, a.d, lds, sums);
+    values_of<C>(sums, acc);
+  }
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm0 = (wave / C::WN) * 32 * C::MB, col0 = n0 + (wave % C::WN) * S::COLS;
   if (a.bias) add_pair_bias<C>(acc, a.bias, col0, a.f);
-  char *const stg = lds + wave * S::BYTES, *const mine = stg + (lane & 31) * S::EP + 8 * (lane >> 5);
-  const bool whole = (a.f & 7) == 0;
+  char *const stg = lds + wave * TileLds<C>::WAVE, *const mine = stg + (lane & 31) * S::EP + 8 * (lane >> 5);
 #pragma unroll
   for (int i = 0; i < C::MB; ++i) {
     const int m = m0 + wm0 + 32 * i, rows = a.rows - m, left = a.f - col0;
@@ -157,19 +172,20 @@ __device__ __forceinline__ void glu_fwd_tile(const PairArgs& a, int m0, int n0, 
     }
     wave_lds_done();
     bf16_t *const h = a.h + (size_t)m * a.f + col0, *const ab = a.ab + (size_t)m * 2 * a.f + col0;
-    if (whole) {
-      const StagePart<C> p = staged<C>(stg);
+    S p, g, v;
+    p.from_lds(stg);
+    if (a.ab) {
+      g.from_lds(stg + S::ONE);
+      v.from_lds(stg + 2 * S::ONE);
+      g.out(ab, 2 * (size_t)a.f, rows, left);
+      v.out(ab + a.f, 2 * (size_t)a.f, rows, left);
+    }
+    p.out(h, a.f, rows, left);
+    if (S::ends(left)) {
+      S::ends_out(stg, h, a.f, rows, left);
       if (a.ab) {
-        const StagePart<C> g = staged<C>(stg + S::ONE), v = staged<C>(stg + 2 * S::ONE);
-        rows_out<C>(g, ab, 2 * (size_t)a.f, rows, left);
-        rows_out<C>(v, ab + a.f, 2 * (size_t)a.f, rows, left);
-      }
-      rows_out<C>(p, h, a.f, rows, left);
-    } else {
-      values_out<C>(stg, h, a.f, rows, left);
-      if (a.ab) {
-        values_out<C>(stg + S::ONE, ab, 2 * (size_t)a.f, rows, left);
-        values_out<C>(stg + 2 * S::ONE, ab + a.f, 2 * (size_t)a.f, rows, left);
+        S::ends_out(stg + S::ONE, ab, 2 * (size_t)a.f, rows, left);
+        S::ends_out(stg + 2 * S::ONE, ab + a.f, 2 * (size_t)a.f, rows, left);
       }
     }
     wave_lds_done();
@@ -193,25 +209,30 @@ __device__ __forceinline__ float half_sum(float v) {
 // The projections again, which leave as dz, and the columns' sums of each 32 C::MB rows of a tile
 template <class C, int PARTS>
 __device__ __forceinline__ void glu_dz_tile(const PairArgs& a, int m0, int n0, char* lds) {
-  typedef Stage<C> S;
-  GemmAcc<C> acc;
-  gemm_tile<C>(a.x, a.w, m0, n0, 0, a.d, lds, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm0 = (wave / C::WN) * 32 * C::MB, col0 = n0 + (wave % C::WN) * S::COLS;
+  typedef Stage<16 * C::NB> S;
+  Values<C> acc;
+  m0 = __builtin_amdgcn_readfirstlane(m0);
+  n0 = __builtin_amdgcn_readfirstlane(n0);
+  {
+    GemmAcc<C> sums;
+    gemm_tile<C>(a.x, a.w, m0, n0, 0, a.d, lds, sums);
+    values_of<C>(sums, acc);
+  }
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm0 = (wave / C::WN) * 32 * C::MB, col0 = n0 + (wave % C::WN) * S::COLS;
   if (a.bias) add_pair_bias<C>(acc, a.bias, col0, a.f);
-  char *const stg = lds + wave * S::BYTES, *const mine = stg + (lane & 31) * S::EP + 8 * (lane >> 5);
-  const bool whole = (a.f & 7) == 0;
-  StagePart<C> dh_rows[C::MB];                         // (all of them on their way at once)
-  if (whole)
-#pragma unroll
-    for (int i = 0; i < C::MB; ++i) {
-      const int m = m0 + wm0 + 32 * i;
-      dh_rows[i] = rows_in<C>(a.dh + (size_t)m * a.f + col0, a.f, a.rows - m, a.f - col0);
-    }
+  char *const stg = lds + wave * TileLds<C>::WAVE, *const mine = stg + (lane & 31) * S::EP + 8 * (lane >> 5);
+  auto ask = [&](int i) {
+    const int m = m0 + wm0 + 32 * i;
+    S rows;
+    rows.in(a.dh + (size_t)m * a.f + col0, a.f, a.rows - m, a.f - col0);
+    return rows;
+  };
+  S next = ask(0);                                     // (one block of rows ahead)
 #pragma unroll
   for (int i = 0; i < C::MB; ++i) {
     const int m = m0 + wm0 + 32 * i;
-    if (whole) stage<C>(stg, dh_rows[i]);
-    else values_in<C>(stg, a.dh + (size_t)m * a.f + col0, a.f, a.rows - m, a.f - col0);
+    next.to_lds(stg);
+    if (i + 1 < C::MB) next = ask(i + 1);
     wave_lds_done();
     const bool there = m + (lane & 31) < a.rows;     // (a row that isn't has the bias for its projections, and a dh of zero)
 #pragma unroll
@@ -227,6 +248,9 @@ __device__ __forceinline__ void glu_dz_tile(const PairArgs& a, int m0, int n0, c
           acc[i][2 * j][4 * q + e] = there ? da : 0.f;
           acc[i][2 * j + 1][4 * q + e] = there ? db : 0.f;
         }
+#if defined(__HIP_DEVICE_COMPILE__)
+        __builtin_amdgcn_sched_barrier(0);             // (four values at a time: the registers are full beside the accumulators)
+#endif
       }
     wave_lds_done();
   }
@@ -255,7 +279,7 @@ __device__ __forceinline__ void glu_dz_tile(const PairArgs& a, int m0, int n0, c
         for (int j = 0; j < C::NB / 2; ++j)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            v16f& p = acc[i][2 * j + side];
+            float* const p = acc[i][2 * j + side];
             const uint2 w = make_uint2(pack_bf16(p[4 * q], p[4 * q + 1]), pack_bf16(p[4 * q + 2], p[4 * q + 3]));
             *reinterpret_cast<uint2*>(mine + side * S::ONE + 64 * j + 16 * q) = w;
             if (part + 1 < PARTS) {                    // what is left
@@ -266,10 +290,12 @@ __device__ __forceinline__ void glu_dz_tile(const PairArgs& a, int m0, int n0, c
             }
           }
       wave_lds_done();
-      const StagePart<C> g = staged<C>(stg), v = staged<C>(stg + S::ONE);
+      S g, v;
+      g.from_lds(stg);
+      v.from_lds(stg + S::ONE);
       bf16_t* const to = a.dz[part] + (size_t)m * a.pitch + col0;
-      rows_out<C>(g, to, a.pitch, a.rows - m, a.half - col0);
-      rows_out<C>(v, to + a.half, a.pitch, a.rows - m, a.half - col0);
+      g.out(to, a.pitch, a.rows - m, a.half - col0);                   // (whole eights)
+      v.out(to + a.half, a.pitch, a.rows - m, a.half - col0);
       wave_lds_done();
     }
   }
@@ -321,7 +347,31 @@ __device__ __forceinline__ void glu_product(const ProductArgs& a, int work, char
   const int m0 = where.m * C::BM, n0 = where.n * C::BN;
   GemmAcc<C> acc;
   gemm_tile<C>(a.a, a.b, m0, n0, split * a.k_per_split, min(a.k, (split + 1) * a.k_per_split), lds, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm0 = (wave / C::WN) * 32 * C::MB, wn0 = (wave % C::WN) * 32 * C::NB;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm0 = (wave / C::WN) * 32 * C::MB, wn0 = (wave % C::WN) * 32 * C::NB;
+  if (a.out) {                                         // whole pieces of rows (four values to a lane as they are: 41379 x 1056 from 272 columns 73 us)
+    typedef Stage<32 * C::NB> S;
+    static_assert(C::WM * C::WN * S::ONE <= C::LDS, "the results' rows fit the operands' place");
+    char* const stg = lds + wave * S::ONE;
+    const int n = n0 + wn0, left = a.cols - n;
+#pragma unroll
+    for (int i = 0; i < C::MB; ++i) {
+      const int m = m0 + wm0 + 32 * i;
+#pragma unroll
+      for (int j = 0; j < C::NB; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<uint2*>(stg + (lane & 31) * S::EP + 8 * (lane >> 5) + 64 * j + 16 * q) =
+              make_uint2(pack_bf16(acc[i][j][4 * q], acc[i][j][4 * q + 1]), pack_bf16(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]));
+      wave_lds_done();
+      S rows;
+      rows.from_lds(stg);
+      bf16_t* const to = a.out + (size_t)m * a.cols + n;
+      rows.out(to, a.cols, a.rows - m, left);
+      if (S::ends(left)) S::ends_out(stg, to, a.cols, a.rows - m, left);
+      wave_lds_done();
+    }
+    return;
+  }
   const bool whole = (a.cols & 7) == 0;
 #pragma unroll
   for (int i = 0; i < C::MB; ++i) {
@@ -333,19 +383,11 @@ __device__ __forceinline__ void glu_product(const ProductArgs& a, int work, char
         const int n = n0 + wn0 + 32 * j + 8 * q + 4 * (lane >> 5);
         if (m >= a.rows || n >= a.cols) continue;
         const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-        if (a.out) {
-          bf16_t* const o = a.out + (size_t)m * a.cols + n;
-          if (whole) { *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])); continue; }
+        float* const o = a.sums + (size_t)split * a.rows * a.cols + (size_t)m * a.cols + n;
+        if (whole) { *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]); continue; }
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (n + e < a.cols) Elem<bf16_t>::store(o + e, v[e]);
-        } else {
-          float* const o = a.sums + (size_t)split * a.rows * a.cols + (size_t)m * a.cols + n;
-          if (whole) { *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]); continue; }
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (n + e < a.cols) o[e] = v[e];
-        }
+        for (int e = 0; e < 4; ++e)
+          if (n + e < a.cols) o[e] = v[e];
       }
   }
 }
@@ -377,7 +419,7 @@ __device__ __forceinline__ void glu_dw(const GluDwArgs& a, int work, char* lds) 
   GemmAcc<C> acc;
   gemm_tile<C>(dz, x, m0, n0, 0, count, lds, acc);
   float* const out = a.out + (size_t)split * 2 * a.f * a.d;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm0 = (wave / C::WN) * 32 * C::MB, wn0 = (wave % C::WN) * 32 * C::NB;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm0 = (wave / C::WN) * 32 * C::MB, wn0 = (wave % C::WN) * 32 * C::NB;
 #pragma unroll
   for (int i = 0; i < C::MB; ++i)
 #pragma unroll
@@ -496,7 +538,7 @@ struct GluPlan16 {
   Choice proj, dx, dw;
   bool together;               // dx and dw in one launch of 64 x 64 tiles
   int db_parts;
-  size_t x, w, sums, dz[3], dx_sums, dw_sums, db, total;
+  size_t x, w, sums, dz[3], dx_sums, dw_sums, db, slabs, total;
 };
 
 GluPlan16 glu_plan16(int rows, int d, int f, bool backward, bool kept) {
@@ -513,7 +555,8 @@ GluPlan16 glu_plan16(int rows, int d, int f, bool backward, bool kept) {
   }
   // few tiles of a long sum: parts of it, whose sums a second launch adds up
   p.proj = choose(RowsByRows, rows, wide, p.dp, 1, 1L << 24, p.dp > 2048 ? up(ceil_div(p.dp, 16), 64) : 128, 1);       // (sixteen parts at most)
-  p.cut = !kept && p.proj.splits > 1 && p.proj.us + (backward ? 7.0 : 2.0) < us;
+  // (and rows of fewer than eight values, which the pair's tiles do not read)
+  p.cut = !kept && ((p.proj.splits > 1 && p.proj.us + (backward ? 7.0 : 2.0) < us) || f < 8);
   // (the pair's tiles take gate and value from where they lie; a product over both, or over their rows, wants each half a multiple of eight)
   p.pad_w = p.pad_x || (p.fp != f && (backward || p.cut));
   size_t at = 0;
@@ -524,14 +567,14 @@ GluPlan16 glu_plan16(int rows, int d, int f, bool backward, bool kept) {
   if (backward) {
     p.dx = choose(ByColumns, rows, d, wide, 1, 1L << 25, 256);
     p.dw = choose(ByColumns, wide, d, rows, p.parts, 1L << 25, 128);
-    const Choice dx = choose(ByColumns, rows, d, wide, 1, 1L << 25, 256, 2), dw = choose(ByColumns, wide, d, rows, p.parts, 1L << 25, 128, 2);
-    p.together = ceil_div(d, 64) * (ceil_div(rows, 64) * dx.splits + ceil_div(wide, 64) * dw.splits) <= 1024;
-    if (p.together) {
-      p.dx = dx; p.dw = dw;
-      // (whole sums save the launch that adds parts)
-      const Choice x1 = choose(ByColumns, rows, d, wide, 1, 0, 256, 2), w1 = choose(ByColumns, wide, d, rows, p.parts, 0, 128, 2);
-      if (x1.us < dx.us + kSaved && w1.us < dw.us + kSaved) { p.dx = x1; p.dw = w1; }
-    }
+    const Choice dx = choose(ByColumns, rows, d, wide, 1, 1L << 25, 256, 2), dw = choose(ByColumns, wide, d, rows, p.parts, 1L << 25, 128, 2);      // 64 x 64
+    const long tx = ceil_div(d, 64) * ceil_div(rows, 64), tw = ceil_div(d, 64) * ceil_div(wide, 64);
+    // (whole sums save the launch that adds parts)
+    const Choice x1 = choose(ByColumns, rows, d, wide, 1, 0, 256, 2), w1 = choose(ByColumns, wide, d, rows, p.parts, 0, 128, 2);
+    const bool sums = !(x1.us < dx.us + kSaved && w1.us < dw.us + kSaved);
+    const Choice &cx = sums ? dx : x1, &cw = sums ? dw : w1;
+    p.together = tx * cx.splits + tw * cw.splits <= 1024;
+    if (p.together) { p.dx = cx; p.dw = cw; }
     // rows of a part of dw: fewer than 4 GiB of dz and of x
     const long most = (0xF0000000L / (2 * (wide > p.dp ? wide : p.dp))) / 64 * 64;
     if (p.dw.k > most) {
@@ -545,6 +588,7 @@ GluPlan16 glu_plan16(int rows, int d, int f, bool backward, bool kept) {
     q.rows = rows; q.f = f;
     p.db_parts = kept || p.cut ? glu_point_shape(q, DT_BF16) : (int)ceil_div(rows, p.tile.db_rows);
     p.db = take((size_t)(kept || p.cut ? p.db_parts : up(rows, p.tile.m) / p.tile.db_rows) * wide * 4);
+    p.slabs = take(p.db_parts > kDbMany ? (size_t)kDbSlabs * wide * 4 : 0);
   }
   p.total = at;
   return p;
@@ -648,6 +692,7 @@ hipError_t glu_bf16(const GluArgs& a, bool backward) {
     if (p.dw.splits > 1) { f.dw_sums = gw.out; f.dw = a.dw; f.dw_count = 2 * (size_t)a.f * a.d; f.dw_splits = p.dw.splits; }
   }
   if (a.db) { f.db_part = db_part; f.db = a.db; f.db_parts = p.db_parts; f.pitch = wide; f.half = p.fp; f.f = a.f; }
+  if (const hipError_t e = glu_db_slabs(f, (float*)(a.ws + p.slabs), st); e != hipSuccess) return e;
   if (p.together) {
     const unsigned bx = whole_eights16(gx.work), bw = whole_eights16(gw.work);
     const dim3 grid(bx + bw + glu_db_blocks(f));

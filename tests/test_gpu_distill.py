@@ -96,7 +96,7 @@ def agree(got, ref, dtype):
 
 SIZES = [(1, 1, 1), (3, 2, 2), (1, 5, 3), (41, 1000, 16), (64, 1000, 128), (65, 1000, 129), (7, 1021, 5), (300, 10, 10), (1100, 17, 3), (5000, 33, 4), (64, 2039, 64),
          (3, 1500, 1024), (5, 4099, 7), (30, 8191, 70), (130, 9001, 100), (6, 16385, 65), (33, 50001, 37), (9, 65530, 3), (4, 131060, 64), (2, 131072, 64),
-         (3, 300007, 100), (1, 1 << 20, 1024), (3, 7, 20)]
+         (3, 300007, 100), (1, 1 << 20, 1024), (3, 7, 20), (20001, 9, 3), (1 << 20, 3, 2), (70000, 40, 5)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

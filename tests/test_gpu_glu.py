@@ -113,7 +113,7 @@ def check_backward(x, w, bias, ab, dh, act, dtype):
 SIZES = [(1, 1, 1), (1, 8, 8), (2, 3, 5), (3, 512, 100), (4, 24, 1), (4, 2050, 37), (5, 16, 16), (5, 2, 9), (1, 4096, 33), (9, 4096, 40), (7, 1160, 1003),
          (64, 64, 64), (65, 72, 57), (130, 96, 200), (257, 264, 130), (300, 40, 1000), (1000, 17, 3), (33, 1027, 129), (31, 2048, 16), (512, 512, 512),
          (2009, 100, 65), (4095, 32, 24), (4096, 32, 24), (4100, 64, 40), (5001, 9, 11), (8192, 256, 1024), (3000, 1024, 512), (16400, 64, 520), (20000, 1, 1),
-         (8449, 1024, 1040), (4161, 1536, 2200)]
+         (8449, 1024, 1040), (4161, 1536, 2200), (70001, 8, 41), (50000, 40, 200), (300, 64, 3), (5000, 64, 7), (9000, 16, 9), (12521, 279, 373)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
