@@ -466,7 +466,7 @@ int acc_op_linear_ce(const void* x, const void* w, const float* bias, const int3
  * ab in fwd may be NULL; otherwise the projections are kept there.  ab in bwd: the kept ones (bias is then not looked at; bf16: gradients are those at the rounded values), or NULL:
  * they are worked out again, half as much work more in place of 2 rows f values of memory.  dx, dw, db in bwd: each may be NULL, at least one is not.
  * Sums and statistics are fp32; [da | db] of bf16 operands is rounded to bf16 for dx, and the sum of two bf16 values (of three for fewer than 4096 rows) for dw.
- * Values that are not finite stay in the results that they enter (an infinity among fp32 operands may make NaN of them).
+ * Values that are not finite stay in the results that they enter (an infinity may come out as NaN).
  * rows <= 2^24, d, f <= 65536, f d (each rounded up to a multiple of 8) below 2^30 - 2^20, rows (d + f) <= 2^36.  workspace: acc_op_glu_workspace() bytes (0
  * forward for up to four rows, and for sizes that are refused); nothing in it needs to be kept or cleared, and it is not shared by calls that overlap.  What is written may not overlap another
  * argument (ACC_EINVAL).  No atomics: the same bits every time. */
@@ -485,7 +485,7 @@ int acc_op_glu_bwd(const void* x, const void* w, const float* bias, const void* 
  * negative class (what stands behind it is not read for anything).  With p = softmax(top / T) over the row's list and q = softmax(z / T) over all classes
  *   loss_rows = alpha T^2 sum_j p_j (log p_j - log q_j) + (1 - alpha) (logsumexp(z) - z[label]),  loss = mean over the rows that count,
  *   dz = (alpha T (q - p) + (1 - alpha) (softmax(z) - onehot)) / rows that count.
- * labels [n] int32 may be NULL, with alpha = 1 (the teacher alone); 0 < alpha <= 1, 0 < T < infinity.  With labels the rows whose label is not `ignore` count
+ * labels [n] int32 may be NULL, with alpha = 1 (the teacher alone); 0 < alpha <= 1, 1e-18 <= T <= 1e18.  With labels the rows whose label is not `ignore` count
  * (ACC_LABEL_NONE: all), without them the rows whose list is not empty; others have loss 0 and gradient 0 whatever their z holds.  A row that counts and has no
  * list has the label's term alone.  A class that is listed twice has the sum of its entries' probabilities in dz, and both entries in the loss.  A
  * listed class beyond the last one makes the row's loss NaN and has no term in dz, and so does a label outside [0, classes) where alpha < 1.  Listed logits of minus infinity have probability 0; a

@@ -141,7 +141,7 @@ struct RowSums {
 };
 // d: the list's parts together
 __device__ __forceinline__ float loss_of(const DistillArgs& a, int length, float d, const RowSums& r, int label, float z_label) {
-  float loss = length ? a.soft * (d + log1pf(r.rest)) : 0.f;
+  float loss = length ? a.soft * (d + log1pf(r.rest)) : 0.f * r.rest;      // (no list, and no distribution of z: none of the loss either)
   if (a.hard > 0.f) loss += (unsigned)label < (unsigned)a.classes ? a.hard * (log1pf(r.rest1) - (z_label - r.max)) : NAN;
   return loss;
 }
@@ -566,7 +566,7 @@ size_t distill_workspace_bytes(int n, int classes, int k, int dtype) { return di
 hipError_t distill(const void* z, const int32_t* index, const float* top, const int32_t* labels, int ignore, float temperature, float alpha, float* loss_rows,
                    float* loss, void* dz, int n, int classes, int k, void* workspace, size_t workspace_bytes, int dtype, hipStream_t st) {
   if (!z || !index || !top || !workspace || !(loss_rows || loss || dz) || !distill_ok(n, classes, k, dtype)) return hipErrorInvalidValue;
-  if (!(temperature > 0.f) || temperature == INFINITY || !(alpha > 0.f && alpha <= 1.f) || (!labels && alpha != 1.f)) return hipErrorInvalidValue;
+  if (!(temperature >= 1e-18f && temperature <= 1e18f) || !(alpha > 0.f && alpha <= 1.f) || (!labels && alpha != 1.f)) return hipErrorInvalidValue;
   const DistillPlan p = distill_plan(n, classes, k, dtype);
   if (workspace_bytes < p.total) return hipErrorInvalidValue;
   char* const ws = (char*)workspace;
@@ -585,7 +585,7 @@ hipError_t distill(const void* z, const int32_t* index, const float* top, const 
   hipError_t e;
   if (dtype == DT_BF16) e = hard ? launch_distill<bf16_t, true>(a, p, st) : launch_distill<bf16_t, false>(a, p, st);
   else e = hard ? launch_distill<float, true>(a, p, st) : launch_distill<float, false>(a, p, st);
-  if (e != hipSuccess || !loss || (p.one || (p.waves && n == 1))) return e;
+  if (e != hipSuccess || !loss || p.one) return e;
   double* const sums = (double*)(ws + p.sums);
   if (p.sum_parts) hipLaunchKernelGGL(distill_sum_kernel, dim3((unsigned)p.count_parts), dim3(256), 0, st, a, sums, p.count_each);
   hipLaunchKernelGGL(distill_mean_kernel, dim3(1), dim3(1024), 0, st, a, sums, p.sum_parts ? p.count_parts : 0);

@@ -348,7 +348,7 @@ extern "C" int acc_op_distill(const void* z, const int32_t* index, const float* 
                               void* stream) {
   if (!dtype_ok(dtype)) return refuse("acc_op_distill: dtype must be ACC_F32 or ACC_BF16");
   if (!al16({z, index, top, labels, loss_rows, loss, dz, workspace})) return refuse("acc_op_distill: pointers must be 16-byte aligned");
-  if (!(temperature > 0.f) || std::isinf(temperature)) return refuse("acc_op_distill: the temperature must be positive and finite");
+  if (!(temperature >= 1e-18f && temperature <= 1e18f)) return refuse("acc_op_distill: the temperature must lie in [1e-18, 1e18]");      // (its square is a fp32 number)
   if (!(alpha > 0.f && alpha <= 1.f) || (!labels && alpha != 1.f)) return refuse("acc_op_distill: alpha must lie in (0, 1], and be 1 without labels");
   if (sizes_ok(n, classes, 1) && k > 0) {
     const size_t list = (size_t)n * k * 4, rows = (size_t)n * 4, map = (size_t)n * classes * dt_size(dtype);

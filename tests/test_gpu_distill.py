@@ -267,3 +267,22 @@ def test_replayed_and_on_another_stream():
         torch.cuda.synchronize()
         got = call(z, index, top, lab, 2.0, 0.5, ignore=-9)
         assert torch.equal(got["dz"], dz) and torch.equal(got["rows"], rows) and torch.equal(got["loss"], loss)
+
+
+@pytest.mark.parametrize("classes,k", [(50, 3), (3000, 80), (300001, 5)])
+def test_a_row_of_z_that_is_no_distribution_has_no_loss_even_without_a_list(classes, k):
+    z, index, top, _ = inputs(4, classes, k, "f32")
+    labels = torch.tensor([0, 1, 2, 3], dtype=torch.int32, device="cuda")
+    z[1], index[1], index[2] = -torch.inf, -1, -1
+    for alpha in (1.0, 0.5):
+        out = call(z, index, top, labels, 2.0, alpha)
+        assert out["rows"][1].isnan() and out["dz"][1].isnan().all() and out["loss"].isnan().all()
+        assert out["rows"][[0, 2, 3]].isfinite().all() and out["dz"][[0, 2, 3]].isfinite().all()
+        assert alpha < 1 or (out["rows"][2] == 0 and not out["dz"][2].any())
+
+
+@pytest.mark.parametrize("temperature", [1e-18, 1e18])
+def test_the_smallest_and_the_largest_temperature(temperature):
+    z, index, top, _ = inputs(5, 200, 7, "f32", labels=False)
+    out = call(z, index, top, None, temperature, 1.0)
+    assert out["dz"].isfinite().all()

@@ -47,3 +47,8 @@ def test_refused_sizes_have_no_workspace():
     # rows that fit the registers of one workgroup need none, longer ones a list for each segment
     assert L.acc_op_top_logits_workspace(64, 65000, 64, B.F32) == 0
     assert L.acc_op_top_logits_workspace(64, 200000, 64, B.F32) >= 2 * 64 * 4 * 64 * 4
+
+
+@pytest.mark.parametrize("temperature", [9e-19, 1.1e18, 1e-45, 3e38])
+def test_a_temperature_whose_square_is_no_fp32_number_is_refused(temperature):
+    refused(L.acc_op_distill, DIS, temperature=temperature)
