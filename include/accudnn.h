@@ -468,7 +468,7 @@ int acc_op_linear_ce(const void* x, const void* w, const float* bias, const int3
  * Sums and statistics are fp32; [da | db] of bf16 operands is rounded to bf16 for dx, and the sum of two bf16 values (of three for fewer than 4096 rows) for dw.
  * Values that are not finite stay in the results that they enter (an infinity may come out as NaN).
  * rows <= 2^24, d, f <= 65536, f d (each rounded up to a multiple of 8) below 2^30 - 2^20, rows (d + f) <= 2^36.  workspace: acc_op_glu_workspace() bytes (0
- * forward for up to four rows, and for sizes that are refused); nothing in it needs to be kept or cleared, and it is not shared by calls that overlap.  What is written may not overlap another
+ * forward for up to three rows, and for sizes that are refused); nothing in it needs to be kept or cleared, and it is not shared by calls that overlap.  What is written may not overlap another
  * argument (ACC_EINVAL).  No atomics: the same bits every time. */
 size_t acc_op_glu_workspace(int rows, int d, int f, int backward, int dtype);
 int acc_op_glu_fwd(const void* x, const void* w, const float* bias, void* h, void* ab, int rows, int d, int f, int act, void* workspace,

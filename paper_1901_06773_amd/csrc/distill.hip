@@ -225,16 +225,14 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, int row, float
   const T* const z = static_cast<const T*>(a.z) + (size_t)row * a.classes;
   T* const dz = a.dz ? static_cast<T*>(a.dz) + (size_t)row * a.classes : nullptr;
   const Row r(z, a.classes, (long)(a.n - row) * a.classes);
-  // Short rows are asked for before it is known whether they count: everything is then on its way at once.
-  constexpr bool EAGER = NT <= 256;
   chunk16 q[CH];
+  // (as a lambda: written out behind the return, the compiler keeps the chunks in scratch memory, and 4096 rows of 65536 take 21 ms in place of 0.22)
   auto ask = [&]() {
 #pragma unroll
     for (int u = 0; u < CH; ++u)
       if (tid + u * NT < r.chunks) q[u] = r.load(z, tid + u * NT);
   };
   int rows = dz ? count_part<NT>(a) : 0;
-  if (EAGER) ask();
   if (!row_counts(a, row)) {
     if (tid == 0) a.loss_rows[row] = 0.f;
     if (dz)
@@ -243,7 +241,7 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, int row, float
         if (tid + u * NT < r.chunks) r.store(dz, tid + u * NT, chunk16{0, 0, 0, 0});
     return;
   }
-  if (!EAGER) ask();
+  ask();
   List l = list_in(lists, a.k);
   const int label = HARD ? a.labels[row] : -1;
   float z_label = 0.f;
@@ -330,9 +328,9 @@ __global__ __launch_bounds__(NT, CH == 8 ? 8 : 4) void distill_rows_kernel(Disti
   distill_row<T, NT, CH, HARD>(a, blockIdx.x, lists, sh);
 }
 
-// A wave per row; in one workgroup (with all rows, sixteen at most) the mean, too
+// A wave per row; in one workgroup (with all rows, four at most) the mean, too
 template <class T, int CH, bool HARD>
-__global__ __launch_bounds__(1024) void distill_waves_kernel(DistillArgs a) {
+__global__ __launch_bounds__(256) void distill_waves_kernel(DistillArgs a) {
   extern __shared__ __attribute__((aligned(16))) float lists[];
   const int wave = threadIdx.x >> 6, row = (int)blockIdx.x * (int)(blockDim.x >> 6) + wave;
   if (row < a.n) {
@@ -499,7 +497,7 @@ constexpr int kMostTop = 1024, kMostClasses = 1 << 20, kMostRows = 1 << 20;
 
 struct DistillPlan {
   bool waves;                  // a wave per row, an entry of its list to a lane
-  bool one;                    // sixteen rows at most, in one workgroup, with the mean
+  bool one;                    // four rows at most, in one workgroup, with the mean
   int splits, chunks_per_split;      // 1: a workgroup per row
   int chunks;
   int count_parts, count_each; // rows that count: parts of so many rows (256 at most); 0: every workgroup counts them all
@@ -510,16 +508,18 @@ DistillPlan distill_plan(int n, int classes, int k, int dtype) {
   DistillPlan p{};
   const int per = dtype == DT_BF16 ? 8 : 4;
   p.chunks = (classes + per - 1) / per + (classes % per ? 1 : 0);      // (a row begins inside one where the rows are not whole ones)
-  p.waves = p.chunks <= 64 * 4 && k <= 64;
-  p.one = p.waves && n <= 16;
+  // (us, fp32, a wave per row / a workgroup per row: 41 rows of 500 7.8 / 7.7, of 1000 8.5 / 7.5, 1000 of 250 10.8 / 10.7, of 1000 12.6 / 11.4, 2000 of 1000 12.9 / 14.0,
+  // 4096 of 250 12.1 / 18.0, of 1000 16.6 / 20.1; the mean by the same workgroup / by another launch: 1 of 1000 6.3 / 8.3, 4 of 1000 7.7 / 8.4, 16 of 1000 11.6 / 8.6)
+  p.one = p.chunks <= 64 * 4 && k <= 64 && n <= 4;
+  p.waves = p.one || (p.chunks <= (n > 1536 ? 64 * 4 : 64 * 2) && k <= 64);
   p.splits = 1;
   if (p.chunks > 1024 * 16) {
     p.splits = (int)ceil_div(p.chunks, 4112);          // 64 KiB to a part: 64 parts at most
     p.chunks_per_split = (int)ceil_div(p.chunks, p.splits);
   }
   p.count_each = n > 65536 ? (int)ceil_div(n, 256) : 256;
-  p.count_parts = n > 1024 ? (int)ceil_div(n, p.count_each) : 0;
-  p.sum_parts = n > 16384;
+  p.count_parts = n > 1024 ? (int)ceil_div(n, p.count_each) : 0;      // (with it / without: 1025 rows 9.6 / 10.5, 2048 10.4 / 16.0, 4096 12.0 / 38.9)
+  p.sum_parts = n > 32768;      // (one launch / two, us: 16385 rows 23.0 / 23.8, 65536 66 / 64, 262144 244 / 225)
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t a = at; at += al256(bytes); return a; };
   p.rows = take((size_t)n * 4);
@@ -542,7 +542,7 @@ template <class T, bool HARD> hipError_t launch_distill(const DistillArgs& a, co
     hipLaunchKernelGGL((distill_part_kernel<T, HARD>), grid, dim3(256), 0, st, a);
     hipLaunchKernelGGL((distill_join_kernel<T, HARD>), grid, dim3(256), lists, st, a);
   } else if (p.waves) {
-    const int threads = p.one ? 64 * a.n : a.n <= 2048 ? 64 : 256;
+    const int threads = p.one ? 64 * a.n : 64;
     const dim3 grid(p.one ? 1u : (unsigned)ceil_div(a.n, threads / 64));
 #define ACC_WAVES(CH) hipLaunchKernelGGL((distill_waves_kernel<T, CH, HARD>), grid, dim3(threads), lists * (threads / 64), st, a)
     if (p.chunks <= 64) ACC_WAVES(1);

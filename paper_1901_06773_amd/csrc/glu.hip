@@ -6,7 +6,7 @@
 // 4 rows d f operations forward, 8 backward and 4 more where the projections were not kept: bound by the matrix cores but for few rows, where reading w is.
 // Gate and value are worked out by the same workgroup, so that neither is in memory unless it is to be kept.  The backward pass writes dz (a workspace), as
 // two products read it.  Few tiles: the projections' sums are cut, and launches that work value by value add the parts and do the rest.
-// Up to four rows: every wave takes a few columns and all rows, the layer's weights once through the vector units.
+// Up to three or four rows: every wave takes a few columns and all rows, the layer's weights once through the vector units.
 #include "kernels.h"
 #include "glu.h"
 #include "product32.h"
@@ -203,7 +203,8 @@ __global__ __launch_bounds__(256) void glu_db_slabs_kernel(const float* __restri
 }
 
 // ---------------------------------------------------------------------------------- few rows
-// R rows: a wave's columns one after the other, sixteen bytes of w's rows to a lane, all rows of x against them.
+// R rows: a wave's columns one after the other, sixteen bytes of gate and value rows of w to a lane, all rows of x against them.  (All loads of four steps are on their
+// way at once: with a test of the row's end around each, 4 rows of 2048 to 2 x 8192 took 30 us in place of 16.)
 template <class T, int R>
 __global__ __launch_bounds__(256) void glu_few_kernel(const T* __restrict__ x, const T* __restrict__ w, const float* __restrict__ bias, T* __restrict__ h,
                                                       T* __restrict__ ab, int d, int f, int act) {
@@ -214,21 +215,24 @@ __global__ __launch_bounds__(256) void glu_few_kernel(const T* __restrict__ x, c
     float a[R], b[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) a[r] = b[r] = 0.f;
-#pragma unroll 2
-    for (int k = lane * V; k < d; k += 64 * V) {
-      float va[V], vb[V], vx[V];
-      get<T, V>(wa + k, d - k, va);
-      get<T, V>(wb + k, d - k, vb);
+    auto add = [&](int k, int left) {
+      float va[V], vb[V], vx[R][V];
+      get<T, V>(wa + k, left, va);
+      get<T, V>(wb + k, left, vb);
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        get<T, V>(x + (size_t)r * d + k, d - k, vx);
+      for (int r = 0; r < R; ++r) get<T, V>(x + (size_t)r * d + k, left, vx[r]);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          a[r] = fmaf(va[e], vx[e], a[r]);
-          b[r] = fmaf(vb[e], vx[e], b[r]);
+          a[r] = fmaf(va[e], vx[r][e], a[r]);
+          b[r] = fmaf(vb[e], vx[r][e], b[r]);
         }
-      }
-    }
+    };
+    int k = lane * V;
+#pragma unroll 4
+    for (; k + V <= d; k += 64 * V) add(k, V);
+    if (k < d) add(k, d - k);
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -246,9 +250,12 @@ __global__ __launch_bounds__(256) void glu_few_kernel(const T* __restrict__ x, c
       }
   }
 }
-constexpr int kFewRows = 4;
+// (us, so / by tiles: 1 row of 512 to 2 x 2048 bf16 3.9 / 5.8, fp32 3.8 / 8.4; 4 rows, bf16, 1024 to 2 x 4096 5.6 / 7.5, 2048 to 2 x 8192 16.0 / 12.8; 3 rows of that 13.1 /
+// 12.9; 4 rows of it in fp32 22 / 27; 1 row of 4096 to 2 x 11008 26.7 / 27.9, which is 6.8 TB/s of weights that the caches hold.)
+inline bool few_rows(int rows, int d, int f, int dtype) { return rows <= 3 || (rows == 4 && (dtype == DT_F32 || (long)d * f <= 1L << 23)); }
 template <class T> hipError_t glu_few(const GluArgs& a) {
-  const dim3 grid((unsigned)(ceil_div(a.f, 4) < 4096 ? ceil_div(a.f, 4) : 4096));
+  const long blocks = ceil_div(a.f, 4);
+  const dim3 grid((unsigned)(blocks < 4096 ? blocks : 4096));
 #define ACC_FEW(R) hipLaunchKernelGGL((glu_few_kernel<T, R>), grid, dim3(256), 0, a.st, (const T*)a.x, (const T*)a.w, a.bias, (T*)a.h, (T*)a.ab, a.d, a.f, a.act)
   switch (a.rows) {
     case 1: ACC_FEW(1); break;
@@ -511,7 +518,7 @@ hipError_t glu_finish(const GluFinish& f, bool db, int dtype, hipStream_t st) {
 
 size_t glu_workspace_bytes(int rows, int d, int f, int backward, int dtype) {
   if (!glu_ok(rows, d, f, dtype)) return 0;
-  if (!backward && rows <= kFewRows) return 0;
+  if (!backward && few_rows(rows, d, f, dtype)) return 0;
   if (dtype == DT_BF16) return glu_bf16_workspace_bytes(rows, d, f, backward != 0);
   const size_t again = glu_plan32(rows, d, f, backward != 0, false).total, kept = backward ? glu_plan32(rows, d, f, true, true).total : 0;
   return again > kept ? again : kept;
@@ -524,7 +531,7 @@ hipError_t glu_forward(const void* x, const void* w, const float* bias, void* h,
   if (workspace_bytes < need || (need && !workspace)) return hipErrorInvalidValue;
   GluArgs a{};
   a.x = x; a.w = w; a.bias = bias; a.h = h; a.ab = ab; a.rows = rows; a.d = d; a.f = f; a.act = act; a.ws = (char*)workspace; a.dtype = dtype; a.st = st;
-  if (rows <= kFewRows) return dtype == DT_BF16 ? glu_few<bf16_t>(a) : glu_few<float>(a);
+  if (few_rows(rows, d, f, dtype)) return dtype == DT_BF16 ? glu_few<bf16_t>(a) : glu_few<float>(a);
   return dtype == DT_BF16 ? glu_bf16(a, false) : glu32(a, false);
 }
 

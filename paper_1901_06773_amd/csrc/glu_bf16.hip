@@ -573,7 +573,10 @@ GluPlan16 glu_plan16(int rows, int d, int f, bool backward, bool kept) {
     const Choice x1 = choose(ByColumns, rows, d, wide, 1, 0, 256, 2), w1 = choose(ByColumns, wide, d, rows, p.parts, 0, 128, 2);
     const bool sums = !(x1.us < dx.us + kSaved && w1.us < dw.us + kSaved);
     const Choice &cx = sums ? dx : x1, &cw = sums ? dw : w1;
-    p.together = tx * cx.splits + tw * cw.splits <= 1024;
+    // Up to 1024 workgroups, or 2048 of few steps: 64 x 64 tiles take twice the LDS reads of larger ones.  (us, all gradients of kept projections, so / each for itself:
+    // 196 x 512 x 1024 18.5 / 22.9, 4096 x 512 x 1024 57 / 65, 3867 x 304 x 1936 100 / 112, 10000 x 512 x 1024 140 / 153, 8192 x 512 x 2048 219 / 204)
+    const long workgroups = tx * cx.splits + tw * cw.splits, steps = tx * ceil_div(wide, 64) + tw * ceil_div(rows, 64) * p.parts;
+    p.together = workgroups <= 1024 || (workgroups <= 2048 && steps <= 600 * 256);
     if (p.together) { p.dx = cx; p.dw = cw; }
     // rows of a part of dw: fewer than 4 GiB of dz and of x
     const long most = (0xF0000000L / (2 * (wide > p.dp ? wide : p.dp))) / 64 * 64;

@@ -35,8 +35,8 @@ struct TopArgs {
 };
 
 // Candidates that LDS has room for, at least k; groups that a thread's values are dealt out to, each of which gives its largest one to the bound.
-template <int NT, int CH, int PER> struct TopShape {
-  static constexpr int room = NT == 64 ? 512 : NT < 1024 ? 1024 : CH == 1 ? 4096 : 2048, groups = NT == 1024 && CH == 1 && PER == 8 ? 4 : 1;
+template <int NT, int CH, int G> struct TopShape {
+  static constexpr int room = NT == 64 ? 512 : NT < 1024 ? 1024 : CH == 1 ? 4096 : 2048, groups = G;
 };
 
 // The largest t, of its upper sixteen bits (a bound: the lower half may as well be zero), that `want` of the threads' keys reach.  Every wave looks at all
@@ -66,10 +66,10 @@ template <int NT, int GROUPS> __device__ __forceinline__ uint32_t reached_by(con
   return t;
 }
 
-template <class T, int NT, int CH>
+template <class T, int NT, int CH, int G>
 __global__ __launch_bounds__(NT, CH == 8 ? 8 : 4) void top_kernel(TopArgs a) {
   typedef RowChunks<T> Row;
-  constexpr int PER = Row::PER, ROOM = TopShape<NT, CH, PER>::room, GROUPS = TopShape<NT, CH, PER>::groups, W = NT / 64;
+  constexpr int PER = Row::PER, ROOM = TopShape<NT, CH, G>::room, GROUPS = TopShape<NT, CH, G>::groups, W = NT / 64;
   __shared__ unsigned long long cand[ROOM];
   __shared__ uint32_t keys[NT * GROUPS];
   __shared__ int counter, waves[2][W];
@@ -252,19 +252,19 @@ template <class T> hipError_t launch_top(const TopArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)(a.n * a.segments));
   // The smallest workgroup that holds a row, of which all values fit LDS or the bound leaves out most: with k as many as three quarters of the groups it still
   // leaves out half (10^3 rows of 1306 bf16 logits, k = 118: by a wave, whose 64 threads bound nothing, 108 us).  Sorting more than 128 values is slow in one wave.
-#define ACC_TOP(NT, CH)                                                                                                    \
+#define ACC_TOP(NT, CH, G)                                                                                                   \
   {                                                                                                                        \
-    typedef TopShape<NT, CH, PER> S;                                                                                       \
+    typedef TopShape<NT, CH, G> S;                                                                                         \
     const bool bounded = 4 * a.k <= 3 * S::groups * (chunks < NT ? chunks : NT);                                           \
-    if (chunks <= NT * CH && a.k <= S::room && (bounded || a.segment <= (NT < 1024 ? 2 * NT : S::room) || (NT == 1024 && CH > 1))) { \
-      hipLaunchKernelGGL((top_kernel<T, NT, CH>), grid, dim3(NT), 0, st, a);                                               \
+    if (chunks <= NT * CH && a.k <= S::room && (bounded || a.segment <= (NT < 1024 ? 2 * NT : S::room) || (NT == 1024 && G == 4))) {  \
+      hipLaunchKernelGGL((top_kernel<T, NT, CH, G>), grid, dim3(NT), 0, st, a);                                               \
       return hipGetLastError();                                                                                            \
     }                                                                                                                      \
   }
-  ACC_TOP(64, 1) ACC_TOP(64, 4)
-  ACC_TOP(256, 1) ACC_TOP(256, 4) ACC_TOP(256, 8)
-  ACC_TOP(512, 8)
-  ACC_TOP(1024, 1) ACC_TOP(1024, 8) ACC_TOP(1024, 16)
+  ACC_TOP(64, 1, 1) ACC_TOP(64, 4, 1)
+  ACC_TOP(256, 1, 1) ACC_TOP(256, 4, 1) ACC_TOP(256, 8, 1)
+  ACC_TOP(512, 8, 1)
+  ACC_TOP(1024, 1, 4) ACC_TOP(1024, 8, 1) ACC_TOP(1024, 8, 4) ACC_TOP(1024, 16, 1) ACC_TOP(1024, 16, 4)
 #undef ACC_TOP
   return hipErrorInvalidValue;
 }

@@ -256,3 +256,11 @@ def test_maps_as_they_lie():
     h = torch.empty(n, hw, hw, f, device="cuda", dtype=x.dtype)
     B().op_glu_fwd(x.view(n, hw, hw, d), w, b, h, None, 2, workspace(n * hw * hw, d, f, False, "bf16"))
     assert torch.equal(h.view(-1, f), forward(x, w, b, "silu", "bf16")[0])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,d,f", [(3, 2048, 4104), (4, 2048, 4104), (4, 2050, 4101), (4, 2048, 4096)])
+def test_few_rows_of_a_wide_layer(rows, d, f, dtype):
+    x, w, b, dh = inputs(rows, d, f, dtype)
+    ab = check_forward(x, w, b, "silu", dtype)
+    check_backward(x, w, b, ab, dh, "silu", dtype)

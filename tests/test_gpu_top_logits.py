@@ -120,3 +120,13 @@ def test_replayed_and_on_another_stream():
         torch.cuda.synchronize()
         a, b = call(z, k)
         assert torch.equal(index, a) and torch.equal(top, b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,classes,k", [(3, 20000, 769), (2, 33001, 1000), (3, 60000, 1024)])
+def test_long_lists_of_long_rows(n, classes, k, dtype):
+    z = logits(n, classes, dtype)
+    check(z, k)
+    check(z.round(), k)
+    z[0, 3:classes - k // 2] = -float("inf")            # fewer finite values than entries
+    check(z, k)
