@@ -5,7 +5,10 @@
 // row.  What reaches the bound, some more than k values, is written into LDS with its column as one 64-bit key and sorted there.  Where that is more than fits
 // (many equal values) or there are fewer threads than k, the k-th largest key is found by halving, one bit after the other, with a count of the row each
 // time, and then the column up to which equal ones are taken.  Rows that no workgroup's registers hold, and long ones where there are few, are cut into segments
-// whose lists are rows of a second launch.  Bound by reading the row from memory.
+// whose lists are rows of a second launch.
+//
+// Bound by reading the rows: 4096 bf16 rows of 65536, k = 64, 128 us (4.2 TB/s; two workgroups of a compute unit cover each other's barriers), of fp32 260.  Short rows and
+// long lists by the steps of a row behind each other: 4096 rows of 8192 30 us (2.2 TB/s), k = 150 47; a few rows of any width 6 to 15.
 #include "kernels.h"
 #include "row_chunks.h"
 
@@ -40,7 +43,7 @@ template <int NT, int CH, int G> struct TopShape {
 };
 
 // The largest t, of its upper sixteen bits (a bound: the lower half may as well be zero), that `want` of the threads' keys reach.  Every wave looks at all
-// keys and tries another value of the next bits: log2 of the waves at a time, one barrier each (one wave, bit by bit: 1024 keys 1.6 us, so 0.5).
+// keys and tries another value of the next bits: log2 of the waves at a time, one barrier each (4096 rows of 65536 bf16 128 us; bit by bit 243).
 template <int NT, int GROUPS> __device__ __forceinline__ uint32_t reached_by(const uint32_t* keys, int want, int (*sh)[NT / 64]) {
   constexpr int W = NT / 64, BITS = W >= 16 ? 4 : W >= 8 ? 3 : W >= 4 ? 2 : 1;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -193,12 +196,14 @@ __global__ __launch_bounds__(NT, CH == 8 ? 8 : 4) void top_kernel(TopArgs a) {
   }
   int size = 1;
   while (size < found) size *= 2;
-  // Few: each is compared with all others, by as many threads as there are for it; its rank is its place.  More: sorted, largest first.  (Per row of 65536, 70
-  // found: sorting 128 in 28 steps with a barrier each took 1.3 us, this 0.2.)
-  if (size <= NT && (size / 64) * size <= NT) {
+  // Few: each is compared with all others, by as many threads as there are for it; its rank is its place.  More: sorted, largest first, in steps with a barrier
+  // each.  (us, ranks / sorted: 4096 bf16 rows of 65536, k = 64 (some 70 found) 128 / 156, 64 fp32 rows of 1000 and k = 100 6.5 / 9.9, 4096 bf16 rows of 8192 and k = 150 (some
+  // 200 found, 256 threads) 54 / 47.)
+  if (size <= NT && found * size <= 160 * NT) {
     const int per = NT / size, i = tid / per, part = tid % per;
     const unsigned long long c = i < found ? cand[i] : 0;
     int rank = 0;
+#pragma unroll 8
     for (int j = part; j < found; j += per) rank += cand[j] > c ? 1 : 0;
     for (int o = 1; o < min(per, 64); o <<= 1) rank += __shfl_xor(rank, o);
     if (per > 64) {                                    // (so few that a wave has only one of them)
@@ -251,7 +256,9 @@ template <class T> hipError_t launch_top(const TopArgs& a, hipStream_t st) {
   const int chunks = (a.segment + PER - 1) / PER + (a.classes % PER ? 1 : 0);
   const dim3 grid((unsigned)(a.n * a.segments));
   // The smallest workgroup that holds a row, of which all values fit LDS or the bound leaves out most: with k as many as three quarters of the groups it still
-  // leaves out half (10^3 rows of 1306 bf16 logits, k = 118: by a wave, whose 64 threads bound nothing, 108 us).  Sorting more than 128 values is slow in one wave.
+  // leaves out half.  (us, so / the smallest that holds the row: 1000 rows of 1306 bf16 logits, k = 118, 12.5 / 85, 1000 of 6000 fp32, k = 300, 23 / 217.)  Four groups a thread where
+  // k asks for them: 64 fp32 rows of 50000, k = 1000, 43 / 429.  A chunk a thread or eight, whose registers leave two workgroups of 1024 threads to a compute unit, and sixteen: with
+  // four (4096 bf16 rows of 8192, k = 64, 43 / 31) the compiler takes half as many registers more.
 #define ACC_TOP(NT, CH, G)                                                                                                   \
   {                                                                                                                        \
     typedef TopShape<NT, CH, G> S;                                                                                         \
@@ -262,7 +269,7 @@ template <class T> hipError_t launch_top(const TopArgs& a, hipStream_t st) {
     }                                                                                                                      \
   }
   ACC_TOP(64, 1, 1) ACC_TOP(64, 4, 1)
-  ACC_TOP(256, 1, 1) ACC_TOP(256, 4, 1) ACC_TOP(256, 8, 1)
+  ACC_TOP(256, 1, 1) ACC_TOP(256, 8, 1)
   ACC_TOP(512, 8, 1)
   ACC_TOP(1024, 1, 4) ACC_TOP(1024, 8, 1) ACC_TOP(1024, 8, 4) ACC_TOP(1024, 16, 1) ACC_TOP(1024, 16, 4)
 #undef ACC_TOP
