@@ -5,12 +5,15 @@
 //   loss_i = alpha T^2 sum_j p_j (log p_j - log q_cj) + (1 - alpha) (lse(z) - z_label),   loss = mean over the rows that count
 //   dz = (alpha T (q - p) + (1 - alpha) (s - onehot)) / rows that count
 //
-// A row is read once, into the registers of a wave or a workgroup, and its gradient written from there: memory bounds it.  Rows that no registers hold, and
-// long ones where there are few, are cut: a launch leaves the sums of each part, the next joins them and writes the gradient.  The list's probabilities are worked out
+// A row is read once, into the registers of a wave or a workgroup, and its gradient written from there: memory bounds it.  Rows that no registers hold are
+// cut: a launch leaves the sums of each part, the next joins them and writes the gradient.  The list's probabilities are worked out
 // by the same threads, an entry each, while the row is on its way; the few classes of the list (and the label) are written again, behind a barrier, with their own terms.
 //
 // Sums of exponentials go without the largest one, which is 1: with R the sum of the others', log(1 + R) and, of a class that both give more than a half,
 // q - p = (1 - p) - (1 - q) keep R where a class is all but certain.
+//
+// us: 4096 bf16 rows of 65536, lists of 64, 223 (4.8 TB/s read and written, as a copy; with labels 254: a second exponential for each logit; the loss alone 106), of fp32 455;
+// 777 of 50001 59 (512 workgroups run at a time, so two rounds); 4096 of 8192 40 (3.4 TB/s); 64 rows of 10^6, cut, 92.
 #include "kernels.h"
 #include "row_chunks.h"
 
@@ -513,7 +516,7 @@ DistillPlan distill_plan(int n, int classes, int k, int dtype) {
   p.one = p.chunks <= 64 * 4 && k <= 64 && n <= 4;
   p.waves = p.one || (p.chunks <= (n > 1536 ? 64 * 4 : 64 * 2) && k <= 64);
   p.splits = 1;
-  if (p.chunks > 1024 * 16) {
+  if (p.chunks > 1024 * 16) {                          // (more than a workgroup's registers)
     p.splits = (int)ceil_div(p.chunks, 4112);          // 64 KiB to a part: 64 parts at most
     p.chunks_per_split = (int)ceil_div(p.chunks, p.splits);
   }

@@ -7,6 +7,9 @@
 // Gate and value are worked out by the same workgroup, so that neither is in memory unless it is to be kept.  The backward pass writes dz (a workspace), as
 // two products read it.  Few tiles: the projections' sums are cut, and launches that work value by value add the parts and do the rest.
 // Up to three or four rows: every wave takes a few columns and all rows, the layer's weights once through the vector units.
+//
+// fp32, us: 2009 rows, 2048 to 2 x 1365 (22 GFLOP) forward 144, its two launches' sums 134 (168 TFLOP/s) and h 10; all gradients 313 (143 TFLOP/s).  12544 x 1024 x 4096 1037 (203
+// TFLOP/s) and 2624 (160).  Value by value, bf16, kept projections of 12544 rows of 2 x 4096 and dh, to dz in two values: 122 to 125, 5.8 TB/s.
 #include "kernels.h"
 #include "glu.h"
 #include "product32.h"
@@ -173,7 +176,7 @@ template <class T> __device__ __forceinline__ void join_many(const float* __rest
   __syncthreads();
   if (threadIdx.x < 64 && i < count) Elem<T>::store(out + i, ((s + sh[threadIdx.x + 64]) + sh[threadIdx.x + 128]) + sh[threadIdx.x + 192]);
 }
-// (us, all gradients, so / in slabs of 1024 values: 196 x 512, 8 parts or so 36 / 41, 48 x 456 23 / 28, 777 x 1160 118 / 114, 1000 x 512 51 / 48)
+// (us, all gradients, fp32, so / a value to a thread: 196 x 512 x 1024, some eight parts, 36 / 41, 48 x 456 23 / 28; more values 777 x 1160 118 / 114, 1000 x 512 51 / 48)
 inline bool many_parts(size_t count, int splits) { return splits >= 16 ? count <= 1u << 20 : splits >= 4 && count <= 1u << 18; }
 template <class T>
 __global__ __launch_bounds__(256) void glu_finish_kernel(GluFinish f, unsigned dx_blocks, unsigned dw_blocks, int many) {
@@ -356,7 +359,7 @@ __global__ __launch_bounds__(256) void glu_grads32_kernel(Product32 dx, Product3
   }
 }
 
-constexpr double kSaved = 3.0;         // us
+constexpr double kSaved = 3.0;         // us: a launch that adds parts
 
 struct GluPlan32 {
   int tile;
@@ -372,7 +375,7 @@ GluPlan32 glu_plan32(int rows, int d, int f, bool backward, bool kept) {
   const Cut whole = cut32(rows, wide, d, 0);
   p.tile = whole.tile;
   p.proj = cut32(rows, wide, d, 1L << 24);
-  p.cut = !kept && p.proj.splits > 1 && p.proj.us + 3.0 < whole.us;
+  p.cut = !kept && p.proj.splits > 1 && p.proj.us + 3.0 < whole.us;      // (us, so / whole: forward 64 x 2048 x 512 12 / 51, 300 x 1024 x 64 9.5 / 26.8, 196 x 512 x 1024 14 / 15)
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t a = at; at += al256(bytes); return a; };
   p.sums = take(p.cut ? (size_t)p.proj.splits * rows * wide * 4 : 0);
@@ -380,6 +383,7 @@ GluPlan32 glu_plan32(int rows, int d, int f, bool backward, bool kept) {
     p.dx = cut32(rows, d, wide, 1L << 25);
     p.dw = cut32(wide, d, rows, 1L << 25);
     const Cut dx = cut32(rows, d, wide, 1L << 25, 1), dw = cut32(wide, d, rows, 1L << 25, 1);
+    // (us, so / each for itself: 196 x 512 x 1024 23.8 / 30.0, 2009 x 512 x 512 55 / 65, 777 x 1160 x 1003, which is more, 106 / 82)
     p.together = ceil_div(d, 64) * (ceil_div(rows, 64) * dx.splits + ceil_div(wide, 64) * dw.splits) <= 1024;
     if (p.together) {
       p.dx = dx; p.dw = dw;

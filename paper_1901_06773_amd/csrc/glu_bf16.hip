@@ -5,8 +5,13 @@
 //
 // dz is kept as the sum of bf16 values, the first the nearest one, the next the nearest to what is left (relative errors of 2^-8, 2^-16, 2^-24).  dx, rounded to
 // bf16 itself, is multiplied from the first: the errors of its 2 f terms are independent and add up to one more rounding of the result's size (relative error of dx,
-// one value / two: measured below at the kernel).  dw, an fp32 result, is multiplied from two, of fewer than 4096 rows from three, where two would show beside
-// the roundings of a sum of so few terms in fp32.
+// one value / two: 2.3e-3 / 1.7e-3, in 300 / 480 us at 12544 rows, 1024 wide, 2 x 4096).  dw, an fp32 result, is multiplied from two, of fewer than 4096 rows from three, where two
+// would show beside the roundings of a sum of so few terms in fp32.  Relative error of dw, 1e-7, two / three / all in fp32: 64 rows 24 / 1.1 / 1.5, 1500 24 / 1.7 / 7.0, 4096
+// 24 / 2.6 / 11.5, 16384 24 / 2.8 / 23; dz and dw of 4096 rows, 512 wide, 2 x 1024, 40 / 51 us.
+//
+// All bound by the matrix cores but for the smallest, which are launches behind each other.  12544 rows, 1024 to 2 x 4096 (210 GFLOP a product), us: forward 204 (1030 TFLOP/s; 218 where the
+// projections are kept), dz from the projections worked out again 320 (660: behind each tile's sums the gradients of its 65536 values, which no other workgroup covers), dx 212-225
+// (960: 196 tiles of 256 x 256 on 256 compute units), dw from two values 300-315 (1370 TFLOP/s of both).  A library's product of these sizes alone takes 141 to 175.
 #include "glu.h"
 
 #include "gemm_bf16.h"
@@ -348,7 +353,7 @@ __device__ __forceinline__ void glu_product(const ProductArgs& a, int work, char
   GemmAcc<C> acc;
   gemm_tile<C>(a.a, a.b, m0, n0, split * a.k_per_split, min(a.k, (split + 1) * a.k_per_split), lds, acc);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm0 = (wave / C::WN) * 32 * C::MB, wn0 = (wave % C::WN) * 32 * C::NB;
-  if (a.out) {                                         // whole pieces of rows (four values to a lane as they are: 41379 x 1056 from 272 columns 73 us)
+  if (a.out) {                                         // (whole pieces of rows: all gradients of 41379 x 1056 x 136 take 191 us, with four values of a lane as they are 206)
     typedef Stage<32 * C::NB> S;
     static_assert(C::WM * C::WN * S::ONE <= C::LDS, "the results' rows fit the operands' place");
     char* const stg = lds + wave * S::ONE;
@@ -527,7 +532,7 @@ double pair_us(const PairTile& t, bool backward, long tiles, double steps) {
   return 3.0 + (most / 2) * round(2) + round(most % 2);
 }
 
-constexpr double kSaved = 3.0;
+constexpr double kSaved = 3.0;         // us: a launch that adds parts
 
 struct GluPlan16 {
   int dp, fp;                  // widths as they are multiplied, multiples of 8
@@ -553,7 +558,7 @@ GluPlan16 glu_plan16(int rows, int d, int f, bool backward, bool kept) {
     const double v = pair_us(t, backward, ceil_div(rows, t.m) * ceil_div(p.fp, t.n / 2), p.dp / 64.0);
     if (us == 0 || v < us) { us = v; p.tile = t; }
   }
-  // few tiles of a long sum: parts of it, whose sums a second launch adds up
+  // few tiles of a long sum: parts of it, whose sums a second launch adds up (us, so / whole: forward 64 x 4096 x 1024 13.3 / 18.7, 1000 x 4096 x 64 12.6 / 18.9; backward 43 / 49, 32 / 40)
   p.proj = choose(RowsByRows, rows, wide, p.dp, 1, 1L << 24, p.dp > 2048 ? up(ceil_div(p.dp, 16), 64) : 128, 1);       // (sixteen parts at most)
   // (and rows of fewer than eight values, which the pair's tiles do not read)
   p.cut = !kept && ((p.proj.splits > 1 && p.proj.us + (backward ? 7.0 : 2.0) < us) || f < 8);

@@ -4,7 +4,7 @@
 // A row is read once, into the registers of a workgroup.  The threads' largest values bound the k-th largest of the row from below: k of them are values of the
 // row.  What reaches the bound, some more than k values, is written into LDS with its column as one 64-bit key and sorted there.  Where that is more than fits
 // (many equal values) or there are fewer threads than k, the k-th largest key is found by halving, one bit after the other, with a count of the row each
-// time, and then the column up to which equal ones are taken.  Rows that no workgroup's registers hold, and long ones where there are few, are cut into segments
+// time, and then the column up to which equal ones are taken.  Rows that no workgroup's registers hold are cut into segments
 // whose lists are rows of a second launch.
 //
 // Bound by reading the rows: 4096 bf16 rows of 65536, k = 64, 128 us (4.2 TB/s; two workgroups of a compute unit cover each other's barriers), of fp32 260.  Short rows and
