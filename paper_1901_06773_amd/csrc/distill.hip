@@ -5,8 +5,8 @@
 //   loss_i = alpha T^2 sum_j p_j (log p_j - log q_cj) + (1 - alpha) (lse(z) - z_label),   loss = mean over the rows that count
 //   dz = (alpha T (q - p) + (1 - alpha) (s - onehot)) / rows that count
 //
-// A row is read once, into the registers of a wave or a workgroup, and its gradient written from there: memory bounds it.  Rows that no registers hold are
-// cut: a launch leaves the sums of each part, the next joins them and writes the gradient.  The list's probabilities are worked out
+// A row is read once, into the registers of a wave or a workgroup, and its gradient written from there: memory bounds it.  Rows that no registers hold, and
+// few long ones, are cut: a launch leaves the sums of each part, the next joins them and writes the gradient.  The list's probabilities are worked out
 // by the same threads, an entry each, while the row is on its way; the few classes of the list (and the label) are written again, behind a barrier, with their own terms.
 //
 // Sums of exponentials go without the largest one, which is 1: with R the sum of the others', log(1 + R) and, of a class that both give more than a half,
@@ -516,8 +516,11 @@ DistillPlan distill_plan(int n, int classes, int k, int dtype) {
   p.one = p.chunks <= 64 * 4 && k <= 64 && n <= 4;
   p.waves = p.one || (p.chunks <= (n > 1536 ? 64 * 4 : 64 * 2) && k <= 64);
   p.splits = 1;
-  if (p.chunks > 1024 * 16) {                          // (more than a workgroup's registers)
-    p.splits = (int)ceil_div(p.chunks, 4112);          // 64 KiB to a part: 64 parts at most
+  // more than a workgroup's registers: 64 KiB to a part, 64 parts at most; few long rows: 8 KiB  (us, so / in one piece: 3 bf16 rows of 111759 15 / 33, of 33591 13.0 / 14.7, 32 of 54159
+  // 15.5 / 20.6, 8 fp32 of 10000, which are in one piece, 12.6 / 10.3)
+  const bool few = n <= 32 && p.chunks > 4096;
+  if (p.chunks > 1024 * 16 || few) {
+    p.splits = few && p.chunks < 64 * 512 ? (int)ceil_div(p.chunks, 512) : few ? 64 : (int)ceil_div(p.chunks, 4112);
     p.chunks_per_split = (int)ceil_div(p.chunks, p.splits);
   }
   p.count_each = n > 65536 ? (int)ceil_div(n, 256) : 256;

@@ -52,17 +52,17 @@ struct Gemm32Operand {
 
 template <class C> using Gemm32Acc = f32x4[C::MB][C::NB];
 
-// Values [at, at + 4) of a row of `limit` values, zero beyond it
-__device__ __forceinline__ f32x4 load_end(const float* row, int at, int limit) {
-  if (limit < 4) {
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+// Values [at, at + 4) of a row of `limit` values, zero beyond it: fewer than four, or read (from where four exist) and shifted
+__device__ __forceinline__ f32x4 load_few(const float* row, int at, int limit) {
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < 3; ++e)
-      if (at + e < limit) v[e] = row[at + e];
-    return v;
-  }
-  const int from = at < limit - 4 ? at : limit - 4, by = at - from;
-  f32x4 v = *reinterpret_cast<const f32x4_any*>(row + from);
+  for (int e = 0; e < 3; ++e)
+    if (at + e < limit) v[e] = row[at + e];
+  return v;
+}
+__device__ __forceinline__ f32x4 load_end(const float* row, int at, int limit) { return *reinterpret_cast<const f32x4_any*>(row + min(at, limit - 4)); }
+__device__ __forceinline__ f32x4 shift_end(f32x4 v, int at, int limit) {
+  const int by = at - min(at, limit - 4);
   if (by & 1) v = f32x4{v.y, v.z, v.w, 0.f};
   if (by & 2) v = f32x4{v.z, v.w, 0.f, 0.f};
   return by < 4 ? v : f32x4{0.f, 0.f, 0.f, 0.f};
@@ -94,17 +94,22 @@ template <int EXTENT, bool T, int LOADS, int PITCH, int THREADS> struct Gemm32Lo
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) q[i] = *reinterpret_cast<const f32x4_any*>(base + off[i]);
     } else {
+      const int limit = T ? end : left < 32 ? left : 32;
+      auto row = [&](int u, int i) { return T ? base + (size_t)min(u / (EXTENT / 4), left - 1) * o.pitch : base + off[i] - (u % 8) * 4; };
+      auto at = [](int u) { return (T ? u % (EXTENT / 4) : u % 8) * 4; };
+      if (limit >= 4) {
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int u = threadIdx.x + i * THREADS;
-        if (T) {
-          const int k = u / (EXTENT / 4);
-          const f32x4 v = load_end(base + (size_t)min(k, left - 1) * o.pitch, (u % (EXTENT / 4)) * 4, end);
-          q[i] = k < left ? v : f32x4{0.f, 0.f, 0.f, 0.f};
-        } else {
-          const int c = (u % 8) * 4;
-          q[i] = load_end(base + off[i] - c, c, left < 32 ? left : 32);
-        }
+        for (int i = 0; i < LOADS; ++i) q[i] = load_end(row(threadIdx.x + i * THREADS, i), at(threadIdx.x + i * THREADS), limit);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) q[i] = shift_end(q[i], at(threadIdx.x + i * THREADS), limit);      // (once all are on their way)
+      } else {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) q[i] = load_few(row(threadIdx.x + i * THREADS, i), at(threadIdx.x + i * THREADS), limit);
+      }
+      if (T && left < 32) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+          if ((threadIdx.x + i * THREADS) / (EXTENT / 4) >= left) q[i] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
     }
     base += T ? (size_t)32 * o.pitch : 32;

@@ -286,3 +286,13 @@ def test_the_smallest_and_the_largest_temperature(temperature):
     z, index, top, _ = inputs(5, 200, 7, "f32", labels=False)
     out = call(z, index, top, None, temperature, 1.0)
     assert out["dz"].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,classes,k", [(1, 16389, 3), (3, 33591, 19), (32, 20003, 70), (33, 20003, 70), (2, 131073, 1024), (32, 270000, 5)])
+def test_few_long_rows(n, classes, k, dtype):
+    for labels, alpha in ((False, 1.0), (True, 0.3)):
+        x = inputs(n, classes, k, dtype, labels=labels, ragged=n > 1)
+        out = call(*x, 2.0, alpha)
+        agree(out, reference(*x, 2.0, alpha), dtype)
+        assert torch.equal(call(*x, 2.0, alpha, inplace=True)["dz"], out["dz"])

@@ -130,3 +130,15 @@ def test_long_lists_of_long_rows(n, classes, k, dtype):
     check(z.round(), k)
     z[0, 3:classes - k // 2] = -float("inf")            # fewer finite values than entries
     check(z, k)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,classes,k", [(40, 100, 60), (40, 200, 40), (40, 259, 125), (3000, 259, 125), (3000, 1000, 50), (3, 1000, 200), (5, 2000, 200), (7, 511, 190)])
+def test_rows_bounded_by_groups_of_a_thread(n, classes, k, dtype):
+    z = logits(n, classes, dtype)
+    check(z, k)
+    check((2 * z).round(), k)
+    z[0] = -float("inf")
+    z[1, 1:] = -float("inf")
+    z[2, ::2] = float("nan")
+    check(z, k)
