@@ -58,6 +58,19 @@ template <class T, int V> __device__ __forceinline__ void put(T* p, int left, co
     if (e < left) Elem<T>::store(p + e, v[e]);
 }
 
+// V values from column c on of a row of f, zeros or values of no use behind its end.  The last ones of a row that is no whole number of them are read with their neighbours before
+// them and shifted: one by one, a load waits for the other (22419 rows of kept projections 2 x 1205 to dz in two values 245 us).
+template <class T, int V> __device__ __forceinline__ void get_row(const T* row, int c, int f, float (&v)[V]) {
+  if (f < V) return get<T, V>(row + c, f - c, v);
+  const int over = c - min(c, f - V);
+  get<T, V>(row + (c - over), V, v);
+  if (f % V == 0) return;
+#pragma unroll
+  for (int by = V / 2; by > 0; by /= 2)
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = over & by ? (e + by < V ? v[e + by] : 0.f) : v[e];
+}
+
 // ---------------------------------------------------------------------------------- value by value
 template <class T> struct PointWidth { static constexpr int value = 16 / (int)sizeof(T); };
 
@@ -67,7 +80,7 @@ __global__ __launch_bounds__(256) void glu_point_kernel(PointArgs a) {
   __shared__ float sh[BWD ? 2 * V : 1][256];
   const int tx = threadIdx.x % a.tx, ty = threadIdx.x / a.tx, step = 256 / a.tx;
   const int across = (int)blockIdx.x % a.across, slab = (int)blockIdx.x / a.across;
-  const int c = (across * a.tx + tx) * V, left = a.f - c;
+  const int c = (across * a.tx + tx) * V, left = ty < step ? a.f - c : 0;
   const size_t whole = (size_t)a.rows * 2 * a.half;
   float ba[V], bb[V], sa[V], sb[V];
 #pragma unroll
@@ -80,7 +93,7 @@ __global__ __launch_bounds__(256) void glu_point_kernel(PointArgs a) {
   for (int r = slab * a.slab + ty; r < r1 && left > 0; r += step) {
     float g[V], v[V];
     if constexpr (SUMS) {
-      const float* const from = a.sums + (size_t)r * 2 * a.half + c;
+      const float* const from = a.sums + (size_t)r * 2 * a.half;
 #pragma unroll
       for (int e = 0; e < V; ++e) { g[e] = ba[e]; v[e] = bb[e]; }
       auto add = [&](int s0, auto several) {           // so many parts on their way at once
@@ -90,8 +103,8 @@ __global__ __launch_bounds__(256) void glu_point_kernel(PointArgs a) {
         for (int u = 0; u < U; ++u)
 #pragma unroll
           for (int e = 0; e < V; e += 4) {
-            get<float, 4>(from + (s0 + u) * whole + e, left - e, *reinterpret_cast<float(*)[4]>(&p[u][e]));
-            get<float, 4>(from + (s0 + u) * whole + a.half + e, left - e, *reinterpret_cast<float(*)[4]>(&q[u][e]));
+            get_row<float, 4>(from + (s0 + u) * whole, c + e, a.half, *reinterpret_cast<float(*)[4]>(&p[u][e]));
+            get_row<float, 4>(from + (s0 + u) * whole + a.half, c + e, a.half, *reinterpret_cast<float(*)[4]>(&q[u][e]));
           }
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -102,9 +115,9 @@ __global__ __launch_bounds__(256) void glu_point_kernel(PointArgs a) {
       for (; s + 4 <= a.splits; s += 4) add(s, std::integral_constant<int, 4>());
       for (; s < a.splits; ++s) add(s, std::integral_constant<int, 1>());
     } else {
-      const T* const from = static_cast<const T*>(a.ab_in) + (size_t)r * 2 * a.f + c;
-      get<T, V>(from, left, g);
-      get<T, V>(from + a.f, left, v);
+      const T* const from = static_cast<const T*>(a.ab_in) + (size_t)r * 2 * a.f;
+      get_row<T, V>(from, c, a.f, g);
+      get_row<T, V>(from + a.f, c, a.f, v);
     }
     if constexpr (!BWD) {
       float h[V];
@@ -118,7 +131,7 @@ __global__ __launch_bounds__(256) void glu_point_kernel(PointArgs a) {
       }
     } else {
       float dh[V];
-      get<T, V>(static_cast<const T*>(a.dh) + (size_t)r * a.f + c, left, dh);
+      get_row<T, V>(static_cast<const T*>(a.dh) + (size_t)r * a.f, c, a.f, dh);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         float da, db;
@@ -476,12 +489,20 @@ bool glu_ok(int rows, int d, int f, int dtype) {
 
 int glu_point_shape(PointArgs& a, int dtype) {
   const int v = dtype == DT_BF16 ? 8 : 4, chunks = (a.f + v - 1) / v;
-  a.tx = 1;
-  while (a.tx < chunks && a.tx < 256) a.tx *= 2;
-  a.across = (int)ceil_div(chunks, a.tx);
-  // some two thousand workgroups, at most 512 of them down a column
+  // The fewest workgroups across that leave the fewest threads without work, three more than needed at most.  (us, so / the fewest: 22419 bf16 rows of 2 x 1205 71 / 126, 20000 of
+  // 2 x 1200 56 / 76, of 2 x 2600 125 / 140)
+  const int least = (int)ceil_div(chunks, 256);
+  int most = 0;
+  for (int across = least; across <= least + 3 && across <= chunks; ++across) {
+    const int tx = (int)(across > 1 ? up(ceil_div(chunks, across), 8) : chunks), busy = (int)((long)chunks * (256 / tx) / ceil_div(chunks, tx));      // (of 256 threads; whole lines of 128 bytes)
+    if (busy <= most + most / 16) continue;            // (a sixteenth more, or it is not worth a shorter piece of a row)
+    most = busy;
+    a.tx = tx;
+    a.across = (int)ceil_div(chunks, tx);
+  }
+  // some thousand workgroups, which run at the same time, at most 512 of them down a column (bf16, 11810 rows of 2 x 4624, us: 127, with twice as many 156)
   const int step = 256 / a.tx;
-  long each = ceil_div((long)a.rows * a.across, 2048);
+  long each = ceil_div((long)a.rows * a.across, 1024);
   if (each < ceil_div(a.rows, 512)) each = ceil_div(a.rows, 512);
   a.slab = (int)up(each, step);
   return (int)ceil_div(a.rows, a.slab);

@@ -1,8 +1,9 @@
 """The gated linear layer against its formulas in 64 bits.
 
 Tolerances.  A projection of d <= 4096 products is off by fewer than 2^-24 (2 d^(1/2) + 8) < 8e-6 of the sum of their sizes (roundings at random; the split
-fp32 products leave out 2^-21 at most): 1e-5.  The activation and its slope are known to 2^-20 of themselves and move by at most 1.1 times what the gate moves (the slope by
-half of that).  From there errors are added up as sizes: of h, and of dz = [da | db], which is held to 2^-8 of itself for the dx of bf16 operands, to
+fp32 products leave out 2^-21 at most): 1e-5.  The activation is known to 2^-20 of itself, its slope s (1 + a (1 - s)) to 2^-20 of what its terms add up to in size (they
+cancel where a = -1.2785: s known to 2^-22 and each product and sum rounded by 2^-24 leave 2^-22 s (1 + |a| (1 - s)) at least), and they move by at most 1.1 times what the
+gate moves (the slope by half of that).  From there errors are added up as sizes: of h, and of dz = [da | db], which is held to 2^-8 of itself for the dx of bf16 operands, to
 2^-16 for their dw and to 2^-24 otherwise, through both products, whose own sums are known to 1e-5 of their sizes; results in bf16 are rounded to
 2^-8.  Where a gate lies within its error of 0 the slope of a ReLU is either.  Sums of sizes are far from what errors at random add up to, so whole
 tensors are held, as norms, to 2e-5 as well (dx in bf16: to 2^-7, a rounding of dz and one of its own)."""
@@ -97,7 +98,8 @@ def check_backward(x, w, bias, ab, dh, act, dtype):
     a, b, ea, eb, g = *p.chunk(2, 1), *size.chunk(2, 1), dh.double()
     v, s = curve(a, act)
     dz = torch.cat([g * b * s, g * v], 1)
-    es = torch.where(a.abs() <= ea, 1.0, 0.0) if act == "relu" else 0.5 * ea + 2.0 ** -20 * (s.abs() + 1e-3) + 2.0 ** -20 * (a * s).abs()
+    terms = torch.sigmoid(a) * (1 + a.abs() * (1 - torch.sigmoid(a))) if act == "silu" else s.abs()
+    es = torch.where(a.abs() <= ea, 1.0, 0.0) if act == "relu" else 0.5 * ea + 2.0 ** -20 * terms + 2.0 ** -20 * (a * s).abs()
     err = torch.cat([g.abs() * (eb * (s.abs() + es) + b.abs() * es), g.abs() * (1.1 * ea + 2.0 ** -20 * v.abs())], 1) + 2.0 ** -22 * dz.abs()
     x64, w64 = x.double(), w.double()
     one, more, half = (2.0 ** -8, 2.0 ** -16, 2.0 ** -8) if dtype == "bf16" else (2.0 ** -24, 2.0 ** -24, 2.0 ** -24)
@@ -261,6 +263,14 @@ def test_maps_as_they_lie():
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,d,f", [(3, 2048, 4104), (4, 2048, 4104), (4, 2050, 4101), (4, 2048, 4096)])
 def test_few_rows_of_a_wide_layer(rows, d, f, dtype):
+    x, w, b, dh = inputs(rows, d, f, dtype)
+    ab = check_forward(x, w, b, "silu", dtype)
+    check_backward(x, w, b, ab, dh, "silu", dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,d,f", [(9, 16, 1205), (600, 8, 2609), (70, 24, 4627), (3, 16, 8191), (1030, 8, 302)])
+def test_rows_of_kept_projections_in_several_pieces(rows, d, f, dtype):
     x, w, b, dh = inputs(rows, d, f, dtype)
     ab = check_forward(x, w, b, "silu", dtype)
     check_backward(x, w, b, ab, dh, "silu", dtype)
