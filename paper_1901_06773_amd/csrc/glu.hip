@@ -494,7 +494,8 @@ int glu_point_shape(PointArgs& a, int dtype) {
   const int least = (int)ceil_div(chunks, 256);
   int most = 0;
   for (int across = least; across <= least + 3 && across <= chunks; ++across) {
-    const int tx = (int)(across > 1 ? up(ceil_div(chunks, across), 8) : chunks), busy = (int)((long)chunks * (256 / tx) / ceil_div(chunks, tx));      // (of 256 threads; whole lines of 128 bytes)
+    // (of 256 threads; whole lines of 128 bytes)
+    const int tx = (int)(across > 1 ? up(ceil_div(chunks, across), 8) : chunks), busy = (int)((long)chunks * (256 / tx) / ceil_div(chunks, tx));
     if (busy <= most + most / 16) continue;            // (a sixteenth more, or it is not worth a shorter piece of a row)
     most = busy;
     a.tx = tx;

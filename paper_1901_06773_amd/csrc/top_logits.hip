@@ -258,7 +258,8 @@ template <class T> hipError_t launch_top(const TopArgs& a, hipStream_t st) {
   // The smallest workgroup that holds a row, of which all values fit LDS or the bound leaves out most: with k as many as three quarters of the groups it still
   // leaves out half.  (us, so / the smallest that holds the row: 1000 rows of 1306 bf16 logits, k = 118, 12.5 / 85, 1000 of 6000 fp32, k = 300, 23 / 217.)  Four groups a thread where
   // k asks for them (so / with one group): 64 fp32 rows of 50000, k = 1000, 43 / 429, 5072 of 200, k = 40, by a wave 7.2 / 16, 5072 bf16 of 2000, k = 200, by 256 threads 46 / 271; a wave
-  // with them or 256 threads without: 5072 fp32 rows of 259, k = 125, 15 / 28, 12 bf16 rows of 1000, k = 50, 7.0 / 5.6.  A chunk a thread or eight, whose registers leave two workgroups of 1024 threads to a compute unit, and sixteen: with
+  // with them or 256 threads without: 5072 fp32 rows of 259, k = 125, 15 / 28, 12 bf16 rows of 1000, k = 50, 7.0 / 5.6.  A chunk a thread or eight, whose
+  // registers leave two workgroups of 1024 threads to a compute unit, and sixteen: with
   // four (4096 bf16 rows of 8192, k = 64, 43 / 31) the compiler takes half as many registers more.
 #define ACC_TOP(NT, CH, G, rule)                                                                                 \
   {                                                                                                              \
