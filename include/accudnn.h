@@ -466,7 +466,8 @@ int acc_op_linear_ce(const void* x, const void* w, const float* bias, const int3
  * ab in fwd may be NULL; otherwise the projections are kept there.  ab in bwd: the kept ones (bias is then not looked at; bf16: gradients are those at the rounded values), or NULL:
  * they are worked out again, half as much work more in place of 2 rows f values of memory.  dx, dw, db in bwd: each may be NULL, at least one is not.
  * Sums and statistics are fp32; [da | db] of bf16 operands is rounded to bf16 for dx, and the sum of two bf16 values (of three for fewer than 4096 rows) for dw.
- * Values that are not finite stay in the results that they enter (an infinity may come out as NaN).
+ * Values that are not finite stay in the results that they enter (an infinity may come out as NaN), also through a closed gate, as 0 times them; a gate of minus
+ * infinity is a closed one: act and its slope are 0 there (ACC_ACT_NONE: minus infinity and 1).
  * rows <= 2^24, d, f <= 65536, f d (each rounded up to a multiple of 8) below 2^30 - 2^20, rows (d + f) <= 2^36.  workspace: acc_op_glu_workspace() bytes (0
  * forward for up to three rows, and for sizes that are refused); nothing in it needs to be kept or cleared, and it is not shared by calls that overlap.  What is written may not overlap another
  * argument (ACC_EINVAL).  No atomics: the same bits every time. */

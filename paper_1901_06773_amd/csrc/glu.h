@@ -12,8 +12,10 @@ namespace acc {
 
 enum { GLU_NONE = 0, GLU_RELU = 1, GLU_SILU = 2 };     // as ACC_ACT_*
 
-// act(a) = a s, act'(a) = s (1 + a (1 - s)) with s = 1, s = 1 where a is above 0 and 0 elsewhere (ReLU), or the sigmoid (SiLU): one way for all three.  (A branch for
-// each makes the code of a tile, whose registers are named in it value by value, three times as long.)  Where s is 0 or 1 a product with it is left out, so that an infinity times 0 makes no NaN.  A value that is no number stays none.
+// act(a) = a s, act'(a) = s (1 + a (1 - s)) with s = 1, s = 1 where a is above 0 and 0 elsewhere (ReLU), or the sigmoid (SiLU): one way for all three.  (A
+// branch for each makes the code of a tile, whose registers are named in it value by value, three times as long.)  Where s is 0 act(a) is 0 whatever a is, minus
+// infinity too, and where it is 1 the slope is 1, so that an infinite gate times 0 makes no NaN.  What else is not finite stays: a NaN in a, and through a
+// closed gate, as 0 times it, b and dh.
 __device__ __forceinline__ float glu_share(int act, float a) {
   const float s = sigmoid(a), step = a <= 0.f ? 0.f : 1.f;
   return act == GLU_SILU ? s : act == GLU_RELU ? step : 1.f;
@@ -25,8 +27,9 @@ __device__ __forceinline__ float glu_act(int act, float a) {
 // gradients of h = act(a) b at a and b
 __device__ __forceinline__ void glu_slopes(int act, float a, float b, float dh, float& da, float& db) {
   const float s = glu_share(act, a);
-  da = s == 0.f ? 0.f : dh * b * (s == 1.f ? 1.f : s * (1.f + a * (1.f - s)));
-  db = s == 0.f ? 0.f : dh * (a * s);
+  const bool closed = s == 0.f;
+  da = (closed ? dh * 0.f : dh) * b * (closed || s == 1.f ? 1.f : s * (1.f + a * (1.f - s)));      // (dh b alone might overflow)
+  db = dh * (closed ? 0.f : a * s);
 }
 
 struct GluArgs {
