@@ -12,6 +12,9 @@
 // Sums of exponentials go without the largest one, which is 1: with R the sum of the others', log(1 + R) and, of a class that both give more than a half,
 // q - p = (1 - p) - (1 - q) keep R where a class is all but certain.
 //
+// At high temperatures, where the list holds nearly all that the row has, T^2 sum p (log p - log q) and T (q - p) are what T^2 and T make of the roundings of numbers
+// one.  They are worked out by differences there (Warm).
+//
 // us: 4096 bf16 rows of 65536, lists of 64, 223 (4.8 TB/s read and written, as a copy; with labels 254: a second exponential for each logit; the loss alone 106), of fp32 455;
 // 777 of 50001 59 (512 workgroups run at a time, so two rounds); 4096 of 8192 40 (3.4 TB/s); 64 rows of 10^6, cut, 92.
 #include "kernels.h"
@@ -37,7 +40,7 @@ struct DistillArgs {
   const float* top;
   const int32_t* labels;       // null: the teacher alone
   int ignore;
-  float inv_t, soft, hard, soft_slope;      // 1 / T, alpha T^2, 1 - alpha, alpha T
+  float inv_t, soft, hard, soft_slope, alpha, t2;      // 1 / T, alpha T^2, 1 - alpha, alpha T, alpha, T^2
   float *loss_rows, *loss;
   void* dz;                    // null: the loss alone
   int n, classes, k;
@@ -45,6 +48,7 @@ struct DistillArgs {
   int count_parts;
   // cut rows
   float *part, *at_list;       // part[row][4][splits]: the largest logit and R at both temperatures; at_list[row][k + 1]: logits of the list and of the label
+  unsigned long long* shares;  // shares[row][splits]: sums of shares()
   int splits, chunks_per_split;
 };
 
@@ -142,9 +146,84 @@ template <int NT> __device__ __forceinline__ float list_loss(const DistillArgs& 
 struct RowSums {
   float max, rest, rest1;      // the largest logit; R at the temperature and at 1
 };
+
+// High temperatures.  With x_j = (t_j - t_max) - (z_j - z_max), m = sum p x, y = (x - m) / T, E and P the sums of the row's and the list's exponentials
+//
+//   sum p (log p - log q) = sum p x / T + log(E / P) = log(1 + sum p (e^-y - 1 + y) + U e^(m / T) / P),   q_j / p_j = e^(-y_j - that)
+//
+// (sum p y = 0), U the exponentials of the classes that are not listed.  Nothing in it cancels but U, the difference of E and of the listed ones' sum: both are added up
+// in whole numbers, of the same roundings of the same exponentials, so that a list of all classes leaves exactly 0.  Relative error of the loss of 512 fp32 rows of
+// 100 classes, all listed, so / by the plain formula: T = 4 - / 7e-6, 20 1e-7 / 2e-4, 100 8e-8 / 6e-3, 1000 and more 7e-8 / nothing right.  Up to 4 the plain formula loses less
+// than T^2 2^-24 log 2^20 = 2e-5, and where the two are half a nat apart or more its roundings are little beside the result.
+constexpr float kWarm = 4.f;
+struct Warm {
+  bool near;                   // less than half a nat apart
+  float mean, kl, loss;        // m; the sum above; alpha T^2 times it
+};
+// The exponential of a logit, and in units of 2^-47.  (A row's sum may pass 2^64; the difference of two that is looked at does not.)
+__device__ __forceinline__ float share(float z, float max, float inv_t2) { return exp2_fast((z - max) * inv_t2); }
+__device__ __forceinline__ unsigned long long whole(float share) {
+  const float v = fmaxf(share, 0.f) * 2147483648.f;    // (no number counts as 0)
+  const uint32_t hi = (uint32_t)v, lo = (uint32_t)((v - (float)hi) * 65536.f);
+  return ((unsigned long long)hi << 16) + lo;
+}
+// KL >= log E - (the entropy of p) >= log E - log(entries): less than half a nat asks for as much
+__device__ __forceinline__ bool may_be_near(const RowSums& r, int length) { return 1.f + r.rest < 1.7f * (float)length; }
+// A thread's part of the whole() of chunks [c0, c1), from memory
+template <int NT, class Row, class T> __device__ __forceinline__ unsigned long long wholes(const Row& r, const T* z, int c0, int c1, float max, float inv_t2) {
+  unsigned long long all = 0;
+#pragma unroll 1
+  for (int c = c0 + (int)threadIdx.x % NT; c < c1; c += NT) {
+    chunk16 q = r.load(z, c);
+    r.cut(q, c);
+#pragma unroll
+    for (int e = 0; e < Row::PER; ++e) all += whole(share(Row::value(q, e), max, inv_t2));
+  }
+  return all;
+}
+template <int NT> struct WarmShared {
+  float v[3][NT / 64];
+  unsigned long long n[2][NT / 64];
+};
+// d: the plain formula's sum of the list's parts; all: of the row's whole(); both known to everybody, as the result
+template <int NT> __device__ __forceinline__ Warm warm_of(const DistillArgs& a, const List& l, float d, const RowSums& r, unsigned long long all, WarmShared<NT>& sh) {
+  const float inv_t2 = a.inv_t * LOG2E;
+  float mean = 0.f;
+  unsigned long long listed = 0;
+  for (int j = threadIdx.x % NT; j < l.length; j += NT)
+    if (l.p[j] != 0.f && l.cls[j] < a.classes) {
+      mean += l.p[j] * ((l.t[j] - l.max) - (l.z[j] - r.max));
+      listed += whole(share(l.z[j], r.max, inv_t2));
+    }
+  mean = row_reduce<NT>(mean, sh.v[0], Add());
+  listed = row_reduce<NT>(listed, sh.n[1], Add());
+  const float scale = exp2_fast(mean * inv_t2) * l.inv;
+  float bent = 0.f;            // T^2 sum p (e^-y - 1 + y)
+  for (int j = threadIdx.x % NT; j < l.length; j += NT)
+    if (l.p[j] != 0.f && l.cls[j] < a.classes) {
+      const float x = (l.t[j] - l.max) - (l.z[j] - r.max) - mean, y = x * a.inv_t, p = l.p[j];
+      if (fabsf(y) < 0.5f) {
+        const float series = 0.5f - y * (1.f / 6 - y * (1.f / 24 - y * (1.f / 120 - y * (1.f / 720 - y * (1.f / 5040 - y * (1.f / 40320 - y * (1.f / 362880)))))));
+        bent += p * (x * x) * series;
+      } else if (y > 0.f) {
+        bent += p * a.t2 * (expm1f(-y) + y);
+      } else {                 // (p e^-y is q times e^KL: no overflow)
+        bent += a.t2 * (share(l.z[j], r.max, inv_t2) * scale + p * (y - 1.f));
+      }
+    }
+  bent = row_reduce<NT>(bent, sh.v[1], Add());
+  Warm w;
+  const float rest = (float)(long long)(all - listed) * 0x1p-47f * scale, v = bent * a.inv_t * a.inv_t + rest;
+  w.near = fabsf(d + log1pf(r.rest)) < 0.5f;           // (false for what is no number)
+  w.mean = mean;
+  w.kl = log1pf(v);
+  // (T^2 v, where v itself may be below fp32's smallest value)
+  w.loss = fabsf(v) > 0x1p-12f ? a.soft * w.kl : (a.alpha * bent + a.soft * rest) * (1.f - v * (0.5f - v * (1.f / 3)));
+  return w;
+}
 // d: the list's parts together
-__device__ __forceinline__ float loss_of(const DistillArgs& a, int length, float d, const RowSums& r, int label, float z_label) {
-  float loss = length ? a.soft * (d + log1pf(r.rest)) : 0.f * r.rest;      // (no list, and no distribution of z: none of the loss either)
+__device__ __forceinline__ float loss_of(const DistillArgs& a, int length, float d, const RowSums& r, const Warm& w, int label, float z_label) {
+  float loss = length ? (w.near ? w.loss : a.soft * (d + log1pf(r.rest))) : 0.f * r.rest;      // (no list, and no distribution of z: none of the loss either)
   if (a.hard > 0.f) loss += (unsigned)label < (unsigned)a.classes ? a.hard * (log1pf(r.rest1) - (z_label - r.max)) : NAN;
   return loss;
 }
@@ -164,8 +243,9 @@ __device__ __forceinline__ Slope slope_of(const DistillArgs& a, const RowSums& r
 }
 
 // The gradient of the classes [lo, hi) that are in the list, and of the label, by NT threads: their own terms.
-template <class T, int NT, bool HARD>
-__device__ __forceinline__ void write_listed(const DistillArgs& a, T* dz, int lo, int hi, const List& l, const RowSums& r, int label, float z_label, float inv_rows) {
+template <class T, int NT, bool HARD, bool WARM>
+__device__ __forceinline__ void write_listed(const DistillArgs& a, T* dz, int lo, int hi, const List& l, const RowSums& r, const Warm& w, int label, float z_label,
+                                             float inv_rows) {
   const float inv = 1.f / (1.f + r.rest), inv1 = 1.f / (1.f + r.rest1);
   for (int j = threadIdx.x % NT; j <= l.length; j += NT) {
     const bool entry = j < l.length;
@@ -195,7 +275,10 @@ __device__ __forceinline__ void write_listed(const DistillArgs& a, T* dz, int lo
     if (l.length) {
       const float u = d * a.inv_t, q = exp2_fast(u * LOG2E) * inv;
       float diff = q - sum;
-      if (entry && times == 1 && q > 0.5f && sum > 0.5f)
+      const float apart = WARM && entry ? ((l.t[j] - l.max) - d - w.mean) * a.inv_t + w.kl : 0.f;      // log(p / q)
+      if (WARM && w.near && entry && times == 1 && sum != 0.f && fabsf(apart) < 0.5f)
+        diff = sum * expm1f(-apart);
+      else if (entry && times == 1 && q > 0.5f && sum > 0.5f)
         diff = (l.rest - expm1f((l.t[j] - l.max) * a.inv_t)) * l.inv - (r.rest - expm1f(u)) * inv;
       v = a.soft_slope * diff;
     }
@@ -214,15 +297,40 @@ __device__ __forceinline__ void add_chunk(const chunk16& q, float max, float inv
 #pragma unroll
   for (int e = 0; e < Row::PER; ++e) {
     const float v = Row::value(q, e), d = v - max;
-    const float x = exp2_fast(d * inv_t2), x1 = HARD ? exp2_fast(d * LOG2E) : 0.f;
+    const float x = share(v, max, inv_t2), x1 = HARD ? exp2_fast(d * LOG2E) : 0.f;
     if (careful && v == max) equal += 1.f;
     else { s += x; s1 += x1; }
   }
 }
 
+// What follows the sums of such a row, from memory: beside the registers that hold a row there is no room for it.  (us, 4096 bf16 rows of 65536 with lists of 64, which are none of
+// these, at T = 20, so / from the registers 224 / 298, with labels 293 / 378 and at T = 2 254; 64 fp32 rows of 1000, all listed, at T = 20 54, at 2 50)
+template <class T, int NT, bool HARD>
+__device__ __forceinline__ void near_row(const DistillArgs& a, int row, const RowChunks<T>& r, const T* z, T* dz, const List& l, const RowSums& t, int label, float z_label,
+                                         float inv_rows, WarmShared<NT>& sh) {
+  typedef RowChunks<T> Row;
+  const float inv_t2 = a.inv_t * LOG2E;
+  const float d = row_reduce<NT>(list_loss<NT>(a, l, t.max), sh.v[2], Add());
+  const unsigned long long all = row_reduce<NT>(wholes<NT, Row>(r, z, 0, r.chunks, t.max, inv_t2), sh.n[0], Add());
+  const Warm w = warm_of<NT>(a, l, d, t, all, sh);
+  if (threadIdx.x % NT == 0) a.loss_rows[row] = loss_of(a, l.length, d, t, w, label, z_label);
+  if (!dz) return;
+  const Slope g = slope_of(a, t, l.length, inv_rows);
+#pragma unroll 1
+  for (int c = threadIdx.x % NT; c < r.chunks; c += NT) {
+    const chunk16 q = r.load(z, c);
+    float v[Row::PER];
+#pragma unroll
+    for (int e = 0; e < Row::PER; ++e) v[e] = g.template of<HARD>(Row::value(q, e));
+    r.store(dz, c, Row::pack(v));
+  }
+  row_sync<NT>();
+  write_listed<T, NT, HARD, true>(a, dz, 0, a.classes, l, t, w, label, z_label, inv_rows);
+}
+
 // A row by NT threads, CH chunks each.  lists: 4 list_pitch(k) words of LDS.
-template <class T, int NT, int CH, bool HARD>
-__device__ __forceinline__ void distill_row(const DistillArgs& a, int row, float* lists, RowShared<NT>& sh) {
+template <class T, int NT, int CH, bool HARD, bool WARM>
+__device__ __forceinline__ void distill_row(const DistillArgs& a, int row, float* lists, RowShared<NT>& sh, WarmShared<WARM ? NT : 64>& warm) {
   typedef RowChunks<T> Row;
   const int tid = threadIdx.x % NT;
   const T* const z = static_cast<const T*>(a.z) + (size_t)row * a.classes;
@@ -305,6 +413,9 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, int row, float
   t.rest = none ? NAN : s + (equal - 1.f);
   t.rest1 = none ? NAN : s1 + (equal - 1.f);
   list_known(l, ls, lequal);
+  if constexpr (WARM) {
+    if (may_be_near(t, l.length)) return near_row<T, NT, HARD>(a, row, r, z, dz, l, t, label, z_label, inv_rows, warm);      // (the same for all threads)
+  }
   float d = wave_reduce(list_loss<NT>(a, l, t.max), Add());
   if (NT > 64 && (tid & 63) == 0) sh.v[7][tid >> 6] = d;
   if (dz) {
@@ -320,25 +431,27 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, int row, float
   }
   row_sync<NT>();
   if (NT > 64 && tid < 64) d = join_waves<NT>(sh.v[7], Add());
-  if (tid == 0) a.loss_rows[row] = loss_of(a, l.length, d, t, label, z_label);
-  if (dz) write_listed<T, NT, HARD>(a, dz, 0, a.classes, l, t, label, z_label, inv_rows);
+  if (tid == 0) a.loss_rows[row] = loss_of(a, l.length, d, t, Warm{}, label, z_label);
+  if (dz) write_listed<T, NT, HARD, false>(a, dz, 0, a.classes, l, t, Warm{}, label, z_label, inv_rows);
 }
 
-template <class T, int NT, int CH, bool HARD>
+template <class T, int NT, int CH, bool HARD, bool WARM>
 __global__ __launch_bounds__(NT, CH == 8 ? 8 : 4) void distill_rows_kernel(DistillArgs a) {
   extern __shared__ __attribute__((aligned(16))) float lists[];
   __shared__ RowShared<NT> sh;
-  distill_row<T, NT, CH, HARD>(a, blockIdx.x, lists, sh);
+  __shared__ WarmShared<WARM ? NT : 64> warm;
+  distill_row<T, NT, CH, HARD, WARM>(a, blockIdx.x, lists, sh, warm);
 }
 
 // A wave per row; in one workgroup (with all rows, four at most) the mean, too
-template <class T, int CH, bool HARD>
+template <class T, int CH, bool HARD, bool WARM>
 __global__ __launch_bounds__(256) void distill_waves_kernel(DistillArgs a) {
   extern __shared__ __attribute__((aligned(16))) float lists[];
   const int wave = threadIdx.x >> 6, row = (int)blockIdx.x * (int)(blockDim.x >> 6) + wave;
   if (row < a.n) {
     RowShared<64> sh;                                  // (one wave needs none of it)
-    distill_row<T, 64, CH, HARD>(a, row, lists + (size_t)wave * 4 * list_pitch(a.k), sh);
+    WarmShared<64> warm;
+    distill_row<T, 64, CH, HARD, WARM>(a, row, lists + (size_t)wave * 4 * list_pitch(a.k), sh, warm);
   }
   if (gridDim.x > 1 || !a.loss) return;
   __threadfence_block();
@@ -397,11 +510,48 @@ __global__ __launch_bounds__(256) void distill_part_kernel(DistillArgs a) {
   }
 }
 
+// The parts' sums joined, by every wave
+__device__ __forceinline__ RowSums sums_of_parts(const DistillArgs& a, int row, int lane) {
+  const float* const at = a.part + (size_t)row * 4 * a.splits;
+  const bool mine = lane < a.splits;
+  const float m = mine ? at[lane] : -INFINITY, rest = mine ? at[a.splits + lane] : -1.f, rest1 = mine ? at[2 * a.splits + lane] : -1.f;
+  RowSums t;
+  t.max = wave_reduce(m, Larger());
+  const bool top = mine && m == t.max;
+  float s = top ? rest : (1.f + rest) * exp2_fast((m - t.max) * (a.inv_t * LOG2E)), s1 = top ? rest1 : (1.f + rest1) * exp2_fast((m - t.max) * LOG2E);
+  if (!mine) s = s1 = 0.f;
+  const float equal = wave_reduce(top ? 1.f : 0.f, Add());
+  s = wave_reduce(s, Add());
+  s1 = wave_reduce(s1, Add());
+  const bool none = fabsf(t.max) == INFINITY;
+  t.rest = none ? NAN : s + (equal - 1.f);
+  t.rest1 = none ? NAN : s1 + (equal - 1.f);
+  return t;
+}
+
+// Cut rows at high temperatures: a part's exponentials about the row's largest logit, in whole numbers
+template <class T>
+__global__ __launch_bounds__(256) void distill_shares_kernel(DistillArgs a) {
+  typedef RowChunks<T> Row;
+  __shared__ unsigned long long sh[4];
+  const int row = (int)blockIdx.x / a.splits, sp = (int)blockIdx.x - row * a.splits, tid = threadIdx.x, lane = tid & 63;
+  if (!row_counts(a, row)) return;
+  const RowSums t = sums_of_parts(a, row, lane);
+  if (!may_be_near(t, a.k)) return;                    // (no list is longer)
+  const T* const z = static_cast<const T*>(a.z) + (size_t)row * a.classes;
+  const Row r(z, a.classes, (long)(a.n - row) * a.classes);
+  const int c0 = sp * a.chunks_per_split, c1 = min(c0 + a.chunks_per_split, r.chunks);
+  const float inv_t2 = a.inv_t * LOG2E;
+  const unsigned long long all = row_reduce<256>(wholes<256, Row>(r, z, c0, c1, t.max, inv_t2), sh, Add());
+  if (tid == 0) a.shares[(size_t)row * a.splits + sp] = all;
+}
+
 // Cut rows: the parts joined (64 at most), the loss by the first workgroup, a part of the gradient by each
-template <class T, bool HARD>
+template <class T, bool HARD, bool WARM>
 __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a) {
   typedef RowChunks<T> Row;
   extern __shared__ __attribute__((aligned(16))) float lists[];
+  __shared__ WarmShared<256> warm;
   __shared__ int shc[4], shn[4];
   __shared__ float sh[4][4];
   const int row = (int)blockIdx.x / a.splits, sp = (int)blockIdx.x - row * a.splits, tid = threadIdx.x, lane = tid & 63;
@@ -417,20 +567,8 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a) {
       for (int c = c0 + tid; c < c1; c += 256) r.store(dz, c, chunk16{0, 0, 0, 0});
     return;
   }
-  const float* const at = a.part + (size_t)row * 4 * a.splits;
   const bool mine = lane < a.splits;
-  const float m = mine ? at[lane] : -INFINITY, rest = mine ? at[a.splits + lane] : -1.f, rest1 = mine ? at[2 * a.splits + lane] : -1.f;
-  RowSums t;
-  t.max = wave_reduce(m, Larger());
-  const bool top = mine && m == t.max;
-  float s = top ? rest : (1.f + rest) * exp2_fast((m - t.max) * (a.inv_t * LOG2E)), s1 = top ? rest1 : (1.f + rest1) * exp2_fast((m - t.max) * LOG2E);
-  if (!mine) s = s1 = 0.f;
-  const float equal = wave_reduce(top ? 1.f : 0.f, Add());
-  s = wave_reduce(s, Add());
-  s1 = wave_reduce(s1, Add());
-  const bool none = fabsf(t.max) == INFINITY;
-  t.rest = none ? NAN : s + (equal - 1.f);
-  t.rest1 = none ? NAN : s1 + (equal - 1.f);
+  const RowSums t = sums_of_parts(a, row, lane);
   const float* const kept = a.at_list + (size_t)row * (a.k + 1);
   const int label = HARD ? a.labels[row] : -1;
   const float z_label = HARD ? kept[a.k] : 0.f;
@@ -443,7 +581,11 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a) {
   lequal = row_reduce<256>(lequal, sh[2], Add());
   list_known(l, ls, lequal);
   const float d = row_reduce<256>(list_loss<256>(a, l, t.max), sh[3], Add());
-  if (tid == 0 && sp == 0) a.loss_rows[row] = loss_of(a, l.length, d, t, label, z_label);
+  Warm w{};
+  if constexpr (WARM) {
+    if (may_be_near(t, l.length)) w = warm_of<256>(a, l, d, t, wave_reduce(mine ? a.shares[(size_t)row * a.splits + lane] : 0ull, Add()), warm);
+  }
+  if (tid == 0 && sp == 0) a.loss_rows[row] = loss_of(a, l.length, d, t, w, label, z_label);
   if (!dz) return;
   const Slope g = slope_of(a, t, l.length, inv_rows);
   for (int c = c0 + tid; c < c1; c += 256) {
@@ -454,7 +596,7 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a) {
     r.store(dz, c, Row::pack(v));
   }
   __syncthreads();
-  write_listed<T, 256, HARD>(a, dz, r.at(c0), c1 < r.chunks ? r.at(c1) : a.classes, l, t, label, z_label, inv_rows);
+  write_listed<T, 256, HARD, WARM>(a, dz, r.at(c0), c1 < r.chunks ? r.at(c1) : a.classes, l, t, w, label, z_label, inv_rows);
 }
 
 // loss = sum of loss_rows / rows that count, in a fixed order; `parts` sums of parts, or the rows themselves (0)
@@ -505,7 +647,7 @@ struct DistillPlan {
   int chunks;
   int count_parts, count_each; // rows that count: parts of so many rows (256 at most); 0: every workgroup counts them all
   bool sum_parts;              // the loss by parts of as many rows
-  size_t rows, counts, sums, part, at_list, total;
+  size_t rows, counts, sums, part, at_list, shares, total;
 };
 DistillPlan distill_plan(int n, int classes, int k, int dtype) {
   DistillPlan p{};
@@ -533,6 +675,7 @@ DistillPlan distill_plan(int n, int classes, int k, int dtype) {
   p.counts = take((size_t)p.count_parts * 4);
   p.part = take(p.splits > 1 ? (size_t)n * 4 * p.splits * 4 : 0);
   p.at_list = take(p.splits > 1 ? (size_t)n * (k + 1) * 4 : 0);
+  p.shares = take(p.splits > 1 ? (size_t)n * p.splits * 8 : 0);
   p.total = at;
   return p;
 }
@@ -541,22 +684,23 @@ bool distill_ok(int n, int classes, int k, int dtype) {
          (long)n * distill_plan(n, classes, k, dtype).splits < 1L << 22;       // (a launch has fewer than 2^32 threads)
 }
 
-template <class T, bool HARD> hipError_t launch_distill(const DistillArgs& a, const DistillPlan& p, hipStream_t st) {
+template <class T, bool HARD, bool WARM> hipError_t launch_distill(const DistillArgs& a, const DistillPlan& p, hipStream_t st) {
   const size_t lists = (size_t)4 * list_pitch(a.k) * 4;
   if (p.splits > 1) {
     const dim3 grid((unsigned)(a.n * p.splits));
     hipLaunchKernelGGL((distill_part_kernel<T, HARD>), grid, dim3(256), 0, st, a);
-    hipLaunchKernelGGL((distill_join_kernel<T, HARD>), grid, dim3(256), lists, st, a);
+    if (WARM) hipLaunchKernelGGL(distill_shares_kernel<T>, grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL((distill_join_kernel<T, HARD, WARM>), grid, dim3(256), lists, st, a);
   } else if (p.waves) {
     const int threads = p.one ? 64 * a.n : 64;
     const dim3 grid(p.one ? 1u : (unsigned)ceil_div(a.n, threads / 64));
-#define ACC_WAVES(CH) hipLaunchKernelGGL((distill_waves_kernel<T, CH, HARD>), grid, dim3(threads), lists * (threads / 64), st, a)
+#define ACC_WAVES(CH) hipLaunchKernelGGL((distill_waves_kernel<T, CH, HARD, WARM>), grid, dim3(threads), lists * (threads / 64), st, a)
     if (p.chunks <= 64) ACC_WAVES(1);
     else if (p.chunks <= 128) ACC_WAVES(2);
     else ACC_WAVES(4);
 #undef ACC_WAVES
   } else {
-#define ACC_ROWS(NT, CH) if (p.chunks <= NT * CH) { hipLaunchKernelGGL((distill_rows_kernel<T, NT, CH, HARD>), dim3((unsigned)a.n), dim3(NT), lists, st, a); break; }
+#define ACC_ROWS(NT, CH) if (p.chunks <= NT * CH) { hipLaunchKernelGGL((distill_rows_kernel<T, NT, CH, HARD, WARM>), dim3((unsigned)a.n), dim3(NT), lists, st, a); break; }
     do {
       ACC_ROWS(256, 2) ACC_ROWS(256, 4) ACC_ROWS(256, 8) ACC_ROWS(512, 8) ACC_ROWS(1024, 8) ACC_ROWS(1024, 16)
     } while (false);
@@ -579,18 +723,23 @@ hipError_t distill(const void* z, const int32_t* index, const float* top, const 
   DistillArgs a{};
   a.z = z; a.index = index; a.top = top; a.labels = labels; a.ignore = ignore;
   a.inv_t = 1.f / temperature; a.soft = alpha * temperature * temperature; a.hard = 1.f - alpha; a.soft_slope = alpha * temperature;
+  a.alpha = alpha; a.t2 = temperature * temperature;
   a.loss_rows = loss_rows ? loss_rows : (float*)(ws + p.rows);
   a.loss = loss; a.dz = dz; a.n = n; a.classes = classes; a.k = k;
-  a.part = (float*)(ws + p.part); a.at_list = (float*)(ws + p.at_list); a.splits = p.splits; a.chunks_per_split = p.chunks_per_split;
+  a.part = (float*)(ws + p.part); a.at_list = (float*)(ws + p.at_list); a.shares = (unsigned long long*)(ws + p.shares); a.splits = p.splits; a.chunks_per_split = p.chunks_per_split;
   if (p.count_parts && (dz || loss)) {
     int* const counts = (int*)(ws + p.counts);
     hipLaunchKernelGGL(distill_count_kernel, dim3((unsigned)p.count_parts), dim3(256), 0, st, a, counts, p.count_each);
     a.counts = counts; a.count_parts = p.count_parts;
   }
-  const bool hard = alpha < 1.f;
+  const bool hard = alpha < 1.f, warm = temperature > kWarm;
   hipError_t e;
-  if (dtype == DT_BF16) e = hard ? launch_distill<bf16_t, true>(a, p, st) : launch_distill<bf16_t, false>(a, p, st);
-  else e = hard ? launch_distill<float, true>(a, p, st) : launch_distill<float, false>(a, p, st);
+#define ACC_DISTILL(T) \
+  e = hard ? warm ? launch_distill<T, true, true>(a, p, st) : launch_distill<T, true, false>(a, p, st) \
+           : warm ? launch_distill<T, false, true>(a, p, st) : launch_distill<T, false, false>(a, p, st)
+  if (dtype == DT_BF16) ACC_DISTILL(bf16_t);
+  else ACC_DISTILL(float);
+#undef ACC_DISTILL
   if (e != hipSuccess || !loss || p.one) return e;
   double* const sums = (double*)(ws + p.sums);
   if (p.sum_parts) hipLaunchKernelGGL(distill_sum_kernel, dim3((unsigned)p.count_parts), dim3(256), 0, st, a, sums, p.count_each);
