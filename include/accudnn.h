@@ -492,7 +492,8 @@ int acc_op_glu_bwd(const void* x, const void* w, const float* bias, const void* 
  * listed class beyond the last one makes the row's loss NaN and has no term in dz, and so does a label outside [0, classes) where alpha < 1.  Listed logits of minus infinity have probability 0; a
  * row whose listed logits or whose z are all minus infinity, or contain infinity, has NaN in its loss and in dz (at the listed classes resp. at all).  Above T = 4
  * the sum and q - p are worked out by differences of logits: T^2 and T stand before no rounding of numbers near one.  loss_rows [n], loss [1], dz [n][classes] (dtype): each
- * may be NULL, at least one is not; dz may be z, nothing else that is written may overlap another argument (ACC_EINVAL).  n, classes <= 2^20, k <= 1024.
+ * may be NULL, at least one is not; dz may be z, nothing else that is written may overlap another argument (ACC_EINVAL).  n, classes <= 2^20, k <= 1024,
+ * fewer than 2^22 workgroups (a row, or 16448 fp32 or 32896 bf16 logits of one that has more than 2^16 resp. 2^17, each).
  * workspace: acc_op_distill_workspace() bytes (0: the sizes are refused); nothing in either workspace needs to be kept or cleared, and none is shared by
  * calls that overlap.  The same bits every time. */
 size_t acc_op_top_logits_workspace(int n, int classes, int k, int dtype);
