@@ -47,7 +47,7 @@ struct DistillArgs {
   const int* counts;           // rows that count, in parts; null: counted here
   int count_parts;
   // cut rows
-  float *part, *at_list;       // part[row][4][splits]: the largest logit and R at both temperatures; at_list[row][k + 1]: logits of the list and of the label
+  float *part, *at_list;       // part[row][3][splits]: the largest logit and R at both temperatures; at_list[row][k + 1]: logits of the list and of the label
   unsigned long long* shares;  // shares[row][splits]: sums of shares()
   int splits, chunks_per_split;
 };
@@ -502,7 +502,7 @@ __global__ __launch_bounds__(256) void distill_part_kernel(DistillArgs a) {
   equal = row_reduce<256>(equal, sh[2], Add());
   if (HARD) s1 = row_reduce<256>(s1, sh[3], Add());
   if (tid == 0) {
-    float* const p = a.part + (size_t)row * 4 * a.splits + sp;
+    float* const p = a.part + (size_t)row * 3 * a.splits + sp;
     const bool none = mx == -INFINITY && !(s != s);    // (nothing but minus infinity: the other parts decide)
     p[0] = mx;
     p[a.splits] = none ? -1.f : s + (equal - 1.f);
@@ -512,7 +512,7 @@ __global__ __launch_bounds__(256) void distill_part_kernel(DistillArgs a) {
 
 // The parts' sums joined, by every wave
 __device__ __forceinline__ RowSums sums_of_parts(const DistillArgs& a, int row, int lane) {
-  const float* const at = a.part + (size_t)row * 4 * a.splits;
+  const float* const at = a.part + (size_t)row * 3 * a.splits;
   const bool mine = lane < a.splits;
   const float m = mine ? at[lane] : -INFINITY, rest = mine ? at[a.splits + lane] : -1.f, rest1 = mine ? at[2 * a.splits + lane] : -1.f;
   RowSums t;
@@ -673,7 +673,7 @@ DistillPlan distill_plan(int n, int classes, int k, int dtype) {
   p.rows = take((size_t)n * 4);
   p.sums = take(p.sum_parts ? (size_t)p.count_parts * 8 : 0);
   p.counts = take((size_t)p.count_parts * 4);
-  p.part = take(p.splits > 1 ? (size_t)n * 4 * p.splits * 4 : 0);
+  p.part = take(p.splits > 1 ? (size_t)n * 3 * p.splits * 4 : 0);
   p.at_list = take(p.splits > 1 ? (size_t)n * (k + 1) * 4 : 0);
   p.shares = take(p.splits > 1 ? (size_t)n * p.splits * 8 : 0);
   p.total = at;
