@@ -4,14 +4,16 @@
 // which works them out again, their gradients da and db, leaves them.  Those are [rows][2 f] = dz, and the rest is that of a linear layer: dx = dz w, dw = dz^T x.
 //
 // dz is kept as the sum of bf16 values, the first the nearest one, the next the nearest to what is left (relative errors of 2^-8, 2^-16, 2^-24).  dx, rounded to
-// bf16 itself, is multiplied from the first: the errors of its 2 f terms are independent and add up to one more rounding of the result's size (relative error of dx,
-// one value / two: 2.3e-3 / 1.7e-3, in 300 / 480 us at 12544 rows, 1024 wide, 2 x 4096).  dw, an fp32 result, is multiplied from two, of fewer than 4096 rows from three, where two
+// bf16 itself, is multiplied from two: one would do if its errors stayed beside the result's own rounding, but where a row of dh sums to zero, as in front of a
+// normalisation, and the values are alike, what the gates' weights have in common cancels in dx and its errors do not (relative error of dx, 300 x 128 x 64, a common
+// part of 10 and 30 times the weights' spread: one value 0.014 and 0.021, two 0.0017, which is the rounding of the result; nothing in common: 0.0023 and 0.0017;
+// 12544 rows, 1024 to 2 x 4096, all gradients of kept projections 672 and 810 us).  dw, an fp32 result, is multiplied from two, of fewer than 4096 rows from three, where two
 // would show beside the roundings of a sum of so few terms in fp32.  Relative error of dw, 1e-7, two / three / all in fp32: 64 rows 24 / 1.1 / 1.5, 1500 24 / 1.7 / 7.0, 4096
 // 24 / 2.6 / 11.5, 16384 24 / 2.8 / 23; dz and dw of 4096 rows, 512 wide, 2 x 1024, 40 / 51 us.
 //
 // All bound by the matrix cores but for the smallest, which are launches behind each other.  12544 rows, 1024 to 2 x 4096 (210 GFLOP a product), us: forward 204 (1030 TFLOP/s; 218 where the
-// projections are kept), dz from the projections worked out again 320 (660: behind each tile's sums the gradients of its 65536 values, which no other workgroup covers), dx 212-225
-// (960: 196 tiles of 256 x 256 on 256 compute units), dw from two values 300-315 (1370 TFLOP/s of both).  A library's product of these sizes alone takes 141 to 175.
+// projections are kept), dz from the projections worked out again 320 (660: behind each tile's sums the gradients of its 65536 values, which no other workgroup covers), dx from two
+// values 350 (1200 TFLOP/s of both), dw from two values 300-315 (1370).  A library's product of these sizes alone takes 141 to 175.
 #include "glu.h"
 
 #include "gemm_bf16.h"
@@ -353,7 +355,7 @@ __device__ __forceinline__ void glu_product(const ProductArgs& a, int work, char
   GemmAcc<C> acc;
   gemm_tile<C>(a.a, a.b, m0, n0, split * a.k_per_split, min(a.k, (split + 1) * a.k_per_split), lds, acc);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm0 = (wave / C::WN) * 32 * C::MB, wn0 = (wave % C::WN) * 32 * C::NB;
-  if (a.out) {                                         // (whole pieces of rows: all gradients of 41379 x 1056 x 136 take 191 us, with four values of a lane as they are 206)
+  if (a.out) {                                         // (whole pieces of rows: 15 us less than four values of a lane as they are, of 41379 x 1056 x 136)
     typedef Stage<32 * C::NB> S;
     static_assert(C::WM * C::WN * S::ONE <= C::LDS, "the results' rows fit the operands' place");
     char* const stg = lds + wave * S::ONE;
@@ -494,9 +496,9 @@ typedef GemmCfg<2, 2, 2, 2, 64, 2, false, false, 1, true, true> G128;
 typedef GemmCfg<2, 1, 1, 2, 64, 3, false, false, 1, true, true> G64;
 typedef GemmCfg<2, 2, 2, 2, 64, 2, false, false, 1, true> S128;            // projections in parts
 typedef GemmCfg<2, 2, 1, 1, 64, 4, false, false, 1, true> S64;
-typedef GemmCfg<2, 4, 4, 2, 64, 2, false, true, 1, true> X256;             // dx
-typedef GemmCfg<2, 2, 2, 2, 64, 2, false, true, 1, true> X128;
-typedef GemmCfg<2, 2, 1, 1, 64, 4, false, true, 1, true> X64;
+typedef GemmCfg<2, 4, 4, 2, 32, 3, false, true, 2, true> X256;             // dx
+typedef GemmCfg<2, 2, 2, 2, 32, 3, false, true, 2, true> X128;
+typedef GemmCfg<2, 2, 1, 1, 32, 4, false, true, 2, true> X64;
 typedef GemmCfg<2, 4, 4, 2, 32, 3, true, true, 2, false> W256;             // dw
 typedef GemmCfg<2, 2, 2, 2, 32, 2, true, true, 2, false> W128;
 typedef GemmCfg<2, 2, 1, 1, 32, 4, true, true, 2, false> W64;
@@ -570,18 +572,18 @@ GluPlan16 glu_plan16(int rows, int d, int f, bool backward, bool kept) {
   p.w = take(p.pad_w ? (size_t)wide * p.dp * 2 : 0);
   p.sums = take(p.cut ? (size_t)p.proj.splits * rows * wide * 4 : 0);
   if (backward) {
-    p.dx = choose(ByColumns, rows, d, wide, 1, 1L << 25, 256);
+    p.dx = choose(ByColumns, rows, d, wide, 2, 1L << 25, 256);
     p.dw = choose(ByColumns, wide, d, rows, p.parts, 1L << 25, 128);
-    const Choice dx = choose(ByColumns, rows, d, wide, 1, 1L << 25, 256, 2), dw = choose(ByColumns, wide, d, rows, p.parts, 1L << 25, 128, 2);      // 64 x 64
+    const Choice dx = choose(ByColumns, rows, d, wide, 2, 1L << 25, 256, 2), dw = choose(ByColumns, wide, d, rows, p.parts, 1L << 25, 128, 2);      // 64 x 64
     const long tx = ceil_div(d, 64) * ceil_div(rows, 64), tw = ceil_div(d, 64) * ceil_div(wide, 64);
     // (whole sums save the launch that adds parts)
-    const Choice x1 = choose(ByColumns, rows, d, wide, 1, 0, 256, 2), w1 = choose(ByColumns, wide, d, rows, p.parts, 0, 128, 2);
+    const Choice x1 = choose(ByColumns, rows, d, wide, 2, 0, 256, 2), w1 = choose(ByColumns, wide, d, rows, p.parts, 0, 128, 2);
     const bool sums = !(x1.us < dx.us + kSaved && w1.us < dw.us + kSaved);
     const Choice &cx = sums ? dx : x1, &cw = sums ? dw : w1;
     // Up to 1024 workgroups, or 2048 of few steps: 64 x 64 tiles take twice the LDS reads of larger ones.  (us, all gradients of kept projections, so / each for itself:
-    // 196 x 512 x 1024 18.5 / 22.9, 4096 x 512 x 1024 57 / 65, 3867 x 304 x 1936 100 / 112, 10000 x 512 x 1024 140 / 153, 8192 x 512 x 2048 219 / 204)
-    const long workgroups = tx * cx.splits + tw * cw.splits, steps = tx * ceil_div(wide, 64) + tw * ceil_div(rows, 64) * p.parts;
-    p.together = workgroups <= 1024 || (workgroups <= 2048 && steps <= 600 * 256);
+    // 196 x 512 x 1024 18.0 / 22.6, 4096 x 512 x 1024 65 / 73, 3867 x 304 x 1936 121 / 130, 5000 x 768 x 1024 108 / 95, 10000 x 512 x 1024 158 / 163, 8192 x 512 x 2048 289 / 236)
+    const long workgroups = tx * cx.splits + tw * cw.splits, steps = tx * ceil_div(wide, 64) * 2 + tw * ceil_div(rows, 64) * p.parts;
+    p.together = workgroups <= 1024 || (workgroups <= 2048 && steps <= 420 * 256);
     if (p.together) { p.dx = cx; p.dw = cw; }
     // rows of a part of dw: fewer than 4 GiB of dz and of x
     const long most = (0xF0000000L / (2 * (wide > p.dp ? wide : p.dp))) / 64 * 64;
@@ -642,7 +644,7 @@ hipError_t glu_bf16(const GluArgs& a, bool backward) {
   const int wide = 2 * p.fp;
   bf16_t* dz[3] = {(bf16_t*)(a.ws + p.dz[0]), (bf16_t*)(a.ws + p.dz[1]), (bf16_t*)(a.ws + p.dz[2])};
   float* const db_part = backward && a.db ? (float*)(a.ws + p.db) : nullptr;
-  const int parts = !a.dw ? 1 : p.parts;
+  const int parts = !a.dw ? 2 : p.parts;
   if (kept || p.cut) {
     PointArgs q{};
     q.ab_in = a.ab_in; q.dh = a.dh; q.h = a.h; q.ab = a.ab;
