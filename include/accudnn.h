@@ -465,7 +465,7 @@ int acc_op_linear_ce(const void* x, const void* w, const float* bias, const int3
  * dtype; bias [2 f], dw [2 f][d] and db [2 f]: fp32.  bias may be NULL (none).  act: ACC_ACT_* (the slope of ACC_ACT_RELU at 0 is 0).
  * ab in fwd may be NULL; otherwise the projections are kept there.  ab in bwd: the kept ones (bias is then not looked at; bf16: gradients are those at the rounded values), or NULL:
  * they are worked out again, half as much work more in place of 2 rows f values of memory.  dx, dw, db in bwd: each may be NULL, at least one is not.
- * Sums and statistics are fp32; [da | db] of bf16 operands is the sum of two bf16 values in dx and dw, of three in dw for fewer than 4096 rows.
+ * Sums and statistics are fp32; [da | db] of bf16 operands is the sum of two bf16 values in dx and dw, of three in dw for fewer than 10240 rows.
  * Values that are not finite stay in the results that they enter (an infinity may come out as NaN), also through a closed gate, as 0 times them; a gate of minus
  * infinity is a closed one: act and its slope are 0 there (ACC_ACT_NONE: minus infinity and 1).
  * rows <= 2^24, d, f <= 65536, f d (each rounded up to a multiple of 8) below 2^30 - 2^20, rows (d + f) <= 2^36.  workspace: acc_op_glu_workspace() bytes (0

@@ -7,9 +7,10 @@
 // bf16 itself, is multiplied from two: one would do if its errors stayed beside the result's own rounding, but where a row of dh sums to zero, as in front of a
 // normalisation, and the values are alike, what the gates' weights have in common cancels in dx and its errors do not (relative error of dx, 300 x 128 x 64, a common
 // part of 10 and 30 times the weights' spread: one value 0.014 and 0.021, two 0.0017, which is the rounding of the result; nothing in common: 0.0023 and 0.0017;
-// 12544 rows, 1024 to 2 x 4096, all gradients of kept projections 672 and 810 us).  dw, an fp32 result, is multiplied from two, of fewer than 4096 rows from three, where two
-// would show beside the roundings of a sum of so few terms in fp32.  Relative error of dw, 1e-7, two / three / all in fp32: 64 rows 24 / 1.1 / 1.5, 1500 24 / 1.7 / 7.0, 4096
-// 24 / 2.6 / 11.5, 16384 24 / 2.8 / 23; dz and dw of 4096 rows, 512 wide, 2 x 1024, 40 / 51 us.
+// 12544 rows, 1024 to 2 x 4096, all gradients of kept projections 672 and 810 us).  dw, an fp32 result, is multiplied from three, from 10240 rows on from two,
+// whose errors are there at most 1.4 times those of a sum of so many terms in fp32.  Relative error of dw, 1e-7, two / three / all in fp32: 64 rows 24 / 1.1 / 1.5, 1500 24 / 1.7 / 7.0,
+// 4096 25 / 5.4 / 11.8, 8192 25 / 7.3 / 16.5, 10000 25 / 8.0 / 18.1, 12544 26 / - / 20, 16384 26 / - / 23, 32768 25 / - / 32; all gradients of kept projections of 4096 rows, 512 wide,
+// 2 x 1024, 65 / 76 us, of 8192, 2 x 2048, 235 / 269.
 //
 // All bound by the matrix cores but for the smallest, which are launches behind each other.  12544 rows, 1024 to 2 x 4096 (210 GFLOP a product), us: forward 204 (1030 TFLOP/s; 218 where the
 // projections are kept), dz from the projections worked out again 320 (660: behind each tile's sums the gradients of its 65536 values, which no other workgroup covers), dx from two
@@ -553,7 +554,7 @@ GluPlan16 glu_plan16(int rows, int d, int f, bool backward, bool kept) {
   p.dp = (int)up(d, 8);
   p.fp = (int)up(f, 8);
   p.pad_x = p.dp != d;
-  p.parts = rows < 4096 ? 3 : 2;
+  p.parts = rows < 10240 ? 3 : 2;
   const long wide = 2L * p.fp;
   double us = 0;
   for (const PairTile& t : kPair) {
@@ -581,7 +582,7 @@ GluPlan16 glu_plan16(int rows, int d, int f, bool backward, bool kept) {
     const bool sums = !(x1.us < dx.us + kSaved && w1.us < dw.us + kSaved);
     const Choice &cx = sums ? dx : x1, &cw = sums ? dw : w1;
     // Up to 1024 workgroups, or 2048 of few steps: 64 x 64 tiles take twice the LDS reads of larger ones.  (us, all gradients of kept projections, so / each for itself:
-    // 196 x 512 x 1024 18.0 / 22.6, 4096 x 512 x 1024 65 / 73, 3867 x 304 x 1936 121 / 130, 5000 x 768 x 1024 108 / 95, 10000 x 512 x 1024 158 / 163, 8192 x 512 x 2048 289 / 236)
+    // 196 x 512 x 1024 18.0 / 22.6, 4096 x 512 x 1024 76 / 79, 3867 x 304 x 1936 121 / 130, 5000 x 768 x 1024 125 / 107, 10000 x 512 x 1024 185 / 192, 8192 x 512 x 2048 334 / 269)
     const long workgroups = tx * cx.splits + tw * cw.splits, steps = tx * ceil_div(wide, 64) * 2 + tw * ceil_div(rows, 64) * p.parts;
     p.together = workgroups <= 1024 || (workgroups <= 2048 && steps <= 420 * 256);
     if (p.together) { p.dx = cx; p.dw = cw; }

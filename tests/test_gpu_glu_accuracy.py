@@ -50,3 +50,18 @@ def test_what_the_weights_have_in_common_cancels_in_dx(rows, d, f, common, kept)
     dz = dz_of(ab.double(), dh, "none")
     ref, summed = dz @ w.double(), dz.abs() @ w.double().abs()
     assert (dx.double() - ref).norm() <= 2.0 ** -8 * ref.norm() + (2.0 ** -16 + 1e-5) * summed.norm()
+
+
+@pytest.mark.parametrize("rows", [1000, 4095, 4096, 6000, 8192, 10239])
+@pytest.mark.parametrize("d,f", [(64, 40), (256, 136), (512, 1024)])
+def test_dw_keeps_the_digits_of_a_sum_in_fp32(rows, d, f):
+    # The running sum of n terms at random is on average n / 2 terms' squares; rounded by 2^-24 of itself at most each time that a product of sixteen terms of one of three
+    # values is added, 3 n / 16 times, it is off by (3 n / 32)^(1/2) 2^-24 of the result, as norms.  dz of kept projections is off by a few roundings of 2^-24 and the activation's 2^-22: 4e-7.
+    g = torch.Generator(device="cuda").manual_seed(rows + d)
+
+    def r(*s):
+        return torch.randn(*s, generator=g, device="cuda")
+    x, w, dh, ab = r(rows, d).bfloat16(), (r(2 * f, d) / d ** 0.5).bfloat16(), r(rows, f).bfloat16(), r(rows, 2 * f).bfloat16()
+    dw = gradients(x, w, None, ab, dh, "silu")[1]
+    ref = dz_of(ab.double(), dh, "silu").T @ x.double()
+    assert (dw.double() - ref).norm() <= (4e-7 + 2.0 ** -24 * (3 * rows / 32) ** 0.5) * ref.norm()
