@@ -56,6 +56,7 @@ struct PointArgs {
   float* db_part;              // [slab][pitch], or null
   int rows, f, act, splits, pitch, half, tx, across, slab;
 };
+// parts: values that dz is kept as the sum of, 0 where it is not kept
 hipError_t glu_point(const PointArgs& a, bool backward, int parts, int dtype, hipStream_t st);
 // slabs of a launch (rows of db_part); sets tx, across and slab
 int glu_point_shape(PointArgs& a, int dtype);

@@ -138,8 +138,11 @@ __global__ __launch_bounds__(256) void glu_point_kernel(PointArgs a) {
         glu_slopes(a.act, g[e], v[e], dh[e], da, db);
         g[e] = e < left ? da : 0.f;
         v[e] = e < left ? db : 0.f;
-        sa[e] += g[e];
-        sb[e] += v[e];
+        {
+#pragma clang fp contract(off)                         // (the same bits whether dz is written or not)
+          sa[e] += g[e];
+          sb[e] += v[e];
+        }
       }
       // (columns up to a.half exist and are zero from a.f on)
 #pragma unroll
@@ -290,7 +293,7 @@ struct Pair32 {
   int rows, d, f, act, tiles_m, tiles;
   float *h, *ab;               // forward
   const float* dh;             // backward
-  float *dz, *db_part;
+  float *dz, *db_part;         // each may be null
 };
 template <class C, bool BWD>
 __global__ __launch_bounds__(C::THREADS) void glu32_kernel(Pair32 a, int blocks) {
@@ -339,8 +342,10 @@ __global__ __launch_bounds__(C::THREADS) void glu32_kernel(Pair32 a, int blocks)
           sa[e] += da;
           sb[e] += db;
         }
-        put<float, 4>(a.dz + m * 2 * f + c, left, g);
-        put<float, 4>(a.dz + m * 2 * f + f + c, left, v);
+        if (a.dz) {
+          put<float, 4>(a.dz + m * 2 * f + c, left, g);
+          put<float, 4>(a.dz + m * 2 * f + f + c, left, v);
+        }
       }
     }
     if (BWD && a.db_part) {
@@ -426,7 +431,7 @@ hipError_t glu32(const GluArgs& a, bool backward) {
   const bool kept = backward && a.ab_in;
   const GluPlan32 p = glu_plan32(a.rows, a.d, a.f, backward, kept);
   const float *x = (const float*)a.x, *w = (const float*)a.w;
-  float *const dz = (float*)(a.ws + p.dz), *const db_part = backward && a.db ? (float*)(a.ws + p.db) : nullptr;
+  float *const dz = a.dx || a.dw ? (float*)(a.ws + p.dz) : nullptr, *const db_part = backward && a.db ? (float*)(a.ws + p.db) : nullptr;
   hipStream_t st = a.st;
   const int wide = 2 * a.f;
   if (kept || p.cut) {
@@ -441,7 +446,7 @@ hipError_t glu32(const GluArgs& a, bool backward) {
       q.sums = g.out; q.splits = p.proj.splits; q.bias = a.bias;
     }
     glu_point_shape(q, DT_F32);
-    if (const hipError_t e = glu_point(q, backward, 1, DT_F32, st); e != hipSuccess || !backward) return e;
+    if (const hipError_t e = glu_point(q, backward, dz ? 1 : 0, DT_F32, st); e != hipSuccess || !backward) return e;
   } else {
     Pair32 g{};
     g.x = {x, a.rows, a.d}; g.w = {w, a.f, a.d, (uint32_t)a.f * (uint32_t)a.d};
@@ -513,10 +518,11 @@ hipError_t glu_point(const PointArgs& a, bool backward, int parts, int dtype, hi
   const dim3 grid((unsigned)(ceil_div(a.rows, a.slab) * a.across));
 #define ACC_POINT(T, BWD, PARTS, SUMS) hipLaunchKernelGGL((glu_point_kernel<T, BWD, PARTS, SUMS>), grid, dim3(256), 0, st, a)
   if (!backward) { if (dtype == DT_F32) ACC_POINT(float, false, 1, true); else ACC_POINT(bf16_t, false, 1, true); }
-  else if (dtype == DT_F32) { if (a.sums) ACC_POINT(float, true, 1, true); else ACC_POINT(float, true, 1, false); }
+  else if (dtype == DT_F32 && parts) { if (a.sums) ACC_POINT(float, true, 1, true); else ACC_POINT(float, true, 1, false); }
+  else if (dtype == DT_F32) { if (a.sums) ACC_POINT(float, true, 0, true); else ACC_POINT(float, true, 0, false); }
   else if (parts == 3) { if (a.sums) ACC_POINT(bf16_t, true, 3, true); else ACC_POINT(bf16_t, true, 3, false); }
   else if (parts == 2) { if (a.sums) ACC_POINT(bf16_t, true, 2, true); else ACC_POINT(bf16_t, true, 2, false); }
-  else { if (a.sums) ACC_POINT(bf16_t, true, 1, true); else ACC_POINT(bf16_t, true, 1, false); }
+  else { if (a.sums) ACC_POINT(bf16_t, true, 0, true); else ACC_POINT(bf16_t, true, 0, false); }
 #undef ACC_POINT
   return hipGetLastError();
 }

@@ -611,6 +611,7 @@ template <class C, class Q> void launch_pair(const PairArgs& g, bool backward, i
   const unsigned blocks = whole_eights16(backward ? g.tiles : g.whole), grid = blocks + whole_eights16(4L * (g.tiles - g.whole));
   if (!backward) hipLaunchKernelGGL((glu_fwd_kernel<C, Q>), dim3(grid), dim3(C::THREADS), 0, st, g, (int)blocks);
   else if (parts == 3) hipLaunchKernelGGL((glu_dz_kernel<C, 3>), dim3(blocks), dim3(C::THREADS), 0, st, g, (int)blocks);
+  else if (parts == 0) hipLaunchKernelGGL((glu_dz_kernel<C, 0>), dim3(blocks), dim3(C::THREADS), 0, st, g, (int)blocks);
   else hipLaunchKernelGGL((glu_dz_kernel<C, 2>), dim3(blocks), dim3(C::THREADS), 0, st, g, (int)blocks);
 }
 template <class C> void launch_product(const ProductArgs& g, hipStream_t st) {
@@ -645,7 +646,7 @@ hipError_t glu_bf16(const GluArgs& a, bool backward) {
   const int wide = 2 * p.fp;
   bf16_t* dz[3] = {(bf16_t*)(a.ws + p.dz[0]), (bf16_t*)(a.ws + p.dz[1]), (bf16_t*)(a.ws + p.dz[2])};
   float* const db_part = backward && a.db ? (float*)(a.ws + p.db) : nullptr;
-  const int parts = !a.dw ? 2 : p.parts;
+  const int parts = a.dw ? p.parts : a.dx ? 2 : 0;     // values of dz that something is multiplied from
   if (kept || p.cut) {
     PointArgs q{};
     q.ab_in = a.ab_in; q.dh = a.dh; q.h = a.h; q.ab = a.ab;
@@ -676,10 +677,10 @@ hipError_t glu_bf16(const GluArgs& a, bool backward) {
     g.h = (bf16_t*)a.h; g.ab = (bf16_t*)a.ab; g.dh = (const bf16_t*)a.dh;
     for (int i = 0; i < 3; ++i) g.dz[i] = dz[i];
     g.pitch = wide; g.half = p.fp; g.db_part = db_part;
-    if (p.tile.m == 256 && p.tile.n == 256) launch_pair<G256, G256Q>(g, backward, p.parts, st);
-    else if (p.tile.m == 256) launch_pair<G256N, G256N>(g, backward, p.parts, st);
-    else if (p.tile.m == 128) launch_pair<G128, G128>(g, backward, p.parts, st);
-    else launch_pair<G64, G64>(g, backward, p.parts, st);
+    if (p.tile.m == 256 && p.tile.n == 256) launch_pair<G256, G256Q>(g, backward, parts, st);
+    else if (p.tile.m == 256) launch_pair<G256N, G256N>(g, backward, parts, st);
+    else if (p.tile.m == 128) launch_pair<G128, G128>(g, backward, parts, st);
+    else launch_pair<G64, G64>(g, backward, parts, st);
     if (!backward) return hipGetLastError();
   }
   const GemmOperand z{dz[0], {dz[1], dz[2]}, a.rows, wide, wide};
