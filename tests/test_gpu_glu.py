@@ -110,8 +110,8 @@ def check_backward(x, w, bias, ab, dh, act, dtype):
     near(got["db"], db, err.sum(0) + E * dz.abs().sum(0) + 2.0 ** -24 * db.abs(), "db", 2e-5 * 4 if act == "relu" else 2e-5)
 
 
-# one row, one value; up to four rows and more; widths of no whole eights and odd ones; each tile, sums that are cut, several launches or one; two and three
-# parts of dz on both sides of 4096 rows
+# one row, one value; up to four rows and more; widths of no whole eights and odd ones; sums that are cut, several launches or one; few and many rows (each tile
+# with each number of values of dz: test_gpu_glu_tiles.py)
 SIZES = [(1, 1, 1), (1, 8, 8), (2, 3, 5), (3, 512, 100), (4, 24, 1), (4, 2050, 37), (5, 16, 16), (5, 2, 9), (1, 4096, 33), (9, 4096, 40), (7, 1160, 1003),
          (64, 64, 64), (65, 72, 57), (130, 96, 200), (257, 264, 130), (300, 40, 1000), (1000, 17, 3), (33, 1027, 129), (31, 2048, 16), (512, 512, 512),
          (2009, 100, 65), (4095, 32, 24), (4096, 32, 24), (4100, 64, 40), (5001, 9, 11), (8192, 256, 1024), (3000, 1024, 512), (16400, 64, 520), (20000, 1, 1),
