@@ -657,6 +657,17 @@ def _fits(name, what, t, shape, dtype, device):
     return t.data_ptr()
 
 
+def _sizes(name, *sizes):
+    """Refuses sizes that the library's 32 bits would take modulo 2^32."""
+    if max(sizes) > 0x7FFFFFFF:
+        raise AccError(ACC_EINVAL, f"{name}: a size passes 32 bits: {sizes}")
+
+
+def _bytes(workspace, *args):
+    """Of a workspace; 0, as for other sizes that are refused, where one passes 32 bits."""
+    return int(workspace(*args)) if max(args) <= 0x7FFFFFFF else 0
+
+
 def _space(name, ws, device):
     if ws.get_device() != device or not ws.is_contiguous():
         raise AccError(ACC_EINVAL, f"{name}: the workspace must be contiguous and on the current device (cuda:{device}), got {ws.device}")
@@ -669,7 +680,7 @@ def _done(rc):
 
 
 def op_gn_workspace(n, hw, c, groups) -> int:
-    return int(_lib.acc_op_gn_workspace(n, hw, c, groups))
+    return _bytes(_lib.acc_op_gn_workspace, n, hw, c, groups)
 
 
 def op_gn_fwd(x, gamma, beta, res, y, mean, istd, groups, act, eps, ws):
@@ -677,11 +688,13 @@ def op_gn_fwd(x, gamma, beta, res, y, mean, istd, groups, act, eps, ws):
     torch, device, stream = _here()
     name, shape, kind, f32, dtype = "op_gn_fwd", x.shape, x.dtype, torch.float32, _dtype_of(x)
     n, c = shape[0], shape[-1]
+    hw = x.numel() // max(n * c, 1)
+    _sizes(name, n, hw, c)
     at, size = _space(name, ws, device)
     _done(_lib.acc_op_gn_fwd(_fits(name, "x", x, shape, kind, device), _fits(name, "gamma", gamma, (c,), f32, device),
                              _fits(name, "beta", beta, (c,), f32, device), None if res is None else _fits(name, "res", res, shape, kind, device),
                              _fits(name, "y", y, shape, kind, device), _fits(name, "mean", mean, (n, groups), f32, device),
-                             _fits(name, "istd", istd, (n, groups), f32, device), n, x.numel() // max(n * c, 1), c, groups, act, eps, at, size, dtype,
+                             _fits(name, "istd", istd, (n, groups), f32, device), n, hw, c, groups, act, eps, at, size, dtype,
                              stream))
 
 
@@ -691,6 +704,8 @@ def op_gn_bwd(x, dy, y, res, gamma, beta, mean, istd, dx, dgamma, dbeta, dres, g
     torch, device, stream = _here()
     name, shape, kind, f32, dtype = "op_gn_bwd", x.shape, x.dtype, torch.float32, _dtype_of(x)
     n, c = shape[0], shape[-1]
+    hw = x.numel() // max(n * c, 1)
+    _sizes(name, n, hw, c)
     at, size = _space(name, ws, device)
     _done(_lib.acc_op_gn_bwd(_fits(name, "x", x, shape, kind, device), _fits(name, "dy", dy, shape, kind, device),
                              None if y is None else _fits(name, "y", y, shape, kind, device),
@@ -698,12 +713,12 @@ def op_gn_bwd(x, dy, y, res, gamma, beta, mean, istd, dx, dgamma, dbeta, dres, g
                              _fits(name, "beta", beta, (c,), f32, device), _fits(name, "mean", mean, (n, groups), f32, device),
                              _fits(name, "istd", istd, (n, groups), f32, device), _fits(name, "dx", dx, shape, kind, device),
                              _fits(name, "dgamma", dgamma, (c,), f32, device), _fits(name, "dbeta", dbeta, (c,), f32, device),
-                             None if dres is None else _fits(name, "dres", dres, shape, kind, device), n, x.numel() // max(n * c, 1), c, groups, act,
+                             None if dres is None else _fits(name, "dres", dres, shape, kind, device), n, hw, c, groups, act,
                              at, size, dtype, stream))
 
 
 def op_linear_ce_workspace(n, d, classes, gradients: bool, dtype: int = F32) -> int:
-    return int(_lib.acc_op_linear_ce_workspace(n, d, classes, 1 if gradients else 0, int(dtype)))
+    return _bytes(_lib.acc_op_linear_ce_workspace, n, d, classes, 1 if gradients else 0, int(dtype))
 
 
 def op_linear_ce(x, w, bias, labels, loss_rows, loss, dx, dw, db, ws, ignore=None):
@@ -714,6 +729,7 @@ def op_linear_ce(x, w, bias, labels, loss_rows, loss, dx, dw, db, ws, ignore=Non
     name, f32, i32, kind, dtype = "op_linear_ce", torch.float32, torch.int32, x.dtype, _dtype_of(x)
     n, d = x.shape
     classes = w.shape[0]
+    _sizes(name, n, d, classes)
 
     def given(what, t, shape, dt):
         return None if t is None else _fits(name, what, t, shape, dt, device)
@@ -725,7 +741,7 @@ def op_linear_ce(x, w, bias, labels, loss_rows, loss, dx, dw, db, ws, ignore=Non
 
 
 def op_glu_workspace(rows, d, f, backward: bool, dtype: int = F32) -> int:
-    return int(_lib.acc_op_glu_workspace(rows, d, f, 1 if backward else 0, int(dtype)))
+    return _bytes(_lib.acc_op_glu_workspace, rows, d, f, 1 if backward else 0, int(dtype))
 
 
 def op_glu_fwd(x, w, bias, h, ab, act, ws):
@@ -734,10 +750,12 @@ def op_glu_fwd(x, w, bias, h, ab, act, ws):
     torch, device, stream = _here()
     name, kind, dtype, shape = "op_glu_fwd", x.dtype, _dtype_of(x), x.shape
     d, f, lead = shape[-1], w.shape[0] // 2, shape[:-1]
+    rows = x.numel() // max(d, 1)
+    _sizes(name, rows, d, f)
     at, size = (None, 0) if ws is None else _space(name, ws, device)
     _done(_lib.acc_op_glu_fwd(_fits(name, "x", x, shape, kind, device), _fits(name, "w", w, (2 * f, d), kind, device),
                               None if bias is None else _fits(name, "bias", bias, (2 * f,), torch.float32, device), _fits(name, "h", h, (*lead, f), kind, device),
-                              None if ab is None else _fits(name, "ab", ab, (*lead, 2 * f), kind, device), x.numel() // max(d, 1), d, f, act, at, size, dtype,
+                              None if ab is None else _fits(name, "ab", ab, (*lead, 2 * f), kind, device), rows, d, f, act, at, size, dtype,
                               stream))
 
 
@@ -747,17 +765,19 @@ def op_glu_bwd(x, w, bias, ab, dh, dx, dw, db, act, ws):
     torch, device, stream = _here()
     name, kind, dtype, shape, f32 = "op_glu_bwd", x.dtype, _dtype_of(x), x.shape, torch.float32
     d, f, lead = shape[-1], w.shape[0] // 2, shape[:-1]
+    rows = x.numel() // max(d, 1)
+    _sizes(name, rows, d, f)
 
     def given(what, t, shape, dt):
         return None if t is None else _fits(name, what, t, shape, dt, device)
     at, size = _space(name, ws, device)
     _done(_lib.acc_op_glu_bwd(_fits(name, "x", x, shape, kind, device), _fits(name, "w", w, (2 * f, d), kind, device), given("bias", bias, (2 * f,), f32),
                               given("ab", ab, (*lead, 2 * f), kind), _fits(name, "dh", dh, (*lead, f), kind, device), given("dx", dx, shape, kind),
-                              given("dw", dw, (2 * f, d), f32), given("db", db, (2 * f,), f32), x.numel() // max(d, 1), d, f, act, at, size, dtype, stream))
+                              given("dw", dw, (2 * f, d), f32), given("db", db, (2 * f,), f32), rows, d, f, act, at, size, dtype, stream))
 
 
 def op_top_logits_workspace(n, classes, k, dtype: int = F32) -> int:
-    return int(_lib.acc_op_top_logits_workspace(n, classes, k, int(dtype)))
+    return _bytes(_lib.acc_op_top_logits_workspace, n, classes, k, int(dtype))
 
 
 def op_top_logits(z, index, top, ws):
@@ -767,13 +787,14 @@ def op_top_logits(z, index, top, ws):
     name, kind, dtype = "op_top_logits", z.dtype, _dtype_of(z)
     n, classes = z.shape
     k = index.shape[-1]
+    _sizes(name, n, classes, k)
     at, size = (None, 0) if ws is None else _space(name, ws, device)
     _done(_lib.acc_op_top_logits(_fits(name, "z", z, (n, classes), kind, device), _fits(name, "index", index, (n, k), torch.int32, device),
                                  _fits(name, "top", top, (n, k), torch.float32, device), n, classes, k, at, size, dtype, stream))
 
 
 def op_distill_workspace(n, classes, k, dtype: int = F32) -> int:
-    return int(_lib.acc_op_distill_workspace(n, classes, k, int(dtype)))
+    return _bytes(_lib.acc_op_distill_workspace, n, classes, k, int(dtype))
 
 
 def op_distill(z, index, top, labels, loss_rows, loss, dz, temperature, alpha, ws, ignore=None):
@@ -784,6 +805,7 @@ def op_distill(z, index, top, labels, loss_rows, loss, dz, temperature, alpha, w
     name, f32, i32, kind, dtype = "op_distill", torch.float32, torch.int32, z.dtype, _dtype_of(z)
     n, classes = z.shape
     k = index.shape[-1]
+    _sizes(name, n, classes, k)
 
     def given(what, t, shape, dt):
         return None if t is None else _fits(name, what, t, shape, dt, device)
