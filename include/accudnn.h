@@ -463,13 +463,15 @@ int acc_op_linear_ce(const void* x, const void* w, const float* bias, const int3
  *   ab = x w^T + bias,  h = act(a) * b;   da = dh b act'(a),  db = dh act(a),  dx = [da | db] w,  dw = [da | db]^T x,  dbias = their sums over the rows.
  * x [rows][d], w [2 f][d] (f rows of the gate, then f of the value), h and dh [rows][f], ab [rows][2 f] (the projections, gate first), dx [rows][d]: stored as
  * dtype; bias [2 f], dw [2 f][d] and db [2 f]: fp32.  bias may be NULL (none).  act: ACC_ACT_* (the slope of ACC_ACT_RELU at 0 is 0).
- * ab in fwd may be NULL; otherwise the projections are kept there.  ab in bwd: the kept ones (bias is then not looked at; bf16: gradients are those at the rounded values), or NULL:
- * they are worked out again, half as much work more in place of 2 rows f values of memory.  dx, dw, db in bwd: each may be NULL, at least one is not.
+ * ab in fwd may be NULL; otherwise the projections are kept there.  ab in bwd: the kept ones (bias is then not looked at; bf16: gradients are those at the
+ * rounded values), or NULL: they are worked out again, half as much work more in place of 2 rows f values of memory.  dx, dw, db in bwd: each may be NULL, at
+ * least one is not.
  * Sums and statistics are fp32; [da | db] of bf16 operands is the sum of two bf16 values in dx and dw, of three in dw for fewer than 10240 rows.
  * Values that are not finite stay in the results that they enter (an infinity may come out as NaN), also through a closed gate, as 0 times them; a gate of minus
  * infinity is a closed one: act and its slope are 0 there (ACC_ACT_NONE: minus infinity and 1).
- * rows <= 2^24, d, f <= 65536, f d (each rounded up to a multiple of 8) below 2^30 - 2^20, rows (d + f) <= 2^36.  workspace: acc_op_glu_workspace() bytes (0
- * forward for up to three rows, and for sizes that are refused); nothing in it needs to be kept or cleared, and it is not shared by calls that overlap.  What is written may not overlap another
+ * rows <= 2^24, d, f <= 65536, f d (each rounded up to a multiple of 8) below 2^30 - 2^20, rows (d + f) <= 2^36.  workspace: acc_op_glu_workspace() bytes; 0 for
+ * sizes that are refused, and forward also for those that need none (up to three rows, and where neither sums are cut nor widths copied): no sign of a refusal
+ * there.  Nothing in it needs to be kept or cleared, and it is not shared by calls that overlap.  What is written may not overlap another
  * argument (ACC_EINVAL).  No atomics: the same bits every time. */
 size_t acc_op_glu_workspace(int rows, int d, int f, int backward, int dtype);
 int acc_op_glu_fwd(const void* x, const void* w, const float* bias, void* h, void* ab, int rows, int d, int f, int act, void* workspace,
@@ -489,11 +491,12 @@ int acc_op_glu_bwd(const void* x, const void* w, const float* bias, const void* 
  * labels [n] int32 may be NULL, with alpha = 1 (the teacher alone); 0 < alpha <= 1, 1e-18 <= T <= 1e18.  With labels the rows whose label is not `ignore` count
  * (ACC_LABEL_NONE: all), without them the rows whose list is not empty; others have loss 0 and gradient 0 whatever their z holds.  A row that counts and has no
  * list has the label's term alone.  A class that is listed twice has the sum of its entries' probabilities in dz, and both entries in the loss.  A
- * listed class beyond the last one makes the row's loss NaN and has no term in dz, and so does a label outside [0, classes) where alpha < 1.  Listed logits of minus infinity have probability 0; a
- * row whose listed logits or whose z are all minus infinity, or contain infinity, has NaN in its loss and in dz (at the listed classes resp. at all).  Above T = 4
- * the sum and q - p are worked out by differences of logits: T^2 and T stand before no rounding of numbers near one.  loss_rows [n], loss [1], dz [n][classes] (dtype): each
- * may be NULL, at least one is not; dz may be z, nothing else that is written may overlap another argument (ACC_EINVAL).  n, classes <= 2^20, k <= 1024,
- * fewer than 2^22 workgroups (a row, or 16448 fp32 or 32896 bf16 logits of one that has more than 2^16 resp. 2^17, each).
+ * listed class beyond the last one makes the row's loss NaN and has no term in dz, and so does a label outside [0, classes) where alpha < 1.  Listed logits of
+ * minus infinity have probability 0; a row whose listed logits or whose z are all minus infinity, or contain infinity, has NaN in its loss and in dz (at the
+ * listed classes resp. at all).  Above T = 4 the sum and q - p are worked out by differences of logits where the list holds nearly all that the row has: T^2
+ * and T stand before no rounding of numbers near one.  loss_rows [n], loss [1], dz [n][classes] (dtype): each may be NULL, at least one is not; dz may be z,
+ * nothing else that is written may overlap another argument (ACC_EINVAL).  n, classes <= 2^20, k <= 1024, fewer than 2^22 workgroups (a row, or 16448 fp32 or
+ * 32896 bf16 logits of one that has more than 2^16 resp. 2^17, each).
  * workspace: acc_op_distill_workspace() bytes (0: the sizes are refused); nothing in either workspace needs to be kept or cleared, and none is shared by
  * calls that overlap.  The same bits every time. */
 size_t acc_op_top_logits_workspace(int n, int classes, int k, int dtype);

@@ -5,18 +5,18 @@
 //   loss_i = alpha T^2 sum_j p_j (log p_j - log q_cj) + (1 - alpha) (lse(z) - z_label),   loss = mean over the rows that count
 //   dz = (alpha T (q - p) + (1 - alpha) (s - onehot)) / rows that count
 //
-// A row is read once, into the registers of a wave or a workgroup, and its gradient written from there: memory bounds it.  Rows that no registers hold, and
-// few long ones, are cut: a launch leaves the sums of each part, the next joins them and writes the gradient.  The list's probabilities are worked out
-// by the same threads, an entry each, while the row is on its way; the few classes of the list (and the label) are written again, behind a barrier, with their own terms.
+// A row is read once, into the registers of a wave or a workgroup, and its gradient written from there: memory bounds it.  Rows that no registers hold, and few
+// long ones, are cut: a launch leaves the sums of each part, the next joins them and writes the gradient.  The list's probabilities are worked out by the same
+// threads, an entry each, while the row is on its way; the few classes of the list (and the label) are written again, behind a barrier, with their own terms.
 //
 // Sums of exponentials go without the largest one, which is 1: with R the sum of the others', log(1 + R) and, of a class that both give more than a half,
 // q - p = (1 - p) - (1 - q) keep R where a class is all but certain.
 //
-// At high temperatures, where the list holds nearly all that the row has, T^2 sum p (log p - log q) and T (q - p) are what T^2 and T make of the roundings of numbers
-// one.  They are worked out by differences there (Warm).
+// At high temperatures, where the list holds nearly all that the row has, T^2 sum p (log p - log q) and T (q - p) are what T^2 and T make of the roundings of
+// numbers near one.  They are worked out by differences there (Warm).
 //
-// us: 4096 bf16 rows of 65536, lists of 64, 223 (4.8 TB/s read and written, as a copy; with labels 254: a second exponential for each logit; the loss alone 106), of fp32 455;
-// 777 of 50001 59 (512 workgroups run at a time, so two rounds); 4096 of 8192 40 (3.4 TB/s); 64 rows of 10^6, cut, 92.
+// us: 4096 bf16 rows of 65536, lists of 64, 223 (4.8 TB/s read and written, as a copy; with labels 254: a second exponential for each logit; the loss alone
+// 106), of fp32 455; 777 of 50001 59 (512 workgroups run at a time, so two rounds); 4096 of 8192 40 (3.4 TB/s); 64 rows of 10^6, cut, 92.
 #include "kernels.h"
 #include "row_chunks.h"
 
@@ -151,10 +151,10 @@ struct RowSums {
 //
 //   sum p (log p - log q) = sum p x / T + log(E / P) = log(1 + sum p (e^-y - 1 + y) + U e^(m / T) / P),   q_j / p_j = e^(-y_j - that)
 //
-// (sum p y = 0), U the exponentials of the classes that are not listed.  Nothing in it cancels but U, the difference of E and of the listed ones' sum: both are added up
-// in whole numbers, of the same roundings of the same exponentials, so that a list of all classes leaves exactly 0.  Relative error of the loss of 512 fp32 rows of
-// 100 classes, all listed, so / by the plain formula: T = 4 - / 7e-6, 20 1e-7 / 2e-4, 100 8e-8 / 6e-3, 1000 and more 7e-8 / nothing right.  Up to 4 the plain formula loses less
-// than T^2 2^-24 log 2^20 = 2e-5, and where the two are half a nat apart or more its roundings are little beside the result.
+// (sum p y = 0), U the exponentials of the classes that are not listed.  Nothing in it cancels but U, the difference of E and of the listed ones' sum: both are
+// added up in whole numbers, of the same roundings of the same exponentials, so that a list of all classes leaves exactly 0.  Relative error of the loss of 512
+// fp32 rows of 100 classes, all listed, so / by the plain formula: T = 4 - / 7e-6, 20 1e-7 / 2e-4, 100 8e-8 / 6e-3, 1000 and more 7e-8 / nothing right.  Up to
+// 4 the plain formula loses less than T^2 2^-24 log 2^20 = 2e-5, and where the two are half a nat apart or more its roundings are little beside the result.
 constexpr float kWarm = 4.f;
 struct Warm {
   bool near;                   // less than half a nat apart
@@ -303,8 +303,9 @@ __device__ __forceinline__ void add_chunk(const chunk16& q, float max, float inv
   }
 }
 
-// What follows the sums of such a row, from memory: beside the registers that hold a row there is no room for it.  (us, 4096 bf16 rows of 65536 with lists of 64, which are none of
-// these, at T = 20, so / from the registers 224 / 298, with labels 293 / 378 and at T = 2 254; 64 fp32 rows of 1000, all listed, at T = 20 54, at 2 50)
+// What follows the sums of such a row, from memory: beside the registers that hold a row there is no room for it.  (us, 4096 bf16 rows of 65536 with lists of
+// 64, which are none of these, at T = 20, so / from the registers 224 / 298, with labels 293 / 378 and at T = 2 254; 64 fp32 rows of 1000, all listed, at T =
+// 20 54, at 2 50)
 template <class T, int NT, bool HARD>
 __device__ __forceinline__ void near_row(const DistillArgs& a, int row, const RowChunks<T>& r, const T* z, T* dz, const List& l, const RowSums& t, int label, float z_label,
                                          float inv_rows, WarmShared<NT>& sh) {
@@ -635,11 +636,6 @@ __global__ __launch_bounds__(256) void distill_count_kernel(DistillArgs a, int* 
   if (threadIdx.x == 0) counts[blockIdx.x] = c;
 }
 
-inline size_t al256(size_t b) { return (b + 255) & ~(size_t)255; }
-inline long ceil_div(long a, long b) { return (a + b - 1) / b; }
-
-constexpr int kMostTop = 1024, kMostClasses = 1 << 20, kMostRows = 1 << 20;
-
 struct DistillPlan {
   bool waves;                  // a wave per row, an entry of its list to a lane
   bool one;                    // four rows at most, in one workgroup, with the mean
@@ -653,13 +649,14 @@ DistillPlan distill_plan(int n, int classes, int k, int dtype) {
   DistillPlan p{};
   const int per = dtype == DT_BF16 ? 8 : 4;
   p.chunks = (classes + per - 1) / per + (classes % per ? 1 : 0);      // (a row begins inside one where the rows are not whole ones)
-  // (us, fp32, a wave per row / a workgroup per row: 41 rows of 500 7.8 / 7.7, of 1000 8.5 / 7.5, 1000 of 250 10.8 / 10.7, of 1000 12.6 / 11.4, 2000 of 1000 12.9 / 14.0,
-  // 4096 of 250 12.1 / 18.0, of 1000 16.6 / 20.1; the mean by the same workgroup / by another launch: 1 of 1000 6.3 / 8.3, 4 of 1000 7.7 / 8.4, 16 of 1000 11.6 / 8.6)
+  // (us, fp32, a wave per row / a workgroup per row: 41 rows of 500 7.8 / 7.7, of 1000 8.5 / 7.5, 1000 of 250 10.8 / 10.7, of 1000 12.6 / 11.4, 2000 of 1000
+  // 12.9 / 14.0, 4096 of 250 12.1 / 18.0, of 1000 16.6 / 20.1; the mean by the same workgroup / by another launch: 1 of 1000 6.3 / 8.3, 4 of 1000 7.7 / 8.4, 16
+  // of 1000 11.6 / 8.6)
   p.one = p.chunks <= 64 * 4 && k <= 64 && n <= 4;
   p.waves = p.one || (p.chunks <= (n > 1536 ? 64 * 4 : 64 * 2) && k <= 64);
   p.splits = 1;
-  // more than a workgroup's registers: 64 KiB to a part, 64 parts at most; few long rows: 8 KiB  (us, so / in one piece: 3 bf16 rows of 111759 15 / 33, of 33591 13.0 / 14.7, 32 of 54159
-  // 15.5 / 20.6, 8 fp32 of 10000, which are in one piece, 12.6 / 10.3)
+  // more than a workgroup's registers: 64 KiB to a part, 64 parts at most; few long rows: 8 KiB  (us, so / in one piece: 3 bf16 rows of 111759 15 / 33, of
+  // 33591 13.0 / 14.7, 32 of 54159 15.5 / 20.6, 8 fp32 of 10000, which are in one piece, 12.6 / 10.3)
   const bool few = n <= 32 && p.chunks > 4096;
   if (p.chunks > 1024 * 16 || few) {
     p.splits = few && p.chunks < 64 * 512 ? (int)ceil_div(p.chunks, 512) : few ? 64 : (int)ceil_div(p.chunks, 4112);
@@ -726,7 +723,8 @@ hipError_t distill(const void* z, const int32_t* index, const float* top, const 
   a.alpha = alpha; a.t2 = temperature * temperature;
   a.loss_rows = loss_rows ? loss_rows : (float*)(ws + p.rows);
   a.loss = loss; a.dz = dz; a.n = n; a.classes = classes; a.k = k;
-  a.part = (float*)(ws + p.part); a.at_list = (float*)(ws + p.at_list); a.shares = (unsigned long long*)(ws + p.shares); a.splits = p.splits; a.chunks_per_split = p.chunks_per_split;
+  a.part = (float*)(ws + p.part); a.at_list = (float*)(ws + p.at_list); a.shares = (unsigned long long*)(ws + p.shares);
+  a.splits = p.splits; a.chunks_per_split = p.chunks_per_split;
   if (p.count_parts && (dz || loss)) {
     int* const counts = (int*)(ws + p.counts);
     hipLaunchKernelGGL(distill_count_kernel, dim3((unsigned)p.count_parts), dim3(256), 0, st, a, counts, p.count_each);

@@ -5,6 +5,8 @@
 #include <cstddef>
 #include <cstdint>
 
+#include "sizes.h"
+
 namespace acc {
 
 // Tile `at` of a launch: every XCD takes a contiguous range (neighbours share operand rows in its L2), rows innermost.
@@ -17,10 +19,6 @@ __device__ __forceinline__ TileAt tile_at(int at, int tiles_m, int tiles) {
   const int block = at / (4 * tiles_m), in = at - block * 4 * tiles_m, left = tiles / tiles_m - 4 * block, width = left < 4 ? left : 4, m = in / width;
   return TileAt{m, 4 * block + in - m * width};
 }
-
-inline size_t al256(size_t b) { return (b + 255) & ~(size_t)255; }
-inline long up(long v, long m) { return (v + m - 1) / m * m; }
-inline long ceil_div(long a, long b) { return (a + b - 1) / b; }
 
 // Which tiles: the ones with the smallest predicted time, microseconds, from the tiles of the busiest compute unit and the steps of 64 values of k
 // (times the parts of A).  256 x 256 has a compute unit to itself, of the others two workgroups share one.  Constants from eleven shapes (41 to 8000 rows, widths

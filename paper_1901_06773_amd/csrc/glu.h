@@ -13,9 +13,9 @@ namespace acc {
 enum { GLU_NONE = 0, GLU_RELU = 1, GLU_SILU = 2 };     // as ACC_ACT_*
 
 // act(a) = a s, act'(a) = s (1 + a (1 - s)) with s = 1, s = 1 where a is above 0 and 0 elsewhere (ReLU), or the sigmoid (SiLU): one way for all three.  (A
-// branch for each makes the code of a tile, whose registers are named in it value by value, three times as long.)  Where s is 0 act(a) is 0 whatever a is, minus
-// infinity too, and where it is 1 the slope is 1, so that an infinite gate times 0 makes no NaN.  What else is not finite stays: a NaN in a, and through a
-// closed gate, as 0 times it, b and dh.
+// branch for each makes the code of a tile, whose registers are named in it value by value, three times as long.)  Where s is 0 act(a) is 0 whatever a is,
+// minus infinity too, and where it is 1 the slope is 1, so that an infinite gate times 0 makes no NaN.  What else is not finite stays: a NaN in a, and through
+// a closed gate, as 0 times it, b and dh.
 __device__ __forceinline__ float glu_share(int act, float a) {
   const float s = sigmoid(a), step = a <= 0.f ? 0.f : 1.f;
   return act == GLU_SILU ? s : act == GLU_RELU ? step : 1.f;
@@ -69,8 +69,8 @@ struct GluFinish {
   size_t dx_count, dw_count;
   int dx_splits, dw_splits, db_parts, pitch, half, f;
 };
-// Many parts of db are added up in slabs first, into `slabs` (kDbSlabs rows of `pitch`), which then are its parts (us, dz and db, so / from all parts at once: 10^6 rows of 16 to 2 x 16
-// 145 / 230, 3 10^5 of 32 to 2 x 32 56 / 79, 41379 of 1056 to 2 x 136, 650 parts, 52 / 52)
+// Many parts of db are added up in slabs first, into `slabs` (kDbSlabs rows of `pitch`), which then are its parts (us, dz and db, so / from all parts at once:
+// 10^6 rows of 16 to 2 x 16 145 / 230, 3 10^5 of 32 to 2 x 32 56 / 79, 41379 of 1056 to 2 x 136, 650 parts, 52 / 52)
 constexpr int kDbSlabs = 64, kDbMany = 512;
 hipError_t glu_db_slabs(GluFinish& f, float* slabs, hipStream_t st);
 // the sums of parts, and db unless another launch has it

@@ -8,8 +8,9 @@
 // two products read it.  Few tiles: the projections' sums are cut, and launches that work value by value add the parts and do the rest.
 // Up to three or four rows: every wave takes a few columns and all rows, the layer's weights once through the vector units.
 //
-// fp32, us: 2009 rows, 2048 to 2 x 1365 (22 GFLOP) forward 144, its two launches' sums 134 (168 TFLOP/s) and h 10; all gradients 313 (143 TFLOP/s).  12544 x 1024 x 4096 1037 (203
-// TFLOP/s) and 2624 (160).  Value by value, bf16, kept projections of 12544 rows of 2 x 4096 and dh, to dz in two values: 122 to 125, 5.8 TB/s.
+// fp32, us: 2009 rows, 2048 to 2 x 1365 (22 GFLOP) forward 144, its two launches' sums 134 (168 TFLOP/s) and h 10; all gradients 313 (143 TFLOP/s).  12544 x
+// 1024 x 4096 1037 (203 TFLOP/s) and 2624 (160).  Value by value, bf16, kept projections of 12544 rows of 2 x 4096 and dh, to dz in two values: 122 to 125, 5.8
+// TB/s.
 #include "kernels.h"
 #include "glu.h"
 #include "product32.h"
@@ -58,8 +59,8 @@ template <class T, int V> __device__ __forceinline__ void put(T* p, int left, co
     if (e < left) Elem<T>::store(p + e, v[e]);
 }
 
-// V values from column c on of a row of f, zeros or values of no use behind its end.  The last ones of a row that is no whole number of them are read with their neighbours before
-// them and shifted: one by one, a load waits for the other (22419 rows of kept projections 2 x 1205 to dz in two values 245 us).
+// V values from column c on of a row of f, zeros or values of no use behind its end.  The last ones of a row that is no whole number of them are read with
+// their neighbours before them and shifted: one by one, a load waits for the other (22419 rows of kept projections 2 x 1205 to dz in two values 245 us).
 template <class T, int V> __device__ __forceinline__ void get_row(const T* row, int c, int f, float (&v)[V]) {
   if (f < V) return get<T, V>(row + c, f - c, v);
   const int over = c - min(c, f - V);
@@ -192,7 +193,8 @@ template <class T> __device__ __forceinline__ void join_many(const float* __rest
   __syncthreads();
   if (threadIdx.x < 64 && i < count) Elem<T>::store(out + i, ((s + sh[threadIdx.x + 64]) + sh[threadIdx.x + 128]) + sh[threadIdx.x + 192]);
 }
-// (us, all gradients, fp32, so / a value to a thread: 196 x 512 x 1024, some eight parts, 36 / 41, 48 x 456 23 / 28; more values 777 x 1160 118 / 114, 1000 x 512 51 / 48)
+// (us, all gradients, fp32, so / a value to a thread: 196 x 512 x 1024, some eight parts, 36 / 41, 48 x 456 23 / 28; more values 777 x 1160 118 / 114, 1000 x
+// 512 51 / 48)
 inline bool many_parts(size_t count, int splits) { return splits >= 16 ? count <= 1u << 20 : splits >= 4 && count <= 1u << 18; }
 template <class T>
 __global__ __launch_bounds__(256) void glu_finish_kernel(GluFinish f, unsigned dx_blocks, unsigned dw_blocks, int many) {
@@ -221,9 +223,9 @@ __global__ __launch_bounds__(256) void glu_db_slabs_kernel(const float* __restri
   if (threadIdx.x < 64 && j < pitch) slabs[(size_t)slab * pitch + j] = (float)(((s + sh[threadIdx.x + 64]) + sh[threadIdx.x + 128]) + sh[threadIdx.x + 192]);
 }
 
-// ---------------------------------------------------------------------------------- few rows
-// R rows: a wave's columns one after the other, sixteen bytes of gate and value rows of w to a lane, all rows of x against them.  (All loads of four steps are on their
-// way at once: with a test of the row's end around each, 4 rows of 2048 to 2 x 8192 took 30 us in place of 16.)
+// ---------------------------------------------------------------------------------- few rows R rows: a wave's columns one after the other, sixteen bytes of
+// gate and value rows of w to a lane, all rows of x against them.  (All loads of four steps are on their way at once: with a test of the row's end around each,
+// 4 rows of 2048 to 2 x 8192 took 30 us in place of 16.)
 template <class T, int R>
 __global__ __launch_bounds__(256) void glu_few_kernel(const T* __restrict__ x, const T* __restrict__ w, const float* __restrict__ bias, T* __restrict__ h,
                                                       T* __restrict__ ab, int d, int f, int act) {
@@ -269,8 +271,8 @@ __global__ __launch_bounds__(256) void glu_few_kernel(const T* __restrict__ x, c
       }
   }
 }
-// (us, so / by tiles: 1 row of 512 to 2 x 2048 bf16 3.9 / 5.8, fp32 3.8 / 8.4; 4 rows, bf16, 1024 to 2 x 4096 5.6 / 7.5, 2048 to 2 x 8192 16.0 / 12.8; 3 rows of that 13.1 /
-// 12.9; 4 rows of it in fp32 22 / 27; 1 row of 4096 to 2 x 11008 26.7 / 27.9, which is 6.8 TB/s of weights that the caches hold.)
+// (us, so / by tiles: 1 row of 512 to 2 x 2048 bf16 3.9 / 5.8, fp32 3.8 / 8.4; 4 rows, bf16, 1024 to 2 x 4096 5.6 / 7.5, 2048 to 2 x 8192 16.0 / 12.8; 3 rows
+// of that 13.1 / 12.9; 4 rows of it in fp32 22 / 27; 1 row of 4096 to 2 x 11008 26.7 / 27.9, which is 6.8 TB/s of weights that the caches hold.)
 inline bool few_rows(int rows, int d, int f, int dtype) { return rows <= 3 || (rows == 4 && (dtype == DT_F32 || (long)d * f <= 1L << 23)); }
 template <class T> hipError_t glu_few(const GluArgs& a) {
   const long blocks = ceil_div(a.f, 4);
@@ -393,7 +395,8 @@ GluPlan32 glu_plan32(int rows, int d, int f, bool backward, bool kept) {
   const Cut whole = cut32(rows, wide, d, 0);
   p.tile = whole.tile;
   p.proj = cut32(rows, wide, d, 1L << 24);
-  p.cut = !kept && p.proj.splits > 1 && p.proj.us + 3.0 < whole.us;      // (us, so / whole: forward 64 x 2048 x 512 12 / 51, 300 x 1024 x 64 9.5 / 26.8, 196 x 512 x 1024 14 / 15)
+  // (us, so / whole: forward 64 x 2048 x 512 12 / 51, 300 x 1024 x 64 9.5 / 26.8, 196 x 512 x 1024 14 / 15)
+  p.cut = !kept && p.proj.splits > 1 && p.proj.us + 3.0 < whole.us;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t a = at; at += al256(bytes); return a; };
   p.sums = take(p.cut ? (size_t)p.proj.splits * rows * wide * 4 : 0);
@@ -494,8 +497,8 @@ bool glu_ok(int rows, int d, int f, int dtype) {
 
 int glu_point_shape(PointArgs& a, int dtype) {
   const int v = dtype == DT_BF16 ? 8 : 4, chunks = (a.f + v - 1) / v;
-  // The fewest workgroups across that leave the fewest threads without work, three more than needed at most.  (us, so / the fewest: 22419 bf16 rows of 2 x 1205 71 / 126, 20000 of
-  // 2 x 1200 56 / 76, of 2 x 2600 125 / 140)
+  // The fewest workgroups across that leave the fewest threads without work, three more than needed at most.  (us, so / the fewest: 22419 bf16 rows of 2 x 1205
+  // 71 / 126, 20000 of 2 x 1200 56 / 76, of 2 x 2600 125 / 140)
   const int least = (int)ceil_div(chunks, 256);
   int most = 0;
   for (int across = least; across <= least + 3 && across <= chunks; ++across) {

@@ -1,20 +1,22 @@
 // The products of the gated layer (glu.hip) for bf16 operands, on the bf16 matrix cores.
 //
 // Gate and value of the same columns are products of one tile (GemmCfg's PAIR): they meet in the same registers, where h = act(a) b, or in the backward pass,
-// which works them out again, their gradients da and db, leaves them.  Those are [rows][2 f] = dz, and the rest is that of a linear layer: dx = dz w, dw = dz^T x.
+// which works them out again, their gradients da and db, leaves them.  Those are [rows][2 f] = dz, and the rest is that of a linear layer: dx = dz w, dw = dz^T
+// x.
 //
-// dz is kept as the sum of bf16 values, the first the nearest one, the next the nearest to what is left (relative errors of 2^-8, 2^-16, 2^-24).  dx, rounded to
-// bf16 itself, is multiplied from two: one would do if its errors stayed beside the result's own rounding, but where a row of dh sums to zero, as in front of a
-// normalisation, and the values are alike, what the gates' weights have in common cancels in dx and its errors do not (relative error of dx, 300 x 128 x 64, a common
-// part of 10 and 30 times the weights' spread: one value 0.014 and 0.021, two 0.0017, which is the rounding of the result; nothing in common: 0.0023 and 0.0017;
-// 12544 rows, 1024 to 2 x 4096, all gradients of kept projections 672 and 810 us).  dw, an fp32 result, is multiplied from three, from 10240 rows on from two,
-// whose errors are there at most 1.4 times those of a sum of so many terms in fp32.  Relative error of dw, 1e-7, two / three / all in fp32: 64 rows 24 / 1.1 / 1.5, 1500 24 / 1.7 / 7.0,
-// 4096 25 / 5.4 / 11.8, 8192 25 / 7.3 / 16.5, 10000 25 / 8.0 / 18.1, 12544 26 / - / 20, 16384 26 / - / 23, 32768 25 / - / 32; all gradients of kept projections of 4096 rows, 512 wide,
-// 2 x 1024, 65 / 76 us, of 8192, 2 x 2048, 235 / 269.
+// dz is kept as the sum of bf16 values, the first the nearest one, the next the nearest to what is left (relative errors of 2^-8, 2^-16, 2^-24).  dx, rounded
+// to bf16 itself, is multiplied from two: one would do if its errors stayed beside the result's own rounding, but where a row of dh sums to zero, as in front
+// of a normalisation, and the values are alike, what the gates' weights have in common cancels in dx and its errors do not (relative error of dx, 300 x 128 x
+// 64, a common part of 10 and 30 times the weights' spread: one value 0.014 and 0.021, two 0.0017, which is the rounding of the result; nothing in common:
+// 0.0023 and 0.0017; 12544 rows, 1024 to 2 x 4096, all gradients of kept projections 672 and 810 us).  dw, an fp32 result, is multiplied from three, from 10240
+// rows on from two, whose errors are there at most 1.4 times those of a sum of so many terms in fp32.  Relative error of dw, 1e-7, two / three / all in fp32:
+// 64 rows 24 / 1.1 / 1.5, 1500 24 / 1.7 / 7.0, 4096 25 / 5.4 / 11.8, 8192 25 / 7.3 / 16.5, 10000 25 / 8.0 / 18.1, 12544 26 / - / 20, 16384 26 / - / 23, 32768
+// 25 / - / 32; all gradients of kept projections of 4096 rows, 512 wide, 2 x 1024, 65 / 76 us, of 8192, 2 x 2048, 235 / 269.
 //
-// All bound by the matrix cores but for the smallest, which are launches behind each other.  12544 rows, 1024 to 2 x 4096 (210 GFLOP a product), us: forward 204 (1030 TFLOP/s; 218 where the
-// projections are kept), dz from the projections worked out again 320 (660: behind each tile's sums the gradients of its 65536 values, which no other workgroup covers), dx from two
-// values 350 (1200 TFLOP/s of both), dw from two values 300-315 (1370).  A library's product of these sizes alone takes 141 to 175.
+// All bound by the matrix cores but for the smallest, which are launches behind each other.  12544 rows, 1024 to 2 x 4096 (210 GFLOP a product), us: forward
+// 204 (1030 TFLOP/s; 218 where the projections are kept), dz from the projections worked out again 320 (660: behind each tile's sums the gradients of its 65536
+// values, which no other workgroup covers), dx from two values 350 (1200 TFLOP/s of both), dw from two values 300-315 (1370).  A library's product of these
+// sizes alone takes 141 to 175.
 #include "glu.h"
 
 #include "gemm_bf16.h"
@@ -61,8 +63,8 @@ template <int COLS_> struct Stage {
       if (r < rows && c + 8 <= left) *reinterpret_cast<any*>(to + ((uint32_t)r * (uint32_t)pitch + (uint32_t)c)) = any{v[it].x, v[it].y, v[it].z, v[it].w};
     }
   }
-  // Rows of eight values or more: the last eight end with the row and are shifted, zeros behind them.  What lies outside is read from the last row and column that exist and
-  // dropped: a branch around a load, with all accumulators alive, made the compiler spill some of them.
+  // Rows of eight values or more: the last eight end with the row and are shifted, zeros behind them.  What lies outside is read from the last row and column
+  // that exist and dropped: a branch around a load, with all accumulators alive, made the compiler spill some of them.
   __device__ __forceinline__ void in(const bf16_t* from, int pitch, int rows, int left) {
     const int lane = threadIdx.x & 63, c = 8 * (lane % PER), over = c + 8 > left ? c + 8 - left : 0;
 #pragma unroll
@@ -464,8 +466,8 @@ __global__ __launch_bounds__(256, 2) void glu_grads_kernel(ProductArgs x, GluDwA
   }
 }
 
-// out[r][0 .. pitch) = in[r][0 .. cols), then zeros; of 2 * split_row rows the second half goes to row r + gap, the `gap` rows before it and behind it are zero.  Eight
-// values per thread, read at any address.
+// out[r][0 .. pitch) = in[r][0 .. cols), then zeros; of 2 * split_row rows the second half goes to row r + gap, the `gap` rows before it and behind it are
+// zero.  Eight values per thread, read at any address.
 __global__ __launch_bounds__(256) void glu_pad_kernel(const bf16_t* __restrict__ in, bf16_t* __restrict__ out, size_t eights, int cols, int pitch, int split_row, int gap) {
   typedef uint32_t any __attribute__((ext_vector_type(4), aligned(2)));
   const size_t across = pitch / 8;
@@ -507,7 +509,8 @@ typedef GemmCfg<2, 4, 4, 2, 32, 2, true, true, 3, false> V256;             // dw
 typedef GemmCfg<2, 2, 2, 2, 32, 2, true, true, 3, false> V128;
 typedef GemmCfg<2, 2, 1, 1, 32, 3, true, true, 3, false> V64;
 
-// Which tile of gate and value, by predicted time as in gemm_tiles.h.  Constants from sixty sizes (rows 32 to 30000, widths 32 to 4096 and 6000), every tile on each.
+// Which tile of gate and value, by predicted time as in gemm_tiles.h.  Constants from sixty sizes (rows 32 to 30000, widths 32 to 4096 and 6000), every tile on
+// each.
 struct PairTile {
   int m, n, db_rows;           // n: columns of both together; rows of a wave
   bool alone;                  // one workgroup a compute unit
@@ -517,8 +520,8 @@ constexpr PairTile kPair[4] = {{256, 256, 64, true, {{6.0, 1.2, 7.7, 1.86}, {22.
                                {256, 128, 128, false, {{4.0, 1.2, 4.0, 1.0}, {14.5, 1.2, 10.9, 0.92}}},
                                {128, 128, 64, false, {{0.1, 0.79, 2.2, 0.5}, {9.9, 0.84, 7.4, 0.5}}},
                                {64, 64, 32, false, {{1.3, 0.24, 0.85, 0.225}, {5.6, 0.42, 1.8, 0.12}}}};
-// Tiles in one piece, forward: those of whole rounds of the compute units, where what is left is half a round at most.  us, without quarters / with: 12544 rows,
-// 1024 to 2 x 4096 (6.1 rounds) 219 / 206, 8449, 1024 to 2 x 1040 (1.2) 52 / 43, 4161, 1536 to 2 x 2200 (1.2) 73 / 60.
+// Tiles in one piece, forward: those of whole rounds of the compute units, where what is left is half a round at most.  us, without quarters / with: 12544
+// rows, 1024 to 2 x 4096 (6.1 rounds) 219 / 206, 8449, 1024 to 2 x 1040 (1.2) 52 / 43, 4161, 1536 to 2 x 2200 (1.2) 73 / 60.
 long pair_whole(const PairTile& t, long tiles) {
   const long rest = tiles % 256;
   return t.alone && tiles > 256 && rest <= 128 ? tiles - rest : tiles;
@@ -561,7 +564,8 @@ GluPlan16 glu_plan16(int rows, int d, int f, bool backward, bool kept) {
     const double v = pair_us(t, backward, ceil_div(rows, t.m) * ceil_div(p.fp, t.n / 2), p.dp / 64.0);
     if (us == 0 || v < us) { us = v; p.tile = t; }
   }
-  // few tiles of a long sum: parts of it, whose sums a second launch adds up (us, so / whole: forward 64 x 4096 x 1024 13.3 / 18.7, 1000 x 4096 x 64 12.6 / 18.9; backward 43 / 49, 32 / 40)
+  // few tiles of a long sum: parts of it, whose sums a second launch adds up (us, so / whole: forward 64 x 4096 x 1024 13.3 / 18.7, 1000 x 4096 x 64 12.6 /
+  // 18.9; backward 43 / 49, 32 / 40)
   p.proj = choose(RowsByRows, rows, wide, p.dp, 1, 1L << 24, p.dp > 2048 ? up(ceil_div(p.dp, 16), 64) : 128, 1);       // (sixteen parts at most)
   // (and rows of fewer than eight values, which the pair's tiles do not read)
   p.cut = !kept && ((p.proj.splits > 1 && p.proj.us + (backward ? 7.0 : 2.0) < us) || f < 8);
@@ -581,8 +585,9 @@ GluPlan16 glu_plan16(int rows, int d, int f, bool backward, bool kept) {
     const Choice x1 = choose(ByColumns, rows, d, wide, 2, 0, 256, 2), w1 = choose(ByColumns, wide, d, rows, p.parts, 0, 128, 2);
     const bool sums = !(x1.us < dx.us + kSaved && w1.us < dw.us + kSaved);
     const Choice &cx = sums ? dx : x1, &cw = sums ? dw : w1;
-    // Up to 1024 workgroups, or 2048 of few steps: 64 x 64 tiles take twice the LDS reads of larger ones.  (us, all gradients of kept projections, so / each for itself:
-    // 196 x 512 x 1024 18.0 / 22.6, 4096 x 512 x 1024 76 / 79, 3867 x 304 x 1936 121 / 130, 5000 x 768 x 1024 125 / 107, 10000 x 512 x 1024 185 / 192, 8192 x 512 x 2048 334 / 269)
+    // Up to 1024 workgroups, or 2048 of few steps: 64 x 64 tiles take twice the LDS reads of larger ones.  (us, all gradients of kept projections, so / each
+    // for itself: 196 x 512 x 1024 18.0 / 22.6, 4096 x 512 x 1024 76 / 79, 3867 x 304 x 1936 121 / 130, 5000 x 768 x 1024 125 / 107, 10000 x 512 x 1024 185 /
+    // 192, 8192 x 512 x 2048 334 / 269)
     const long workgroups = tx * cx.splits + tw * cw.splits, steps = tx * ceil_div(wide, 64) * 2 + tw * ceil_div(rows, 64) * p.parts;
     p.together = workgroups <= 1024 || (workgroups <= 2048 && steps <= 420 * 256);
     if (p.together) { p.dx = cx; p.dw = cw; }

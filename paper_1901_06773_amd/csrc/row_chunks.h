@@ -11,8 +11,12 @@
 #include <type_traits>
 
 #include "dtype.h"
+#include "sizes.h"
 
 namespace acc {
+
+// of the top logits and of the distillation from them: entries of a list, classes, rows
+constexpr int kMostTop = 1024, kMostClasses = 1 << 20, kMostRows = 1 << 20;
 
 typedef unsigned chunk16 __attribute__((ext_vector_type(4)));
 

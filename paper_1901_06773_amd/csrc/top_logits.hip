@@ -7,8 +7,8 @@
 // time, and then the column up to which equal ones are taken.  Rows that no workgroup's registers hold are cut into segments
 // whose lists are rows of a second launch.
 //
-// Bound by reading the rows: 4096 bf16 rows of 65536, k = 64, 128 us (4.2 TB/s; two workgroups of a compute unit cover each other's barriers), of fp32 260.  Short rows and
-// long lists by the steps of a row behind each other: 4096 rows of 8192 30 us (2.2 TB/s), k = 150 47; a few rows of any width 6 to 15.
+// Bound by reading the rows: 4096 bf16 rows of 65536, k = 64, 128 us (4.2 TB/s; two workgroups of a compute unit cover each other's barriers), of fp32 260.
+// Short rows and long lists by the steps of a row behind each other: 4096 rows of 8192 30 us (2.2 TB/s), k = 150 47; a few rows of any width 6 to 15.
 #include "kernels.h"
 #include "row_chunks.h"
 
@@ -197,8 +197,8 @@ __global__ __launch_bounds__(NT, CH == 8 ? 8 : 4) void top_kernel(TopArgs a) {
   int size = 1;
   while (size < found) size *= 2;
   // Few: each is compared with all others, by as many threads as there are for it; its rank is its place.  More: sorted, largest first, in steps with a barrier
-  // each.  (us, ranks / sorted: 4096 bf16 rows of 65536, k = 64 (some 70 found) 128 / 156, 64 fp32 rows of 1000 and k = 100 6.5 / 9.9, 4096 bf16 rows of 8192 and k = 150 (some
-  // 200 found, 256 threads) 54 / 47.)
+  // each.  (us, ranks / sorted: 4096 bf16 rows of 65536, k = 64 (some 70 found) 128 / 156, 64 fp32 rows of 1000 and k = 100 6.5 / 9.9, 4096 bf16 rows of 8192
+  // and k = 150 (some 200 found, 256 threads) 54 / 47.)
   if (size <= NT && found * size <= 160 * NT) {
     const int per = NT / size, i = tid / per, part = tid % per;
     const unsigned long long c = i < found ? cand[i] : 0;
@@ -229,11 +229,6 @@ __global__ __launch_bounds__(NT, CH == 8 ? 8 : 4) void top_kernel(TopArgs a) {
   for (int i = tid; i < want; i += NT) give(i, cand[i]);
 }
 
-inline size_t al256(size_t b) { return (b + 255) & ~(size_t)255; }
-inline long ceil_div(long a, long b) { return (a + b - 1) / b; }
-
-constexpr int kMostTop = 1024, kMostClasses = 1 << 20, kMostRows = 1 << 20;
-
 struct TopPlan {
   int segment, segments;
   size_t top, total;           // offsets in the workspace: columns, values
@@ -256,11 +251,11 @@ template <class T> hipError_t launch_top(const TopArgs& a, hipStream_t st) {
   const int chunks = (a.segment + PER - 1) / PER + (a.classes % PER ? 1 : 0);
   const dim3 grid((unsigned)(a.n * a.segments));
   // The smallest workgroup that holds a row, of which all values fit LDS or the bound leaves out most: with k as many as three quarters of the groups it still
-  // leaves out half.  (us, so / the smallest that holds the row: 1000 rows of 1306 bf16 logits, k = 118, 12.5 / 85, 1000 of 6000 fp32, k = 300, 23 / 217.)  Four groups a thread where
-  // k asks for them (so / with one group): 64 fp32 rows of 50000, k = 1000, 43 / 429, 5072 of 200, k = 40, by a wave 7.2 / 16, 5072 bf16 of 2000, k = 200, by 256 threads 46 / 271; a wave
-  // with them or 256 threads without: 5072 fp32 rows of 259, k = 125, 15 / 28, 12 bf16 rows of 1000, k = 50, 7.0 / 5.6.  A chunk a thread or eight, whose
-  // registers leave two workgroups of 1024 threads to a compute unit, and sixteen: with
-  // four (4096 bf16 rows of 8192, k = 64, 43 / 31) the compiler takes half as many registers more.
+  // leaves out half.  (us, so / the smallest that holds the row: 1000 rows of 1306 bf16 logits, k = 118, 12.5 / 85, 1000 of 6000 fp32, k = 300, 23 / 217.)
+  // Four groups a thread where k asks for them (so / with one group): 64 fp32 rows of 50000, k = 1000, 43 / 429, 5072 of 200, k = 40, by a wave 7.2 / 16, 5072
+  // bf16 of 2000, k = 200, by 256 threads 46 / 271; a wave with them or 256 threads without: 5072 fp32 rows of 259, k = 125, 15 / 28, 12 bf16 rows of 1000, k =
+  // 50, 7.0 / 5.6.  A chunk a thread or eight, whose registers leave two workgroups of 1024 threads to a compute unit, and sixteen: with four (4096 bf16 rows
+  // of 8192, k = 64, 43 / 31) the compiler takes half as many registers more.
 #define ACC_TOP(NT, CH, G, rule)                                                                                 \
   {                                                                                                              \
     const bool bounded = 4 * a.k <= 3 * G * (chunks < NT ? chunks : NT), all = a.segment <= (NT < 1024 ? 2 * NT : 4096); \

@@ -1,6 +1,6 @@
-"""Distillation by every kind of launch that its rules choose from: a wave per row of one, two and four chunks, alone and in one workgroup, a workgroup per row of each size, rows that are cut
-where there are few of them and where there are many; and the second launch of the top logits of cut rows by each size of workgroup.  At temperatures on both sides of
-the one that divides the ways.  Tolerances are those of test_gpu_distill.py."""
+"""Distillation by every kind of launch that its rules choose from: a wave per row of one, two and four chunks, alone and in one workgroup, a workgroup per row
+of each size, rows that are cut where there are few of them and where there are many; and the second launch of the top logits of cut rows by each size of
+workgroup.  At temperatures on both sides of the one that divides the ways.  Tolerances are those of test_gpu_distill.py."""
 import pytest
 import torch
 

@@ -3,10 +3,12 @@
 With x_j = (t_j - t_max) - (z_j - z_max) of a list that holds every class, p its probabilities and x' what lies about the mean of x, T^2 KL is
 T^2 log sum p e^(-x' / T) = sum p x'^2 / 2 (1 + O(x' / T)) and T (q - p) is T p (e^(-x' / T - KL) - 1).
 
-Tolerances.  Four roundings of 2^-24 of the logits' range R leave x' off by 2^-22 R.  A probability is known to 2^-20 of itself (exponents below 16: 16 roundings of 2^-24 of
-one, and a few of the sum and the quotient), and so is what is left to the unlisted classes.  So T^2 KL is off by sum p |x'| 2^-22 R <= 2^-22 R (2 T^2 KL)^(1/2), doubled for the
-higher terms, and 2^-18 of itself; T (q - p) by 2^-21 R and 2^-18 of T (q - p) / p times the larger of p and q; a bf16 result by its own rounding, 2^-8 of it, besides.
-Where T is 10^5 or more 64 bits hold less of the definition than these, and its limit takes its place, off by |x'| / T <= 2^-10 of itself at 10^5, by less than 2^-24 from 10^9 on."""
+Tolerances.  Four roundings of 2^-24 of the logits' range R leave x' off by 2^-22 R.  A probability is known to 2^-20 of itself (exponents below 16: 16
+roundings of 2^-24 of one, and a few of the sum and the quotient), and so is what is left to the unlisted classes.  So T^2 KL is off by sum p |x'| 2^-22 R <=
+2^-22 R (2 T^2 KL)^(1/2), doubled for the higher terms, and 2^-18 of itself; T (q - p) by 2^-21 R and 2^-18 of T (q - p) / p times the larger of p and q; a bf16
+result by its own rounding, 2^-8 of it, besides.
+
+The reference, in 64 bits, works by differences, too; at the highest temperatures the limit, half the variance of x, stands beside it."""
 import pytest
 import torch
 

@@ -1,7 +1,7 @@
 """How many bits the gradients of the gated layer keep, against 64 bits, where fewer would show.
 
-Tolerances.  A value held as the sum of two bf16 values is off by 2^-16 of itself at most, of three by 2^-24; a result rounded to bf16 by 2^-8 of itself.  Projections and
-sums add 1e-5 of the magnitudes that are summed (test_gpu_glu.py)."""
+Tolerances.  A value held as the sum of two bf16 values is off by 2^-16 of itself at most, of three by 2^-24; a result rounded to bf16 by 2^-8 of itself.
+Projections and sums add 1e-5 of the magnitudes that are summed (test_gpu_glu.py)."""
 import pytest
 import torch
 
@@ -55,8 +55,9 @@ def test_what_the_weights_have_in_common_cancels_in_dx(rows, d, f, common, kept)
 @pytest.mark.parametrize("rows", [1000, 4095, 4096, 6000, 8192, 10239])
 @pytest.mark.parametrize("d,f", [(64, 40), (256, 136), (512, 1024)])
 def test_dw_keeps_the_digits_of_a_sum_in_fp32(rows, d, f):
-    # The running sum of n terms at random is on average n / 2 terms' squares; rounded by 2^-24 of itself at most each time that a product of sixteen terms of one of three
-    # values is added, 3 n / 16 times, it is off by (3 n / 32)^(1/2) 2^-24 of the result, as norms.  dz of kept projections is off by a few roundings of 2^-24 and the activation's 2^-22: 4e-7.
+    # The running sum of n terms at random is on average n / 2 terms' squares; rounded by 2^-24 of itself at most each time that a product of sixteen terms of
+    # one of three values is added, 3 n / 16 times, it is off by (3 n / 32)^(1/2) 2^-24 of the result, as norms.  dz of kept projections is off by a few
+    # roundings of 2^-24 and the activation's 2^-22: 4e-7.
     g = torch.Generator(device="cuda").manual_seed(rows + d)
 
     def r(*s):

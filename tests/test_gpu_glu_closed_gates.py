@@ -1,5 +1,5 @@
-"""Gradients and values that are not finite at gates that are closed (ReLU at or below 0, SiLU where the sigmoid is 0 in fp32): db = dh act(a) and da = dh b act'(a) are 0
-times them, which is no number.  What they do not enter keeps its bits.  A gate of minus infinity is closed like any other."""
+"""Gradients and values that are not finite at gates that are closed (ReLU at or below 0, SiLU where the sigmoid is 0 in fp32): db = dh act(a) and da = dh b
+act'(a) are 0 times them, which is no number.  What they do not enter keeps its bits.  A gate of minus infinity is closed like any other."""
 import pytest
 import torch
 

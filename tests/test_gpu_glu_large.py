@@ -1,5 +1,5 @@
-"""The gated layer at its largest: fp32 tensors beyond 4 GiB, and weights of nearly 2^30 values a side, which is the limit, in both types.  As norms, which test_gpu_glu.py holds
-to 2e-5, results in bf16 to their rounding of 2^-8 and dw of bf16 operands to 2^-16 besides."""
+"""The gated layer at its largest: fp32 tensors beyond 4 GiB, and weights of nearly 2^30 values a side, which is the limit, in both types.  As norms, which
+test_gpu_glu.py holds to 2e-5, results in bf16 to their rounding of 2^-8 and dw of bf16 operands to 2^-16 besides."""
 import pytest
 import torch
 

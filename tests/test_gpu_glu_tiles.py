@@ -1,11 +1,13 @@
-"""The gated layer at sizes that between them are multiplied by every kind of tile that its rules choose from, with sums whole and in parts, on both sides of 10240 rows;
-none of them fills its tiles.  Tolerances are those of test_gpu_glu.py; a sum, or a part of one that is cut, has up to 31000 terms, which the matrix cores add up by four or more: it is off
-by fewer than 2^-24 (2 (n / 4)^(1/2) + 8) = 1.1e-5 of the sum of their sizes where roundings are at random, of which those sums of terms of both signs use a small part.
+"""The gated layer at sizes that between them are multiplied by every kind of tile that its rules choose from, with sums whole and in parts, on both sides of
+10240 rows; none of them fills its tiles.  Tolerances are those of test_gpu_glu.py; a sum, or a part of one that is cut, has up to 31000 terms, which the matrix
+cores add up by four or more: it is off by fewer than 2^-24 (2 (n / 4)^(1/2) + 8) = 1.1e-5 of the sum of their sizes where roundings are at random, of which
+those sums of terms of both signs use a small part.
 
-Gradients of a ReLU whose gates are worked out again are held, as norms, to more than the 2e-5 of the others.  A gate of spread 1, the sum of d products that are added sixteen at a
-time, is rounded d / 16 times by 2^-24 of about one at most: off by e = 2^-24 d^(1/2) / 4.  So of all gates, whose density at 0 is 0.4, a share of 0.4 e = 2^-24 d^(1/2) / 10 = s is on the other
-side of 0 than it should be, and takes or leaves out a whole term da beside the half that are open: (2 s)^(1/2) of the norm of the gradients at the gates (3.7e-4 at
-d = 137, where one gate alone of 10787 x 2317 is 2.8e-4).  Twice that, for the few that they are.  Values by themselves are held as ever: near 0 the slope is either."""
+Gradients of a ReLU whose gates are worked out again are held, as norms, to more than the 2e-5 of the others.  A gate of spread 1, the sum of d products that
+are added sixteen at a time, is rounded d / 16 times by 2^-24 of about one at most: off by e = 2^-24 d^(1/2) / 4.  So of all gates, whose density at 0 is 0.4, a
+share of 0.4 e = 2^-24 d^(1/2) / 10 = s is on the other side of 0 than it should be, and takes or leaves out a whole term da beside the half that are open: (2
+s)^(1/2) of the norm of the gradients at the gates (3.7e-4 at d = 137, where one gate alone of 10787 x 2317 is 2.8e-4).  Twice that, for the few that they are.
+Values by themselves are held as ever: near 0 the slope is either."""
 import pytest
 import torch
 

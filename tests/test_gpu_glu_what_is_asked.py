@@ -1,5 +1,5 @@
-"""The gated layer's backward pass writes no more of [da | db] than what is asked for is multiplied from: in bf16 three values of it for dw of fewer than 10240 rows, two for dw of
-more and for dx, none for dbias; in fp32 the one for dx and dw, none for dbias.  What is written is seen in a workspace full of one byte."""
+"""The gated layer's backward pass writes no more of [da | db] than what is asked for is multiplied from: in bf16 three values of it for dw of fewer than 10240
+rows, two for dw of more and for dx, none for dbias; in fp32 the one for dx and dw, none for dbias.  What is written is seen in a workspace full of one byte."""
 import pytest
 import torch
 
