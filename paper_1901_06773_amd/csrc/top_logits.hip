@@ -7,8 +7,10 @@
 // time, and then the column up to which equal ones are taken.  Rows that no workgroup's registers hold are cut into segments
 // whose lists are rows of a second launch.
 //
-// Bound by reading the rows: 4096 bf16 rows of 65536, k = 64, 128 us (4.2 TB/s; two workgroups of a compute unit cover each other's barriers), of fp32 260.
-// Short rows and long lists by the steps of a row behind each other: 4096 rows of 8192 30 us (2.2 TB/s), k = 150 47; a few rows of any width 6 to 15.
+// Bound by reading the rows: 4096 bf16 rows of 65536, k = 64, 128 us (4.2 TB/s; two workgroups of a compute unit cover each other's barriers), of fp32 230 to
+// 260.  Short rows and long lists by the steps of a row behind each other: 4096 rows of 8192 30 us (2.2 TB/s), k = 150 47; a few rows of any width 6 to 15.
+// Rows with more equal values at the k-th than LDS has room for take some fifty sweeps from the caches: of one value throughout, 4096 bf16 rows of 65536 5400
+// us, fp32 7200, 4096 bf16 rows of 8192 630, 64 fp32 rows of 1000, k = 16, 79 (others 5.4); of logits rounded to whole numbers, of which few are the largest, 162.
 #include "kernels.h"
 #include "row_chunks.h"
 
