@@ -9,7 +9,7 @@
 // Up to three or four rows: every wave takes a few columns and all rows, the layer's weights once through the vector units.
 //
 // fp32, us: 2009 rows, 2048 to 2 x 1365 (22 GFLOP) forward 144, its two launches' sums 134 (168 TFLOP/s) and h 10; all gradients 313 (143 TFLOP/s).  12544 x
-// 1024 x 4096 1037 (203 TFLOP/s) and 2624 (160).  Value by value, bf16, kept projections of 12544 rows of 2 x 4096 and dh, to dz in two values: 122 to 125, 5.8
+// 1024 x 4096 1037 (203 TFLOP/s) and 2624 (160).  Value by value, bf16, kept projections of 12544 rows of 2 x 4096 and dh, to dz in two values: 112, 6.4
 // TB/s.
 #include "kernels.h"
 #include "glu.h"
