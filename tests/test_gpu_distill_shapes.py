@@ -44,3 +44,17 @@ def test_rows_that_do_not_count(n, classes, k, dtype):
 def test_top_logits_of_cut_rows(n, classes, k, dtype):
     check(logits(n, classes, dtype), k)
     check((2 * logits(n, classes, dtype)).round(), k)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,classes,k", [(1 << 20, 3, 2), (70001, 40, 5), (300000, 130, 100)])
+def test_top_logits_of_many_rows(n, classes, k, dtype):
+    check(logits(n, classes, dtype), k)
+    check((2 * logits(n, classes, dtype)).round(), k)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,classes,k", [(1 << 20, 3, 2), (70001, 40, 40)])
+def test_many_rows_at_a_high_temperature(n, classes, k, dtype):
+    x = inputs(n, classes, k, dtype, labels=True)
+    agree(call(*x, 8.0, 0.5), reference(*x, 8.0, 0.5), dtype)

@@ -62,3 +62,28 @@ def test_the_largest_weights(d, f, dtype, rows):
         near(got["dw"][c:c + 4096], dz[:, c:c + 4096].T @ x.double(), 2.0 ** -16 + 2e-5, "dw")
     del got
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d,f", [(8, 8), (3, 9), (1, 2)])
+def test_the_most_rows(d, f, dtype):
+    # dh is 0 but in a few thousand rows: gradients' sums over all of them are no longer than those that test_gpu_glu.py holds
+    rows = 1 << 24
+    x, w, b, dh = inputs(rows, d, f, dtype)
+    h, ab = forward(x, w, b, "silu", dtype)
+    at = torch.cat([torch.arange(1500, device="cuda"), torch.arange(rows - 1500, rows, device="cuda"), torch.arange(0, rows, 1 << 13, device="cuda")]).unique()
+    p, _ = projections(x[at], w, b)
+    a, v = p.chunk(2, 1)
+    value, slope = curve(a, "silu")
+    half = 2.0 ** -8 if dtype == "bf16" else 0
+    near(h[at], value * v, half + 2e-5, "h")
+    near(ab[at], p, half + 2e-5, "ab")
+    assert torch.isfinite(h).all()
+    only = torch.zeros_like(dh)
+    only[at] = dh[at]
+    dz = torch.cat([dh[at].double() * v * slope, dh[at].double() * value], 1)
+    got = backward(x, w, b, None, only, "silu", dtype)
+    near(got["dx"][at], dz @ w.double(), half + 2e-5, "dx")
+    near(got["dw"], dz.T @ x[at].double(), 2.0 ** -16 + 2e-5, "dw")
+    near(got["db"], dz.sum(0), 1e-4, "db")
+    assert int((got["dx"] != 0).any(1).sum()) <= len(at)
